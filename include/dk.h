@@ -391,6 +391,107 @@ DK_API dk_status dk_relu_pool_fwd(dk_ctx* ctx, const float* x, int64_t n, int32_
 DK_API dk_status dk_relu_pool_bwd(dk_ctx* ctx, const float* dy, const float* x, int64_t n, int32_t h, int32_t w,
                                   int32_t c, int32_t pool, float* dx, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The rest of a training step around the masked products: a normalisation
+ * between two layers, the loss that gives the first output gradient, the update
+ * made of a decoded weight gradient.  None of it is masked arithmetic.  Tensors
+ * are DK_F32 or DK_BF16 (one type per call; sums, statistics, norms and the
+ * contractions' accumulators are fp32), contiguous and 16-byte aligned;
+ * parameters, statistics and losses are fp32.  Large scratch memory is the
+ * workspace of dk_set_workspace, sized by the *_workspace_bytes calls.
+ * ------------------------------------------------------------------------- */
+enum { DK_F32 = 0, DK_BF16 = 1 };
+enum { DK_ACT_NONE = 0, DK_ACT_RELU = 1, DK_ACT_SILU = 2 };
+
+/* Group normalisation with an activation on channels-last tensors
+ * x[n][h][w][c] (a vector per sample: h = w = 1).  The c channels form `groups`
+ * groups of c/groups consecutive channels.  The statistics are those of ONE
+ * sample: the inputs of a virtual batch, which may belong to different owners,
+ * do not meet in them (as they would in a batch normalisation). */
+typedef struct {
+  int64_t n;          /* samples (0: nothing to do; the gradients of gamma and beta are zero) */
+  int32_t h, w, c;    /* c <= 16384                                               */
+  int32_t groups;     /* divides c                                                */
+  int32_t act;        /* DK_ACT_NONE | DK_ACT_RELU | DK_ACT_SILU (z*sigmoid(z))   */
+  int32_t dtype;      /* of x, y, dy, dx                                          */
+  float eps;          /* >= 0, added to the variance                              */
+} dk_norm;
+
+DK_API dk_status dk_norm_workspace_bytes(const dk_norm* q, size_t* bytes);
+
+/* mean and variance (divided by N = h*w*c/groups) of every sample and group, then
+ *   z = (x - mean)*rstd*gamma[channel] + beta[channel],  rstd = 1/sqrt(var + eps)
+ *   y = act(z)
+ * gamma, beta: fp32 [c].  stats (fp32 [n][groups][2]: mean, rstd) is kept for the
+ * backward call.  HBM-bound.  Needs the workspace. */
+DK_API dk_status dk_group_norm_fwd(dk_ctx* ctx, const dk_norm* q, const void* x, const float* gamma,
+                                   const float* beta, void* y, float* stats, void* stream);
+
+/* Gradients of the forward call, the activation's input z formed again from x:
+ *   d = dy*act'(z) (act'(0) = 0 for DK_ACT_RELU),  xhat = (x - mean)*rstd
+ *   dgamma = sum d*xhat, dbeta = sum d     over samples and pixels
+ *   dx = rstd*(q - mean_N(q) - xhat*mean_N(q*xhat)),  q = d*gamma
+ * dgamma, dbeta: fp32 [c], overwritten; the order of every sum is fixed.  Needs
+ * the workspace. */
+DK_API dk_status dk_group_norm_bwd(dk_ctx* ctx, const dk_norm* q, const void* dy, const void* x,
+                                   const float* gamma, const float* beta, const float* stats, void* dx,
+                                   float* dgamma, float* dbeta, void* stream);
+
+/* A last linear layer with softmax cross entropy over many classes, the logits
+ * never kept: they are formed tile by tile, in pieces of the vocabulary, and
+ * formed again for the gradient. */
+typedef struct {
+  int64_t rows;       /* tokens or samples (0: nothing to do; dW is zero)         */
+  int32_t d;          /* features                                                 */
+  int32_t vocab;      /* classes                                                  */
+  int32_t dtype;      /* of h, W, dh, dW                                          */
+} dk_xent;
+
+DK_API dk_status dk_xent_workspace_bytes(const dk_xent* q, size_t* bytes);
+
+/* h: [rows][d], W: [vocab][d], target: int64 [rows] on the device.
+ *   l = <h[r], W[v]>,  lse[r] = log sum_v exp(l[v]),  loss[r] = lse[r] - l[target[r]]
+ * loss, lse: fp32 [rows].  A row whose target is negative is left out: its loss
+ * and lse are 0 and its values of h, whatever they are, are not used.  A target
+ * >= vocab is left out likewise and reported by dk_device_status as
+ * DK_ERR_INVALID_ARG.  DK_F32 contracts on the tensor cores with each operand
+ * as two fp16 terms under a common power of two (22 significant bits down to
+ * 2^-18 of the tensor's largest magnitude, an absolute error of 2^-40 of that
+ * magnitude below).  Needs the workspace. */
+DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
+                                    const int64_t* target, float* loss, float* lse, void* stream);
+
+/* Gradients of scale * sum_r dloss[r]*loss[r] (dloss: fp32 [rows], nullable = 1):
+ *   p[r][v] = scale*dloss[r]*(exp(l[v] - lse[r]) - [v == target[r]]), 0 for rows left out
+ *   dh = p.W,  dW = p^T.h
+ * lse: from the forward call.  With DK_BF16 p is rounded to bf16 for the two
+ * products, with DK_F32 it is kept as two fp16 terms.  dh and dW are
+ * overwritten.  Needs the workspace. */
+DK_API dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
+                                    const int64_t* target, const float* lse, const float* dloss, float scale,
+                                    void* dh, void* dW, void* stream);
+
+/* The orthogonalised update of a weight matrix (of `batch` matrices x[m][n] of
+ * one shape; a convolution's weights are [cout][kh*kw*cin]): Newton-Schulz
+ * products that drive every singular value towards 1,
+ *   X = x/(|x|_F + eps);  `steps` times: A = X X^T, X = a X + (b A + c A A) X
+ * (A = X^T X and products from the right where m > n), then
+ *   out = keep*out + scale*X.
+ * keep = 0 writes the update itself (out is not read); keep = 1 - lr*decay and
+ * scale = -lr with `out` the weights applies it.  x may be the dW of
+ * dk_linear_bwd_wgrad or a running mean of it; x and out are different tensors. */
+typedef struct {
+  int32_t batch, m, n; /* m, n <= 65536                                           */
+  int32_t dtype;       /* of x and out                                            */
+  int32_t steps;       /* 0 .. 32                                                 */
+  float a, b, c;       /* |a| + 2|b| + 4|c| <= 31                                 */
+  float eps;           /* >= 0; a zero matrix gives a zero update when eps > 0    */
+} dk_ortho;
+
+DK_API dk_status dk_ortho_workspace_bytes(const dk_ortho* q, size_t* bytes);
+DK_API dk_status dk_orthogonalize(dk_ctx* ctx, const dk_ortho* q, const void* x, float scale, float keep,
+                                  void* out, void* stream);
+
 /* Errors raised ON THE DEVICE by calls that have no dk_verdict to carry them
  * (dk_linear_fwd, dk_linear_bwd_wgrad): every wait inside the kernels is
  * bounded, and a kernel whose wait expires stops, leaves its output incomplete

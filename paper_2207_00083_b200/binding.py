@@ -62,6 +62,25 @@ class dk_field_fault(ctypes.Structure):
                 ("out_index", ctypes.c_int64), ("delta", ctypes.c_uint32)]
 
 
+DK_F32, DK_BF16 = 0, 1
+DK_ACT_NONE, DK_ACT_RELU, DK_ACT_SILU = 0, 1, 2
+
+
+class dk_norm(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("h", ctypes.c_int32), ("w", ctypes.c_int32), ("c", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class dk_xent(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class dk_ortho(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("m", ctypes.c_int32), ("n", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+
 VERDICT_BYTES = ctypes.sizeof(dk_verdict)
 _lib = None
 
@@ -99,6 +118,14 @@ def _signatures():
         "dk_field_masked_linear": [vp, pp, ctypes.c_uint32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                    ctypes.POINTER(dk_field_fault), vp],
         "dk_field_linear_bwd_wgrad": [vp, pp, ctypes.c_uint32, vp, vp, i32, vp, vp, vp, vp],
+        "dk_norm_workspace_bytes": [ctypes.POINTER(dk_norm), ctypes.POINTER(ctypes.c_size_t)],
+        "dk_group_norm_fwd": [vp, ctypes.POINTER(dk_norm), vp, vp, vp, vp, vp, vp],
+        "dk_group_norm_bwd": [vp, ctypes.POINTER(dk_norm), vp, vp, vp, vp, vp, vp, vp, vp, vp],
+        "dk_xent_workspace_bytes": [ctypes.POINTER(dk_xent), ctypes.POINTER(ctypes.c_size_t)],
+        "dk_linear_xent_fwd": [vp, ctypes.POINTER(dk_xent), vp, vp, vp, vp, vp, vp],
+        "dk_linear_xent_bwd": [vp, ctypes.POINTER(dk_xent), vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp],
+        "dk_ortho_workspace_bytes": [ctypes.POINTER(dk_ortho), ctypes.POINTER(ctypes.c_size_t)],
+        "dk_orthogonalize": [vp, ctypes.POINTER(dk_ortho), vp, ctypes.c_float, ctypes.c_float, vp, vp],
         "dk_profile_enable": [vp, ctypes.c_int],
         "dk_profile_read": [vp, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
                             ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)],
@@ -194,10 +221,20 @@ class Context:
         _check(lib().dk_field_workspace_bytes(ctypes.byref(p), ctypes.byref(n)), "dk_field_workspace_bytes")
         return n.value
 
-    def ensure_workspace(self, p: dk_problem, field: bool = False):
-        """Grows the torch-owned workspace to what `p` needs and registers it
-        (``field=True``: what the finite-field calls need)."""
-        need = self.field_workspace_bytes(p) if field else self.workspace_bytes(p)
+    def step_workspace_bytes(self, q) -> int:
+        """Workspace of a dk_norm, dk_xent or dk_ortho call."""
+        name = f"{type(q).__name__}_workspace_bytes"
+        n = ctypes.c_size_t()
+        _check(getattr(lib(), name)(ctypes.byref(q), ctypes.byref(n)), name)
+        return n.value
+
+    def ensure_workspace(self, p, field: bool = False):
+        """Grows the torch-owned workspace to what `p` (a dk_problem, dk_norm, dk_xent or dk_ortho) needs and
+        registers it (``field=True``: what the finite-field calls need)."""
+        if not isinstance(p, dk_problem):
+            need = self.step_workspace_bytes(p)
+        else:
+            need = self.field_workspace_bytes(p) if field else self.workspace_bytes(p)
         if self._ws is None or self._ws.numel() < need + 256:
             self._ws = None
             self._ws = torch.empty(need + 256, dtype=torch.uint8, device=f"cuda:{self.device}")
@@ -388,3 +425,70 @@ def dk_field_linear_bwd_wgrad(ctx: Context, p: dk_problem, prime: int, deltaq, x
     _check(lib().dk_field_linear_bwd_wgrad(ctx.handle, ctypes.byref(p), prime, _res(deltaq), _res(xbar), xbar_rows,
                                            _host_u32(C), _host_u32(gamma), _res(dWq), _stream()),
            "dk_field_linear_bwd_wgrad")
+
+
+# ---------------------------------------------------------------------------
+# the rest of a training step: group normalisation with activation, linear layer with softmax cross entropy,
+# orthogonalised update.  x, y, h, W and their gradients are fp32 or bf16 as the descriptor's dtype says,
+# parameters, statistics and losses fp32, targets int64.
+# ---------------------------------------------------------------------------
+_STEP_TYPES = {DK_F32: torch.float32, DK_BF16: torch.bfloat16}
+
+
+def _typed(t: torch.Tensor, dtype: int, numel: int, what: str):
+    want = _STEP_TYPES.get(dtype)
+    if not (t.is_cuda and t.dtype == want and t.is_contiguous() and t.numel() == numel):
+        raise ValueError(f"{what}: expected a contiguous {want} CUDA tensor of {numel} elements")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _f32(t: torch.Tensor, numel: int, what: str):
+    return _typed(t, DK_F32, numel, what)
+
+
+def _norm_sizes(q: dk_norm):
+    return q.n * q.h * q.w * q.c, q.c, q.n * q.groups * 2
+
+
+def dk_group_norm_fwd(ctx: Context, q: dk_norm, x, gamma, beta, y, stats):
+    e, c, s = _norm_sizes(q)
+    _check(lib().dk_group_norm_fwd(ctx.handle, ctypes.byref(q), _typed(x, q.dtype, e, "x"), _f32(gamma, c, "gamma"),
+                                   _f32(beta, c, "beta"), _typed(y, q.dtype, e, "y"), _f32(stats, s, "stats"),
+                                   _stream()), "dk_group_norm_fwd")
+
+
+def dk_group_norm_bwd(ctx: Context, q: dk_norm, dy, x, gamma, beta, stats, dx, dgamma, dbeta):
+    e, c, s = _norm_sizes(q)
+    _check(lib().dk_group_norm_bwd(ctx.handle, ctypes.byref(q), _typed(dy, q.dtype, e, "dy"),
+                                   _typed(x, q.dtype, e, "x"), _f32(gamma, c, "gamma"), _f32(beta, c, "beta"),
+                                   _f32(stats, s, "stats"), _typed(dx, q.dtype, e, "dx"), _f32(dgamma, c, "dgamma"),
+                                   _f32(dbeta, c, "dbeta"), _stream()), "dk_group_norm_bwd")
+
+
+def _targets(t: torch.Tensor, rows: int):
+    if not (t.is_cuda and t.dtype == torch.int64 and t.is_contiguous() and t.numel() == rows):
+        raise ValueError(f"target: expected a contiguous int64 CUDA tensor of {rows} elements")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def dk_linear_xent_fwd(ctx: Context, q: dk_xent, h, W, target, loss, lse):
+    _check(lib().dk_linear_xent_fwd(ctx.handle, ctypes.byref(q), _typed(h, q.dtype, q.rows * q.d, "h"),
+                                    _typed(W, q.dtype, q.vocab * q.d, "W"), _targets(target, q.rows),
+                                    _f32(loss, q.rows, "loss"), _f32(lse, q.rows, "lse"), _stream()),
+           "dk_linear_xent_fwd")
+
+
+def dk_linear_xent_bwd(ctx: Context, q: dk_xent, h, W, target, lse, dloss: Optional[torch.Tensor], scale: float, dh,
+                       dW):
+    _check(lib().dk_linear_xent_bwd(ctx.handle, ctypes.byref(q), _typed(h, q.dtype, q.rows * q.d, "h"),
+                                    _typed(W, q.dtype, q.vocab * q.d, "W"), _targets(target, q.rows),
+                                    _f32(lse, q.rows, "lse"), None if dloss is None else _f32(dloss, q.rows, "dloss"),
+                                    ctypes.c_float(scale), _typed(dh, q.dtype, q.rows * q.d, "dh"),
+                                    _typed(dW, q.dtype, q.vocab * q.d, "dW"), _stream()), "dk_linear_xent_bwd")
+
+
+def dk_orthogonalize(ctx: Context, q: dk_ortho, x, scale: float, keep: float, out):
+    e = q.batch * q.m * q.n
+    _check(lib().dk_orthogonalize(ctx.handle, ctypes.byref(q), _typed(x, q.dtype, e, "x"), ctypes.c_float(scale),
+                                  ctypes.c_float(keep), _typed(out, q.dtype, e, "out"), _stream()),
+           "dk_orthogonalize")

@@ -1,0 +1,456 @@
+// Matrix products C = A.B^T of 16-bit operands on CTA pairs (tcgen05 kind::f16, cta_group::2), for the operators
+// around the masked products: bf16 operands as they are, or fp32 operands as two fp16 terms each,
+//   v*2^s = hi + lo + e,  hi = fp16(v*2^s),  lo = fp16(v*2^s - hi),  |e| <= 2^-22 |v*2^s| (absolute 2^-25 below),
+// of which hi.hi + hi.lo + lo.hi are kept (lo.lo is 2^-22 of the product).  fp16 terms run at the full 16-bit rate of
+// the tensor cores, twice that of TF32, at the same 22 significant bits; what they lack is range, which the common
+// power of two 2^s supplies.
+//
+// A pair computes a 256 x BN tile: each CTA stages its own 128 rows of A and its half of the BN rows of B, 64
+// contraction elements (128 bytes) per stage.  An operand is K-major (rows contiguous along the contraction) or
+// MN-major (contiguous along M or N: a stored matrix used transposed needs no transposed copy).  Roles, barriers and
+// bounded waits are those of the masked products' pair kernel (dk_tc_pair.cuh).
+//
+// The tensor pipe truncates when it adds, so the accumulator in tensor memory takes `chunk` stages at a time and the
+// epilogue warps add the chunks up in fp32 registers, rounding to nearest.  Two accumulators of BN columns let the
+// epilogue of one tile run beside the products of the next.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "dk_step.h"
+#include "dk_tc_pair.cuh"
+
+namespace dk {
+namespace g16 {
+
+using tc::smem_u32;
+
+constexpr int BK = 64;                       // contraction elements per stage: one 128-byte swizzle span
+constexpr int ROWS = 128;                    // rows of A per CTA = TMEM lanes
+constexpr int TILE_M = 256;
+constexpr int kEpi = 8;                      // epilogue warps per CTA
+constexpr int kThreadsG = 32 * (4 + kEpi);
+
+struct Params {
+  int MT, NT, nbatch;          // tiles along M (256 rows), along N (BN rows), matrices
+  int sym;                     // 1: C is symmetric, only tiles with mt >= nt (needs BN = 256)
+  int tiles;                   // tiles of one matrix
+  int group;                   // tiles along M that are walked before the next tile along N
+  int KB, ksplit, kb_per_split;
+  int chunk;                   // stages added up in tensor memory before promotion
+  int nitems;                  // nbatch * tiles * ksplit
+  int nstages;
+  unsigned spin_cap;
+  int withhold;                // test hook: the producer arms its n-th stage but issues no copy (-1 = off)
+  int bf16;                    // operand type: 1 bf16, 0 fp16
+  int M, N;
+  int* status;
+};
+
+// a stored matrix: `rows` rows of `cols` contiguous elements, `pitch` elements apart (a multiple of 8), one or two
+// planes
+struct Operand {
+  const void* hi;
+  const void* lo;
+  long long rows, cols, pitch, batch_stride;     // in elements
+};
+
+__device__ __forceinline__ void item_tile(const Params& p, int w, int& batch, int& ks, int& mt, int& nt) {
+  ks = w % p.ksplit;
+  int t = w / p.ksplit;
+  batch = t / p.tiles;
+  t -= batch * p.tiles;
+  if (p.sym) {
+    mt = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while (mt * (mt + 1) / 2 > t) --mt;
+    while ((mt + 1) * (mt + 2) / 2 <= t) ++mt;
+    nt = t - mt * (mt + 1) / 2;
+  } else {
+    const int per = p.group * p.NT, gi = t / per, m0 = gi * p.group;
+    const int gm = min(p.group, p.MT - m0);
+    t -= gi * per;
+    nt = t / gm;
+    mt = m0 + t - nt * gm;
+  }
+}
+
+__device__ __forceinline__ void mma_f16_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                             uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void ld32(uint32_t taddr, float* v) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// Descriptor of an MN-major tile: [64 contraction rows][64 elements] boxes of 8 KiB, 8-row groups 1 KiB apart, the
+// next 64 elements of M or N in the next box.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr >> 4) & 0x3FFF);
+  d |= (uint64_t)(8192 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// `rows` rows (of M or N) from r0 on, contraction elements from k0 on, of one plane
+template <bool MN, int NROWS>
+__device__ __forceinline__ void load_tile(unsigned char* dst, const CUtensorMap* map, uint32_t bar, int r0, int k0,
+                                          int batch) {
+  if constexpr (MN) {
+#pragma unroll
+    for (int i = 0; i < NROWS / 64; ++i)
+      tc::tma_pair_load_3d(dst + i * 8192, map, bar, (r0 + 64 * i) * 2, k0, batch);
+  } else {
+    tc::tma_pair_load_3d(dst, map, bar, k0 * 2, r0, batch);
+  }
+}
+
+template <int NPROD, int BN>
+__host__ __device__ constexpr int stage_bytes() { return (NPROD == 3 ? 2 : 1) * (ROWS + BN / 2) * 128; }
+
+// Epi: __device__ void operator()(const Params&, float (&acc)[BN/2], int batch, int ks, int row, int col0) is called
+// by every epilogue thread with its row of C and its BN/2 columns from col0 on (row and columns may lie outside C).
+template <int NPROD, bool AMN, bool BMN, int BN, class Epi>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsG, 1)
+gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constant__ CUtensorMap map_a_lo,
+              const __grid_constant__ CUtensorMap map_b_hi, const __grid_constant__ CUtensorMap map_b_lo, const Params p,
+              const Epi epi) {
+  constexpr int A_BYTES = ROWS * 128, B_BYTES = BN / 2 * 128;
+  constexpr int PL = NPROD == 3 ? 2 : 1;
+  constexpr int STAGE = stage_bytes<NPROD, BN>();
+  constexpr int NH = BN / 2;
+  static_assert(BN == 256 || BN == 128, "tile width");
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                         ~static_cast<uintptr_t>(1023));
+  unsigned char* ctrl = smem + (size_t)p.nstages * STAGE;
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(ctrl);      // used in the leader only
+  uint64_t* empty_bar = full_bar + tc::kMaxStages;
+  uint64_t* tfull_bar = empty_bar + tc::kMaxStages;
+  uint64_t* tempty_bar = tfull_bar + 2;                        // used in the leader only
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty_bar + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_ctarank();
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.nstages; ++s) { tc::mbar_init(full_bar + s, 1); tc::mbar_init(empty_bar + s, 1); }
+    for (int b = 0; b < 2; ++b) { tc::mbar_init(tfull_bar + b, 1); tc::mbar_init(tempty_bar + b, 2 * kEpi); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::cluster_sync_all();
+  tc::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  static_assert(40 * 128 + 232 * 256 <= 168 * kThreadsG, "setmaxnreg budget exceeds the CTA's register pool");
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
+    if (warp == 0) {
+      // ---------------- TMA producer (both CTAs) ----------------
+      if (lane == 0) {
+        int stage = 0, issued = 0;
+        uint32_t phase = 0;
+        bool alive = true;
+        for (int w = pair; alive && w < p.nitems; w += npairs) {
+          int batch, ks, mt, nt;
+          item_tile(p, w, batch, ks, mt, nt);
+          const int m0 = mt * TILE_M + (int)rank * ROWS, n0 = nt * BN + (int)rank * (BN / 2);
+          const int kb_lo = ks * p.kb_per_split, kb_hi = min(p.KB, kb_lo + p.kb_per_split);
+          for (int kb = kb_lo; kb < kb_hi; ++kb) {
+            if (!tc::mbar_wait(empty_bar + stage, phase ^ 1u, abort_flag, p.spin_cap)) { alive = false; break; }
+            if (rank == 0) tc::mbar_expect_tx(full_bar + stage, (uint32_t)(2 * STAGE));
+            if (issued++ == p.withhold) { alive = false; break; }
+            unsigned char* st = smem + (size_t)stage * STAGE;
+            const uint32_t bar = tc::mapa_shared(smem_u32(full_bar + stage), 0u);
+            load_tile<AMN, ROWS>(st, &map_a_hi, bar, m0, kb * BK, batch);
+            load_tile<BMN, BN / 2>(st + PL * A_BYTES, &map_b_hi, bar, n0, kb * BK, batch);
+            if constexpr (NPROD == 3) {
+              load_tile<AMN, ROWS>(st + A_BYTES, &map_a_lo, bar, m0, kb * BK, batch);
+              load_tile<BMN, BN / 2>(st + PL * A_BYTES + B_BYTES, &map_b_lo, bar, n0, kb * BK, batch);
+            }
+            if (++stage == p.nstages) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+    } else if (warp == 1 && rank == 0) {
+      // ---------------- MMA issuer (leader only) ----------------
+      if (lane == 0) {
+        const uint32_t idesc = (1u << 4) | ((uint32_t)p.bf16 << 7) | ((uint32_t)p.bf16 << 10) |
+                               ((AMN ? 1u : 0u) << 15) | ((BMN ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) |
+                               ((uint32_t)(TILE_M >> 4) << 24);
+        // 16 contraction elements: 32 bytes along a K-major row, 16 rows of an MN-major box; in 16-byte units
+        constexpr uint64_t STEP_A = AMN ? 128 : 2, STEP_B = BMN ? 128 : 2;
+        int stage = 0;
+        uint32_t phase = 0, acc_it = 0;
+        bool alive = true;
+        for (int w = pair; alive && w < p.nitems; w += npairs) {
+          const int ks = w % p.ksplit;
+          const int kb_lo = ks * p.kb_per_split, kb_hi = min(p.KB, kb_lo + p.kb_per_split);
+          for (int kb = kb_lo; alive && kb < kb_hi; kb += p.chunk, ++acc_it) {
+            const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
+            if (!tc::mbar_wait(tempty_bar + buf, aphase ^ 1u, abort_flag, p.spin_cap)) { alive = false; break; }
+            tc::tc_fence_after();
+            const uint32_t d_tmem = tmem_base + buf * 256u;
+            const int kb_end = min(kb_hi, kb + p.chunk);
+            for (int k = kb; k < kb_end; ++k) {
+              if (!tc::mbar_wait(full_bar + stage, phase, abort_flag, p.spin_cap)) { alive = false; break; }
+              tc::tc_fence_after();
+              const uint32_t st = smem_u32(smem + (size_t)stage * STAGE);
+              const uint64_t a_hi = AMN ? desc_mn(st) : tc::make_desc<128>(st);
+              const uint64_t b_hi = BMN ? desc_mn(st + PL * A_BYTES) : tc::make_desc<128>(st + PL * A_BYTES);
+              const bool first = k == kb;
+#pragma unroll
+              for (int kk = 0; kk < BK / 16; ++kk) {
+                mma_f16_pair(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, (first && kk == 0) ? 0u : 1u);
+                if constexpr (NPROD == 3) {
+                  constexpr uint64_t LO_A = A_BYTES / 16, LO_B = B_BYTES / 16;
+                  mma_f16_pair(d_tmem, a_hi + kk * STEP_A, b_hi + LO_B + kk * STEP_B, idesc, 1u);
+                  mma_f16_pair(d_tmem, a_hi + LO_A + kk * STEP_A, b_hi + kk * STEP_B, idesc, 1u);
+                }
+              }
+              tc::tc_pair_commit(empty_bar + stage);
+              if (++stage == p.nstages) { stage = 0; phase ^= 1u; }
+            }
+            if (alive) tc::tc_pair_commit(tfull_bar + buf);
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;" ::: "memory");
+    // ---------------- epilogue: warps 4..11 of both CTAs ----------------
+    const int quad = warp & 3, half = (warp - 4) >> 2;
+    uint32_t acc_it = 0;
+    bool alive = true;
+    float acc[NH];
+    for (int w = pair; alive && w < p.nitems; w += npairs) {
+      int batch, ks, mt, nt;
+      item_tile(p, w, batch, ks, mt, nt);
+      const int kb_lo = ks * p.kb_per_split, kb_hi = min(p.KB, kb_lo + p.kb_per_split);
+      for (int kb = kb_lo; kb < kb_hi; kb += p.chunk, ++acc_it) {
+        const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
+        if (!tc::mbar_wait(tfull_bar + buf, aphase, abort_flag, p.spin_cap)) { alive = false; break; }
+        tc::tc_fence_after();
+        const uint32_t t = tmem_base + buf * 256u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NH);
+        if (kb == kb_lo) {
+#pragma unroll
+          for (int c = 0; c < NH; c += 32) ld32(t + (uint32_t)c, acc + c);
+          tc::tc_wait_ld();
+        } else {
+#pragma unroll
+          for (int c = 0; c < NH; c += 32) {
+            float tmp[32];
+            ld32(t + (uint32_t)c, tmp);
+            tc::tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[c + j] += tmp[j];
+          }
+        }
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_cluster(tc::mapa_shared(smem_u32(tempty_bar + buf), 0u));
+      }
+      if (!alive) break;
+      epi(p, acc, batch, ks, mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, nt * BN + half * NH);
+    }
+  }
+
+  // ---------------- teardown ----------------
+  tc::tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (threadIdx.x == 0 && p.status != nullptr) atomicExch(p.status, (int)DK_ERR_TIMEOUT);
+    for (int i = 0; i < 64; ++i) __nanosleep(16384);
+    __syncthreads();
+  }
+  tc::cluster_sync_all();
+  if (warp == 1) {
+    tc::tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// epilogues shared by the operators
+// ---------------------------------------------------------------------------
+
+// NV consecutive fp32 values of one thread to dst[0 .. count)
+template <int NV>
+__device__ __forceinline__ void store_f32(float* dst, const float (&v)[NV], int count, bool vec) {
+  if (vec && count >= NV) {
+#pragma unroll
+    for (int j = 0; j < NV; j += 4)
+      *reinterpret_cast<float4*>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j < count) dst[j] = v[j];
+  }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 t = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+template <int NV>
+__device__ __forceinline__ void store_bf16(__nv_bfloat16* dst, const float (&v)[NV], int count, bool vec) {
+  if (vec && count >= NV) {
+#pragma unroll
+    for (int j = 0; j < NV; j += 8)
+      *reinterpret_cast<uint4*>(dst + j) = make_uint4(pack_bf16(v[j], v[j + 1]), pack_bf16(v[j + 2], v[j + 3]),
+                                                      pack_bf16(v[j + 4], v[j + 5]), pack_bf16(v[j + 6], v[j + 7]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j < count) dst[j] = __float2bfloat16_rn(v[j]);
+  }
+}
+// two fp16 terms of v[j]
+template <int NV>
+__device__ __forceinline__ void store_planes(__half* hi, __half* lo, const float (&v)[NV], int count) {
+  // (pitches are multiples of 8 and padding columns may be written: they are zero, as the operands' are)
+#pragma unroll
+  for (int j = 0; j < NV; j += 8) {
+    if (j < count) {
+      uint32_t h[4], l[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float a = v[j + 2 * q], b = v[j + 2 * q + 1];
+        const __half2 t = __floats2half2_rn(a, b);
+        h[q] = *reinterpret_cast<const uint32_t*>(&t);
+        l[q] = pack_f16(a - __low2float(t), b - __high2float(t));
+      }
+      *reinterpret_cast<uint4*>(hi + j) = make_uint4(h[0], h[1], h[2], h[3]);
+      *reinterpret_cast<uint4*>(lo + j) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+  }
+}
+
+// fp32 partial sums of a contraction slice: part[ks][batch][M][pitch]
+struct EpiPartial {
+  float* part;
+  int pitch;             // multiple of 4
+  template <int NH>
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int ks, int row,
+                                             int col0) const {
+    if (row >= p.M || col0 >= p.N) return;
+    float* dst = part + ((size_t)(ks * p.nbatch + batch) * p.M + row) * pitch + col0;
+    store_f32<NH>(dst, acc, min(NH, p.N - col0), true);
+  }
+};
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+struct Tiling {
+  int MT, NT, tiles, KB, ksplit, kb_per_split;
+};
+// ksplit > 1 when the tiles alone leave pairs idle: enough slices that every pair has one, of at least `min_kb`
+// stages each
+inline Tiling plan(long long M, long long N, long long K, int BN, int nbatch, bool sym, int pairs, int min_kb) {
+  Tiling t;
+  t.MT = (int)((M + TILE_M - 1) / TILE_M);
+  t.NT = (int)((N + BN - 1) / BN);
+  t.tiles = sym ? t.MT * (t.MT + 1) / 2 : t.MT * t.NT;
+  t.KB = (int)((K + BK - 1) / BK);
+  int want = pairs / (t.tiles * nbatch);
+  if (want < 1) want = 1;
+  int per = (t.KB + want - 1) / want;
+  if (per < min_kb) per = min_kb;
+  if (per > t.KB) per = t.KB;
+  t.kb_per_split = per;
+  t.ksplit = (t.KB + per - 1) / per;
+  return t;
+}
+
+inline bool make_map(const dk_ctx* ctx, CUtensorMap* m, const void* base, const Operand& o, int nbatch, bool mn,
+                     int box_rows) {
+  const unsigned long long dims[3] = {(unsigned long long)o.cols * 2, (unsigned long long)o.rows,
+                                      (unsigned long long)nbatch};
+  const unsigned long long str[2] = {(unsigned long long)o.pitch * 2,
+                                     (unsigned long long)(nbatch > 1 ? o.batch_stride : o.pitch * o.rows) * 2};
+  const unsigned int box[3] = {128, mn ? (unsigned)BK : (unsigned)box_rows, 1};
+  return tc_encode_map_bytes(ctx, m, base, 3, dims, str, box, 128);
+}
+
+// Per kernel instantiation and device, looked up once.
+struct Prepared {
+  bool done[64];
+};
+
+// p: MT, NT, nbatch, sym, tiles, KB, ksplit, kb_per_split, M, N, chunk are set by the caller
+template <int NPROD, bool AMN, bool BMN, int BN, class Epi>
+dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, const Epi& epi, cudaStream_t st) {
+  static Prepared prep = {};
+  CUtensorMap ma, mal, mb, mbl;
+  if (!make_map(ctx, &ma, A.hi, A, p.nbatch, AMN, ROWS) || !make_map(ctx, &mb, B.hi, B, p.nbatch, BMN, BN / 2))
+    return DK_ERR_CUDA;
+  mal = ma; mbl = mb;
+  if (NPROD == 3 && (!make_map(ctx, &mal, A.lo, A, p.nbatch, AMN, ROWS) ||
+                     !make_map(ctx, &mbl, B.lo, B, p.nbatch, BMN, BN / 2)))
+    return DK_ERR_CUDA;
+  constexpr int STAGE = stage_bytes<NPROD, BN>();
+  constexpr int CTRL = (2 * tc::kMaxStages + 4) * 8 + 16;
+  p.nstages = (227 * 1024 - 1024 - CTRL) / STAGE;
+  if (p.nstages > tc::kMaxStages) p.nstages = tc::kMaxStages;
+  const int smem = p.nstages * STAGE + CTRL + 1024;
+  if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
+  auto kern = gemm16_kernel<NPROD, AMN, BMN, BN, Epi>;
+  if (ctx->device >= 64) return DK_ERR_UNSUPPORTED;
+  if (!prep.done[ctx->device]) {
+    cudaFuncAttributes fa;
+    if (cudaFuncGetAttributes(&fa, kern) != cudaSuccess) return DK_ERR_CUDA;
+    // the setmaxnreg split draws on threads * registers at launch; a smaller pool would wait forever
+    if (fa.numRegs * kThreadsG < 40 * 128 + 232 * 256) return DK_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+      return DK_ERR_CUDA;
+    prep.done[ctx->device] = true;
+  }
+  p.nitems = p.nbatch * p.tiles * p.ksplit;
+  p.group = p.MT < 16 ? p.MT : 16;
+  p.spin_cap = (unsigned)ctx->opt.v[DK_OPT_SPIN_LIMIT];
+  p.withhold = ctx->opt.v[DK_OPT_TEST_WITHHOLD];
+  ctx->opt.v[DK_OPT_TEST_WITHHOLD] = -1;
+  p.status = device_status_word(ctx);
+  int pairs = ctx->sm_count / 2;
+  if (pairs > p.nitems) pairs = p.nitems;
+  kern<<<2 * pairs, kThreadsG, smem, st>>>(ma, mal, mb, mbl, p, epi);
+  return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+}
+
+}  // namespace g16
+}  // namespace dk

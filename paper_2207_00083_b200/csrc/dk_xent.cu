@@ -1,0 +1,700 @@
+// A last linear layer with softmax cross entropy over many classes, without keeping the logits.
+//
+// Forward: l = h.W^T tile by tile on the tensor cores; the epilogue of a tile leaves, per row, the maximum and the
+// sum of exponentials of its columns (and the target's logit), a second kernel joins them:
+//   m = max m_i,  lse = m + log sum_i s_i exp(m_i - m),  loss = lse - l[target].
+// Backward, per piece of the vocabulary: the same product again, whose epilogue writes
+//   p = scale*dloss*(exp(l - lse) - onehot)
+// for the piece, then dh += p.W and dW = p^T.h, which read p and the stored operands in place (transposed where the
+// contraction runs across their rows).  The three products of a piece are what the call costs; the piece is as wide
+// as keeps p near the size of L2.
+#include <math.h>
+
+#include "dk_gemm16.cuh"
+
+namespace dk {
+namespace {
+
+using g16::Operand;
+using g16::Params;
+
+constexpr int kRowThreads = 256;
+
+struct Meta {                  // first words of the workspace
+  unsigned int hmax, wmax, gmax;     // bit patterns of the largest magnitudes (fp32 calls)
+};
+
+// The power of two that brings a largest magnitude (given by its bits) to [2^14, 2^15); 1 when it is zero, infinite or
+// NaN.  The products undo it with inv_scale.
+__device__ __forceinline__ int scale_exp(unsigned int bits) {
+  const int e = (int)(bits >> 23) - 127;
+  if (bits == 0u || e > 127) return 0;
+  const int s = 14 - e;
+  return s > 126 ? 126 : s;
+}
+__device__ __forceinline__ float pow2(int e) {      // -126 <= e <= 126
+  return __int_as_float((e + 127) << 23);
+}
+
+__device__ __forceinline__ bool left_out(long long t, int vocab) { return t < 0 || t >= vocab; }
+
+// largest magnitudes of h (rows that take part), W and dloss
+__global__ void __launch_bounds__(256)
+xent_absmax_kernel(const float* __restrict__ h, const float* __restrict__ W, const int64_t* __restrict__ target,
+                   const float* __restrict__ dloss, float scale, long long rows, int d, int vocab, Meta* meta) {
+  __shared__ unsigned int s[3];
+  if (threadIdx.x < 3) s[threadIdx.x] = 0u;
+  __syncthreads();
+  unsigned int mh = 0, mw = 0, mg = 0;
+  const long long nw = (long long)vocab * d, nh = rows * d, step = (long long)gridDim.x * blockDim.x;
+  const long long i0 = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  const long long nw4 = nw / 4;
+  for (long long i = i0; i < nw4; i += step) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(W) + i);
+    mw = max(mw, max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)));
+  }
+  for (long long i = nw4 * 4 + i0; i < nw; i += step) mw = max(mw, __float_as_uint(W[i]) & 0x7fffffffu);
+  if (d % 4 == 0) {
+    const int d4 = d / 4;
+    for (long long i = i0; i < nh / 4; i += step) {
+      if (left_out(target[i / d4], vocab)) continue;
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(h) + i);
+      mh = max(mh, max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)));
+    }
+  } else {
+    for (long long i = i0; i < nh; i += step)
+      if (!left_out(target[i / d], vocab)) mh = max(mh, __float_as_uint(h[i]) & 0x7fffffffu);
+  }
+  for (long long i = i0; i < rows; i += step)
+    if (!left_out(target[i], vocab))
+      mg = max(mg, __float_as_uint(dloss != nullptr ? dloss[i] * scale : scale) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    mh = max(mh, __shfl_xor_sync(0xffffffffu, mh, o));
+    mw = max(mw, __shfl_xor_sync(0xffffffffu, mw, o));
+    mg = max(mg, __shfl_xor_sync(0xffffffffu, mg, o));
+  }
+  if ((threadIdx.x & 31) == 0) {
+    atomicMax(&s[0], mh); atomicMax(&s[1], mw); atomicMax(&s[2], mg);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    atomicMax(&meta->hmax, s[0]); atomicMax(&meta->wmax, s[1]); atomicMax(&meta->gmax, s[2]);
+  }
+}
+
+// One matrix of the operand preparation: rows of d values to rows of dp (a multiple of 8, padded with zeros), rows
+// that are left out (target given) cleared.
+struct Prep {
+  const void* src;
+  void* hi;
+  void* lo;
+  const int64_t* target;
+  const unsigned int* maxbits;
+  long long rows;
+};
+
+template <bool F32>
+__device__ __forceinline__ void prep_rows(const Prep& q, int d, int dp, int vocab, long long i0, long long step) {
+  const int d8 = dp / 8;
+  const float sc = F32 ? pow2(scale_exp(*q.maxbits)) : 1.f;
+  for (long long i = i0; i < q.rows * d8; i += step) {
+    const long long r = i / d8;
+    const int c = (int)(i - r * d8) * 8;
+    const bool keep = q.target == nullptr || !left_out(q.target[r], vocab);
+    if constexpr (F32) {
+      const float* s = static_cast<const float*>(q.src) + r * d + c;
+      float v[8];
+      if (d % 4 == 0 && c + 8 <= d) {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(s)), b = __ldg(reinterpret_cast<const float4*>(s) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < d ? s[j] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = keep ? v[j] * sc : 0.f;
+      g16::store_planes<8>(static_cast<__half*>(q.hi) + r * dp + c, static_cast<__half*>(q.lo) + r * dp + c, v, 8);
+    } else {
+      const uint16_t* s = static_cast<const uint16_t*>(q.src) + r * d + c;
+      uint16_t v[8];
+      if (d % 8 == 0) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(s));
+        *reinterpret_cast<uint4*>(v) = a;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < d ? s[j] : (uint16_t)0;
+      }
+      const uint4 z = make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(q.hi) + r * dp + c) = keep ? *reinterpret_cast<uint4*>(v) : z;
+    }
+  }
+}
+template <bool F32>
+__global__ void __launch_bounds__(256) xent_prep_kernel(const Prep a, const Prep b, int d, int dp, int vocab) {
+  const long long step = (long long)gridDim.x * blockDim.x, i0 = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (a.src != nullptr) prep_rows<F32>(a, d, dp, vocab, i0, step);
+  if (b.src != nullptr) prep_rows<F32>(b, d, dp, vocab, i0, step);
+}
+
+// what undoes the operands' powers of two: product*f0*f1
+struct Undo {
+  const unsigned int* a;       // null: nothing to undo
+  const unsigned int* b;
+  __device__ __forceinline__ void get(float& f0, float& f1) const {
+    f0 = a != nullptr ? pow2(-scale_exp(*a)) : 1.f;
+    f1 = b != nullptr ? pow2(-scale_exp(*b)) : 1.f;
+  }
+};
+
+// forward epilogue: maximum and sum of exponentials of this thread's columns of its row, and the target's logit
+struct EpiLse {
+  float2* part;                // [columns / (BN/2)][rows]
+  float* tlogit;               // [rows]
+  const int64_t* target;
+  Undo undo;
+  template <int NH>
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0) const {
+    if (row >= p.M || col0 >= p.N) return;
+    float f0, f1;
+    undo.get(f0, f1);
+    const int count = min(NH, p.N - col0);
+    const long long t = target[row];
+    const int at = (t >= col0 && t < (long long)col0 + count) ? (int)(t - col0) : -1;
+    float m = -INFINITY, tl = 0.f;
+#pragma unroll
+    for (int j = 0; j < NH; ++j) {
+      acc[j] = j < count ? acc[j] * f0 * f1 : -INFINITY;
+      m = fmaxf(m, acc[j]);
+      if (j == at) tl = acc[j];
+    }
+    // (all columns -inf: the differences would be NaN; the row's sum is 0 under maximum -inf)
+    const float ref = m == -INFINITY ? 0.f : m;
+    // eight sums: one alone would round its way up 128 times in the same direction where the terms are alike
+    float s[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NH; ++j) s[j & 7] += __expf(acc[j] - ref);
+    part[(size_t)(col0 / NH) * p.M + row] =
+        make_float2(m, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
+    if (at >= 0) tlogit[row] = tl;
+  }
+};
+
+__device__ __forceinline__ float p_value(float l, float lse, bool hit, float g) {
+  return g * (__expf(l - lse) - (hit ? 1.f : 0.f));
+}
+
+struct RowArgs {
+  const int64_t* target;
+  const float* lse;
+  const float* dloss;
+  float scale;
+  int vocab, v0;               // first class of the piece
+  const unsigned int* gmax;    // fp32: p is stored as two fp16 terms under this magnitude's power of two
+  void* hi;
+  void* lo;
+  long long pitch;
+};
+
+// backward epilogue: p of this piece
+template <bool F32>
+struct EpiP {
+  RowArgs r;
+  Undo undo;
+  template <int NH>
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0) const {
+    if (row >= p.M || col0 >= p.N) return;
+    float f0, f1;
+    undo.get(f0, f1);
+    const int count = min(NH, p.N - col0);
+    const long long t = r.target[row];
+    const bool keep = !left_out(t, r.vocab);
+    const float lse = keep ? r.lse[row] : 0.f;
+    float g = keep ? (r.dloss != nullptr ? r.dloss[row] * r.scale : r.scale) : 0.f;
+    if (F32) g *= pow2(scale_exp(*r.gmax));
+    const long long at = t - r.v0 - col0;
+#pragma unroll
+    for (int j = 0; j < NH; ++j)
+      acc[j] = keep && j < count ? p_value(acc[j] * f0 * f1, lse, at == j, g) : 0.f;
+    if constexpr (F32) {
+      g16::store_planes<NH>(static_cast<__half*>(r.hi) + row * r.pitch + col0,
+                            static_cast<__half*>(r.lo) + row * r.pitch + col0, acc, count);
+    } else {
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(r.hi) + row * r.pitch + col0;
+#pragma unroll
+      for (int j = 0; j < NH; j += 8)
+        if (j < count)       // (the pitch is a multiple of 8: padding columns are written as zeros)
+          *reinterpret_cast<uint4*>(dst + j) =
+              make_uint4(g16::pack_bf16(acc[j], acc[j + 1]), g16::pack_bf16(acc[j + 2], acc[j + 3]),
+                         g16::pack_bf16(acc[j + 4], acc[j + 5]), g16::pack_bf16(acc[j + 6], acc[j + 7]));
+    }
+  }
+};
+
+// gradients: out = alpha*product (+ what earlier pieces left in `acc`), as fp32 in `acc` or rounded in `out`
+template <bool F32>
+struct EpiGrad {
+  void* out;                   // null: the sum goes to accum
+  float* accum;                // fp32 [M][pitch_acc]
+  long long pitch, pitch_acc;
+  int add;                     // accum holds earlier pieces
+  int vec;                     // rows of `out` start on 16 bytes
+  Undo undo;
+  template <int NH>
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0) const {
+    if (row >= p.M || col0 >= p.N) return;
+    float f0, f1;
+    undo.get(f0, f1);
+    const int count = min(NH, p.N - col0);
+    float* a = accum + (size_t)row * pitch_acc + col0;
+#pragma unroll
+    for (int j = 0; j < NH; j += 4) {
+      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (add && j < count) t = *reinterpret_cast<const float4*>(a + j);
+      acc[j] = fmaf(acc[j] * f0, f1, t.x); acc[j + 1] = fmaf(acc[j + 1] * f0, f1, t.y);
+      acc[j + 2] = fmaf(acc[j + 2] * f0, f1, t.z); acc[j + 3] = fmaf(acc[j + 3] * f0, f1, t.w);
+    }
+    if (out == nullptr) {
+#pragma unroll
+      for (int j = 0; j < NH; j += 4)
+        if (j < count) *reinterpret_cast<float4*>(a + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+    } else if constexpr (F32) {
+      g16::store_f32<NH>(static_cast<float*>(out) + (size_t)row * pitch + col0, acc, count, vec != 0);
+    } else {
+      g16::store_bf16<NH>(static_cast<__nv_bfloat16*>(out) + (size_t)row * pitch + col0, acc, count, vec != 0);
+    }
+  }
+};
+
+// ---- what follows a product whose contraction was sliced: the slices' sums are joined in order ----
+
+__device__ __forceinline__ float slice_sum(const float* part, size_t at, size_t slice, int ks) {
+  float v = part[at];
+  for (int k = 1; k < ks; ++k) v += part[at + k * slice];
+  return v;
+}
+
+__device__ __forceinline__ void finish_row(long long t, int vocab, float m, float s, float tl, float* loss, float* lse,
+                                           int* status) {
+  const bool keep = !left_out(t, vocab);
+  const float v = m + logf(s);
+  *lse = keep ? v : 0.f;
+  *loss = keep ? v - tl : 0.f;
+  if (t >= vocab) atomicExch(status, (int)DK_ERR_INVALID_ARG);
+}
+
+// one warp per row: joins the tiles' (maximum, sum)
+__global__ void __launch_bounds__(kRowThreads)
+xent_join_kernel(const float2* __restrict__ part, const float* __restrict__ tlogit, const int64_t* __restrict__ target,
+                 long long rows, int slots, int vocab, float* loss, float* lse, int* status) {
+  const int lane = threadIdx.x & 31;
+  const long long row = ((long long)blockIdx.x * kRowThreads + threadIdx.x) >> 5;
+  if (row >= rows) return;
+  float m = -INFINITY, s = 0.f;
+  for (int i = lane; i < slots; i += 32) {
+    const float2 v = part[(size_t)i * rows + row];
+    const float n = fmaxf(m, v.x);
+    if (n != -INFINITY) s = s * __expf(m - n) + v.y * __expf(v.x - n);
+    if (!(v.y == v.y)) s = v.y;
+    m = n;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float mo = __shfl_xor_sync(0xffffffffu, m, o), so = __shfl_xor_sync(0xffffffffu, s, o);
+    const float n = fmaxf(m, mo);
+    const float a = s == 0.f ? 0.f : s * __expf(m - n), b = so == 0.f ? 0.f : so * __expf(mo - n);
+    s = a + b;
+    m = n;
+  }
+  if (lane == 0)
+    finish_row(target[row], vocab, m, s, left_out(target[row], vocab) ? 0.f : tlogit[row], loss + row, lse + row,
+               status);
+}
+
+// one block per row of sliced logits
+__global__ void __launch_bounds__(kRowThreads)
+xent_slices_lse_kernel(const float* __restrict__ part, int ks, long long rows, int vocab, int pitch,
+                       const int64_t* __restrict__ target, const Undo undo, float* loss, float* lse, int* status) {
+  __shared__ float sm[kRowThreads / 32], ss[kRowThreads / 32], st;
+  const long long row = blockIdx.x;
+  float f0, f1;
+  undo.get(f0, f1);
+  const size_t slice = (size_t)rows * pitch;
+  const long long t = target[row];
+  float m = -INFINITY, s = 0.f;
+  if (threadIdx.x == 0) st = 0.f;
+  __syncthreads();
+  for (int v = threadIdx.x; v < vocab; v += kRowThreads) {
+    const float l = slice_sum(part, (size_t)row * pitch + v, slice, ks) * f0 * f1;
+    if (v == t) st = l;
+    const float n = fmaxf(m, l);
+    if (n != -INFINITY) s = s * __expf(m - n) + __expf(l - n);
+    if (!(l == l)) s = l;
+    m = n;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float mo = __shfl_xor_sync(0xffffffffu, m, o), so = __shfl_xor_sync(0xffffffffu, s, o);
+    const float n = fmaxf(m, mo);
+    const float a = s == 0.f ? 0.f : s * __expf(m - n), b = so == 0.f ? 0.f : so * __expf(mo - n);
+    s = a + b;
+    m = n;
+  }
+  if ((threadIdx.x & 31) == 0) { sm[threadIdx.x >> 5] = m; ss[threadIdx.x >> 5] = s; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float M = sm[0];
+    for (int i = 1; i < kRowThreads / 32; ++i) M = fmaxf(M, sm[i]);
+    float S = 0.f;
+    for (int i = 0; i < kRowThreads / 32; ++i) S += ss[i] == 0.f ? 0.f : ss[i] * __expf(sm[i] - M);
+    finish_row(t, vocab, M, S, st, loss + row, lse + row, status);
+  }
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(256)
+xent_slices_p_kernel(const float* __restrict__ part, int ks, long long rows, int n, int pitch, const RowArgs r,
+                     const Undo undo) {
+  float f0, f1;
+  undo.get(f0, f1);
+  const size_t slice = (size_t)rows * pitch;
+  const int n8 = (int)(r.pitch / 8);
+  const float gs = F32 ? pow2(scale_exp(*r.gmax)) : 1.f;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < rows * n8;
+       i += (long long)gridDim.x * blockDim.x) {
+    const long long row = i / n8;
+    const int c = (int)(i - row * n8) * 8;
+    const long long t = r.target[row];
+    const bool keep = !left_out(t, r.vocab);
+    const float lse = keep ? r.lse[row] : 0.f;
+    const float g = keep ? (r.dloss != nullptr ? r.dloss[row] * r.scale : r.scale) * gs : 0.f;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      v[j] = keep && c + j < n
+                 ? p_value(slice_sum(part, (size_t)row * pitch + c + j, slice, ks) * f0 * f1, lse, t - r.v0 == c + j, g)
+                 : 0.f;
+    if constexpr (F32)
+      g16::store_planes<8>(static_cast<__half*>(r.hi) + row * r.pitch + c, static_cast<__half*>(r.lo) + row * r.pitch + c,
+                           v, 8);
+    else
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.hi) + row * r.pitch + c) =
+          make_uint4(g16::pack_bf16(v[0], v[1]), g16::pack_bf16(v[2], v[3]), g16::pack_bf16(v[4], v[5]),
+                     g16::pack_bf16(v[6], v[7]));
+  }
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(256)
+xent_slices_grad_kernel(const float* __restrict__ part, int ks, long long rows, int n, int pitch,
+                        const EpiGrad<F32> e) {
+  float f0, f1;
+  e.undo.get(f0, f1);
+  const size_t slice = (size_t)rows * pitch;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < rows * n;
+       i += (long long)gridDim.x * blockDim.x) {
+    const long long row = i / n;
+    const int c = (int)(i - row * n);
+    float v = slice_sum(part, (size_t)row * pitch + c, slice, ks) * f0 * f1;
+    float* a = e.accum + row * e.pitch_acc + c;
+    if (e.add) v += *a;
+    if (e.out == nullptr) *a = v;
+    else if constexpr (F32) static_cast<float*>(e.out)[row * e.pitch + c] = v;
+    else static_cast<__nv_bfloat16*>(e.out)[row * e.pitch + c] = __float2bfloat16_rn(v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+constexpr int BN = 256;
+constexpr long long kPieceBytes = 128LL << 20;       // aim for p of one piece (both terms)
+
+size_t up(size_t v) { return (v + 1023) / 1024 * 1024; }
+
+struct Plan {
+  bool f32, copy_w, copy_h;    // fwd: operands are laid out anew (fp32 terms, or rows that do not start on 16 bytes)
+  int dp, vp, pieces;
+  size_t off_h, off_w, off_p, off_acc, off_part, off_slots, off_tl, total;
+};
+
+// slices of a product: every (tile, slice) has at most one pair's tile of fp32 sums
+constexpr size_t kPartBytes = (size_t)(kMaxSms / 2) * g16::TILE_M * BN * sizeof(float);
+
+Plan plan_xent(const dk_xent& q) {
+  Plan p;
+  p.f32 = q.dtype == DK_F32;
+  p.dp = (q.d + 7) / 8 * 8;
+  p.copy_w = p.f32 || q.d % 8 != 0;
+  p.copy_h = p.copy_w;
+  const size_t es = p.f32 ? 4 : 2;             // bytes of one operand element, both terms
+  const long long T = q.rows > 0 ? q.rows : 1;
+  long long vp = kPieceBytes / (T * (long long)es) / BN * BN;
+  if (vp < 8 * BN) vp = 8 * BN;
+  if (vp >= q.vocab) vp = q.vocab;
+  p.pieces = (int)((q.vocab + vp - 1) / vp);
+  if (p.pieces > 1) {                           // even pieces
+    vp = (q.vocab + p.pieces - 1) / p.pieces;
+    vp = (vp + BN - 1) / BN * BN;
+    p.pieces = (int)((q.vocab + vp - 1) / vp);
+  }
+  p.vp = (int)((vp + 7) / 8 * 8);
+  size_t off = 1024;
+  p.off_h = off; off += up((size_t)T * p.dp * es);
+  p.off_w = off; off += p.copy_w ? up((size_t)q.vocab * p.dp * es) : 0;
+  p.off_p = off; off += up((size_t)T * p.vp * es);
+  p.off_acc = off; off += p.pieces > 1 ? up((size_t)T * p.dp * 4) : 0;
+  p.off_part = off; off += up(kPartBytes);
+  p.off_slots = off; off += up(((size_t)q.vocab + BN / 2 - 1) / (BN / 2) * T * sizeof(float2));
+  p.off_tl = off; off += up((size_t)T * sizeof(float));
+  p.total = off;
+  return p;
+}
+
+dk_status check_xent(const dk_xent* q) {
+  if (!q) return DK_ERR_INVALID_ARG;
+  if (q->dtype != DK_F32 && q->dtype != DK_BF16) return DK_ERR_INVALID_ARG;
+  if (q->rows < 0 || q->d < 1 || q->vocab < 1) return DK_ERR_SHAPE;
+  if (q->rows > (1LL << 24) || q->d > (1 << 20) || q->vocab > (1 << 24)) return DK_ERR_SHAPE;
+  return DK_OK;
+}
+
+Params gemm_params(const g16::Tiling& t, long long M, long long N, bool f32) {
+  Params p = {};
+  p.MT = t.MT; p.NT = t.NT; p.nbatch = 1; p.sym = 0; p.tiles = t.tiles;
+  p.KB = t.KB; p.ksplit = t.ksplit; p.kb_per_split = t.kb_per_split;
+  p.M = (int)M; p.N = (int)N;
+  p.bf16 = f32 ? 0 : 1;
+  p.chunk = f32 ? 2 : 16;
+  return p;
+}
+
+unsigned grid_of(long long items, int sms) {
+  long long b = (items + 255) / 256;
+  if (b > (long long)sms * 8) b = (long long)sms * 8;
+  return b < 1 ? 1u : (unsigned)b;
+}
+
+struct Call {
+  dk_ctx* ctx;
+  const dk_xent* q;
+  Plan pl;
+  char* ws;
+  cudaStream_t st;
+  Operand h, w;
+  Undo undo_hw;
+  Meta* meta() const { return reinterpret_cast<Meta*>(ws); }
+  float* part() const { return reinterpret_cast<float*>(ws + pl.off_part); }
+};
+
+// lays out h (always when `clear_h`: rows that are left out are cleared, so that what they hold meets no product) and
+// W, and finds the magnitudes of the fp32 terms
+template <bool F32>
+dk_status prepare(Call& c, const void* h, const void* W, const int64_t* target, const float* dloss, float scale,
+                  bool clear_h) {
+  const dk_xent& q = *c.q;
+  const Plan& pl = c.pl;
+  Meta* meta = c.meta();
+  const bool copy_h = pl.copy_h || clear_h;
+  __half* hh = reinterpret_cast<__half*>(c.ws + pl.off_h);
+  __half* wh = reinterpret_cast<__half*>(c.ws + pl.off_w);
+  const long long nh = q.rows * pl.dp, nw = (long long)q.vocab * pl.dp;
+  Prep a = {}, b = {};
+  if (copy_h) a = Prep{h, hh, hh + nh, target, &meta->hmax, q.rows};
+  if (pl.copy_w) b = Prep{W, wh, wh + nw, nullptr, &meta->wmax, q.vocab};
+  c.undo_hw = Undo{nullptr, nullptr};
+  if (F32) {
+    DK_CUDA_CHECK(cudaMemsetAsync(meta, 0, sizeof(Meta), c.st));
+    xent_absmax_kernel<<<grid_of((nw + nh) / 4, c.ctx->sm_count), 256, 0, c.st>>>(
+        static_cast<const float*>(h), static_cast<const float*>(W), target, dloss, scale, q.rows, q.d, q.vocab, meta);
+    c.undo_hw = Undo{&meta->hmax, &meta->wmax};
+  }
+  if (copy_h || pl.copy_w)
+    xent_prep_kernel<F32><<<grid_of(((copy_h ? nh : 0) + (pl.copy_w ? nw : 0)) / 8, c.ctx->sm_count), 256, 0, c.st>>>(
+        a, b, q.d, pl.dp, q.vocab);
+  c.h = Operand{copy_h ? (const void*)hh : h, hh + nh, q.rows, q.d, pl.dp, 0};
+  c.w = Operand{pl.copy_w ? (const void*)wh : W, wh + nw, q.vocab, q.d, pl.dp, 0};
+  return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+}
+
+template <bool F32>
+dk_status forward(Call& c, const int64_t* target, float* loss, float* lse) {
+  constexpr int NP = F32 ? 3 : 1;
+  const dk_xent& q = *c.q;
+  const Plan& pl = c.pl;
+  const g16::Tiling t = g16::plan(q.rows, q.vocab, q.d, BN, 1, false, c.ctx->sm_count / 2, 4);
+  Params p = gemm_params(t, q.rows, q.vocab, F32);
+  int* status = device_status_word(c.ctx);
+  dk_status s;
+  if (t.ksplit > 1) {
+    const int pitch = (q.vocab + 3) / 4 * 4;
+    s = g16::launch<NP, false, false, BN>(c.ctx, c.h, c.w, p, g16::EpiPartial{c.part(), pitch}, c.st);
+    if (s != DK_OK) return s;
+    xent_slices_lse_kernel<<<(unsigned)q.rows, kRowThreads, 0, c.st>>>(c.part(), t.ksplit, q.rows, q.vocab, pitch,
+                                                                      target, c.undo_hw, loss, lse, status);
+  } else {
+    float2* slots = reinterpret_cast<float2*>(c.ws + pl.off_slots);
+    float* tl = reinterpret_cast<float*>(c.ws + pl.off_tl);
+    s = g16::launch<NP, false, false, BN>(c.ctx, c.h, c.w, p, EpiLse{slots, tl, target, c.undo_hw}, c.st);
+    if (s != DK_OK) return s;
+    const int nslots = (q.vocab + BN / 2 - 1) / (BN / 2);
+    xent_join_kernel<<<(unsigned)((q.rows * 32 + kRowThreads - 1) / kRowThreads), kRowThreads, 0, c.st>>>(
+        slots, tl, target, q.rows, nslots, q.vocab, loss, lse, status);
+  }
+  return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+}
+
+template <bool F32>
+dk_status backward(Call& c, const int64_t* target, const float* lse, const float* dloss, float scale, void* dh,
+                   void* dW) {
+  constexpr int NP = F32 ? 3 : 1;
+  const dk_xent& q = *c.q;
+  const Plan& pl = c.pl;
+  const long long T = q.rows;
+  const int pairs = c.ctx->sm_count / 2;
+  const size_t es = F32 ? 4 : 2;
+  __half* ph = reinterpret_cast<__half*>(c.ws + pl.off_p);
+  float* accum = reinterpret_cast<float*>(c.ws + pl.off_acc);
+  const Undo undo_pw{F32 ? &c.meta()->gmax : nullptr, F32 ? &c.meta()->wmax : nullptr};
+  const Undo undo_ph{F32 ? &c.meta()->gmax : nullptr, F32 ? &c.meta()->hmax : nullptr};
+  const int vec = ((size_t)q.d * es) % 16 == 0;
+  for (int i = 0; i < pl.pieces; ++i) {
+    const int v0 = i * pl.vp, nv = q.vocab - v0 < pl.vp ? q.vocab - v0 : pl.vp;
+    const long long pitch_p = (nv + 7) / 8 * 8;
+    __half* pl_lo = ph + T * pitch_p;
+    Operand w = c.w;
+    w.hi = static_cast<const __half*>(c.w.hi) + (size_t)v0 * pl.dp;
+    w.lo = static_cast<const __half*>(c.w.lo) + (size_t)v0 * pl.dp;
+    w.rows = nv;
+    const Operand pop{ph, pl_lo, T, nv, pitch_p, 0};
+    const RowArgs r{target, lse, dloss, scale, q.vocab, v0, &c.meta()->gmax, ph, pl_lo, pitch_p};
+
+    // p of the piece
+    g16::Tiling t = g16::plan(T, nv, q.d, BN, 1, false, pairs, 4);
+    Params p = gemm_params(t, T, nv, F32);
+    dk_status s;
+    if (t.ksplit > 1) {
+      const int pitch = (nv + 3) / 4 * 4;
+      s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
+      if (s != DK_OK) return s;
+      xent_slices_p_kernel<F32><<<grid_of(T * pitch_p / 8, c.ctx->sm_count), 256, 0, c.st>>>(
+          c.part(), t.ksplit, T, nv, pitch, r, c.undo_hw);
+    } else {
+      s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, EpiP<F32>{r, c.undo_hw}, c.st);
+      if (s != DK_OK) return s;
+    }
+
+    // dh += p.W
+    const bool last = i + 1 == pl.pieces;
+    EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, vec, undo_pw};
+    t = g16::plan(T, q.d, nv, BN, 1, false, pairs, 4);
+    p = gemm_params(t, T, q.d, F32);
+    if (t.ksplit > 1) {
+      const int pitch = (q.d + 3) / 4 * 4;
+      s = g16::launch<NP, false, true, BN>(c.ctx, pop, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
+      if (s != DK_OK) return s;
+      xent_slices_grad_kernel<F32><<<grid_of(T * q.d, c.ctx->sm_count), 256, 0, c.st>>>(c.part(), t.ksplit, T, q.d,
+                                                                                       pitch, e);
+    } else {
+      s = g16::launch<NP, false, true, BN>(c.ctx, pop, w, p, e, c.st);
+      if (s != DK_OK) return s;
+    }
+
+    // dW of the piece = p^T.h
+    e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, vec, undo_ph};
+    t = g16::plan(nv, q.d, T, BN, 1, false, pairs, 4);
+    p = gemm_params(t, nv, q.d, F32);
+    if (t.ksplit > 1) {
+      const int pitch = (q.d + 3) / 4 * 4;
+      s = g16::launch<NP, true, true, BN>(c.ctx, pop, c.h, p, g16::EpiPartial{c.part(), pitch}, c.st);
+      if (s != DK_OK) return s;
+      xent_slices_grad_kernel<F32><<<grid_of((long long)nv * q.d, c.ctx->sm_count), 256, 0, c.st>>>(
+          c.part(), t.ksplit, nv, q.d, pitch, e);
+    } else {
+      s = g16::launch<NP, true, true, BN>(c.ctx, pop, c.h, p, e, c.st);
+      if (s != DK_OK) return s;
+    }
+    if (cudaGetLastError() != cudaSuccess) return DK_ERR_CUDA;
+  }
+  return DK_OK;
+}
+
+dk_status begin(dk_ctx* ctx, const dk_xent* q, void* stream, Call* c) {
+  c->ctx = ctx;
+  c->q = q;
+  c->pl = plan_xent(*q);
+  c->ws = static_cast<char*>(ctx->ws);
+  c->st = static_cast<cudaStream_t>(stream);
+  return ctx->ws && ctx->ws_bytes >= c->pl.total ? DK_OK : DK_ERR_WORKSPACE;
+}
+
+}  // namespace
+}  // namespace dk
+
+using namespace dk;
+
+extern "C" {
+
+dk_status dk_xent_workspace_bytes(const dk_xent* q, size_t* bytes) {
+  if (!bytes) return DK_ERR_INVALID_ARG;
+  dk_status s = check_xent(q);
+  if (s != DK_OK) return s;
+  *bytes = plan_xent(*q).total;
+  return DK_OK;
+}
+
+dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W, const int64_t* target,
+                             float* loss, float* lse, void* stream) {
+  dk_status s = check_xent(q);
+  if (s != DK_OK) return s;
+  if (!ctx) return DK_ERR_INVALID_ARG;
+  if (q->rows == 0) return DK_OK;           // (tensors without elements may be NULL)
+  if (!h || !W || !target || !loss || !lse) return DK_ERR_INVALID_ARG;
+  if (!aligned_to(h, 16) || !aligned_to(W, 16) || !aligned_to(target, 16) || !aligned_to(loss, 16) ||
+      !aligned_to(lse, 16))
+    return DK_ERR_INVALID_ARG;
+  Call c;
+  s = begin(ctx, q, stream, &c);
+  if (s != DK_OK) return s;
+  OnDevice dev(ctx->device);
+  if (!dev.ok) return DK_ERR_CUDA;
+  ProfScope ps(ctx, DK_KERNEL_OTHER, 2 + (c.pl.copy_w ? 1 : 0) + (c.pl.f32 ? 1 : 0), c.st);
+  if (c.pl.f32) {
+    s = prepare<true>(c, h, W, target, nullptr, 1.f, false);
+    return s == DK_OK ? forward<true>(c, target, loss, lse) : s;
+  }
+  s = prepare<false>(c, h, W, target, nullptr, 1.f, false);
+  return s == DK_OK ? forward<false>(c, target, loss, lse) : s;
+}
+
+dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W, const int64_t* target,
+                             const float* lse, const float* dloss, float scale, void* dh, void* dW, void* stream) {
+  dk_status s = check_xent(q);
+  if (s != DK_OK) return s;
+  if (!ctx || !dW) return DK_ERR_INVALID_ARG;
+  if (q->rows > 0 && (!h || !W || !target || !lse || !dh)) return DK_ERR_INVALID_ARG;
+  if (!aligned_to(h, 16) || !aligned_to(W, 16) || !aligned_to(target, 16) || !aligned_to(lse, 16) ||
+      !aligned_to(dloss, 16) || !aligned_to(dh, 16) || !aligned_to(dW, 16))
+    return DK_ERR_INVALID_ARG;
+  OnDevice dev(ctx->device);
+  if (!dev.ok) return DK_ERR_CUDA;
+  if (q->rows == 0) {
+    DK_CUDA_CHECK(cudaMemsetAsync(dW, 0, (size_t)q->vocab * q->d * (q->dtype == DK_F32 ? 4 : 2),
+                                  static_cast<cudaStream_t>(stream)));
+    return DK_OK;
+  }
+  Call c;
+  s = begin(ctx, q, stream, &c);
+  if (s != DK_OK) return s;
+  ProfScope ps(ctx, DK_KERNEL_OTHER, 1 + (c.pl.f32 ? 1 : 0) + 3 * c.pl.pieces, c.st);
+  if (c.pl.f32) {
+    s = prepare<true>(c, h, W, target, dloss, scale, true);
+    return s == DK_OK ? backward<true>(c, target, lse, dloss, scale, dh, dW) : s;
+  }
+  s = prepare<false>(c, h, W, target, dloss, scale, true);
+  return s == DK_OK ? backward<false>(c, target, lse, dloss, scale, dh, dW) : s;
+}
+
+}  // extern "C"

@@ -1,0 +1,75 @@
+"""Argument checks of the training-step calls that need no GPU: the workspace sizes."""
+import ctypes
+
+import pytest
+
+from paper_2207_00083_b200 import binding as dk
+
+
+def size(q):
+    n = ctypes.c_size_t()
+    s = getattr(dk.lib(), f"{type(q).__name__}_workspace_bytes")(ctypes.byref(q), ctypes.byref(n))
+    return s, n.value
+
+
+def test_struct_layouts_match_header():
+    assert ctypes.sizeof(dk.dk_norm) == 40 and dk.dk_norm.eps.offset == 32
+    assert ctypes.sizeof(dk.dk_xent) == 24 and dk.dk_xent.dtype.offset == 16
+    assert ctypes.sizeof(dk.dk_ortho) == 36
+
+
+GOOD = [dk.dk_norm(4, 7, 7, 512, 32, 1, 0, 1e-5), dk.dk_norm(0, 1, 1, 1, 1, 0, 1, 0.0),
+        dk.dk_xent(256, 4096, 1000, 0), dk.dk_xent(0, 1, 1, 1), dk.dk_xent(4096, 4096, 128000, 1),
+        dk.dk_ortho(1, 4096, 25088, 0, 5, 3.4445, -4.775, 2.0315, 1e-7), dk.dk_ortho(3, 1, 1, 1, 0, 1.5, -0.5, 0.0, 0.0)]
+
+
+@pytest.mark.parametrize("q", GOOD, ids=lambda q: type(q).__name__)
+def test_accepted(q):
+    s, n = size(q)
+    assert s == 0 and n % 256 == 0
+
+
+def test_workspace_holds_the_operands():
+    # fp32: both terms of h and W, and of one piece of p
+    s, n = size(dk.dk_xent(256, 4096, 1000, 0))
+    assert n >= 4 * (256 * 4096 + 1000 * 4096 + 256 * 1000)
+    # two generations of X, A and B
+    s, n = size(dk.dk_ortho(2, 512, 4608, 0, 5, 3.4445, -4.775, 2.0315, 1e-7))
+    assert n >= 4 * 2 * (2 * 512 * 4608 + 2 * 512 * 512)
+
+
+SHAPE, INVALID = 2, 1
+REFUSED = [
+    (dk.dk_norm(1, 1, 1, 6, 4, 0, 0, 1e-5), SHAPE), (dk.dk_norm(1, 0, 1, 6, 2, 0, 0, 1e-5), SHAPE),
+    (dk.dk_norm(-1, 1, 1, 6, 2, 0, 0, 1e-5), SHAPE), (dk.dk_norm(1, 1, 1, 20000, 2, 0, 0, 1e-5), SHAPE),
+    (dk.dk_norm(1, 1, 1, 6, 0, 0, 0, 1e-5), SHAPE), (dk.dk_norm(1, 1, 1, 6, 2, 3, 0, 1e-5), INVALID),
+    (dk.dk_norm(1, 1, 1, 6, 2, 0, 2, 1e-5), INVALID), (dk.dk_norm(1, 1, 1, 6, 2, 0, 0, -1.0), INVALID),
+    (dk.dk_norm(1, 1, 1, 6, 2, 0, 0, float("nan")), INVALID), (dk.dk_norm(1, 65536, 65536, 1, 1, 0, 0, 1e-5), SHAPE),
+    (dk.dk_xent(-1, 8, 8, 0), SHAPE), (dk.dk_xent(8, 0, 8, 0), SHAPE), (dk.dk_xent(8, 8, 0, 0), SHAPE),
+    (dk.dk_xent(8, 8, 8, 5), INVALID), (dk.dk_xent(1 << 30, 8, 8, 0), SHAPE),
+    (dk.dk_ortho(0, 8, 8, 0, 5, 1.5, -0.5, 0.0, 0.0), SHAPE), (dk.dk_ortho(1, 0, 8, 0, 5, 1.5, -0.5, 0.0, 0.0), SHAPE),
+    (dk.dk_ortho(1, 8, 70000, 0, 5, 1.5, -0.5, 0.0, 0.0), SHAPE), (dk.dk_ortho(1, 8, 8, 0, 33, 1.5, -0.5, 0.0, 0.0), SHAPE),
+    (dk.dk_ortho(1, 8, 8, 3, 5, 1.5, -0.5, 0.0, 0.0), INVALID), (dk.dk_ortho(1, 8, 8, 0, 5, 40.0, -0.5, 0.0, 0.0), INVALID),
+    (dk.dk_ortho(1, 8, 8, 0, 5, float("nan"), -0.5, 0.0, 0.0), INVALID),
+    (dk.dk_ortho(1, 8, 8, 0, 5, 1.5, -0.5, 0.0, -1.0), INVALID),
+]
+
+
+@pytest.mark.parametrize("q,status", REFUSED)
+def test_refused(q, status):
+    assert size(q)[0] == status
+
+
+def test_null_arguments():
+    L = dk.lib()
+    n = ctypes.c_size_t()
+    for t in ("norm", "xent", "ortho"):
+        f = getattr(L, f"dk_{t}_workspace_bytes")
+        assert f(None, ctypes.byref(n)) == INVALID
+    q = dk.dk_norm(1, 1, 1, 6, 2, 0, 0, 1e-5)
+    assert L.dk_norm_workspace_bytes(ctypes.byref(q), None) == INVALID
+    assert L.dk_group_norm_fwd(None, ctypes.byref(q), None, None, None, None, None, None) == INVALID
+    x = dk.dk_xent(8, 8, 8, 0)
+    assert L.dk_linear_xent_fwd(None, ctypes.byref(x), None, None, None, None, None, None) == INVALID
+    o = dk.dk_ortho(1, 8, 8, 0, 5, 1.5, -0.5, 0.0, 0.0)
+    assert L.dk_orthogonalize(None, ctypes.byref(o), None, 1.0, 0.0, None, None) == INVALID
