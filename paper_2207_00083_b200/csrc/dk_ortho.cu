@@ -252,9 +252,9 @@ Plan plan_ortho(const dk_ortho& q) {
   for (int i = 0; i < 2; ++i) { p.off_x[i] = off; off += up(p.x_plane * 4); }
   p.off_a = off; off += up(p.s_plane * 4);
   p.off_b = off; off += up(p.s_plane * 4);
-  // slices of a product: every (tile, slice) has at most one pair's tile of fp32 sums; a symmetric product always goes
-  // through them
-  size_t part = (size_t)(kMaxSms / 2) * g16::TILE_M * BN * sizeof(float);
+  // Slices of a product: every (tile, slice) has a pair of its own, but a slice of a symmetric product takes the room of
+  // the whole square, up to twice its tiles.  A symmetric product always goes through them.
+  size_t part = (size_t)2 * (kMaxSms / 2) * g16::TILE_M * BN * sizeof(float);
   const size_t square = (size_t)q.batch * p.s * p.sp * sizeof(float);
   if (square > part) part = square;
   p.off_part = off; off += up(part);
