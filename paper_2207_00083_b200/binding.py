@@ -433,13 +433,14 @@ def dk_field_linear_bwd_wgrad(ctx: Context, p: dk_problem, prime: int, deltaq, x
 # parameters, statistics and losses fp32, targets int64.
 # ---------------------------------------------------------------------------
 _STEP_TYPES = {DK_F32: torch.float32, DK_BF16: torch.bfloat16}
+# (the calls below take microseconds on the GPU for small layers: the marshalling is kept to plain integers)
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _typed(t: torch.Tensor, dtype: int, numel: int, what: str):
-    want = _STEP_TYPES.get(dtype)
-    if not (t.is_cuda and t.dtype == want and t.is_contiguous() and t.numel() == numel):
-        raise ValueError(f"{what}: expected a contiguous {want} CUDA tensor of {numel} elements")
-    return ctypes.c_void_p(t.data_ptr())
+def _typed(t: torch.Tensor, dtype: int, numel: int, what: str) -> int:
+    if t.dtype is not _STEP_TYPES.get(dtype) or t.numel() != numel or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: expected a contiguous {_STEP_TYPES.get(dtype)} CUDA tensor of {numel} elements")
+    return t.data_ptr()
 
 
 def _f32(t: torch.Tensor, numel: int, what: str):
@@ -447,14 +448,15 @@ def _f32(t: torch.Tensor, numel: int, what: str):
 
 
 def _norm_sizes(q: dk_norm):
-    return q.n * q.h * q.w * q.c, q.c, q.n * q.groups * 2
+    n, c = q.n, q.c
+    return n * q.h * q.w * c, c, n * q.groups * 2
 
 
 def dk_group_norm_fwd(ctx: Context, q: dk_norm, x, gamma, beta, y, stats):
     e, c, s = _norm_sizes(q)
     _check(lib().dk_group_norm_fwd(ctx.handle, ctypes.byref(q), _typed(x, q.dtype, e, "x"), _f32(gamma, c, "gamma"),
                                    _f32(beta, c, "beta"), _typed(y, q.dtype, e, "y"), _f32(stats, s, "stats"),
-                                   _stream()), "dk_group_norm_fwd")
+                                   _raw_stream(ctx.device)), "dk_group_norm_fwd")
 
 
 def dk_group_norm_bwd(ctx: Context, q: dk_norm, dy, x, gamma, beta, stats, dx, dgamma, dbeta):
@@ -462,19 +464,19 @@ def dk_group_norm_bwd(ctx: Context, q: dk_norm, dy, x, gamma, beta, stats, dx, d
     _check(lib().dk_group_norm_bwd(ctx.handle, ctypes.byref(q), _typed(dy, q.dtype, e, "dy"),
                                    _typed(x, q.dtype, e, "x"), _f32(gamma, c, "gamma"), _f32(beta, c, "beta"),
                                    _f32(stats, s, "stats"), _typed(dx, q.dtype, e, "dx"), _f32(dgamma, c, "dgamma"),
-                                   _f32(dbeta, c, "dbeta"), _stream()), "dk_group_norm_bwd")
+                                   _f32(dbeta, c, "dbeta"), _raw_stream(ctx.device)), "dk_group_norm_bwd")
 
 
 def _targets(t: torch.Tensor, rows: int):
     if not (t.is_cuda and t.dtype == torch.int64 and t.is_contiguous() and t.numel() == rows):
         raise ValueError(f"target: expected a contiguous int64 CUDA tensor of {rows} elements")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def dk_linear_xent_fwd(ctx: Context, q: dk_xent, h, W, target, loss, lse):
     _check(lib().dk_linear_xent_fwd(ctx.handle, ctypes.byref(q), _typed(h, q.dtype, q.rows * q.d, "h"),
                                     _typed(W, q.dtype, q.vocab * q.d, "W"), _targets(target, q.rows),
-                                    _f32(loss, q.rows, "loss"), _f32(lse, q.rows, "lse"), _stream()),
+                                    _f32(loss, q.rows, "loss"), _f32(lse, q.rows, "lse"), _raw_stream(ctx.device)),
            "dk_linear_xent_fwd")
 
 
@@ -483,12 +485,12 @@ def dk_linear_xent_bwd(ctx: Context, q: dk_xent, h, W, target, lse, dloss: Optio
     _check(lib().dk_linear_xent_bwd(ctx.handle, ctypes.byref(q), _typed(h, q.dtype, q.rows * q.d, "h"),
                                     _typed(W, q.dtype, q.vocab * q.d, "W"), _targets(target, q.rows),
                                     _f32(lse, q.rows, "lse"), None if dloss is None else _f32(dloss, q.rows, "dloss"),
-                                    ctypes.c_float(scale), _typed(dh, q.dtype, q.rows * q.d, "dh"),
-                                    _typed(dW, q.dtype, q.vocab * q.d, "dW"), _stream()), "dk_linear_xent_bwd")
+                                    scale, _typed(dh, q.dtype, q.rows * q.d, "dh"),
+                                    _typed(dW, q.dtype, q.vocab * q.d, "dW"), _raw_stream(ctx.device)), "dk_linear_xent_bwd")
 
 
 def dk_orthogonalize(ctx: Context, q: dk_ortho, x, scale: float, keep: float, out):
     e = q.batch * q.m * q.n
-    _check(lib().dk_orthogonalize(ctx.handle, ctypes.byref(q), _typed(x, q.dtype, e, "x"), ctypes.c_float(scale),
-                                  ctypes.c_float(keep), _typed(out, q.dtype, e, "out"), _stream()),
+    _check(lib().dk_orthogonalize(ctx.handle, ctypes.byref(q), _typed(x, q.dtype, e, "x"), scale,
+                                  keep, _typed(out, q.dtype, e, "out"), _raw_stream(ctx.device)),
            "dk_orthogonalize")

@@ -344,7 +344,9 @@ dk_status dk_create(dk_ctx** out, int device) {
             cudaMalloc(&c->d_stage, kCoefSlots * kCoefSlotBytes) == cudaSuccess &&
             cudaMalloc(&c->d_vstats, (kVerifyStatFloats + 64) * sizeof(float)) == cudaSuccess &&
             cudaMemset(c->d_vstats, 0, (kVerifyStatFloats + 64) * sizeof(float)) == cudaSuccess &&
-            cudaMalloc(&c->d_cand, kCandCap * sizeof(Candidate)) == cudaSuccess;
+            cudaMalloc(&c->d_cand, kCandCap * sizeof(Candidate)) == cudaSuccess &&
+            cudaMalloc(&c->d_step, kStepCounters * sizeof(unsigned int)) == cudaSuccess &&
+            cudaMemset(c->d_step, 0, kStepCounters * sizeof(unsigned int)) == cudaSuccess;
   for (int i = 0; ok && i < kCoefSlots; ++i)
     ok = cudaEventCreateWithFlags(&c->slot_ev[i], cudaEventDisableTiming) == cudaSuccess;
   ok = ok && cudaStreamCreateWithFlags(&c->side, cudaStreamNonBlocking) == cudaSuccess &&
@@ -378,6 +380,7 @@ dk_status dk_destroy(dk_ctx* c) {
   if (c->d_stage) cudaFree(c->d_stage);
   if (c->d_vstats) cudaFree(c->d_vstats);
   if (c->d_cand) cudaFree(c->d_cand);
+  if (c->d_step) cudaFree(c->d_step);
   delete c;
   return DK_OK;
 }

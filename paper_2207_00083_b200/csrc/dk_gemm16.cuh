@@ -154,6 +154,8 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
   const uint32_t rank = tc::cluster_ctarank();
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
 
+  // what follows up to wait_for_previous touches nothing that an earlier kernel writes
+  allow_next();
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.nstages; ++s) { tc::mbar_init(full_bar + s, 1); tc::mbar_init(empty_bar + s, 1); }
     for (int b = 0; b < 2; ++b) { tc::mbar_init(tfull_bar + b, 1); tc::mbar_init(tempty_bar + b, 2 * kEpi); }
@@ -172,6 +174,7 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
   tc::cluster_sync_all();
   tc::tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  wait_for_previous();
 
   static_assert(40 * 128 + 232 * 256 <= 168 * kThreadsG, "setmaxnreg budget exceeds the CTA's register pool");
   if (warp < 4) {
@@ -448,8 +451,9 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
   p.status = device_status_word(ctx);
   int pairs = ctx->sm_count / 2;
   if (pairs > p.nitems) pairs = p.nitems;
-  kern<<<2 * pairs, kThreadsG, smem, st>>>(ma, mal, mb, mbl, p, epi);
-  return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+  return launch_chained(kern, dim3(2 * (unsigned)pairs), kThreadsG, (size_t)smem, st, ma, mal, mb, mbl, p, epi) == cudaSuccess
+             ? DK_OK
+             : DK_ERR_CUDA;
 }
 
 }  // namespace g16

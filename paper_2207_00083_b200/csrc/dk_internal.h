@@ -50,6 +50,7 @@ struct CoefView {
   const unsigned char* chunk_tab;   // one value per group (device; null when the tables were not derived)
 };
 
+constexpr int kStepCounters = 16384;
 constexpr int kCoefSlots = 8;
 constexpr int kMaxSlabs = 8;       // most launches one call's groups are cut into
 constexpr size_t kCoefSlotBytes = 512 * 1024;
@@ -102,6 +103,7 @@ struct dk_ctx {
   cudaStream_t side;
   cudaEvent_t ev_fork;
   cudaEvent_t ev_slab[dk::kMaxSlabs];
+  unsigned int* d_step;       // dk::kStepCounters words, zero between calls (see dk_step.h)
 };
 
 namespace dk {

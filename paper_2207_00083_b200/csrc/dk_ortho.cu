@@ -32,6 +32,7 @@ __device__ __forceinline__ float load1(const void* p, size_t i) {
 // sums of squares in fp64: neither tiny nor huge gradients leave its range
 template <int DT>
 __global__ void __launch_bounds__(256) ortho_sumsq_kernel(const void* x, long long per, double* part) {
+  chained_launch();
   __shared__ double s[8];
   const size_t base = (size_t)blockIdx.y * per;
   double t = 0.0;
@@ -54,6 +55,7 @@ template <int DT>
 __global__ void __launch_bounds__(256)
 ortho_load_kernel(const void* x, const double* part, int nparts, double eps, long long m, int n, int pitch, __half* hi,
                   __half* lo) {
+  chained_launch();
   __shared__ float f;
   if (threadIdx.x < 32) {
     double t = 0.0;
@@ -90,6 +92,7 @@ struct SymArgs {
   __half* lo;
 };
 __global__ void __launch_bounds__(256) ortho_sym_kernel(const SymArgs q) {
+  chained_launch();
   __shared__ float tile[32][33];
   const int bi = blockIdx.y, bj = blockIdx.x, batch = blockIdx.z;
   if (bj > bi) return;
@@ -187,6 +190,7 @@ struct EpiX {
 __global__ void __launch_bounds__(256)
 ortho_x_kernel(const XArgs a, const float* part, int ks, int pitch_part, const __half* x_hi, const __half* x_lo,
                long long rows, int pitch_x) {
+  chained_launch();
   const int n8 = (a.n + 7) / 8;
   const size_t slice = (size_t)rows * pitch_part;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * n8; i += (long long)gridDim.x * 256) {
@@ -304,13 +308,15 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
   const dim3 gs((unsigned)nb, (unsigned)q.batch);
   const dim3 gl(grid_of((long long)q.m * pl.np / 8, sms), (unsigned)q.batch);
   if (q.dtype == DK_F32) {
-    ortho_sumsq_kernel<DK_F32><<<gs, 256, 0, st>>>(x, per, sums);
-    ortho_load_kernel<DK_F32><<<gl, 256, 0, st>>>(x, sums, nb, (double)q.eps, q.m, q.n, pl.np, xs[0],
-                                                  xs[0] + pl.x_plane);
+    DK_CUDA_CHECK(launch_chained(ortho_sumsq_kernel<DK_F32>, gs, 256, 0, st,
+                                 x, per, sums));
+    DK_CUDA_CHECK(launch_chained(ortho_load_kernel<DK_F32>, gl, 256, 0, st,
+                                 x, sums, nb, (double)q.eps, q.m, q.n, pl.np, xs[0], xs[0] + pl.x_plane));
   } else {
-    ortho_sumsq_kernel<DK_BF16><<<gs, 256, 0, st>>>(x, per, sums);
-    ortho_load_kernel<DK_BF16><<<gl, 256, 0, st>>>(x, sums, nb, (double)q.eps, q.m, q.n, pl.np, xs[0],
-                                                   xs[0] + pl.x_plane);
+    DK_CUDA_CHECK(launch_chained(ortho_sumsq_kernel<DK_BF16>, gs, 256, 0, st,
+                                 x, per, sums));
+    DK_CUDA_CHECK(launch_chained(ortho_load_kernel<DK_BF16>, gl, 256, 0, st,
+                                 x, sums, nb, (double)q.eps, q.m, q.n, pl.np, xs[0], xs[0] + pl.x_plane));
   }
 
   const size_t es = q.dtype == DK_F32 ? 4 : 2;
@@ -320,8 +326,8 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
   const long long rows = (long long)q.batch * q.m;
   if (q.steps == 0) {
     fin.f = 1.f / kX;
-    ortho_x_kernel<<<grid_of(rows * ((q.n + 7) / 8), sms), 256, 0, st>>>(fin, nullptr, 0, 0, xs[0],
-                                                                         xs[0] + pl.x_plane, rows, pl.np);
+    DK_CUDA_CHECK(launch_chained(ortho_x_kernel, dim3(grid_of(rows * ((q.n + 7) / 8), sms)), 256, 0, st,
+                                 fin, nullptr, 0, 0, xs[0], xs[0] + pl.x_plane, rows, pl.np));
     return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
   }
 
@@ -348,13 +354,15 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
                           : g16::launch<3, false, false, BN>(ctx, X, X, p, ep, st);
     if (s != DK_OK) return s;
     sa.ks = tg.ksplit; sa.f = kA / (kX * kX); sa.poly = 0; sa.hi = am; sa.lo = am + pl.s_plane;
-    ortho_sym_kernel<<<dim3(nt, nt, (unsigned)q.batch), 256, 0, st>>>(sa);
+    DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st,
+                                 sa));
     // B
     p = gemm_params(tp, q, pl.s, pl.s, true);
     s = g16::launch<3, false, false, BN>(ctx, A, A, p, ep, st);
     if (s != DK_OK) return s;
     sa.ks = tp.ksplit; sa.f = 1.f / (kA * kA); sa.poly = 1; sa.hi = bm; sa.lo = bm + pl.s_plane;
-    ortho_sym_kernel<<<dim3(nt, nt, (unsigned)q.batch), 256, 0, st>>>(sa);
+    DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st,
+                                 sa));
     // X
     XArgs xa = fin;
     if (k + 1 < q.steps) {
@@ -369,8 +377,8 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
       s = pl.tall ? g16::launch<3, false, false, BN>(ctx, X, B, p, ex, st)
                   : g16::launch<3, false, true, BN>(ctx, B, X, p, ex, st);
       if (s != DK_OK) return s;
-      ortho_x_kernel<<<grid_of(rows * ((q.n + 7) / 8), sms), 256, 0, st>>>(xa, part, tx.ksplit, pitch_x, nullptr, nullptr,
-                                                                           rows, 0);
+      DK_CUDA_CHECK(launch_chained(ortho_x_kernel, dim3(grid_of(rows * ((q.n + 7) / 8), sms)), 256, 0, st,
+                                 xa, part, tx.ksplit, pitch_x, nullptr, nullptr, rows, 0));
     } else {
       s = pl.tall ? g16::launch<3, false, false, BN>(ctx, X, B, p, EpiX{xa}, st)
                   : g16::launch<3, false, true, BN>(ctx, B, X, p, EpiX{xa}, st);

@@ -13,6 +13,10 @@ constexpr int kMaxSms = 160;
 
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Words with which the last CTA of several finds that it is the last; zero at the start of every kernel that uses them
+// and left at zero by it.
+inline unsigned int* step_counters(const dk_ctx* ctx) { return ctx->d_step; }
+
 // Makes the context's device current for the length of a call.
 struct OnDevice {
   int prev, dev;
@@ -25,5 +29,28 @@ struct OnDevice {
     if (ok && prev != dev) cudaSetDevice(prev);
   }
 };
+
+// Programmatic dependent launch: the next kernel of the stream may be set up while this one runs (its own call of this
+// function then waits for this one's end and its writes).  At the start of kernels that follow one another closely.
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chained_launch() {
+  allow_next();
+  wait_for_previous();
+}
+template <typename... K, typename... A>
+cudaError_t launch_chained(void (*kern)(K...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
 
 }  // namespace dk

@@ -42,6 +42,7 @@ __device__ __forceinline__ bool left_out(long long t, int vocab) { return t < 0 
 __global__ void __launch_bounds__(256)
 xent_absmax_kernel(const float* __restrict__ h, const float* __restrict__ W, const int64_t* __restrict__ target,
                    const float* __restrict__ dloss, float scale, long long rows, int d, int vocab, Meta* meta) {
+  chained_launch();
   __shared__ unsigned int s[3];
   if (threadIdx.x < 3) s[threadIdx.x] = 0u;
   __syncthreads();
@@ -132,6 +133,7 @@ __device__ __forceinline__ void prep_rows(const Prep& q, int d, int dp, int voca
 }
 template <bool F32>
 __global__ void __launch_bounds__(256) xent_prep_kernel(const Prep a, const Prep b, int d, int dp, int vocab) {
+  chained_launch();
   const long long step = (long long)gridDim.x * blockDim.x, i0 = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (a.src != nullptr) prep_rows<F32>(a, d, dp, vocab, i0, step);
   if (b.src != nullptr) prep_rows<F32>(b, d, dp, vocab, i0, step);
@@ -289,6 +291,7 @@ __device__ __forceinline__ void finish_row(long long t, int vocab, float m, floa
 __global__ void __launch_bounds__(kRowThreads)
 xent_join_kernel(const float2* __restrict__ part, const float* __restrict__ tlogit, const int64_t* __restrict__ target,
                  long long rows, int slots, int vocab, float* loss, float* lse, int* status) {
+  chained_launch();
   const int lane = threadIdx.x & 31;
   const long long row = ((long long)blockIdx.x * kRowThreads + threadIdx.x) >> 5;
   if (row >= rows) return;
@@ -317,6 +320,7 @@ xent_join_kernel(const float2* __restrict__ part, const float* __restrict__ tlog
 __global__ void __launch_bounds__(kRowThreads)
 xent_slices_lse_kernel(const float* __restrict__ part, int ks, long long rows, int vocab, int pitch,
                        const int64_t* __restrict__ target, const Undo undo, float* loss, float* lse, int* status) {
+  chained_launch();
   __shared__ float sm[kRowThreads / 32], ss[kRowThreads / 32], st;
   const long long row = blockIdx.x;
   float f0, f1;
@@ -357,6 +361,7 @@ template <bool F32>
 __global__ void __launch_bounds__(256)
 xent_slices_p_kernel(const float* __restrict__ part, int ks, long long rows, int n, int pitch, const RowArgs r,
                      const Undo undo) {
+  chained_launch();
   float f0, f1;
   undo.get(f0, f1);
   const size_t slice = (size_t)rows * pitch;
@@ -390,6 +395,7 @@ template <bool F32>
 __global__ void __launch_bounds__(256)
 xent_slices_grad_kernel(const float* __restrict__ part, int ks, long long rows, int n, int pitch,
                         const EpiGrad<F32> e) {
+  chained_launch();
   float f0, f1;
   e.undo.get(f0, f1);
   const size_t slice = (size_t)rows * pitch;
@@ -507,13 +513,13 @@ dk_status prepare(Call& c, const void* h, const void* W, const int64_t* target, 
   c.undo_hw = Undo{nullptr, nullptr};
   if (F32) {
     DK_CUDA_CHECK(cudaMemsetAsync(meta, 0, sizeof(Meta), c.st));
-    xent_absmax_kernel<<<grid_of((nw + nh) / 4, c.ctx->sm_count), 256, 0, c.st>>>(
-        static_cast<const float*>(h), static_cast<const float*>(W), target, dloss, scale, q.rows, q.d, q.vocab, meta);
+    DK_CUDA_CHECK(launch_chained(xent_absmax_kernel, dim3(grid_of((nw + nh) / 4, c.ctx->sm_count)), 256, 0, c.st,
+                                 static_cast<const float*>(h), static_cast<const float*>(W), target, dloss, scale, q.rows, q.d, q.vocab, meta));
     c.undo_hw = Undo{&meta->hmax, &meta->wmax};
   }
   if (copy_h || pl.copy_w)
-    xent_prep_kernel<F32><<<grid_of(((copy_h ? nh : 0) + (pl.copy_w ? nw : 0)) / 8, c.ctx->sm_count), 256, 0, c.st>>>(
-        a, b, q.d, pl.dp, q.vocab);
+    DK_CUDA_CHECK(launch_chained(xent_prep_kernel<F32>, dim3(grid_of(((copy_h ? nh : 0) + (pl.copy_w ? nw : 0)) / 8, c.ctx->sm_count)), 256, 0, c.st,
+                                 a, b, q.d, pl.dp, q.vocab));
   c.h = Operand{copy_h ? (const void*)hh : h, hh + nh, q.rows, q.d, pl.dp, 0};
   c.w = Operand{pl.copy_w ? (const void*)wh : W, wh + nw, q.vocab, q.d, pl.dp, 0};
   return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
@@ -532,16 +538,16 @@ dk_status forward(Call& c, const int64_t* target, float* loss, float* lse) {
     const int pitch = (q.vocab + 3) / 4 * 4;
     s = g16::launch<NP, false, false, BN>(c.ctx, c.h, c.w, p, g16::EpiPartial{c.part(), pitch}, c.st);
     if (s != DK_OK) return s;
-    xent_slices_lse_kernel<<<(unsigned)q.rows, kRowThreads, 0, c.st>>>(c.part(), t.ksplit, q.rows, q.vocab, pitch,
-                                                                      target, c.undo_hw, loss, lse, status);
+    DK_CUDA_CHECK(launch_chained(xent_slices_lse_kernel, dim3((unsigned)q.rows), kRowThreads, 0, c.st,
+                                 c.part(), t.ksplit, q.rows, q.vocab, pitch, target, c.undo_hw, loss, lse, status));
   } else {
     float2* slots = reinterpret_cast<float2*>(c.ws + pl.off_slots);
     float* tl = reinterpret_cast<float*>(c.ws + pl.off_tl);
     s = g16::launch<NP, false, false, BN>(c.ctx, c.h, c.w, p, EpiLse{slots, tl, target, c.undo_hw}, c.st);
     if (s != DK_OK) return s;
     const int nslots = (q.vocab + BN / 2 - 1) / (BN / 2);
-    xent_join_kernel<<<(unsigned)((q.rows * 32 + kRowThreads - 1) / kRowThreads), kRowThreads, 0, c.st>>>(
-        slots, tl, target, q.rows, nslots, q.vocab, loss, lse, status);
+    DK_CUDA_CHECK(launch_chained(xent_join_kernel, dim3((unsigned)((q.rows * 32 + kRowThreads - 1) / kRowThreads)), kRowThreads, 0, c.st,
+                                 slots, tl, target, q.rows, nslots, q.vocab, loss, lse, status));
   }
   return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
 }
@@ -579,8 +585,8 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
       const int pitch = (nv + 3) / 4 * 4;
       s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
-      xent_slices_p_kernel<F32><<<grid_of(T * pitch_p / 8, c.ctx->sm_count), 256, 0, c.st>>>(
-          c.part(), t.ksplit, T, nv, pitch, r, c.undo_hw);
+      DK_CUDA_CHECK(launch_chained(xent_slices_p_kernel<F32>, dim3(grid_of(T * pitch_p / 8, c.ctx->sm_count)), 256, 0, c.st,
+                                 c.part(), t.ksplit, T, nv, pitch, r, c.undo_hw));
     } else {
       s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, EpiP<F32>{r, c.undo_hw}, c.st);
       if (s != DK_OK) return s;
@@ -595,8 +601,8 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
       const int pitch = (q.d + 3) / 4 * 4;
       s = g16::launch<NP, false, true, BN>(c.ctx, pop, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
-      xent_slices_grad_kernel<F32><<<grid_of(T * q.d, c.ctx->sm_count), 256, 0, c.st>>>(c.part(), t.ksplit, T, q.d,
-                                                                                       pitch, e);
+      DK_CUDA_CHECK(launch_chained(xent_slices_grad_kernel<F32>, dim3(grid_of(T * q.d, c.ctx->sm_count)), 256, 0, c.st,
+                                 c.part(), t.ksplit, T, q.d, pitch, e));
     } else {
       s = g16::launch<NP, false, true, BN>(c.ctx, pop, w, p, e, c.st);
       if (s != DK_OK) return s;
@@ -610,8 +616,8 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
       const int pitch = (q.d + 3) / 4 * 4;
       s = g16::launch<NP, true, true, BN>(c.ctx, pop, c.h, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
-      xent_slices_grad_kernel<F32><<<grid_of((long long)nv * q.d, c.ctx->sm_count), 256, 0, c.st>>>(
-          c.part(), t.ksplit, nv, q.d, pitch, e);
+      DK_CUDA_CHECK(launch_chained(xent_slices_grad_kernel<F32>, dim3(grid_of((long long)nv * q.d, c.ctx->sm_count)), 256, 0, c.st,
+                                 c.part(), t.ksplit, nv, q.d, pitch, e));
     } else {
       s = g16::launch<NP, true, true, BN>(c.ctx, pop, c.h, p, e, c.st);
       if (s != DK_OK) return s;
