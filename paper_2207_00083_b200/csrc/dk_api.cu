@@ -943,7 +943,11 @@ dk_status dk_device_status(dk_ctx* ctx, int32_t* status) {
   int v = 0;
   DK_CUDA_CHECK(cudaDeviceSynchronize());
   DK_CUDA_CHECK(cudaMemcpy(&v, ctx_status_word(ctx), sizeof(int), cudaMemcpyDeviceToHost));
-  if (v != 0) DK_CUDA_CHECK(cudaMemset(ctx_status_word(ctx), 0, sizeof(int)));
+  if (v != 0) {
+    DK_CUDA_CHECK(cudaMemset(ctx_status_word(ctx), 0, sizeof(int)));
+    // a call that gave up may have left its counters as they were
+    DK_CUDA_CHECK(cudaMemset(ctx->d_step, 0, kStepCounters * sizeof(unsigned int)));
+  }
   *status = v;
   return DK_OK;
 }

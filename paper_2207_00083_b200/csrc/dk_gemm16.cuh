@@ -305,6 +305,207 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
 }
 
 // ---------------------------------------------------------------------------
+// Few tiles: 128 x 128 tiles of single CTAs, one tile per cluster of CS CTAs that share its contraction.  Each CTA
+// sums its slice, leaves the sums in shared memory, and takes CS-th of the tile's columns, whose slices it adds up over
+// distributed shared memory in the slices' order.  Nothing goes through global memory and no second kernel joins it.
+// ---------------------------------------------------------------------------
+constexpr int SMALL = 128;
+
+__device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+template <bool MN, int NROWS>
+__device__ __forceinline__ void load_tile_cta(unsigned char* dst, const CUtensorMap* map, uint64_t* bar, int r0, int k0,
+                                              int batch) {
+  if constexpr (MN) {
+#pragma unroll
+    for (int i = 0; i < NROWS / 64; ++i) tc::tma_load_3d(dst + i * 8192, map, bar, (r0 + 64 * i) * 2, k0, batch);
+  } else {
+    tc::tma_load_3d(dst, map, bar, k0 * 2, r0, batch);
+  }
+}
+
+template <int NPROD, bool AMN, bool BMN, int CS, class Epi>
+__global__ void __launch_bounds__(kThreadsG, 1)
+gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constant__ CUtensorMap map_a_lo,
+                    const __grid_constant__ CUtensorMap map_b_hi, const __grid_constant__ CUtensorMap map_b_lo,
+                    const Params p, const Epi epi) {
+  constexpr int OP = SMALL * 128;                  // bytes of one operand plane in a stage
+  constexpr int PL = NPROD == 3 ? 2 : 1;
+  constexpr int STAGE = 2 * PL * OP;
+  constexpr int NC = SMALL / 2;                    // columns a thread holds (8 epilogue warps: 4 x 32 rows, 2 halves)
+  constexpr int NH = NC / CS;                      // columns it finishes
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                         ~static_cast<uintptr_t>(1023));
+  unsigned char* ctrl = smem + (size_t)p.nstages * STAGE;
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(ctrl);
+  uint64_t* empty_bar = full_bar + tc::kMaxStages;
+  uint64_t* tfull_bar = empty_bar + tc::kMaxStages;
+  uint64_t* tempty_bar = tfull_bar + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty_bar + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x % CS;
+  int batch, ks, mt, nt;
+  item_tile(p, blockIdx.x / CS, batch, ks, mt, nt);
+  const int kb_lo = min(p.KB, rank * p.kb_per_split), kb_hi = min(p.KB, kb_lo + p.kb_per_split);
+
+  allow_next();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.nstages; ++s) { tc::mbar_init(full_bar + s, 1); tc::mbar_init(empty_bar + s, 1); }
+    for (int b = 0; b < 2; ++b) { tc::mbar_init(tfull_bar + b, 1); tc::mbar_init(tempty_bar + b, kEpi); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(256u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  wait_for_previous();
+
+  const int quad = warp & 3, half = (warp - 4) >> 2;
+  const int row = quad * 32 + lane;
+  float acc[NC];
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0, issued = 0;
+      uint32_t phase = 0;
+      const int m0 = mt * SMALL, n0 = nt * SMALL;
+      for (int kb = kb_lo; kb < kb_hi; ++kb) {
+        if (!tc::mbar_wait(empty_bar + stage, phase ^ 1u, abort_flag, p.spin_cap)) break;
+        tc::mbar_expect_tx(full_bar + stage, (uint32_t)STAGE);
+        if (issued++ == p.withhold) break;
+        unsigned char* st = smem + (size_t)stage * STAGE;
+        load_tile_cta<AMN, SMALL>(st, &map_a_hi, full_bar + stage, m0, kb * BK, batch);
+        load_tile_cta<BMN, SMALL>(st + PL * OP, &map_b_hi, full_bar + stage, n0, kb * BK, batch);
+        if constexpr (NPROD == 3) {
+          load_tile_cta<AMN, SMALL>(st + OP, &map_a_lo, full_bar + stage, m0, kb * BK, batch);
+          load_tile_cta<BMN, SMALL>(st + PL * OP + OP, &map_b_lo, full_bar + stage, n0, kb * BK, batch);
+        }
+        if (++stage == p.nstages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = (1u << 4) | ((uint32_t)p.bf16 << 7) | ((uint32_t)p.bf16 << 10) | ((AMN ? 1u : 0u) << 15) |
+                             ((BMN ? 1u : 0u) << 16) | ((uint32_t)(SMALL >> 3) << 17) | ((uint32_t)(SMALL >> 4) << 24);
+      constexpr uint64_t STEP_A = AMN ? 128 : 2, STEP_B = BMN ? 128 : 2, LO = OP / 16;
+      int stage = 0;
+      uint32_t phase = 0, acc_it = 0;
+      bool alive = true;
+      for (int kb = kb_lo; alive && kb < kb_hi; kb += p.chunk, ++acc_it) {
+        const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
+        if (!tc::mbar_wait(tempty_bar + buf, aphase ^ 1u, abort_flag, p.spin_cap)) break;
+        tc::tc_fence_after();
+        const uint32_t d_tmem = tmem_base + buf * 128u;
+        const int kb_end = min(kb_hi, kb + p.chunk);
+        for (int k = kb; k < kb_end; ++k) {
+          if (!tc::mbar_wait(full_bar + stage, phase, abort_flag, p.spin_cap)) { alive = false; break; }
+          tc::tc_fence_after();
+          const uint32_t st = smem_u32(smem + (size_t)stage * STAGE);
+          const uint64_t a_hi = AMN ? desc_mn(st) : tc::make_desc<128>(st);
+          const uint64_t b_hi = BMN ? desc_mn(st + PL * OP) : tc::make_desc<128>(st + PL * OP);
+#pragma unroll
+          for (int kk = 0; kk < BK / 16; ++kk) {
+            mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, (k == kb && kk == 0) ? 0u : 1u);
+            if constexpr (NPROD == 3) {
+              mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + LO + kk * STEP_B, idesc, 1u);
+              mma_f16(d_tmem, a_hi + LO + kk * STEP_A, b_hi + kk * STEP_B, idesc, 1u);
+            }
+          }
+          tc::tc_commit(empty_bar + stage);
+          if (++stage == p.nstages) { stage = 0; phase ^= 1u; }
+        }
+        if (alive) tc::tc_commit(tfull_bar + buf);
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    uint32_t acc_it = 0;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) acc[j] = 0.f;
+    for (int kb = kb_lo; kb < kb_hi; kb += p.chunk, ++acc_it) {
+      const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
+      if (!tc::mbar_wait(tfull_bar + buf, aphase, abort_flag, p.spin_cap)) break;
+      tc::tc_fence_after();
+      const uint32_t t = tmem_base + buf * 128u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NC);
+#pragma unroll
+      for (int c = 0; c < NC; c += 32) {
+        float tmp[32];
+        ld32(t + (uint32_t)c, tmp);
+        tc::tc_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) acc[c + j] += tmp[j];
+      }
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(tempty_bar + buf);
+    }
+    if constexpr (CS > 1) {
+      // [column][row]: every product of this CTA is done, its stages are free
+      float* red = reinterpret_cast<float*>(smem);
+#pragma unroll
+      for (int j = 0; j < NC; ++j) red[(half * NC + j) * SMALL + row] = acc[j];
+    }
+  }
+  const bool failed = __syncthreads_or(*abort_flag != 0);
+  if constexpr (CS > 1) tc::cluster_sync_all();
+  if (warp >= 4 && !failed) {
+    const int c0 = rank * (SMALL / CS) + half * NH;        // first of the columns this thread finishes
+    float fin[NH];
+    if constexpr (CS > 1) {
+#pragma unroll
+      for (int j = 0; j < NH; ++j) fin[j] = 0.f;
+      const uint32_t mine = smem_u32(smem) + (uint32_t)((c0 * SMALL + row) * 4);
+#pragma unroll
+      for (int r = 0; r < CS; ++r) {
+        const uint32_t from = tc::mapa_shared(mine, (uint32_t)r);
+#pragma unroll
+        for (int j = 0; j < NH; ++j) fin[j] += ld_cluster(from + (uint32_t)(j * SMALL * 4));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NH; ++j) fin[j] = acc[j];
+    }
+    epi(p, fin, batch, 0, mt * SMALL + row, nt * SMALL + c0);
+  }
+  // ---------------- teardown ----------------
+  tc::tc_fence_before();
+  __syncthreads();
+  if (failed) {
+    if (threadIdx.x == 0 && p.status != nullptr) atomicExch(p.status, (int)DK_ERR_TIMEOUT);
+    for (int i = 0; i < 64; ++i) __nanosleep(16384);
+    __syncthreads();
+  }
+  if constexpr (CS > 1) tc::cluster_sync_all();      // no CTA leaves while its sums are being read
+  if (warp == 1) {
+    tc::tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------
 // epilogues shared by the operators
 // ---------------------------------------------------------------------------
 
@@ -379,25 +580,58 @@ struct EpiPartial {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
+// How a product is computed: `cs` = 0: 256 x 256 tiles of CTA pairs, `ksplit` slices of the contraction with partial
+// sums in global memory; cs > 0: 128 x 128 tiles, clusters of cs CTAs sharing the contraction.
+constexpr int kSmallCtas = 8 * kMaxSms;      // most CTAs of a product in small tiles
 struct Tiling {
+  int cs;
   int MT, NT, tiles, KB, ksplit, kb_per_split;
 };
-// ksplit > 1 when the tiles alone leave pairs idle: enough slices that every pair has one, of at least `min_kb`
-// stages each
-inline Tiling plan(long long M, long long N, long long K, int BN, int nbatch, bool sym, int pairs, int min_kb) {
-  Tiling t;
-  t.MT = (int)((M + TILE_M - 1) / TILE_M);
-  t.NT = (int)((N + BN - 1) / BN);
-  t.tiles = sym ? t.MT * (t.MT + 1) / 2 : t.MT * t.NT;
-  t.KB = (int)((K + BK - 1) / BK);
-  int want = pairs / (t.tiles * nbatch);
-  if (want < 1) want = 1;
-  int per = (t.KB + want - 1) / want;
-  if (per < min_kb) per = min_kb;
-  if (per > t.KB) per = t.KB;
-  t.kb_per_split = per;
-  t.ksplit = (t.KB + per - 1) / per;
-  return t;
+
+// Cost in cycles of either way, from what was measured: a stage (64 contraction elements) of the pair's tile takes 512
+// cycles per product, of the small tile 256, but the small tile's operands arrive at ~50 bytes per cycle and SM, which
+// is what binds it (16 KiB per operand plane); some 9000 cycles go to a launch's start, fill and epilogue, 6000 more to
+// joining a cluster's slices, 20000 to the partial sums' way through global memory and a second kernel.  Clusters of
+// four and eight do not tile the GPCs: 33 and 15 of them are resident at once on 148 SMs.
+inline Tiling plan(long long M, long long N, long long K, int nbatch, bool sym, int sms, int nprod) {
+  Tiling best = {};
+  double least = 0;
+  const int KB = (int)((K + BK - 1) / BK);
+  for (int cs = 0; cs <= 8; cs = cs ? 2 * cs : 1) {
+    const int tm = cs ? SMALL : TILE_M;
+    Tiling t = {};
+    t.cs = cs;
+    const long long MT = (M + tm - 1) / tm, NT = (N + tm - 1) / tm;
+    const long long tiles = sym ? MT * (MT + 1) / 2 : MT * NT;
+    if (tiles * nbatch >= (1LL << 26)) { if (cs) continue; }
+    t.MT = (int)MT; t.NT = (int)NT; t.tiles = (int)tiles;
+    t.KB = KB;
+    double cost;
+    if (cs == 0) {
+      const int pairs = sms / 2;
+      int want = (int)(pairs / (tiles * nbatch));
+      if (want < 1) want = 1;
+      int per = (KB + want - 1) / want;
+      if (per < 4) per = 4;
+      if (per > KB) per = KB;
+      t.kb_per_split = per;
+      t.ksplit = (KB + per - 1) / per;
+      const double waves = (double)((tiles * nbatch * t.ksplit + pairs - 1) / pairs);
+      cost = waves * per * 512.0 * nprod + 9000.0 + (t.ksplit > 1 ? 20000.0 : 0.0);
+    } else {
+      if (cs > 1 && KB < 2 * cs) continue;             // at least two stages each
+      const long long ctas = tiles * nbatch * cs;
+      if (ctas > kSmallCtas) continue;
+      const long long resident = cs <= 2 ? sms / cs : cs == 4 ? sms * 33 / 148 : sms * 15 / 148;
+      const double waves = (double)((tiles * nbatch + resident - 1) / resident);
+      t.kb_per_split = (KB + cs - 1) / cs;
+      t.ksplit = 1;
+      const double stage = (nprod == 3 ? 4 : 2) * 16384.0 / 50.0;
+      cost = waves * (t.kb_per_split * (stage > 256.0 * nprod ? stage : 256.0 * nprod) + 9000.0 + (cs > 1 ? 6000.0 : 0.0));
+    }
+    if (cs == 0 || cost < least) { least = cost; best = t; }
+  }
+  return best;
 }
 
 inline bool make_map(const dk_ctx* ctx, CUtensorMap* m, const void* base, const Operand& o, int nbatch, bool mn,
@@ -414,6 +648,52 @@ inline bool make_map(const dk_ctx* ctx, CUtensorMap* m, const void* base, const 
 struct Prepared {
   bool done[64];
 };
+
+template <int NPROD, bool AMN, bool BMN, int CS, class Epi>
+dk_status launch_small(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, const Epi& epi, cudaStream_t st) {
+  static Prepared prep = {};
+  CUtensorMap ma, mal, mb, mbl;
+  if (!make_map(ctx, &ma, A.hi, A, p.nbatch, AMN, SMALL) || !make_map(ctx, &mb, B.hi, B, p.nbatch, BMN, SMALL))
+    return DK_ERR_CUDA;
+  mal = ma; mbl = mb;
+  if (NPROD == 3 && (!make_map(ctx, &mal, A.lo, A, p.nbatch, AMN, SMALL) ||
+                     !make_map(ctx, &mbl, B.lo, B, p.nbatch, BMN, SMALL)))
+    return DK_ERR_CUDA;
+  constexpr int STAGE = (NPROD == 3 ? 4 : 2) * SMALL * 128;
+  constexpr int CTRL = (2 * tc::kMaxStages + 4) * 8 + 16;
+  p.nstages = NPROD == 3 ? 3 : 6;
+  const int smem = p.nstages * STAGE + CTRL + 1024;
+  if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
+  auto kern = gemm16_small_kernel<NPROD, AMN, BMN, CS, Epi>;
+  if (ctx->device >= 64) return DK_ERR_UNSUPPORTED;
+  if (!prep.done[ctx->device]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+      return DK_ERR_CUDA;
+    prep.done[ctx->device] = true;
+  }
+  p.ksplit = 1;
+  p.nitems = p.nbatch * p.tiles;
+  p.group = p.MT < 16 ? p.MT : 16;
+  p.spin_cap = (unsigned)ctx->opt.v[DK_OPT_SPIN_LIMIT];
+  p.withhold = ctx->opt.v[DK_OPT_TEST_WITHHOLD];
+  ctx->opt.v[DK_OPT_TEST_WITHHOLD] = -1;
+  p.status = device_status_word(ctx);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.nitems * CS));
+  cfg.blockDim = dim3(kThreadsG);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = CS;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = CS > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, ma, mal, mb, mbl, p, epi) == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+}
 
 // p: MT, NT, nbatch, sym, tiles, KB, ksplit, kb_per_split, M, N, chunk are set by the caller
 template <int NPROD, bool AMN, bool BMN, int BN, class Epi>
@@ -454,6 +734,20 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
   return launch_chained(kern, dim3(2 * (unsigned)pairs), kThreadsG, (size_t)smem, st, ma, mal, mb, mbl, p, epi) == cudaSuccess
              ? DK_OK
              : DK_ERR_CUDA;
+}
+
+// The product by the way `t` says; `epi` finishes its elements (t.cs > 0 or t.ksplit == 1).
+template <int NPROD, bool AMN, bool BMN, class Epi>
+dk_status product(dk_ctx* ctx, const Tiling& t, const Operand& A, const Operand& B, const Params& p, const Epi& epi,
+                  cudaStream_t st) {
+  switch (t.cs) {
+    case 0: return launch<NPROD, AMN, BMN, 256, Epi>(ctx, A, B, p, epi, st);
+    case 1: return launch_small<NPROD, AMN, BMN, 1, Epi>(ctx, A, B, p, epi, st);
+    case 2: return launch_small<NPROD, AMN, BMN, 2, Epi>(ctx, A, B, p, epi, st);
+    case 4: return launch_small<NPROD, AMN, BMN, 4, Epi>(ctx, A, B, p, epi, st);
+    case 8: return launch_small<NPROD, AMN, BMN, 8, Epi>(ctx, A, B, p, epi, st);
+  }
+  return DK_ERR_UNSUPPORTED;
 }
 
 }  // namespace g16

@@ -19,7 +19,7 @@ using g16::Operand;
 using g16::Params;
 
 constexpr int BN = 256;
-constexpr int kSumBlocks = 256;                 // partial sums of squares per matrix
+constexpr int kSumBlocks = 1184;                 // partial sums of squares per matrix
 // powers of two of the stored terms: |X| < 8, |A| < 8, |B| < 32
 constexpr float kX = 8192.f, kA = 8192.f, kB = 2048.f;
 
@@ -34,11 +34,38 @@ template <int DT>
 __global__ void __launch_bounds__(256) ortho_sumsq_kernel(const void* x, long long per, double* part) {
   chained_launch();
   __shared__ double s[8];
+  constexpr int V = DT == DK_F32 ? 4 : 8;              // elements of 16 bytes
+  constexpr int U = 4;                                 // loads in flight
   const size_t base = (size_t)blockIdx.y * per;
+  // (every matrix but the first may start off a 16-byte boundary)
+  const long long head = (long long)((V - base % V) % V) < per ? (long long)((V - base % V) % V) : per;
+  const long long vecs = (per - head) / V;
+  const uint4* xv = reinterpret_cast<const uint4*>(static_cast<const char*>(x) + (base + head) * (16 / V));
   double t = 0.0;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < per; i += (long long)gridDim.x * 256) {
-    const double v = (double)load1<DT>(x, base + i);
-    t = fma(v, v, t);
+  auto add = [&](double v) { t = fma(v, v, t); };
+  const long long step = (long long)gridDim.x * 256;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < vecs; i += U * step) {
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = i + u * step < vecs ? __ldg(xv + i + u * step) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (DT == DK_F32) {
+          add((double)__uint_as_float(w[k]));
+        } else {
+          add((double)__uint_as_float(w[k] << 16));
+          add((double)__uint_as_float(w[k] & 0xffff0000u));
+        }
+      }
+    }
+  }
+  if (blockIdx.x == 0) {
+    if ((long long)threadIdx.x < head) add((double)load1<DT>(x, base + threadIdx.x));
+    const long long rest = head + vecs * V + threadIdx.x;
+    if (rest < per && (long long)threadIdx.x < V) add((double)load1<DT>(x, base + rest));
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
@@ -139,6 +166,56 @@ __global__ void __launch_bounds__(256) ortho_sym_kernel(const SymArgs q) {
   }
 }
 
+// The same from a product that is finished where it is formed (tiles of the small kernel): this thread's NH columns of
+// its row, on or below the diagonal, and their mirror images.
+struct EpiSym {
+  SymArgs q;
+  template <int NH>
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int, int row,
+                                             int col0) const {
+    if (row >= q.s || col0 >= q.s) return;
+    const size_t plane = (size_t)batch * q.s * q.pitch;
+    const size_t at = plane + (size_t)row * q.pitch + col0;
+    const int count = min(NH, q.s - col0);
+#pragma unroll
+    for (int j = 0; j < NH; j += 8) {
+      // (col0 and the pitch are multiples of 8; columns behind s are read as what an earlier product left there, and
+      // not used)
+      uint4 ah = make_uint4(0u, 0u, 0u, 0u), al = ah;
+      if (q.poly && j < count) {
+        ah = *reinterpret_cast<const uint4*>(q.a_hi + at + j);
+        al = *reinterpret_cast<const uint4*>(q.a_lo + at + j);
+      }
+      const __half2* h2 = reinterpret_cast<const __half2*>(&ah);
+      const __half2* l2 = reinterpret_cast<const __half2*>(&al);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        float v = acc[j + k] * q.f;
+        if (q.poly) {
+          const float2 h = __half22float2(h2[k / 2]), l = __half22float2(l2[k / 2]);
+          const float av = (k & 1 ? h.y + l.y : h.x + l.x) * (1.f / kA);
+          v = fmaf(q.c, v, q.b * av);
+          if (col0 + j + k == row) v += q.a;
+          v *= kB;
+        }
+        acc[j + k] = j + k < count ? v : 0.f;
+      }
+    }
+    const bool below = col0 + NH - 1 <= row;       // all of them on or below the diagonal
+    if (below) g16::store_planes<NH>(q.hi + at, q.lo + at, acc, count);
+#pragma unroll
+    for (int j = 0; j < NH; ++j) {
+      if (j < count && col0 + j <= row) {
+        const __half h = __float2half_rn(acc[j]), l = __float2half_rn(acc[j] - __half2float(h));
+        if (!below) { q.hi[at + j] = h; q.lo[at + j] = l; }
+        const size_t m = plane + (size_t)(col0 + j) * q.pitch + row;
+        q.hi[m] = h;
+        q.lo[m] = l;
+      }
+    }
+  }
+};
+
 // the result of a step: the next X as two terms (hi given), or the update itself
 struct XArgs {
   __half* hi;
@@ -232,6 +309,363 @@ ortho_x_kernel(const XArgs a, const float* part, int ks, int pitch_part, const _
 }
 
 // ---------------------------------------------------------------------------
+// Short sides of at most 128: the whole call in one kernel.  What bounds such matrices is not the products but 15
+// launches of them, one after the other.  Here a gang of co-resident CTAs holds the matrix, each `C` columns (of the
+// wide orientation) as two fp16 terms in shared memory for all steps.  Per step a CTA forms its columns' share of A on
+// the tensor core and leaves it in global memory; the gang meets; every CTA adds the shares up (gangs of more than
+// kDirect first add up a slice each and meet again), forms B = a I + b A + c A A by itself, and multiplies its own
+// columns.  One block layout serves all three products: [128 rows][64 columns], 128-byte rows swizzled, is the K-major
+// operand of X X^T and the MN-major operand of B X.
+// ---------------------------------------------------------------------------
+constexpr int kResThreads = 256;
+constexpr int kDirect = 8;
+constexpr int kBlock = 128 * 128;            // bytes of one [128][64] fp16 block
+
+struct ResArgs {
+  const void* x;
+  void* out;
+  double* sums;            // [batch][gang]
+  float* part;             // [batch][gang][128 columns][128 rows]
+  float* asum;             // [batch][128][128]
+  unsigned int* count;     // [batch], zero at the start and at the end
+  int m, n, s, L, tall, steps, C, gang;
+  float a, b, c, scale, keep;
+  double eps;
+  unsigned int spin_cap;
+  int* status;
+};
+
+__device__ __forceinline__ uint64_t desc_mn_blocks(uint32_t smem_addr) {      // as g16::desc_mn, blocks of 128 rows
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr >> 4) & 0x3FFF);
+  d |= (uint64_t)(kBlock >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+// byte of (row, column) in consecutive [128][64] blocks
+__device__ __forceinline__ uint32_t block_at(int row, int col) {
+  return (uint32_t)((col >> 6) * kBlock + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4) + (col & 7) * 2);
+}
+// eight consecutive columns (col a multiple of 8) as two terms
+__device__ __forceinline__ void put8(unsigned char* hi, unsigned char* lo, int row, int col, const float* v) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const __half2 t = __floats2half2_rn(v[2 * q], v[2 * q + 1]);
+    h[q] = *reinterpret_cast<const uint32_t*>(&t);
+    l[q] = g16::pack_f16(v[2 * q] - __low2float(t), v[2 * q + 1] - __high2float(t));
+  }
+  const uint32_t at = block_at(row, col);
+  *reinterpret_cast<uint4*>(hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<uint4*>(lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const ResArgs q) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int failed;
+  __shared__ double dsum[kResThreads / 32];
+  unsigned char* const base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                               ~static_cast<uintptr_t>(1023));
+  const int nblk = q.C / 64;
+  unsigned char* const xh = base;
+  unsigned char* const xl = xh + nblk * kBlock;
+  unsigned char* const ah = xl + nblk * kBlock;
+  unsigned char* const al = ah + 2 * kBlock;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
+  const int mat = blockIdx.x / q.gang, g = blockIdx.x % q.gang;
+  const int c0 = g * q.C, cols = min(q.C, q.L - c0);
+  const size_t mbase = (size_t)mat * q.m * q.n;
+
+  chained_launch();
+  if (threadIdx.x == 0) {
+    tc::mbar_init(&bar, 1);
+    failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&tmem_slot)),
+                 "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = tmem_slot, lanes = (uint32_t)(quad * 32) << 16;
+
+  unsigned int epoch = 0;
+  uint32_t phase = 0;
+  // the gang's CTAs meet; what they wrote to global memory before is visible after
+  auto meet = [&]() -> bool {
+    ++epoch;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      __threadfence();
+      atomicAdd(q.count + mat, 1u);
+      const unsigned int target = epoch * (unsigned int)q.gang;
+      bool ok = false;
+      for (unsigned int i = 0; i < q.spin_cap; ++i) {
+        unsigned int v;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(q.count + mat) : "memory");
+        if (v >= target) { ok = true; break; }
+      }
+      if (!ok) failed = 1;
+    }
+    __syncthreads();
+    return failed == 0;
+  };
+  // all products issued so far are complete
+  auto products_done = [&]() -> bool {
+    bool ok = tc::mbar_wait(&bar, phase, &failed, q.spin_cap);
+    phase ^= 1u;
+    tc::tc_fence_after();
+    return !__syncthreads_or(!ok);
+  };
+  auto operands_ready = [&]() {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+  };
+
+  // ---- the columns, brought to |X|_F = 1 ----
+  // position of this CTA's i-th element: contiguous in memory along consecutive i
+  const int count = q.s * cols;
+  auto element = [&](int i, int& r, int& c) -> size_t {
+    if (q.tall) {
+      c = i / q.s; r = i - c * q.s;
+      return mbase + (size_t)(c0 + c) * q.n + r;
+    }
+    r = i / cols; c = i - r * cols;
+    return mbase + (size_t)r * q.n + c0 + c;
+  };
+  {
+    double t = 0.0;
+    for (int i = threadIdx.x; i < count; i += 8 * kResThreads) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        int r, c;
+        v[u] = i + u * kResThreads < count ? load1<DT>(q.x, element(i + u * kResThreads, r, c)) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) t = fma((double)v[u], (double)v[u], t);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (lane == 0) dsum[warp] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int i = 1; i < kResThreads / 32; ++i) t += dsum[i];
+      __stcg(q.sums + (size_t)mat * q.gang + g, t);
+    }
+    // meanwhile: rows and columns that do not exist are zero
+    for (int i = threadIdx.x; i < 2 * nblk * kBlock / 16; i += kResThreads)
+      reinterpret_cast<uint4*>(xh)[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+  bool alive = meet();
+  if (alive) {
+    double t = 0.0;
+    for (int i = 0; i < q.gang; ++i) t += __ldcg(q.sums + (size_t)mat * q.gang + i);
+    const float f = (float)((double)kX / (sqrt(t) + q.eps));
+    for (int i = threadIdx.x; i < count; i += 8 * kResThreads) {
+      float v[8];
+      uint32_t at[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        int r = 0, c = 0;
+        const bool in = i + u * kResThreads < count;
+        v[u] = in ? load1<DT>(q.x, element(i + u * kResThreads, r, c)) * f : 0.f;
+        at[u] = block_at(r, c);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (i + u * kResThreads < count) {
+          const __half h = __float2half_rn(v[u]);
+          *reinterpret_cast<__half*>(xh + at[u]) = h;
+          *reinterpret_cast<__half*>(xl + at[u]) = __float2half_rn(v[u] - __half2float(h));
+        }
+      }
+    }
+  }
+
+  constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);      // fp16, 128 x 128
+  const uint32_t idesc_x = (1u << 4) | (1u << 16) | ((uint32_t)(q.C >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+  const uint32_t uxh = tc::smem_u32(xh), uxl = tc::smem_u32(xl), uah = tc::smem_u32(ah), ual = tc::smem_u32(al);
+  const size_t mine = ((size_t)mat * q.gang + g) * 128 * 128;
+  for (int step = 0; alive && step < q.steps; ++step) {
+    // ---- this CTA's share of A: two blocks (128 columns) per accumulator ----
+    operands_ready();
+    if (threadIdx.x == 0) {
+      for (int k = 0; k < nblk; ++k) {
+        const uint64_t h = tc::make_desc<128>(uxh + k * kBlock), l = tc::make_desc<128>(uxl + k * kBlock);
+        const uint32_t d = tmem + (uint32_t)(k >> 1) * 128u;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          g16::mma_f16(d, h + 2 * kk, h + 2 * kk, idesc, ((k & 1) | kk) ? 1u : 0u);
+          g16::mma_f16(d, h + 2 * kk, l + 2 * kk, idesc, 1u);
+          g16::mma_f16(d, l + 2 * kk, h + 2 * kk, idesc, 1u);
+        }
+      }
+      tc::tc_commit(&bar);
+    }
+    if (!products_done()) { alive = false; break; }
+    float A[64];
+#pragma unroll
+    for (int c = 0; c < 64; c += 32) {
+      g16::ld32(tmem + lanes + (uint32_t)(half * 64 + c), A + c);
+      tc::tc_wait_ld();
+      if (nblk > 2) {
+        float t[32];
+        g16::ld32(tmem + lanes + (uint32_t)(128 + half * 64 + c), t);
+        tc::tc_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) A[c + j] += t[j];
+      }
+    }
+    if (q.gang > 1) {
+      if (row < q.s) {
+#pragma unroll
+        for (int j = 0; j < 64; ++j)
+          if (half * 64 + j < q.s) __stcg(q.part + mine + (half * 64 + j) * 128 + row, A[j]);
+      }
+      if (!meet()) { alive = false; break; }
+      const float* shares = q.part + (size_t)mat * q.gang * 128 * 128;
+      int parts = q.gang;
+      if (q.gang > kDirect) {
+        // each CTA adds up its slice of the elements (those below s), in the shares' order
+        float* sum = q.asum + (size_t)mat * 128 * 128;
+        const int all = 128 * q.s, per = (all + q.gang - 1) / q.gang;
+        for (int i = g * per + threadIdx.x; i < min(all, (g + 1) * per); i += kResThreads) {
+          if ((i & 127) >= q.s) continue;
+          float t = 0.f;
+#pragma unroll 8
+          for (int k = 0; k < q.gang; ++k) t += __ldcg(shares + (size_t)k * 128 * 128 + i);
+          __stcg(sum + i, t);
+        }
+        if (!meet()) { alive = false; break; }
+        shares = sum;
+        parts = 1;
+      }
+#pragma unroll
+      for (int j = 0; j < 64; ++j) A[j] = 0.f;
+      // (every CTA's share has room for 128 x 128: reading past s costs less than branching around it)
+      const float* from = shares + half * 64 * 128 + row;
+      for (int k = 0; k < parts; ++k, from += 128 * 128) {
+#pragma unroll
+        for (int c = 0; c < 64; c += 16) {
+          float t[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) t[j] = __ldcg(from + (c + j) * 128);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) A[c + j] += row < q.s && half * 64 + c + j < q.s ? t[j] : 0.f;
+        }
+      }
+    }
+    // ---- A's terms, A A, B's terms in their place ----
+#pragma unroll
+    for (int j = 0; j < 64; j += 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) A[j + k] *= kA / (kX * kX);
+      put8(ah, al, row, half * 64 + j, A + j);
+    }
+    operands_ready();
+    if (threadIdx.x == 0) {
+      for (int k = 0; k < 2; ++k) {
+        const uint64_t h = tc::make_desc<128>(uah + k * kBlock), l = tc::make_desc<128>(ual + k * kBlock);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          g16::mma_f16(tmem, h + 2 * kk, h + 2 * kk, idesc, (k | kk) ? 1u : 0u);
+          g16::mma_f16(tmem, h + 2 * kk, l + 2 * kk, idesc, 1u);
+          g16::mma_f16(tmem, l + 2 * kk, h + 2 * kk, idesc, 1u);
+        }
+      }
+      tc::tc_commit(&bar);
+    }
+    if (!products_done()) { alive = false; break; }
+#pragma unroll
+    for (int c = 0; c < 64; c += 32) {
+      float t[32];
+      g16::ld32(tmem + lanes + (uint32_t)(half * 64 + c), t);
+      tc::tc_wait_ld();
+#pragma unroll
+      for (int j = 0; j < 32; j += 8) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          v[k] = fmaf(q.c, t[j + k] * (1.f / (kA * kA)), q.b * (A[c + j + k] * (1.f / kA)));
+          if (half * 64 + c + j + k == row) v[k] += q.a;
+          v[k] *= kB;
+        }
+        put8(ah, al, row, half * 64 + c + j, v);
+      }
+    }
+    // ---- this CTA's columns of B X ----
+    operands_ready();
+    if (threadIdx.x == 0) {
+      const uint64_t xhd = desc_mn_blocks(uxh), xld = desc_mn_blocks(uxl);
+      for (int k = 0; k < 8; ++k) {          // 16 rows of X each
+        const uint64_t bh = tc::make_desc<128>(uah + (k >> 2) * kBlock) + 2 * (k & 3);
+        const uint64_t bl = tc::make_desc<128>(ual + (k >> 2) * kBlock) + 2 * (k & 3);
+        g16::mma_f16(tmem + 256u, bh, xhd + 128 * k, idesc_x, k ? 1u : 0u);
+        g16::mma_f16(tmem + 256u, bh, xld + 128 * k, idesc_x, 1u);
+        g16::mma_f16(tmem + 256u, bl, xhd + 128 * k, idesc_x, 1u);
+      }
+      tc::tc_commit(&bar);
+    }
+    if (!products_done()) { alive = false; break; }
+    const bool last = step + 1 == q.steps;
+    for (int c = half * (q.C / 2); c < (half + 1) * (q.C / 2); c += 32) {
+      float t[32];
+      g16::ld32(tmem + lanes + 256u + (uint32_t)c, t);
+      tc::tc_wait_ld();
+      if (!last) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[j + k] *= 1.f / kB;
+          put8(xh, xl, row, c + j, t + j);
+        }
+      } else if (row < q.s) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          if (c + j < cols) {
+            const size_t e = q.tall ? mbase + (size_t)(c0 + c + j) * q.n + row : mbase + (size_t)row * q.n + c0 + c + j;
+            const float v = t[j] * (1.f / (kB * kX)) * q.scale;
+            if constexpr (DT == DK_F32) {
+              float* o = static_cast<float*>(q.out) + e;
+              *o = q.keep != 0.f ? fmaf(q.keep, *o, v) : v;
+            } else {
+              __nv_bfloat16* o = static_cast<__nv_bfloat16*>(q.out) + e;
+              *o = __float2bfloat16_rn(q.keep != 0.f ? fmaf(q.keep, __bfloat162float(*o), v) : v);
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // ---- teardown: the last CTA of the gang leaves the counter at zero ----
+  tc::tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    if (failed) atomicExch(q.status, (int)DK_ERR_TIMEOUT);
+    else if (atomicAdd(q.count + mat, 1u) + 1u == (epoch + 1u) * (unsigned int)q.gang) q.count[mat] = 0u;
+  }
+  if (warp == 0) {
+    tc::tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
 size_t up(size_t v) { return (v + 1023) / 1024 * 1024; }
@@ -239,7 +673,7 @@ size_t up(size_t v) { return (v + 1023) / 1024 * 1024; }
 struct Plan {
   bool tall;
   int s, np, sp;               // shorter side; pitches of X and of the square matrices
-  size_t off_sum, off_x[2], off_a, off_b, off_part, total;
+  size_t off_sum, off_x[2], off_a, off_b, off_part, off_asum, total;
   size_t x_plane, s_plane;     // elements of one term of all matrices
 };
 
@@ -262,8 +696,20 @@ Plan plan_ortho(const dk_ortho& q) {
   const size_t square = (size_t)q.batch * p.s * p.sp * sizeof(float);
   if (square > part) part = square;
   p.off_part = off; off += up(part);
+  p.off_asum = off; off += p.s <= 128 ? up((size_t)(q.batch < kMaxSms ? q.batch : kMaxSms) * 128 * 128 * sizeof(float)) : 0;
   p.total = off;
   return p;
+}
+
+// Columns per CTA of the resident kernel (0: it does not take the call): 128, whose share of A is one accumulator's
+// sum, or more where that leaves more CTAs than SMs.
+int resident_columns(const dk_ortho& q, const Plan& pl, int sms) {
+  if (pl.s > 128 || q.steps < 1) return 0;
+  const int L = pl.tall ? q.m : q.n;
+  if (sms > kMaxSms) sms = kMaxSms;
+  for (int C = L <= 64 ? 64 : 128; C <= 256; C += 64)
+    if ((long long)q.batch * ((L + C - 1) / C) <= sms) return C;
+  return 0;
 }
 
 dk_status check_ortho(const dk_ortho* q) {
@@ -295,7 +741,7 @@ unsigned grid_of(long long items, int sms) {
 dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const void* x, float scale, float keep,
                         void* out, cudaStream_t st) {
   char* ws = static_cast<char*>(ctx->ws);
-  const int sms = ctx->sm_count, pairs = sms / 2;
+  const int sms = ctx->sm_count;
   double* sums = reinterpret_cast<double*>(ws + pl.off_sum);
   float* part = reinterpret_cast<float*>(ws + pl.off_part);
   __half* xs[2] = {reinterpret_cast<__half*>(ws + pl.off_x[0]), reinterpret_cast<__half*>(ws + pl.off_x[1])};
@@ -303,7 +749,34 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
   __half* bm = reinterpret_cast<__half*>(ws + pl.off_b);
   const long long per = (long long)q.m * q.n;
 
-  int nb = (int)((per + 2047) / 2048);
+  if (const int C = resident_columns(q, pl, sms)) {
+    ResArgs r = {};
+    r.x = x; r.out = out; r.sums = sums; r.part = part;
+    r.asum = reinterpret_cast<float*>(ws + pl.off_asum);
+    r.count = step_counters(ctx);
+    r.m = q.m; r.n = q.n; r.s = pl.s; r.L = pl.tall ? q.m : q.n; r.tall = pl.tall; r.steps = q.steps; r.C = C;
+    r.gang = (r.L + C - 1) / C;
+    r.a = q.a; r.b = q.b; r.c = q.c; r.scale = scale; r.keep = keep; r.eps = (double)q.eps;
+    r.spin_cap = (unsigned)ctx->opt.v[DK_OPT_SPIN_LIMIT];
+    r.status = device_status_word(ctx);
+    auto kern = q.dtype == DK_F32 ? ortho_resident_kernel<DK_F32> : ortho_resident_kernel<DK_BF16>;
+    const int smem = (2 * (C / 64) + 4) * kBlock + 1024;
+    if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return DK_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(q.batch * r.gang));
+    cfg.blockDim = dim3(kResThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeCooperative;
+    at[0].val.cooperative = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = r.gang > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, r) == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+  }
+
+  int nb = (int)((per + 8191) / 8192);
   if (nb > kSumBlocks) nb = kSumBlocks;
   const dim3 gs((unsigned)nb, (unsigned)q.batch);
   const dim3 gl(grid_of((long long)q.m * pl.np / 8, sms), (unsigned)q.batch);
@@ -331,9 +804,9 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
     return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
   }
 
-  const g16::Tiling tg = g16::plan(pl.s, pl.s, pl.tall ? q.m : q.n, BN, q.batch, true, pairs, 4);
-  const g16::Tiling tp = g16::plan(pl.s, pl.s, pl.s, BN, q.batch, true, pairs, 4);
-  const g16::Tiling tx = g16::plan(q.m, q.n, pl.s, BN, q.batch, false, pairs, 4);
+  const g16::Tiling tg = g16::plan(pl.s, pl.s, pl.tall ? q.m : q.n, q.batch, true, sms, 3);
+  const g16::Tiling tp = g16::plan(pl.s, pl.s, pl.s, q.batch, true, sms, 3);
+  const g16::Tiling tx = g16::plan(q.m, q.n, pl.s, q.batch, false, sms, 3);
   const int pitch_s = (pl.s + 3) / 4 * 4, pitch_x = (q.n + 3) / 4 * 4;
   const unsigned nt = (unsigned)((pl.sp + 31) / 32);
   SymArgs sa = {};
@@ -348,21 +821,31 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
     __half* nxt = xs[(k + 1) & 1];
     const Operand X{cur, cur + pl.x_plane, q.m, q.n, pl.np, (long long)q.m * pl.np};
     // A
-    Params p = gemm_params(tg, q, pl.s, pl.s, true);
     const g16::EpiPartial ep{part, pitch_s};
-    dk_status s = pl.tall ? g16::launch<3, true, true, BN>(ctx, X, X, p, ep, st)
-                          : g16::launch<3, false, false, BN>(ctx, X, X, p, ep, st);
-    if (s != DK_OK) return s;
+    Params p = gemm_params(tg, q, pl.s, pl.s, true);
+    dk_status s;
     sa.ks = tg.ksplit; sa.f = kA / (kX * kX); sa.poly = 0; sa.hi = am; sa.lo = am + pl.s_plane;
-    DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st,
-                                 sa));
+    if (tg.cs) {
+      s = pl.tall ? g16::product<3, true, true>(ctx, tg, X, X, p, EpiSym{sa}, st)
+                  : g16::product<3, false, false>(ctx, tg, X, X, p, EpiSym{sa}, st);
+      if (s != DK_OK) return s;
+    } else {
+      s = pl.tall ? g16::launch<3, true, true, BN>(ctx, X, X, p, ep, st)
+                  : g16::launch<3, false, false, BN>(ctx, X, X, p, ep, st);
+      if (s != DK_OK) return s;
+      DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st, sa));
+    }
     // B
     p = gemm_params(tp, q, pl.s, pl.s, true);
-    s = g16::launch<3, false, false, BN>(ctx, A, A, p, ep, st);
-    if (s != DK_OK) return s;
     sa.ks = tp.ksplit; sa.f = 1.f / (kA * kA); sa.poly = 1; sa.hi = bm; sa.lo = bm + pl.s_plane;
-    DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st,
-                                 sa));
+    if (tp.cs) {
+      s = g16::product<3, false, false>(ctx, tp, A, A, p, EpiSym{sa}, st);
+      if (s != DK_OK) return s;
+    } else {
+      s = g16::launch<3, false, false, BN>(ctx, A, A, p, ep, st);
+      if (s != DK_OK) return s;
+      DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st, sa));
+    }
     // X
     XArgs xa = fin;
     if (k + 1 < q.steps) {
@@ -372,7 +855,7 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
       xa.f = 1.f / (kB * kX);
     }
     p = gemm_params(tx, q, q.m, q.n, false);
-    if (tx.ksplit > 1) {
+    if (!tx.cs && tx.ksplit > 1) {
       const g16::EpiPartial ex{part, pitch_x};
       s = pl.tall ? g16::launch<3, false, false, BN>(ctx, X, B, p, ex, st)
                   : g16::launch<3, false, true, BN>(ctx, B, X, p, ex, st);
@@ -380,8 +863,8 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
       DK_CUDA_CHECK(launch_chained(ortho_x_kernel, dim3(grid_of(rows * ((q.n + 7) / 8), sms)), 256, 0, st,
                                  xa, part, tx.ksplit, pitch_x, nullptr, nullptr, rows, 0));
     } else {
-      s = pl.tall ? g16::launch<3, false, false, BN>(ctx, X, B, p, EpiX{xa}, st)
-                  : g16::launch<3, false, true, BN>(ctx, B, X, p, EpiX{xa}, st);
+      s = pl.tall ? g16::product<3, false, false>(ctx, tx, X, B, p, EpiX{xa}, st)
+                  : g16::product<3, false, true>(ctx, tx, B, X, p, EpiX{xa}, st);
       if (s != DK_OK) return s;
     }
   }
@@ -414,7 +897,7 @@ dk_status dk_orthogonalize(dk_ctx* ctx, const dk_ortho* q, const void* x, float 
   OnDevice dev(ctx->device);
   if (!dev.ok) return DK_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  ProfScope ps(ctx, DK_KERNEL_OTHER, 2 + 5 * q->steps, st);
+  ProfScope ps(ctx, DK_KERNEL_OTHER, resident_columns(*q, pl, ctx->sm_count) ? 1 : 2 + 3 * q->steps, st);
   return orthogonalize(ctx, *q, pl, x, scale, keep, out, st);
 }
 

@@ -453,7 +453,11 @@ Plan plan_xent(const dk_xent& q) {
   p.off_p = off; off += up((size_t)T * p.vp * es);
   p.off_acc = off; off += p.pieces > 1 ? up((size_t)T * p.dp * 4) : 0;
   p.off_part = off; off += up(kPartBytes);
-  p.off_slots = off; off += up(((size_t)q.vocab + BN / 2 - 1) / (BN / 2) * T * sizeof(float2));
+  // (maximum, sum) per row and the columns one thread finishes: BN/2 in the large tiles; in the small ones, of which
+  // there are at most kSmallCtas CTAs with SMALL rows each, two to a CTA
+  size_t slots = ((size_t)q.vocab + BN / 2 - 1) / (BN / 2) * T;
+  if (slots < (size_t)g16::kSmallCtas * 2 * g16::SMALL) slots = (size_t)g16::kSmallCtas * 2 * g16::SMALL;
+  p.off_slots = off; off += up(slots * sizeof(float2));
   p.off_tl = off; off += up((size_t)T * sizeof(float));
   p.total = off;
   return p;
@@ -530,11 +534,11 @@ dk_status forward(Call& c, const int64_t* target, float* loss, float* lse) {
   constexpr int NP = F32 ? 3 : 1;
   const dk_xent& q = *c.q;
   const Plan& pl = c.pl;
-  const g16::Tiling t = g16::plan(q.rows, q.vocab, q.d, BN, 1, false, c.ctx->sm_count / 2, 4);
+  const g16::Tiling t = g16::plan(q.rows, q.vocab, q.d, 1, false, c.ctx->sm_count, NP);
   Params p = gemm_params(t, q.rows, q.vocab, F32);
   int* status = device_status_word(c.ctx);
   dk_status s;
-  if (t.ksplit > 1) {
+  if (!t.cs && t.ksplit > 1) {
     const int pitch = (q.vocab + 3) / 4 * 4;
     s = g16::launch<NP, false, false, BN>(c.ctx, c.h, c.w, p, g16::EpiPartial{c.part(), pitch}, c.st);
     if (s != DK_OK) return s;
@@ -543,9 +547,10 @@ dk_status forward(Call& c, const int64_t* target, float* loss, float* lse) {
   } else {
     float2* slots = reinterpret_cast<float2*>(c.ws + pl.off_slots);
     float* tl = reinterpret_cast<float*>(c.ws + pl.off_tl);
-    s = g16::launch<NP, false, false, BN>(c.ctx, c.h, c.w, p, EpiLse{slots, tl, target, c.undo_hw}, c.st);
+    s = g16::product<NP, false, false>(c.ctx, t, c.h, c.w, p, EpiLse{slots, tl, target, c.undo_hw}, c.st);
     if (s != DK_OK) return s;
-    const int nslots = (q.vocab + BN / 2 - 1) / (BN / 2);
+    const int cols = t.cs ? g16::SMALL / 2 / t.cs : BN / 2;      // columns a thread of the product finishes
+    const int nslots = (q.vocab + cols - 1) / cols;
     DK_CUDA_CHECK(launch_chained(xent_join_kernel, dim3((unsigned)((q.rows * 32 + kRowThreads - 1) / kRowThreads)), kRowThreads, 0, c.st,
                                  slots, tl, target, q.rows, nslots, q.vocab, loss, lse, status));
   }
@@ -559,7 +564,7 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
   const dk_xent& q = *c.q;
   const Plan& pl = c.pl;
   const long long T = q.rows;
-  const int pairs = c.ctx->sm_count / 2;
+  const int sms = c.ctx->sm_count;
   const size_t es = F32 ? 4 : 2;
   __half* ph = reinterpret_cast<__half*>(c.ws + pl.off_p);
   float* accum = reinterpret_cast<float*>(c.ws + pl.off_acc);
@@ -578,48 +583,48 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
     const RowArgs r{target, lse, dloss, scale, q.vocab, v0, &c.meta()->gmax, ph, pl_lo, pitch_p};
 
     // p of the piece
-    g16::Tiling t = g16::plan(T, nv, q.d, BN, 1, false, pairs, 4);
+    g16::Tiling t = g16::plan(T, nv, q.d, 1, false, sms, NP);
     Params p = gemm_params(t, T, nv, F32);
     dk_status s;
-    if (t.ksplit > 1) {
+    if (!t.cs && t.ksplit > 1) {
       const int pitch = (nv + 3) / 4 * 4;
       s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
       DK_CUDA_CHECK(launch_chained(xent_slices_p_kernel<F32>, dim3(grid_of(T * pitch_p / 8, c.ctx->sm_count)), 256, 0, c.st,
                                  c.part(), t.ksplit, T, nv, pitch, r, c.undo_hw));
     } else {
-      s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, EpiP<F32>{r, c.undo_hw}, c.st);
+      s = g16::product<NP, false, false>(c.ctx, t, c.h, w, p, EpiP<F32>{r, c.undo_hw}, c.st);
       if (s != DK_OK) return s;
     }
 
     // dh += p.W
     const bool last = i + 1 == pl.pieces;
     EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, vec, undo_pw};
-    t = g16::plan(T, q.d, nv, BN, 1, false, pairs, 4);
+    t = g16::plan(T, q.d, nv, 1, false, sms, NP);
     p = gemm_params(t, T, q.d, F32);
-    if (t.ksplit > 1) {
+    if (!t.cs && t.ksplit > 1) {
       const int pitch = (q.d + 3) / 4 * 4;
       s = g16::launch<NP, false, true, BN>(c.ctx, pop, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
       DK_CUDA_CHECK(launch_chained(xent_slices_grad_kernel<F32>, dim3(grid_of(T * q.d, c.ctx->sm_count)), 256, 0, c.st,
                                  c.part(), t.ksplit, T, q.d, pitch, e));
     } else {
-      s = g16::launch<NP, false, true, BN>(c.ctx, pop, w, p, e, c.st);
+      s = g16::product<NP, false, true>(c.ctx, t, pop, w, p, e, c.st);
       if (s != DK_OK) return s;
     }
 
     // dW of the piece = p^T.h
     e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, vec, undo_ph};
-    t = g16::plan(nv, q.d, T, BN, 1, false, pairs, 4);
+    t = g16::plan(nv, q.d, T, 1, false, sms, NP);
     p = gemm_params(t, nv, q.d, F32);
-    if (t.ksplit > 1) {
+    if (!t.cs && t.ksplit > 1) {
       const int pitch = (q.d + 3) / 4 * 4;
       s = g16::launch<NP, true, true, BN>(c.ctx, pop, c.h, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
       DK_CUDA_CHECK(launch_chained(xent_slices_grad_kernel<F32>, dim3(grid_of((long long)nv * q.d, c.ctx->sm_count)), 256, 0, c.st,
                                  c.part(), t.ksplit, nv, q.d, pitch, e));
     } else {
-      s = g16::launch<NP, true, true, BN>(c.ctx, pop, c.h, p, e, c.st);
+      s = g16::product<NP, true, true>(c.ctx, t, pop, c.h, p, e, c.st);
       if (s != DK_OK) return s;
     }
     if (cudaGetLastError() != cudaSuccess) return DK_ERR_CUDA;
