@@ -10,6 +10,8 @@
 // the diagonal are formed.
 #include <math.h>
 
+#include <type_traits>
+
 #include "dk_gemm16.cuh"
 
 namespace dk {
@@ -318,7 +320,8 @@ ortho_x_kernel(const XArgs a, const float* part, int ks, int pitch_part, const _
 // operand of X X^T and the MN-major operand of B X.
 // ---------------------------------------------------------------------------
 constexpr int kResThreads = 256;
-constexpr int kDirect = 8;
+constexpr int kDirect = 28 * 1024;      // elements of A times CTAs of the gang
+
 constexpr int kBlock = 128 * 128;            // bytes of one [128][64] fp16 block
 
 struct ResArgs {
@@ -436,35 +439,38 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
   };
 
   // ---- the columns, brought to |X|_F = 1 ----
-  // position of this CTA's i-th element: contiguous in memory along consecutive i
-  const int count = q.s * cols;
-  auto element = [&](int i, int& r, int& c) -> size_t {
-    if (q.tall) {
-      c = i / q.s; r = i - c * q.s;
-      return mbase + (size_t)(c0 + c) * q.n + r;
+  // Lines of the stored matrix: rows of the wide orientation, or columns where it is tall; a warp takes four lines at a
+  // time, a lane every 32nd element of 128.
+  const int lines = q.tall ? cols : q.s, length = q.tall ? q.s : cols;
+  const size_t line0 = mbase + (q.tall ? (size_t)c0 * q.n : (size_t)c0);
+  auto fetch = [&](int l0, int e0, float (&v)[16]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int l = l0 + 8 * u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = e0 + 32 * j;
+        v[4 * u + j] = l < lines && e < length ? load1<DT>(q.x, line0 + (size_t)l * q.n + e) : 0.f;
+      }
     }
-    r = i / cols; c = i - r * cols;
-    return mbase + (size_t)r * q.n + c0 + c;
   };
   {
-    double t = 0.0;
-    for (int i = threadIdx.x; i < count; i += 8 * kResThreads) {
-      float v[8];
+    double t[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int e0 = lane; e0 < length; e0 += 128)
+      for (int l0 = warp; l0 < lines; l0 += 32) {
+        float v[16];
+        fetch(l0, e0, v);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        int r, c;
-        v[u] = i + u * kResThreads < count ? load1<DT>(q.x, element(i + u * kResThreads, r, c)) : 0.f;
+        for (int i = 0; i < 16; ++i) t[i & 3] = fma((double)v[i], (double)v[i], t[i & 3]);
       }
+    double sum = (t[0] + t[1]) + (t[2] + t[3]);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) t = fma((double)v[u], (double)v[u], t);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-    if (lane == 0) dsum[warp] = t;
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) dsum[warp] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-      for (int i = 1; i < kResThreads / 32; ++i) t += dsum[i];
-      __stcg(q.sums + (size_t)mat * q.gang + g, t);
+      for (int i = 1; i < kResThreads / 32; ++i) sum += dsum[i];
+      __stcg(q.sums + (size_t)mat * q.gang + g, sum);
     }
     // meanwhile: rows and columns that do not exist are zero
     for (int i = threadIdx.x; i < 2 * nblk * kBlock / 16; i += kResThreads)
@@ -473,27 +479,26 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
   bool alive = meet();
   if (alive) {
     double t = 0.0;
-    for (int i = 0; i < q.gang; ++i) t += __ldcg(q.sums + (size_t)mat * q.gang + i);
+    for (int i = lane; i < q.gang; i += 32) t += __ldcg(q.sums + (size_t)mat * q.gang + i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
     const float f = (float)((double)kX / (sqrt(t) + q.eps));
-    for (int i = threadIdx.x; i < count; i += 8 * kResThreads) {
-      float v[8];
-      uint32_t at[8];
+    for (int e0 = lane; e0 < length; e0 += 128)
+      for (int l0 = warp; l0 < lines; l0 += 32) {
+        float v[16];
+        fetch(l0, e0, v);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        int r = 0, c = 0;
-        const bool in = i + u * kResThreads < count;
-        v[u] = in ? load1<DT>(q.x, element(i + u * kResThreads, r, c)) * f : 0.f;
-        at[u] = block_at(r, c);
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        if (i + u * kResThreads < count) {
-          const __half h = __float2half_rn(v[u]);
-          *reinterpret_cast<__half*>(xh + at[u]) = h;
-          *reinterpret_cast<__half*>(xl + at[u]) = __float2half_rn(v[u] - __half2float(h));
+        for (int i = 0; i < 16; ++i) {
+          const int l = l0 + 8 * (i >> 2), e = e0 + 32 * (i & 3);
+          if (l < lines && e < length) {
+            const uint32_t at = q.tall ? block_at(e, l) : block_at(l, e);
+            const float w = v[i] * f;
+            const __half h = __float2half_rn(w);
+            *reinterpret_cast<__half*>(xh + at) = h;
+            *reinterpret_cast<__half*>(xl + at) = __float2half_rn(w - __half2float(h));
+          }
         }
       }
-    }
   }
 
   constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);      // fp16, 128 x 128
@@ -537,37 +542,61 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
           if (half * 64 + j < q.s) __stcg(q.part + mine + (half * 64 + j) * 128 + row, A[j]);
       }
       if (!meet()) { alive = false; break; }
+      // The shares are added up in order, every thread taking elements (column i / s, row i % s) of its own, and pass to
+      // the threads that need them through the room of A's terms.
       const float* shares = q.part + (size_t)mat * q.gang * 128 * 128;
+      float* const sums = reinterpret_cast<float*>(ah);          // [column][row]
+      const int all = q.s * q.s;
       int parts = q.gang;
-      if (q.gang > kDirect) {
-        // each CTA adds up its slice of the elements (those below s), in the shares' order
-        float* sum = q.asum + (size_t)mat * 128 * 128;
-        const int all = 128 * q.s, per = (all + q.gang - 1) / q.gang;
-        for (int i = g * per + threadIdx.x; i < min(all, (g + 1) * per); i += kResThreads) {
-          if ((i & 127) >= q.s) continue;
-          float t = 0.f;
-#pragma unroll 8
-          for (int k = 0; k < q.gang; ++k) t += __ldcg(shares + (size_t)k * 128 * 128 + i);
-          __stcg(sum + i, t);
+      // elements [lo, hi): U per thread and D shares at a time, all loads in flight
+      auto add_some = [&](auto U_, auto D_, int lo, int hi, float* to, bool global) {
+        constexpr int U = decltype(U_)::value, D = decltype(D_)::value;
+        for (int i0 = lo + (int)threadIdx.x; i0 < hi; i0 += U * kResThreads) {
+          float t[U];
+          int at[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int i = min(i0 + u * kResThreads, hi - 1);      // (the last element again rather than a branch)
+            at[u] = i / q.s * 128 + i % q.s;
+            t[u] = 0.f;
+          }
+          for (int k = 0; k < parts; k += D) {
+            float v[D][U];
+#pragma unroll
+            for (int d = 0; d < D; ++d)
+#pragma unroll
+              for (int u = 0; u < U; ++u) v[d][u] = __ldcg(shares + (size_t)min(k + d, parts - 1) * 128 * 128 + at[u]);
+#pragma unroll
+            for (int d = 0; d < D; ++d)
+#pragma unroll
+              for (int u = 0; u < U; ++u) t[u] += k + d < parts ? v[d][u] : 0.f;
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (global) __stcg(to + at[u], t[u]);
+            else to[at[u]] = t[u];
+          }
         }
+      };
+      auto add_up = [&](int lo, int hi, float* to, bool global) {
+        using std::integral_constant;
+        if (parts == 1) add_some(integral_constant<int, 32>(), integral_constant<int, 1>(), lo, hi, to, global);
+        else if (hi - lo > 2 * kResThreads) add_some(integral_constant<int, 8>(), integral_constant<int, 4>(), lo, hi, to, global);
+        else add_some(integral_constant<int, 2>(), integral_constant<int, 16>(), lo, hi, to, global);
+      };
+      if (all * q.gang > kDirect) {
+        float* sum = q.asum + (size_t)mat * 128 * 128;
+        const int per = (all + q.gang - 1) / q.gang;
+        add_up(min(all, g * per), min(all, (g + 1) * per), sum, true);
         if (!meet()) { alive = false; break; }
         shares = sum;
         parts = 1;
       }
+      add_up(0, all, sums, false);
+      __syncthreads();
 #pragma unroll
-      for (int j = 0; j < 64; ++j) A[j] = 0.f;
-      // (every CTA's share has room for 128 x 128: reading past s costs less than branching around it)
-      const float* from = shares + half * 64 * 128 + row;
-      for (int k = 0; k < parts; ++k, from += 128 * 128) {
-#pragma unroll
-        for (int c = 0; c < 64; c += 16) {
-          float t[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) t[j] = __ldcg(from + (c + j) * 128);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) A[c + j] += row < q.s && half * 64 + c + j < q.s ? t[j] : 0.f;
-        }
-      }
+      for (int j = 0; j < 64; ++j) A[j] = row < q.s && half * 64 + j < q.s ? sums[(half * 64 + j) * 128 + row] : 0.f;
+      __syncthreads();
     }
     // ---- A's terms, A A, B's terms in their place ----
 #pragma unroll
