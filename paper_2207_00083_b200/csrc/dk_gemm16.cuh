@@ -127,8 +127,9 @@ __device__ __forceinline__ void load_tile(unsigned char* dst, const CUtensorMap*
 template <int NPROD, int BN>
 __host__ __device__ constexpr int stage_bytes() { return (NPROD == 3 ? 2 : 1) * (ROWS + BN / 2) * 128; }
 
-// Epi: __device__ void operator()(const Params&, float (&acc)[BN/2], int batch, int ks, int row, int col0) is called
-// by every epilogue thread with its row of C and its BN/2 columns from col0 on (row and columns may lie outside C).
+// Epi: __device__ void operator()(const Params&, float (&acc)[BN/2], int batch, int ks, int row, int col0, char* sm) is
+// called by every epilogue thread with its row of C and its BN/2 columns from col0 on (row and columns may lie outside
+// C), by whole warps of 32 consecutive rows; sm: 4 KiB of the warp's own (see warp_pieces).
 template <int NPROD, bool AMN, bool BMN, int BN, class Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsG, 1)
 gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constant__ CUtensorMap map_a_lo,
@@ -142,7 +143,8 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                          ~static_cast<uintptr_t>(1023));
-  unsigned char* ctrl = smem + (size_t)p.nstages * STAGE;
+  char* rows_mem = reinterpret_cast<char*>(smem + (size_t)p.nstages * STAGE);
+  unsigned char* ctrl = reinterpret_cast<unsigned char*>(rows_mem + kEpi * 4096);
   uint64_t* full_bar = reinterpret_cast<uint64_t*>(ctrl);      // used in the leader only
   uint64_t* empty_bar = full_bar + tc::kMaxStages;
   uint64_t* tfull_bar = empty_bar + tc::kMaxStages;
@@ -285,7 +287,8 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
         if (lane == 0) tc::mbar_arrive_cluster(tc::mapa_shared(smem_u32(tempty_bar + buf), 0u));
       }
       if (!alive) break;
-      epi(p, acc, batch, ks, mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, nt * BN + half * NH);
+      epi(p, acc, batch, ks, mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, nt * BN + half * NH,
+          rows_mem + (warp - 4) * 4096);
     }
   }
 
@@ -488,7 +491,9 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
 #pragma unroll
       for (int j = 0; j < NH; ++j) fin[j] = acc[j];
     }
-    epi(p, fin, batch, 0, mt * SMALL + row, nt * SMALL + c0);
+    // (the stages behind the cluster's sums are free)
+    epi(p, fin, batch, 0, mt * SMALL + row, nt * SMALL + c0,
+        reinterpret_cast<char*>(smem + SMALL * SMALL * 4) + (warp - 4) * 4096);
   }
   // ---------------- teardown ----------------
   tc::tc_fence_before();
@@ -509,19 +514,6 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
 // epilogues shared by the operators
 // ---------------------------------------------------------------------------
 
-// NV consecutive fp32 values of one thread to dst[0 .. count)
-template <int NV>
-__device__ __forceinline__ void store_f32(float* dst, const float (&v)[NV], int count, bool vec) {
-  if (vec && count >= NV) {
-#pragma unroll
-    for (int j = 0; j < NV; j += 4)
-      *reinterpret_cast<float4*>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j < count) dst[j] = v[j];
-  }
-}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
@@ -529,19 +521,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 t = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
-}
-template <int NV>
-__device__ __forceinline__ void store_bf16(__nv_bfloat16* dst, const float (&v)[NV], int count, bool vec) {
-  if (vec && count >= NV) {
-#pragma unroll
-    for (int j = 0; j < NV; j += 8)
-      *reinterpret_cast<uint4*>(dst + j) = make_uint4(pack_bf16(v[j], v[j + 1]), pack_bf16(v[j + 2], v[j + 3]),
-                                                      pack_bf16(v[j + 4], v[j + 5]), pack_bf16(v[j + 6], v[j + 7]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j < count) dst[j] = __float2bfloat16_rn(v[j]);
-  }
 }
 // two fp16 terms of v[j]
 template <int NV>
@@ -564,16 +543,128 @@ __device__ __forceinline__ void store_planes(__half* hi, __half* lo, const float
   }
 }
 
+// A thread holds columns of its row, the 32 lanes 32 rows.  Stored like that, every store instruction touches 32 lines
+// and the tile's epilogue takes 14000 cycles, longer than the products of a short contraction (256 x 256 x 512: 12600).
+// So a warp turns 16-byte pieces over in shared memory (their places exchanged within a row against bank conflicts): P
+// pieces of its row go in from every thread, and f(r, q, piece) gets piece q of row r, P neighbouring lanes a row.
+// P * 512 bytes of `sm`.
+template <int P, class F>
+__device__ __forceinline__ void warp_pieces(const uint4 (&v)[P], char* sm, F f) {
+  static_assert(P == 1 || P == 2 || P == 4 || P == 8, "pieces of a row");
+  const int lane = threadIdx.x & 31;
+  auto place = [](int r, int q) { return (r * P + (q ^ ((r * P >> 3) & (P - 1)))) * 16; };
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(sm + place(lane, q)) = v[q];
+  __syncwarp();
+  uint4 t[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) t[i] = *reinterpret_cast<const uint4*>(sm + place(i * (32 / P) + lane / P, lane % P));
+#pragma unroll
+  for (int i = 0; i < P; ++i) f(i * (32 / P) + lane / P, lane % P, t[i]);
+}
+// fp32 values of a row, W at a time: f(r, c, value of columns c .. c+3)
+template <int NH, class F>
+__device__ __forceinline__ void warp_rows_f32(const float (&v)[NH], char* sm, F f) {
+  constexpr int W = NH < 32 ? NH : 32;
+#pragma unroll
+  for (int c = 0; c < NH; c += W) {
+    uint4 t[W / 4];
+#pragma unroll
+    for (int q = 0; q < W / 4; ++q)
+      t[q] = make_uint4(__float_as_uint(v[c + 4 * q]), __float_as_uint(v[c + 4 * q + 1]), __float_as_uint(v[c + 4 * q + 2]),
+                        __float_as_uint(v[c + 4 * q + 3]));
+    warp_pieces<W / 4>(t, sm, [&](int r, int q, const uint4& u) {
+      f(r, c + 4 * q, make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)));
+    });
+  }
+}
+// 16-bit values of a block of W <= 64 columns, two to a word: f(r, c, columns c .. c+7 of the block)
+template <int W, class F>
+__device__ __forceinline__ void warp_block_16(const uint32_t (&v)[W / 2], char* sm, F f) {
+  uint4 t[W / 8];
+#pragma unroll
+  for (int q = 0; q < W / 8; ++q) t[q] = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+  warp_pieces<W / 8>(t, sm, [&](int r, int q, const uint4& u) { f(r, 8 * q, u); });
+}
+// bf16 of a row's values: f(r, c, columns c .. c+7)
+template <int NH, class F>
+__device__ __forceinline__ void warp_rows_bf16(const float (&v)[NH], char* sm, F f) {
+  constexpr int W = NH < 64 ? NH : 64;
+#pragma unroll
+  for (int c = 0; c < NH; c += W) {
+    uint32_t w[W / 2];
+#pragma unroll
+    for (int j = 0; j < W / 2; ++j) w[j] = pack_bf16(v[c + 2 * j], v[c + 2 * j + 1]);
+    warp_block_16<W>(w, sm, [&](int r, int k, const uint4& u) { f(r, c + k, u); });
+  }
+}
+// two fp16 terms of W of a thread's values from v[c] on
+template <int W, int NH>
+__device__ __forceinline__ void to_terms(const float (&v)[NH], int c, uint32_t (&hi)[W / 2], uint32_t (&lo)[W / 2]) {
+#pragma unroll
+  for (int j = 0; j < W / 2; ++j) {
+    const float a = v[c + 2 * j], b = v[c + 2 * j + 1];
+    const __half2 t = __floats2half2_rn(a, b);
+    hi[j] = *reinterpret_cast<const uint32_t*>(&t);
+    lo[j] = pack_f16(a - __low2float(t), b - __high2float(t));
+  }
+}
+// a piece of eight 16-bit (four 32-bit) elements of which `count` exist
+__device__ __forceinline__ void put_piece16(void* dst, const uint4& u, int count) {
+  if (count >= 8 && (reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
+    *static_cast<uint4*>(dst) = u;
+  } else {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint16_t* d = static_cast<uint16_t*>(dst);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < count) d[j] = (uint16_t)(j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu);
+  }
+}
+__device__ __forceinline__ void put_piece32(float* dst, const float4& u, int count) {
+  if (count >= 4 && (reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
+    *reinterpret_cast<float4*>(dst) = u;
+  } else {
+    const float w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < count) dst[j] = w[j];
+  }
+}
+// rows of two fp16 terms to planes whose pitch is a multiple of 8 (padding columns may be written); rows, cols: how many
+// of the warp's 32 rows and of the columns exist
+template <int NH>
+__device__ __forceinline__ void store_terms(const float (&v)[NH], char* sm, __half* hi, __half* lo, long long pitch, int rows,
+                                            int cols) {
+  constexpr int W = NH < 64 ? NH : 64;
+#pragma unroll
+  for (int c0 = 0; c0 < NH; c0 += W) {
+    uint32_t h[W / 2], l[W / 2];
+    to_terms<W>(v, c0, h, l);
+    warp_block_16<W>(h, sm, [&](int r, int c, const uint4& u) {
+      if (r < rows && c0 + c < cols) *reinterpret_cast<uint4*>(hi + r * pitch + c0 + c) = u;
+    });
+    warp_block_16<W>(l, sm, [&](int r, int c, const uint4& u) {
+      if (r < rows && c0 + c < cols) *reinterpret_cast<uint4*>(lo + r * pitch + c0 + c) = u;
+    });
+  }
+}
+
 // fp32 partial sums of a contraction slice: part[ks][batch][M][pitch]
 struct EpiPartial {
   float* part;
   int pitch;             // multiple of 4
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int ks, int row,
-                                             int col0) const {
-    if (row >= p.M || col0 >= p.N) return;
-    float* dst = part + ((size_t)(ks * p.nbatch + batch) * p.M + row) * pitch + col0;
-    store_f32<NH>(dst, acc, min(NH, p.N - col0), true);
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int ks, int row, int col0,
+                                             char* sm) const {
+    const int row0 = row - (int)(threadIdx.x & 31);
+    if (row0 >= p.M || col0 >= p.N) return;
+    float* dst = part + ((size_t)(ks * p.nbatch + batch) * p.M + row0) * pitch + col0;
+    const int rows = p.M - row0, cols = p.N - col0;
+    warp_rows_f32<NH>(acc, sm, [&](int r, int c, const float4& u) {
+      if (r < rows && c < cols) *reinterpret_cast<float4*>(dst + (size_t)r * pitch + c) = u;
+    });
   }
 };
 
@@ -708,9 +799,10 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
     return DK_ERR_CUDA;
   constexpr int STAGE = stage_bytes<NPROD, BN>();
   constexpr int CTRL = (2 * tc::kMaxStages + 4) * 8 + 16;
-  p.nstages = (227 * 1024 - 1024 - CTRL) / STAGE;
+  constexpr int ROWS_MEM = kEpi * 4096;
+  p.nstages = (227 * 1024 - 1024 - CTRL - ROWS_MEM) / STAGE;
   if (p.nstages > tc::kMaxStages) p.nstages = tc::kMaxStages;
-  const int smem = p.nstages * STAGE + CTRL + 1024;
+  const int smem = p.nstages * STAGE + ROWS_MEM + CTRL + 1024;
   if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
   auto kern = gemm16_kernel<NPROD, AMN, BMN, BN, Epi>;
   if (ctx->device >= 64) return DK_ERR_UNSUPPORTED;

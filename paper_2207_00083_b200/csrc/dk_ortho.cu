@@ -173,47 +173,60 @@ __global__ void __launch_bounds__(256) ortho_sym_kernel(const SymArgs q) {
 struct EpiSym {
   SymArgs q;
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int, int row,
-                                             int col0) const {
-    if (row >= q.s || col0 >= q.s) return;
+  __device__ __forceinline__ void operator()(const Params&, float (&acc)[NH], int batch, int, int row, int col0,
+                                             char* sm) const {
+    const int row0 = row - (int)(threadIdx.x & 31);
+    if (row0 >= q.s || col0 >= q.s || col0 > row0 + 31) return;      // (nothing there on or below the diagonal)
     const size_t plane = (size_t)batch * q.s * q.pitch;
-    const size_t at = plane + (size_t)row * q.pitch + col0;
-    const int count = min(NH, q.s - col0);
+    // Mirrored positions are neighbours across the lanes (rows): A is read there, and both of a value's terms are
+    // written there, a line for all 32.
+    const size_t mirror = plane + (size_t)col0 * q.pitch + row;
+    const int last = min(NH - 1, (row < q.s ? row : -1) - col0);      // this thread's last column on or below the diagonal
+    if (q.poly) {
 #pragma unroll
-    for (int j = 0; j < NH; j += 8) {
-      // (col0 and the pitch are multiples of 8; columns behind s are read as what an earlier product left there, and
-      // not used)
-      uint4 ah = make_uint4(0u, 0u, 0u, 0u), al = ah;
-      if (q.poly && j < count) {
-        ah = *reinterpret_cast<const uint4*>(q.a_hi + at + j);
-        al = *reinterpret_cast<const uint4*>(q.a_lo + at + j);
-      }
-      const __half2* h2 = reinterpret_cast<const __half2*>(&ah);
-      const __half2* l2 = reinterpret_cast<const __half2*>(&al);
+      for (int c = 0; c < NH; c += 8) {
+        __half h[8], l[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        float v = acc[j + k] * q.f;
-        if (q.poly) {
-          const float2 h = __half22float2(h2[k / 2]), l = __half22float2(l2[k / 2]);
-          const float av = (k & 1 ? h.y + l.y : h.x + l.x) * (1.f / kA);
-          v = fmaf(q.c, v, q.b * av);
-          if (col0 + j + k == row) v += q.a;
-          v *= kB;
+        for (int j = 0; j < 8; ++j) {
+          h[j] = l[j] = __float2half(0.f);
+          if (c + j <= last) {
+            h[j] = q.a_hi[mirror + (size_t)(c + j) * q.pitch];
+            l[j] = q.a_lo[mirror + (size_t)(c + j) * q.pitch];
+          }
         }
-        acc[j + k] = j + k < count ? v : 0.f;
-      }
-    }
-    const bool below = col0 + NH - 1 <= row;       // all of them on or below the diagonal
-    if (below) g16::store_planes<NH>(q.hi + at, q.lo + at, acc, count);
 #pragma unroll
-    for (int j = 0; j < NH; ++j) {
-      if (j < count && col0 + j <= row) {
-        const __half h = __float2half_rn(acc[j]), l = __float2half_rn(acc[j] - __half2float(h));
-        if (!below) { q.hi[at + j] = h; q.lo[at + j] = l; }
-        const size_t m = plane + (size_t)(col0 + j) * q.pitch + row;
-        q.hi[m] = h;
-        q.lo[m] = l;
+        for (int j = 0; j < 8; ++j) {
+          const float av = (__half2float(h[j]) + __half2float(l[j])) * (1.f / kA);
+          float v = fmaf(q.c, acc[c + j] * q.f, q.b * av);
+          if (col0 + c + j == row) v += q.a;
+          acc[c + j] = v * kB;
+        }
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NH; ++j) acc[j] *= q.f;
+    }
+    const size_t to = plane + (size_t)row0 * q.pitch + col0;
+    constexpr int W = NH < 32 ? NH : 32;
+#pragma unroll
+    for (int c0 = 0; c0 < NH; c0 += W) {
+      uint32_t h[W / 2], l[W / 2];
+      g16::to_terms<W>(acc, c0, h, l);
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        if (c0 + j <= last) {
+          const size_t at = mirror + (size_t)(c0 + j) * q.pitch;
+          reinterpret_cast<uint16_t*>(q.hi)[at] = (uint16_t)(j & 1 ? h[j / 2] >> 16 : h[j / 2]);
+          reinterpret_cast<uint16_t*>(q.lo)[at] = (uint16_t)(j & 1 ? l[j / 2] >> 16 : l[j / 2]);
+        }
+      }
+      // elements on and below the diagonal only: what lies above it is the mirror image of others
+      auto put = [&](__half* dst, int r, int c, const uint4& u) {
+        const int count = min(row0 + r, q.s - 1) - (col0 + c0 + c) + 1;
+        if (row0 + r < q.s && count > 0) g16::put_piece16(dst + to + (size_t)r * q.pitch + c0 + c, u, count);
+      };
+      g16::warp_block_16<W>(h, sm, [&](int r, int c, const uint4& u) { put(q.hi, r, c, u); });
+      g16::warp_block_16<W>(l, sm, [&](int r, int c, const uint4& u) { put(q.lo, r, c, u); });
     }
   }
 };
@@ -227,40 +240,48 @@ struct XArgs {
   int n, dtype;
   float f;                     // undoes the operands' powers of two (and brings X to its own)
   float scale, keep;
-  int vec;
 };
 struct EpiX {
   XArgs a;
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int, int row,
-                                             int col0) const {
-    if (row >= p.M || col0 >= p.N) return;
-    const int count = min(NH, p.N - col0);
-    if (a.hi != nullptr) {
-      const size_t e = ((size_t)batch * p.M + row) * a.pitch + col0;
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int, int row, int col0,
+                                             char* sm) const {
+    const int row0 = row - (int)(threadIdx.x & 31);
+    if (row0 >= p.M || col0 >= p.N) return;
+    const size_t first = (size_t)batch * p.M + row0;
+    const int rows = p.M - row0, cols = p.N - col0;
+    const float f = a.hi != nullptr ? a.f : a.f * a.scale;
 #pragma unroll
-      for (int j = 0; j < NH; ++j) acc[j] *= a.f;
-      g16::store_planes<NH>(a.hi + e, a.lo + e, acc, count);
+    for (int j = 0; j < NH; ++j) acc[j] *= f;
+    if (a.hi != nullptr) {
+      const size_t to = first * a.pitch + col0;
+      g16::store_terms<NH>(acc, sm, a.hi + to, a.lo + to, a.pitch, rows, cols);
       return;
     }
-    const size_t e = ((size_t)batch * p.M + row) * a.n + col0;
-    const float s = a.f * a.scale;
+    const size_t to = first * a.n + col0;
     if (a.dtype == DK_F32) {
-      float* o = static_cast<float*>(a.out) + e;
-#pragma unroll
-      for (int j = 0; j < NH; ++j) {
-        acc[j] *= s;
-        if (a.keep != 0.f && j < count) acc[j] = fmaf(a.keep, o[j], acc[j]);
-      }
-      g16::store_f32<NH>(o, acc, count, a.vec != 0);
+      float* out = static_cast<float*>(a.out) + to;
+      g16::warp_rows_f32<NH>(acc, sm, [&](int r, int c, float4 u) {
+        if (r >= rows || c >= cols) return;
+        float* o = out + (size_t)r * a.n + c;
+        if (a.keep != 0.f) {
+          u.x = fmaf(a.keep, o[0], u.x);
+          if (c + 1 < cols) u.y = fmaf(a.keep, o[1], u.y);
+          if (c + 2 < cols) u.z = fmaf(a.keep, o[2], u.z);
+          if (c + 3 < cols) u.w = fmaf(a.keep, o[3], u.w);
+        }
+        g16::put_piece32(o, u, cols - c);
+      });
     } else {
-      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(a.out) + e;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + to;
+      if (a.keep != 0.f) {
 #pragma unroll
-      for (int j = 0; j < NH; ++j) {
-        acc[j] *= s;
-        if (a.keep != 0.f && j < count) acc[j] = fmaf(a.keep, __bfloat162float(o[j]), acc[j]);
+        for (int j = 0; j < NH; ++j)
+          if (row < p.M && j < cols) acc[j] = fmaf(a.keep, __bfloat162float(out[(size_t)(row - row0) * a.n + j]), acc[j]);
       }
-      g16::store_bf16<NH>(o, acc, count, a.vec != 0);
+      g16::warp_rows_bf16<NH>(acc, sm, [&](int r, int c, const uint4& u) {
+        if (r < rows && c < cols) g16::put_piece16(out + (size_t)r * a.n + c, u, cols - c);
+      });
     }
   }
 };
@@ -821,10 +842,8 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
                                  x, sums, nb, (double)q.eps, q.m, q.n, pl.np, xs[0], xs[0] + pl.x_plane));
   }
 
-  const size_t es = q.dtype == DK_F32 ? 4 : 2;
   XArgs fin = {};
   fin.out = out; fin.n = q.n; fin.dtype = q.dtype; fin.scale = scale; fin.keep = keep;
-  fin.vec = (size_t)q.n * es % 16 == 0;
   const long long rows = (long long)q.batch * q.m;
   if (q.steps == 0) {
     fin.f = 1.f / kX;

@@ -156,7 +156,7 @@ struct EpiLse {
   const int64_t* target;
   Undo undo;
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0) const {
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char*) const {
     if (row >= p.M || col0 >= p.N) return;
     float f0, f1;
     undo.get(f0, f1);
@@ -206,12 +206,13 @@ struct EpiP {
   RowArgs r;
   Undo undo;
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0) const {
-    if (row >= p.M || col0 >= p.N) return;
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
+    const int row0 = row - (int)(threadIdx.x & 31);
+    if (row0 >= p.M || col0 >= p.N) return;
     float f0, f1;
     undo.get(f0, f1);
     const int count = min(NH, p.N - col0);
-    const long long t = r.target[row];
+    const long long t = row < p.M ? r.target[row] : -1;
     const bool keep = !left_out(t, r.vocab);
     const float lse = keep ? r.lse[row] : 0.f;
     float g = keep ? (r.dloss != nullptr ? r.dloss[row] * r.scale : r.scale) : 0.f;
@@ -220,17 +221,17 @@ struct EpiP {
 #pragma unroll
     for (int j = 0; j < NH; ++j)
       acc[j] = keep && j < count ? p_value(acc[j] * f0 * f1, lse, at == j, g) : 0.f;
+    // (the pitch is a multiple of 8: padding columns are written as zeros)
+    const long long to = (long long)row0 * r.pitch + col0;
     if constexpr (F32) {
-      g16::store_planes<NH>(static_cast<__half*>(r.hi) + row * r.pitch + col0,
-                            static_cast<__half*>(r.lo) + row * r.pitch + col0, acc, count);
+      g16::store_terms<NH>(acc, sm, static_cast<__half*>(r.hi) + to, static_cast<__half*>(r.lo) + to, r.pitch, p.M - row0,
+                           count);
     } else {
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(r.hi) + row * r.pitch + col0;
-#pragma unroll
-      for (int j = 0; j < NH; j += 8)
-        if (j < count)       // (the pitch is a multiple of 8: padding columns are written as zeros)
-          *reinterpret_cast<uint4*>(dst + j) =
-              make_uint4(g16::pack_bf16(acc[j], acc[j + 1]), g16::pack_bf16(acc[j + 2], acc[j + 3]),
-                         g16::pack_bf16(acc[j + 4], acc[j + 5]), g16::pack_bf16(acc[j + 6], acc[j + 7]));
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(r.hi) + to;
+      const int rows = p.M - row0;
+      g16::warp_rows_bf16<NH>(acc, sm, [&](int i, int c, const uint4& u) {
+        if (i < rows && c < count) *reinterpret_cast<uint4*>(dst + i * r.pitch + c) = u;
+      });
     }
   }
 };
@@ -242,31 +243,49 @@ struct EpiGrad {
   float* accum;                // fp32 [M][pitch_acc]
   long long pitch, pitch_acc;
   int add;                     // accum holds earlier pieces
-  int vec;                     // rows of `out` start on 16 bytes
   Undo undo;
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0) const {
-    if (row >= p.M || col0 >= p.N) return;
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
+    const int row0 = row - (int)(threadIdx.x & 31);
+    if (row0 >= p.M || col0 >= p.N) return;
     float f0, f1;
     undo.get(f0, f1);
-    const int count = min(NH, p.N - col0);
-    float* a = accum + (size_t)row * pitch_acc + col0;
 #pragma unroll
-    for (int j = 0; j < NH; j += 4) {
-      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (add && j < count) t = *reinterpret_cast<const float4*>(a + j);
-      acc[j] = fmaf(acc[j] * f0, f1, t.x); acc[j + 1] = fmaf(acc[j + 1] * f0, f1, t.y);
-      acc[j + 2] = fmaf(acc[j + 2] * f0, f1, t.z); acc[j + 3] = fmaf(acc[j + 3] * f0, f1, t.w);
+    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1;
+    const int rows = p.M - row0, cols = p.N - col0;
+    const size_t to = (size_t)row0 * pitch + col0;
+    if (!F32 && out != nullptr && !add) {
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(out) + to;
+      g16::warp_rows_bf16<NH>(acc, sm, [&](int r, int c, const uint4& u) {
+        if (r < rows && c < cols) g16::put_piece16(dst + r * pitch + c, u, cols - c);
+      });
+      return;
     }
-    if (out == nullptr) {
+    // (accum's pitch is a multiple of 8: its padding columns may be read and written)
+    float* sums = accum + (size_t)row0 * pitch_acc + col0;
+    g16::warp_rows_f32<NH>(acc, sm, [&](int r, int c, float4 u) {
+      if (r >= rows || c >= cols) return;
+      float4* s = reinterpret_cast<float4*>(sums + (size_t)r * pitch_acc + c);
+      if (add) {
+        const float4 t = *s;
+        u.x += t.x; u.y += t.y; u.z += t.z; u.w += t.w;
+      }
+      if (out == nullptr) {
+        *s = u;
+      } else if constexpr (F32) {
+        g16::put_piece32(static_cast<float*>(out) + to + r * pitch + c, u, cols - c);
+      } else {
+        __nv_bfloat16* d = static_cast<__nv_bfloat16*>(out) + to + r * pitch + c;
+        if (cols - c >= 4 && (reinterpret_cast<uintptr_t>(d) & 7) == 0) {
+          *reinterpret_cast<uint2*>(d) = make_uint2(g16::pack_bf16(u.x, u.y), g16::pack_bf16(u.z, u.w));
+        } else {
+          const float w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int j = 0; j < NH; j += 4)
-        if (j < count) *reinterpret_cast<float4*>(a + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
-    } else if constexpr (F32) {
-      g16::store_f32<NH>(static_cast<float*>(out) + (size_t)row * pitch + col0, acc, count, vec != 0);
-    } else {
-      g16::store_bf16<NH>(static_cast<__nv_bfloat16*>(out) + (size_t)row * pitch + col0, acc, count, vec != 0);
-    }
+          for (int j = 0; j < 4; ++j)
+            if (c + j < cols) d[j] = __float2bfloat16_rn(w[j]);
+        }
+      }
+    });
   }
 };
 
@@ -570,7 +589,6 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
   float* accum = reinterpret_cast<float*>(c.ws + pl.off_acc);
   const Undo undo_pw{F32 ? &c.meta()->gmax : nullptr, F32 ? &c.meta()->wmax : nullptr};
   const Undo undo_ph{F32 ? &c.meta()->gmax : nullptr, F32 ? &c.meta()->hmax : nullptr};
-  const int vec = ((size_t)q.d * es) % 16 == 0;
   for (int i = 0; i < pl.pieces; ++i) {
     const int v0 = i * pl.vp, nv = q.vocab - v0 < pl.vp ? q.vocab - v0 : pl.vp;
     const long long pitch_p = (nv + 7) / 8 * 8;
@@ -599,7 +617,7 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
 
     // dh += p.W
     const bool last = i + 1 == pl.pieces;
-    EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, vec, undo_pw};
+    EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, undo_pw};
     t = g16::plan(T, q.d, nv, 1, false, sms, NP);
     p = gemm_params(t, T, q.d, F32);
     if (!t.cs && t.ksplit > 1) {
@@ -614,7 +632,7 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
     }
 
     // dW of the piece = p^T.h
-    e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, vec, undo_ph};
+    e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, undo_ph};
     t = g16::plan(nv, q.d, T, 1, false, sms, NP);
     p = gemm_params(t, nv, q.d, F32);
     if (!t.cs && t.ksplit > 1) {
