@@ -10,9 +10,11 @@
 // MN-major (contiguous along M or N: a stored matrix used transposed needs no transposed copy).  Roles, barriers and
 // bounded waits are those of the masked products' pair kernel (dk_tc_pair.cuh).
 //
-// The tensor pipe truncates when it adds, so the accumulator in tensor memory takes `chunk` stages at a time and the
-// epilogue warps add the chunks up in fp32 registers, rounding to nearest.  Two accumulators of BN columns let the
-// epilogue of one tile run beside the products of the next.
+// The tensor pipe truncates when it adds, a loss of about half a unit of the accumulator per addition whatever is added.
+// So the accumulator in tensor memory takes `chunk` stages at a time and the epilogue warps add the chunks up in fp32
+// registers, rounding to nearest.  What is lost within a chunk is a bias, the same relative amount again and again where
+// the terms have one sign (the squares on the diagonal of X X^T), and `comp`, per stage, gives it back on average.  Two
+// accumulators of BN columns let the epilogue of one tile run beside the products of the next.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -39,6 +41,7 @@ struct Params {
   int group;                   // tiles along M that are walked before the next tile along N
   int KB, ksplit, kb_per_split;
   int chunk;                   // stages added up in tensor memory before promotion
+  float comp, comp_small;      // relative loss of a stage's additions that promotion makes good (large, small tiles)
   int nitems;                  // nbatch * tiles * ksplit
   int nstages;
   unsigned spin_cap;
@@ -268,10 +271,15 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
         if (!tc::mbar_wait(tfull_bar + buf, aphase, abort_flag, p.spin_cap)) { alive = false; break; }
         tc::tc_fence_after();
         const uint32_t t = tmem_base + buf * 256u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NH);
+        const float comp = p.comp * (float)min(p.chunk, kb_hi - kb);
         if (kb == kb_lo) {
 #pragma unroll
           for (int c = 0; c < NH; c += 32) ld32(t + (uint32_t)c, acc + c);
           tc::tc_wait_ld();
+          if (comp != 0.f) {
+#pragma unroll
+            for (int j = 0; j < NH; ++j) acc[j] = fmaf(acc[j], comp, acc[j]);
+          }
         } else {
 #pragma unroll
           for (int c = 0; c < NH; c += 32) {
@@ -279,7 +287,7 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
             ld32(t + (uint32_t)c, tmp);
             tc::tc_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) acc[c + j] += tmp[j];
+            for (int j = 0; j < 32; ++j) acc[c + j] += fmaf(tmp[j], comp, tmp[j]);
           }
         }
         tc::tc_fence_before();
@@ -376,7 +384,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
-                 "r"(256u)
+                 "r"(512u)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -433,8 +441,8 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
           for (int kk = 0; kk < BK / 16; ++kk) {
             mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, (k == kb && kk == 0) ? 0u : 1u);
             if constexpr (NPROD == 3) {
-              mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + LO + kk * STEP_B, idesc, 1u);
-              mma_f16(d_tmem, a_hi + LO + kk * STEP_A, b_hi + kk * STEP_B, idesc, 1u);
+              mma_f16(tmem_base + 256u, a_hi + kk * STEP_A, b_hi + LO + kk * STEP_B, idesc, (k == kb_lo && kk == 0) ? 0u : 1u);
+              mma_f16(tmem_base + 256u, a_hi + LO + kk * STEP_A, b_hi + kk * STEP_B, idesc, 1u);
             }
           }
           tc::tc_commit(empty_bar + stage);
@@ -453,13 +461,24 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
       if (!tc::mbar_wait(tfull_bar + buf, aphase, abort_flag, p.spin_cap)) break;
       tc::tc_fence_after();
       const uint32_t t = tmem_base + buf * 128u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NC);
+      const float comp = p.comp_small * (float)min(p.chunk, kb_hi - kb);
 #pragma unroll
       for (int c = 0; c < NC; c += 32) {
         float tmp[32];
         ld32(t + (uint32_t)c, tmp);
         tc::tc_wait_ld();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) acc[c + j] += tmp[j];
+        for (int j = 0; j < 32; ++j) acc[c + j] += fmaf(tmp[j], comp, tmp[j]);
+      }
+      if (NPROD == 3 && kb + p.chunk >= kb_hi) {
+#pragma unroll
+        for (int c = 0; c < NC; c += 32) {
+          float tmp[32];
+          ld32(tmem_base + 256u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NC + c), tmp);
+          tc::tc_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) acc[c + j] += tmp[j];
+        }
       }
       tc::tc_fence_before();
       __syncwarp();
@@ -506,7 +525,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
   if constexpr (CS > 1) tc::cluster_sync_all();      // no CTA leaves while its sums are being read
   if (warp == 1) {
     tc::tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
   }
 }
 

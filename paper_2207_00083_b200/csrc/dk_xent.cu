@@ -497,6 +497,9 @@ Params gemm_params(const g16::Tiling& t, long long M, long long N, bool f32) {
   p.M = (int)M; p.N = (int)N;
   p.bf16 = f32 ? 0 : 1;
   p.chunk = f32 ? 2 : 16;
+  // what the tensor pipe loses per stage in sums of random sign (large tiles, small tiles; measured, see g16::Params)
+  p.comp = f32 ? 3.6f / 16777216.f : 0.f;
+  p.comp_small = f32 ? 1.2f / 16777216.f : 0.f;
   return p;
 }
 
