@@ -701,7 +701,7 @@ struct Tiling {
 // Cost in cycles of either way, from what was measured: a stage (64 contraction elements) of the pair's tile takes 512
 // cycles per product, of the small tile 256, but the small tile's operands arrive at ~50 bytes per cycle and SM, which
 // is what binds it (16 KiB per operand plane); some 9000 cycles go to a launch's start, fill and epilogue, 6000 more to
-// joining a cluster's slices, 20000 to the partial sums' way through global memory and a second kernel.  Clusters of
+// joining a cluster's slices, 24000 to the partial sums' way through global memory and a second kernel.  Clusters of
 // four and eight do not tile the GPCs: 33 and 15 of them are resident at once on 148 SMs.
 inline Tiling plan(long long M, long long N, long long K, int nbatch, bool sym, int sms, int nprod) {
   Tiling best = {};
@@ -727,7 +727,7 @@ inline Tiling plan(long long M, long long N, long long K, int nbatch, bool sym, 
       t.kb_per_split = per;
       t.ksplit = (KB + per - 1) / per;
       const double waves = (double)((tiles * nbatch * t.ksplit + pairs - 1) / pairs);
-      cost = waves * per * 512.0 * nprod + 9000.0 + (t.ksplit > 1 ? 20000.0 : 0.0);
+      cost = waves * per * 512.0 * nprod + 9000.0 + (t.ksplit > 1 ? 24000.0 : 0.0);
     } else {
       if (cs > 1 && KB < 2 * cs) continue;             // at least two stages each
       const long long ctas = tiles * nbatch * cs;

@@ -345,7 +345,7 @@ constexpr int kDirect = 28 * 1024;      // elements of A times CTAs of the gang
 
 constexpr int kBlock = 128 * 128;            // bytes of one [128][64] fp16 block
 // what the tensor pipe loses per 64 contraction elements (see kLossSquares)
-constexpr float kResLossSquares = 4.4f / 16777216.f, kResLossMixed = 2.5f / 16777216.f;
+constexpr float kResLossSquares = 4.4f / 16777216.f, kResLossMixed = 1.2f / 16777216.f;
 
 struct ResArgs {
   const void* x;
@@ -786,9 +786,9 @@ dk_status check_ortho(const dk_ortho* q) {
 // What the tensor pipe loses per stage when it adds, in 2^-24 of the sum (the large tiles add all three products into one
 // accumulator, the small ones the low terms' apart): measured on sums of squares 6.6 and 4.4, of products of random sign
 // 3.6 and 1.2, within 0.7 of that for chunks of 1 to 8 stages and contractions of 64 to 4096.  X X^T and A A have their
-// weight on the diagonal, a sum of squares; B X is dominated by a few terms of each sum.
+// weight on the diagonal, a sum of squares.
 constexpr float kUlp = 1.f / 16777216.f;
-constexpr float kLossSquares[2] = {6.6f * kUlp, 4.4f * kUlp}, kLossMixed[2] = {5.f * kUlp, 2.5f * kUlp};
+constexpr float kLossSquares[2] = {6.6f * kUlp, 4.4f * kUlp}, kLossMixed[2] = {3.6f * kUlp, 1.2f * kUlp};
 
 Params gemm_params(const g16::Tiling& t, const dk_ortho& q, long long M, long long N, bool sym) {
   Params p = {};

@@ -20,8 +20,12 @@ using g16::Params;
 
 constexpr int kRowThreads = 256;
 
-struct Meta {                  // first words of the workspace
-  unsigned int hmax, wmax, gmax;     // bit patterns of the largest magnitudes (fp32 calls)
+// First words of the workspace (fp32 backward calls): bit patterns of the largest magnitudes, of every block of
+// xent_absmax_kernel and (written by xent_prep_kernel) of all.
+constexpr int kMaxBlocks = 592;
+struct Meta {
+  unsigned int hmax, wmax, gmax, unused;
+  uint4 block[kMaxBlocks];
 };
 
 // The power of two that brings a largest magnitude (given by its bits) to [2^14, 2^15); 1 when it is zero, infinite or
@@ -79,9 +83,7 @@ xent_absmax_kernel(const float* __restrict__ h, const float* __restrict__ W, con
     atomicMax(&s[0], mh); atomicMax(&s[1], mw); atomicMax(&s[2], mg);
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    atomicMax(&meta->hmax, s[0]); atomicMax(&meta->wmax, s[1]); atomicMax(&meta->gmax, s[2]);
-  }
+  if (threadIdx.x == 0) meta->block[blockIdx.x] = make_uint4(s[0], s[1], s[2], 0u);
 }
 
 // One matrix of the operand preparation: rows of d values to rows of dp (a multiple of 8, padded with zeros), rows
@@ -91,14 +93,12 @@ struct Prep {
   void* hi;
   void* lo;
   const int64_t* target;
-  const unsigned int* maxbits;
   long long rows;
 };
 
 template <bool F32>
-__device__ __forceinline__ void prep_rows(const Prep& q, int d, int dp, int vocab, long long i0, long long step) {
+__device__ __forceinline__ void prep_rows(const Prep& q, int d, int dp, int vocab, float sc, long long i0, long long step) {
   const int d8 = dp / 8;
-  const float sc = F32 ? pow2(scale_exp(*q.maxbits)) : 1.f;
   for (long long i = i0; i < q.rows * d8; i += step) {
     const long long r = i / d8;
     const int c = (int)(i - r * d8) * 8;
@@ -131,12 +131,108 @@ __device__ __forceinline__ void prep_rows(const Prep& q, int d, int dp, int voca
     }
   }
 }
+// (F32: joins the blocks' magnitudes first)
 template <bool F32>
-__global__ void __launch_bounds__(256) xent_prep_kernel(const Prep a, const Prep b, int d, int dp, int vocab) {
+__global__ void __launch_bounds__(256) xent_prep_kernel(const Prep a, const Prep b, int d, int dp, int vocab, Meta* meta,
+                                                        int blocks) {
   chained_launch();
   const long long step = (long long)gridDim.x * blockDim.x, i0 = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (a.src != nullptr) prep_rows<F32>(a, d, dp, vocab, i0, step);
-  if (b.src != nullptr) prep_rows<F32>(b, d, dp, vocab, i0, step);
+  float sh = 1.f, sw = 1.f;
+  if constexpr (F32) {
+    __shared__ unsigned int most[8][3];
+    uint4 m = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = threadIdx.x; i < blocks; i += 256) {
+      const uint4 t = meta->block[i];
+      m.x = max(m.x, t.x); m.y = max(m.y, t.y); m.z = max(m.z, t.z);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      m.x = max(m.x, __shfl_xor_sync(0xffffffffu, m.x, o));
+      m.y = max(m.y, __shfl_xor_sync(0xffffffffu, m.y, o));
+      m.z = max(m.z, __shfl_xor_sync(0xffffffffu, m.z, o));
+    }
+    if ((threadIdx.x & 31) == 0) {
+      most[threadIdx.x >> 5][0] = m.x; most[threadIdx.x >> 5][1] = m.y; most[threadIdx.x >> 5][2] = m.z;
+    }
+    __syncthreads();
+    unsigned int h = 0, w = 0, g = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { h = max(h, most[i][0]); w = max(w, most[i][1]); g = max(g, most[i][2]); }
+    if (blockIdx.x == 0 && threadIdx.x == 0) { meta->hmax = h; meta->wmax = w; meta->gmax = g; }
+    sh = pow2(scale_exp(h));
+    sw = pow2(scale_exp(w));
+  }
+  if (a.src != nullptr) prep_rows<F32>(a, d, dp, vocab, sh, i0, step);
+  if (b.src != nullptr) prep_rows<F32>(b, d, dp, vocab, sw, i0, step);
+}
+
+// The operands of a forward call: fp32 rows as two fp16 terms under a power of two of each row's own (a forward product
+// never sums over rows, so nothing needs a common one, and one reading from HBM is enough); inv undoes it.  One warp (or
+// block) per row.
+struct PrepRows {
+  const float* src;
+  __half* hi;
+  __half* lo;
+  float* inv;
+  const int64_t* target;
+  long long rows;
+};
+// (WIDE: a whole block per row, for long rows)
+template <bool WIDE>
+__global__ void __launch_bounds__(256) xent_prep_forward_kernel(const PrepRows a, const PrepRows b, int d, int dp, int vocab) {
+  chained_launch();
+  __shared__ unsigned int most[8];
+  constexpr int THREADS = WIDE ? 256 : 32;
+  const int lane = threadIdx.x & (THREADS - 1);
+  const long long first_row = WIDE ? blockIdx.x : (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long step = WIDE ? gridDim.x : (long long)gridDim.x * 8;
+  for (long long i = first_row; i < a.rows + b.rows; i += step) {
+    const bool first = i < a.rows;
+    const long long r = first ? i : i - a.rows;
+    const float* src = (first ? a.src : b.src) + r * d;
+    __half* hi = (first ? a.hi : b.hi) + r * dp;
+    __half* lo = (first ? a.lo : b.lo) + r * dp;
+    const bool keep = !first || !left_out(a.target[r], vocab);
+    auto eight = [&](int c, float (&v)[8]) {
+      if (d % 4 == 0 && c + 8 <= d) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(src + c)), y = __ldg(reinterpret_cast<const float4*>(src + c) + 1);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < d ? __ldg(src + c + j) : 0.f;
+      }
+    };
+    unsigned int m = 0;
+    if (keep) {
+#pragma unroll 2
+      for (int c = lane * 8; c < d; c += THREADS * 8) {
+        float v[8];
+        eight(c, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if constexpr (WIDE) {
+      if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = m;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m = max(m, most[k]);
+      __syncthreads();
+    }
+    const int e = scale_exp(m);
+    const float sc = pow2(e);
+    if (lane == 0) (first ? a.inv : b.inv)[r] = pow2(-e);
+#pragma unroll 2
+    for (int c = lane * 8; c < dp; c += THREADS * 8) {
+      float v[8];
+      eight(c, v);      // (from L1)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = keep ? v[j] * sc : 0.f;
+      g16::store_planes<8>(hi + c, lo + c, v, 8);
+    }
+  }
 }
 
 // what undoes the operands' powers of two: product*f0*f1
@@ -154,22 +250,36 @@ struct EpiLse {
   float2* part;                // [columns / (BN/2)][rows]
   float* tlogit;               // [rows]
   const int64_t* target;
-  Undo undo;
+  const float* inv_h;          // fp32: undo the rows' powers of two; null: bf16
+  const float* inv_w;
   template <int NH>
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char*) const {
     if (row >= p.M || col0 >= p.N) return;
-    float f0, f1;
-    undo.get(f0, f1);
     const int count = min(NH, p.N - col0);
+    if (inv_h != nullptr) {
+      const float f = inv_h[row];
+#pragma unroll
+      for (int j = 0; j < NH; j += 4) {      // (inv_w has room for whole tiles)
+        const float4 w = __ldg(reinterpret_cast<const float4*>(inv_w + col0 + j));
+        acc[j] = acc[j] * f * w.x; acc[j + 1] = acc[j + 1] * f * w.y;
+        acc[j + 2] = acc[j + 2] * f * w.z; acc[j + 3] = acc[j + 3] * f * w.w;
+      }
+    }
     const long long t = target[row];
     const int at = (t >= col0 && t < (long long)col0 + count) ? (int)(t - col0) : -1;
-    float m = -INFINITY, tl = 0.f;
+    if (count < NH) {
 #pragma unroll
-    for (int j = 0; j < NH; ++j) {
-      acc[j] = j < count ? acc[j] * f0 * f1 : -INFINITY;
-      m = fmaxf(m, acc[j]);
-      if (j == at) tl = acc[j];
+      for (int j = 0; j < NH; ++j) acc[j] = j < count ? acc[j] : -INFINITY;
     }
+    if (at >= 0) {                 // (few rows have their target among these columns)
+      float tl = 0.f;
+#pragma unroll
+      for (int j = 0; j < NH; ++j) tl = j == at ? acc[j] : tl;
+      tlogit[row] = tl;
+    }
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NH; ++j) m = fmaxf(m, acc[j]);
     // (all columns -inf: the differences would be NaN; the row's sum is 0 under maximum -inf)
     const float ref = m == -INFINITY ? 0.f : m;
     // eight sums: one alone would round its way up 128 times in the same direction where the terms are alike
@@ -180,7 +290,6 @@ struct EpiLse {
     for (int j = 0; j < NH; ++j) s[j & 7] += __expf(acc[j] - ref);
     part[(size_t)(col0 / NH) * p.M + row] =
         make_float2(m, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
-    if (at >= 0) tlogit[row] = tl;
   }
 };
 
@@ -209,18 +318,30 @@ struct EpiP {
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
     const int row0 = row - (int)(threadIdx.x & 31);
     if (row0 >= p.M || col0 >= p.N) return;
-    float f0, f1;
-    undo.get(f0, f1);
     const int count = min(NH, p.N - col0);
     const long long t = row < p.M ? r.target[row] : -1;
     const bool keep = !left_out(t, r.vocab);
     const float lse = keep ? r.lse[row] : 0.f;
     float g = keep ? (r.dloss != nullptr ? r.dloss[row] * r.scale : r.scale) : 0.f;
-    if (F32) g *= pow2(scale_exp(*r.gmax));
-    const long long at = t - r.v0 - col0;
+    if constexpr (F32) {
+      float f0, f1;
+      undo.get(f0, f1);
+      g *= pow2(scale_exp(*r.gmax));
 #pragma unroll
-    for (int j = 0; j < NH; ++j)
-      acc[j] = keep && j < count ? p_value(acc[j] * f0 * f1, lse, at == j, g) : 0.f;
+      for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1;
+    }
+#pragma unroll
+    for (int j = 0; j < NH; ++j) acc[j] = g * __expf(acc[j] - lse);
+    const long long off = t - r.v0 - col0;
+    if (off >= 0 && off < count) {      // (few rows have their target among these columns)
+      const int at = (int)off;
+#pragma unroll
+      for (int j = 0; j < NH; ++j) acc[j] = j == at ? acc[j] - g : acc[j];
+    }
+    if (!keep || count < NH) {
+#pragma unroll
+      for (int j = 0; j < NH; ++j) acc[j] = keep && j < count ? acc[j] : 0.f;
+    }
     // (the pitch is a multiple of 8: padding columns are written as zeros)
     const long long to = (long long)row0 * r.pitch + col0;
     if constexpr (F32) {
@@ -248,10 +369,12 @@ struct EpiGrad {
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
     const int row0 = row - (int)(threadIdx.x & 31);
     if (row0 >= p.M || col0 >= p.N) return;
-    float f0, f1;
-    undo.get(f0, f1);
+    if constexpr (F32) {
+      float f0, f1;
+      undo.get(f0, f1);
 #pragma unroll
-    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1;
+      for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1;
+    }
     const int rows = p.M - row0, cols = p.N - col0;
     const size_t to = (size_t)row0 * pitch + col0;
     if (!F32 && out != nullptr && !add) {
@@ -292,8 +415,14 @@ struct EpiGrad {
 // ---- what follows a product whose contraction was sliced: the slices' sums are joined in order ----
 
 __device__ __forceinline__ float slice_sum(const float* part, size_t at, size_t slice, int ks) {
-  float v = part[at];
-  for (int k = 1; k < ks; ++k) v += part[at + k * slice];
+  float v = 0.f;
+  for (int k = 0; k < ks; k += 8) {      // eight loads in flight
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = __ldg(part + at + (size_t)min(k + i, ks - 1) * slice);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += k + i < ks ? t[i] : 0.f;
+  }
   return v;
 }
 
@@ -338,19 +467,19 @@ xent_join_kernel(const float2* __restrict__ part, const float* __restrict__ tlog
 // one block per row of sliced logits
 __global__ void __launch_bounds__(kRowThreads)
 xent_slices_lse_kernel(const float* __restrict__ part, int ks, long long rows, int vocab, int pitch,
-                       const int64_t* __restrict__ target, const Undo undo, float* loss, float* lse, int* status) {
+                       const int64_t* __restrict__ target, const float* __restrict__ inv_h,
+                       const float* __restrict__ inv_w, float* loss, float* lse, int* status) {
   chained_launch();
   __shared__ float sm[kRowThreads / 32], ss[kRowThreads / 32], st;
   const long long row = blockIdx.x;
-  float f0, f1;
-  undo.get(f0, f1);
+  const float f0 = inv_h != nullptr ? inv_h[row] : 1.f;
   const size_t slice = (size_t)rows * pitch;
   const long long t = target[row];
   float m = -INFINITY, s = 0.f;
   if (threadIdx.x == 0) st = 0.f;
   __syncthreads();
   for (int v = threadIdx.x; v < vocab; v += kRowThreads) {
-    const float l = slice_sum(part, (size_t)row * pitch + v, slice, ks) * f0 * f1;
+    const float l = slice_sum(part, (size_t)row * pitch + v, slice, ks) * f0 * (inv_w != nullptr ? inv_w[v] : 1.f);
     if (v == t) st = l;
     const float n = fmaxf(m, l);
     if (n != -INFINITY) s = s * __expf(m - n) + __expf(l - n);
@@ -442,7 +571,7 @@ size_t up(size_t v) { return (v + 1023) / 1024 * 1024; }
 struct Plan {
   bool f32, copy_w, copy_h;    // fwd: operands are laid out anew (fp32 terms, or rows that do not start on 16 bytes)
   int dp, vp, pieces;
-  size_t off_h, off_w, off_p, off_acc, off_part, off_slots, off_tl, total;
+  size_t off_h, off_w, off_p, off_acc, off_part, off_slots, off_tl, off_inv, total;
 };
 
 // slices of a product: every (tile, slice) has at most one pair's tile of fp32 sums
@@ -466,7 +595,7 @@ Plan plan_xent(const dk_xent& q) {
     p.pieces = (int)((q.vocab + vp - 1) / vp);
   }
   p.vp = (int)((vp + 7) / 8 * 8);
-  size_t off = 1024;
+  size_t off = up(sizeof(Meta));
   p.off_h = off; off += up((size_t)T * p.dp * es);
   p.off_w = off; off += p.copy_w ? up((size_t)q.vocab * p.dp * es) : 0;
   p.off_p = off; off += up((size_t)T * p.vp * es);
@@ -478,6 +607,8 @@ Plan plan_xent(const dk_xent& q) {
   if (slots < (size_t)g16::kSmallCtas * 2 * g16::SMALL) slots = (size_t)g16::kSmallCtas * 2 * g16::SMALL;
   p.off_slots = off; off += up(slots * sizeof(float2));
   p.off_tl = off; off += up((size_t)T * sizeof(float));
+  // (inverse powers of two of the rows; those of W in whole tiles)
+  p.off_inv = off; off += p.f32 ? up(((size_t)T + 4 + (size_t)q.vocab + 256) * sizeof(float)) : 0;
   p.total = off;
   return p;
 }
@@ -517,38 +648,56 @@ struct Call {
   cudaStream_t st;
   Operand h, w;
   Undo undo_hw;
+  const float *inv_h, *inv_w;
   Meta* meta() const { return reinterpret_cast<Meta*>(ws); }
   float* part() const { return reinterpret_cast<float*>(ws + pl.off_part); }
 };
 
-// lays out h (always when `clear_h`: rows that are left out are cleared, so that what they hold meets no product) and
-// W, and finds the magnitudes of the fp32 terms
+// Lays out what the products read.  Backward: h always, rows that are left out cleared, so that what they hold meets no
+// product (bf16: a copy), and fp32 operands under one power of two each.
 template <bool F32>
 dk_status prepare(Call& c, const void* h, const void* W, const int64_t* target, const float* dloss, float scale,
-                  bool clear_h) {
+                  bool backward) {
   const dk_xent& q = *c.q;
   const Plan& pl = c.pl;
-  Meta* meta = c.meta();
-  const bool copy_h = pl.copy_h || clear_h;
+  const bool copy_h = pl.copy_h || backward;
   __half* hh = reinterpret_cast<__half*>(c.ws + pl.off_h);
   __half* wh = reinterpret_cast<__half*>(c.ws + pl.off_w);
   const long long nh = q.rows * pl.dp, nw = (long long)q.vocab * pl.dp;
-  Prep a = {}, b = {};
-  if (copy_h) a = Prep{h, hh, hh + nh, target, &meta->hmax, q.rows};
-  if (pl.copy_w) b = Prep{W, wh, wh + nw, nullptr, &meta->wmax, q.vocab};
+  const int sms = c.ctx->sm_count;
   c.undo_hw = Undo{nullptr, nullptr};
-  if (F32) {
-    DK_CUDA_CHECK(cudaMemsetAsync(meta, 0, sizeof(Meta), c.st));
-    DK_CUDA_CHECK(launch_chained(xent_absmax_kernel, dim3(grid_of((nw + nh) / 4, c.ctx->sm_count)), 256, 0, c.st,
-                                 static_cast<const float*>(h), static_cast<const float*>(W), target, dloss, scale, q.rows, q.d, q.vocab, meta));
-    c.undo_hw = Undo{&meta->hmax, &meta->wmax};
+  c.inv_h = c.inv_w = nullptr;
+  if (F32 && !backward) {
+    float* inv_h = reinterpret_cast<float*>(c.ws + pl.off_inv);
+    float* inv_w = inv_h + (q.rows + 3) / 4 * 4;
+    const PrepRows a{static_cast<const float*>(h), hh, hh + nh, inv_h, target, q.rows};
+    const PrepRows b{static_cast<const float*>(W), wh, wh + nw, inv_w, nullptr, q.vocab};
+    // (a block per row keeps one reading of 2048 elements or more in flight: 256 + 1000 rows of 4096 in 14 us by warps)
+    const bool wide = q.d >= 1024;
+    DK_CUDA_CHECK(launch_chained(wide ? xent_prep_forward_kernel<true> : xent_prep_forward_kernel<false>,
+                                 dim3(grid_of((q.rows + q.vocab) * (wide ? 256 : 32), sms)), 256, 0, c.st, a, b, q.d, pl.dp,
+                                 q.vocab));
+    c.inv_h = inv_h;
+    c.inv_w = inv_w;
+  } else if (copy_h || pl.copy_w) {
+    Prep a = {}, b = {};
+    if (copy_h) a = Prep{h, hh, hh + nh, target, q.rows};
+    if (pl.copy_w) b = Prep{W, wh, wh + nw, nullptr, q.vocab};
+    Meta* meta = c.meta();
+    unsigned blocks = grid_of((nw + nh) / 4, sms);
+    if (blocks > kMaxBlocks) blocks = kMaxBlocks;
+    if (F32) {
+      DK_CUDA_CHECK(launch_chained(xent_absmax_kernel, dim3(blocks), 256, 0, c.st, static_cast<const float*>(h),
+                                   static_cast<const float*>(W), target, dloss, scale, q.rows, q.d, q.vocab, meta));
+      c.undo_hw = Undo{&meta->hmax, &meta->wmax};
+    }
+    DK_CUDA_CHECK(launch_chained(xent_prep_kernel<F32>,
+                                 dim3(grid_of(((copy_h ? nh : 0) + (pl.copy_w ? nw : 0)) / 8, sms)), 256, 0, c.st, a, b, q.d,
+                                 pl.dp, q.vocab, meta, (int)blocks));
   }
-  if (copy_h || pl.copy_w)
-    DK_CUDA_CHECK(launch_chained(xent_prep_kernel<F32>, dim3(grid_of(((copy_h ? nh : 0) + (pl.copy_w ? nw : 0)) / 8, c.ctx->sm_count)), 256, 0, c.st,
-                                 a, b, q.d, pl.dp, q.vocab));
   c.h = Operand{copy_h ? (const void*)hh : h, hh + nh, q.rows, q.d, pl.dp, 0};
   c.w = Operand{pl.copy_w ? (const void*)wh : W, wh + nw, q.vocab, q.d, pl.dp, 0};
-  return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+  return DK_OK;
 }
 
 template <bool F32>
@@ -565,11 +714,11 @@ dk_status forward(Call& c, const int64_t* target, float* loss, float* lse) {
     s = g16::launch<NP, false, false, BN>(c.ctx, c.h, c.w, p, g16::EpiPartial{c.part(), pitch}, c.st);
     if (s != DK_OK) return s;
     DK_CUDA_CHECK(launch_chained(xent_slices_lse_kernel, dim3((unsigned)q.rows), kRowThreads, 0, c.st,
-                                 c.part(), t.ksplit, q.rows, q.vocab, pitch, target, c.undo_hw, loss, lse, status));
+                                 c.part(), t.ksplit, q.rows, q.vocab, pitch, target, c.inv_h, c.inv_w, loss, lse, status));
   } else {
     float2* slots = reinterpret_cast<float2*>(c.ws + pl.off_slots);
     float* tl = reinterpret_cast<float*>(c.ws + pl.off_tl);
-    s = g16::product<NP, false, false>(c.ctx, t, c.h, c.w, p, EpiLse{slots, tl, target, c.undo_hw}, c.st);
+    s = g16::product<NP, false, false>(c.ctx, t, c.h, c.w, p, EpiLse{slots, tl, target, c.inv_h, c.inv_w}, c.st);
     if (s != DK_OK) return s;
     const int cols = t.cs ? g16::SMALL / 2 / t.cs : BN / 2;      // columns a thread of the product finishes
     const int nslots = (q.vocab + cols - 1) / cols;
@@ -692,7 +841,7 @@ dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const
   if (s != DK_OK) return s;
   OnDevice dev(ctx->device);
   if (!dev.ok) return DK_ERR_CUDA;
-  ProfScope ps(ctx, DK_KERNEL_OTHER, 2 + (c.pl.copy_w ? 1 : 0) + (c.pl.f32 ? 1 : 0), c.st);
+  ProfScope ps(ctx, DK_KERNEL_OTHER, 2 + (c.pl.copy_w ? 1 : 0), c.st);
   if (c.pl.f32) {
     s = prepare<true>(c, h, W, target, nullptr, 1.f, false);
     return s == DK_OK ? forward<true>(c, target, loss, lse) : s;
