@@ -331,9 +331,10 @@ __device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr)
+               : "memory");
   return v;
 }
 template <bool MN, int NROWS>
@@ -397,6 +398,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
   const int quad = warp & 3, half = (warp - 4) >> 2;
   const int row = quad * 32 + lane;
   float acc[NC];
+  uint32_t ahead[Epi::kAhead ? NH : 1];            // what the epilogue reads, fetched while the products run
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0, issued = 0;
@@ -453,6 +455,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
     }
     __syncwarp();
   } else if (warp >= 4) {
+    if constexpr (Epi::kAhead) epi.fetch(batch, mt * SMALL + row, nt * SMALL + rank * (SMALL / CS) + half * NH, ahead);
     uint32_t acc_it = 0;
 #pragma unroll
     for (int j = 0; j < NC; ++j) acc[j] = 0.f;
@@ -485,10 +488,11 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
       if (lane == 0) tc::mbar_arrive(tempty_bar + buf);
     }
     if constexpr (CS > 1) {
-      // [column][row]: every product of this CTA is done, its stages are free
-      float* red = reinterpret_cast<float*>(smem);
+      // [column / 4][row][column % 4]: every product of this CTA is done, its stages are free
+      float4* red = reinterpret_cast<float4*>(smem);
 #pragma unroll
-      for (int j = 0; j < NC; ++j) red[(half * NC + j) * SMALL + row] = acc[j];
+      for (int j = 0; j < NC; j += 4)
+        red[(half * NC + j) / 4 * SMALL + row] = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
     }
   }
   const bool failed = __syncthreads_or(*abort_flag != 0);
@@ -499,20 +503,29 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
     if constexpr (CS > 1) {
 #pragma unroll
       for (int j = 0; j < NH; ++j) fin[j] = 0.f;
-      const uint32_t mine = smem_u32(smem) + (uint32_t)((c0 * SMALL + row) * 4);
+      const uint32_t mine = smem_u32(smem) + (uint32_t)((c0 / 4 * SMALL + row) * 16);
+      float4 t[CS][NH / 4];
 #pragma unroll
       for (int r = 0; r < CS; ++r) {
         const uint32_t from = tc::mapa_shared(mine, (uint32_t)r);
 #pragma unroll
-        for (int j = 0; j < NH; ++j) fin[j] += ld_cluster(from + (uint32_t)(j * SMALL * 4));
+        for (int j = 0; j < NH / 4; ++j) t[r][j] = ld_cluster4(from + (uint32_t)(j * SMALL * 16));
+      }
+#pragma unroll
+      for (int r = 0; r < CS; ++r) {
+#pragma unroll
+        for (int j = 0; j < NH / 4; ++j) {
+          fin[4 * j] += t[r][j].x; fin[4 * j + 1] += t[r][j].y; fin[4 * j + 2] += t[r][j].z; fin[4 * j + 3] += t[r][j].w;
+        }
       }
     } else {
 #pragma unroll
       for (int j = 0; j < NH; ++j) fin[j] = acc[j];
     }
     // (the stages behind the cluster's sums are free)
-    epi(p, fin, batch, 0, mt * SMALL + row, nt * SMALL + c0,
-        reinterpret_cast<char*>(smem + SMALL * SMALL * 4) + (warp - 4) * 4096);
+    char* sm = reinterpret_cast<char*>(smem + SMALL * SMALL * 4) + (warp - 4) * 4096;
+    if constexpr (Epi::kAhead) epi(p, fin, batch, mt * SMALL + row, nt * SMALL + c0, sm, ahead);
+    else epi(p, fin, batch, 0, mt * SMALL + row, nt * SMALL + c0, sm);
   }
   // ---------------- teardown ----------------
   tc::tc_fence_before();
@@ -672,6 +685,7 @@ __device__ __forceinline__ void store_terms(const float (&v)[NH], char* sm, __ha
 
 // fp32 partial sums of a contraction slice: part[ks][batch][M][pitch]
 struct EpiPartial {
+  static constexpr bool kAhead = false;
   float* part;
   int pitch;             // multiple of 4
   template <int NH>
@@ -847,12 +861,15 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
              : DK_ERR_CUDA;
 }
 
-// The product by the way `t` says; `epi` finishes its elements (t.cs > 0 or t.ksplit == 1).
+// The product by the way `t` says; `epi` finishes its elements (t.cs > 0, or t.ksplit == 1 and an epilogue that has
+// nothing to fetch ahead).
 template <int NPROD, bool AMN, bool BMN, class Epi>
 dk_status product(dk_ctx* ctx, const Tiling& t, const Operand& A, const Operand& B, const Params& p, const Epi& epi,
                   cudaStream_t st) {
+  if constexpr (!Epi::kAhead) {
+    if (t.cs == 0) return launch<NPROD, AMN, BMN, 256, Epi>(ctx, A, B, p, epi, st);
+  }
   switch (t.cs) {
-    case 0: return launch<NPROD, AMN, BMN, 256, Epi>(ctx, A, B, p, epi, st);
     case 1: return launch_small<NPROD, AMN, BMN, 1, Epi>(ctx, A, B, p, epi, st);
     case 2: return launch_small<NPROD, AMN, BMN, 2, Epi>(ctx, A, B, p, epi, st);
     case 4: return launch_small<NPROD, AMN, BMN, 4, Epi>(ctx, A, B, p, epi, st);

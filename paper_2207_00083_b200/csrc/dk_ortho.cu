@@ -171,40 +171,37 @@ __global__ void __launch_bounds__(256) ortho_sym_kernel(const SymArgs q) {
 // The same from a product that is finished where it is formed (tiles of the small kernel): this thread's NH columns of
 // its row, on or below the diagonal, and their mirror images.
 struct EpiSym {
+  static constexpr bool kAhead = true;
   SymArgs q;
+  // A at this thread's columns (both terms of each in a word), from the mirrored positions: neighbours across the lanes
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params&, float (&acc)[NH], int batch, int, int row, int col0,
-                                             char* sm) const {
-    const int row0 = row - (int)(threadIdx.x & 31);
+  __device__ __forceinline__ void fetch(int batch, int row, int col0, uint32_t (&a)[NH]) const {
+    const size_t mirror = (size_t)batch * q.s * q.pitch + (size_t)col0 * q.pitch + row;
+    const uint16_t* hi = reinterpret_cast<const uint16_t*>(q.a_hi) + mirror;
+    const uint16_t* lo = reinterpret_cast<const uint16_t*>(q.a_lo) + mirror;
+    const int last = q.poly ? min(NH - 1, (row < q.s ? row : -1) - col0) : -1;
+#pragma unroll
+    for (int j = 0; j < NH; ++j) {
+      a[j] = 0u;
+      if (j <= last) a[j] = (uint32_t)hi[(size_t)j * q.pitch] | (uint32_t)lo[(size_t)j * q.pitch] << 16;
+    }
+  }
+  template <int NH>
+  __device__ __forceinline__ void operator()(const Params&, float (&acc)[NH], int batch, int row, int col0, char* sm,
+                                             const uint32_t (&a)[NH]) const {
+    const int lane = threadIdx.x & 31, row0 = row - lane;
     if (row0 >= q.s || col0 >= q.s || col0 > row0 + 31) return;      // (nothing there on or below the diagonal)
     const size_t plane = (size_t)batch * q.s * q.pitch;
-    // Mirrored positions are neighbours across the lanes (rows): A is read there, and both of a value's terms are
-    // written there, a line for all 32.
-    const size_t mirror = plane + (size_t)col0 * q.pitch + row;
-    const int last = min(NH - 1, (row < q.s ? row : -1) - col0);      // this thread's last column on or below the diagonal
-    if (q.poly) {
 #pragma unroll
-      for (int c = 0; c < NH; c += 8) {
-        __half h[8], l[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          h[j] = l[j] = __float2half(0.f);
-          if (c + j <= last) {
-            h[j] = q.a_hi[mirror + (size_t)(c + j) * q.pitch];
-            l[j] = q.a_lo[mirror + (size_t)(c + j) * q.pitch];
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float av = (__half2float(h[j]) + __half2float(l[j])) * (1.f / kA);
-          float v = fmaf(q.c, acc[c + j] * q.f, q.b * av);
-          if (col0 + c + j == row) v += q.a;
-          acc[c + j] = v * kB;
-        }
+    for (int j = 0; j < NH; ++j) {
+      float v = acc[j] * q.f;
+      if (q.poly) {
+        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&a[j]));
+        v = fmaf(q.c, v, q.b * ((t.x + t.y) * (1.f / kA)));
+        if (col0 + j == row) v += q.a;
+        v *= kB;
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NH; ++j) acc[j] *= q.f;
+      acc[j] = v;
     }
     const size_t to = plane + (size_t)row0 * q.pitch + col0;
     constexpr int W = NH < 32 ? NH : 32;
@@ -212,14 +209,6 @@ struct EpiSym {
     for (int c0 = 0; c0 < NH; c0 += W) {
       uint32_t h[W / 2], l[W / 2];
       g16::to_terms<W>(acc, c0, h, l);
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        if (c0 + j <= last) {
-          const size_t at = mirror + (size_t)(c0 + j) * q.pitch;
-          reinterpret_cast<uint16_t*>(q.hi)[at] = (uint16_t)(j & 1 ? h[j / 2] >> 16 : h[j / 2]);
-          reinterpret_cast<uint16_t*>(q.lo)[at] = (uint16_t)(j & 1 ? l[j / 2] >> 16 : l[j / 2]);
-        }
-      }
       // elements on and below the diagonal only: what lies above it is the mirror image of others
       auto put = [&](__half* dst, int r, int c, const uint4& u) {
         const int count = min(row0 + r, q.s - 1) - (col0 + c0 + c) + 1;
@@ -227,6 +216,38 @@ struct EpiSym {
       };
       g16::warp_block_16<W>(h, sm, [&](int r, int c, const uint4& u) { put(q.hi, r, c, u); });
       g16::warp_block_16<W>(l, sm, [&](int r, int c, const uint4& u) { put(q.lo, r, c, u); });
+      // the mirror image: both terms of an element in a word, [column][row], and eight rows of a column to a store
+      uint32_t* words = reinterpret_cast<uint32_t*>(sm);
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+        words[j * 32 + lane] = j & 1 ? __byte_perm(h[j / 2], l[j / 2], 0x7632) : __byte_perm(h[j / 2], l[j / 2], 0x5410);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < W / 8; ++i) {
+        const int c = i * 8 + lane / 4, r = (lane % 4) * 8, col = col0 + c0 + c;
+        const uint4 u = *reinterpret_cast<const uint4*>(words + c * 32 + r), v = *reinterpret_cast<const uint4*>(words + c * 32 + r + 4);
+        const uint4 hi = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.z, u.w, 0x5410),
+                                    __byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x5410));
+        const uint4 lo = make_uint4(__byte_perm(u.x, u.y, 0x7632), __byte_perm(u.z, u.w, 0x7632),
+                                    __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x7632));
+        const int first = row0 + r;
+        if (col >= q.s || first >= q.s) continue;
+        const size_t at = plane + (size_t)col * q.pitch + first;
+        if (col < first) {                 // strictly below the diagonal (the pitch has room for whole pieces)
+          *reinterpret_cast<uint4*>(q.hi + at) = hi;
+          *reinterpret_cast<uint4*>(q.lo + at) = lo;
+        } else {
+          const uint32_t hw[4] = {hi.x, hi.y, hi.z, hi.w}, lw[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (first + k < q.s && first + k > col) {
+              reinterpret_cast<uint16_t*>(q.hi)[at + k] = (uint16_t)(k & 1 ? hw[k / 2] >> 16 : hw[k / 2] & 0xffffu);
+              reinterpret_cast<uint16_t*>(q.lo)[at + k] = (uint16_t)(k & 1 ? lw[k / 2] >> 16 : lw[k / 2] & 0xffffu);
+            }
+          }
+        }
+      }
     }
   }
 };
@@ -242,6 +263,7 @@ struct XArgs {
   float scale, keep;
 };
 struct EpiX {
+  static constexpr bool kAhead = false;
   XArgs a;
   template <int NH>
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int batch, int, int row, int col0,

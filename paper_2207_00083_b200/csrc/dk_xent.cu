@@ -247,6 +247,7 @@ struct Undo {
 
 // forward epilogue: maximum and sum of exponentials of this thread's columns of its row, and the target's logit
 struct EpiLse {
+  static constexpr bool kAhead = false;
   float2* part;                // [columns / (BN/2)][rows]
   float* tlogit;               // [rows]
   const int64_t* target;
@@ -312,6 +313,7 @@ struct RowArgs {
 // backward epilogue: p of this piece
 template <bool F32>
 struct EpiP {
+  static constexpr bool kAhead = false;
   RowArgs r;
   Undo undo;
   template <int NH>
@@ -360,6 +362,7 @@ struct EpiP {
 // gradients: out = alpha*product (+ what earlier pieces left in `acc`), as fp32 in `acc` or rounded in `out`
 template <bool F32>
 struct EpiGrad {
+  static constexpr bool kAhead = false;
   void* out;                   // null: the sum goes to accum
   float* accum;                // fp32 [M][pitch_acc]
   long long pitch, pitch_acc;
