@@ -237,6 +237,40 @@ def test_offsets_past_32_bits(ctx):
     assert float((dx[-1:].double() - want).abs().max()) <= 2.0 ** -8 * 8
 
 
+def test_in_a_graph(ctx):
+    """Captured and replayed on other values: nothing but the launches is kept."""
+    for shape, groups in (((2, 7, 7, 64), 8), ((6, 90, 90, 64), 16)):
+        x, gamma, beta, dy = draw(*shape, torch.float32, seed=11)
+        q, y, stats = run_fwd(ctx, x, gamma, beta, groups, "silu", dk.DK_F32)
+        dx, dg, db = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+        dk.dk_group_norm_bwd(ctx, q, dy, x, gamma, beta, stats, dx, dg, db)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            dk.dk_group_norm_fwd(ctx, q, x, gamma, beta, y, stats)
+            dk.dk_group_norm_bwd(ctx, q, dy, x, gamma, beta, stats, dx, dg, db)
+        x.copy_(draw(*shape, torch.float32, seed=12)[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        _, y2, stats2 = run_fwd(ctx, x, gamma, beta, groups, "silu", dk.DK_F32)
+        dx2, dg2, db2 = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+        dk.dk_group_norm_bwd(ctx, q, dy, x, gamma, beta, stats2, dx2, dg2, db2)
+        assert all(torch.equal(a, b) for a, b in ((y, y2), (stats, stats2), (dx, dx2), (dg, dg2), (db, db2)))
+
+
+def test_more_samples_than_counters(ctx):
+    """Samples in slabs, more of them than the context has counters for."""
+    x, gamma, beta, dy = draw(17000, 3, 3, 2048, torch.bfloat16, seed=13)
+    q, y, stats = run_fwd(ctx, x, gamma, beta, 1, "none", dk.DK_BF16)
+    want, _, mean, rstd = forward64(x[-3:], gamma, beta, 1, "none")
+    assert float((y[-3:].double() - want).abs().max()) <= 2.0 ** -8 * 8
+    dx, dg, db = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+    dk.dk_group_norm_bwd(ctx, q, dy, x, gamma, beta, stats, dx, dg, db)
+    total = dy.double().sum(dim=(0, 1, 2))
+    assert float((db.double() - total).abs().max()) <= 64 * 2.0 ** -24 * float(dy.double().abs().sum(dim=(0, 1, 2)).max())
+    want = backward64(dy[-3:], x[-3:], gamma, beta, 1, "none", stats[-3:, :, 0].double(), stats[-3:, :, 1].double())[0]
+    assert float((dx[-3:].double() - want).abs().max()) <= 2.0 ** -8 * 8 * float(gamma.abs().max())
+
+
 def test_another_stream(ctx):
     x, gamma, beta, _ = draw(2, 30, 30, 64, torch.float32, seed=10)
     want = run_fwd(ctx, x, gamma, beta, 8, "silu", dk.DK_F32)[1]
