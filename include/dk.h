@@ -398,7 +398,10 @@ DK_API dk_status dk_relu_pool_bwd(dk_ctx* ctx, const float* dy, const float* x, 
  * are DK_F32 or DK_BF16 (one type per call; sums, statistics, norms and the
  * contractions' accumulators are fp32), contiguous and 16-byte aligned;
  * parameters, statistics and losses are fp32.  Large scratch memory is the
- * workspace of dk_set_workspace, sized by the *_workspace_bytes calls.
+ * workspace of dk_set_workspace, sized by the *_workspace_bytes calls.  Every
+ * sum has a fixed order: the same call gives the same bits.  A wait that expires
+ * (dk_device_status: DK_ERR_TIMEOUT) leaves this call's output incomplete, and
+ * later ones' until dk_device_status has been called.
  * ------------------------------------------------------------------------- */
 enum { DK_F32 = 0, DK_BF16 = 1 };
 enum { DK_ACT_NONE = 0, DK_ACT_RELU = 1, DK_ACT_SILU = 2 };
@@ -455,9 +458,9 @@ DK_API dk_status dk_xent_workspace_bytes(const dk_xent* q, size_t* bytes);
  * and lse are 0 and its values of h, whatever they are, are not used.  A target
  * >= vocab is left out likewise and reported by dk_device_status as
  * DK_ERR_INVALID_ARG.  DK_F32 contracts on the tensor cores with each operand
- * as two fp16 terms under a common power of two (22 significant bits down to
- * 2^-18 of the tensor's largest magnitude, an absolute error of 2^-40 of that
- * magnitude below).  Needs the workspace. */
+ * as two fp16 terms under a power of two of each row of h and W (22 significant
+ * bits down to 2^-18 of the row's largest magnitude, an absolute error of 2^-40
+ * of that magnitude below).  Needs the workspace. */
 DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
                                     const int64_t* target, float* loss, float* lse, void* stream);
 
@@ -465,8 +468,9 @@ DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h
  *   p[r][v] = scale*dloss[r]*(exp(l[v] - lse[r]) - [v == target[r]]), 0 for rows left out
  *   dh = p.W,  dW = p^T.h
  * lse: from the forward call.  With DK_BF16 p is rounded to bf16 for the two
- * products, with DK_F32 it is kept as two fp16 terms.  dh and dW are
- * overwritten.  Needs the workspace. */
+ * products, with DK_F32 it is kept as two fp16 terms, and h and W are taken
+ * under one power of two each (of the whole tensor: the products sum over their
+ * rows).  dh and dW are overwritten.  Needs the workspace. */
 DK_API dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
                                     const int64_t* target, const float* lse, const float* dloss, float scale,
                                     void* dh, void* dW, void* stream);
@@ -479,9 +483,14 @@ DK_API dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h
  *   out = keep*out + scale*X.
  * keep = 0 writes the update itself (out is not read); keep = 1 - lr*decay and
  * scale = -lr with `out` the weights applies it.  x may be the dW of
- * dk_linear_bwd_wgrad or a running mean of it; x and out are different tensors. */
+ * dk_linear_bwd_wgrad or a running mean of it; x and out are different tensors.
+ * The contractions keep X, A and b A + c A A as two fp16 terms under fixed powers
+ * of two, whose range holds while no singular value exceeds sqrt(2) on its way
+ * from [0, 1]: (3.4445, -4.7750, 2.0315) reaches 1.21, (1.5, -0.5, 0) reaches 1.
+ * Coefficients that let one grow further give infinities or NaN.  The result has
+ * the accuracy of fp32 arithmetic; a DK_BF16 result is rounded once. */
 typedef struct {
-  int32_t batch, m, n; /* m, n <= 65536                                           */
+  int32_t batch, m, n; /* batch <= 4096; m, n <= 65536; batch*m*n <= 4e10         */
   int32_t dtype;       /* of x and out                                            */
   int32_t steps;       /* 0 .. 32                                                 */
   float a, b, c;       /* |a| + 2|b| + 4|c| <= 31                                 */

@@ -14,7 +14,9 @@
 // So the accumulator in tensor memory takes `chunk` stages at a time and the epilogue warps add the chunks up in fp32
 // registers, rounding to nearest.  What is lost within a chunk is a bias, the same relative amount again and again where
 // the terms have one sign (the squares on the diagonal of X X^T), and `comp`, per stage, gives it back on average.  Two
-// accumulators of BN columns let the epilogue of one tile run beside the products of the next.
+// accumulators of BN columns let the epilogue of one tile run beside the products of the next.  (The small tiles have
+// columns to spare: there the products with a low term have an accumulator of their own, 2^-11 times as large, whose
+// losses do not count.)
 #pragma once
 
 #include <cuda_bf16.h>

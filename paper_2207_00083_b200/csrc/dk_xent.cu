@@ -591,7 +591,7 @@ Plan plan_xent(const dk_xent& q) {
   const size_t es = p.f32 ? 4 : 2;             // bytes of one operand element, both terms
   const long long T = q.rows > 0 ? q.rows : 1;
   long long vp = kPieceBytes / (T * (long long)es) / BN * BN;
-  if (vp < 8 * BN) vp = 8 * BN;
+  if (vp < 2 * BN) vp = 2 * BN;
   if (vp >= q.vocab) vp = q.vocab;
   p.pieces = (int)((q.vocab + vp - 1) / vp);
   if (p.pieces > 1) {                           // even pieces

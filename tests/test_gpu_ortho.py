@@ -69,6 +69,60 @@ def test_against_the_formula(ctx, b, m, n, kind, dtype):
     assert dk.dk_device_status(ctx) == 0
 
 
+# large tiles with and without slices of the contraction; a short side whose columns do not fit in all SMs at once; more
+# matrices than SMs; gangs of CTAs of every kind
+PATHS = [(1, 2300, 2500), (1, 2500, 2300), (1, 16, 60000), (1, 60000, 16), (200, 8, 300), (30, 64, 640), (1, 128, 18900),
+         (1, 128, 33000), (2, 40, 70), (1, 128, 128), (1, 129, 700), (1, 65, 64), (5, 200, 1500)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,m,n", PATHS)
+def test_every_way_through(ctx, b, m, n, dtype):
+    dt, tt = TYPES[dtype]
+    x = draw(b, m, n, tt, seed=11, kind="decay")
+    got, want = call(ctx, x, dt), exact(x)
+    tol = 2.0 ** -8 if dtype == "bf16" else 1e-4
+    for g, w in zip(got, want):
+        assert float((g.double() - w).norm()) <= tol * float(w.norm())
+    assert dk.dk_device_status(ctx) == 0
+    assert torch.equal(got, call(ctx, x, dt))
+
+
+def test_interleaved_with_other_calls(ctx):
+    """Calls that use the context's counters and the workspace one after the other, none waited for."""
+    x, y = draw(1, 64, 576, torch.float32, seed=12), draw(3, 100, 900, torch.float32, seed=13)
+    h = torch.randn((4, 60, 60, 32), device="cuda")
+    q = dk.dk_norm(4, 60, 60, 32, 4, 1, 0, 1e-5)
+    gamma, beta, stats = torch.ones(32, device="cuda"), torch.zeros(32, device="cuda"), torch.empty((4, 4, 2), device="cuda")
+    for p in (q, dk.dk_ortho(3, 100, 900, 0, 5, *QUINTIC, EPS)):
+        ctx.ensure_workspace(p)
+    want = []
+    for i in range(6):
+        z = torch.empty_like(h)
+        a = call(ctx, x, dk.DK_F32)
+        ctx.ensure_workspace(q)
+        dk.dk_group_norm_fwd(ctx, q, h, gamma, beta, z, stats)
+        b = call(ctx, y, dk.DK_F32)
+        want.append((a, z, b))
+    for got in want[1:]:
+        assert all(torch.equal(u, v) for u, v in zip(got, want[0]))
+
+
+def test_in_a_graph(ctx):
+    """Captured and replayed on other values: nothing but the launches is kept."""
+    cases = [draw(1, 64, 576, torch.float32, seed=14), draw(1, 300, 700, torch.float32, seed=15)]
+    for x in cases:
+        out = call(ctx, x, dk.DK_F32)
+        q = dk.dk_ortho(*x.shape, dk.DK_F32, 5, *QUINTIC, EPS)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            dk.dk_orthogonalize(ctx, q, x, 1.0, 0.0, out)
+        x.copy_(draw(*x.shape, torch.float32, seed=16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, call(ctx, x, dk.DK_F32))
+
+
 def test_singular_values_are_brought_together(ctx):
     """Five steps of the quintic take every singular value of a well-conditioned matrix into [0.65, 1.25]."""
     x = draw(1, 200, 900, torch.float32, seed=2)

@@ -238,6 +238,31 @@ def test_offsets_past_32_bits(ctx):
     assert bool(torch.isfinite(dh).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,vocab", [(50, 64, 900), (900, 256, 4000)])
+def test_in_a_graph(ctx, dtype, rows, d, vocab):
+    """Captured and replayed on other values: nothing but the launches is kept."""
+    dt, tt = TYPES[dtype]
+    h, W, t = draw(rows, d, vocab, tt, seed=17)
+    loss, lse, dh, dW = call(ctx, h, W, t, dt)
+    q = dk.dk_xent(rows, d, vocab, dt)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dk.dk_linear_xent_fwd(ctx, q, h, W, t, loss, lse)
+        dk.dk_linear_xent_bwd(ctx, q, h, W, t, lse, None, 1.0, dh, dW)
+    h2, W2, t2 = draw(rows, d, vocab, tt, seed=18)
+    h.copy_(h2); W.copy_(W2); t.copy_(t2)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((loss, lse, dh, dW), call(ctx, h, W, t, dt)))
+
+
+def test_many_rows(ctx):
+    """So many rows that a piece is a few hundred classes wide."""
+    h, W, t = draw(150000, 16, 1400, torch.float32, seed=19)
+    check(ctx, h, W, t, "f32", scale=1e-3)
+
+
 def test_another_stream(ctx):
     h, W, t = draw(300, 128, 2000, torch.bfloat16, seed=15)
     want = call(ctx, h, W, t, dk.DK_BF16)
