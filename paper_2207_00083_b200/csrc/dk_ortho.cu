@@ -366,8 +366,11 @@ constexpr int kResThreads = 256;
 constexpr int kDirect = 28 * 1024;      // elements of A times CTAs of the gang
 
 constexpr int kBlock = 128 * 128;            // bytes of one [128][64] fp16 block
-// what the tensor pipe loses per 64 contraction elements (see kLossSquares)
-constexpr float kResLossSquares = 4.4f / 16777216.f, kResLossMixed = 1.2f / 16777216.f;
+// What the tensor pipe loses per 16 contraction elements, one instruction (see kLossSquares).  What it gives back is an
+// average; in A A, which the polynomial's first steps amplify most, what is left is halved by three accumulators
+// (against plain fp32, 64x576: 1.5 times its error with one, 0.9 with three; 128x1152: 1.2 and 0.75; 2 us of 120).
+// (A A's own constant is the best of 0, 0.3, .. 1.7 over short sides of 16 to 128.)
+constexpr float kResLossSquares = 1.1f / 16777216.f, kResLossAA = 1.5f / 16777216.f, kResLossMixed = 0.3f / 16777216.f;
 
 struct ResArgs {
   const void* x;
@@ -550,39 +553,38 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
   const uint32_t idesc_x = (1u << 4) | (1u << 16) | ((uint32_t)(q.C >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
   const uint32_t uxh = tc::smem_u32(xh), uxl = tc::smem_u32(xl), uah = tc::smem_u32(ah), ual = tc::smem_u32(al);
   const size_t mine = ((size_t)mat * q.gang + g) * 128 * 128;
+  // instructions (of 16) that cover the columns and the shorter side: zeros beyond them are not multiplied
+  const int kcols = (cols + 15) / 16, ks = (q.s + 15) / 16;
+  // 32 columns of this thread's row: the products with a low term (from column 0 of tensor memory), and those of high
+  // terms, `k` instructions in accumulators of `per` from column `first`, with what the instructions lose given back
+  auto sum_of = [&](uint32_t col, uint32_t first, int k, int per, float loss, float* to) {
+    g16::ld32(tmem + lanes + col, to);
+    for (int k0 = 0; k0 < k; k0 += per, first += 128u) {
+      float t[32];
+      g16::ld32(tmem + lanes + first + col, t);
+      tc::tc_wait_ld();
+      const float f = (float)min(per, k - k0) * loss;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) to[j] += fmaf(t[j], f, t[j]);
+    }
+  };
   for (int step = 0; alive && step < q.steps; ++step) {
-    // ---- this CTA's share of A: two blocks (128 columns) per accumulator, the low terms' products in one apart ----
+    // ---- this CTA's share of A ----
     operands_ready();
     if (threadIdx.x == 0) {
-      for (int k = 0; k < nblk; ++k) {
-        const uint64_t h = tc::make_desc<128>(uxh + k * kBlock), l = tc::make_desc<128>(uxl + k * kBlock);
-        const uint32_t d = tmem + (uint32_t)(k >> 1) * 128u;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          g16::mma_f16(d, h + 2 * kk, h + 2 * kk, idesc, ((k & 1) | kk) ? 1u : 0u);
-          g16::mma_f16(tmem + 256u, h + 2 * kk, l + 2 * kk, idesc, (k | kk) ? 1u : 0u);
-          g16::mma_f16(tmem + 256u, l + 2 * kk, h + 2 * kk, idesc, 1u);
-        }
+      for (int k = 0; k < kcols; ++k) {
+        const uint64_t h = tc::make_desc<128>(uxh + (k >> 2) * kBlock) + 2 * (k & 3);
+        const uint64_t l = tc::make_desc<128>(uxl + (k >> 2) * kBlock) + 2 * (k & 3);
+        g16::mma_f16(tmem + 128u, h, h, idesc, k ? 1u : 0u);
+        g16::mma_f16(tmem, h, l, idesc, k ? 1u : 0u);
+        g16::mma_f16(tmem, l, h, idesc, 1u);
       }
       tc::tc_commit(&bar);
     }
     if (!products_done()) { alive = false; break; }
     float A[64];
 #pragma unroll
-    for (int c = 0; c < 64; c += 32) {
-      g16::ld32(tmem + lanes + (uint32_t)(half * 64 + c), A + c);
-      tc::tc_wait_ld();
-#pragma unroll
-      for (int j = 0; j < 32; ++j) A[c + j] = fmaf(A[c + j], (nblk > 1 ? 2.f : 1.f) * kResLossSquares, A[c + j]);
-      for (uint32_t more = nblk > 2 ? 128u : 256u; more <= 256u; more += 128u) {
-        float t[32];
-        g16::ld32(tmem + lanes + more + (uint32_t)(half * 64 + c), t);
-        tc::tc_wait_ld();
-        const float loss = more == 256u ? 0.f : (float)(nblk - 2) * kResLossSquares;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) A[c + j] += fmaf(t[j], loss, t[j]);
-      }
-    }
+    for (int c = 0; c < 64; c += 32) sum_of((uint32_t)(half * 64 + c), 128u, kcols, kcols, kResLossSquares, A + c);
     if (q.gang > 1) {
       if (row < q.s) {
 #pragma unroll
@@ -646,35 +648,30 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
       for (int j = 0; j < 64; ++j) A[j] = row < q.s && half * 64 + j < q.s ? sums[(half * 64 + j) * 128 + row] : 0.f;
       __syncthreads();
     }
-    // ---- A's terms, A A, B's terms in their place ----
+    // ---- A's terms, A A (in up to three accumulators), B's terms in their place ----
 #pragma unroll
     for (int j = 0; j < 64; j += 8) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) A[j + k] *= kA / (kX * kX);
       put8(ah, al, row, half * 64 + j, A + j);
     }
+    const int per = (ks + 2) / 3;
     operands_ready();
     if (threadIdx.x == 0) {
-      for (int k = 0; k < 2; ++k) {
-        const uint64_t h = tc::make_desc<128>(uah + k * kBlock), l = tc::make_desc<128>(ual + k * kBlock);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          g16::mma_f16(tmem, h + 2 * kk, h + 2 * kk, idesc, (k | kk) ? 1u : 0u);
-          g16::mma_f16(tmem + 128u, h + 2 * kk, l + 2 * kk, idesc, (k | kk) ? 1u : 0u);
-          g16::mma_f16(tmem + 128u, l + 2 * kk, h + 2 * kk, idesc, 1u);
-        }
+      for (int k = 0; k < ks; ++k) {
+        const uint64_t h = tc::make_desc<128>(uah + (k >> 2) * kBlock) + 2 * (k & 3);
+        const uint64_t l = tc::make_desc<128>(ual + (k >> 2) * kBlock) + 2 * (k & 3);
+        g16::mma_f16(tmem + 128u * (uint32_t)(1 + k / per), h, h, idesc, k % per ? 1u : 0u);
+        g16::mma_f16(tmem, h, l, idesc, k ? 1u : 0u);
+        g16::mma_f16(tmem, l, h, idesc, 1u);
       }
       tc::tc_commit(&bar);
     }
     if (!products_done()) { alive = false; break; }
 #pragma unroll
     for (int c = 0; c < 64; c += 32) {
-      float t[32], low[32];
-      g16::ld32(tmem + lanes + (uint32_t)(half * 64 + c), t);
-      g16::ld32(tmem + lanes + 128u + (uint32_t)(half * 64 + c), low);
-      tc::tc_wait_ld();
-#pragma unroll
-      for (int j = 0; j < 32; ++j) t[j] += fmaf(t[j], 2.f * kResLossSquares, low[j]);
+      float t[32];
+      sum_of((uint32_t)(half * 64 + c), 128u, ks, per, kResLossAA, t);
 #pragma unroll
       for (int j = 0; j < 32; j += 8) {
         float v[8];
@@ -691,7 +688,7 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
     operands_ready();
     if (threadIdx.x == 0) {
       const uint64_t xhd = desc_mn_blocks(uxh), xld = desc_mn_blocks(uxl);
-      for (int k = 0; k < 8; ++k) {          // 16 rows of X each
+      for (int k = 0; k < ks; ++k) {         // 16 rows of X each
         const uint64_t bh = tc::make_desc<128>(uah + (k >> 2) * kBlock) + 2 * (k & 3);
         const uint64_t bl = tc::make_desc<128>(ual + (k >> 2) * kBlock) + 2 * (k & 3);
         g16::mma_f16(tmem + 256u, bh, xhd + 128 * k, idesc_x, k ? 1u : 0u);
@@ -703,12 +700,8 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
     if (!products_done()) { alive = false; break; }
     const bool last = step + 1 == q.steps;
     for (int c = half * (q.C / 2); c < (half + 1) * (q.C / 2); c += 32) {
-      float t[32], low[32];
-      g16::ld32(tmem + lanes + 256u + (uint32_t)c, t);
-      g16::ld32(tmem + lanes + (uint32_t)c, low);
-      tc::tc_wait_ld();
-#pragma unroll
-      for (int j = 0; j < 32; ++j) t[j] += fmaf(t[j], 2.f * kResLossMixed, low[j]);
+      float t[32];
+      sum_of((uint32_t)c, 256u, ks, ks, kResLossMixed, t);
       if (!last) {
 #pragma unroll
         for (int j = 0; j < 32; j += 8) {
@@ -812,13 +805,22 @@ dk_status check_ortho(const dk_ortho* q) {
 constexpr float kUlp = 1.f / 16777216.f;
 constexpr float kLossSquares[2] = {6.6f * kUlp, 4.4f * kUlp}, kLossMixed[2] = {3.6f * kUlp, 1.2f * kUlp};
 
-Params gemm_params(const g16::Tiling& t, const dk_ortho& q, long long M, long long N, bool sym) {
+// Stages added up in tensor memory: as even as at most four allow.  What is lost in A A counts most (the polynomial's
+// first steps amplify it, the more the smaller the matrices are): up to a short side of 512 each stage is promoted
+// (against plain fp32, at 4 stages and at 1: 256x2304 2.2 times its error and 0.8, 320x10000 2.7 and 1.2, 512x4608
+// 1.05 and 0.8, for 1-5 % of the call; 1001x1961 0.8 and 0.5, 4096x25088 0.7 and 0.35 for 4 % and 10 % are not taken).
+int chunk_of(const g16::Tiling& t, int most) {
+  const int chunks = (t.kb_per_split + most - 1) / most;
+  return (t.kb_per_split + chunks - 1) / chunks;
+}
+
+Params gemm_params(const g16::Tiling& t, const dk_ortho& q, long long M, long long N, bool sym, int most = 4) {
   Params p = {};
   p.MT = t.MT; p.NT = t.NT; p.nbatch = q.batch; p.sym = sym ? 1 : 0; p.tiles = t.tiles;
   p.KB = t.KB; p.ksplit = t.ksplit; p.kb_per_split = t.kb_per_split;
   p.M = (int)M; p.N = (int)N;
   p.bf16 = 0;
-  p.chunk = 4;
+  p.chunk = chunk_of(t, most);
   p.comp = sym ? kLossSquares[0] : kLossMixed[0];
   p.comp_small = sym ? kLossSquares[1] : kLossMixed[1];
   return p;
@@ -926,7 +928,7 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
       DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st, sa));
     }
     // B
-    p = gemm_params(tp, q, pl.s, pl.s, true);
+    p = gemm_params(tp, q, pl.s, pl.s, true, pl.s <= 512 ? 1 : 4);
     sa.ks = tp.ksplit; sa.f = 1.f / (kA * kA); sa.poly = 1; sa.hi = bm; sa.lo = bm + pl.s_plane;
     if (tp.cs) {
       s = g16::product<3, false, false>(ctx, tp, A, A, p, EpiSym{sa}, st);
