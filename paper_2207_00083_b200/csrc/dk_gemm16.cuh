@@ -671,7 +671,7 @@ __device__ __forceinline__ void put_piece32(float* dst, const float4& u, int cou
 template <int NH>
 __device__ __forceinline__ void store_terms(const float (&v)[NH], char* sm, __half* hi, __half* lo, long long pitch, int rows,
                                             int cols) {
-  constexpr int W = NH < 64 ? NH : 64;
+  constexpr int W = NH <= 64 ? NH : 32;            // (64 of 128 values at a time spill)
 #pragma unroll
   for (int c0 = 0; c0 < NH; c0 += W) {
     uint32_t h[W / 2], l[W / 2];
@@ -711,15 +711,19 @@ struct EpiPartial {
 constexpr int kSmallCtas = 8 * kMaxSms;      // most CTAs of a product in small tiles
 struct Tiling {
   int cs;
+  int narrow;                  // cs = 0: tiles of 256 x 128
   int MT, NT, tiles, KB, ksplit, kb_per_split;
 };
 
 // Cost in cycles of either way, from what was measured: a stage (64 contraction elements) of the pair's tile takes 512
-// cycles per product, of the small tile 256, but the small tile's operands arrive at ~50 bytes per cycle and SM, which
-// is what binds it (16 KiB per operand plane); some 9000 cycles go to a launch's start, fill and epilogue, 6000 more to
-// joining a cluster's slices, 24000 to the partial sums' way through global memory and a second kernel.  Clusters of
-// four and eight do not tile the GPCs: 33 and 15 of them are resident at once on 148 SMs.
-inline Tiling plan(long long M, long long N, long long K, int nbatch, bool sym, int sms, int nprod) {
+// cycles per product, of the small tile 256, but what binds the small tile is shared memory, where its operands arrive
+// and every product reads them again (measured as 16 KiB per operand plane at 50 bytes per cycle); some 9000 cycles go
+// to a launch's start, fill and epilogue, 6000 more to joining a cluster's slices, 24000 to the partial sums' way through
+// global memory and a second kernel.  Clusters of four and eight do not tile the GPCs: 33 and 15 of them are resident at
+// once on 148 SMs.  `narrow`: the caller has a kernel of three products for pair tiles of 256 x 128 too (the update's X:
+// 3 x 512x4608, 216 tiles instead of 108 on 74 pairs, 300 us -> 293 for the whole update; 4 x 130x5000 251 -> 236).
+inline Tiling plan(long long M, long long N, long long K, int nbatch, bool sym, int sms, int nprod,
+                   bool narrow = false) {
   Tiling best = {};
   double least = 0;
   const int KB = (int)((K + BK - 1) / BK);
@@ -756,6 +760,23 @@ inline Tiling plan(long long M, long long N, long long K, int nbatch, bool sym, 
       cost = waves * (t.kb_per_split * (stage > 256.0 * nprod ? stage : 256.0 * nprod) + 9000.0 + (cs > 1 ? 6000.0 : 0.0));
     }
     if (cs == 0 || cost < least) { least = cost; best = t; }
+  }
+  // Pair tiles of 256 x 128 instead of 256 x 256: a stage of three products takes 1150 cycles (operands through shared
+  // memory) against 1600, but they fill whole waves better, and their epilogue is half as long (3000 cycles against
+  // 6000, which a short contraction does not hide).
+  if (narrow && !best.cs && best.ksplit == 1) {
+    const int pairs = sms / 2;
+    Tiling t = best;
+    t.narrow = 1;
+    t.NT = (int)((N + 127) / 128);
+    auto cost = [&](const Tiling& v, double stage, double epilogue) {
+      const double waves = (double)(((long long)v.MT * v.NT * nbatch + pairs - 1) / pairs);
+      return waves * (KB * stage > epilogue ? KB * stage : epilogue) + epilogue;
+    };
+    if ((long long)t.MT * t.NT * nbatch < (1LL << 26) && cost(t, 1150.0, 3000.0) < cost(best, 1600.0, 6000.0)) {
+      t.tiles = t.MT * t.NT;
+      best = t;
+    }
   }
   return best;
 }
@@ -865,9 +886,12 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
 
 // The product by the way `t` says; `epi` finishes its elements (t.cs > 0, or t.ksplit == 1 and an epilogue that has
 // nothing to fetch ahead).
-template <int NPROD, bool AMN, bool BMN, class Epi>
+template <int NPROD, bool AMN, bool BMN, bool NARROW = false, class Epi>
 dk_status product(dk_ctx* ctx, const Tiling& t, const Operand& A, const Operand& B, const Params& p, const Epi& epi,
                   cudaStream_t st) {
+  if constexpr (NARROW) {
+    if (t.narrow) return launch<NPROD, AMN, BMN, 128, Epi>(ctx, A, B, p, epi, st);
+  }
   if constexpr (!Epi::kAhead) {
     if (t.cs == 0) return launch<NPROD, AMN, BMN, 256, Epi>(ctx, A, B, p, epi, st);
   }

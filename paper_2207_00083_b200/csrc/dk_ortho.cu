@@ -258,10 +258,12 @@ struct XArgs {
   __half* lo;
   long long pitch;             // of the terms
   void* out;
-  int n, dtype;
+  int n, dtype;                // (dtype: ortho_x_kernel's)
   float f;                     // undoes the operands' powers of two (and brings X to its own)
   float scale, keep;
 };
+constexpr int kTerms = 2;            // OUT: DK_F32, DK_BF16 or this
+template <int OUT>
 struct EpiX {
   static constexpr bool kAhead = false;
   XArgs a;
@@ -272,16 +274,13 @@ struct EpiX {
     if (row0 >= p.M || col0 >= p.N) return;
     const size_t first = (size_t)batch * p.M + row0;
     const int rows = p.M - row0, cols = p.N - col0;
-    const float f = a.hi != nullptr ? a.f : a.f * a.scale;
+    const float f = OUT == kTerms ? a.f : a.f * a.scale;
 #pragma unroll
     for (int j = 0; j < NH; ++j) acc[j] *= f;
-    if (a.hi != nullptr) {
-      const size_t to = first * a.pitch + col0;
+    const size_t to = first * (OUT == kTerms ? a.pitch : (long long)a.n) + col0;
+    if constexpr (OUT == kTerms) {
       g16::store_terms<NH>(acc, sm, a.hi + to, a.lo + to, a.pitch, rows, cols);
-      return;
-    }
-    const size_t to = first * a.n + col0;
-    if (a.dtype == DK_F32) {
+    } else if constexpr (OUT == DK_F32) {
       float* out = static_cast<float*>(a.out) + to;
       g16::warp_rows_f32<NH>(acc, sm, [&](int r, int c, float4 u) {
         if (r >= rows || c >= cols) return;
@@ -898,7 +897,7 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
 
   const g16::Tiling tg = g16::plan(pl.s, pl.s, pl.tall ? q.m : q.n, q.batch, true, sms, 3);
   const g16::Tiling tp = g16::plan(pl.s, pl.s, pl.s, q.batch, true, sms, 3);
-  const g16::Tiling tx = g16::plan(q.m, q.n, pl.s, q.batch, false, sms, 3);
+  const g16::Tiling tx = g16::plan(q.m, q.n, pl.s, q.batch, false, sms, 3, true);
   const int pitch_s = (pl.s + 3) / 4 * 4, pitch_x = (q.n + 3) / 4 * 4;
   const unsigned nt = (unsigned)((pl.sp + 31) / 32);
   SymArgs sa = {};
@@ -955,8 +954,12 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
       DK_CUDA_CHECK(launch_chained(ortho_x_kernel, dim3(grid_of(rows * ((q.n + 7) / 8), sms)), 256, 0, st,
                                  xa, part, tx.ksplit, pitch_x, nullptr, nullptr, rows, 0));
     } else {
-      s = pl.tall ? g16::product<3, false, false>(ctx, tx, X, B, p, EpiX{xa}, st)
-                  : g16::product<3, false, true>(ctx, tx, B, X, p, EpiX{xa}, st);
+      auto x_product = [&](auto epi) {
+        return pl.tall ? g16::product<3, false, false, true>(ctx, tx, X, B, p, epi, st)
+                       : g16::product<3, false, true, true>(ctx, tx, B, X, p, epi, st);
+      };
+      s = k + 1 < q.steps ? x_product(EpiX<kTerms>{xa})
+          : q.dtype == DK_F32 ? x_product(EpiX<DK_F32>{xa}) : x_product(EpiX<DK_BF16>{xa});
       if (s != DK_OK) return s;
     }
   }
