@@ -460,7 +460,9 @@ DK_API dk_status dk_xent_workspace_bytes(const dk_xent* q, size_t* bytes);
  * DK_ERR_INVALID_ARG.  DK_F32 contracts on the tensor cores with each operand
  * as two fp16 terms under a power of two of each row of h and W (22 significant
  * bits down to 2^-18 of the row's largest magnitude, an absolute error of 2^-40
- * of that magnitude below).  Needs the workspace. */
+ * of that magnitude below).  A token or a few (up to 8 rows with DK_F32, one with
+ * DK_BF16, d <= 8192) contract in fp32 instead, reading W once.  Needs the
+ * workspace. */
 DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
                                     const int64_t* target, float* loss, float* lse, void* stream);
 

@@ -263,6 +263,44 @@ def test_many_rows(ctx):
     check(ctx, h, W, t, "f32", scale=1e-3)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 2, 4, 5, 8, 9])
+@pytest.mark.parametrize("d,vocab", [(1, 1), (64, 33), (255, 1000), (258, 4097), (512, 20011), (1024, 60000), (4096, 700),
+                                     (2047, 300), (12288, 90), (30000, 40)])
+def test_few_rows(ctx, rows, d, vocab, dtype):
+    """A token or a handful, at lengths around a warp's step and vocabularies with and without classes for every warp."""
+    h, W, t = draw(rows, d, vocab, TYPES[dtype][1], seed=20, ignored=0.3)
+    t[-1] = vocab - 1
+    check(ctx, h, W, t, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_rows_extremes(ctx, dtype):
+    """A row that is left out keeps its NaN to itself, another's infinity or lowest value does what the formula says."""
+    dt, tt = TYPES[dtype]
+    h, W, _ = draw(6, 128, 3000, tt, seed=21)
+    t = torch.tensor([5, -1, 2999, 0, 3000, 7], device="cuda")
+    h[1], h[4, 3] = float("nan"), float("inf")
+    h[3] = 0
+    W[11] = 0
+    W[11, 0] = torch.finfo(tt).min / 2          # the class's logit is far below all others, or far above
+    h[0, 0], h[2, 0], h[5, 0] = 1.0, 1.0, 1.0
+    q = dk.dk_xent(6, 128, 3000, dt)
+    ctx.ensure_workspace(q)
+    loss, lse = torch.empty(6, device="cuda"), torch.empty(6, device="cuda")
+    dk.dk_linear_xent_fwd(ctx, q, h, W, t, loss, lse)
+    want = exact(h, W, t)
+    for r in (0, 2, 3, 5):
+        assert abs(float(lse[r].double() - want[1][r])) <= 1e-4 and abs(float(loss[r].double() - want[0][r])) <= 1e-4
+    for r in (1, 4):
+        assert float(loss[r]) == 0 and float(lse[r]) == 0
+    assert dk.dk_device_status(ctx) == 1                        # DK_ERR_INVALID_ARG
+    h[5, 0] = float("nan")
+    dk.dk_linear_xent_fwd(ctx, q, h, W, torch.tensor([5, -1, 2999, 0, -1, 7], device="cuda"), loss, lse)
+    assert bool(torch.isnan(loss[5])) and bool(torch.isnan(lse[5])) and not bool(torch.isnan(loss[:5]).any())
+    assert dk.dk_device_status(ctx) == 0
+
+
 def test_another_stream(ctx):
     h, W, t = draw(300, 128, 2000, torch.bfloat16, seed=15)
     want = call(ctx, h, W, t, dk.DK_BF16)
