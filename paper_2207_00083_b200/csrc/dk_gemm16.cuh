@@ -358,6 +358,10 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
   constexpr int OP = SMALL * 128;                  // bytes of one operand plane in a stage
   constexpr int PL = NPROD == 3 ? 2 : 1;
   constexpr int STAGE = 2 * PL * OP;
+  // Columns of tensor memory between the two accumulators.  With three products each is followed by the low terms' own,
+  // so that hi.hi and hi.lo are one instruction over both planes of B (they lie one after the other) and A's rows are read
+  // from shared memory once for both (update of 3 x 512x4608 294 -> 288 us, of 1961x1001 273 -> 268).
+  constexpr uint32_t ACC = NPROD == 3 ? 256u : 128u;
   constexpr int NC = SMALL / 2;                    // columns a thread holds (8 epilogue warps: 4 x 32 rows, 2 halves)
   constexpr int NH = NC / CS;                      // columns it finishes
   extern __shared__ unsigned char smem_raw[];
@@ -425,6 +429,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
     if (lane == 0) {
       const uint32_t idesc = (1u << 4) | ((uint32_t)p.bf16 << 7) | ((uint32_t)p.bf16 << 10) | ((AMN ? 1u : 0u) << 15) |
                              ((BMN ? 1u : 0u) << 16) | ((uint32_t)(SMALL >> 3) << 17) | ((uint32_t)(SMALL >> 4) << 24);
+      const uint32_t idesc_both = idesc + ((uint32_t)(SMALL >> 3) << 17);
       constexpr uint64_t STEP_A = AMN ? 128 : 2, STEP_B = BMN ? 128 : 2, LO = OP / 16;
       int stage = 0;
       uint32_t phase = 0, acc_it = 0;
@@ -433,7 +438,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
         const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
         if (!tc::mbar_wait(tempty_bar + buf, aphase ^ 1u, abort_flag, p.spin_cap)) break;
         tc::tc_fence_after();
-        const uint32_t d_tmem = tmem_base + buf * 128u;
+        const uint32_t d_tmem = tmem_base + buf * ACC;
         const int kb_end = min(kb_hi, kb + p.chunk);
         for (int k = kb; k < kb_end; ++k) {
           if (!tc::mbar_wait(full_bar + stage, phase, abort_flag, p.spin_cap)) { alive = false; break; }
@@ -443,10 +448,17 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
           const uint64_t b_hi = BMN ? desc_mn(st + PL * OP) : tc::make_desc<128>(st + PL * OP);
 #pragma unroll
           for (int kk = 0; kk < BK / 16; ++kk) {
-            mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, (k == kb && kk == 0) ? 0u : 1u);
-            if constexpr (NPROD == 3) {
-              mma_f16(tmem_base + 256u, a_hi + kk * STEP_A, b_hi + LO + kk * STEP_B, idesc, (k == kb_lo && kk == 0) ? 0u : 1u);
-              mma_f16(tmem_base + 256u, a_hi + LO + kk * STEP_A, b_hi + kk * STEP_B, idesc, 1u);
+            const bool first = k == kb && kk == 0;
+            if constexpr (NPROD == 1) {
+              mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, first ? 0u : 1u);
+            } else {
+              if (first && acc_it >= 2) {      // a new sum of high terms, the low terms' goes on
+                mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, 0u);
+                mma_f16(d_tmem + 128u, a_hi + kk * STEP_A, b_hi + LO + kk * STEP_B, idesc, 1u);
+              } else {
+                mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc_both, first ? 0u : 1u);
+              }
+              mma_f16(d_tmem + 128u, a_hi + LO + kk * STEP_A, b_hi + kk * STEP_B, idesc, 1u);
             }
           }
           tc::tc_commit(empty_bar + stage);
@@ -465,7 +477,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
       const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
       if (!tc::mbar_wait(tfull_bar + buf, aphase, abort_flag, p.spin_cap)) break;
       tc::tc_fence_after();
-      const uint32_t t = tmem_base + buf * 128u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NC);
+      const uint32_t t = tmem_base + buf * ACC + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NC);
       const float comp = p.comp_small * (float)min(p.chunk, kb_hi - kb);
 #pragma unroll
       for (int c = 0; c < NC; c += 32) {
@@ -475,14 +487,16 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
 #pragma unroll
         for (int j = 0; j < 32; ++j) acc[c + j] += fmaf(tmp[j], comp, tmp[j]);
       }
-      if (NPROD == 3 && kb + p.chunk >= kb_hi) {
+      if (NPROD == 3 && kb + p.chunk >= kb_hi) {           // (nothing overwrites them: this was the last chunk)
+        for (uint32_t b = 0; b <= min(acc_it, 1u); ++b) {
 #pragma unroll
-        for (int c = 0; c < NC; c += 32) {
-          float tmp[32];
-          ld32(tmem_base + 256u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NC + c), tmp);
-          tc::tc_wait_ld();
+          for (int c = 0; c < NC; c += 32) {
+            float tmp[32];
+            ld32(tmem_base + b * ACC + 128u + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NC + c), tmp);
+            tc::tc_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) acc[c + j] += tmp[j];
+            for (int j = 0; j < 32; ++j) acc[c + j] += tmp[j];
+          }
         }
       }
       tc::tc_fence_before();
