@@ -375,7 +375,7 @@ struct ResArgs {
   const void* x;
   void* out;
   double* sums;            // [batch][gang]
-  float* part;             // [batch][gang][128 columns][128 rows]
+  float* part;             // [2][batch][gang][128 columns][128 rows], see `mine`
   float* asum;             // [batch][128][128]
   unsigned int* count;     // [batch], zero at the start and at the end
   int m, n, s, L, tall, steps, C, gang;
@@ -551,7 +551,10 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
   constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);      // fp16, 128 x 128
   const uint32_t idesc_x = (1u << 4) | (1u << 16) | ((uint32_t)(q.C >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
   const uint32_t uxh = tc::smem_u32(xh), uxl = tc::smem_u32(xl), uah = tc::smem_u32(ah), ual = tc::smem_u32(al);
-  const size_t mine = ((size_t)mat * q.gang + g) * 128 * 128;
+  // Shares of A: two sets, used by even and odd steps.  A gang that adds all shares up directly meets once a step, so a
+  // CTA may store its share of step k + 1 while a slower one still reads those of step k; it stores the share of step
+  // k + 2 only after the meeting of step k + 1, where every CTA arrives with its reading of step k behind it.
+  const size_t set = (size_t)gridDim.x * 128 * 128, mine = ((size_t)mat * q.gang + g) * 128 * 128;
   // instructions (of 16) that cover the columns and the shorter side: zeros beyond them are not multiplied
   const int kcols = (cols + 15) / 16, ks = (q.s + 15) / 16;
   // 32 columns of this thread's row: the products with a low term (from column 0 of tensor memory), and those of high
@@ -585,15 +588,16 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
 #pragma unroll
     for (int c = 0; c < 64; c += 32) sum_of((uint32_t)(half * 64 + c), 128u, kcols, kcols, kResLossSquares, A + c);
     if (q.gang > 1) {
+      float* const part = q.part + (step & 1) * set;
       if (row < q.s) {
 #pragma unroll
         for (int j = 0; j < 64; ++j)
-          if (half * 64 + j < q.s) __stcg(q.part + mine + (half * 64 + j) * 128 + row, A[j]);
+          if (half * 64 + j < q.s) __stcg(part + mine + (half * 64 + j) * 128 + row, A[j]);
       }
       if (!meet()) { alive = false; break; }
       // The shares are added up in order, every thread taking elements (column i / s, row i % s) of its own, and pass to
       // the threads that need them through the room of A's terms.
-      const float* shares = q.part + (size_t)mat * q.gang * 128 * 128;
+      const float* shares = part + (size_t)mat * q.gang * 128 * 128;
       float* const sums = reinterpret_cast<float*>(ah);          // [column][row]
       const int all = q.s * q.s;
       int parts = q.gang;
@@ -766,8 +770,10 @@ Plan plan_ortho(const dk_ortho& q) {
   p.off_a = off; off += up(p.s_plane * 4);
   p.off_b = off; off += up(p.s_plane * 4);
   // Slices of a product: every (tile, slice) has a pair of its own, but a slice of a symmetric product takes the room of
-  // the whole square, up to twice its tiles.  A symmetric product always goes through them.
+  // the whole square, up to twice its tiles.  A symmetric product always goes through them.  (The resident kernel's two
+  // sets of shares, 64 KiB for each of at most kMaxSms CTAs, take half of this room.)
   size_t part = (size_t)2 * (kMaxSms / 2) * g16::TILE_M * BN * sizeof(float);
+  static_assert(2 * 128 * 128 * kMaxSms <= 2 * (kMaxSms / 2) * g16::TILE_M * BN, "room for two sets of shares");
   const size_t square = (size_t)q.batch * p.s * p.sp * sizeof(float);
   if (square > part) part = square;
   p.off_part = off; off += up(part);

@@ -226,3 +226,25 @@ def test_expired_wait_is_reported(ctx):
         dk.dk_set_option(ctx, dk.DK_OPT_SPIN_LIMIT, 1 << 22)
     got, want = call(ctx, x, dk.DK_F32), exact(x)
     assert float((got.double() - want).norm()) <= 1e-4 * float(want.norm())
+
+
+@pytest.mark.parametrize("b,m,n,steps", [(1, 64, 576, 12), (1, 48, 1100, 12), (3, 576, 64, 8), (1, 100, 250, 12),
+                                         (1, 30, 3900, 9), (2, 90, 2000, 8)])
+def test_gangs_beside_other_work(ctx, b, m, n, steps):
+    """Gangs that add their shares up directly meet once a step (the last case: twice).  What delays single CTAs of a
+    gang, traffic and kernels of another stream, must not mix the shares of two steps: every result has the same bits."""
+    x = draw(b, m, n, torch.float32, seed=17)
+    want = call(ctx, x, dk.DK_F32, steps, CUBIC)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big, small = torch.empty(1 << 27, device="cuda"), torch.randn((300, 300), device="cuda")
+    outs = []
+    for i in range(40):
+        with torch.cuda.stream(side):
+            big.mul_(1.0)
+            for _ in range(4):
+                small @ small
+        outs.extend(call(ctx, x, dk.DK_F32, steps, CUBIC) for _ in range(10))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    assert dk.dk_device_status(ctx) == 0
