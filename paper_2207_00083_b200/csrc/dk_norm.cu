@@ -182,13 +182,17 @@ __device__ __forceinline__ Moments sum_moments(const void* x, long long base, in
   return tot;
 }
 
-// The same for the backward pass: sums of d and d*xhat per channel of the vector.
+// The same for the backward pass: sums of d and d*xhat per channel of the vector.  z is formed by the very expression of
+// write_values, so that at ReLU's kink the sums, dx and the forward call's y agree on which elements are active.
 template <int DT, int VEC, int ACT>
 __device__ __forceinline__ void sum_gradients(const void* x, const void* dy, long long base, int b, int e, int c, int TY,
                                               const float (&mean)[VEC], const float (&rstd)[VEC],
                                               const float (&ga)[VEC], const float (&be)[VEC], float (&sb)[VEC],
                                               float (&sg)[VEC]) {
   constexpr int L = kLoads / 2;
+  float f[VEC];
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) f[k] = ga[k] * rstd[k];
   for (int i0 = b; i0 < e; i0 += L * TY) {
     typename Vec<DT, VEC>::Raw rx[L], rd[L];
 #pragma unroll
@@ -205,10 +209,10 @@ __device__ __forceinline__ void sum_gradients(const void* x, const void* dy, lon
         Vec<DT, VEC>::unpack(rd[u], d);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
-          const float xh = (a[k] - mean[k]) * rstd[k];
-          const float t = d[k] * act_slope(fmaf(xh, ga[k], be[k]), ACT);
+          const float dev = a[k] - mean[k];
+          const float t = d[k] * act_slope(fmaf(dev, f[k], be[k]), ACT);
           sb[k] += t;
-          sg[k] = fmaf(t, xh, sg[k]);
+          sg[k] = fmaf(t, dev * rstd[k], sg[k]);
         }
       }
   }

@@ -303,3 +303,29 @@ def test_refusals(ctx):
                              y.reshape(-1)[:128], stats.reshape(-1)[:4])
     assert e.value.status == 1
     assert bool(torch.isfinite(x).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,h,w,c,groups", [(2, 6, 5, 256, 8), (2, 60, 60, 256, 8), (3, 9, 7, 60, 5), (40, 30, 30, 35, 7)])
+def test_relu_mask_at_the_kink(ctx, n, h, w, c, groups, dtype):
+    """Each channel's beta puts the value of one element within a rounding of the kink.  With dy = 1, dbeta counts the
+    active elements of a channel (small integers: exact); it has to count those that the forward call let through, and dx
+    has to take the same decision (the group sums being what they are, dx + rstd*(m0 + xhat*m1) is rstd*gamma where
+    active and 0 elsewhere: half of that separates the two)."""
+    dt, tt = TYPES[dtype]
+    x, gamma, beta, _ = draw(n, h, w, c, tt, seed=21)
+    q, y, stats = run_fwd(ctx, x, gamma, beta, groups, "relu", dt)
+    mean, rstd = (stats[0, :, i].repeat_interleave(c // groups) for i in (0, 1))
+    beta = -((x[0, 0, 0].float() - mean) * (gamma * rstd))
+    q, y, stats = run_fwd(ctx, x, gamma, beta, groups, "relu", dt)
+    dy, dx, dg, db = torch.ones_like(x), torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+    dk.dk_group_norm_bwd(ctx, q, dy, x, gamma, beta, stats, dx, dg, db)
+    active = y > 0
+    assert torch.equal(db.double(), active.sum(dim=(0, 1, 2)).double())
+    shape = (n, h * w, groups, c // groups)
+    m, r = stats[..., 0].double()[:, None, :, None], stats[..., 1].double()[:, None, :, None]
+    xh = (x.double().reshape(shape) - m) * r
+    qv = (active.double() * gamma.double()).reshape(shape)
+    back = dx.double().reshape(shape) + r * (qv.mean(dim=(1, 3), keepdim=True)
+                                             + xh * (qv * xh).mean(dim=(1, 3), keepdim=True))
+    assert torch.equal((back > 0.5 * r * gamma.double().reshape(groups, -1)).reshape(x.shape), active)
