@@ -413,7 +413,7 @@ enum { DK_ACT_NONE = 0, DK_ACT_RELU = 1, DK_ACT_SILU = 2 };
  * do not meet in them (as they would in a batch normalisation). */
 typedef struct {
   int64_t n;          /* samples (0: nothing to do; the gradients of gamma and beta are zero) */
-  int32_t h, w, c;    /* c <= 16384                                               */
+  int32_t h, w, c;    /* h*w <= 2^31 - 4096, c <= 16384                           */
   int32_t groups;     /* divides c                                                */
   int32_t act;        /* DK_ACT_NONE | DK_ACT_RELU | DK_ACT_SILU (z*sigmoid(z))   */
   int32_t dtype;      /* of x, y, dy, dx                                          */

@@ -33,6 +33,9 @@ namespace {
 constexpr int kThreads = 256;      // slab kernels
 constexpr int kLoads = 8;          // vectors of one tensor a thread has in flight
 constexpr int kMaxC = 16384;
+// Pixels of an image: a loop's index passes the last pixel by less than a step, at most kLoads * 512 threads' pixels, and
+// stays below 2^31.  (Unsigned indices would do without the limit and cost the backward sums 1 to 2 %.)
+constexpr long long kMaxPix = (1LL << 31) - 4096;
 
 // VEC consecutive elements: as stored (Raw, one access of at most 16 bytes) and as fp32
 template <int DT, int VEC>
@@ -285,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) norm_sums_kernel(const NormParams p)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long s = blockIdx.x / p.slabs;
   const int slab = blockIdx.x % p.slabs;
-  const int p0 = slab * p.slab_pix, p1 = min(p.pix, p0 + p.slab_pix);
+  const int p0 = slab * p.slab_pix, p1 = (int)min((unsigned)p.pix, (unsigned)p0 + p.slab_pix);
   const long long base = s * p.pix * (long long)p.c;
   if (ty < p.TY) {
     for (int v = tx; v < cv; v += p.TX) {
@@ -423,7 +426,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p
   const unsigned int block = gridDim.x - 1 - blockIdx.x;
   const long long s = block / p.slabs;
   const int slab = block % p.slabs;
-  const int p0 = slab * p.slab_pix, p1 = min(p.pix, p0 + p.slab_pix);
+  const int p0 = slab * p.slab_pix, p1 = (int)min((unsigned)p.pix, (unsigned)p0 + p.slab_pix);
   const long long base = s * p.pix * (long long)p.c;
   for (int v = tx; v < cv; v += p.TX) {
     float mean[VEC], rstd[VEC], m0[VEC], m1[VEC], ga[VEC], be[VEC];
@@ -566,7 +569,7 @@ dk_status check_norm(const dk_norm* q) {
   if (q->n < 0 || q->h < 1 || q->w < 1 || q->c < 1 || q->groups < 1) return DK_ERR_SHAPE;
   if (q->c > kMaxC || q->c % q->groups) return DK_ERR_SHAPE;
   const long long pix = (long long)q->h * q->w;
-  if (pix >= (1LL << 31) || (double)q->n * (double)pix * q->c >= 1e15) return DK_ERR_SHAPE;
+  if (pix > kMaxPix || (double)q->n * (double)pix * q->c >= 1e15) return DK_ERR_SHAPE;
   return DK_OK;
 }
 
@@ -623,7 +626,7 @@ NormPlan plan_norm(const dk_norm& q) {
   if (want > most) want = most;
   if (want < 1) want = 1;
   p.slab_pix = (int)((pix + want - 1) / want);
-  p.slabs = (pix + p.slab_pix - 1) / p.slab_pix;
+  p.slabs = (int)(((long long)pix + p.slab_pix - 1) / p.slab_pix);
   size_t part = 0, rows_c = kSampleGrid;
   if (!p.sample[0]) part = (size_t)q.n * p.slabs * q.groups * 3;
   if (!p.sample[1]) {

@@ -329,3 +329,40 @@ def test_relu_mask_at_the_kink(ctx, n, h, w, c, groups, dtype):
     back = dx.double().reshape(shape) + r * (qv.mean(dim=(1, 3), keepdim=True)
                                              + xh * (qv * xh).mean(dim=(1, 3), keepdim=True))
     assert torch.equal((back > 0.5 * r * gamma.double().reshape(groups, -1)).reshape(x.shape), active)
+
+
+def test_pixels_up_to_two_to_the_31(ctx):
+    """One channel of 2^31 - 4096 pixels, the most: the last slab's index with a step on top stays in 32 bits.  Mean and
+    variance are joined over some 750 sums one after the other, half a unit each, the counts likewise: below 448 units of
+    2^-24 (64 times 1 + |x|/spread) together; values and gradients are bf16."""
+    pix, step = 2 ** 31 - 4096, 1 << 27
+    g = torch.Generator(device="cuda").manual_seed(22)
+    x, dy = (torch.empty((1, 1, pix, 1), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (x, dy):
+        for i in range(0, pix, step):
+            v = t.view(-1)[i:i + step]
+            v.copy_(torch.randn(v.shape, generator=g, device="cuda"))
+    gamma, beta = torch.full((1,), 1.5, device="cuda"), torch.full((1,), 0.25, device="cuda")
+    q, y, stats = run_fwd(ctx, x, gamma, beta, 1, "none", dk.DK_BF16)
+
+    def total(f):
+        return sum(float(f(x.view(-1)[i:i + step].double(), dy.view(-1)[i:i + step].double()).sum())
+                   for i in range(0, pix, step))
+
+    mean = total(lambda a, d: a) / pix
+    rstd = (total(lambda a, d: (a - mean) ** 2) / pix + EPS) ** -0.5
+    amp = float(x.view(-1)[:step].float().abs().max())
+    assert abs(float(stats[0, 0, 0]) - mean) <= ULPS * amp
+    assert abs(float(stats[0, 0, 1]) / rstd - 1) <= ULPS * (1 + amp * rstd)
+    dx, dg, db = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+    dk.dk_group_norm_bwd(ctx, q, dy, x, gamma, beta, stats, dx, dg, db)
+    sb, sg = total(lambda a, d: d), total(lambda a, d: d * (a - mean) * rstd)
+    assert abs(float(db) - sb) <= ULPS * total(lambda a, d: d.abs())
+    assert abs(float(dg) - sg) <= ULPS * total(lambda a, d: (d * (a - mean) * rstd).abs())
+    for i in range(0, pix, step):
+        a, d = x.view(-1)[i:i + step].double(), dy.view(-1)[i:i + step].double()
+        xh = (a - mean) * rstd
+        assert float((y.view(-1)[i:i + step].double() - (xh * 1.5 + 0.25)).abs().max()) <= 2.0 ** -8 * 12
+        want = rstd * 1.5 * (d - sb / pix - xh * sg / pix)
+        assert float((dx.view(-1)[i:i + step].double() - want).abs().max()) <= 2.0 ** -8 * 12
+    assert dk.dk_device_status(ctx) == 0

@@ -73,3 +73,15 @@ def test_null_arguments():
     assert L.dk_linear_xent_fwd(None, ctypes.byref(x), None, None, None, None, None, None) == INVALID
     o = dk.dk_ortho(1, 8, 8, 0, 5, 1.5, -0.5, 0.0, 0.0)
     assert L.dk_orthogonalize(None, ctypes.byref(o), None, 1.0, 0.0, None, None) == INVALID
+
+
+@pytest.mark.parametrize("h,w,c", [(46340, 46340, 1), (1, 2 ** 31 - 4096, 1), (1, 2 ** 31 - 4096, 8), (2, 2 ** 30 - 2048, 3)])
+def test_images_of_almost_two_to_the_31_pixels(h, w, c):
+    """The number of slabs is formed in 64 bits: the workspace is some slabs' sums, far less than the tensor."""
+    s, n = size(dk.dk_norm(1, h, w, c, 1, 0, 1, 1e-5))
+    assert s == 0 and 0 < n < 64 << 20
+
+
+@pytest.mark.parametrize("h,w", [(1, 2 ** 31 - 4095), (1, 2 ** 31 - 1), (46341, 46341)])
+def test_images_past_the_limit_are_refused(h, w):
+    assert size(dk.dk_norm(1, h, w, 1, 1, 0, 1, 1e-5))[0] == SHAPE
