@@ -805,14 +805,9 @@ inline bool make_map(const dk_ctx* ctx, CUtensorMap* m, const void* base, const 
   return tc_encode_map_bytes(ctx, m, base, 3, dims, str, box, 128);
 }
 
-// Per kernel instantiation and device, looked up once.
-struct Prepared {
-  bool done[64];
-};
-
 template <int NPROD, bool AMN, bool BMN, int CS, class Epi>
 dk_status launch_small(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, const Epi& epi, cudaStream_t st) {
-  static Prepared prep = {};
+  static SmemLimit limit;
   CUtensorMap ma, mal, mb, mbl;
   if (!make_map(ctx, &ma, A.hi, A, p.nbatch, AMN, SMALL) || !make_map(ctx, &mb, B.hi, B, p.nbatch, BMN, SMALL))
     return DK_ERR_CUDA;
@@ -826,12 +821,8 @@ dk_status launch_small(dk_ctx* ctx, const Operand& A, const Operand& B, Params p
   const int smem = p.nstages * STAGE + CTRL + 1024;
   if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
   auto kern = gemm16_small_kernel<NPROD, AMN, BMN, CS, Epi>;
-  if (ctx->device >= 64) return DK_ERR_UNSUPPORTED;
-  if (!prep.done[ctx->device]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-      return DK_ERR_CUDA;
-    prep.done[ctx->device] = true;
-  }
+  const dk_status r = allow_smem(limit, ctx->device, kern, smem);
+  if (r != DK_OK) return r;
   p.ksplit = 1;
   p.nitems = p.nbatch * p.tiles;
   p.group = p.MT < 16 ? p.MT : 16;
@@ -859,7 +850,7 @@ dk_status launch_small(dk_ctx* ctx, const Operand& A, const Operand& B, Params p
 // p: MT, NT, nbatch, sym, tiles, KB, ksplit, kb_per_split, M, N, chunk are set by the caller
 template <int NPROD, bool AMN, bool BMN, int BN, class Epi>
 dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, const Epi& epi, cudaStream_t st) {
-  static Prepared prep = {};
+  static SmemLimit limit;
   CUtensorMap ma, mal, mb, mbl;
   if (!make_map(ctx, &ma, A.hi, A, p.nbatch, AMN, ROWS) || !make_map(ctx, &mb, B.hi, B, p.nbatch, BMN, BN / 2))
     return DK_ERR_CUDA;
@@ -875,16 +866,9 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
   const int smem = p.nstages * STAGE + ROWS_MEM + CTRL + 1024;
   if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
   auto kern = gemm16_kernel<NPROD, AMN, BMN, BN, Epi>;
-  if (ctx->device >= 64) return DK_ERR_UNSUPPORTED;
-  if (!prep.done[ctx->device]) {
-    cudaFuncAttributes fa;
-    if (cudaFuncGetAttributes(&fa, kern) != cudaSuccess) return DK_ERR_CUDA;
-    // the setmaxnreg split draws on threads * registers at launch; a smaller pool would wait forever
-    if (fa.numRegs * kThreadsG < 40 * 128 + 232 * 256) return DK_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-      return DK_ERR_CUDA;
-    prep.done[ctx->device] = true;
-  }
+  // (the setmaxnreg split draws on threads * registers at launch; a smaller pool would wait forever)
+  const dk_status r = allow_smem(limit, ctx->device, kern, smem, kThreadsG, 40 * 128 + 232 * 256);
+  if (r != DK_OK) return r;
   p.nitems = p.nbatch * p.tiles * p.ksplit;
   p.group = p.MT < 16 ? p.MT : 16;
   p.spin_cap = (unsigned)ctx->opt.v[DK_OPT_SPIN_LIMIT];

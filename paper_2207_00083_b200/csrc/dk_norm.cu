@@ -645,23 +645,22 @@ NormPlan plan_norm(const dk_norm& q) {
   return p;
 }
 
-template <typename F>
-dk_status with_smem(F kern, size_t bytes) {
-  if (bytes > 40 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) !=
-                               cudaSuccess)
-    return DK_ERR_CUDA;
-  return DK_OK;
-}
+// most dynamic shared memory of any call: the forward sums of kMaxC channels that share no vector
+constexpr int kMaxSmem = 3 * kMaxC * (int)sizeof(float);
 
 // whole samples: one launch, and one for the parameters' gradients
 template <int DT, int VEC, int ACT, bool FWD>
-dk_status run_sample(NormParams p, const NormPlan& pl, int sms, cudaStream_t st) {
+dk_status run_sample(NormParams p, const NormPlan& pl, int device, int sms, cudaStream_t st) {
   auto kern = norm_sample_kernel<DT, VEC, ACT, FWD>;
   p.TX = pl.sTX; p.TY = pl.sTY; p.cb = pl.cb;
   const int nblk = p.c / p.cb;
   const size_t smem =
       ((FWD ? (size_t)3 * p.TY * p.TX : (size_t)2 * p.TY * p.cb) + 2 * (size_t)(p.cb / p.cg)) * sizeof(float);
-  if (with_smem(kern, smem) != DK_OK) return DK_ERR_CUDA;
+  static SmemLimit limit;
+  if (smem > 40 * 1024) {
+    const dk_status r = allow_smem(limit, device, kern, kMaxSmem);
+    if (r != DK_OK) return r;
+  }
   long long per = (long long)(sms < kMaxSms ? sms : kMaxSms) * (2048 / pl.threads > 16 ? 16 : 2048 / pl.threads) / nblk;
   if (per < 1) per = 1;
   if (per > p.n) per = p.n;
@@ -674,13 +673,17 @@ dk_status run_sample(NormParams p, const NormPlan& pl, int sms, cudaStream_t st)
 
 // slabs: sums (forward with vectors within a group, backward per channel), then values
 template <int DT, int VEC, int ACT, bool FWD>
-dk_status run_sums(NormParams p, const NormPlan& pl, cudaStream_t st) {
+dk_status run_sums(NormParams p, const NormPlan& pl, int device, cudaStream_t st) {
   auto kern = norm_sums_kernel<DT, VEC, ACT, FWD>;
   p.TX = pl.TX[FWD ? 0 : 1]; p.TY = pl.TY[FWD ? 0 : 1];
   size_t smem = FWD ? (size_t)3 * p.TY * (p.c / VEC) : (size_t)2 * p.TY * p.c;
   if (!FWD && smem < (size_t)2 * kThreads) smem = 2 * kThreads;
   smem *= sizeof(float);
-  if (with_smem(kern, smem) != DK_OK) return DK_ERR_CUDA;
+  static SmemLimit limit;
+  if (smem > 40 * 1024) {
+    const dk_status r = allow_smem(limit, device, kern, kMaxSmem);
+    if (r != DK_OK) return r;
+  }
   return launch_chained(kern, dim3((unsigned)(p.n * p.slabs)), kThreads, smem, st, p) == cudaSuccess ? DK_OK
                                                                                                      : DK_ERR_CUDA;
 }
@@ -715,14 +718,14 @@ dk_status run_apply(NormParams p, const NormPlan& pl, cudaStream_t st) {
   } while (0)
 
 template <bool FWD>
-dk_status dispatch_sample(const NormParams& p, const NormPlan& pl, int dtype, int sms, cudaStream_t st) {
-#define DK_NORM_CALL(DT, V, ACT) run_sample<DT, V, ACT, FWD>(p, pl, sms, st)
+dk_status dispatch_sample(const NormParams& p, const NormPlan& pl, int dtype, int device, int sms, cudaStream_t st) {
+#define DK_NORM_CALL(DT, V, ACT) run_sample<DT, V, ACT, FWD>(p, pl, device, sms, st)
   DK_NORM_TYPES(pl.vec, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
 template <bool FWD>
-dk_status dispatch_sums(const NormParams& p, const NormPlan& pl, int dtype, cudaStream_t st) {
-#define DK_NORM_CALL(DT, V, ACT) run_sums<DT, V, FWD ? DK_ACT_NONE : ACT, FWD>(p, pl, st)
+dk_status dispatch_sums(const NormParams& p, const NormPlan& pl, int dtype, int device, cudaStream_t st) {
+#define DK_NORM_CALL(DT, V, ACT) run_sums<DT, V, FWD ? DK_ACT_NONE : ACT, FWD>(p, pl, device, st)
   DK_NORM_TYPES(FWD ? pl.vec : pl.wide, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
@@ -734,10 +737,10 @@ dk_status dispatch_apply(const NormParams& p, const NormPlan& pl, int dtype, cud
 }
 
 template <bool FWD>
-dk_status dispatch(const NormParams& p, const NormPlan& pl, int dtype, int sms, cudaStream_t st) {
-  if (pl.sample[FWD ? 0 : 1]) return dispatch_sample<FWD>(p, pl, dtype, sms, st);
+dk_status dispatch(const NormParams& p, const NormPlan& pl, int dtype, int device, int sms, cudaStream_t st) {
+  if (pl.sample[FWD ? 0 : 1]) return dispatch_sample<FWD>(p, pl, dtype, device, sms, st);
   if (p.n > kStepCounters) DK_CUDA_CHECK(cudaMemsetAsync(p.count, 0, (size_t)p.n * sizeof(unsigned int), st));
-  const dk_status s = dispatch_sums<FWD>(p, pl, dtype, st);
+  const dk_status s = dispatch_sums<FWD>(p, pl, dtype, device, st);
   return s == DK_OK ? dispatch_apply<FWD>(p, pl, dtype, st) : s;
 }
 
@@ -794,7 +797,7 @@ dk_status dk_group_norm_fwd(dk_ctx* ctx, const dk_norm* q, const void* x, const 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.x = x; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats;
   ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, true), st);
-  return dispatch<true>(p, pl, q->dtype, ctx->sm_count, st);
+  return dispatch<true>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
 }
 
 dk_status dk_group_norm_bwd(dk_ctx* ctx, const dk_norm* q, const void* dy, const void* x, const float* gamma,
@@ -822,7 +825,7 @@ dk_status dk_group_norm_bwd(dk_ctx* ctx, const dk_norm* q, const void* dy, const
   p.x = x; p.dy = dy; p.out = dx; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float*>(stats);
   p.dgamma = dgamma; p.dbeta = dbeta;
   ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, false), st);
-  return dispatch<false>(p, pl, q->dtype, ctx->sm_count, st);
+  return dispatch<false>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
 }
 
 }  // extern "C"

@@ -362,6 +362,7 @@ ortho_x_kernel(const XArgs a, const float* part, int ks, int pitch_part, const _
 // operand of X X^T and the MN-major operand of B X.
 // ---------------------------------------------------------------------------
 constexpr int kResThreads = 256;
+constexpr int kMaxColumns = 256;        // of a CTA
 constexpr int kDirect = 28 * 1024;      // elements of A times CTAs of the gang
 
 constexpr int kBlock = 128 * 128;            // bytes of one [128][64] fp16 block
@@ -788,7 +789,7 @@ int resident_columns(const dk_ortho& q, const Plan& pl, int sms) {
   if (pl.s > 128 || q.steps < 1) return 0;
   const int L = pl.tall ? q.m : q.n;
   if (sms > kMaxSms) sms = kMaxSms;
-  for (int C = L <= 64 ? 64 : 128; C <= 256; C += 64)
+  for (int C = L <= 64 ? 64 : 128; C <= kMaxColumns; C += 64)
     if ((long long)q.batch * ((L + C - 1) / C) <= sms) return C;
   return 0;
 }
@@ -859,9 +860,11 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
     r.spin_cap = (unsigned)ctx->opt.v[DK_OPT_SPIN_LIMIT];
     r.status = device_status_word(ctx);
     auto kern = q.dtype == DK_F32 ? ortho_resident_kernel<DK_F32> : ortho_resident_kernel<DK_BF16>;
-    const int smem = (2 * (C / 64) + 4) * kBlock + 1024;
-    if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return DK_ERR_CUDA;
+    const int smem = (2 * (C / 64) + 4) * kBlock + 1024, most = (2 * (kMaxColumns / 64) + 4) * kBlock + 1024;
+    if (most > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
+    static SmemLimit limit[2];
+    const dk_status s = allow_smem(limit[q.dtype == DK_F32 ? 0 : 1], ctx->device, kern, most);
+    if (s != DK_OK) return s;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(q.batch * r.gang));
     cfg.blockDim = dim3(kResThreads);

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "dk_internal.h"
 
 namespace dk {
@@ -29,6 +31,26 @@ struct OnDevice {
     if (ok && prev != dev) cudaSetDevice(prev);
   }
 };
+
+// The most dynamic shared memory that any call gives a kernel, told to the runtime once per kernel and device and never
+// lowered after: another thread's context may be about to launch the same kernel with more than this call needs.
+// (One SmemLimit, static, per kernel; a CTA of `threads` that re-partitions its registers needs `pool` of them.)
+struct SmemLimit {
+  std::atomic<bool> done[64];
+};
+template <typename K>
+dk_status allow_smem(SmemLimit& limit, int device, K kern, int bytes, int threads = 0, int pool = 0) {
+  if (device < 0 || device >= 64) return DK_ERR_UNSUPPORTED;
+  if (limit.done[device].load(std::memory_order_acquire)) return DK_OK;
+  if (pool > 0) {
+    cudaFuncAttributes fa;
+    if (cudaFuncGetAttributes(&fa, kern) != cudaSuccess) return DK_ERR_CUDA;
+    if (fa.numRegs * threads < pool) return DK_ERR_UNSUPPORTED;
+  }
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return DK_ERR_CUDA;
+  limit.done[device].store(true, std::memory_order_release);
+  return DK_OK;
+}
 
 // Programmatic dependent launch: the next kernel of the stream may be set up while this one runs (its own call of this
 // function then waits for this one's end and its writes).  At the start of kernels that follow one another closely.

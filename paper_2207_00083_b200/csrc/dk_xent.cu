@@ -878,13 +878,9 @@ dk_status few_rows(dk_ctx* ctx, const Plan& pl, char* ws, FewArgs a, float* loss
   a.tlogit = reinterpret_cast<float*>(ws + pl.off_tl);
   const size_t smem = (size_t)R * a.dpad * sizeof(float);
   auto kern = xent_few_rows_kernel<DT, VEC, R, V>;
-  static bool done[64];
-  if (ctx->device >= 64) return DK_ERR_UNSUPPORTED;
-  if (!done[ctx->device]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem) != cudaSuccess)
-      return DK_ERR_CUDA;
-    done[ctx->device] = true;
-  }
+  static SmemLimit limit;
+  const dk_status r = allow_smem(limit, ctx->device, kern, (int)kFewSmem);
+  if (r != DK_OK) return r;
   long long per_sm = (long long)(200 * 1024 / (smem + 2048));
   if (per_sm > 4) per_sm = 4;
   const int classes = kFewThreads / 32 * V;
