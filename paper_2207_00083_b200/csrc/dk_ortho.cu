@@ -79,22 +79,31 @@ __global__ void __launch_bounds__(256) ortho_sumsq_kernel(const void* x, long lo
   }
 }
 
+// What brings x to |X|_F = 1 and to X's power of two: x*f.x*f.y, where f.x is a power of two.  One fp32 factor would be
+// infinite for norms (and eps) below 2^-115, and the zeros of x then NaN, and subnormal above 2^139.  (In 64 bits the
+// kernel of the smallest matrices takes 1 us longer.)
+__device__ __forceinline__ float2 norm_factor(double sum_of_squares, double eps) {
+  const double f = (double)kX / (sqrt(sum_of_squares) + eps);
+  const float p = f > 0x1p64 ? 0x1p64f : f < 0x1p-64 ? 0x1p-64f : 1.f;
+  return make_float2(p, (float)(f / (double)p));
+}
+
 // X as two fp16 terms, rows padded to `pitch` with zeros
 template <int DT>
 __global__ void __launch_bounds__(256)
 ortho_load_kernel(const void* x, const double* part, int nparts, double eps, long long m, int n, int pitch, __half* hi,
                   __half* lo) {
   chained_launch();
-  __shared__ float f;
+  __shared__ float2 f;
   if (threadIdx.x < 32) {
     double t = 0.0;
     for (int i = threadIdx.x; i < nparts; i += 32) t += part[blockIdx.y * nparts + i];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-    if (threadIdx.x == 0) f = (float)((double)kX / (sqrt(t) + eps));
+    if (threadIdx.x == 0) f = norm_factor(t, eps);
   }
   __syncthreads();
-  const float fac = f;
+  const float2 fac = f;
   const int n8 = pitch / 8;
   const size_t src = (size_t)blockIdx.y * m * n, dst = (size_t)blockIdx.y * m * pitch;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < m * n8; i += (long long)gridDim.x * 256) {
@@ -102,7 +111,7 @@ ortho_load_kernel(const void* x, const double* part, int nparts, double eps, lon
     const int c = (int)(i - r * n8) * 8;
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? load1<DT>(x, src + (size_t)r * n + c + j) * fac : 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? load1<DT>(x, src + (size_t)r * n + c + j) * fac.x * fac.y : 0.f;
     g16::store_planes<8>(hi + dst + r * pitch + c, lo + dst + r * pitch + c, v, 8);
   }
 }
@@ -530,7 +539,7 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
     for (int i = lane; i < q.gang; i += 32) t += __ldcg(q.sums + (size_t)mat * q.gang + i);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-    const float f = (float)((double)kX / (sqrt(t) + q.eps));
+    const float2 f = norm_factor(t, q.eps);
     for (int e0 = lane; e0 < length; e0 += 128)
       for (int l0 = warp; l0 < lines; l0 += 32) {
         float v[16];
@@ -540,7 +549,7 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
           const int l = l0 + 8 * (i >> 2), e = e0 + 32 * (i & 3);
           if (l < lines && e < length) {
             const uint32_t at = q.tall ? block_at(e, l) : block_at(l, e);
-            const float w = v[i] * f;
+            const float w = v[i] * f.x * f.y;
             const __half h = __float2half_rn(w);
             *reinterpret_cast<__half*>(xh + at) = h;
             *reinterpret_cast<__half*>(xl + at) = __float2half_rn(w - __half2float(h));

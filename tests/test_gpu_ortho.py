@@ -248,3 +248,21 @@ def test_gangs_beside_other_work(ctx, b, m, n, steps):
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
     assert dk.dk_device_status(ctx) == 0
+
+
+@pytest.mark.parametrize("m,n", [(90, 200), (200, 90), (300, 700), (300, 701)])
+def test_ends_of_the_range(ctx, m, n):
+    """Matrices whose norm is near either end of fp32's range (the small ones from numbers of few bits, so that being
+    subnormal costs them none), and a zero matrix with an eps as small."""
+    x = draw(1, m, n, torch.bfloat16, seed=18).float()
+    x = torch.where(x.abs() < 2.0 ** -5, torch.zeros_like(x), x)
+    small, large = (x * 2.0 ** -70 * 2.0 ** -64).contiguous(), (x * 2.0 ** 124).contiguous()
+    assert torch.equal(small.double(), x.double() * 2.0 ** -134)
+    for v in (small, large):
+        got, want = call(ctx, v, dk.DK_F32, eps=0.0), exact(v, eps=0.0)
+        assert float((got.double() - want).norm()) <= 1e-4 * float(want.norm())
+    x[:] = 0
+    assert float(call(ctx, x, dk.DK_F32, eps=1e-38).abs().max()) == 0.0
+    x[0, 3, 5] = 2.0 ** -120
+    got, want = call(ctx, x, dk.DK_F32, eps=1e-38), exact(x, eps=1e-38)
+    assert float((got.double() - want).norm()) <= 1e-4 * float(want.norm())
