@@ -246,7 +246,9 @@ DK_API dk_status dk_destroy(dk_ctx* ctx);
  *                     next tensor-core forward or weight-gradient kernel arms the
  *                     barrier of its n-th pipeline stage but issues no copy for
  *                     it and stops, so every consumer's wait runs out; nothing is
- *                     read or written out of bounds.  The option switches itself
+ *                     read or written out of bounds.  (dk_orthogonalize's form
+ *                     for short sides of at most 128: a CTA does not count at its
+ *                     n-th meeting with the others.)  The option switches itself
  *                     off after one launch. */
 enum {
   DK_OPT_TC_CHUNK = 0, DK_OPT_WG_CHUNK = 1, DK_OPT_TC_BK = 2, DK_OPT_TC_PAIR = 3, DK_OPT_WG_PACK = 4,

@@ -392,6 +392,7 @@ struct ResArgs {
   float a, b, c, scale, keep;
   double eps;
   unsigned int spin_cap;
+  int withhold;            // test hook: the first CTA waits at its n-th meeting without arriving (-1 = off)
   int* status;
 };
 
@@ -461,6 +462,7 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
   const uint32_t tmem = tmem_slot, lanes = (uint32_t)(quad * 32) << 16;
 
   unsigned int epoch = 0;
+  const unsigned int silent = blockIdx.x == 0 ? (unsigned int)(q.withhold + 1) : 0u;      // 0: at no meeting
   uint32_t phase = 0;
   // the gang's CTAs meet; what they wrote to global memory before is visible after
   auto meet = [&]() -> bool {
@@ -468,7 +470,7 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
     __syncthreads();
     if (threadIdx.x == 0) {
       __threadfence();
-      atomicAdd(q.count + mat, 1u);
+      atomicAdd(q.count + mat, epoch == silent ? 0u : 1u);
       const unsigned int target = epoch * (unsigned int)q.gang;
       bool ok = false;
       for (unsigned int i = 0; i < q.spin_cap; ++i) {
@@ -748,6 +750,10 @@ __global__ void __launch_bounds__(kResThreads, 1) ortho_resident_kernel(const Re
     if (failed) atomicExch(q.status, (int)DK_ERR_TIMEOUT);
     else if (atomicAdd(q.count + mat, 1u) + 1u == (epoch + 1u) * (unsigned int)q.gang) q.count[mat] = 0u;
   }
+  if (failed) {      // (products may be in flight still: time for them to end)
+    for (int i = 0; i < 64; ++i) __nanosleep(16384);
+    __syncthreads();
+  }
   if (warp == 0) {
     tc::tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
@@ -867,6 +873,8 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
     r.gang = (r.L + C - 1) / C;
     r.a = q.a; r.b = q.b; r.c = q.c; r.scale = scale; r.keep = keep; r.eps = (double)q.eps;
     r.spin_cap = (unsigned)ctx->opt.v[DK_OPT_SPIN_LIMIT];
+    r.withhold = ctx->opt.v[DK_OPT_TEST_WITHHOLD];
+    ctx->opt.v[DK_OPT_TEST_WITHHOLD] = -1;
     r.status = device_status_word(ctx);
     auto kern = q.dtype == DK_F32 ? ortho_resident_kernel<DK_F32> : ortho_resident_kernel<DK_BF16>;
     const int smem = (2 * (C / 64) + 4) * kBlock + 1024, most = (2 * (kMaxColumns / 64) + 4) * kBlock + 1024;
