@@ -35,7 +35,7 @@ struct Meta {
 };
 
 // The power of two that brings a largest magnitude (given by its bits) to [2^14, 2^15); 1 when it is zero, infinite or
-// NaN.  The products undo it with inv_scale.
+// NaN (a forward row's own).  The products undo it with inv_scale.
 __device__ __forceinline__ int scale_exp(unsigned int bits) {
   const int e = (int)(bits >> 23) - 127;
   if (bits == 0u || e > 127) return 0;
@@ -47,6 +47,13 @@ __device__ __forceinline__ float pow2(int e) {      // -126 <= e <= 126
 }
 
 __device__ __forceinline__ bool left_out(long long t, int vocab) { return t < 0 || t >= vocab; }
+
+// The bits of a magnitude for a maximum: an infinity or a NaN counts as nothing.  (It makes its own row's results NaN; as
+// the maximum it would leave all other rows without their power of two.)
+__device__ __forceinline__ unsigned int magnitude(unsigned int bits) {
+  bits &= 0x7fffffffu;
+  return bits < 0x7f800000u ? bits : 0u;
+}
 
 // largest magnitudes of h (rows that take part), W and dloss
 __global__ void __launch_bounds__(256)
@@ -62,23 +69,23 @@ xent_absmax_kernel(const float* __restrict__ h, const float* __restrict__ W, con
   const long long nw4 = nw / 4;
   for (long long i = i0; i < nw4; i += step) {
     const uint4 v = __ldg(reinterpret_cast<const uint4*>(W) + i);
-    mw = max(mw, max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)));
+    mw = max(mw, max(max(magnitude(v.x), magnitude(v.y)), max(magnitude(v.z), magnitude(v.w))));
   }
-  for (long long i = nw4 * 4 + i0; i < nw; i += step) mw = max(mw, __float_as_uint(W[i]) & 0x7fffffffu);
+  for (long long i = nw4 * 4 + i0; i < nw; i += step) mw = max(mw, magnitude(__float_as_uint(W[i])));
   if (d % 4 == 0) {
     const int d4 = d / 4;
     for (long long i = i0; i < nh / 4; i += step) {
       if (left_out(target[i / d4], vocab)) continue;
       const uint4 v = __ldg(reinterpret_cast<const uint4*>(h) + i);
-      mh = max(mh, max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)));
+      mh = max(mh, max(max(magnitude(v.x), magnitude(v.y)), max(magnitude(v.z), magnitude(v.w))));
     }
   } else {
     for (long long i = i0; i < nh; i += step)
-      if (!left_out(target[i / d], vocab)) mh = max(mh, __float_as_uint(h[i]) & 0x7fffffffu);
+      if (!left_out(target[i / d], vocab)) mh = max(mh, magnitude(__float_as_uint(h[i])));
   }
   for (long long i = i0; i < rows; i += step)
     if (!left_out(target[i], vocab))
-      mg = max(mg, __float_as_uint(dloss != nullptr ? dloss[i] * scale : scale) & 0x7fffffffu);
+      mg = max(mg, magnitude(__float_as_uint(dloss != nullptr ? dloss[i] * scale : scale)));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     mh = max(mh, __shfl_xor_sync(0xffffffffu, mh, o));

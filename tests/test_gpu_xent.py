@@ -345,3 +345,29 @@ def test_expired_wait_is_reported(ctx, rows, d, vocab):
     finally:
         dk.dk_set_option(ctx, dk.DK_OPT_SPIN_LIMIT, 1 << 22)
     check(ctx, h, W, t, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("magnitude", [1.0, 1e5, 1e-5])
+@pytest.mark.parametrize("rows,vocab", [(20, 500), (300, 500), (2000, 6000)])
+def test_non_finite_values_stay_in_their_row(ctx, rows, vocab, magnitude, dtype):
+    """A row that takes part and holds a NaN or an infinity, or whose weight is one: its loss and dh are NaN, and dW, to
+    which it belongs; every other row has the bits that it has without it, whatever the operands' magnitudes."""
+    dt, tt = TYPES[dtype]
+    h, W, t = draw(rows, 64, vocab, torch.float32, seed=23, ignored=0.1)
+    t[7] = 3
+    h[7, 5] = 0.0                                              # (not the largest magnitude)
+    dloss = torch.ones(rows, device="cuda")
+    dloss[8] = 2.0
+    h, W = (h * magnitude).to(tt), (W / magnitude).to(tt)
+    others = torch.arange(rows, device="cuda") != 7
+    clean = call(ctx, h, W, t, dt, dloss=dloss)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        h2, d2 = h.clone(), dloss.clone()
+        h2[7, 5], d2[7] = bad, bad
+        for got, own in ((call(ctx, h2, W, t, dt, dloss=dloss), (0, 1, 2)), (call(ctx, h, W, t, dt, dloss=d2), (2,))):
+            for i in range(3):
+                assert torch.equal(got[i][others], clean[i][others])
+                assert not bool(torch.isfinite(got[i][7]).any()) if i in own else torch.equal(got[i][7], clean[i][7])
+            assert not bool(torch.isfinite(got[3]).any())
+    assert dk.dk_device_status(ctx) == 0
