@@ -472,9 +472,13 @@ DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h
  *   p[r][v] = scale*dloss[r]*(exp(l[v] - lse[r]) - [v == target[r]]), 0 for rows left out
  *   dh = p.W,  dW = p^T.h
  * lse: from the forward call.  With DK_BF16 p is rounded to bf16 for the two
- * products, with DK_F32 it is kept as two fp16 terms, and h and W are taken
- * under one power of two each (of the whole tensor: the products sum over their
- * rows).  dh and dW are overwritten.  Needs the workspace. */
+ * products.  With DK_F32 h, W and p enter as two fp16 terms each, 22 bits: h and
+ * W under one power of two each (of the whole tensor: the products sum over their
+ * rows; 22 bits down to 2^-18 of the tensor's largest finite magnitude, an
+ * absolute error of 2^-40 of it below), p under one of each class.  So a row of
+ * dW keeps its digits however improbable its class is, and a row of dh those
+ * down to 2^-18 of the largest |scale*dloss|, with an absolute error of 2^-40 of
+ * it (times W) below.  dh and dW are overwritten.  Needs the workspace. */
 DK_API dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
                                     const int64_t* target, const float* lse, const float* dloss, float scale,
                                     void* dh, void* dW, void* stream);

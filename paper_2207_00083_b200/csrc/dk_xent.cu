@@ -9,6 +9,16 @@
 // contraction runs across their rows).  The three products of a piece are what the call costs; the piece is as wide
 // as its room allows.
 //
+// Range of p with fp32 tensors.  p falls over many powers of ten, from the target's down to those of classes that are
+// improbable in every row; two fp16 terms under one power of two would leave such a class's row of dW a few bits, and
+// nothing below 2^-40 of the largest.  So the epilogue leaves p's own 32 bits (an upper and a lower half) and each class's
+// largest magnitude; xent_class_terms_kernel then makes the terms under a power of two of the class, 2^e_v, and puts
+// 2^-e_v on the class's row of W, so that dh = (p 2^e).(2^-e W) needs nothing undone; dW's epilogue undoes 2^e_v row by
+// row.  200 x 64, 600 classes whose largest probability falls from 6e-3 to 3e-17: each row of dW is off by 2e-7 to 5e-6 of
+// itself, as in plain fp32 (one power of two for all: 1e-4 at 1e-8, 1e-1 at 1e-11, all of it below 1e-12).  The pass over
+// p costs 3.4 us of 48 (64 x 512, 1000 classes), 0.2 ms of 2.65 (4000 x 768, 32000 classes: 1 GB at 5.2 TB/s), and a fifth
+// of the call where features are few (8192 x 256, 20000 classes).
+//
 // Forward calls of one or a few rows take dot products instead (xent_few_rows_kernel).
 //
 // Measured: 4096 x 4096, 128000 classes, bf16, both directions 14.5 ms (1.19 PFLOP/s over its four products, 84 % of the
@@ -44,6 +54,13 @@ __device__ __forceinline__ int scale_exp(unsigned int bits) {
 }
 __device__ __forceinline__ float pow2(int e) {      // -126 <= e <= 126
   return __int_as_float((e + 127) << 23);
+}
+
+// The power of two of a class beyond that of all p, from the bits of its largest magnitude (under the common one, below
+// 2^15).  None down to 2^-17 of the largest p: the two terms have 22 bits of the class's largest value there.
+__device__ __forceinline__ int class_exp(unsigned int bits) {
+  const int e = scale_exp(bits);
+  return bits == 0u || e <= 17 ? 0 : e;
 }
 
 __device__ __forceinline__ bool left_out(long long t, int vocab) { return t < 0 || t >= vocab; }
@@ -144,14 +161,15 @@ __device__ __forceinline__ void prep_rows(const Prep& q, int d, int dp, int voca
     }
   }
 }
-// (F32: joins the blocks' magnitudes first)
+// (F32: joins the blocks' magnitudes first, and clears the classes' for the products' epilogues)
 template <bool F32>
 __global__ void __launch_bounds__(256) xent_prep_kernel(const Prep a, const Prep b, int d, int dp, int vocab, Meta* meta,
-                                                        int blocks) {
+                                                        int blocks, unsigned int* class_max) {
   chained_launch();
   const long long step = (long long)gridDim.x * blockDim.x, i0 = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   float sh = 1.f, sw = 1.f;
   if constexpr (F32) {
+    for (long long i = i0; i < vocab; i += step) class_max[i] = 0u;
     __shared__ unsigned int most[8][3];
     uint4 m = make_uint4(0u, 0u, 0u, 0u);
     for (int i = threadIdx.x; i < blocks; i += 256) {
@@ -317,13 +335,37 @@ struct RowArgs {
   const float* dloss;
   float scale;
   int vocab, v0;               // first class of the piece
-  const unsigned int* gmax;    // fp32: p is stored as two fp16 terms under this magnitude's power of two
-  void* hi;
+  const unsigned int* gmax;    // fp32: p is taken under this magnitude's power of two
+  unsigned int* class_max;     // fp32: of the piece, largest magnitudes of p
+  void* hi;                    // p; fp32: the upper and the lower 16 bits of each value
   void* lo;
   long long pitch;
 };
 
-// backward epilogue: p of this piece
+// The 32 bits of a row's values as planes of upper and of lower halves, as g16::store_terms stores terms.
+template <int NH>
+__device__ __forceinline__ void store_halves(const float (&v)[NH], char* sm, uint16_t* hi, uint16_t* lo, long long pitch,
+                                             int rows, int cols) {
+  constexpr int W = NH <= 64 ? NH : 32;
+#pragma unroll
+  for (int c0 = 0; c0 < NH; c0 += W) {
+    uint32_t w[W / 2];
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      uint16_t* const to = part ? lo : hi;
+#pragma unroll
+      for (int j = 0; j < W / 2; ++j)
+        w[j] = __byte_perm(__float_as_uint(v[c0 + 2 * j]), __float_as_uint(v[c0 + 2 * j + 1]), part ? 0x5410 : 0x7632);
+      g16::warp_block_16<W>(w, sm, [&](int r, int c, const uint4& u) {
+        if (r < rows && c0 + c < cols) *reinterpret_cast<uint4*>(to + r * pitch + c0 + c) = u;
+      });
+    }
+  }
+}
+
+// backward epilogue: p of this piece.  With bf16 tensors p is rounded to bf16: one product each for dh and dW instead of
+// two, and the results are rounded to as many bits; what it adds shows beside that rounding as 1 to 4 % of the error
+// (2047 x 1024 on 50257 classes, 4096 x 4096 on 128000).
 template <bool F32>
 struct EpiP {
   static constexpr bool kAhead = false;
@@ -360,8 +402,20 @@ struct EpiP {
     // (the pitch is a multiple of 8: padding columns are written as zeros)
     const long long to = (long long)row0 * r.pitch + col0;
     if constexpr (F32) {
-      g16::store_terms<NH>(acc, sm, static_cast<__half*>(r.hi) + to, static_cast<__half*>(r.lo) + to, r.pitch, p.M - row0,
-                           count);
+      // the classes' largest magnitudes over the warp's rows: lane l keeps those of columns l, l + 32, ..
+      const int lane = threadIdx.x & 31;
+      constexpr int KEEP = (NH + 31) / 32;
+      unsigned int most[KEEP];
+#pragma unroll
+      for (int j = 0; j < NH; ++j) {
+        const unsigned int m = __reduce_max_sync(0xffffffffu, magnitude(__float_as_uint(acc[j])));
+        if (j % 32 == 0 || lane == j % 32) most[j / 32] = m;
+      }
+#pragma unroll
+      for (int k = 0; k < KEEP; ++k)
+        if (32 * k + lane < count && most[k] != 0u) atomicMax(r.class_max + col0 + 32 * k + lane, most[k]);
+      store_halves<NH>(acc, sm, static_cast<uint16_t*>(r.hi) + to, static_cast<uint16_t*>(r.lo) + to, r.pitch, p.M - row0,
+                       count);
     } else {
       __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(r.hi) + to;
       const int rows = p.M - row0;
@@ -381,6 +435,10 @@ struct EpiGrad {
   long long pitch, pitch_acc;
   int add;                     // accum holds earlier pieces
   Undo undo;
+  const unsigned int* class_max;      // fp32, dW: of the rows; null: no power of two of their own
+  __device__ __forceinline__ float undo_class(long long row) const {
+    return class_max != nullptr ? pow2(-class_exp(class_max[row])) : 1.f;
+  }
   template <int NH>
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
     const int row0 = row - (int)(threadIdx.x & 31);
@@ -388,8 +446,9 @@ struct EpiGrad {
     if constexpr (F32) {
       float f0, f1;
       undo.get(f0, f1);
+      const float fc = undo_class(min(row, p.M - 1));      // (one after the other: together they may leave fp32's range)
 #pragma unroll
-      for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1;
+      for (int j = 0; j < NH; ++j) acc[j] = acc[j] * fc * f0 * f1;
     }
     const int rows = p.M - row0, cols = p.N - col0;
     const size_t to = (size_t)row0 * pitch + col0;
@@ -681,6 +740,18 @@ xent_slices_lse_kernel(const float* __restrict__ part, int ks, long long rows, i
   }
 }
 
+// eight values' upper and lower halves
+__device__ __forceinline__ void put_halves(const uint32_t (&w)[8], uint16_t* hi, uint16_t* lo) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    h[j] = __byte_perm(w[2 * j], w[2 * j + 1], 0x7632);
+    l[j] = __byte_perm(w[2 * j], w[2 * j + 1], 0x5410);
+  }
+  *reinterpret_cast<uint4*>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
 template <bool F32>
 __global__ void __launch_bounds__(256)
 xent_slices_p_kernel(const float* __restrict__ part, int ks, long long rows, int n, int pitch, const RowArgs r,
@@ -705,13 +776,87 @@ xent_slices_p_kernel(const float* __restrict__ part, int ks, long long rows, int
       v[j] = keep && c + j < n
                  ? p_value(slice_sum(part, (size_t)row * pitch + c + j, slice, ks) * f0 * f1, lse, t - r.v0 == c + j, g)
                  : 0.f;
-    if constexpr (F32)
-      g16::store_planes<8>(static_cast<__half*>(r.hi) + row * r.pitch + c, static_cast<__half*>(r.lo) + row * r.pitch + c,
-                           v, 8);
-    else
+    if constexpr (F32) {
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = __float_as_uint(v[j]);
+        const unsigned int m = magnitude(w[j]);
+        if (c + j < n && m > __ldcg(r.class_max + c + j)) atomicMax(r.class_max + c + j, m);
+      }
+      put_halves(w, static_cast<uint16_t*>(r.hi) + row * r.pitch + c, static_cast<uint16_t*>(r.lo) + row * r.pitch + c);
+    } else {
       *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(r.hi) + row * r.pitch + c) =
           make_uint4(g16::pack_bf16(v[0], v[1]), g16::pack_bf16(v[2], v[3]), g16::pack_bf16(v[4], v[5]),
                      g16::pack_bf16(v[6], v[7]));
+    }
+  }
+}
+
+// Between the product that forms p and those that read it (fp32): p's halves become, in place, two fp16 terms under the
+// class's power of two; the rows of W of classes that have one of their own are laid out anew with its inverse.
+struct ClassArgs {
+  void* hi;
+  void* lo;
+  long long rows, pitch;       // of p; the pitch a multiple of 8
+  const unsigned int* class_max;
+  int n, d, dp;                // classes of the piece, features
+  const float* W;              // the piece's rows, as given and as terms
+  __half* w_hi;
+  __half* w_lo;
+  const unsigned int* wmax;
+};
+// A warp has 256 classes (512 bytes of either plane) and every eighth of the block's rows.  The classes written last, which
+// are the likeliest to be in L2, come first.
+constexpr int kTermRows = 4;             // of a warp, in flight together
+__global__ void __launch_bounds__(256) xent_class_terms_kernel(const ClassArgs q) {
+  chained_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = (int)(gridDim.y - 1 - blockIdx.y) * 256 + lane * 8;
+  const long long per = (q.rows + gridDim.x - 1) / gridDim.x, end = min(q.rows, (blockIdx.x + 1) * per);
+  if (c < q.pitch) {
+    // (what lies behind the last class is zero in p)
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = c + j < q.n ? pow2(class_exp(__ldg(q.class_max + c + j))) : 0.f;
+    for (long long r = blockIdx.x * per + warp; r < end; r += 8 * kTermRows) {
+      uint4 a[kTermRows], b[kTermRows];
+#pragma unroll
+      for (int u = 0; u < kTermRows; ++u)
+        if (r + 8 * u < end) {
+          a[u] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(q.hi) + (r + 8 * u) * q.pitch + c);
+          b[u] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(q.lo) + (r + 8 * u) * q.pitch + c);
+        }
+#pragma unroll
+      for (int u = 0; u < kTermRows; ++u)
+        if (r + 8 * u < end) {
+          const uint32_t aw[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, bw[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
+          float v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            v[j] = __uint_as_float(__byte_perm(bw[j / 2], aw[j / 2], j & 1 ? 0x7632 : 0x5410)) * f[j];
+          g16::store_planes<8>(static_cast<__half*>(q.hi) + (r + 8 * u) * q.pitch + c,
+                               static_cast<__half*>(q.lo) + (r + 8 * u) * q.pitch + c, v, 8);
+        }
+    }
+  }
+  // a warp looks at the classes of its lanes, and lays out those that need it together
+  const long long warps = (long long)gridDim.x * gridDim.y * 8, first = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 8 + warp;
+  for (long long r0 = first; r0 < q.n; r0 += 32 * warps) {
+    const long long mine = r0 + lane * warps;
+    const int e_mine = mine < q.n ? class_exp(__ldg(q.class_max + mine)) : 0;
+    for (unsigned left = __ballot_sync(0xffffffffu, e_mine != 0); left != 0u; left &= left - 1u) {
+      const int l = __ffs(left) - 1;
+      const long long r = r0 + l * warps;
+      const float f = pow2(-__shfl_sync(0xffffffffu, e_mine, l)), sw = pow2(scale_exp(*q.wmax));
+      const float* src = q.W + r * q.d;
+      for (int c8 = lane * 8; c8 < q.dp; c8 += 256) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c8 + j < q.d ? __ldg(src + c8 + j) * sw * f : 0.f;
+        g16::store_planes<8>(q.w_hi + r * q.dp + c8, q.w_lo + r * q.dp + c8, v, 8);
+      }
+    }
   }
 }
 
@@ -727,7 +872,7 @@ xent_slices_grad_kernel(const float* __restrict__ part, int ks, long long rows, 
        i += (long long)gridDim.x * blockDim.x) {
     const long long row = i / n;
     const int c = (int)(i - row * n);
-    float v = slice_sum(part, (size_t)row * pitch + c, slice, ks) * f0 * f1;
+    float v = slice_sum(part, (size_t)row * pitch + c, slice, ks) * e.undo_class(row) * f0 * f1;
     float* a = e.accum + row * e.pitch_acc + c;
     if (e.add) v += *a;
     if (e.out == nullptr) *a = v;
@@ -749,7 +894,7 @@ size_t up(size_t v) { return (v + 1023) / 1024 * 1024; }
 struct Plan {
   bool f32, copy_w, copy_h;    // fwd: operands are laid out anew (fp32 terms, or rows that do not start on 16 bytes)
   int dp, vp, pieces;
-  size_t off_h, off_w, off_p, off_acc, off_part, off_slots, off_tl, off_inv, total;
+  size_t off_h, off_w, off_p, off_acc, off_part, off_slots, off_tl, off_inv, off_class, total;
 };
 
 // slices of a product: every (tile, slice) has at most one pair's tile of fp32 sums
@@ -787,6 +932,7 @@ Plan plan_xent(const dk_xent& q) {
   p.off_tl = off; off += up((size_t)T * sizeof(float));
   // (inverse powers of two of the rows; those of W in whole tiles)
   p.off_inv = off; off += p.f32 ? up(((size_t)T + 4 + (size_t)q.vocab + 256) * sizeof(float)) : 0;
+  p.off_class = off; off += p.f32 ? up(((size_t)q.vocab + 8) * sizeof(unsigned int)) : 0;
   p.total = off;
   return p;
 }
@@ -828,6 +974,7 @@ struct Call {
   Undo undo_hw;
   const float *inv_h, *inv_w;
   Meta* meta() const { return reinterpret_cast<Meta*>(ws); }
+  unsigned int* class_max() const { return reinterpret_cast<unsigned int*>(ws + pl.off_class); }
   float* part() const { return reinterpret_cast<float*>(ws + pl.off_part); }
 };
 
@@ -871,7 +1018,7 @@ dk_status prepare(Call& c, const void* h, const void* W, const int64_t* target, 
     }
     DK_CUDA_CHECK(launch_chained(xent_prep_kernel<F32>,
                                  dim3(grid_of(((copy_h ? nh : 0) + (pl.copy_w ? nw : 0)) / 8, sms)), 256, 0, c.st, a, b, q.d,
-                                 pl.dp, q.vocab, meta, (int)blocks));
+                                 pl.dp, q.vocab, meta, (int)blocks, c.class_max()));
   }
   c.h = Operand{copy_h ? (const void*)hh : h, hh + nh, q.rows, q.d, pl.dp, 0};
   c.w = Operand{pl.copy_w ? (const void*)wh : W, wh + nw, q.vocab, q.d, pl.dp, 0};
@@ -952,8 +1099,8 @@ dk_status forward(Call& c, const int64_t* target, float* loss, float* lse) {
 }
 
 template <bool F32>
-dk_status backward(Call& c, const int64_t* target, const float* lse, const float* dloss, float scale, void* dh,
-                   void* dW) {
+dk_status backward(Call& c, const void* W, const int64_t* target, const float* lse, const float* dloss, float scale,
+                   void* dh, void* dW) {
   constexpr int NP = F32 ? 3 : 1;
   const dk_xent& q = *c.q;
   const Plan& pl = c.pl;
@@ -973,7 +1120,7 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
     w.lo = static_cast<const __half*>(c.w.lo) + (size_t)v0 * pl.dp;
     w.rows = nv;
     const Operand pop{ph, pl_lo, T, nv, pitch_p, 0};
-    const RowArgs r{target, lse, dloss, scale, q.vocab, v0, &c.meta()->gmax, ph, pl_lo, pitch_p};
+    const RowArgs r{target, lse, dloss, scale, q.vocab, v0, &c.meta()->gmax, c.class_max() + v0, ph, pl_lo, pitch_p};
 
     // p of the piece
     g16::Tiling t = g16::plan(T, nv, q.d, 1, false, sms, NP);
@@ -990,9 +1137,21 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
       if (s != DK_OK) return s;
     }
 
+    if constexpr (F32) {
+      const ClassArgs a{ph, pl_lo, T, pitch_p, r.class_max, nv, q.d, pl.dp, static_cast<const float*>(W) + (size_t)v0 * q.d,
+                        static_cast<__half*>(const_cast<void*>(w.hi)), static_cast<__half*>(const_cast<void*>(w.lo)),
+                        &c.meta()->wmax};
+      const unsigned strips = (unsigned)((pitch_p + 255) / 256);
+      // parts of the rows: 32 rows each, or as many parts as give every class a warp that lays its row of W out
+      long long parts = (T + 31) / 32 > 32 ? (T + 31) / 32 : 32;
+      if (parts > 8LL * sms / strips) parts = 8LL * sms / strips;
+      if (parts < 1) parts = 1;
+      DK_CUDA_CHECK(launch_chained(xent_class_terms_kernel, dim3((unsigned)parts, strips), 256, 0, c.st, a));
+    }
+
     // dh += p.W
     const bool last = i + 1 == pl.pieces;
-    EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, undo_pw};
+    EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, undo_pw, nullptr};
     t = g16::plan(T, q.d, nv, 1, false, sms, NP);
     p = gemm_params(t, T, q.d, F32);
     if (!t.cs && t.ksplit > 1) {
@@ -1007,7 +1166,7 @@ dk_status backward(Call& c, const int64_t* target, const float* lse, const float
     }
 
     // dW of the piece = p^T.h
-    e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, undo_ph};
+    e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, undo_ph, F32 ? r.class_max : nullptr};
     t = g16::plan(nv, q.d, T, 1, false, sms, NP);
     p = gemm_params(t, nv, q.d, F32);
     if (!t.cs && t.ksplit > 1) {
@@ -1102,13 +1261,13 @@ dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const
   Call c;
   s = begin(ctx, q, stream, &c);
   if (s != DK_OK) return s;
-  ProfScope ps(ctx, DK_KERNEL_OTHER, 1 + (c.pl.f32 ? 1 : 0) + 3 * c.pl.pieces, c.st);
+  ProfScope ps(ctx, DK_KERNEL_OTHER, c.pl.f32 ? 2 + 4 * c.pl.pieces : 1 + 3 * c.pl.pieces, c.st);
   if (c.pl.f32) {
     s = prepare<true>(c, h, W, target, dloss, scale, true);
-    return s == DK_OK ? backward<true>(c, target, lse, dloss, scale, dh, dW) : s;
+    return s == DK_OK ? backward<true>(c, W, target, lse, dloss, scale, dh, dW) : s;
   }
   s = prepare<false>(c, h, W, target, dloss, scale, true);
-  return s == DK_OK ? backward<false>(c, target, lse, dloss, scale, dh, dW) : s;
+  return s == DK_OK ? backward<false>(c, W, target, lse, dloss, scale, dh, dW) : s;
 }
 
 }  // extern "C"

@@ -371,3 +371,37 @@ def test_non_finite_values_stay_in_their_row(ctx, rows, vocab, magnitude, dtype)
                 assert not bool(torch.isfinite(got[i][7]).any()) if i in own else torch.equal(got[i][7], clean[i][7])
             assert not bool(torch.isfinite(got[3]).any())
     assert dk.dk_device_status(ctx) == 0
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(9, 64, 600), (200, 64, 600), (64, 512, 1000), (3000, 300, 4001), (9, 30000, 200),
+                                          (2100, 40, 40000), (300, 2000, 2600)])
+@pytest.mark.parametrize("scale_h,scale_w,weight", [(1.0, 1.0, 1.0), (2.0 ** -80, 2.0 ** 80, 2.0 ** -30),
+                                                    (2.0 ** 70, 2.0 ** -70, 2.0 ** 40)])
+def test_improbable_classes_keep_their_digits(ctx, rows, d, vocab, scale_h, scale_w, weight):
+    """dW row by row, for classes whose probability falls to 1e-17 in every row: each row's error is relative to its own
+    terms.  A probability is off by twice the logits' error (2^-19 of the terms, as above) and exp's own rounding
+    (2^-22 of its argument); the two terms add 2^-22 of the class's largest probability per row, h and the sums 2^-19."""
+    h, W, t = draw(rows, d, vocab, torch.float32, seed=24, gain=0.5)
+    g = torch.Generator(device="cuda").manual_seed(25)
+    h[:, 0] = 1.0
+    W[:, 0] = -40.0 * torch.rand(vocab, generator=g, device="cuda")
+    W[:8, 0] = 0.0
+    t = torch.where(t >= 0, t % 8, t)                          # targets among the probable classes
+    h, W = h * scale_h, W * scale_w
+    dloss = weight * (0.5 + torch.rand(rows, generator=g, device="cuda"))
+    loss, lse, dh, dW = call(ctx, h, W, t, dk.DK_F32, dloss=dloss)
+    want = exact(h, W, t, dloss=dloss)
+    keep = t >= 0
+    hk, tk = h.double()[keep], t[keep]
+    z = hk @ W.double().T
+    p = torch.exp(z - torch.logsumexp(z, dim=1)[:, None])
+    assert float(p.max(dim=0).values.min()) < 1e-15
+    p[torch.arange(len(tk), device="cuda"), tk] = 1.0          # (1 - p there: relative to one)
+    p *= dloss.double()[keep][:, None]
+    size = hk.norm(dim=1)
+    rel = 2.0 ** -18 * float((hk.abs() @ W.double().abs().T).max()) + 2.0 ** -22 * 60 + 2.0 ** -18
+    bound = rel * (p.T @ size) + 2.0 ** -22 * p.max(dim=0).values * size.sum()
+    bound += 2.0 ** -149 * d ** 0.5                            # (where the result itself is subnormal)
+    err = (dW.double() - want[3]).norm(dim=1)
+    assert bool((err <= bound).all())
+    assert float((dh.double() - want[2]).norm()) <= rel * float(want[2].norm()) + 2.0 ** -22 * weight * float(W.double().norm())
