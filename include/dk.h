@@ -461,10 +461,10 @@ DK_API dk_status dk_xent_workspace_bytes(const dk_xent* q, size_t* bytes);
  * >= vocab is left out likewise and reported by dk_device_status as
  * DK_ERR_INVALID_ARG.  DK_F32 contracts on the tensor cores with each operand
  * as two fp16 terms under a power of two of each row of h and W (22 significant
- * bits down to 2^-18 of the row's largest magnitude, an absolute error of 2^-40
- * of that magnitude below).  A token or a few (up to 8 rows with DK_F32, one with
- * DK_BF16, d <= 8192) contract in fp32 instead, reading W once.  Needs the
- * workspace. */
+ * bits down to 2^-17 of the row's largest magnitude, an absolute error of 2^-39
+ * of that magnitude below).  A token or a few contract in fp32 instead, reading W
+ * once: one row up to d = 8192, with DK_F32 also 2 to 4 rows up to d = 6144 and 5
+ * to 8 up to d = 3072, on 2 classes or more.  Needs the workspace. */
 DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
                                     const int64_t* target, float* loss, float* lse, void* stream);
 
@@ -474,10 +474,10 @@ DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h
  * lse: from the forward call.  With DK_BF16 p is rounded to bf16 for the two
  * products.  With DK_F32 h, W and p enter as two fp16 terms each, 22 bits: h and
  * W under one power of two each (of the whole tensor: the products sum over their
- * rows; 22 bits down to 2^-18 of the tensor's largest finite magnitude, an
- * absolute error of 2^-40 of it below), p under one of each class.  So a row of
+ * rows; 22 bits down to 2^-17 of the tensor's largest finite magnitude, an
+ * absolute error of 2^-39 of it below), p under one of each class.  So a row of
  * dW keeps its digits however improbable its class is, and a row of dh those
- * down to 2^-18 of the largest |scale*dloss|, with an absolute error of 2^-40 of
+ * down to 2^-17 of the largest |scale*dloss|, with an absolute error of 2^-39 of
  * it (times W) below.  dh and dW are overwritten.  Needs the workspace. */
 DK_API dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
                                     const int64_t* target, const float* lse, const float* dloss, float scale,

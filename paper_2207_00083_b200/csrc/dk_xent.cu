@@ -1060,7 +1060,8 @@ dk_status few_rows(dk_ctx* ctx, const Plan& pl, char* ws, const FewArgs& a, floa
 }
 
 // Both sides of the rule, in us (rows x d, classes; here | tensor cores): fp32 1 x 4096, 1000 19.5 | 29.6; 3 x 1538, 6216
-// 36 | 56; 8 x 1024, 50257 69 | 204; 1 x 2048, 128000 198 | 746; but 1 x 12288, 64 36 | 28: a warp walks its row alone.
+// 36 | 56; 8 x 1024, 50257 69 | 204; 1 x 2048, 128000 198 | 746; but 1 x 12288, 64 36 | 28: a warp walks its row alone.  h takes
+// its room of shared memory in 1, 4 or 8 rows: 2 to 4 rows stop at 6144 features, 5 to 8 at 3072.
 // bf16, where the tensor cores read W as it is: 1 x 2048, 128000 108 | 144, but 4 rows 144 | 126.  A lone class has
 // probability one exactly: both directions have to see the same logit, so it takes the backward call's way.
 bool takes_few_rows(const dk_xent& q) {

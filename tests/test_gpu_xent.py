@@ -405,3 +405,21 @@ def test_improbable_classes_keep_their_digits(ctx, rows, d, vocab, scale_h, scal
     err = (dW.double() - want[3]).norm(dim=1)
     assert bool((err <= bound).all())
     assert float((dh.double() - want[2]).norm()) <= rel * float(want[2].norm()) + 2.0 ** -22 * weight * float(W.double().norm())
+
+
+@pytest.mark.parametrize("dtype,rows,d,few", [
+    ("f32", 1, 8192, True), ("f32", 1, 8193, False), ("f32", 1, 8160, True), ("f32", 2, 6144, True), ("f32", 4, 6143, True),
+    ("f32", 4, 6112, True), ("f32", 4, 6145, False), ("f32", 3, 6160, False), ("f32", 5, 3071, True), ("f32", 8, 3040, True),
+    ("f32", 8, 3071, True), ("f32", 8, 3073, False), ("f32", 5, 3088, False), ("f32", 9, 64, False),
+    ("bf16", 1, 8192, True), ("bf16", 1, 8191, True), ("bf16", 1, 8200, False), ("bf16", 2, 64, False)])
+def test_limits_of_the_dot_products(ctx, dtype, rows, d, few):
+    """Either side of each limit that dk.h states, and which way was taken: the dot products are two kernels (with the one
+    that joins), the tensor cores' way one more where operands are laid out (fp32, or rows off 16-byte boundaries)."""
+    h, W, t = draw(rows, d, 300, TYPES[dtype][1], seed=26, ignored=0.0)
+    check(ctx, h, W, t, dtype)
+    q = dk.dk_xent(rows, d, 300, TYPES[dtype][0])
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dk.dk_profile_reset(ctx)
+    dk.dk_linear_xent_fwd(ctx, q, h, W, t, loss, lse)
+    launches = dk.dk_profile_read(ctx)["other"][2]
+    assert launches == (2 if few or (dtype == "bf16" and d % 8 == 0) else 3)
