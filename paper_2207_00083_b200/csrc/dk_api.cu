@@ -225,6 +225,10 @@ ProfScope::~ProfScope() {
   if (slot >= 0) cudaEventRecord(ctx->prof->ev[2 * slot + 1], st);
 }
 
+void count_launches(dk_ctx* c, int kind, int nkernels) {
+  if (c->prof) c->prof->launches[kind] += nkernels;
+}
+
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 struct WsPlan {

@@ -183,6 +183,8 @@ struct ProfScope {
   ProfScope(dk_ctx* c, int kind, int nkernels, cudaStream_t s);
   ~ProfScope();
 };
+// kernels of `kind` beyond those that a ProfScope was told of (for calls whose way is chosen after it)
+void count_launches(dk_ctx* ctx, int kind, int nkernels);
 
 // tensor-core path (dk_tc.cu)
 dk_status tc_init(dk_ctx* ctx);

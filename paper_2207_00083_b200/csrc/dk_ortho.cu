@@ -950,6 +950,7 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
       s = pl.tall ? g16::launch<3, true, true, BN>(ctx, X, X, p, ep, st)
                   : g16::launch<3, false, false, BN>(ctx, X, X, p, ep, st);
       if (s != DK_OK) return s;
+      count_launches(ctx, DK_KERNEL_OTHER, 1);
       DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st, sa));
     }
     // B
@@ -961,6 +962,7 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
     } else {
       s = g16::launch<3, false, false, BN>(ctx, A, A, p, ep, st);
       if (s != DK_OK) return s;
+      count_launches(ctx, DK_KERNEL_OTHER, 1);
       DK_CUDA_CHECK(launch_chained(ortho_sym_kernel, dim3(nt, nt, (unsigned)q.batch), 256, 0, st, sa));
     }
     // X
@@ -977,6 +979,7 @@ dk_status orthogonalize(dk_ctx* ctx, const dk_ortho& q, const Plan& pl, const vo
       s = pl.tall ? g16::launch<3, false, false, BN>(ctx, X, B, p, ex, st)
                   : g16::launch<3, false, true, BN>(ctx, B, X, p, ex, st);
       if (s != DK_OK) return s;
+      count_launches(ctx, DK_KERNEL_OTHER, 1);
       DK_CUDA_CHECK(launch_chained(ortho_x_kernel, dim3(grid_of(rows * ((q.n + 7) / 8), sms)), 256, 0, st,
                                  xa, part, tx.ksplit, pitch_x, nullptr, nullptr, rows, 0));
     } else {
@@ -1018,7 +1021,8 @@ dk_status dk_orthogonalize(dk_ctx* ctx, const dk_ortho* q, const void* x, float 
   OnDevice dev(ctx->device);
   if (!dev.ok) return DK_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  ProfScope ps(ctx, DK_KERNEL_OTHER, resident_columns(*q, pl, ctx->sm_count) ? 1 : 2 + 3 * q->steps, st);
+  // (kernels that join slices are counted where they are launched)
+  ProfScope ps(ctx, DK_KERNEL_OTHER, resident_columns(*q, pl, ctx->sm_count) ? 1 : q->steps ? 2 + 3 * q->steps : 3, st);
   return orthogonalize(ctx, *q, pl, x, scale, keep, out, st);
 }
 

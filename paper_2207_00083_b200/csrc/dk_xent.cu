@@ -1131,6 +1131,7 @@ dk_status backward(Call& c, const void* W, const int64_t* target, const float* l
       const int pitch = (nv + 3) / 4 * 4;
       s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
+      count_launches(c.ctx, DK_KERNEL_OTHER, 1);
       DK_CUDA_CHECK(launch_chained(xent_slices_p_kernel<F32>, dim3(grid_of(T * pitch_p / 8, c.ctx->sm_count)), 256, 0, c.st,
                                  c.part(), t.ksplit, T, nv, pitch, r, c.undo_hw));
     } else {
@@ -1159,6 +1160,7 @@ dk_status backward(Call& c, const void* W, const int64_t* target, const float* l
       const int pitch = (q.d + 3) / 4 * 4;
       s = g16::launch<NP, false, true, BN>(c.ctx, pop, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
+      count_launches(c.ctx, DK_KERNEL_OTHER, 1);
       DK_CUDA_CHECK(launch_chained(xent_slices_grad_kernel<F32>, dim3(grid_of(T * q.d, c.ctx->sm_count)), 256, 0, c.st,
                                  c.part(), t.ksplit, T, q.d, pitch, e));
     } else {
@@ -1174,6 +1176,7 @@ dk_status backward(Call& c, const void* W, const int64_t* target, const float* l
       const int pitch = (q.d + 3) / 4 * 4;
       s = g16::launch<NP, true, true, BN>(c.ctx, pop, c.h, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
+      count_launches(c.ctx, DK_KERNEL_OTHER, 1);
       DK_CUDA_CHECK(launch_chained(xent_slices_grad_kernel<F32>, dim3(grid_of((long long)nv * q.d, c.ctx->sm_count)), 256, 0, c.st,
                                  c.part(), t.ksplit, nv, q.d, pitch, e));
     } else {
@@ -1262,6 +1265,7 @@ dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const
   Call c;
   s = begin(ctx, q, stream, &c);
   if (s != DK_OK) return s;
+  // (slices of a product that are joined by a kernel of their own are counted where that is launched)
   ProfScope ps(ctx, DK_KERNEL_OTHER, c.pl.f32 ? 2 + 4 * c.pl.pieces : 1 + 3 * c.pl.pieces, c.st);
   if (c.pl.f32) {
     s = prepare<true>(c, h, W, target, dloss, scale, true);
