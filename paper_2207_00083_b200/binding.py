@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from types import SimpleNamespace
 from typing import Optional
 
 import numpy as np
@@ -162,11 +163,11 @@ def problem_from_spec(spec, layout: int = DK_NHWC, precision: Optional[int] = No
                       spec.stride, spec.pad, spec.K, spec.G if G is None else G, precision, tol)
 
 
-def _dev(t: Optional[torch.Tensor]):
+def _dev(ctx, t: Optional[torch.Tensor]):
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous()):
-        raise ValueError("expected a contiguous fp32 CUDA tensor")
+    if not (t.get_device() == ctx.device and t.dtype == torch.float32 and t.is_contiguous()):
+        raise ValueError(f"expected a contiguous fp32 tensor on CUDA device {ctx.device}")
     return ctypes.c_void_p(t.data_ptr())
 
 
@@ -176,8 +177,12 @@ def _host(a: np.ndarray):
     return ctypes.c_void_p(a.ctypes.data)
 
 
-def _stream() -> ctypes.c_void_p:
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+# (some of the calls take microseconds on the GPU for small layers: their marshalling is kept to plain integers)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _stream(ctx) -> ctypes.c_void_p:
+    return ctypes.c_void_p(_raw_stream(ctx.device))
 
 
 def _check(status: int, where: str):
@@ -290,25 +295,27 @@ def read_verdict(v: torch.Tensor) -> dict:
 
 
 def dk_encode(ctx: Context, p: dk_problem, x, r, C: np.ndarray, xbar):
-    _check(lib().dk_encode(ctx.handle, ctypes.byref(p), _dev(x), _dev(r), _host(C), _dev(xbar), _stream()),
-           "dk_encode")
+    _check(lib().dk_encode(ctx.handle, ctypes.byref(p), _dev(ctx, x), _dev(ctx, r), _host(C), _dev(ctx, xbar),
+                           _stream(ctx)), "dk_encode")
 
 
 def dk_linear_fwd(ctx: Context, p: dk_problem, W, xbar, ybar):
-    _check(lib().dk_linear_fwd(ctx.handle, ctypes.byref(p), _dev(W), _dev(xbar), _dev(ybar), _stream()),
-           "dk_linear_fwd")
+    _check(lib().dk_linear_fwd(ctx.handle, ctypes.byref(p), _dev(ctx, W), _dev(ctx, xbar), _dev(ctx, ybar),
+                               _stream(ctx)), "dk_linear_fwd")
 
 
 def dk_decode_verify(ctx: Context, p: dk_problem, ybar, C: np.ndarray, bias, y, verdict):
-    _check(lib().dk_decode_verify(ctx.handle, ctypes.byref(p), _dev(ybar), _host(C), _dev(bias), _dev(y),
-                                  ctypes.c_void_p(verdict.data_ptr()), _stream()), "dk_decode_verify")
+    _check(lib().dk_decode_verify(ctx.handle, ctypes.byref(p), _dev(ctx, ybar), _host(C), _dev(ctx, bias),
+                                  _dev(ctx, y), ctypes.c_void_p(verdict.data_ptr()), _stream(ctx)),
+           "dk_decode_verify")
 
 
 def dk_decode_verify_static(device: int, p: dk_problem, ybar, C: np.ndarray, bias, y, verdict):
     """Same result as dk_decode_verify, for callers that may not allocate: no
     context, scratch in a fixed array inside the library (see include/dk.h)."""
-    _check(lib().dk_decode_verify_static(device, ctypes.byref(p), _dev(ybar), _host(C), _dev(bias), _dev(y),
-                                         ctypes.c_void_p(verdict.data_ptr()), _stream()),
+    on = SimpleNamespace(device=device)
+    _check(lib().dk_decode_verify_static(device, ctypes.byref(p), _dev(on, ybar), _host(C), _dev(on, bias),
+                                         _dev(on, y), ctypes.c_void_p(verdict.data_ptr()), _stream(on)),
            "dk_decode_verify_static")
 
 
@@ -323,58 +330,58 @@ def dk_device_status(ctx: Context) -> int:
 def dk_masked_linear(ctx: Context, p: dk_problem, W, x, r, C: np.ndarray, bias, y, xbar_save, verdict,
                      fault: Optional[dk_fault] = None):
     fp = ctypes.byref(fault) if fault is not None else None
-    _check(lib().dk_masked_linear(ctx.handle, ctypes.byref(p), _dev(W), _dev(x), _dev(r), _host(C),
-                                  _dev(bias), _dev(y), _dev(xbar_save),
-                                  ctypes.c_void_p(verdict.data_ptr()), fp, _stream()), "dk_masked_linear")
+    _check(lib().dk_masked_linear(ctx.handle, ctypes.byref(p), _dev(ctx, W), _dev(ctx, x), _dev(ctx, r), _host(C),
+                                  _dev(ctx, bias), _dev(ctx, y), _dev(ctx, xbar_save),
+                                  ctypes.c_void_p(verdict.data_ptr()), fp, _stream(ctx)), "dk_masked_linear")
 
 
 def dk_linear_bwd_wgrad_verify(ctx: Context, p: dk_problem, delta, xbar, C: np.ndarray, gamma: np.ndarray,
                                scale: float, tol_w: float, dW, verdict, fault=None):
     fp = ctypes.byref(fault) if fault is not None else None
-    _check(lib().dk_linear_bwd_wgrad_verify(ctx.handle, ctypes.byref(p), _dev(delta), _dev(xbar), _host(C),
-                                            _host(gamma), ctypes.c_float(scale), ctypes.c_float(tol_w), _dev(dW),
-                                            ctypes.c_void_p(verdict.data_ptr()), fp, _stream()),
+    _check(lib().dk_linear_bwd_wgrad_verify(ctx.handle, ctypes.byref(p), _dev(ctx, delta), _dev(ctx, xbar), _host(C),
+                                            _host(gamma), ctypes.c_float(scale), ctypes.c_float(tol_w), _dev(ctx, dW),
+                                            ctypes.c_void_p(verdict.data_ptr()), fp, _stream(ctx)),
            "dk_linear_bwd_wgrad_verify")
 
 
 def dk_linear_bwd_wgrad(ctx: Context, p: dk_problem, delta, xbar, xbar_rows: int, C: np.ndarray,
                         gamma: np.ndarray, scale: float, dW):
-    _check(lib().dk_linear_bwd_wgrad(ctx.handle, ctypes.byref(p), _dev(delta), _dev(xbar), xbar_rows,
-                                     _host(C), _host(gamma), ctypes.c_float(scale), _dev(dW), _stream()),
+    _check(lib().dk_linear_bwd_wgrad(ctx.handle, ctypes.byref(p), _dev(ctx, delta), _dev(ctx, xbar), xbar_rows,
+                                     _host(C), _host(gamma), ctypes.c_float(scale), _dev(ctx, dW), _stream(ctx)),
            "dk_linear_bwd_wgrad")
 
 
 def dk_linear_bwd_wgrad_accumulate(ctx: Context, p: dk_problem, delta, xbar, xbar_rows: int, C: np.ndarray,
                                    gamma: np.ndarray, scale: float, dW):
-    _check(lib().dk_linear_bwd_wgrad_accumulate(ctx.handle, ctypes.byref(p), _dev(delta), _dev(xbar), xbar_rows,
-                                                _host(C), _host(gamma), ctypes.c_float(scale), _dev(dW),
-                                                _stream()), "dk_linear_bwd_wgrad_accumulate")
+    _check(lib().dk_linear_bwd_wgrad_accumulate(ctx.handle, ctypes.byref(p), _dev(ctx, delta), _dev(ctx, xbar),
+                                                xbar_rows, _host(C), _host(gamma), ctypes.c_float(scale),
+                                                _dev(ctx, dW), _stream(ctx)), "dk_linear_bwd_wgrad_accumulate")
 
 
 def dk_linear_bwd_dgrad(ctx: Context, p: dk_problem, W, delta, dx):
-    _check(lib().dk_linear_bwd_dgrad(ctx.handle, ctypes.byref(p), _dev(W), _dev(delta), _dev(dx), _stream()),
-           "dk_linear_bwd_dgrad")
+    _check(lib().dk_linear_bwd_dgrad(ctx.handle, ctypes.byref(p), _dev(ctx, W), _dev(ctx, delta), _dev(ctx, dx),
+                                     _stream(ctx)), "dk_linear_bwd_dgrad")
 
 
 def dk_relu_pool_fwd(ctx: Context, x, n: int, h: int, w: int, c: int, pool: bool, y):
-    _check(lib().dk_relu_pool_fwd(ctx.handle, _dev(x), n, h, w, c, int(pool), _dev(y), _stream()),
+    _check(lib().dk_relu_pool_fwd(ctx.handle, _dev(ctx, x), n, h, w, c, int(pool), _dev(ctx, y), _stream(ctx)),
            "dk_relu_pool_fwd")
 
 
 def dk_relu_pool_bwd(ctx: Context, dy, x, n: int, h: int, w: int, c: int, pool: bool, dx):
-    _check(lib().dk_relu_pool_bwd(ctx.handle, _dev(dy), _dev(x), n, h, w, c, int(pool), _dev(dx), _stream()),
-           "dk_relu_pool_bwd")
+    _check(lib().dk_relu_pool_bwd(ctx.handle, _dev(ctx, dy), _dev(ctx, x), n, h, w, c, int(pool), _dev(ctx, dx),
+                                  _stream(ctx)), "dk_relu_pool_bwd")
 
 
 # ---------------------------------------------------------------------------
 # finite-field calls: residues are int32 CUDA tensors holding values in [0, p)
 # (the library reads them as uint32), coefficient arrays NumPy uint32 on the host
 # ---------------------------------------------------------------------------
-def _res(t: Optional[torch.Tensor]):
+def _res(ctx, t: Optional[torch.Tensor]):
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()):
-        raise ValueError("expected a contiguous int32 CUDA tensor of residues")
+    if not (t.get_device() == ctx.device and t.dtype == torch.int32 and t.is_contiguous()):
+        raise ValueError(f"expected a contiguous int32 tensor of residues on CUDA device {ctx.device}")
     return ctypes.c_void_p(t.data_ptr())
 
 
@@ -385,45 +392,45 @@ def _host_u32(a: np.ndarray):
 
 
 def dk_field_quantize(ctx: Context, v, scale_bits: int, prime: int, vq):
-    _check(lib().dk_field_quantize(ctx.handle, _dev(v), v.numel(), scale_bits, prime, _res(vq), _stream()),
-           "dk_field_quantize")
+    _check(lib().dk_field_quantize(ctx.handle, _dev(ctx, v), v.numel(), scale_bits, prime, _res(ctx, vq),
+                                   _stream(ctx)), "dk_field_quantize")
 
 
 def dk_field_dequantize(ctx: Context, vq, scale_bits: int, prime: int, v):
-    _check(lib().dk_field_dequantize(ctx.handle, _res(vq), vq.numel(), scale_bits, prime, _dev(v), _stream()),
-           "dk_field_dequantize")
+    _check(lib().dk_field_dequantize(ctx.handle, _res(ctx, vq), vq.numel(), scale_bits, prime, _dev(ctx, v),
+                                     _stream(ctx)), "dk_field_dequantize")
 
 
 def dk_field_encode(ctx: Context, p: dk_problem, prime: int, xq, rq, C: np.ndarray, xbar):
-    _check(lib().dk_field_encode(ctx.handle, ctypes.byref(p), prime, _res(xq), _res(rq), _host_u32(C),
-                                 _res(xbar), _stream()), "dk_field_encode")
+    _check(lib().dk_field_encode(ctx.handle, ctypes.byref(p), prime, _res(ctx, xq), _res(ctx, rq), _host_u32(C),
+                                 _res(ctx, xbar), _stream(ctx)), "dk_field_encode")
 
 
 def dk_field_linear_fwd(ctx: Context, p: dk_problem, prime: int, Wq, xbar, ybar):
-    _check(lib().dk_field_linear_fwd(ctx.handle, ctypes.byref(p), prime, _res(Wq), _res(xbar), _res(ybar),
-                                     _stream()), "dk_field_linear_fwd")
+    _check(lib().dk_field_linear_fwd(ctx.handle, ctypes.byref(p), prime, _res(ctx, Wq), _res(ctx, xbar),
+                                     _res(ctx, ybar), _stream(ctx)), "dk_field_linear_fwd")
 
 
 def dk_field_decode_verify(ctx: Context, p: dk_problem, prime: int, l: int, ybar, C: np.ndarray, bias_q, yq, y,
                            verdict):
-    _check(lib().dk_field_decode_verify(ctx.handle, ctypes.byref(p), prime, l, _res(ybar), _host_u32(C),
-                                        _res(bias_q), _res(yq), _dev(y), ctypes.c_void_p(verdict.data_ptr()),
-                                        _stream()), "dk_field_decode_verify")
+    _check(lib().dk_field_decode_verify(ctx.handle, ctypes.byref(p), prime, l, _res(ctx, ybar), _host_u32(C),
+                                        _res(ctx, bias_q), _res(ctx, yq), _dev(ctx, y),
+                                        ctypes.c_void_p(verdict.data_ptr()), _stream(ctx)), "dk_field_decode_verify")
 
 
 def dk_field_masked_linear(ctx: Context, p: dk_problem, prime: int, l: int, W, x, rq, C: np.ndarray, bias, y, yq,
                            xbar_save, verdict, fault: Optional[dk_field_fault] = None):
     fp = ctypes.byref(fault) if fault is not None else None
-    _check(lib().dk_field_masked_linear(ctx.handle, ctypes.byref(p), prime, l, _dev(W), _dev(x), _res(rq),
-                                        _host_u32(C), _dev(bias), _dev(y), _res(yq), _res(xbar_save),
-                                        ctypes.c_void_p(verdict.data_ptr()), fp, _stream()),
-           "dk_field_masked_linear")
+    _check(lib().dk_field_masked_linear(ctx.handle, ctypes.byref(p), prime, l, _dev(ctx, W), _dev(ctx, x),
+                                        _res(ctx, rq), _host_u32(C), _dev(ctx, bias), _dev(ctx, y), _res(ctx, yq),
+                                        _res(ctx, xbar_save), ctypes.c_void_p(verdict.data_ptr()), fp,
+                                        _stream(ctx)), "dk_field_masked_linear")
 
 
 def dk_field_linear_bwd_wgrad(ctx: Context, p: dk_problem, prime: int, deltaq, xbar, xbar_rows: int, C: np.ndarray,
                               gamma: np.ndarray, dWq):
-    _check(lib().dk_field_linear_bwd_wgrad(ctx.handle, ctypes.byref(p), prime, _res(deltaq), _res(xbar), xbar_rows,
-                                           _host_u32(C), _host_u32(gamma), _res(dWq), _stream()),
+    _check(lib().dk_field_linear_bwd_wgrad(ctx.handle, ctypes.byref(p), prime, _res(ctx, deltaq), _res(ctx, xbar),
+                                           xbar_rows, _host_u32(C), _host_u32(gamma), _res(ctx, dWq), _stream(ctx)),
            "dk_field_linear_bwd_wgrad")
 
 
@@ -433,18 +440,18 @@ def dk_field_linear_bwd_wgrad(ctx: Context, p: dk_problem, prime: int, deltaq, x
 # parameters, statistics and losses fp32, targets int64.
 # ---------------------------------------------------------------------------
 _STEP_TYPES = {DK_F32: torch.float32, DK_BF16: torch.bfloat16}
-# (the calls below take microseconds on the GPU for small layers: the marshalling is kept to plain integers)
-_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _typed(t: torch.Tensor, dtype: int, numel: int, what: str) -> int:
-    if t.dtype is not _STEP_TYPES.get(dtype) or t.numel() != numel or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what}: expected a contiguous {_STEP_TYPES.get(dtype)} CUDA tensor of {numel} elements")
+def _typed(ctx, t: torch.Tensor, dtype: int, numel: int, what: str) -> int:
+    if (t.dtype is not _STEP_TYPES.get(dtype) or t.numel() != numel or not t.is_contiguous()
+            or t.get_device() != ctx.device):
+        raise ValueError(f"{what}: expected a contiguous {_STEP_TYPES.get(dtype)} tensor of {numel} elements on CUDA "
+                         f"device {ctx.device}")
     return t.data_ptr()
 
 
-def _f32(t: torch.Tensor, numel: int, what: str):
-    return _typed(t, DK_F32, numel, what)
+def _f32(ctx, t: torch.Tensor, numel: int, what: str):
+    return _typed(ctx, t, DK_F32, numel, what)
 
 
 def _norm_sizes(q: dk_norm):
@@ -454,43 +461,47 @@ def _norm_sizes(q: dk_norm):
 
 def dk_group_norm_fwd(ctx: Context, q: dk_norm, x, gamma, beta, y, stats):
     e, c, s = _norm_sizes(q)
-    _check(lib().dk_group_norm_fwd(ctx.handle, ctypes.byref(q), _typed(x, q.dtype, e, "x"), _f32(gamma, c, "gamma"),
-                                   _f32(beta, c, "beta"), _typed(y, q.dtype, e, "y"), _f32(stats, s, "stats"),
+    _check(lib().dk_group_norm_fwd(ctx.handle, ctypes.byref(q), _typed(ctx, x, q.dtype, e, "x"),
+                                   _f32(ctx, gamma, c, "gamma"), _f32(ctx, beta, c, "beta"),
+                                   _typed(ctx, y, q.dtype, e, "y"), _f32(ctx, stats, s, "stats"),
                                    _raw_stream(ctx.device)), "dk_group_norm_fwd")
 
 
 def dk_group_norm_bwd(ctx: Context, q: dk_norm, dy, x, gamma, beta, stats, dx, dgamma, dbeta):
     e, c, s = _norm_sizes(q)
-    _check(lib().dk_group_norm_bwd(ctx.handle, ctypes.byref(q), _typed(dy, q.dtype, e, "dy"),
-                                   _typed(x, q.dtype, e, "x"), _f32(gamma, c, "gamma"), _f32(beta, c, "beta"),
-                                   _f32(stats, s, "stats"), _typed(dx, q.dtype, e, "dx"), _f32(dgamma, c, "dgamma"),
-                                   _f32(dbeta, c, "dbeta"), _raw_stream(ctx.device)), "dk_group_norm_bwd")
+    _check(lib().dk_group_norm_bwd(ctx.handle, ctypes.byref(q), _typed(ctx, dy, q.dtype, e, "dy"),
+                                   _typed(ctx, x, q.dtype, e, "x"), _f32(ctx, gamma, c, "gamma"),
+                                   _f32(ctx, beta, c, "beta"), _f32(ctx, stats, s, "stats"),
+                                   _typed(ctx, dx, q.dtype, e, "dx"), _f32(ctx, dgamma, c, "dgamma"),
+                                   _f32(ctx, dbeta, c, "dbeta"), _raw_stream(ctx.device)), "dk_group_norm_bwd")
 
 
-def _targets(t: torch.Tensor, rows: int):
-    if not (t.is_cuda and t.dtype == torch.int64 and t.is_contiguous() and t.numel() == rows):
-        raise ValueError(f"target: expected a contiguous int64 CUDA tensor of {rows} elements")
+def _targets(ctx, t: torch.Tensor, rows: int):
+    if not (t.get_device() == ctx.device and t.dtype == torch.int64 and t.is_contiguous() and t.numel() == rows):
+        raise ValueError(f"target: expected a contiguous int64 tensor of {rows} elements on CUDA device {ctx.device}")
     return t.data_ptr()
 
 
 def dk_linear_xent_fwd(ctx: Context, q: dk_xent, h, W, target, loss, lse):
-    _check(lib().dk_linear_xent_fwd(ctx.handle, ctypes.byref(q), _typed(h, q.dtype, q.rows * q.d, "h"),
-                                    _typed(W, q.dtype, q.vocab * q.d, "W"), _targets(target, q.rows),
-                                    _f32(loss, q.rows, "loss"), _f32(lse, q.rows, "lse"), _raw_stream(ctx.device)),
-           "dk_linear_xent_fwd")
+    _check(lib().dk_linear_xent_fwd(ctx.handle, ctypes.byref(q), _typed(ctx, h, q.dtype, q.rows * q.d, "h"),
+                                    _typed(ctx, W, q.dtype, q.vocab * q.d, "W"), _targets(ctx, target, q.rows),
+                                    _f32(ctx, loss, q.rows, "loss"), _f32(ctx, lse, q.rows, "lse"),
+                                    _raw_stream(ctx.device)), "dk_linear_xent_fwd")
 
 
 def dk_linear_xent_bwd(ctx: Context, q: dk_xent, h, W, target, lse, dloss: Optional[torch.Tensor], scale: float, dh,
                        dW):
-    _check(lib().dk_linear_xent_bwd(ctx.handle, ctypes.byref(q), _typed(h, q.dtype, q.rows * q.d, "h"),
-                                    _typed(W, q.dtype, q.vocab * q.d, "W"), _targets(target, q.rows),
-                                    _f32(lse, q.rows, "lse"), None if dloss is None else _f32(dloss, q.rows, "dloss"),
-                                    scale, _typed(dh, q.dtype, q.rows * q.d, "dh"),
-                                    _typed(dW, q.dtype, q.vocab * q.d, "dW"), _raw_stream(ctx.device)), "dk_linear_xent_bwd")
+    _check(lib().dk_linear_xent_bwd(ctx.handle, ctypes.byref(q), _typed(ctx, h, q.dtype, q.rows * q.d, "h"),
+                                    _typed(ctx, W, q.dtype, q.vocab * q.d, "W"), _targets(ctx, target, q.rows),
+                                    _f32(ctx, lse, q.rows, "lse"),
+                                    None if dloss is None else _f32(ctx, dloss, q.rows, "dloss"), scale,
+                                    _typed(ctx, dh, q.dtype, q.rows * q.d, "dh"),
+                                    _typed(ctx, dW, q.dtype, q.vocab * q.d, "dW"), _raw_stream(ctx.device)),
+           "dk_linear_xent_bwd")
 
 
 def dk_orthogonalize(ctx: Context, q: dk_ortho, x, scale: float, keep: float, out):
     e = q.batch * q.m * q.n
-    _check(lib().dk_orthogonalize(ctx.handle, ctypes.byref(q), _typed(x, q.dtype, e, "x"), scale,
-                                  keep, _typed(out, q.dtype, e, "out"), _raw_stream(ctx.device)),
+    _check(lib().dk_orthogonalize(ctx.handle, ctypes.byref(q), _typed(ctx, x, q.dtype, e, "x"), scale,
+                                  keep, _typed(ctx, out, q.dtype, e, "out"), _raw_stream(ctx.device)),
            "dk_orthogonalize")

@@ -1,7 +1,10 @@
 """Argument checks of the training-step calls that need no GPU: the workspace sizes."""
 import ctypes
+from types import SimpleNamespace
 
+import numpy as np
 import pytest
+import torch
 
 from paper_2207_00083_b200 import binding as dk
 
@@ -85,3 +88,57 @@ def test_images_of_almost_two_to_the_31_pixels(h, w, c):
 @pytest.mark.parametrize("h,w", [(1, 2 ** 31 - 4095), (1, 2 ** 31 - 1), (46341, 46341)])
 def test_images_past_the_limit_are_refused(h, w):
     assert size(dk.dk_norm(1, h, w, 1, 1, 0, 1, 1e-5))[0] == SHAPE
+
+
+class Elsewhere:
+    """What the binding asks of a tensor, on a device of choice."""
+
+    def __init__(self, device, numel, dtype):
+        self.device_index, self.n, self.dtype, self.is_cuda = device, numel, dtype, device >= 0
+
+    def get_device(self):
+        return self.device_index
+
+    def numel(self):
+        return self.n
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+NORM, XENT, ORTHO = dk.dk_norm(2, 3, 3, 8, 2, 1, 0, 1e-5), dk.dk_xent(4, 8, 16, 0), dk.dk_ortho(1, 8, 8, 0, 5, 1.5, -0.5, 0.0, 0.0)
+CONV = dk.dk_problem(dk.DK_FC, dk.DK_NHWC, 8, 8, 1, 1, 1, 1, 1, 0, 4, 1, 0, 0.0)
+F, I64, I32 = torch.float32, torch.int64, torch.int32
+COEF = np.zeros((1, 6, 5), np.float32)
+CALLS = {
+    "dk_group_norm_fwd": (lambda f, c, t: f(c, NORM, *t), [(144, F), (8, F), (8, F), (144, F), (8, F)]),
+    "dk_group_norm_bwd": (lambda f, c, t: f(c, NORM, *t), [(144, F), (144, F), (8, F), (8, F), (8, F), (144, F), (8, F), (8, F)]),
+    "dk_linear_xent_fwd": (lambda f, c, t: f(c, XENT, *t), [(32, F), (128, F), (4, I64), (4, F), (4, F)]),
+    "dk_linear_xent_bwd": (lambda f, c, t: f(c, XENT, *t[:5], 1.0, *t[5:]),
+                           [(32, F), (128, F), (4, I64), (4, F), (4, F), (32, F), (128, F)]),
+    "dk_orthogonalize": (lambda f, c, t: f(c, ORTHO, t[0], 1.0, 0.0, t[1]), [(64, F), (64, F)]),
+    "dk_encode": (lambda f, c, t: f(c, CONV, t[0], t[1], COEF, t[2]), [(32, F), (8, F), (48, F)]),
+    "dk_linear_bwd_dgrad": (lambda f, c, t: f(c, CONV, *t), [(64, F), (32, F), (32, F)]),
+    "dk_relu_pool_fwd": (lambda f, c, t: f(c, t[0], 4, 1, 1, 8, False, t[1]), [(32, F), (32, F)]),
+    "dk_field_quantize": (lambda f, c, t: f(c, t[0], 8, 2 ** 25 - 39, t[1]), [(32, F), (32, I32)]),
+}
+
+
+@pytest.mark.parametrize("device,other", [(0, 1), (1, 0), (0, -1)])
+@pytest.mark.parametrize("name", CALLS)
+def test_tensors_of_another_device_are_refused(name, device, other, monkeypatch):
+    """Each argument in turn lies on another device than the context (or on the host): refused before the library sees a
+    pointer; with all of them in place the library is reached (and refuses the missing context)."""
+    monkeypatch.setattr(dk, "_raw_stream", lambda d: 0)
+    call, sizes = CALLS[name]
+    ctx = SimpleNamespace(handle=None, device=device)
+    for wrong in range(len(sizes)):
+        tensors = [Elsewhere(other if i == wrong else device, *s) for i, s in enumerate(sizes)]
+        with pytest.raises(ValueError):
+            call(getattr(dk, name), ctx, tensors)
+    with pytest.raises(dk.DkError) as e:
+        call(getattr(dk, name), ctx, [Elsewhere(device, *s) for s in sizes])
+    assert e.value.status == INVALID
