@@ -44,3 +44,10 @@ def test_gradients_of_a_step(example):
         got = grads[k].double().cpu()
         assert float((got - leaf.grad).norm()) <= 5e-3 * float(leaf.grad.norm()), k
     net.ctx.close()
+
+
+def test_every_step_trains(example):
+    """The loss falls over the whole run and never reaches zero, where the gradients would be rounding noise."""
+    losses = example.main(steps=25)
+    fives = [sum(losses[i:i + 5]) / 5 for i in range(0, 25, 5)]
+    assert all(b < a for a, b in zip(fives, fives[1:])) and min(losses) > 0.1
