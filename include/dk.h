@@ -452,7 +452,10 @@ typedef struct {
   int32_t dtype;      /* of h, W, dh, dW                                          */
 } dk_xent;
 
+/* For both directions; dk_xent_fwd_workspace_bytes for programs that only score
+ * (a row against 128000 classes of 2048 features, fp32: 6 KiB instead of 1.07 GB). */
 DK_API dk_status dk_xent_workspace_bytes(const dk_xent* q, size_t* bytes);
+DK_API dk_status dk_xent_fwd_workspace_bytes(const dk_xent* q, size_t* bytes);
 
 /* h: [rows][d], W: [vocab][d], target: int64 [rows] on the device.
  *   l = <h[r], W[v]>,  lse[r] = log sum_v exp(l[v]),  loss[r] = lse[r] - l[target[r]]

@@ -123,6 +123,7 @@ def _signatures():
         "dk_group_norm_fwd": [vp, ctypes.POINTER(dk_norm), vp, vp, vp, vp, vp, vp],
         "dk_group_norm_bwd": [vp, ctypes.POINTER(dk_norm), vp, vp, vp, vp, vp, vp, vp, vp, vp],
         "dk_xent_workspace_bytes": [ctypes.POINTER(dk_xent), ctypes.POINTER(ctypes.c_size_t)],
+        "dk_xent_fwd_workspace_bytes": [ctypes.POINTER(dk_xent), ctypes.POINTER(ctypes.c_size_t)],
         "dk_linear_xent_fwd": [vp, ctypes.POINTER(dk_xent), vp, vp, vp, vp, vp, vp],
         "dk_linear_xent_bwd": [vp, ctypes.POINTER(dk_xent), vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp],
         "dk_ortho_workspace_bytes": [ctypes.POINTER(dk_ortho), ctypes.POINTER(ctypes.c_size_t)],
@@ -226,18 +227,19 @@ class Context:
         _check(lib().dk_field_workspace_bytes(ctypes.byref(p), ctypes.byref(n)), "dk_field_workspace_bytes")
         return n.value
 
-    def step_workspace_bytes(self, q) -> int:
-        """Workspace of a dk_norm, dk_xent or dk_ortho call."""
-        name = f"{type(q).__name__}_workspace_bytes"
+    def step_workspace_bytes(self, q, forward: bool = False) -> int:
+        """Workspace of a dk_norm, dk_xent or dk_ortho call (``forward=True``: of dk_linear_xent_fwd alone)."""
+        name = f"{type(q).__name__}{'_fwd' if forward and isinstance(q, dk_xent) else ''}_workspace_bytes"
         n = ctypes.c_size_t()
         _check(getattr(lib(), name)(ctypes.byref(q), ctypes.byref(n)), name)
         return n.value
 
-    def ensure_workspace(self, p, field: bool = False):
+    def ensure_workspace(self, p, field: bool = False, forward: bool = False):
         """Grows the torch-owned workspace to what `p` (a dk_problem, dk_norm, dk_xent or dk_ortho) needs and
-        registers it (``field=True``: what the finite-field calls need)."""
+        registers it (``field=True``: what the finite-field calls need; ``forward=True`` with a dk_xent: what
+        dk_linear_xent_fwd alone needs)."""
         if not isinstance(p, dk_problem):
-            need = self.step_workspace_bytes(p)
+            need = self.step_workspace_bytes(p, forward)
         else:
             need = self.field_workspace_bytes(p) if field else self.workspace_bytes(p)
         if self._ws is None or self._ws.numel() < need + 256:

@@ -553,6 +553,7 @@ xent_join_kernel(const float2* __restrict__ part, const float* __restrict__ tlog
 constexpr int kFewRows = 8;
 constexpr int kFewThreads = 256;
 constexpr size_t kFewSmem = 96 * 1024;               // two CTAs per SM
+constexpr int kFewCtas = 4 * kMaxSms;                // of a call, at most
 
 struct FewArgs {
   const void* h;
@@ -900,11 +901,26 @@ struct Plan {
 // slices of a product: every (tile, slice) has at most one pair's tile of fp32 sums
 constexpr size_t kPartBytes = (size_t)(kMaxSms / 2) * g16::TILE_M * BN * sizeof(float);
 
-Plan plan_xent(const dk_xent& q) {
+// Both sides of the rule, in us (rows x d, classes; here | tensor cores): fp32 1 x 4096, 1000 19.5 | 29.6; 3 x 1538, 6216
+// 36 | 56; 8 x 1024, 50257 69 | 204; 1 x 2048, 128000 198 | 746; but 1 x 12288, 64 36 | 28: a warp walks its row alone.  h takes
+// its room of shared memory in 1, 4 or 8 rows: 2 to 4 rows stop at 6144 features, 5 to 8 at 3072.
+// bf16, where the tensor cores read W as it is: 1 x 2048, 128000 108 | 144, but 4 rows 144 | 126.  A lone class has
+// probability one exactly: both directions have to see the same logit, so it takes the backward call's way.
+bool takes_few_rows(const dk_xent& q) {
+  if (q.vocab < 2 || q.d > 8192) return false;
+  if (q.dtype == DK_BF16) return q.rows == 1;
+  const size_t r = q.rows == 1 ? 1 : q.rows <= 4 ? 4 : kFewRows;
+  return q.rows <= kFewRows && r * (((size_t)q.d + 127) / 128 * 128) * sizeof(float) <= kFewSmem;
+}
+
+// `forward`: the room of dk_linear_xent_fwd alone, whose plan it is (a row against 128000 classes of 2048 features, fp32:
+// 6 KiB; both directions 1.07 GB)
+Plan plan_xent(const dk_xent& q, bool forward) {
   Plan p;
   p.f32 = q.dtype == DK_F32;
   p.dp = (q.d + 7) / 8 * 8;
-  p.copy_w = p.f32 || q.d % 8 != 0;
+  const bool few = forward && takes_few_rows(q);
+  p.copy_w = !few && (p.f32 || q.d % 8 != 0);
   p.copy_h = p.copy_w;
   const size_t es = p.f32 ? 4 : 2;             // bytes of one operand element, both terms
   const long long T = q.rows > 0 ? q.rows : 1;
@@ -918,23 +934,35 @@ Plan plan_xent(const dk_xent& q) {
     p.pieces = (int)((q.vocab + vp - 1) / vp);
   }
   p.vp = (int)((vp + 7) / 8 * 8);
-  size_t off = up(sizeof(Meta));
-  p.off_h = off; off += up((size_t)T * p.dp * es);
-  p.off_w = off; off += p.copy_w ? up((size_t)q.vocab * p.dp * es) : 0;
-  p.off_p = off; off += up((size_t)T * p.vp * es);
-  p.off_acc = off; off += p.pieces > 1 ? up((size_t)T * p.dp * 4) : 0;
-  p.off_part = off; off += up(kPartBytes);
+  size_t off = 0;
+  auto room = [&off](bool needed, size_t bytes) {
+    const size_t at = off;
+    off += needed ? up(bytes) : 0;
+    return at;
+  };
+  room(!forward, sizeof(Meta));
+  p.off_h = room(!forward || p.copy_h, (size_t)T * p.dp * es);
+  p.off_w = room(p.copy_w, (size_t)q.vocab * p.dp * es);
+  p.off_p = room(!forward, (size_t)T * p.vp * es);
+  p.off_acc = room(!forward && p.pieces > 1, (size_t)T * p.dp * 4);
+  p.off_part = room(!few, kPartBytes);
   // (maximum, sum) per row and the columns one thread finishes: BN/2 in the large tiles; in the small ones, of which
-  // there are at most kSmallCtas CTAs with SMALL rows each, two to a CTA
+  // there are at most kSmallCtas CTAs with SMALL rows each, two to a CTA; per row and CTA of the dot products
   size_t slots = ((size_t)q.vocab + BN / 2 - 1) / (BN / 2) * T;
   if (slots < (size_t)g16::kSmallCtas * 2 * g16::SMALL) slots = (size_t)g16::kSmallCtas * 2 * g16::SMALL;
-  p.off_slots = off; off += up(slots * sizeof(float2));
-  p.off_tl = off; off += up((size_t)T * sizeof(float));
+  if (few) slots = (size_t)kFewCtas * T;
+  p.off_slots = room(forward, slots * sizeof(float2));
+  p.off_tl = room(forward, (size_t)T * sizeof(float));
   // (inverse powers of two of the rows; those of W in whole tiles)
-  p.off_inv = off; off += p.f32 ? up(((size_t)T + 4 + (size_t)q.vocab + 256) * sizeof(float)) : 0;
-  p.off_class = off; off += p.f32 ? up(((size_t)q.vocab + 8) * sizeof(unsigned int)) : 0;
+  p.off_inv = room(forward && !few && p.f32, ((size_t)T + 4 + (size_t)q.vocab + 256) * sizeof(float));
+  p.off_class = room(!forward && p.f32, ((size_t)q.vocab + 8) * sizeof(unsigned int));
   p.total = off;
   return p;
+}
+
+size_t workspace_of(const dk_xent& q, bool forward) {
+  const size_t f = plan_xent(q, true).total, b = plan_xent(q, false).total;
+  return forward || f > b ? f : b;
 }
 
 dk_status check_xent(const dk_xent* q) {
@@ -1040,6 +1068,7 @@ dk_status few_rows(dk_ctx* ctx, const Plan& pl, char* ws, FewArgs a, float* loss
   const int classes = kFewThreads / 32 * V;
   long long grid = ((long long)a.vocab + classes - 1) / classes;
   if (grid > per_sm * ctx->sm_count) grid = per_sm * ctx->sm_count;
+  if (grid > kFewCtas) grid = kFewCtas;
   DK_CUDA_CHECK(launch_chained(kern, dim3((unsigned)grid), kFewThreads, smem, st, a));
   DK_CUDA_CHECK(launch_chained(xent_join_kernel, dim3((unsigned)((a.rows * 32 + kRowThreads - 1) / kRowThreads)), kRowThreads,
                                0, st, a.part, a.tlogit, a.target, (long long)a.rows, (int)grid, a.vocab, loss, lse,
@@ -1057,18 +1086,6 @@ dk_status few_rows(dk_ctx* ctx, const Plan& pl, char* ws, const FewArgs& a, floa
     return four ? few_rows<DT, VEC, 8, 4>(ctx, pl, ws, a, loss, lse, st) : few_rows<DT, VEC, 8, 1>(ctx, pl, ws, a, loss, lse, st);
   }
   return DK_ERR_UNSUPPORTED;
-}
-
-// Both sides of the rule, in us (rows x d, classes; here | tensor cores): fp32 1 x 4096, 1000 19.5 | 29.6; 3 x 1538, 6216
-// 36 | 56; 8 x 1024, 50257 69 | 204; 1 x 2048, 128000 198 | 746; but 1 x 12288, 64 36 | 28: a warp walks its row alone.  h takes
-// its room of shared memory in 1, 4 or 8 rows: 2 to 4 rows stop at 6144 features, 5 to 8 at 3072.
-// bf16, where the tensor cores read W as it is: 1 x 2048, 128000 108 | 144, but 4 rows 144 | 126.  A lone class has
-// probability one exactly: both directions have to see the same logit, so it takes the backward call's way.
-bool takes_few_rows(const dk_xent& q) {
-  if (q.vocab < 2 || q.d > 8192) return false;
-  if (q.dtype == DK_BF16) return q.rows == 1;
-  const size_t r = q.rows == 1 ? 1 : q.rows <= 4 ? 4 : kFewRows;
-  return q.rows <= kFewRows && r * (((size_t)q.d + 127) / 128 * 128) * sizeof(float) <= kFewSmem;
 }
 
 template <bool F32>
@@ -1188,10 +1205,10 @@ dk_status backward(Call& c, const void* W, const int64_t* target, const float* l
   return DK_OK;
 }
 
-dk_status begin(dk_ctx* ctx, const dk_xent* q, void* stream, Call* c) {
+dk_status begin(dk_ctx* ctx, const dk_xent* q, bool forward, void* stream, Call* c) {
   c->ctx = ctx;
   c->q = q;
-  c->pl = plan_xent(*q);
+  c->pl = plan_xent(*q, forward);
   c->ws = static_cast<char*>(ctx->ws);
   c->st = static_cast<cudaStream_t>(stream);
   return ctx->ws && ctx->ws_bytes >= c->pl.total ? DK_OK : DK_ERR_WORKSPACE;
@@ -1208,7 +1225,15 @@ dk_status dk_xent_workspace_bytes(const dk_xent* q, size_t* bytes) {
   if (!bytes) return DK_ERR_INVALID_ARG;
   dk_status s = check_xent(q);
   if (s != DK_OK) return s;
-  *bytes = plan_xent(*q).total;
+  *bytes = workspace_of(*q, false);
+  return DK_OK;
+}
+
+dk_status dk_xent_fwd_workspace_bytes(const dk_xent* q, size_t* bytes) {
+  if (!bytes) return DK_ERR_INVALID_ARG;
+  dk_status s = check_xent(q);
+  if (s != DK_OK) return s;
+  *bytes = workspace_of(*q, true);
   return DK_OK;
 }
 
@@ -1223,7 +1248,7 @@ dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const
       !aligned_to(lse, 16))
     return DK_ERR_INVALID_ARG;
   Call c;
-  s = begin(ctx, q, stream, &c);
+  s = begin(ctx, q, true, stream, &c);
   if (s != DK_OK) return s;
   OnDevice dev(ctx->device);
   if (!dev.ok) return DK_ERR_CUDA;
@@ -1263,7 +1288,7 @@ dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const
     return DK_OK;
   }
   Call c;
-  s = begin(ctx, q, stream, &c);
+  s = begin(ctx, q, false, stream, &c);
   if (s != DK_OK) return s;
   // (slices of a product that are joined by a kernel of their own are counted where that is launched)
   ProfScope ps(ctx, DK_KERNEL_OTHER, c.pl.f32 ? 2 + 4 * c.pl.pieces : 1 + 3 * c.pl.pieces, c.st);

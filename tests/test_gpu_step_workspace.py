@@ -62,3 +62,34 @@ def test_guard_behind_the_workspace(q):
     assert all(bool(torch.isfinite(o).all()) for o in out)
     assert bool((buf[off + need:] == 0xA5).all()) and bool((buf[:off] == 0xA5).all())
     ctx.close()
+
+
+@pytest.mark.parametrize("rows,d,vocab,dtype", [(1, 2048, 128000, 0), (1, 2047, 9000, 1), (8, 1024, 5000, 0), (4, 6144, 300, 0),
+                                                (64, 512, 1000, 0), (9, 30000, 40, 0), (9, 60000, 40, 1), (2000, 77, 30001, 0),
+                                                (700, 2000, 300, 1), (5000, 64, 20000, 1)])
+def test_scoring_in_its_own_workspace(rows, d, vocab, dtype):
+    """The forward call alone, in a workspace of dk_xent_fwd_workspace_bytes: the bits it has in the larger one, nothing
+    written behind; the backward call refuses that workspace where it is too small."""
+    ctx, q = dk.Context(0), dk.dk_xent(rows, d, vocab, dtype)
+    tt = torch.bfloat16 if dtype == dk.DK_BF16 else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(2)
+    h, W = torch.randn((rows, d), generator=g, device="cuda").to(tt), torch.randn((vocab, d), generator=g, device="cuda").to(tt)
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    ctx.ensure_workspace(q)
+    want = [torch.empty(rows, device="cuda") for _ in range(2)]
+    dk.dk_linear_xent_fwd(ctx, q, h, W, t, *want)
+    torch.cuda.synchronize()
+    need = ctx.step_workspace_bytes(q, forward=True)
+    buf = torch.full((need + GUARD + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    off = (-buf.data_ptr()) % 256
+    assert dk.lib().dk_set_workspace(ctx.handle, ctypes.c_void_p(buf.data_ptr() + off), need) == 0
+    got = [torch.full((rows,), float("nan"), device="cuda") for _ in range(2)]
+    dk.dk_linear_xent_fwd(ctx, q, h, W, t, *got)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert bool((buf[off + need:] == 0xA5).all()) and bool((buf[:off] == 0xA5).all())
+    if need < ctx.step_workspace_bytes(q):
+        with pytest.raises(dk.DkError) as e:
+            dk.dk_linear_xent_bwd(ctx, q, h, W, t, got[1], None, 1.0, torch.empty_like(h), torch.empty_like(W))
+        assert e.value.status == 4                              # DK_ERR_WORKSPACE
+    ctx.close()

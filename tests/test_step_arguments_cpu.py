@@ -142,3 +142,23 @@ def test_tensors_of_another_device_are_refused(name, device, other, monkeypatch)
     with pytest.raises(dk.DkError) as e:
         call(getattr(dk, name), ctx, [Elsewhere(device, *s) for s in sizes])
     assert e.value.status == INVALID
+
+
+@pytest.mark.parametrize("rows,d,vocab,dtype", [(1, 2048, 128000, 0), (1, 2048, 128000, 1), (8, 1024, 50257, 0), (64, 512, 1000, 0),
+                                                (2047, 1024, 50257, 1), (300, 100, 5001, 1), (0, 1, 1, 0), (1, 30000, 40, 0)])
+def test_scoring_needs_no_more_than_both_directions(rows, d, vocab, dtype):
+    q, n = dk.dk_xent(rows, d, vocab, dtype), ctypes.c_size_t()
+    assert dk.lib().dk_xent_fwd_workspace_bytes(ctypes.byref(q), ctypes.byref(n)) == 0
+    es = 4 if dtype == 0 else 2
+    assert n.value % 256 == 0 and n.value <= size(q)[1]
+    if rows <= 8 and 1 <= rows and d <= 2048 and dtype == 0 or rows == 1 and d <= 8192:
+        assert n.value < 64 << 10                               # dot products: nothing is laid out anew
+    if dtype == 1 and d % 8 == 0:
+        assert n.value < (64 << 20) + 8 * rows * vocab // 128 + 16 * rows      # operands are read in place
+    assert n.value < (64 << 20) + 2 * es * (rows + vocab) * (d + 8) + 8 * rows * (vocab // 128 + 1)
+
+
+def test_scoring_workspace_refusals():
+    n = ctypes.c_size_t()
+    assert dk.lib().dk_xent_fwd_workspace_bytes(None, ctypes.byref(n)) == INVALID
+    assert dk.lib().dk_xent_fwd_workspace_bytes(ctypes.byref(dk.dk_xent(8, 0, 8, 0)), ctypes.byref(n)) == SHAPE
