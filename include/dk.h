@@ -467,14 +467,16 @@ DK_API dk_status dk_xent_fwd_workspace_bytes(const dk_xent* q, size_t* bytes);
  * bits down to 2^-17 of the row's largest magnitude, an absolute error of 2^-39
  * of that magnitude below).  A token or a few contract in fp32 instead, reading W
  * once: one row up to d = 8192, with DK_F32 also 2 to 4 rows up to d = 6144 and 5
- * to 8 up to d = 3072, on 2 classes or more.  Needs the workspace. */
+ * to 8 up to d = 3072, on 2 classes or more (in the backward call likewise).
+ * Needs the workspace. */
 DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const void* W,
                                     const int64_t* target, float* loss, float* lse, void* stream);
 
 /* Gradients of scale * sum_r dloss[r]*loss[r] (dloss: fp32 [rows], nullable = 1):
  *   p[r][v] = scale*dloss[r]*(exp(l[v] - lse[r]) - [v == target[r]]), 0 for rows left out
  *   dh = p.W,  dW = p^T.h
- * lse: from the forward call.  With DK_BF16 p is rounded to bf16 for the two
+ * lse: from the forward call (its rounding, 2^-24 of it, is what p = exp(..) - 1
+ * at the target of a sure row is exact to).  With DK_BF16 p is rounded to bf16 for the two
  * products.  With DK_F32 h, W and p enter as two fp16 terms each, 22 bits: h and
  * W under one power of two each (of the whole tensor: the products sum over their
  * rows; 22 bits down to 2^-17 of the tensor's largest finite magnitude, an

@@ -19,7 +19,7 @@
 // p costs 3.4 us of 48 (64 x 512, 1000 classes), 0.2 ms of 2.65 (4000 x 768, 32000 classes: 1 GB at 5.2 TB/s), and a fifth
 // of the call where features are few (8192 x 256, 20000 classes).
 //
-// Forward calls of one or a few rows take dot products instead (xent_few_rows_kernel).
+// One or a few rows take dot products instead for their logits, in both directions (xent_few_rows_kernel).
 //
 // Measured: 4096 x 4096, 128000 classes, bf16, both directions 14.5 ms (1.19 PFLOP/s over its four products, 84 % of the
 // library's sustained rate); 2047 x 1024, 50257 classes 0.84 ms; 256 x 4096, 1000 classes, fp32, forward 28.5 us; 64 x
@@ -562,6 +562,7 @@ struct FewArgs {
   float2* part;                // [CTAs][rows]
   float* tlogit;
   int rows, d, dpad, vocab;    // dpad: d rounded up to the 32*VEC elements of a warp's step
+  RowArgs r;                   // backward: of the piece (W, vocab: its classes)
 };
 
 // VEC elements from element e on, in one access
@@ -591,7 +592,11 @@ __device__ __forceinline__ void load_few(const void* p, size_t e, float (&v)[VEC
   }
 }
 
-template <int DT, int VEC, int R, int V>
+// P: the backward call's p instead, from logits of the very same bits.  (A logit formed in another way differs from the
+// one in lse by some 2^-22 of its terms, which is all that p has at the target where the model is sure: 4 x 256, 1000
+// classes, dh off by 7e-5 of itself at p = 0.986 and by 2.8 times itself at 1 - 2e-6; now 1e-5 and 0.2, which is lse's
+// rounding.)
+template <int DT, int VEC, int R, int V, bool P>
 __global__ void __launch_bounds__(kFewThreads) xent_few_rows_kernel(const FewArgs q) {
   chained_launch();
   extern __shared__ float hs[];                      // [R][dpad]
@@ -627,6 +632,10 @@ __global__ void __launch_bounds__(kFewThreads) xent_few_rows_kernel(const FewArg
   const int mine = lane >> SHIFT, myv = mine / R, myr = mine % R;
   const long long t = myr < q.rows ? q.target[myr] : -1;
   float m = -INFINITY, s = 0.f;
+  const bool keep = P && !left_out(t, q.r.vocab), writes = myr < q.rows && (lane & ((1 << SHIFT) - 1)) == 0;
+  const float lse = keep ? q.r.lse[myr] : 0.f;
+  float g = keep ? (q.r.dloss != nullptr ? q.r.dloss[myr] * q.r.scale : q.r.scale) : 0.f;
+  if constexpr (P && DT == DK_F32) g *= pow2(scale_exp(*q.r.gmax));
   for (int v0 = (blockIdx.x * (kFewThreads / 32) + warp) * V; v0 < q.vocab; v0 += gridDim.x * (kFewThreads / 32) * V) {
     float x[N];
 #pragma unroll
@@ -678,7 +687,21 @@ __global__ void __launch_bounds__(kFewThreads) xent_few_rows_kernel(const FewArg
       }
     }
     const float l = x[0];
-    if (v0 + myv < q.vocab) {
+    if constexpr (P) {
+      const int v = v0 + myv;
+      if (v < q.vocab && writes) {
+        const float p = keep ? p_value(l, lse, t - q.r.v0 == v, g) : 0.f;
+        const size_t to = (size_t)myr * q.r.pitch + v;
+        if constexpr (DT == DK_F32) {
+          const unsigned int bits = __float_as_uint(p), most = magnitude(bits);
+          static_cast<uint16_t*>(q.r.hi)[to] = (uint16_t)(bits >> 16);
+          static_cast<uint16_t*>(q.r.lo)[to] = (uint16_t)(bits & 0xffffu);
+          if (most > __ldcg(q.r.class_max + v)) atomicMax(q.r.class_max + v, most);
+        } else {
+          static_cast<__nv_bfloat16*>(q.r.hi)[to] = __float2bfloat16_rn(p);
+        }
+      }
+    } else if (v0 + myv < q.vocab) {
       if (v0 + myv == t) q.tlogit[myr] = l;
       const float n = fmaxf(m, l);
       if (n != -INFINITY) s = s * __expf(m - n) + __expf(l - n);
@@ -686,17 +709,19 @@ __global__ void __launch_bounds__(kFewThreads) xent_few_rows_kernel(const FewArg
       m = n;
     }
   }
-  // the V lanes of a row, then the warps, in order
+  if constexpr (!P) {
+    // the V lanes of a row, then the warps, in order
 #pragma unroll
-  for (int o = R << SHIFT; o < 32; o <<= 1)
-    join_pair(m, s, __shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
-  if (myv == 0 && (lane & ((1 << SHIFT) - 1)) == 0) joined[warp][myr] = make_float2(m, s);
-  __syncthreads();
-  if ((int)threadIdx.x < q.rows) {
-    float2 a = joined[0][threadIdx.x];
+    for (int o = R << SHIFT; o < 32; o <<= 1)
+      join_pair(m, s, __shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
+    if (myv == 0 && (lane & ((1 << SHIFT) - 1)) == 0) joined[warp][myr] = make_float2(m, s);
+    __syncthreads();
+    if ((int)threadIdx.x < q.rows) {
+      float2 a = joined[0][threadIdx.x];
 #pragma unroll
-    for (int i = 1; i < kFewThreads / 32; ++i) join_pair(a.x, a.y, joined[i][threadIdx.x].x, joined[i][threadIdx.x].y);
-    q.part[(size_t)blockIdx.x * q.rows + threadIdx.x] = a;
+      for (int i = 1; i < kFewThreads / 32; ++i) join_pair(a.x, a.y, joined[i][threadIdx.x].x, joined[i][threadIdx.x].y);
+      q.part[(size_t)blockIdx.x * q.rows + threadIdx.x] = a;
+    }
   }
 }
 
@@ -1053,13 +1078,11 @@ dk_status prepare(Call& c, const void* h, const void* W, const int64_t* target, 
   return DK_OK;
 }
 
-template <int DT, int VEC, int R, int V>
-dk_status few_rows(dk_ctx* ctx, const Plan& pl, char* ws, FewArgs a, float* loss, float* lse, cudaStream_t st) {
+template <int DT, int VEC, int R, int V, bool P>
+dk_status few_rows(dk_ctx* ctx, FewArgs a, float* loss, float* lse, cudaStream_t st) {
   a.dpad = (a.d + 32 * VEC - 1) / (32 * VEC) * (32 * VEC);
-  a.part = reinterpret_cast<float2*>(ws + pl.off_slots);
-  a.tlogit = reinterpret_cast<float*>(ws + pl.off_tl);
   const size_t smem = (size_t)R * a.dpad * sizeof(float);
-  auto kern = xent_few_rows_kernel<DT, VEC, R, V>;
+  auto kern = xent_few_rows_kernel<DT, VEC, R, V, P>;
   static SmemLimit limit;
   const dk_status r = allow_smem(limit, ctx->device, kern, (int)kFewSmem);
   if (r != DK_OK) return r;
@@ -1070,22 +1093,38 @@ dk_status few_rows(dk_ctx* ctx, const Plan& pl, char* ws, FewArgs a, float* loss
   if (grid > per_sm * ctx->sm_count) grid = per_sm * ctx->sm_count;
   if (grid > kFewCtas) grid = kFewCtas;
   DK_CUDA_CHECK(launch_chained(kern, dim3((unsigned)grid), kFewThreads, smem, st, a));
-  DK_CUDA_CHECK(launch_chained(xent_join_kernel, dim3((unsigned)((a.rows * 32 + kRowThreads - 1) / kRowThreads)), kRowThreads,
-                               0, st, a.part, a.tlogit, a.target, (long long)a.rows, (int)grid, a.vocab, loss, lse,
-                               device_status_word(ctx)));
+  if (!P)
+    DK_CUDA_CHECK(launch_chained(xent_join_kernel, dim3((unsigned)((a.rows * 32 + kRowThreads - 1) / kRowThreads)),
+                                 kRowThreads, 0, st, a.part, a.tlogit, a.target, (long long)a.rows, (int)grid, a.vocab, loss,
+                                 lse, device_status_word(ctx)));
   return cudaGetLastError() == cudaSuccess ? DK_OK : DK_ERR_CUDA;
 }
 
-template <int DT, int VEC>
-dk_status few_rows(dk_ctx* ctx, const Plan& pl, char* ws, const FewArgs& a, float* loss, float* lse, cudaStream_t st) {
+template <int DT, int VEC, int R, bool P>
+dk_status few_rows(dk_ctx* ctx, const FewArgs& a, float* loss, float* lse, cudaStream_t st) {
   // four classes at a time where each warp still has some; one where there would be idle SMs
   const bool four = (long long)a.vocab >= 4LL * 4 * (kFewThreads / 32) * ctx->sm_count;
-  if (a.rows == 1) return four ? few_rows<DT, VEC, 1, 4>(ctx, pl, ws, a, loss, lse, st) : few_rows<DT, VEC, 1, 1>(ctx, pl, ws, a, loss, lse, st);
+  return four ? few_rows<DT, VEC, R, 4, P>(ctx, a, loss, lse, st) : few_rows<DT, VEC, R, 1, P>(ctx, a, loss, lse, st);
+}
+
+// (what either direction takes follows from the call's sizes alone, so that both form a row's logits alike)
+template <int DT, int VEC, bool P>
+dk_status few_rows(dk_ctx* ctx, const FewArgs& a, float* loss, float* lse, cudaStream_t st) {
+  if (a.rows == 1) return few_rows<DT, VEC, 1, P>(ctx, a, loss, lse, st);
   if constexpr (DT == DK_F32) {
-    if (a.rows <= 4) return four ? few_rows<DT, VEC, 4, 4>(ctx, pl, ws, a, loss, lse, st) : few_rows<DT, VEC, 4, 1>(ctx, pl, ws, a, loss, lse, st);
-    return four ? few_rows<DT, VEC, 8, 4>(ctx, pl, ws, a, loss, lse, st) : few_rows<DT, VEC, 8, 1>(ctx, pl, ws, a, loss, lse, st);
+    if (a.rows <= 4) return few_rows<DT, VEC, 4, P>(ctx, a, loss, lse, st);
+    return few_rows<DT, VEC, 8, P>(ctx, a, loss, lse, st);
   }
   return DK_ERR_UNSUPPORTED;
+}
+
+template <bool P>
+dk_status few_rows(dk_ctx* ctx, bool f32, const FewArgs& a, float* loss, float* lse, cudaStream_t st) {
+  if (f32)
+    return a.d % 4 == 0 ? few_rows<DK_F32, 4, P>(ctx, a, loss, lse, st) : few_rows<DK_F32, 1, P>(ctx, a, loss, lse, st);
+  return a.d % 8 == 0   ? few_rows<DK_BF16, 8, P>(ctx, a, loss, lse, st)
+         : a.d % 2 == 0 ? few_rows<DK_BF16, 2, P>(ctx, a, loss, lse, st)
+                        : few_rows<DK_BF16, 1, P>(ctx, a, loss, lse, st);
 }
 
 template <bool F32>
@@ -1117,7 +1156,7 @@ dk_status forward(Call& c, const int64_t* target, float* loss, float* lse) {
 }
 
 template <bool F32>
-dk_status backward(Call& c, const void* W, const int64_t* target, const float* lse, const float* dloss, float scale,
+dk_status backward(Call& c, const void* h, const void* W, const int64_t* target, const float* lse, const float* dloss, float scale,
                    void* dh, void* dW) {
   constexpr int NP = F32 ? 3 : 1;
   const dk_xent& q = *c.q;
@@ -1144,7 +1183,11 @@ dk_status backward(Call& c, const void* W, const int64_t* target, const float* l
     g16::Tiling t = g16::plan(T, nv, q.d, 1, false, sms, NP);
     Params p = gemm_params(t, T, nv, F32);
     dk_status s;
-    if (!t.cs && t.ksplit > 1) {
+    if (takes_few_rows(q)) {
+      const FewArgs a = {h, static_cast<const char*>(W) + (size_t)v0 * q.d * es, target, nullptr, nullptr, (int)T, q.d, 0, nv, r};
+      s = few_rows<true>(c.ctx, F32, a, nullptr, nullptr, c.st);
+      if (s != DK_OK) return s;
+    } else if (!t.cs && t.ksplit > 1) {
       const int pitch = (nv + 3) / 4 * 4;
       s = g16::launch<NP, false, false, BN>(c.ctx, c.h, w, p, g16::EpiPartial{c.part(), pitch}, c.st);
       if (s != DK_OK) return s;
@@ -1255,13 +1298,9 @@ dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h, const
   const bool few = takes_few_rows(*q);
   ProfScope ps(ctx, DK_KERNEL_OTHER, 2 + (!few && c.pl.copy_w ? 1 : 0), c.st);
   if (few) {
-    const FewArgs a = {h, W, target, nullptr, nullptr, (int)q->rows, q->d, 0, q->vocab};
-    if (c.pl.f32)
-      return q->d % 4 == 0 ? few_rows<DK_F32, 4>(ctx, c.pl, c.ws, a, loss, lse, c.st)
-                           : few_rows<DK_F32, 1>(ctx, c.pl, c.ws, a, loss, lse, c.st);
-    return q->d % 8 == 0   ? few_rows<DK_BF16, 8>(ctx, c.pl, c.ws, a, loss, lse, c.st)
-           : q->d % 2 == 0 ? few_rows<DK_BF16, 2>(ctx, c.pl, c.ws, a, loss, lse, c.st)
-                           : few_rows<DK_BF16, 1>(ctx, c.pl, c.ws, a, loss, lse, c.st);
+    const FewArgs a = {h, W, target, reinterpret_cast<float2*>(c.ws + c.pl.off_slots),
+                       reinterpret_cast<float*>(c.ws + c.pl.off_tl), (int)q->rows, q->d, 0, q->vocab, {}};
+    return few_rows<false>(ctx, c.pl.f32, a, loss, lse, c.st);
   }
   if (c.pl.f32) {
     s = prepare<true>(c, h, W, target, nullptr, 1.f, false);
@@ -1294,10 +1333,10 @@ dk_status dk_linear_xent_bwd(dk_ctx* ctx, const dk_xent* q, const void* h, const
   ProfScope ps(ctx, DK_KERNEL_OTHER, c.pl.f32 ? 2 + 4 * c.pl.pieces : 1 + 3 * c.pl.pieces, c.st);
   if (c.pl.f32) {
     s = prepare<true>(c, h, W, target, dloss, scale, true);
-    return s == DK_OK ? backward<true>(c, W, target, lse, dloss, scale, dh, dW) : s;
+    return s == DK_OK ? backward<true>(c, h, W, target, lse, dloss, scale, dh, dW) : s;
   }
   s = prepare<false>(c, h, W, target, dloss, scale, true);
-  return s == DK_OK ? backward<false>(c, W, target, lse, dloss, scale, dh, dW) : s;
+  return s == DK_OK ? backward<false>(c, h, W, target, lse, dloss, scale, dh, dW) : s;
 }
 
 }  // extern "C"

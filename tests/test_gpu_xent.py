@@ -423,3 +423,28 @@ def test_limits_of_the_dot_products(ctx, dtype, rows, d, few):
     dk.dk_linear_xent_fwd(ctx, q, h, W, t, loss, lse)
     launches = dk.dk_profile_read(ctx)["other"][2]
     assert launches == (2 if few or (dtype == "bf16" and d % 8 == 0) else 3)
+
+
+@pytest.mark.parametrize("dtype,rows", [("f32", 1), ("f32", 3), ("f32", 8), ("bf16", 1)])
+@pytest.mark.parametrize("margin", [5.0, 10.0, 15.0, 20.0])
+@pytest.mark.parametrize("d,vocab", [(256, 1000), (255, 3001), (1024, 30000)])
+def test_sure_rows(ctx, dtype, rows, margin, d, vocab):
+    """Rows whose target's probability is almost one: what is left of p there is a difference.  Both directions form a
+    row's logits alike, so what p misses at the target is lse's rounding and exp's (2^-22), never the logits' own error."""
+    tt = TYPES[dtype][1]
+    g = torch.Generator(device="cuda").manual_seed(27)
+    W = torch.randn((vocab, d), generator=g, device="cuda") / d ** 0.5
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    h = 0.5 * torch.randn((rows, d), generator=g, device="cuda") + W[t] / W[t].norm(dim=1, keepdim=True) ** 2 * (margin + 6)
+    h, W = h.to(tt), W.to(tt)
+    _, lse, dh, _ = call(ctx, h, W, t, TYPES[dtype][0])
+    z = h.double() @ W.double().T
+    p = torch.exp(z - torch.logsumexp(z, dim=1)[:, None])
+    at = torch.arange(rows, device="cuda")
+    p[at, t] = 0
+    p[at, t] = -p.sum(dim=1)                                   # (exactly, where 1 - p would cancel)
+    want = p @ W.double()
+    off = 2.0 ** -22 + 2.0 ** -24 * lse.double().abs()
+    rel = 2.0 ** -18 * float((h.double().abs() @ W.double().abs().T).max()) + (2.0 ** -7 if dtype == "bf16" else 2.0 ** -17)
+    bound = 2 * off * W.double()[t].norm(dim=1) + rel * (p.abs() @ W.double().abs()).norm(dim=1)
+    assert bool(((dh.double() - want).norm(dim=1) <= bound).all())
