@@ -685,7 +685,7 @@ __device__ __forceinline__ void put_piece32(float* dst, const float4& u, int cou
 template <int NH>
 __device__ __forceinline__ void store_terms(const float (&v)[NH], char* sm, __half* hi, __half* lo, long long pitch, int rows,
                                             int cols) {
-  constexpr int W = NH <= 64 ? NH : 32;            // (64 of 128 values at a time spill)
+  constexpr int W = NH <= 64 ? NH : 32;            // (of 128: 32 at a time spill 52 bytes a thread, 64 at a time 640)
 #pragma unroll
   for (int c0 = 0; c0 < NH; c0 += W) {
     uint32_t h[W / 2], l[W / 2];
@@ -731,7 +731,9 @@ struct Tiling {
 
 // Cost in cycles of either way, from what was measured: a stage (64 contraction elements) of the pair's tile takes 512
 // cycles per product, of the small tile 256, but what binds the small tile is shared memory, where its operands arrive
-// and every product reads them again (measured as 16 KiB per operand plane at 50 bytes per cycle); some 9000 cycles go
+// and every product reads them again (taken as 16 KiB per operand plane at 50 bytes per cycle, 1311 cycles for three
+// products; with A's rows read once for both planes of B the slope over the contraction is 1430 to 1520 cycles where 128 to
+// 144 CTAs are at work, 64 KiB each through L2); some 9000 cycles go
 // to a launch's start, fill and epilogue, 6000 more to joining a cluster's slices, 24000 to the partial sums' way through
 // global memory and a second kernel.  Clusters of four and eight do not tile the GPCs: 33 and 15 of them are resident at
 // once on 148 SMs.  `narrow`: the caller has a kernel of three products for pair tiles of 256 x 128 too (the update's X:

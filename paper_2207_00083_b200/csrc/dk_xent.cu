@@ -16,14 +16,14 @@
 // 2^-e_v on the class's row of W, so that dh = (p 2^e).(2^-e W) needs nothing undone; dW's epilogue undoes 2^e_v row by
 // row.  200 x 64, 600 classes whose largest probability falls from 6e-3 to 3e-17: each row of dW is off by 2e-7 to 5e-6 of
 // itself, as in plain fp32 (one power of two for all: 1e-4 at 1e-8, 1e-1 at 1e-11, all of it below 1e-12).  The pass over
-// p costs 3.4 us of 48 (64 x 512, 1000 classes), 0.2 ms of 2.65 (4000 x 768, 32000 classes: 1 GB at 5.2 TB/s), and a fifth
+// p costs 3.4 us of 48 (64 x 512, 1000 classes), 0.16 ms of 2.63 (4000 x 768, 32000 classes: 1 GB at 6.5 TB/s), and a fifth
 // of the call where features are few (8192 x 256, 20000 classes).
 //
 // One or a few rows take dot products instead for their logits, in both directions (xent_few_rows_kernel).
 //
-// Measured: 4096 x 4096, 128000 classes, bf16, both directions 14.5 ms (1.19 PFLOP/s over its four products, 84 % of the
-// library's sustained rate); 2047 x 1024, 50257 classes 0.84 ms; 256 x 4096, 1000 classes, fp32, forward 28.5 us; 64 x
-// 512, both directions, 46 us (eight launches of 4 to 10 us).
+// Measured: 4096 x 4096, 128000 classes, bf16, both directions 14.7 ms (1.17 PFLOP/s over its four products, 83 % of the
+// library's sustained rate); 2047 x 1024, 50257 classes 0.84 ms; 4000 x 768, 32000 classes, fp32 2.63 ms; 256 x 4096, 1000
+// classes, fp32, forward 28 us; 64 x 512, both directions, 48.5 us (nine launches of 4 to 10 us).
 #include <math.h>
 
 #include "dk_gemm16.cuh"
@@ -912,7 +912,7 @@ xent_slices_grad_kernel(const float* __restrict__ part, int ks, long long rows, 
 // ---------------------------------------------------------------------------
 constexpr int BN = 256;
 // Room for p of one piece (both terms).  Wider pieces mean fewer readings and writings of dh's sums and fewer launches:
-// 4096x4096x128000 bf16 14.5 ms with 128 MiB, 14.3 with 256, 14.1 with 512; 4000x768x32000 fp32 3.15, 2.81, 2.70 ms.
+// 4096x4096x128000 bf16 15.2 ms with 128 MiB, 14.8 with 256, 14.7 with 512; 4000x768x32000 fp32 2.82, 2.63, 2.58 ms.
 constexpr long long kPieceBytes = 256LL << 20;
 
 size_t up(size_t v) { return (v + 1023) / 1024 * 1024; }
@@ -926,10 +926,10 @@ struct Plan {
 // slices of a product: every (tile, slice) has at most one pair's tile of fp32 sums
 constexpr size_t kPartBytes = (size_t)(kMaxSms / 2) * g16::TILE_M * BN * sizeof(float);
 
-// Both sides of the rule, in us (rows x d, classes; here | tensor cores): fp32 1 x 4096, 1000 19.5 | 29.6; 3 x 1538, 6216
-// 36 | 56; 8 x 1024, 50257 69 | 204; 1 x 2048, 128000 198 | 746; but 1 x 12288, 64 36 | 28: a warp walks its row alone.  h takes
+// Both sides of the rule, in us (rows x d, classes; here | tensor cores): fp32 1 x 4096, 1000 19.5 | 29.7; 3 x 1538, 6216
+// 34 | 55; 8 x 1024, 50257 69 | 200; 1 x 2048, 128000 198 | 752; but 1 x 12288, 64 36 | 26: a warp walks its row alone.  h takes
 // its room of shared memory in 1, 4 or 8 rows: 2 to 4 rows stop at 6144 features, 5 to 8 at 3072.
-// bf16, where the tensor cores read W as it is: 1 x 2048, 128000 108 | 144, but 4 rows 144 | 126.  A lone class has
+// bf16, where the tensor cores read W as it is: 1 x 2048, 128000 108 | 146, but 4 rows 144 | 124.  A lone class has
 // probability one exactly: both directions have to see the same logit, so it takes the backward call's way.
 bool takes_few_rows(const dk_xent& q) {
   if (q.vocab < 2 || q.d > 8192) return false;
