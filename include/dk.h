@@ -476,8 +476,8 @@ DK_API dk_status dk_linear_xent_fwd(dk_ctx* ctx, const dk_xent* q, const void* h
  *   p[r][v] = scale*dloss[r]*(exp(l[v] - lse[r]) - [v == target[r]]), 0 for rows left out
  *   dh = p.W,  dW = p^T.h
  * lse: from the forward call (its rounding, 2^-24 of it, is what p = exp(..) - 1
- * at the target of a sure row is exact to).  With DK_BF16 p is rounded to bf16 for the two
- * products.  With DK_F32 h, W and p enter as two fp16 terms each, 22 bits: h and
+ * at the target of a sure row is exact to).  With DK_BF16 p without `scale` is rounded to bf16
+ * for the two products.  With DK_F32 h, W and p enter as two fp16 terms each, 22 bits: h and
  * W under one power of two each (of the whole tensor: the products sum over their
  * rows; 22 bits down to 2^-17 of the tensor's largest finite magnitude, an
  * absolute error of 2^-39 of it below), p under one of each class.  So a row of

@@ -333,7 +333,7 @@ struct RowArgs {
   const int64_t* target;
   const float* lse;
   const float* dloss;
-  float scale;
+  float scale;                 // (bf16: 1)
   int vocab, v0;               // first class of the piece
   const unsigned int* gmax;    // fp32: p is taken under this magnitude's power of two
   unsigned int* class_max;     // fp32: of the piece, largest magnitudes of p
@@ -365,7 +365,8 @@ __device__ __forceinline__ void store_halves(const float (&v)[NH], char* sm, uin
 
 // backward epilogue: p of this piece.  With bf16 tensors p is rounded to bf16: one product each for dh and dW instead of
 // two, and the results are rounded to as many bits; what it adds shows beside that rounding as 1 to 4 % of the error
-// (2047 x 1024 on 50257 classes, 4096 x 4096 on 128000).
+// (2047 x 1024 on 50257 classes, 4096 x 4096 on 128000).  `scale` is left to the gradients' epilogues: -1 at a target that
+// is not predicted at all is exact, -1/15 is not, and every row's error would be the same (0.4 % of the gradients).
 template <bool F32>
 struct EpiP {
   static constexpr bool kAhead = false;
@@ -426,7 +427,7 @@ struct EpiP {
   }
 };
 
-// gradients: out = alpha*product (+ what earlier pieces left in `acc`), as fp32 in `acc` or rounded in `out`
+// gradients: out = alpha*product (+ what earlier pieces left in `accum`), as fp32 in `accum` or rounded in `out`
 template <bool F32>
 struct EpiGrad {
   static constexpr bool kAhead = false;
@@ -434,6 +435,7 @@ struct EpiGrad {
   float* accum;                // fp32 [M][pitch_acc]
   long long pitch, pitch_acc;
   int add;                     // accum holds earlier pieces
+  float alpha;                 // bf16: what p was formed without
   Undo undo;
   const unsigned int* class_max;      // fp32, dW: of the rows; null: no power of two of their own
   __device__ __forceinline__ float undo_class(long long row) const {
@@ -449,6 +451,9 @@ struct EpiGrad {
       const float fc = undo_class(min(row, p.M - 1));      // (one after the other: together they may leave fp32's range)
 #pragma unroll
       for (int j = 0; j < NH; ++j) acc[j] = acc[j] * fc * f0 * f1;
+    } else {
+#pragma unroll
+      for (int j = 0; j < NH; ++j) acc[j] *= alpha;
     }
     const int rows = p.M - row0, cols = p.N - col0;
     const size_t to = (size_t)row0 * pitch + col0;
@@ -898,7 +903,8 @@ xent_slices_grad_kernel(const float* __restrict__ part, int ks, long long rows, 
        i += (long long)gridDim.x * blockDim.x) {
     const long long row = i / n;
     const int c = (int)(i - row * n);
-    float v = slice_sum(part, (size_t)row * pitch + c, slice, ks) * e.undo_class(row) * f0 * f1;
+    float v = slice_sum(part, (size_t)row * pitch + c, slice, ks);
+    v = F32 ? v * e.undo_class(row) * f0 * f1 : v * e.alpha;
     float* a = e.accum + row * e.pitch_acc + c;
     if (e.add) v += *a;
     if (e.out == nullptr) *a = v;
@@ -1177,7 +1183,7 @@ dk_status backward(Call& c, const void* h, const void* W, const int64_t* target,
     w.lo = static_cast<const __half*>(c.w.lo) + (size_t)v0 * pl.dp;
     w.rows = nv;
     const Operand pop{ph, pl_lo, T, nv, pitch_p, 0};
-    const RowArgs r{target, lse, dloss, scale, q.vocab, v0, &c.meta()->gmax, c.class_max() + v0, ph, pl_lo, pitch_p};
+    const RowArgs r{target, lse, dloss, F32 ? scale : 1.f, q.vocab, v0, &c.meta()->gmax, c.class_max() + v0, ph, pl_lo, pitch_p};
 
     // p of the piece
     g16::Tiling t = g16::plan(T, nv, q.d, 1, false, sms, NP);
@@ -1213,7 +1219,7 @@ dk_status backward(Call& c, const void* h, const void* W, const int64_t* target,
 
     // dh += p.W
     const bool last = i + 1 == pl.pieces;
-    EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, undo_pw, nullptr};
+    EpiGrad<F32> e{last ? dh : nullptr, accum, q.d, pl.dp, i > 0, scale, undo_pw, nullptr};
     t = g16::plan(T, q.d, nv, 1, false, sms, NP);
     p = gemm_params(t, T, q.d, F32);
     if (!t.cs && t.ksplit > 1) {
@@ -1229,7 +1235,7 @@ dk_status backward(Call& c, const void* h, const void* W, const int64_t* target,
     }
 
     // dW of the piece = p^T.h
-    e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, undo_ph, F32 ? r.class_max : nullptr};
+    e = EpiGrad<F32>{static_cast<char*>(dW) + (size_t)v0 * q.d * es, nullptr, q.d, 0, 0, scale, undo_ph, F32 ? r.class_max : nullptr};
     t = g16::plan(nv, q.d, T, 1, false, sms, NP);
     p = gemm_params(t, nv, q.d, F32);
     if (!t.cs && t.ksplit > 1) {

@@ -448,3 +448,27 @@ def test_sure_rows(ctx, dtype, rows, margin, d, vocab):
     rel = 2.0 ** -18 * float((h.double().abs() @ W.double().abs().T).max()) + (2.0 ** -7 if dtype == "bf16" else 2.0 ** -17)
     bound = 2 * off * W.double()[t].norm(dim=1) + rel * (p.abs() @ W.double().abs()).norm(dim=1)
     assert bool(((dh.double() - want).norm(dim=1) <= bound).all())
+
+
+@pytest.mark.parametrize("scale", [1.0 / 15, 1.0 / 2047, 0.3])
+@pytest.mark.parametrize("rows,d,vocab", [(1, 2048, 5000), (100, 64, 5000), (2000, 500, 3000), (3000, 64, 40000), (9, 60000, 400)])
+def test_p_is_rounded_without_its_scale(ctx, rows, d, vocab, scale):
+    """bf16, a flat softmax: p is nearly -scale at every target, and rounded with the scale in it would take up to 2^-8 off
+    the whole gradient.  Element by element: scale times the products of p rounded without it, off by the result's rounding
+    (2^-8 of it), by a probability that rounds the other way (2^-8 of the terms that are not targets, whose 1 - 1/vocab is
+    not halfway between two bf16 numbers), and by the sums (2^-19 of all terms)."""
+    h, W, t = draw(rows, d, vocab, torch.bfloat16, seed=28, gain=0.01, ignored=0.0)
+    _, _, dh, dW = call(ctx, h, W, t, dk.DK_BF16, scale=scale)
+    hd, Wd, at = h.double(), W.double(), torch.arange(rows, device="cuda")
+    z = hd @ Wd.T
+    p = torch.exp(z - torch.logsumexp(z, dim=1)[:, None])
+    p[at, t] -= 1
+    p = p.float().to(torch.bfloat16).double()
+    small = p.abs()
+    small[at, t] = 0
+    live = t.unique()
+    for got, want, rest, terms in (
+            (dh, p @ Wd, small @ Wd.abs(), p.abs() @ Wd.abs()),
+            (dW[live], p[:, live].T @ hd, small[:, live].T @ hd.abs(), p[:, live].abs().T @ hd.abs())):
+        bound = scale * (2.0 ** -8 * (want.abs() + 2 * rest) + 2.0 ** -19 * terms)
+        assert bool(((got.double() - scale * want).abs() <= bound).all())
