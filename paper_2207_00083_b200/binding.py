@@ -237,7 +237,8 @@ class Context:
     def ensure_workspace(self, p, field: bool = False, forward: bool = False):
         """Grows the torch-owned workspace to what `p` (a dk_problem, dk_norm, dk_xent or dk_ortho) needs and
         registers it (``field=True``: what the finite-field calls need; ``forward=True`` with a dk_xent: what
-        dk_linear_xent_fwd alone needs)."""
+        dk_linear_xent_fwd alone needs).  Growing it releases the buffer before: no call in flight on another stream
+        and no captured graph may still use that."""
         if not isinstance(p, dk_problem):
             need = self.step_workspace_bytes(p, forward)
         else:
