@@ -21,9 +21,10 @@
 //
 // One or a few rows take dot products instead for their logits, in both directions (xent_few_rows_kernel).
 //
-// Measured: 4096 x 4096, 128000 classes, bf16, both directions 14.7 ms (1.17 PFLOP/s over its four products, 83 % of the
-// library's sustained rate); 2047 x 1024, 50257 classes 0.84 ms; 4000 x 768, 32000 classes, fp32 2.63 ms; 256 x 4096, 1000
-// classes, fp32, forward 28 us; 64 x 512, both directions, 48.5 us (nine launches of 4 to 10 us).
+// Measured: 4096 x 4096, 128000 classes, bf16, both directions 14.3 to 14.7 ms (1.17 to 1.2 PFLOP/s over its four
+// products, 83 to 85 % of the library's sustained rate); 2047 x 1024, 50257 classes 0.84 ms; 4000 x 768, 32000 classes,
+// fp32 2.63 ms; 256 x 4096, 1000 classes, fp32, forward 28 us; 64 x 512, both directions, 48.5 us (nine launches of 4 to
+// 10 us).
 #include <math.h>
 
 #include "dk_gemm16.cuh"
@@ -45,7 +46,7 @@ struct Meta {
 };
 
 // The power of two that brings a largest magnitude (given by its bits) to [2^14, 2^15); 1 when it is zero, infinite or
-// NaN (a forward row's own).  The products undo it with inv_scale.
+// NaN (a forward row's own).  Undo, or the rows' inverses, take it back.
 __device__ __forceinline__ int scale_exp(unsigned int bits) {
   const int e = (int)(bits >> 23) - 127;
   if (bits == 0u || e > 127) return 0;
@@ -872,7 +873,8 @@ __global__ void __launch_bounds__(256) xent_class_terms_kernel(const ClassArgs q
     }
   }
   // a warp looks at the classes of its lanes, and lays out those that need it together
-  const long long warps = (long long)gridDim.x * gridDim.y * 8, first = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 8 + warp;
+  const long long warps = (long long)gridDim.x * gridDim.y * 8;
+  const long long first = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 8 + warp;
   for (long long r0 = first; r0 < q.n; r0 += 32 * warps) {
     const long long mine = r0 + lane * warps;
     const int e_mine = mine < q.n ? class_exp(__ldg(q.class_max + mine)) : 0;
