@@ -514,6 +514,119 @@ DK_API dk_status dk_ortho_workspace_bytes(const dk_ortho* q, size_t* bytes);
 DK_API dk_status dk_orthogonalize(dk_ctx* ctx, const dk_ortho* q, const void* x, float scale, float keep,
                                   void* out, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * What a training step keeps from the forward to the backward pass, in 8 bits,
+ * and the norms between two residual blocks.  The conventions of the calls above
+ * hold: DK_F32 or DK_BF16 tensors, contiguous and 16-byte aligned; parameters,
+ * their gradients and statistics fp32; sums in a fixed order.
+ * ------------------------------------------------------------------------- */
+
+/* An activation checkpoint: a tensor of rows x d values in 8 bits.  For each 32
+ * consecutive values of a row (the last block of a row may be shorter) one power
+ * of two and whole numbers q, |q| <= 127:
+ *   value = q*2^(b - 127)
+ * with the least b from 1 to 248 under which no value of the block rounds beyond
+ * 127; q is the nearest whole number, halves to even.  So a value is off by at most
+ * half of 2^(b - 127), at most 1/127 of the block's largest magnitude (magnitudes
+ * beyond 127.5*2^121, 3.39e38, become 127*2^121).  A block
+ * with an infinity or a NaN (b = 255) comes back as NaN, all of it; what lies
+ * below 2^-127 comes back as 0.
+ * Layout: q [rows][32*ceil(d/32)] (signed bytes, zeros behind d), then
+ * b [rows][ceil(d/32)].  The calls that write a checkpoint write all of it. */
+typedef struct {
+  int64_t rows;       /* 0: nothing to do                                         */
+  int32_t d;          /* values of a row, 1 .. 2^20                               */
+  int32_t dtype;      /* of the tensor that is stored or loaded                   */
+} dk_ckpt8;
+
+DK_API dk_status dk_ckpt8_bytes(const dk_ckpt8* q, size_t* bytes);
+/* x -> checkpoint, and back (in the same or the other type: 7 bits and a power of
+ * two are a bf16 number).  HBM-bound; no workspace. */
+DK_API dk_status dk_ckpt8_store(dk_ctx* ctx, const dk_ckpt8* q, const void* x, void* ckpt, void* stream);
+DK_API dk_status dk_ckpt8_load(dk_ctx* ctx, const dk_ckpt8* q, const void* ckpt, void* x, void* stream);
+
+/* dk_group_norm_fwd that also leaves a checkpoint of x (rows = n*h*w, d = c), and
+ * dk_group_norm_bwd that reads x from one.  Outputs, statistics and workspace are
+ * those of the calls without a checkpoint; x itself need not outlive the forward
+ * call.  xhat and z are formed from the checkpoint's values with the statistics
+ * of x. */
+DK_API dk_status dk_group_norm_fwd_ckpt8(dk_ctx* ctx, const dk_norm* q, const void* x, const float* gamma,
+                                         const float* beta, void* y, float* stats, void* ckpt, void* stream);
+DK_API dk_status dk_group_norm_bwd_ckpt8(dk_ctx* ctx, const dk_norm* q, const void* dy, const void* ckpt,
+                                         const float* gamma, const float* beta, const float* stats, void* dx,
+                                         float* dgamma, float* dbeta, void* stream);
+
+/* Weight gradient of a linear layer y = W.x + b without masking, from the
+ * checkpoint of its input x[rows][d]:
+ *   dW[o][c] = keep*dW[o][c] + scale*sum_r dy[r][o]*x[r][c]
+ *   db[o]    = keep*db[o]    + scale*sum_r dy[r][o]
+ * dy: [rows][out]; dW, db: fp32, db nullable.  keep = 0: neither is read.  The
+ * checkpoint's values enter the tensor cores as they are.  DK_BF16: so does dy.
+ * DK_F32: dy as two fp16 terms under a power of two of each output (22 bits down
+ * to 2^-17 of the output's largest magnitude, an absolute error of 2^-39 of it
+ * below), and the checkpoint's values under one power of two of all of it, exact
+ * for blocks whose b lies within 32 of the largest, with an absolute error below
+ * 2^-39 of the tensor's largest value for those further down.  Needs the
+ * workspace. */
+typedef struct {
+  int64_t rows;       /* 0: dW and db become keep times themselves                */
+  int32_t d, out;     /* features of x and of dy                                  */
+  int32_t dtype;      /* of dy                                                    */
+} dk_wgrad8;
+
+DK_API dk_status dk_wgrad8_workspace_bytes(const dk_wgrad8* q, size_t* bytes);
+DK_API dk_status dk_linear_bwd_wgrad_ckpt8(dk_ctx* ctx, const dk_wgrad8* q, const void* dy, const void* ckpt,
+                                           float scale, float keep, float* dW, float* db, void* stream);
+
+/* The norms before and after a residual block, fused with its gate and residual
+ * scale: everything between the output u of one block and the input n of the
+ * next.  Per row:
+ *   uhat = (u - mean_u)*rstd_u,  h' = keep*h + scale*gate*post*uhat
+ *   n = (h' - mean_h)*rstd_h*pre + shift
+ * DK_BLOCK_LAYER: mean and variance (divided by d); DK_BLOCK_RMS: the means are
+ * 0 and rstd = 1/sqrt(mean of squares + eps).  h' is rounded once, as h_out; n is
+ * formed from it before that. */
+enum { DK_BLOCK_RMS = 0, DK_BLOCK_LAYER = 1 };
+typedef struct {
+  int64_t rows;          /* tokens, pixels (0: nothing to do; gradients of parameters are zero) */
+  int32_t d;             /* features, 1 .. 16384                                     */
+  int64_t rows_per_gate; /* consecutive rows that share a row of gate (>= 1)         */
+  int32_t kind;          /* DK_BLOCK_RMS | DK_BLOCK_LAYER                            */
+  int32_t dtype;         /* of h, u, h_out, n and their gradients                    */
+  float eps;             /* >= 0, added to the variance or mean of squares           */
+  float keep, scale;     /* of the residual and of the branch                        */
+} dk_block;
+
+DK_API dk_status dk_block_workspace_bytes(const dk_block* q, size_t* bytes);
+
+/* post, pre, shift: fp32 [d]; gate: fp32 [ceil(rows/rows_per_gate)][d] (a learned
+ * gate: rows_per_gate >= rows).  Nullable: gate (1), shift (0); u with post and
+ * h_out (no branch: h' = h, before the first block); n with pre (no norm, after the
+ * last one); stats, fp32 [rows][4]: mean_u, rstd_u, mean_h, rstd_h (not kept);
+ * ckpt_h and ckpt_u, checkpoints of h and u.  h_out may be h.  One launch, no
+ * workspace; HBM-bound. */
+DK_API dk_status dk_block_norm_fwd(dk_ctx* ctx, const dk_block* q, const void* h, const void* u, const float* gate,
+                                   const float* post, const float* pre, const float* shift, void* h_out, void* n,
+                                   float* stats, void* ckpt_h, void* ckpt_u, void* stream);
+
+/* Gradients of the forward call from its inputs h and u (or their checkpoints) and
+ * its statistics; dh_out: of h_out, dn: of n.
+ *   D = dh_out + rstd_h*(q - mean(q) - hhat*mean(q*hhat)),  q = dn*pre,  dh = keep*D
+ *   du = rstd_u*(s - mean(s) - uhat*mean(s*uhat)),  s = scale*gate*post*D
+ *   dpre = sum dn*hhat,  dshift = sum dn,  dpost = sum scale*D*gate*uhat,
+ *   dgate = sum over the gate's rows of scale*D*post*uhat
+ * (root mean square: without mean(q) and mean(s)).  Nullable: dh_out (zero) or dn
+ * with pre and dpre; u with post, du and dpost; gate with dgate; dshift.  dh may be
+ * dh_out.  Parameters' gradients are fp32 and overwritten.  Needs the workspace. */
+DK_API dk_status dk_block_norm_bwd(dk_ctx* ctx, const dk_block* q, const void* dh_out, const void* dn, const void* h,
+                                   const void* u, const float* gate, const float* post, const float* pre,
+                                   const float* stats, void* dh, void* du, float* dgate, float* dpost, float* dpre,
+                                   float* dshift, void* stream);
+DK_API dk_status dk_block_norm_bwd_ckpt8(dk_ctx* ctx, const dk_block* q, const void* dh_out, const void* dn,
+                                         const void* ckpt_h, const void* ckpt_u, const float* gate, const float* post,
+                                         const float* pre, const float* stats, void* dh, void* du, float* dgate,
+                                         float* dpost, float* dpre, float* dshift, void* stream);
+
 /* Errors raised ON THE DEVICE by calls that have no dk_verdict to carry them
  * (dk_linear_fwd, dk_linear_bwd_wgrad): every wait inside the kernels is
  * bounded, and a kernel whose wait expires stops, leaves its output incomplete

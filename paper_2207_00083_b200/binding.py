@@ -82,6 +82,23 @@ class dk_ortho(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
+DK_BLOCK_RMS, DK_BLOCK_LAYER = 0, 1
+
+
+class dk_ckpt8(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class dk_wgrad8(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("out", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class dk_block(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("rows_per_gate", ctypes.c_int64),
+                ("kind", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("keep", ctypes.c_float),
+                ("scale", ctypes.c_float)]
+
+
 VERDICT_BYTES = ctypes.sizeof(dk_verdict)
 _lib = None
 
@@ -128,6 +145,17 @@ def _signatures():
         "dk_linear_xent_bwd": [vp, ctypes.POINTER(dk_xent), vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp],
         "dk_ortho_workspace_bytes": [ctypes.POINTER(dk_ortho), ctypes.POINTER(ctypes.c_size_t)],
         "dk_orthogonalize": [vp, ctypes.POINTER(dk_ortho), vp, ctypes.c_float, ctypes.c_float, vp, vp],
+        "dk_ckpt8_bytes": [ctypes.POINTER(dk_ckpt8), ctypes.POINTER(ctypes.c_size_t)],
+        "dk_ckpt8_store": [vp, ctypes.POINTER(dk_ckpt8), vp, vp, vp],
+        "dk_ckpt8_load": [vp, ctypes.POINTER(dk_ckpt8), vp, vp, vp],
+        "dk_group_norm_fwd_ckpt8": [vp, ctypes.POINTER(dk_norm), vp, vp, vp, vp, vp, vp, vp],
+        "dk_group_norm_bwd_ckpt8": [vp, ctypes.POINTER(dk_norm), vp, vp, vp, vp, vp, vp, vp, vp, vp],
+        "dk_wgrad8_workspace_bytes": [ctypes.POINTER(dk_wgrad8), ctypes.POINTER(ctypes.c_size_t)],
+        "dk_linear_bwd_wgrad_ckpt8": [vp, ctypes.POINTER(dk_wgrad8), vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp],
+        "dk_block_workspace_bytes": [ctypes.POINTER(dk_block), ctypes.POINTER(ctypes.c_size_t)],
+        "dk_block_norm_fwd": [vp, ctypes.POINTER(dk_block)] + [vp] * 12,
+        "dk_block_norm_bwd": [vp, ctypes.POINTER(dk_block)] + [vp] * 15,
+        "dk_block_norm_bwd_ckpt8": [vp, ctypes.POINTER(dk_block)] + [vp] * 15,
         "dk_profile_enable": [vp, ctypes.c_int],
         "dk_profile_read": [vp, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
                             ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)],
@@ -228,15 +256,16 @@ class Context:
         return n.value
 
     def step_workspace_bytes(self, q, forward: bool = False) -> int:
-        """Workspace of a dk_norm, dk_xent or dk_ortho call (``forward=True``: of dk_linear_xent_fwd alone)."""
+        """Workspace of a dk_norm, dk_xent, dk_ortho, dk_wgrad8 or dk_block call (``forward=True``: of
+        dk_linear_xent_fwd alone)."""
         name = f"{type(q).__name__}{'_fwd' if forward and isinstance(q, dk_xent) else ''}_workspace_bytes"
         n = ctypes.c_size_t()
         _check(getattr(lib(), name)(ctypes.byref(q), ctypes.byref(n)), name)
         return n.value
 
     def ensure_workspace(self, p, field: bool = False, forward: bool = False):
-        """Grows the torch-owned workspace to what `p` (a dk_problem, dk_norm, dk_xent or dk_ortho) needs and
-        registers it (``field=True``: what the finite-field calls need; ``forward=True`` with a dk_xent: what
+        """Grows the torch-owned workspace to what `p` (a dk_problem, dk_norm, dk_xent, dk_ortho, dk_wgrad8 or dk_block)
+        needs and registers it (``field=True``: what the finite-field calls need; ``forward=True`` with a dk_xent: what
         dk_linear_xent_fwd alone needs).  Growing it releases the buffer before: no call in flight on another stream
         and no captured graph may still use that."""
         if not isinstance(p, dk_problem):
@@ -508,3 +537,105 @@ def dk_orthogonalize(ctx: Context, q: dk_ortho, x, scale: float, keep: float, ou
     _check(lib().dk_orthogonalize(ctx.handle, ctypes.byref(q), _typed(ctx, x, q.dtype, e, "x"), scale,
                                   keep, _typed(ctx, out, q.dtype, e, "out"), _raw_stream(ctx.device)),
            "dk_orthogonalize")
+
+
+# ---------------------------------------------------------------------------
+# what is kept between the two directions in 8 bits, and the norms between two residual blocks: checkpoints are uint8
+# tensors of dk_ckpt8_bytes
+# ---------------------------------------------------------------------------
+def _padded(d: int) -> int:
+    return (d + 31) // 32 * 32
+
+
+def dk_ckpt8_bytes(q: dk_ckpt8) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().dk_ckpt8_bytes(ctypes.byref(q), ctypes.byref(n)), "dk_ckpt8_bytes")
+    return n.value
+
+
+def _kept(ctx, t: torch.Tensor, rows: int, d: int, what: str) -> int:
+    n = rows * _padded(d) + rows * (_padded(d) // 32)
+    if t.dtype is not torch.uint8 or t.numel() != n or not t.is_contiguous() or t.get_device() != ctx.device:
+        raise ValueError(f"{what}: expected a contiguous uint8 tensor of {n} elements on CUDA device {ctx.device}")
+    return t.data_ptr()
+
+
+def dk_ckpt8_store(ctx: Context, q: dk_ckpt8, x, ckpt):
+    _check(lib().dk_ckpt8_store(ctx.handle, ctypes.byref(q), _typed(ctx, x, q.dtype, q.rows * q.d, "x"),
+                                _kept(ctx, ckpt, q.rows, q.d, "ckpt"), _raw_stream(ctx.device)), "dk_ckpt8_store")
+
+
+def dk_ckpt8_load(ctx: Context, q: dk_ckpt8, ckpt, x):
+    _check(lib().dk_ckpt8_load(ctx.handle, ctypes.byref(q), _kept(ctx, ckpt, q.rows, q.d, "ckpt"),
+                               _typed(ctx, x, q.dtype, q.rows * q.d, "x"), _raw_stream(ctx.device)), "dk_ckpt8_load")
+
+
+def dk_group_norm_fwd_ckpt8(ctx: Context, q: dk_norm, x, gamma, beta, y, stats, ckpt):
+    e, c, s = _norm_sizes(q)
+    _check(lib().dk_group_norm_fwd_ckpt8(ctx.handle, ctypes.byref(q), _typed(ctx, x, q.dtype, e, "x"),
+                                         _f32(ctx, gamma, c, "gamma"), _f32(ctx, beta, c, "beta"),
+                                         _typed(ctx, y, q.dtype, e, "y"), _f32(ctx, stats, s, "stats"),
+                                         _kept(ctx, ckpt, q.n * q.h * q.w, c, "ckpt"), _raw_stream(ctx.device)),
+           "dk_group_norm_fwd_ckpt8")
+
+
+def dk_group_norm_bwd_ckpt8(ctx: Context, q: dk_norm, dy, ckpt, gamma, beta, stats, dx, dgamma, dbeta):
+    e, c, s = _norm_sizes(q)
+    _check(lib().dk_group_norm_bwd_ckpt8(ctx.handle, ctypes.byref(q), _typed(ctx, dy, q.dtype, e, "dy"),
+                                         _kept(ctx, ckpt, q.n * q.h * q.w, c, "ckpt"), _f32(ctx, gamma, c, "gamma"),
+                                         _f32(ctx, beta, c, "beta"), _f32(ctx, stats, s, "stats"),
+                                         _typed(ctx, dx, q.dtype, e, "dx"), _f32(ctx, dgamma, c, "dgamma"),
+                                         _f32(ctx, dbeta, c, "dbeta"), _raw_stream(ctx.device)),
+           "dk_group_norm_bwd_ckpt8")
+
+
+def dk_linear_bwd_wgrad_ckpt8(ctx: Context, q: dk_wgrad8, dy, ckpt, scale: float, keep: float, dW,
+                              db: Optional[torch.Tensor]):
+    _check(lib().dk_linear_bwd_wgrad_ckpt8(ctx.handle, ctypes.byref(q), _typed(ctx, dy, q.dtype, q.rows * q.out, "dy"),
+                                           _kept(ctx, ckpt, q.rows, q.d, "ckpt"), scale, keep,
+                                           _f32(ctx, dW, q.out * q.d, "dW"),
+                                           None if db is None else _f32(ctx, db, q.out, "db"), _raw_stream(ctx.device)),
+           "dk_linear_bwd_wgrad_ckpt8")
+
+
+def _or_null(f, ctx, t: Optional[torch.Tensor], *rest):
+    return None if t is None else f(ctx, t, *rest)
+
+
+def _gate(ctx, q: dk_block, t: Optional[torch.Tensor], what: str):
+    return _or_null(_f32, ctx, t, -(-q.rows // q.rows_per_gate) * q.d if q.rows_per_gate > 0 else -1, what)
+
+
+def dk_block_norm_fwd(ctx: Context, q: dk_block, h, u, gate, post, pre, shift, h_out, n, stats, ckpt_h=None, ckpt_u=None):
+    """Every tensor but h may be None where the C call takes NULL."""
+    e, d = q.rows * q.d, q.d
+    _check(lib().dk_block_norm_fwd(
+        ctx.handle, ctypes.byref(q), _typed(ctx, h, q.dtype, e, "h"), _or_null(_typed, ctx, u, q.dtype, e, "u"),
+        _gate(ctx, q, gate, "gate"), _or_null(_f32, ctx, post, d, "post"), _or_null(_f32, ctx, pre, d, "pre"),
+        _or_null(_f32, ctx, shift, d, "shift"), _or_null(_typed, ctx, h_out, q.dtype, e, "h_out"),
+        _or_null(_typed, ctx, n, q.dtype, e, "n"), _or_null(_f32, ctx, stats, 4 * q.rows, "stats"),
+        _or_null(_kept, ctx, ckpt_h, q.rows, d, "ckpt_h"), _or_null(_kept, ctx, ckpt_u, q.rows, d, "ckpt_u"),
+        _raw_stream(ctx.device)), "dk_block_norm_fwd")
+
+
+def _block_bwd(name, held, ctx, q, dh_out, dn, h, u, gate, post, pre, stats, dh, du, dgate, dpost, dpre, dshift):
+    e, d = q.rows * q.d, q.d
+    _check(getattr(lib(), name)(
+        ctx.handle, ctypes.byref(q), _or_null(_typed, ctx, dh_out, q.dtype, e, "dh_out"),
+        _or_null(_typed, ctx, dn, q.dtype, e, "dn"), held(h, "h"), None if u is None else held(u, "u"),
+        _gate(ctx, q, gate, "gate"), _or_null(_f32, ctx, post, d, "post"), _or_null(_f32, ctx, pre, d, "pre"),
+        _f32(ctx, stats, 4 * q.rows, "stats"), _typed(ctx, dh, q.dtype, e, "dh"),
+        _or_null(_typed, ctx, du, q.dtype, e, "du"), _gate(ctx, q, dgate, "dgate"), _or_null(_f32, ctx, dpost, d, "dpost"),
+        _or_null(_f32, ctx, dpre, d, "dpre"), _or_null(_f32, ctx, dshift, d, "dshift"), _raw_stream(ctx.device)), name)
+
+
+def dk_block_norm_bwd(ctx: Context, q: dk_block, dh_out, dn, h, u, gate, post, pre, stats, dh, du, dgate, dpost, dpre,
+                      dshift):
+    _block_bwd("dk_block_norm_bwd", lambda t, what: _typed(ctx, t, q.dtype, q.rows * q.d, what), ctx, q, dh_out, dn, h, u,
+               gate, post, pre, stats, dh, du, dgate, dpost, dpre, dshift)
+
+
+def dk_block_norm_bwd_ckpt8(ctx: Context, q: dk_block, dh_out, dn, ckpt_h, ckpt_u, gate, post, pre, stats, dh, du, dgate,
+                            dpost, dpre, dshift):
+    _block_bwd("dk_block_norm_bwd_ckpt8", lambda t, what: _kept(ctx, t, q.rows, q.d, "ckpt_" + what), ctx, q, dh_out, dn,
+               ckpt_h, ckpt_u, gate, post, pre, stats, dh, du, dgate, dpost, dpre, dshift)

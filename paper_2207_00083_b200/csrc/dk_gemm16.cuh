@@ -1,9 +1,9 @@
 // Matrix products C = A.B^T of 16-bit operands on CTA pairs (tcgen05 kind::f16, cta_group::2), for the operators
 // around the masked products: bf16 operands as they are, or fp32 operands as two fp16 terms each,
 //   v*2^s = hi + lo + e,  hi = fp16(v*2^s),  lo = fp16(v*2^s - hi),  |e| <= 2^-22 |v*2^s| (absolute 2^-25 below),
-// of which hi.hi + hi.lo + lo.hi are kept (lo.lo is 2^-22 of the product).  fp16 terms run at the full 16-bit rate of
-// the tensor cores, twice that of TF32, at the same 22 significant bits; what they lack is range, which the common
-// power of two 2^s supplies.
+// of which hi.hi + hi.lo + lo.hi are kept (lo.lo is 2^-22 of the product), or hi.B + lo.B where B needs
+// no second term.  fp16 terms run at the full 16-bit rate of the tensor cores, twice that of TF32, at the same 22
+// significant bits; what they lack is range, which the common power of two 2^s supplies.
 //
 // A pair computes a 256 x BN tile: each CTA stages its own 128 rows of A and its half of the BN rows of B, 64
 // contraction elements (128 bytes) per stage.  An operand is K-major (rows contiguous along the contraction) or
@@ -104,6 +104,25 @@ __device__ __forceinline__ void ld32(uint32_t taddr, float* v) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// The power of two that brings a largest magnitude (given by its bits) to [2^14, 2^15); 1 when it is zero, infinite or
+// NaN (a forward row's own).  Undo, or the rows' inverses, take it back.
+__device__ __forceinline__ int scale_exp(unsigned int bits) {
+  const int e = (int)(bits >> 23) - 127;
+  if (bits == 0u || e > 127) return 0;
+  const int s = 14 - e;
+  return s > 126 ? 126 : s;
+}
+__device__ __forceinline__ float pow2(int e) {      // -126 <= e <= 126
+  return __int_as_float((e + 127) << 23);
+}
+
+// The bits of a magnitude for a maximum: an infinity or a NaN counts as nothing.  (It makes its own row's results NaN; as
+// the maximum it would leave all other rows without their power of two.)
+__device__ __forceinline__ unsigned int magnitude(unsigned int bits) {
+  bits &= 0x7fffffffu;
+  return bits < 0x7f800000u ? bits : 0u;
+}
+
 // Descriptor of an MN-major tile: [64 contraction rows][64 elements] boxes of 8 KiB, 8-row groups 1 KiB apart, the
 // next 64 elements of M or N in the next box.
 __device__ __forceinline__ uint64_t desc_mn(uint32_t smem_addr) {
@@ -129,8 +148,14 @@ __device__ __forceinline__ void load_tile(unsigned char* dst, const CUtensorMap*
   }
 }
 
+// planes of A and of B: 1 and 1 (one product), 2 and 1 (two), 2 and 2 (three)
+template <int NPROD>
+constexpr int kPlanesA = NPROD == 1 ? 1 : 2;
+template <int NPROD>
+constexpr int kPlanesB = NPROD == 3 ? 2 : 1;
+
 template <int NPROD, int BN>
-__host__ __device__ constexpr int stage_bytes() { return (NPROD == 3 ? 2 : 1) * (ROWS + BN / 2) * 128; }
+__host__ __device__ constexpr int stage_bytes() { return (kPlanesA<NPROD> * ROWS + kPlanesB<NPROD> * BN / 2) * 128; }
 
 // Epi: __device__ void operator()(const Params&, float (&acc)[BN/2], int batch, int ks, int row, int col0, char* sm) is
 // called by every epilogue thread with its row of C and its BN/2 columns from col0 on (row and columns may lie outside
@@ -141,7 +166,7 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
               const __grid_constant__ CUtensorMap map_b_hi, const __grid_constant__ CUtensorMap map_b_lo, const Params p,
               const Epi epi) {
   constexpr int A_BYTES = ROWS * 128, B_BYTES = BN / 2 * 128;
-  constexpr int PL = NPROD == 3 ? 2 : 1;
+  constexpr int PL = kPlanesA<NPROD>;
   constexpr int STAGE = stage_bytes<NPROD, BN>();
   constexpr int NH = BN / 2;
   static_assert(BN == 256 || BN == 128, "tile width");
@@ -205,10 +230,9 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
             const uint32_t bar = tc::mapa_shared(smem_u32(full_bar + stage), 0u);
             load_tile<AMN, ROWS>(st, &map_a_hi, bar, m0, kb * BK, batch);
             load_tile<BMN, BN / 2>(st + PL * A_BYTES, &map_b_hi, bar, n0, kb * BK, batch);
-            if constexpr (NPROD == 3) {
-              load_tile<AMN, ROWS>(st + A_BYTES, &map_a_lo, bar, m0, kb * BK, batch);
+            if constexpr (NPROD >= 2) load_tile<AMN, ROWS>(st + A_BYTES, &map_a_lo, bar, m0, kb * BK, batch);
+            if constexpr (NPROD == 3)
               load_tile<BMN, BN / 2>(st + PL * A_BYTES + B_BYTES, &map_b_lo, bar, n0, kb * BK, batch);
-            }
             if (++stage == p.nstages) { stage = 0; phase ^= 1u; }
           }
         }
@@ -243,11 +267,11 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
 #pragma unroll
               for (int kk = 0; kk < BK / 16; ++kk) {
                 mma_f16_pair(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, (first && kk == 0) ? 0u : 1u);
-                if constexpr (NPROD == 3) {
-                  constexpr uint64_t LO_A = A_BYTES / 16, LO_B = B_BYTES / 16;
+                constexpr uint64_t LO_A = A_BYTES / 16, LO_B = B_BYTES / 16;
+                if constexpr (NPROD == 3)
                   mma_f16_pair(d_tmem, a_hi + kk * STEP_A, b_hi + LO_B + kk * STEP_B, idesc, 1u);
+                if constexpr (NPROD >= 2)
                   mma_f16_pair(d_tmem, a_hi + LO_A + kk * STEP_A, b_hi + kk * STEP_B, idesc, 1u);
-                }
               }
               tc::tc_pair_commit(empty_bar + stage);
               if (++stage == p.nstages) { stage = 0; phase ^= 1u; }
@@ -356,12 +380,12 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
                     const __grid_constant__ CUtensorMap map_b_hi, const __grid_constant__ CUtensorMap map_b_lo,
                     const Params p, const Epi epi) {
   constexpr int OP = SMALL * 128;                  // bytes of one operand plane in a stage
-  constexpr int PL = NPROD == 3 ? 2 : 1;
-  constexpr int STAGE = 2 * PL * OP;
-  // Columns of tensor memory between the two accumulators.  With three products each is followed by the low terms' own,
-  // so that hi.hi and hi.lo are one instruction over both planes of B (they lie one after the other) and A's rows are read
-  // from shared memory once for both (update of 3 x 512x4608 294 -> 288 us, of 1961x1001 273 -> 268).
-  constexpr uint32_t ACC = NPROD == 3 ? 256u : 128u;
+  constexpr int PL = kPlanesA<NPROD>;
+  constexpr int STAGE = (PL + kPlanesB<NPROD>) * OP;
+  // Columns of tensor memory between the two accumulators.  With two or three products each is followed by the low terms'
+  // own; with three so that hi.hi and hi.lo are one instruction over both planes of B (they lie one after the other) and
+  // A's rows are read from shared memory once for both (update of 3 x 512x4608 294 -> 288 us, of 1961x1001 273 -> 268).
+  constexpr uint32_t ACC = NPROD >= 2 ? 256u : 128u;
   constexpr int NC = SMALL / 2;                    // columns a thread holds (8 epilogue warps: 4 x 32 rows, 2 halves)
   constexpr int NH = NC / CS;                      // columns it finishes
   extern __shared__ unsigned char smem_raw[];
@@ -417,10 +441,9 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
         unsigned char* st = smem + (size_t)stage * STAGE;
         load_tile_cta<AMN, SMALL>(st, &map_a_hi, full_bar + stage, m0, kb * BK, batch);
         load_tile_cta<BMN, SMALL>(st + PL * OP, &map_b_hi, full_bar + stage, n0, kb * BK, batch);
-        if constexpr (NPROD == 3) {
-          load_tile_cta<AMN, SMALL>(st + OP, &map_a_lo, full_bar + stage, m0, kb * BK, batch);
+        if constexpr (NPROD >= 2) load_tile_cta<AMN, SMALL>(st + OP, &map_a_lo, full_bar + stage, m0, kb * BK, batch);
+        if constexpr (NPROD == 3)
           load_tile_cta<BMN, SMALL>(st + PL * OP + OP, &map_b_lo, full_bar + stage, n0, kb * BK, batch);
-        }
         if (++stage == p.nstages) { stage = 0; phase ^= 1u; }
       }
     }
@@ -451,6 +474,9 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
             const bool first = k == kb && kk == 0;
             if constexpr (NPROD == 1) {
               mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, first ? 0u : 1u);
+            } else if constexpr (NPROD == 2) {
+              mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, first ? 0u : 1u);
+              mma_f16(d_tmem + 128u, a_hi + LO + kk * STEP_A, b_hi + kk * STEP_B, idesc, first && acc_it < 2 ? 0u : 1u);
             } else {
               if (first && acc_it >= 2) {      // a new sum of high terms, the low terms' goes on
                 mma_f16(d_tmem, a_hi + kk * STEP_A, b_hi + kk * STEP_B, idesc, 0u);
@@ -487,7 +513,7 @@ gemm16_small_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_c
 #pragma unroll
         for (int j = 0; j < 32; ++j) acc[c + j] += fmaf(tmp[j], comp, tmp[j]);
       }
-      if (NPROD == 3 && kb + p.chunk >= kb_hi) {           // (nothing overwrites them: this was the last chunk)
+      if (NPROD >= 2 && kb + p.chunk >= kb_hi) {           // (nothing overwrites them: this was the last chunk)
         for (uint32_t b = 0; b <= min(acc_it, 1u); ++b) {
 #pragma unroll
           for (int c = 0; c < NC; c += 32) {
@@ -772,7 +798,7 @@ inline Tiling plan(long long M, long long N, long long K, int nbatch, bool sym, 
       const double waves = (double)((tiles * nbatch + resident - 1) / resident);
       t.kb_per_split = (KB + cs - 1) / cs;
       t.ksplit = 1;
-      const double stage = (nprod == 3 ? 4 : 2) * 16384.0 / 50.0;
+      const double stage = (nprod + 1) * 16384.0 / 50.0;
       cost = waves * (t.kb_per_split * (stage > 256.0 * nprod ? stage : 256.0 * nprod) + 9000.0 + (cs > 1 ? 6000.0 : 0.0));
     }
     if (cs == 0 || cost < least) { least = cost; best = t; }
@@ -814,12 +840,12 @@ dk_status launch_small(dk_ctx* ctx, const Operand& A, const Operand& B, Params p
   if (!make_map(ctx, &ma, A.hi, A, p.nbatch, AMN, SMALL) || !make_map(ctx, &mb, B.hi, B, p.nbatch, BMN, SMALL))
     return DK_ERR_CUDA;
   mal = ma; mbl = mb;
-  if (NPROD == 3 && (!make_map(ctx, &mal, A.lo, A, p.nbatch, AMN, SMALL) ||
-                     !make_map(ctx, &mbl, B.lo, B, p.nbatch, BMN, SMALL)))
+  if ((NPROD >= 2 && !make_map(ctx, &mal, A.lo, A, p.nbatch, AMN, SMALL)) ||
+      (NPROD == 3 && !make_map(ctx, &mbl, B.lo, B, p.nbatch, BMN, SMALL)))
     return DK_ERR_CUDA;
-  constexpr int STAGE = (NPROD == 3 ? 4 : 2) * SMALL * 128;
+  constexpr int STAGE = (kPlanesA<NPROD> + kPlanesB<NPROD>) * SMALL * 128;
   constexpr int CTRL = (2 * tc::kMaxStages + 4) * 8 + 16;
-  p.nstages = NPROD == 3 ? 3 : 6;
+  p.nstages = NPROD == 3 ? 3 : NPROD == 2 ? 4 : 6;
   const int smem = p.nstages * STAGE + CTRL + 1024;
   if (smem > tc_smem_optin(ctx)) return DK_ERR_UNSUPPORTED;
   auto kern = gemm16_small_kernel<NPROD, AMN, BMN, CS, Epi>;
@@ -857,8 +883,8 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
   if (!make_map(ctx, &ma, A.hi, A, p.nbatch, AMN, ROWS) || !make_map(ctx, &mb, B.hi, B, p.nbatch, BMN, BN / 2))
     return DK_ERR_CUDA;
   mal = ma; mbl = mb;
-  if (NPROD == 3 && (!make_map(ctx, &mal, A.lo, A, p.nbatch, AMN, ROWS) ||
-                     !make_map(ctx, &mbl, B.lo, B, p.nbatch, BMN, BN / 2)))
+  if ((NPROD >= 2 && !make_map(ctx, &mal, A.lo, A, p.nbatch, AMN, ROWS)) ||
+      (NPROD == 3 && !make_map(ctx, &mbl, B.lo, B, p.nbatch, BMN, BN / 2)))
     return DK_ERR_CUDA;
   constexpr int STAGE = stage_bytes<NPROD, BN>();
   constexpr int CTRL = (2 * tc::kMaxStages + 4) * 8 + 16;

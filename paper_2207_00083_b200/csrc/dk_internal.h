@@ -169,6 +169,9 @@ dk_status launch_simt_fwd(const Geom& g, const float* W, const float* xbar, floa
 dk_status launch_simt_wgrad(const Geom& g, const float* dtil, const float* xbar, int xbar_rows,
                             float scale, float* dW, int sm_count, cudaStream_t st, bool clear = true);
 
+// an activation checkpoint stored (store) or loaded, in one launch (dk_ckpt8.cu)
+dk_status launch_ckpt8(const dk_ckpt8& q, bool store, const void* x, void* y, void* ckpt, int sms, cudaStream_t st);
+
 // the context's status word (see dk_device_status) and the offsets of workspace regions that
 // other translation units borrow (dk_api.cu)
 int* device_status_word(dk_ctx* ctx);

@@ -20,12 +20,10 @@
 // bounded by the few dozen values that share a pivot and not by how far the mean lies from zero; the (count, mean,
 // sum of squared deviations) of batches, threads and slabs are then joined pairwise,
 //   M2 = M2a + M2b + (mean_b - mean_a)^2 * na*nb/(na + nb).
-#include <cuda_bf16.h>
-
-#include <type_traits>
-
+#include "dk_ckpt8.cuh"
 #include "dk_internal.h"
 #include "dk_step.h"
+#include "dk_vec.cuh"
 
 namespace dk {
 namespace {
@@ -36,61 +34,6 @@ constexpr int kMaxC = 16384;
 // Pixels of an image: a loop's index passes the last pixel by less than a step, at most kLoads * 512 threads' pixels, and
 // stays below 2^31.  (Unsigned indices would do without the limit and cost the backward sums 1 to 2 %.)
 constexpr long long kMaxPix = (1LL << 31) - 4096;
-
-// VEC consecutive elements: as stored (Raw, one access of at most 16 bytes) and as fp32
-template <int DT, int VEC>
-struct Vec {
-  static constexpr int BYTES = VEC * (DT == DK_F32 ? 4 : 2);
-  using Raw = typename std::conditional<
-      BYTES == 16, uint4,
-      typename std::conditional<BYTES == 8, uint2,
-                                typename std::conditional<BYTES == 4, uint32_t, uint16_t>::type>::type>::type;
-  static __device__ __forceinline__ Raw get(const void* base, long long e) {
-    return *reinterpret_cast<const Raw*>(static_cast<const char*>(base) + e * (BYTES / VEC));
-  }
-  static __device__ __forceinline__ void put(void* base, long long e, const Raw r) {
-    *reinterpret_cast<Raw*>(static_cast<char*>(base) + e * (BYTES / VEC)) = r;
-  }
-  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[VEC]) {
-    if constexpr (DT == DK_F32) {
-      const float* f = reinterpret_cast<const float*>(&r);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = f[i];
-    } else if constexpr (VEC == 1) {
-      v[0] = __uint_as_float((uint32_t)r << 16);
-    } else {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
-#pragma unroll
-      for (int i = 0; i < VEC / 2; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
-  }
-  static __device__ __forceinline__ Raw pack(const float (&v)[VEC]) {
-    Raw r;
-    if constexpr (DT == DK_F32) {
-      float* f = reinterpret_cast<float*>(&r);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) f[i] = v[i];
-    } else if constexpr (VEC == 1) {
-      const __nv_bfloat16 t = __float2bfloat16_rn(v[0]);
-      r = *reinterpret_cast<const uint16_t*>(&t);
-    } else {
-      uint32_t* w = reinterpret_cast<uint32_t*>(&r);
-#pragma unroll
-      for (int i = 0; i < VEC / 2; ++i) {
-        const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&t);
-      }
-    }
-    return r;
-  }
-  static __device__ __forceinline__ void load(const void* base, long long e, float (&v)[VEC]) {
-    unpack(get(base, e), v);
-  }
-  static __device__ __forceinline__ void store(void* base, long long e, const float (&v)[VEC]) { put(base, e, pack(v)); }
-};
 
 // z*sigmoid(z) = z/(1 + exp(-z)): exp overflows to infinity for very negative z, the quotient is then -0
 __device__ __forceinline__ float act_value(float z, int act) {
@@ -106,32 +49,10 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   return s * (1.f + z * (1.f - s));
 }
 
-// (count, mean, sum of squared deviations) of the union of two sets
-struct Moments {
-  float n, mean, m2;
-};
-__device__ __forceinline__ Moments join(const Moments a, const Moments b) {
-  const float n = a.n + b.n;
-  if (b.n == 0.f) return a;
-  if (a.n == 0.f) return b;
-  const float d = b.mean - a.mean, f = __fdividef(b.n, n);
-  return {n, fmaf(d, f, a.mean), a.m2 + b.m2 + d * d * a.n * f};
-}
-__device__ __forceinline__ Moments warp_join(Moments m) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Moments t;
-    t.n = __shfl_xor_sync(0xffffffffu, m.n, o);
-    t.mean = __shfl_xor_sync(0xffffffffu, m.mean, o);
-    t.m2 = __shfl_xor_sync(0xffffffffu, m.m2, o);
-    // (both lanes of a pair join in the same order)
-    m = (threadIdx.x & o) ? join(t, m) : join(m, t);
-  }
-  return m;
-}
-
 struct NormParams {
-  const void* x;
+  const void* x;          // (null where x comes from a checkpoint)
+  const uint8_t* codes;   // the checkpoint: rows of dp codes, and the exponents of their blocks
+  const uint8_t* exps;
   const void* dy;
   void* out;
   const float* gamma;
@@ -146,10 +67,40 @@ struct NormParams {
   long long n;
   long long rows;         // of csum
   int pix, c, groups, cg, slabs, slab_pix, act;
+  int dp;                 // codes of a checkpoint's row
   int TX, TY;             // threads along the channel vectors, and along the pixels
   int param_blocks;       // of norm_apply_kernel
   int cb;                 // channels of an item of norm_sample_kernel
   float eps;
+};
+
+// The vectors of x at one place of each pixel of a sample, as given (K8 = false) or from a checkpoint.
+template <int DT, int VEC, bool K8>
+struct XVectors;
+template <int DT, int VEC>
+struct XVectors<DT, VEC, false> {
+  using Raw = typename Vec<DT, VEC>::Raw;
+  const void* x;
+  long long base;
+  int c;
+  __device__ __forceinline__ XVectors(const NormParams& p, long long s, int ch)
+      : x(p.x), base(s * p.pix * (long long)p.c + ch), c(p.c) {}
+  __device__ __forceinline__ Raw get(int i) const { return Vec<DT, VEC>::get(x, base + (long long)i * c); }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[VEC]) { Vec<DT, VEC>::unpack(r, v); }
+};
+template <int DT, int VEC>
+struct XVectors<DT, VEC, true> {
+  using Raw = ckpt8::Raw<VEC>;
+  const uint8_t* codes;
+  const uint8_t* exps;
+  int dp;
+  __device__ __forceinline__ XVectors(const NormParams& p, long long s, int ch)
+      : codes(p.codes + s * p.pix * (long long)p.dp + ch),
+        exps(p.exps + s * p.pix * (long long)(p.dp / ckpt8::kBlock) + ch / ckpt8::kBlock), dp(p.dp) {}
+  __device__ __forceinline__ Raw get(int i) const {
+    return ckpt8::get<VEC>(codes + (long long)i * dp, exps + (long long)i * (dp / ckpt8::kBlock));
+  }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[VEC]) { ckpt8::unpack<VEC>(r, v); }
 };
 
 // Sums of the pixels [b, e) (every TY-th from ty on) of the channel vector at `base`: forward, about a pivot per batch.
@@ -187,8 +138,8 @@ __device__ __forceinline__ Moments sum_moments(const void* x, long long base, in
 
 // The same for the backward pass: sums of d and d*xhat per channel of the vector.  z is formed by the very expression of
 // write_values, so that at ReLU's kink the sums, dx and the forward call's y agree on which elements are active.
-template <int DT, int VEC, int ACT>
-__device__ __forceinline__ void sum_gradients(const void* x, const void* dy, long long base, int b, int e, int c, int TY,
+template <int DT, int VEC, int ACT, bool K8>
+__device__ __forceinline__ void sum_gradients(const XVectors<DT, VEC, K8>& x, const void* dy, long long base, int b, int e, int c, int TY,
                                               const float (&mean)[VEC], const float (&rstd)[VEC],
                                               const float (&ga)[VEC], const float (&be)[VEC], float (&sb)[VEC],
                                               float (&sg)[VEC]) {
@@ -197,18 +148,19 @@ __device__ __forceinline__ void sum_gradients(const void* x, const void* dy, lon
 #pragma unroll
   for (int k = 0; k < VEC; ++k) f[k] = ga[k] * rstd[k];
   for (int i0 = b; i0 < e; i0 += L * TY) {
-    typename Vec<DT, VEC>::Raw rx[L], rd[L];
+    typename XVectors<DT, VEC, K8>::Raw rx[L];
+    typename Vec<DT, VEC>::Raw rd[L];
 #pragma unroll
     for (int u = 0; u < L; ++u)
       if (i0 + u * TY < e) {
-        rx[u] = Vec<DT, VEC>::get(x, base + (long long)(i0 + u * TY) * c);
+        rx[u] = x.get(i0 + u * TY);
         rd[u] = Vec<DT, VEC>::get(dy, base + (long long)(i0 + u * TY) * c);
       }
 #pragma unroll
     for (int u = 0; u < L; ++u)
       if (i0 + u * TY < e) {
         float a[VEC], d[VEC];
-        Vec<DT, VEC>::unpack(rx[u], a);
+        x.unpack(rx[u], a);
         Vec<DT, VEC>::unpack(rd[u], d);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
@@ -222,8 +174,8 @@ __device__ __forceinline__ void sum_gradients(const void* x, const void* dy, lon
 }
 
 // The values of those pixels: y, or dx given the means m0 of q and m1 of q*xhat.
-template <int DT, int VEC, int ACT, bool FWD>
-__device__ __forceinline__ void write_values(const void* x, const void* dy, void* out, long long base, int b, int e,
+template <int DT, int VEC, int ACT, bool FWD, bool K8>
+__device__ __forceinline__ void write_values(const XVectors<DT, VEC, K8>& x, const void* dy, void* out, long long base, int b, int e,
                                              int c, int TY, const float (&mean)[VEC], const float (&rstd)[VEC],
                                              const float (&m0)[VEC], const float (&m1)[VEC], const float (&ga)[VEC],
                                              const float (&be)[VEC]) {
@@ -233,18 +185,19 @@ __device__ __forceinline__ void write_values(const void* x, const void* dy, void
 #pragma unroll
   for (int k = 0; k < VEC; ++k) { f[k] = ga[k] * rstd[k]; c1[k] = rstd[k] * m1[k]; }
   for (int i0 = b; i0 < e; i0 += L * TY) {
-    typename Vec<DT, VEC>::Raw rx[L], rd[FWD ? 1 : L];
+    typename XVectors<DT, VEC, K8>::Raw rx[L];
+    typename Vec<DT, VEC>::Raw rd[FWD ? 1 : L];
 #pragma unroll
     for (int u = 0; u < L; ++u)
       if (i0 + u * TY < e) {
-        rx[u] = Vec<DT, VEC>::get(x, base + (long long)(i0 + u * TY) * c);
+        rx[u] = x.get(i0 + u * TY);
         if constexpr (!FWD) rd[u] = Vec<DT, VEC>::get(dy, base + (long long)(i0 + u * TY) * c);
       }
 #pragma unroll
     for (int u = 0; u < L; ++u)
       if (i0 + u * TY < e) {
         float a[VEC];
-        Vec<DT, VEC>::unpack(rx[u], a);
+        x.unpack(rx[u], a);
         if constexpr (FWD) {
 #pragma unroll
           for (int k = 0; k < VEC; ++k) a[k] = act_value(fmaf(a[k] - mean[k], f[k], be[k]), ACT);
@@ -279,7 +232,7 @@ __device__ __forceinline__ bool last_to_arrive(const NormParams& p, long long s)
 }
 
 // Sums of one slab.  Dynamic shared memory: forward [TY][c/VEC][3], backward [TY][c][2] floats.
-template <int DT, int VEC, int ACT, bool FWD>
+template <int DT, int VEC, int ACT, bool FWD, bool K8>
 __global__ void __launch_bounds__(kThreads) norm_sums_kernel(const NormParams p) {
   extern __shared__ float sm[];
   chained_launch();
@@ -305,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) norm_sums_kernel(const NormParams p)
           ga[k] = __ldg(p.gamma + v * VEC + k); be[k] = __ldg(p.beta + v * VEC + k);
           sb[k] = sg[k] = 0.f;
         }
-        sum_gradients<DT, VEC, ACT>(p.x, p.dy, base + v * VEC, p0 + ty, p1, p.c, p.TY, mean, rstd, ga, be, sb, sg);
+        sum_gradients<DT, VEC, ACT, K8>(XVectors<DT, VEC, K8>(p, s, v * VEC), p.dy, base + v * VEC, p0 + ty, p1, p.c, p.TY, mean, rstd, ga, be, sb, sg);
         float* e = sm + 2 * ((size_t)ty * p.c + v * VEC);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { e[2 * k] = sb[k]; e[2 * k + 1] = sg[k]; }
@@ -410,7 +363,7 @@ __global__ void __launch_bounds__(256) norm_param_kernel(const NormParams p) {
 
 // The values.  A vector may hold channels of several groups.  Backward: the first p.param_blocks CTAs form the
 // parameters' gradients instead.
-template <int DT, int VEC, int ACT, bool FWD>
+template <int DT, int VEC, int ACT, bool FWD, bool K8>
 __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p) {
   chained_launch();
   if constexpr (!FWD) {
@@ -438,7 +391,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p
       mean[k] = st.x; rstd[k] = st.y; m0[k] = ms.x; m1[k] = ms.y;
       ga[k] = __ldg(p.gamma + v * VEC + k); be[k] = __ldg(p.beta + v * VEC + k);
     }
-    write_values<DT, VEC, ACT, FWD>(p.x, p.dy, p.out, base + v * VEC, p0 + ty, p1, p.c, p.TY, mean, rstd, m0, m1, ga, be);
+    write_values<DT, VEC, ACT, FWD, K8>(XVectors<DT, VEC, K8>(p, s, v * VEC), p.dy, p.out, base + v * VEC, p0 + ty, p1, p.c, p.TY, mean, rstd, m0, m1, ga, be);
   }
 }
 
@@ -446,7 +399,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p
 // multiple of the number of blocks, so a CTA keeps its channels.  Dynamic shared memory: [TY][cb/VEC][3] or, backward,
 // [TY][cb][2], then [groups of a block][2].
 constexpr int kSampleThreads = 512;
-template <int DT, int VEC, int ACT, bool FWD>
+template <int DT, int VEC, int ACT, bool FWD, bool K8>
 __global__ void __launch_bounds__(kSampleThreads, 2) norm_sample_kernel(const NormParams p) {
   extern __shared__ float sm[];
   constexpr int NS = FWD ? 3 : 2;
@@ -481,7 +434,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) norm_sample_kernel(const No
         float mean[VEC], rstd[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { mean[k] = given.x; rstd[k] = given.y; }
-        sum_gradients<DT, VEC, ACT>(p.x, p.dy, base, ty, p.pix, p.c, p.TY, mean, rstd, ga, be, sb, sg);
+        sum_gradients<DT, VEC, ACT, K8>(XVectors<DT, VEC, K8>(p, s, ch0), p.dy, base, ty, p.pix, p.c, p.TY, mean, rstd, ga, be, sb, sg);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
           cb[k] += sb[k]; cg[k] += sg[k];
@@ -523,7 +476,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) norm_sample_kernel(const No
         mean[k] = FWD ? t0 : given.x; rstd[k] = FWD ? t1 : given.y;
         m0[k] = t0; m1[k] = t1;
       }
-      write_values<DT, VEC, ACT, FWD>(p.x, p.dy, p.out, base, ty, p.pix, p.c, p.TY, mean, rstd, m0, m1, ga, be);
+      write_values<DT, VEC, ACT, FWD, K8>(XVectors<DT, VEC, K8>(p, s, ch0), p.dy, p.out, base, ty, p.pix, p.c, p.TY, mean, rstd, m0, m1, ga, be);
     }
     // (the next sample's sums go to `sm`, which was read before the second barrier; `st` is written after another one)
   }
@@ -649,9 +602,9 @@ NormPlan plan_norm(const dk_norm& q) {
 constexpr int kMaxSmem = 3 * kMaxC * (int)sizeof(float);
 
 // whole samples: one launch, and one for the parameters' gradients
-template <int DT, int VEC, int ACT, bool FWD>
+template <int DT, int VEC, int ACT, bool FWD, bool K8>
 dk_status run_sample(NormParams p, const NormPlan& pl, int device, int sms, cudaStream_t st) {
-  auto kern = norm_sample_kernel<DT, VEC, ACT, FWD>;
+  auto kern = norm_sample_kernel<DT, VEC, ACT, FWD, K8>;
   p.TX = pl.sTX; p.TY = pl.sTY; p.cb = pl.cb;
   const int nblk = p.c / p.cb;
   const size_t smem =
@@ -672,9 +625,9 @@ dk_status run_sample(NormParams p, const NormPlan& pl, int device, int sms, cuda
 }
 
 // slabs: sums (forward with vectors within a group, backward per channel), then values
-template <int DT, int VEC, int ACT, bool FWD>
+template <int DT, int VEC, int ACT, bool FWD, bool K8>
 dk_status run_sums(NormParams p, const NormPlan& pl, int device, cudaStream_t st) {
-  auto kern = norm_sums_kernel<DT, VEC, ACT, FWD>;
+  auto kern = norm_sums_kernel<DT, VEC, ACT, FWD, K8>;
   p.TX = pl.TX[FWD ? 0 : 1]; p.TY = pl.TY[FWD ? 0 : 1];
   size_t smem = FWD ? (size_t)3 * p.TY * (p.c / VEC) : (size_t)2 * p.TY * p.c;
   if (!FWD && smem < (size_t)2 * kThreads) smem = 2 * kThreads;
@@ -687,12 +640,12 @@ dk_status run_sums(NormParams p, const NormPlan& pl, int device, cudaStream_t st
   return launch_chained(kern, dim3((unsigned)(p.n * p.slabs)), kThreads, smem, st, p) == cudaSuccess ? DK_OK
                                                                                                      : DK_ERR_CUDA;
 }
-template <int DT, int VEC, int ACT, bool FWD>
+template <int DT, int VEC, int ACT, bool FWD, bool K8>
 dk_status run_apply(NormParams p, const NormPlan& pl, cudaStream_t st) {
   p.TX = pl.TX[1]; p.TY = pl.TY[1];
   p.rows = p.n;
   p.param_blocks = FWD ? 0 : (p.c + 15) / 16;
-  return launch_chained(norm_apply_kernel<DT, VEC, ACT, FWD>, dim3((unsigned)(p.n * p.slabs + p.param_blocks)), kThreads, 0,
+  return launch_chained(norm_apply_kernel<DT, VEC, ACT, FWD, K8>, dim3((unsigned)(p.n * p.slabs + p.param_blocks)), kThreads, 0,
                         st, p) == cudaSuccess
              ? DK_OK
              : DK_ERR_CUDA;
@@ -717,31 +670,31 @@ dk_status run_apply(NormParams p, const NormPlan& pl, cudaStream_t st) {
     DK_NORM_ACTS(DK_BF16, 1, CALL);                                     \
   } while (0)
 
-template <bool FWD>
+template <bool FWD, bool K8>
 dk_status dispatch_sample(const NormParams& p, const NormPlan& pl, int dtype, int device, int sms, cudaStream_t st) {
-#define DK_NORM_CALL(DT, V, ACT) run_sample<DT, V, ACT, FWD>(p, pl, device, sms, st)
+#define DK_NORM_CALL(DT, V, ACT) run_sample<DT, V, ACT, FWD, K8>(p, pl, device, sms, st)
   DK_NORM_TYPES(pl.vec, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
-template <bool FWD>
+template <bool FWD, bool K8>
 dk_status dispatch_sums(const NormParams& p, const NormPlan& pl, int dtype, int device, cudaStream_t st) {
-#define DK_NORM_CALL(DT, V, ACT) run_sums<DT, V, FWD ? DK_ACT_NONE : ACT, FWD>(p, pl, device, st)
+#define DK_NORM_CALL(DT, V, ACT) run_sums<DT, V, FWD ? DK_ACT_NONE : ACT, FWD, K8>(p, pl, device, st)
   DK_NORM_TYPES(FWD ? pl.vec : pl.wide, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
-template <bool FWD>
+template <bool FWD, bool K8>
 dk_status dispatch_apply(const NormParams& p, const NormPlan& pl, int dtype, cudaStream_t st) {
-#define DK_NORM_CALL(DT, V, ACT) run_apply<DT, V, ACT, FWD>(p, pl, st)
+#define DK_NORM_CALL(DT, V, ACT) run_apply<DT, V, ACT, FWD, K8>(p, pl, st)
   DK_NORM_TYPES(pl.wide, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
 
-template <bool FWD>
+template <bool FWD, bool K8>
 dk_status dispatch(const NormParams& p, const NormPlan& pl, int dtype, int device, int sms, cudaStream_t st) {
-  if (pl.sample[FWD ? 0 : 1]) return dispatch_sample<FWD>(p, pl, dtype, device, sms, st);
+  if (pl.sample[FWD ? 0 : 1]) return dispatch_sample<FWD, K8>(p, pl, dtype, device, sms, st);
   if (p.n > kStepCounters) DK_CUDA_CHECK(cudaMemsetAsync(p.count, 0, (size_t)p.n * sizeof(unsigned int), st));
-  const dk_status s = dispatch_sums<FWD>(p, pl, dtype, device, st);
-  return s == DK_OK ? dispatch_apply<FWD>(p, pl, dtype, st) : s;
+  const dk_status s = dispatch_sums<FWD, K8>(p, pl, dtype, device, st);
+  return s == DK_OK ? dispatch_apply<FWD, K8>(p, pl, dtype, st) : s;
 }
 
 dk_status begin(dk_ctx* ctx, const dk_norm* q, NormPlan* pl, NormParams* p) {
@@ -763,30 +716,16 @@ dk_status begin(dk_ctx* ctx, const dk_norm* q, NormPlan* pl, NormParams* p) {
 // kernels of a call, for the launch counters
 int launches(const NormPlan& pl, bool fwd) { return pl.sample[fwd ? 0 : 1] && fwd ? 1 : 2; }
 
-}  // namespace
-}  // namespace dk
-
-using namespace dk;
-
-extern "C" {
-
-dk_status dk_norm_workspace_bytes(const dk_norm* q, size_t* bytes) {
-  if (!bytes) return DK_ERR_INVALID_ARG;
-  dk_status s = check_norm(q);
-  if (s != DK_OK) return s;
-  *bytes = plan_norm(*q).total;
-  return DK_OK;
-}
-
-dk_status dk_group_norm_fwd(dk_ctx* ctx, const dk_norm* q, const void* x, const float* gamma, const float* beta,
-                            void* y, float* stats, void* stream) {
+// kept: a checkpoint of x is written too
+dk_status norm_forward(dk_ctx* ctx, const dk_norm* q, const void* x, const float* gamma, const float* beta, void* y,
+                       float* stats, void* ckpt, bool kept, void* stream) {
   dk_status s = check_norm(q);
   if (s != DK_OK) return s;
   if (!ctx) return DK_ERR_INVALID_ARG;
   if (q->n == 0) return DK_OK;              // (tensors without elements may be NULL)
-  if (!x || !gamma || !beta || !y || !stats) return DK_ERR_INVALID_ARG;
+  if (!x || !gamma || !beta || !y || !stats || (kept && !ckpt)) return DK_ERR_INVALID_ARG;
   if (!aligned_to(x, 16) || !aligned_to(y, 16) || !aligned_to(gamma, 16) || !aligned_to(beta, 16) ||
-      !aligned_to(stats, 16))
+      !aligned_to(stats, 16) || !aligned_to(ckpt, 16))
     return DK_ERR_INVALID_ARG;
   NormPlan pl;
   NormParams p = {};
@@ -796,13 +735,19 @@ dk_status dk_group_norm_fwd(dk_ctx* ctx, const dk_norm* q, const void* x, const 
   if (!dev.ok) return DK_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.x = x; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats;
-  ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, true), st);
-  return dispatch<true>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
+  ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, true) + (kept ? 1 : 0), st);
+  if (kept) {                                   // (first: y may be x)
+    const dk_ckpt8 k{q->n * p.pix, q->c, q->dtype};
+    s = launch_ckpt8(k, true, x, nullptr, ckpt, ctx->sm_count, st);
+    if (s != DK_OK) return s;
+  }
+  return dispatch<true, false>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
 }
 
-dk_status dk_group_norm_bwd(dk_ctx* ctx, const dk_norm* q, const void* dy, const void* x, const float* gamma,
-                            const float* beta, const float* stats, void* dx, float* dgamma, float* dbeta,
-                            void* stream) {
+// K8: x is a checkpoint
+template <bool K8>
+dk_status norm_backward(dk_ctx* ctx, const dk_norm* q, const void* dy, const void* x, const float* gamma,
+                        const float* beta, const float* stats, void* dx, float* dgamma, float* dbeta, void* stream) {
   dk_status s = check_norm(q);
   if (s != DK_OK) return s;
   if (!ctx || !dgamma || !dbeta) return DK_ERR_INVALID_ARG;
@@ -822,10 +767,54 @@ dk_status dk_group_norm_bwd(dk_ctx* ctx, const dk_norm* q, const void* dy, const
   NormParams p = {};
   s = begin(ctx, q, &pl, &p);
   if (s != DK_OK) return s;
-  p.x = x; p.dy = dy; p.out = dx; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float*>(stats);
+  if (K8) {
+    p.dp = ckpt8::padded(q->c);
+    p.codes = static_cast<const uint8_t*>(x);
+    p.exps = p.codes + ckpt8::code_bytes(q->n * p.pix, q->c);
+  } else {
+    p.x = x;
+  }
+  p.dy = dy; p.out = dx; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float*>(stats);
   p.dgamma = dgamma; p.dbeta = dbeta;
   ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, false), st);
-  return dispatch<false>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
+  return dispatch<false, K8>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
+}
+
+}  // namespace
+}  // namespace dk
+
+using namespace dk;
+
+extern "C" {
+
+dk_status dk_norm_workspace_bytes(const dk_norm* q, size_t* bytes) {
+  if (!bytes) return DK_ERR_INVALID_ARG;
+  dk_status s = check_norm(q);
+  if (s != DK_OK) return s;
+  *bytes = plan_norm(*q).total;
+  return DK_OK;
+}
+
+dk_status dk_group_norm_fwd(dk_ctx* ctx, const dk_norm* q, const void* x, const float* gamma, const float* beta,
+                            void* y, float* stats, void* stream) {
+  return norm_forward(ctx, q, x, gamma, beta, y, stats, nullptr, false, stream);
+}
+
+dk_status dk_group_norm_fwd_ckpt8(dk_ctx* ctx, const dk_norm* q, const void* x, const float* gamma, const float* beta,
+                                  void* y, float* stats, void* ckpt, void* stream) {
+  return norm_forward(ctx, q, x, gamma, beta, y, stats, ckpt, true, stream);
+}
+
+dk_status dk_group_norm_bwd(dk_ctx* ctx, const dk_norm* q, const void* dy, const void* x, const float* gamma,
+                            const float* beta, const float* stats, void* dx, float* dgamma, float* dbeta,
+                            void* stream) {
+  return norm_backward<false>(ctx, q, dy, x, gamma, beta, stats, dx, dgamma, dbeta, stream);
+}
+
+dk_status dk_group_norm_bwd_ckpt8(dk_ctx* ctx, const dk_norm* q, const void* dy, const void* ckpt, const float* gamma,
+                                  const float* beta, const float* stats, void* dx, float* dgamma, float* dbeta,
+                                  void* stream) {
+  return norm_backward<true>(ctx, q, dy, ckpt, gamma, beta, stats, dx, dgamma, dbeta, stream);
 }
 
 }  // extern "C"

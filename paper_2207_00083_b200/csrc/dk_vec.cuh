@@ -1,0 +1,92 @@
+// Vectors of consecutive fp32 or bf16 elements, and moments of values: shared by the normalisations.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "dk.h"
+
+namespace dk {
+
+// VEC consecutive elements: as stored (Raw, one access of at most 16 bytes) and as fp32
+template <int DT, int VEC>
+struct Vec {
+  static constexpr int BYTES = VEC * (DT == DK_F32 ? 4 : 2);
+  using Raw = typename std::conditional<
+      BYTES == 16, uint4,
+      typename std::conditional<BYTES == 8, uint2,
+                                typename std::conditional<BYTES == 4, uint32_t, uint16_t>::type>::type>::type;
+  static __device__ __forceinline__ Raw get(const void* base, long long e) {
+    return *reinterpret_cast<const Raw*>(static_cast<const char*>(base) + e * (BYTES / VEC));
+  }
+  static __device__ __forceinline__ void put(void* base, long long e, const Raw r) {
+    *reinterpret_cast<Raw*>(static_cast<char*>(base) + e * (BYTES / VEC)) = r;
+  }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[VEC]) {
+    if constexpr (DT == DK_F32) {
+      const float* f = reinterpret_cast<const float*>(&r);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = f[i];
+    } else if constexpr (VEC == 1) {
+      v[0] = __uint_as_float((uint32_t)r << 16);
+    } else {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
+  static __device__ __forceinline__ Raw pack(const float (&v)[VEC]) {
+    Raw r;
+    if constexpr (DT == DK_F32) {
+      float* f = reinterpret_cast<float*>(&r);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = v[i];
+    } else if constexpr (VEC == 1) {
+      const __nv_bfloat16 t = __float2bfloat16_rn(v[0]);
+      r = *reinterpret_cast<const uint16_t*>(&t);
+    } else {
+      uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&t);
+      }
+    }
+    return r;
+  }
+  static __device__ __forceinline__ void load(const void* base, long long e, float (&v)[VEC]) {
+    unpack(get(base, e), v);
+  }
+  static __device__ __forceinline__ void store(void* base, long long e, const float (&v)[VEC]) { put(base, e, pack(v)); }
+};
+
+// (count, mean, sum of squared deviations) of the union of two sets
+struct Moments {
+  float n, mean, m2;
+};
+__device__ __forceinline__ Moments join(const Moments a, const Moments b) {
+  const float n = a.n + b.n;
+  if (b.n == 0.f) return a;
+  if (a.n == 0.f) return b;
+  const float d = b.mean - a.mean, f = __fdividef(b.n, n);
+  return {n, fmaf(d, f, a.mean), a.m2 + b.m2 + d * d * a.n * f};
+}
+__device__ __forceinline__ Moments warp_join(Moments m) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    Moments t;
+    t.n = __shfl_xor_sync(0xffffffffu, m.n, o);
+    t.mean = __shfl_xor_sync(0xffffffffu, m.mean, o);
+    t.m2 = __shfl_xor_sync(0xffffffffu, m.m2, o);
+    // (both lanes of a pair join in the same order)
+    m = (threadIdx.x & o) ? join(t, m) : join(m, t);
+  }
+  return m;
+}
+
+}  // namespace dk

@@ -1,0 +1,472 @@
+// Weight gradient of a linear layer from the 8-bit checkpoint of its input: dW = keep*dW + scale*dy^T.x, db likewise.
+//
+// The product contracts over rows, across which the checkpoint's powers of two change; so a block's power cannot leave the
+// sum, and the tensor cores' 8-bit formats (whose scales run along the contraction) do not apply.  But q*2^k is a bf16
+// number as it stands.  bf16: dy and x enter unrounded, one product.  fp32: dy as two fp16 terms under a power of two of
+// each output (its column of dy, its row of dW), x as one fp16 plane under a power of two of the whole checkpoint (q*2^k
+// is an fp16 number for 33 powers of two, subnormals included), two products.
+//   wgrad8_columns_kernel: sums (for db) and largest magnitudes of dy's columns, the checkpoint's largest exponent
+//   wgrad8_prep_kernel: the operands, and db
+//   the product (dk_gemm16.cuh), both operands read across their rows in place
+#include <math.h>
+
+#include "dk_ckpt8.cuh"
+#include "dk_gemm16.cuh"
+#include "dk_vec.cuh"
+
+namespace dk {
+namespace {
+
+using g16::magnitude;
+using g16::Operand;
+using g16::Params;
+using g16::pow2;
+using g16::scale_exp;
+
+constexpr int kThreads = 256;
+constexpr int kMaxParts = 64;            // parts of the rows in which columns are summed
+constexpr int kMaxBlocks = 1024;         // of wgrad8_columns_kernel that look at the exponents
+
+struct Wg8 {
+  const void* dy;
+  const uint8_t* codes;
+  const uint8_t* exps;
+  void* x16;                 // [rows][dp]
+  void* hi;                  // [rows][op] (dy's terms, or a copy with whole pitch)
+  void* lo;
+  float* sums;               // [parts][out]
+  unsigned int* most;        // [parts][out]; then [out] of all
+  unsigned int* most_all;
+  unsigned int* block_exp;   // [columns blocks]: largest exponent; block_exp[kMaxBlocks]: of all
+  float* db;
+  long long rows;
+  int d, dp, out, op, parts, blocks, copy_dy;
+  float scale, keep;
+};
+
+// the checkpoint's power of two: its largest step becomes 2^8, so the largest value is below 2^15
+__device__ __forceinline__ int x_exp(unsigned int largest) {
+  const int s = 8 - ((int)largest - 127);
+  return largest == 0u ? 0 : min(s, 126);
+}
+
+// grid (strips of 32 vectors, parts of the rows)
+template <int DT, int VEC>
+__global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
+  chained_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = (blockIdx.x * 32 + lane) * VEC;
+  const long long per = (a.rows + a.parts - 1) / a.parts;
+  const long long r0 = blockIdx.y * per, r1 = min(a.rows, r0 + per);
+  float s[VEC];
+  unsigned int m[VEC];
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) { s[k] = 0.f; m[k] = 0u; }
+  if (c < a.out) {
+    constexpr int U = 4;
+    for (long long r = r0 + warp; r < r1; r += 8 * U) {
+      typename Vec<DT, VEC>::Raw raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (r + 8 * u < r1) raw[u] = Vec<DT, VEC>::get(a.dy, (r + 8 * u) * a.out + c);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (r + 8 * u < r1) {
+          float v[VEC];
+          Vec<DT, VEC>::unpack(raw[u], v);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            s[k] += v[k];
+            if (DT == DK_F32) m[k] = max(m[k], magnitude(__float_as_uint(v[k])));
+          }
+        }
+    }
+  }
+  __shared__ float ss[8][32 * VEC + 1];
+  __shared__ unsigned int sm[DT == DK_F32 ? 8 : 1][32 * VEC + 1];
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) {
+    ss[warp][lane * VEC + k] = s[k];
+    if (DT == DK_F32) sm[warp][lane * VEC + k] = m[k];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * VEC; i += kThreads) {
+    const int col = blockIdx.x * 32 * VEC + i;
+    if (col >= a.out) continue;
+    float t = 0.f;
+    unsigned int u = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      t += ss[w][i];
+      if (DT == DK_F32) u = max(u, sm[w][i]);
+    }
+    a.sums[(long long)blockIdx.y * a.out + col] = t;
+    if (DT == DK_F32) a.most[(long long)blockIdx.y * a.out + col] = u;
+  }
+  if constexpr (DT == DK_F32) {
+    // this block's share of the exponents
+    const int block = blockIdx.y * gridDim.x + blockIdx.x, blocks = a.blocks;
+    if (block >= blocks) return;
+    const long long n = a.rows * (a.dp / ckpt8::kBlock);
+    unsigned int e = 0;
+    for (long long i = (long long)block * kThreads + threadIdx.x; i < n; i += (long long)blocks * kThreads) {
+      const unsigned int b = a.exps[i];
+      e = max(e, b == 255u ? 0u : b);
+    }
+    e = __reduce_max_sync(0xffffffffu, e);
+    __shared__ unsigned int se[8];
+    if (lane == 0) se[warp] = e;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+      for (int w = 1; w < 8; ++w) e = max(e, se[w]);
+      a.block_exp[block] = e;
+    }
+  }
+}
+
+// The operands.  The first CTAs take dy's columns (grid_dy of them: strips of 256 columns by row parts), the others the
+// checkpoint, eight values a thread.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int strips, int row_parts, int grid_dy,
+                                                               int with_db) {
+  chained_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if ((int)blockIdx.x < grid_dy) {
+    const int strip = blockIdx.x % strips, part = blockIdx.x / strips;
+    const int c = strip * 256 + lane * 8;
+    if (c >= a.op) return;
+    float f[8];
+    if constexpr (DT == DK_F32) {
+      unsigned int m[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m[k] = 0u;
+      for (int p = 0; p < a.parts; ++p) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c + k < a.out) m[k] = max(m[k], __ldg(a.most + (long long)p * a.out + c + k));
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        f[k] = pow2(scale_exp(m[k]));
+        if (part == 0 && warp == 0 && c + k < a.out) a.most_all[c + k] = m[k];
+      }
+    }
+    if (with_db && part == 0 && warp == 1) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < a.out) {
+          float t = 0.f;
+          for (int p = 0; p < a.parts; ++p) t += __ldg(a.sums + (long long)p * a.out + c + k);
+          t *= a.scale;
+          a.db[c + k] = a.keep != 0.f ? fmaf(a.keep, a.db[c + k], t) : t;
+        }
+    }
+    if (DT == DK_BF16 && !a.copy_dy) return;
+    for (long long r = (long long)part * 8 + warp; r < a.rows; r += (long long)row_parts * 8) {
+      if constexpr (DT == DK_F32) {
+        const float* s = static_cast<const float*>(a.dy) + r * a.out + c;
+        float v[8];
+        if (a.out % 4 == 0 && c + 8 <= a.out) {
+          const float4 x = __ldg(reinterpret_cast<const float4*>(s)), y = __ldg(reinterpret_cast<const float4*>(s) + 1);
+          v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = c + k < a.out ? __ldg(s + k) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= f[k];
+        g16::store_planes<8>(static_cast<__half*>(a.hi) + r * a.op + c, static_cast<__half*>(a.lo) + r * a.op + c, v, 8);
+      } else {
+        const uint16_t* s = static_cast<const uint16_t*>(a.dy) + r * a.out + c;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          w[k] = (c + 2 * k < a.out ? (uint32_t)s[2 * k] : 0u) | (c + 2 * k + 1 < a.out ? (uint32_t)s[2 * k + 1] << 16 : 0u);
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.hi) + r * a.op + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    return;
+  }
+  int s = 0;
+  if constexpr (DT == DK_F32) {
+    __shared__ unsigned int se[8];
+    unsigned int e = 0;
+    for (int i = threadIdx.x; i < a.blocks; i += kThreads) e = max(e, __ldg(a.block_exp + i));
+    e = __reduce_max_sync(0xffffffffu, e);
+    if (lane == 0) se[warp] = e;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) e = max(e, se[w]);
+    if ((int)blockIdx.x == grid_dy && threadIdx.x == 0) a.block_exp[kMaxBlocks] = e;
+    s = x_exp(e);
+  }
+  constexpr int U = 4;
+  const long long units = a.rows * (a.dp / 8), step = (long long)(gridDim.x - grid_dy) * kThreads;
+  for (long long i = (long long)(blockIdx.x - grid_dy) * kThreads + threadIdx.x; i < units; i += U * step) {
+    ckpt8::Raw<8> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * step < units) r[u] = ckpt8::get<8>(a.codes + (i + u * step) * 8, a.exps + (i + u * step) / 4);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u * step >= units) continue;
+      float v[8];
+      uint32_t w[4];
+      if constexpr (DT == DK_F32) {
+        if (r[u].b != 255u) r[u].b = (uint32_t)min(max((int)r[u].b + s, 0), 254);
+        ckpt8::unpack<8>(r[u], v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = g16::pack_f16(v[2 * k], v[2 * k + 1]);
+      } else {
+        ckpt8::unpack<8>(r[u], v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __byte_perm(__float_as_uint(v[2 * k]), __float_as_uint(v[2 * k + 1]), 0x7632);
+      }
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.x16) + (i + u * step) * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+// dW = keep*dW + scale*product, the operands' powers of two undone
+struct EpiW {
+  static constexpr bool kAhead = false;
+  float* dW;
+  long long pitch;
+  float scale, keep;
+  const unsigned int* most;          // fp32: of the outputs; null: nothing to undo
+  const unsigned int* x_largest;
+  // (two factors, the smaller one first: together they may leave fp32's range where the result does not)
+  __device__ __forceinline__ float undo(int row, float& second) const {
+    if (most == nullptr) return second = 1.f;
+    const float fx = pow2(-x_exp(*x_largest)), fo = pow2(-scale_exp(most[row]));
+    second = fmaxf(fx, fo);
+    return fminf(fx, fo);
+  }
+  template <int NH>
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
+    const int row0 = row - (int)(threadIdx.x & 31);
+    if (row0 >= p.M || col0 >= p.N) return;
+    float f1;
+    const float f0 = undo(min(row, p.M - 1), f1);
+#pragma unroll
+    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1 * scale;
+    const int rows = p.M - row0, cols = p.N - col0;
+    float* dst = dW + (long long)row0 * pitch + col0;
+    g16::warp_rows_f32<NH>(acc, sm, [&](int r, int c, float4 u) {
+      if (r >= rows || c >= cols) return;
+      float* to = dst + (long long)r * pitch + c;
+      if (keep != 0.f) {
+        u.x = fmaf(keep, to[0], u.x);
+        if (c + 1 < cols) u.y = fmaf(keep, to[1], u.y);
+        if (c + 2 < cols) u.z = fmaf(keep, to[2], u.z);
+        if (c + 3 < cols) u.w = fmaf(keep, to[3], u.w);
+      }
+      g16::put_piece32(to, u, cols - c);
+    });
+  }
+};
+
+// joins the slices of a contraction that was cut
+__global__ void __launch_bounds__(kThreads) wgrad8_slices_kernel(const float* __restrict__ part, int ks, int out, int d,
+                                                                 int pitch, const EpiW e) {
+  chained_launch();
+  const long long n = (long long)out * d, slice = (long long)out * pitch;
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kThreads) {
+    const int row = (int)(i / d), c = (int)(i - (long long)row * d);
+    float v = 0.f;
+    for (int k = 0; k < ks; k += 8) {            // eight loads in flight
+      float t[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = __ldg(part + min(k + j, ks - 1) * slice + (long long)row * pitch + c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v += k + j < ks ? t[j] : 0.f;
+    }
+    float f1;
+    const float f0 = e.undo(row, f1);
+    v = v * f0 * f1 * e.scale;
+    e.dW[i] = e.keep != 0.f ? fmaf(e.keep, e.dW[i], v) : v;
+  }
+}
+
+// no rows: what is left of dW and db
+__global__ void __launch_bounds__(kThreads) wgrad8_scale_kernel(float* dW, long long n, float* db, int out, float keep) {
+  chained_launch();
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n + out; i += (long long)gridDim.x * kThreads) {
+    float* at = i < n ? dW + i : db != nullptr ? db + (i - n) : nullptr;
+    if (at != nullptr) *at = keep != 0.f ? keep * *at : 0.f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+struct Plan {
+  bool f32, copy_dy;
+  int dp, op, parts, strips;         // strips: of wgrad8_columns_kernel
+  size_t off_x, off_dy, off_sums, off_most, off_all, off_exp, off_part, total;
+};
+
+constexpr size_t kPartBytes = (size_t)(kMaxSms / 2) * g16::TILE_M * 256 * sizeof(float);
+
+size_t up(size_t v) { return (v + 1023) / 1024 * 1024; }
+
+Plan plan_of(const dk_wgrad8& q) {
+  Plan p = {};
+  p.f32 = q.dtype == DK_F32;
+  p.dp = ckpt8::padded(q.d);
+  p.op = (q.out + 7) / 8 * 8;
+  p.copy_dy = p.f32 || q.out % 8 != 0;
+  int vec = p.f32 ? 4 : 8;
+  while (q.out % vec) vec /= 2;
+  p.strips = (q.out + 32 * vec - 1) / (32 * vec);
+  // parts of the rows: two CTAs for every SM, 32 rows each at least
+  long long parts = 2 * 148 / p.strips;
+  if (parts > kMaxParts) parts = kMaxParts;
+  if (parts > (q.rows + 31) / 32) parts = (q.rows + 31) / 32;
+  p.parts = parts < 1 ? 1 : (int)parts;
+  size_t off = 0;
+  auto room = [&off](size_t bytes) {
+    const size_t at = off;
+    off += up(bytes);
+    return at;
+  };
+  p.off_x = room((size_t)q.rows * p.dp * 2);
+  p.off_dy = room(p.copy_dy ? (size_t)q.rows * p.op * (p.f32 ? 4 : 2) : 0);
+  p.off_sums = room((size_t)p.parts * q.out * sizeof(float));
+  p.off_most = room(p.f32 ? (size_t)p.parts * q.out * sizeof(unsigned int) : 0);
+  p.off_all = room(p.f32 ? (size_t)q.out * sizeof(unsigned int) : 0);
+  p.off_exp = room(p.f32 ? (kMaxBlocks + 1) * sizeof(unsigned int) : 0);
+  p.off_part = room(kPartBytes);
+  p.total = off;
+  return p;
+}
+
+dk_status check(const dk_wgrad8* q) {
+  if (!q) return DK_ERR_INVALID_ARG;
+  if (q->dtype != DK_F32 && q->dtype != DK_BF16) return DK_ERR_INVALID_ARG;
+  if (q->rows < 0 || q->d < 1 || q->out < 1) return DK_ERR_SHAPE;
+  if (q->rows > (1LL << 24) || q->d > (1 << 20) || q->out > (1 << 20)) return DK_ERR_SHAPE;
+  return DK_OK;
+}
+
+template <int DT>
+cudaError_t columns(const Wg8& a, const dim3 grid, int vec, cudaStream_t st) {
+  if constexpr (DT == DK_BF16)
+    if (vec == 8) return launch_chained(wgrad8_columns_kernel<DT, 8>, grid, kThreads, 0, st, a);
+  if (vec == 4) return launch_chained(wgrad8_columns_kernel<DT, 4>, grid, kThreads, 0, st, a);
+  if (vec == 2) return launch_chained(wgrad8_columns_kernel<DT, 2>, grid, kThreads, 0, st, a);
+  return launch_chained(wgrad8_columns_kernel<DT, 1>, grid, kThreads, 0, st, a);
+}
+
+template <bool F32>
+dk_status run(dk_ctx* ctx, const dk_wgrad8& q, const Plan& pl, Wg8& a, float* dW, cudaStream_t st) {
+  constexpr int DT = F32 ? DK_F32 : DK_BF16, NP = F32 ? 2 : 1;
+  const int sms = ctx->sm_count;
+  char* ws = static_cast<char*>(ctx->ws);
+  int vec = F32 ? 4 : 8;
+  while (q.out % vec) vec /= 2;
+  if (F32 || a.db != nullptr) {
+    const dim3 grid((unsigned)pl.strips, (unsigned)pl.parts);
+    a.blocks = (int)(grid.x * grid.y < kMaxBlocks ? grid.x * grid.y : kMaxBlocks);
+    DK_CUDA_CHECK(columns<DT>(a, grid, vec, st));
+    count_launches(ctx, DK_KERNEL_OTHER, 1);
+  }
+  {
+    const int strips = (pl.op + 255) / 256;
+    long long row_parts = (q.rows + 31) / 32;
+    if (row_parts > 8LL * sms / strips) row_parts = 8LL * sms / strips;
+    if (row_parts < 1 || !pl.copy_dy) row_parts = 1;
+    const int grid_dy = pl.copy_dy || a.db != nullptr ? (int)(strips * row_parts) : 0;
+    long long grid_x = (q.rows * (pl.dp / 8) + kThreads - 1) / kThreads;
+    if (grid_x > 8LL * sms) grid_x = 8LL * sms;
+    DK_CUDA_CHECK(launch_chained(wgrad8_prep_kernel<DT>, dim3((unsigned)(grid_dy + grid_x)), kThreads, 0, st, a, strips,
+                                 (int)row_parts, grid_dy, a.db != nullptr ? 1 : 0));
+  }
+  const size_t plane = (size_t)q.rows * pl.op;
+  const Operand dy{pl.copy_dy ? (const void*)a.hi : a.dy, static_cast<const uint16_t*>(a.hi) + plane, q.rows, q.out, pl.op, 0};
+  const Operand x{a.x16, nullptr, q.rows, q.d, pl.dp, 0};
+  const g16::Tiling t = g16::plan(q.out, q.d, q.rows, 1, false, sms, NP);
+  Params p = {};
+  p.MT = t.MT; p.NT = t.NT; p.nbatch = 1; p.tiles = t.tiles;
+  p.KB = t.KB; p.ksplit = t.ksplit; p.kb_per_split = t.kb_per_split;
+  p.M = q.out; p.N = q.d;
+  p.bf16 = F32 ? 0 : 1;
+  // stages between promotions, and what the tensor pipe loses in one (sums of random sign; a third of what three products
+  // lose for each product that shares the accumulator)
+  p.chunk = F32 ? 2 : 4;
+  p.comp = (F32 ? 2.4f : 1.2f) / 16777216.f;
+  p.comp_small = 1.2f / 16777216.f;
+  const EpiW e{dW, q.d, a.scale, a.keep, F32 ? a.most_all : nullptr, F32 ? a.block_exp + kMaxBlocks : nullptr};
+  if (!t.cs && t.ksplit > 1) {
+    float* part = reinterpret_cast<float*>(ws + pl.off_part);
+    const int pitch = (q.d + 3) / 4 * 4;
+    const dk_status s = g16::launch<NP, true, true, 256>(ctx, dy, x, p, g16::EpiPartial{part, pitch}, st);
+    if (s != DK_OK) return s;
+    count_launches(ctx, DK_KERNEL_OTHER, 1);
+    long long grid = ((long long)q.out * q.d + kThreads - 1) / kThreads;
+    if (grid > 8LL * sms) grid = 8LL * sms;
+    DK_CUDA_CHECK(launch_chained(wgrad8_slices_kernel, dim3((unsigned)grid), kThreads, 0, st, part, t.ksplit, q.out, q.d, pitch, e));
+    return DK_OK;
+  }
+  return g16::product<NP, true, true>(ctx, t, dy, x, p, e, st);
+}
+
+}  // namespace
+}  // namespace dk
+
+using namespace dk;
+
+extern "C" {
+
+dk_status dk_wgrad8_workspace_bytes(const dk_wgrad8* q, size_t* bytes) {
+  if (!bytes) return DK_ERR_INVALID_ARG;
+  const dk_status s = check(q);
+  if (s != DK_OK) return s;
+  *bytes = plan_of(*q).total;
+  return DK_OK;
+}
+
+dk_status dk_linear_bwd_wgrad_ckpt8(dk_ctx* ctx, const dk_wgrad8* q, const void* dy, const void* ckpt, float scale,
+                                    float keep, float* dW, float* db, void* stream) {
+  dk_status s = check(q);
+  if (s != DK_OK) return s;
+  if (!ctx || !dW || !(scale - scale == 0.f) || !(keep - keep == 0.f)) return DK_ERR_INVALID_ARG;
+  if (q->rows > 0 && (!dy || !ckpt)) return DK_ERR_INVALID_ARG;
+  if (!aligned_to(dy, 16) || !aligned_to(ckpt, 16) || !aligned_to(dW, 16) || !aligned_to(db, 16)) return DK_ERR_INVALID_ARG;
+  OnDevice dev(ctx->device);
+  if (!dev.ok) return DK_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (q->rows == 0) {
+    long long grid = ((long long)q->out * (q->d + 1) + kThreads - 1) / kThreads;
+    if (grid > 8LL * ctx->sm_count) grid = 8LL * ctx->sm_count;
+    ProfScope ps(ctx, DK_KERNEL_OTHER, 1, st);
+    DK_CUDA_CHECK(launch_chained(wgrad8_scale_kernel, dim3((unsigned)grid), kThreads, 0, st, dW, (long long)q->out * q->d, db,
+                                 q->out, keep));
+    return DK_OK;
+  }
+  const Plan pl = plan_of(*q);
+  if (!ctx->ws || ctx->ws_bytes < pl.total) return DK_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(ctx->ws);
+  Wg8 a = {};
+  a.dy = dy;
+  a.codes = static_cast<const uint8_t*>(ckpt);
+  a.exps = a.codes + ckpt8::code_bytes(q->rows, q->d);
+  a.x16 = ws + pl.off_x;
+  a.hi = ws + pl.off_dy;
+  a.lo = static_cast<uint16_t*>(a.hi) + (size_t)q->rows * pl.op;
+  a.sums = reinterpret_cast<float*>(ws + pl.off_sums);
+  a.most = reinterpret_cast<unsigned int*>(ws + pl.off_most);
+  a.most_all = reinterpret_cast<unsigned int*>(ws + pl.off_all);
+  a.block_exp = reinterpret_cast<unsigned int*>(ws + pl.off_exp);
+  a.db = db;
+  a.rows = q->rows;
+  a.d = q->d; a.dp = pl.dp; a.out = q->out; a.op = pl.op;
+  a.parts = pl.parts;
+  a.copy_dy = pl.copy_dy;
+  a.scale = scale; a.keep = keep;
+  ProfScope ps(ctx, DK_KERNEL_OTHER, 2, st);
+  return pl.f32 ? run<true>(ctx, *q, pl, a, dW, st) : run<false>(ctx, *q, pl, a, dW, st);
+}
+
+}  // extern "C"

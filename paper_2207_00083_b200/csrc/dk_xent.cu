@@ -32,8 +32,11 @@
 namespace dk {
 namespace {
 
+using g16::magnitude;
 using g16::Operand;
 using g16::Params;
+using g16::pow2;
+using g16::scale_exp;
 
 constexpr int kRowThreads = 256;
 
@@ -45,18 +48,6 @@ struct Meta {
   uint4 block[kMaxBlocks];
 };
 
-// The power of two that brings a largest magnitude (given by its bits) to [2^14, 2^15); 1 when it is zero, infinite or
-// NaN (a forward row's own).  Undo, or the rows' inverses, take it back.
-__device__ __forceinline__ int scale_exp(unsigned int bits) {
-  const int e = (int)(bits >> 23) - 127;
-  if (bits == 0u || e > 127) return 0;
-  const int s = 14 - e;
-  return s > 126 ? 126 : s;
-}
-__device__ __forceinline__ float pow2(int e) {      // -126 <= e <= 126
-  return __int_as_float((e + 127) << 23);
-}
-
 // The power of two of a class beyond that of all p, from the bits of its largest magnitude (under the common one, below
 // 2^15).  None down to 2^-17 of the largest p: the two terms have 22 bits of the class's largest value there.
 __device__ __forceinline__ int class_exp(unsigned int bits) {
@@ -65,13 +56,6 @@ __device__ __forceinline__ int class_exp(unsigned int bits) {
 }
 
 __device__ __forceinline__ bool left_out(long long t, int vocab) { return t < 0 || t >= vocab; }
-
-// The bits of a magnitude for a maximum: an infinity or a NaN counts as nothing.  (It makes its own row's results NaN; as
-// the maximum it would leave all other rows without their power of two.)
-__device__ __forceinline__ unsigned int magnitude(unsigned int bits) {
-  bits &= 0x7fffffffu;
-  return bits < 0x7f800000u ? bits : 0u;
-}
 
 // largest magnitudes of h (rows that take part), W and dloss
 __global__ void __launch_bounds__(256)
