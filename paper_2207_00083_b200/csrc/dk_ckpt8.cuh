@@ -87,14 +87,16 @@ __device__ __forceinline__ Raw<VEC> get(const uint8_t* codes, const uint8_t* exp
   return r;
 }
 // (a code with its sign bit turned over, put into the low bits of 2^23, is 2^23 + 128 + q)
+constexpr float kBias = 8388736.f;
+template <int VEC>
+__device__ __forceinline__ float biased(const Raw<VEC>& r, int i) {
+  return __uint_as_float(__byte_perm(r.w[i / 4] ^ 0x80808080u, 0x4b000000u, 0x7540u | (uint32_t)(i & 3)));
+}
 template <int VEC>
 __device__ __forceinline__ void unpack(const Raw<VEC>& r, float (&v)[VEC]) {
   const float s = step_of(r.b);
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) {
-    const uint32_t u = __byte_perm(r.w[i / 4] ^ 0x80808080u, 0x4b000000u, 0x7540u | (uint32_t)(i & 3));
-    v[i] = (__uint_as_float(u) - 8388736.f) * s;
-  }
+  for (int i = 0; i < VEC; ++i) v[i] = (biased<VEC>(r, i) - kBias) * s;
 }
 
 // the largest magnitude (as bits) over the lanes of a block: 32/VEC neighbours
@@ -103,6 +105,7 @@ __device__ __forceinline__ uint32_t block_most(const float (&v)[VEC]) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < VEC; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  if constexpr (VEC == 1) return __reduce_max_sync(0xffffffffu, m);
 #pragma unroll
   for (int o = kBlock / VEC / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
   return m;
