@@ -588,7 +588,8 @@ DK_API dk_status dk_linear_bwd_wgrad_ckpt8(dk_ctx* ctx, const dk_wgrad8* q, cons
  * formed from it before that. */
 enum { DK_BLOCK_RMS = 0, DK_BLOCK_LAYER = 1 };
 typedef struct {
-  int64_t rows;          /* tokens, pixels (0: nothing to do; gradients of parameters are zero) */
+  int64_t rows;          /* tokens, pixels, at most 2^30 (0: nothing to do; gradients of parameters
+                            are zero)                                                */
   int32_t d;             /* features, 1 .. 16384                                     */
   int64_t rows_per_gate; /* consecutive rows that share a row of gate (>= 1)         */
   int32_t kind;          /* DK_BLOCK_RMS | DK_BLOCK_LAYER                            */

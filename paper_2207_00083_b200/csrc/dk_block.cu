@@ -21,8 +21,9 @@ namespace {
 constexpr int kMaxD = 16384;
 constexpr int kHeld = 8192;            // longest rows that are held in registers
 // Values of a thread, and threads of a CTA at most (they share out the registers).
-template <int DT>
-constexpr int kValues = DT == DK_F32 ? 8 : 16;
+// (bf16 rows of whole vectors 16: see below; of single values 8, sixteen of which spill)
+template <int DT, bool WHOLE>
+constexpr int kValues = DT == DK_BF16 && WHOLE ? 16 : 8;
 template <int DT>
 constexpr int kFwdThreads = DT == DK_F32 ? 768 : 512;
 template <int DT>
@@ -43,8 +44,7 @@ struct BlockArgs {
   float* dgate;
   float* part;             // [3][CTAs][d]: dpre, dshift, dpost
   float* part_e;           // [teams or CTAs][d]
-  long long rows, per;     // per: rows of a gate
-  long long chunk;         // rows of a team
+  int rows, per, chunk;    // per: rows of a gate; chunk: of a team
   int split;               // teams that share a gate's rows (0: a team has whole gates)
   int join_e;              // E is joined over a CTA's teams
   int d, dp, tl, teams;    // tl: threads of a team; teams: of a CTA
@@ -138,10 +138,10 @@ __device__ __forceinline__ float2 row_moments(const float (&v)[NV][VEC], const b
 template <int VEC>
 __device__ __forceinline__ void keep_vector(uint8_t* codes, uint8_t* exps, const float (&v)[VEC], long long row, int c,
                                             const BlockArgs& a, bool valid) {
-  const uint32_t b = ckpt8::exponent_byte(ckpt8::block_most<VEC>(v));
+  const ckpt8::Scale s = ckpt8::scale_of(ckpt8::block_most<VEC>(v));
   if (valid && c < a.dp) {
-    ckpt8::put_codes<VEC>(codes + row * a.dp + c, v, b);
-    if (c % ckpt8::kBlock == 0) exps[row * (a.dp / ckpt8::kBlock) + c / ckpt8::kBlock] = (uint8_t)b;
+    ckpt8::put_codes<VEC>(codes + row * a.dp + c, v, s);
+    if (c % ckpt8::kBlock == 0) exps[row * (a.dp / ckpt8::kBlock) + c / ckpt8::kBlock] = (uint8_t)s.byte;
   }
 }
 
@@ -266,10 +266,10 @@ __global__ void __launch_bounds__(1024) block_bwd_wide_kernel(const BlockArgs a)
   if (a.split) {
     const long long seg = team / a.split;
     r0 = seg * a.per + team % a.split * a.chunk;
-    r1 = min(min(r0 + a.chunk, (seg + 1) * a.per), a.rows);
+    r1 = min(min(r0 + a.chunk, (seg + 1) * a.per), (long long)a.rows);
   } else {
     r0 = team * a.chunk;
-    r1 = min(r0 + a.chunk, a.rows);
+    r1 = min(r0 + a.chunk, (long long)a.rows);
   }
   float* const my_post = a.part + (2LL * gridDim.x + blockIdx.x) * a.d;      // this CTA's sums of dpost
   for (int j = 0; j < NV; ++j) {
@@ -420,385 +420,375 @@ __device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_gr
 template <int LEFT>
 __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// a row of a tensor of `rows` rows of `bytes` bytes, 16-byte aligned, by a whole team
-__device__ __forceinline__ void copy_row(uint32_t dst, const void* base, long long row, int bytes, long long rows, int lane,
-                                         int tl) {
-  const long long at = row * bytes, from = at & ~15LL;
-  const int n = ((int)(at & 15) + bytes + 15) >> 4;
-  const char* src = static_cast<const char*>(base) + from;
-  for (int i = lane; i < n; i += tl) {
-    const long long left = rows * bytes - from - i * 16LL;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * 16), "l"(src + i * 16),
-                 "r"(left >= 16 ? 16 : (int)left)
-                 : "memory");
-  }
-}
 __host__ __device__ inline int row_room(int bytes) { return (bytes + 15 + 15) / 16 * 16; }
-
-// A team and a thread's place in it.  Its values: VEC at a time, 2 * P/VEC vectors tl*VEC apart; as pairs in that order.
-struct Team {
-  int lane, tl, warps;         // warps: of a team that is the CTA, else 0
-  float* sm;                   // [2][2*kMostWarps], zero behind the team's warps
-  int turn;
-};
-__device__ __forceinline__ void team_sync(const Team& t) {
-  if (t.warps) __syncthreads(); else __syncwarp();
-}
-__device__ __forceinline__ float team_sum1(float x, Team& t) {
-  if (t.tl < 32) {
-    for (int o = t.tl >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if (t.warps == 0) return x;
-  float* s = t.sm + t.turn * 2 * kMostWarps;
-  t.turn ^= 1;
-  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
-  __syncthreads();
-  F2 y = f2(0.f);
-#pragma unroll
-  for (int w = 0; w < kMostWarps; w += 4)
-    if (w < t.warps) {
-      const float4 v = *reinterpret_cast<const float4*>(s + w);
-      y = y + (f2(v.x, v.y) + f2(v.z, v.w));
-    }
-  return sum(y);
-}
-__device__ __forceinline__ void team_sum2(float& a, float& b, Team& t) {
-  if (t.tl < 32) {
-    for (int o = t.tl >> 1; o > 0; o >>= 1) {
-      a += __shfl_xor_sync(0xffffffffu, a, o);
-      b += __shfl_xor_sync(0xffffffffu, b, o);
-    }
-    return;
-  }
-  const int lane = threadIdx.x & 31;
-  const bool upper = lane & 16;      // the lower half of the warp goes on with a, the upper with b
-  float x = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if (t.warps == 0) {
-    const float y = __shfl_xor_sync(0xffffffffu, x, 16);
-    a = upper ? y : x;
-    b = upper ? x : y;
-    return;
-  }
-  float* s = t.sm + t.turn * 2 * kMostWarps;
-  t.turn ^= 1;
-  if ((lane & 15) == 0) s[(threadIdx.x >> 5) * 2 + (lane >> 4)] = x;
-  __syncthreads();
-  F2 y = f2(0.f);
-#pragma unroll
-  for (int w = 0; w < kMostWarps; w += 2)
-    if (w < t.warps) {
-      const float4 v = *reinterpret_cast<const float4*>(s + 2 * w);
-      y = y + (f2(v.x, v.y) + f2(v.z, v.w));
-    }
-  const float2 r = split(y);
-  a = r.x;
-  b = r.y;
-}
-
-template <int VEC>
-__device__ __forceinline__ int column(int e, const Team& t) { return ((e / VEC) * t.tl + t.lane) * VEC + e % VEC; }
-
-template <int DT, int VEC, int P>
-__device__ __forceinline__ void take(const char* row, const Team& t, int d, F2 (&v)[P]) {
-  float x[2 * P];
-#pragma unroll
-  for (int e = 0; e < 2 * P; e += VEC) {
-    const int c = column<VEC>(e, t);
-    float y[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) y[k] = 0.f;
-    if (c < d) Vec<DT, VEC>::load(row, c, y);
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) x[e + k] = y[k];
-  }
-#pragma unroll
-  for (int i = 0; i < P; ++i) v[i] = f2(x[2 * i], x[2 * i + 1]);
-}
-// A row of a checkpoint: the codes as numbers (WHOLE: and each vector's step, else each value's).
-template <int VEC, int P>
-__device__ __forceinline__ void take_codes(const char* codes, const char* exps, const Team& t, int dp, F2 (&v)[P]) {
-#pragma unroll
-  for (int e = 0; e < 2 * P; e += (VEC > 1 ? VEC : 2)) {
-    if constexpr (VEC > 1) {
-      const int c = column<VEC>(e, t);
-      ckpt8::Raw<VEC> r = {};
-      if (c < dp)
-        r = ckpt8::get<VEC>(reinterpret_cast<const uint8_t*>(codes) + c, reinterpret_cast<const uint8_t*>(exps) + c / ckpt8::kBlock);
-      const F2 step = f2(ckpt8::step_of(r.b));
-#pragma unroll
-      for (int k = 0; k < VEC; k += 2)
-        v[(e + k) / 2] = (f2(ckpt8::biased<VEC>(r, k), ckpt8::biased<VEC>(r, k + 1)) + f2(-ckpt8::kBias)) * step;
-    } else {
-      float x[2], s[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int c = column<1>(e + k, t);
-        ckpt8::Raw<1> r = {};
-        if (c < dp)
-          r = ckpt8::get<1>(reinterpret_cast<const uint8_t*>(codes) + c, reinterpret_cast<const uint8_t*>(exps) + c / ckpt8::kBlock);
-        x[k] = ckpt8::biased<1>(r, 0);
-        s[k] = ckpt8::step_of(r.b);
-      }
-      v[e / 2] = (f2(x[0], x[1]) + f2(-ckpt8::kBias)) * f2(s[0], s[1]);
-    }
-  }
-}
-template <int DT, int VEC, int P>
-__device__ __forceinline__ void give(void* base, long long row, const Team& t, int d, const F2 (&v)[P]) {
-  char* const to = static_cast<char*>(base) + row * d * (DT == DK_F32 ? 4 : 2);
-#pragma unroll
-  for (int e = 0; e < 2 * P; e += VEC) {
-    const int c = column<VEC>(e, t);
-    if (c >= d) continue;
-    float y[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const float2 p = split(v[(e + k) / 2]);
-      y[k] = (e + k) & 1 ? p.y : p.x;
-    }
-    Vec<DT, VEC>::store(to, c, y);
-  }
-}
-// a parameter's values of this thread (0 behind the row; null: `otherwise`)
-template <int VEC, int P>
-__device__ __forceinline__ void take_param(const float* p, const Team& t, int d, float otherwise, F2 (&v)[P]) {
-  float x[2 * P];
-#pragma unroll
-  for (int e = 0; e < 2 * P; e += VEC) {
-    const int c = column<VEC>(e, t);
-    float y[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) y[k] = c < d ? otherwise : 0.f;
-    if (c < d && p != nullptr) load_param<VEC>(p, c, y);
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) x[e + k] = y[k];
-  }
-#pragma unroll
-  for (int i = 0; i < P; ++i) v[i] = f2(x[2 * i], x[2 * i + 1]);
-}
-// a thread's values to fp32 `to`, which only it reads again or which is a part of the sums over rows
-template <int VEC, int P>
-__device__ __forceinline__ void give_sums(float* to, const Team& t, int d, const F2 (&v)[P]) {
-#pragma unroll
-  for (int e = 0; e < 2 * P; e += VEC) {
-    const int c = column<VEC>(e, t);
-    if (c >= d) continue;
-    if constexpr (VEC == 1) {
-      const float2 y = split(v[e / 2]);
-      to[c] = e & 1 ? y.y : y.x;
-    } else if constexpr (VEC == 2) {
-      *reinterpret_cast<float2*>(to + c) = split(v[e / 2]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < VEC; k += 4) {
-        const float2 x = split(v[(e + k) / 2]), y = split(v[(e + k) / 2 + 1]);
-        *reinterpret_cast<float4*>(to + c + k) = make_float4(x.x, x.y, y.x, y.y);
-      }
-    }
-  }
-}
-// (from shared memory: what give_sums has put there)
-template <int VEC, int P>
-__device__ __forceinline__ void take_own(const float* p, const Team& t, int d, F2 (&v)[P]) {
-#pragma unroll
-  for (int e = 0; e < 2 * P; e += (VEC > 1 ? VEC : 2)) {
-    const int c = column<VEC>(e, t);
-    if constexpr (VEC == 2) {
-      float2 x = make_float2(0.f, 0.f);
-      if (c < d) x = *reinterpret_cast<const float2*>(p + c);
-      v[e / 2] = f2(x.x, x.y);
-    } else if constexpr (VEC > 2) {
-#pragma unroll
-      for (int k = 0; k < VEC; k += 4) {
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < d) x = *reinterpret_cast<const float4*>(p + c + k);
-        v[(e + k) / 2] = f2(x.x, x.y);
-        v[(e + k) / 2 + 1] = f2(x.z, x.w);
-      }
-    } else {
-      const int c1 = column<1>(e + 1, t);
-      v[e / 2] = f2(c < d ? p[c] : 0.f, c1 < d ? p[c1] : 0.f);
-    }
-  }
-}
-// gate*post*scale
-template <int VEC, int P>
-__device__ __forceinline__ void take_factors(const BlockArgs& a, long long seg, const Team& t, F2 (&gps)[P]) {
-  F2 g[P];
-  take_param<VEC>(a.gate != nullptr ? a.gate + seg * a.d : nullptr, t, a.d, 1.f, g);
-  take_param<VEC>(a.post, t, a.d, 0.f, gps);
-#pragma unroll
-  for (int i = 0; i < P; ++i) gps[i] = gps[i] * g[i] * f2(a.scale);
-}
-// the next gate's row on its way into L2
-__device__ __forceinline__ void fetch_gate(const BlockArgs& a, long long seg, const Team& t) {
-  for (int c = t.lane * 32; c < a.d; c += t.tl * 32)
-    asm volatile("prefetch.global.L2 [%0];" ::"l"(a.gate + seg * a.d + c));
-}
 
 // 1/sqrt(x): the instruction's 22 bits and one step of Newton's method
 __device__ __forceinline__ float inverse_root(float x) {
   const float r = rsqrtf(x);
   return x > 1e-36f && x < 1e36f ? fmaf(r * 0.5f, fmaf(-x * r, r, 1.f), r) : 1.f / sqrtf(x);
 }
-// (x - mean) in place of x, and 1/sqrt(variance + eps)
-template <int VEC, int P>
-__device__ __forceinline__ float2 normalise(F2 (&v)[P], const BlockArgs& a, bool ragged, Team& t) {
-  float mean = 0.f;
-  if (a.layer) {
-    F2 s = v[0];
+
+// A team and a thread's place in it.  Its N values: NV vectors of VEC, tl*VEC apart; as P pairs in that order.
+// FULL: every thread of every team has all of its values (whole warps; rows are multiples of 32*N values).
+template <int DT, int VEC, bool FULL>
+struct Team {
+  static constexpr int ES = DT == DK_F32 ? 4 : 2;
+  static constexpr bool WHOLE = VEC * ES == 16;      // rows of whole 16-byte vectors
+  static constexpr int N = kValues<DT, WHOLE>, NV = N / VEC, P = N / 2;
+  using Pairs = F2[P];
+  int lane, tl, warps;         // warps: of a team that is the CTA, else 0
+  int c0, cs;                  // first column, and from one vector to the next
+  bool lives[NV];              // vectors that exist
+  bool ragged;                 // not all of them
+  float* sm;                   // [2][2*kMostWarps], zero behind the team's warps
+  int turn;
+
+  __device__ __forceinline__ Team(const BlockArgs& a, float* shared) {
+    lane = threadIdx.x % a.tl; tl = a.tl;
+    warps = a.tl > 32 ? a.tl >> 5 : 0;
+    c0 = lane * VEC; cs = tl * VEC;
 #pragma unroll
-    for (int i = 1; i < P; ++i) s = s + v[i];
-    mean = team_sum1(sum(s), t) * a.inv_d;
+    for (int j = 0; j < NV; ++j) lives[j] = column(j) < a.d;
+    ragged = !live(NV - 1);
+    sm = shared;
+    turn = 0;
+    for (int i = threadIdx.x; i < 4 * kMostWarps; i += blockDim.x) sm[i] = 0.f;
+  }
+  __device__ __forceinline__ int column(int j) const { return c0 + j * cs; }
+  __device__ __forceinline__ bool live(int j) const { return FULL || lives[j]; }
+  __device__ __forceinline__ void sync() const {
+    if (warps) __syncthreads(); else __syncwarp();
+  }
+
+  __device__ __forceinline__ float sum1(float x) {
+    if (!FULL && tl < 32) {
+      for (int o = tl >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+      return x;
+    }
 #pragma unroll
-    for (int i = 0; i < P; ++i) v[i] = v[i] + f2(-mean);
-    if (ragged) {                  // (deviations of values that do not exist count as zero)
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (warps == 0) return x;
+    float* s = sm + turn * 2 * kMostWarps;
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
+    __syncthreads();
+    F2 y = f2(0.f);
+    for (int w = 0; w < warps; w += 8) {
+      const float4 u = *reinterpret_cast<const float4*>(s + w), v = *reinterpret_cast<const float4*>(s + w + 4);
+      y = y + ((f2(u.x, u.y) + f2(u.z, u.w)) + (f2(v.x, v.y) + f2(v.z, v.w)));
+    }
+    return sum(y);
+  }
+  __device__ __forceinline__ void sum2(float& a, float& b) {
+    if (!FULL && tl < 32) {
+      for (int o = tl >> 1; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+      }
+      return;
+    }
+    const int l = threadIdx.x & 31;
+    const bool upper = l & 16;      // the lower half of the warp goes on with a, the upper with b
+    float x = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const float2 x = split(v[i]);
-        v[i] = f2(column<VEC>(2 * i, t) < a.d ? x.x : 0.f, column<VEC>(2 * i + 1, t) < a.d ? x.y : 0.f);
+    for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (warps == 0) {
+      const float y = __shfl_xor_sync(0xffffffffu, x, 16);
+      a = upper ? y : x;
+      b = upper ? x : y;
+      return;
+    }
+    float* s = sm + turn * 2 * kMostWarps;
+    turn ^= 1;
+    if ((l & 15) == 0) s[(threadIdx.x >> 5) * 2 + (l >> 4)] = x;
+    __syncthreads();
+    F2 y = f2(0.f);
+    for (int w = 0; w < warps; w += 4) {
+      const float4 u = *reinterpret_cast<const float4*>(s + 2 * w), v = *reinterpret_cast<const float4*>(s + 2 * w + 4);
+      y = y + ((f2(u.x, u.y) + f2(u.z, u.w)) + (f2(v.x, v.y) + f2(v.z, v.w)));
+    }
+    const float2 r = split(y);
+    a = r.x;
+    b = r.y;
+  }
+
+  // values of a row (in shared memory; zero where there are none)
+  __device__ __forceinline__ void take(const char* row, bool valid, Pairs& v) const {
+    float x[N];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float y[VEC];
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) y[k] = 0.f;
+      if ((FULL || valid) && live(j)) Vec<DT, VEC>::load(row, column(j), y);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) x[j * VEC + k] = y[k];
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = f2(x[2 * i], x[2 * i + 1]);
+  }
+  __device__ __forceinline__ void give(void* base, int row, int d, const Pairs& v) const {
+    char* const to = static_cast<char*>(base) + (long long)row * (d * ES);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float y[VEC];
+      vector(v, j, y);
+      if (live(j)) Vec<DT, VEC>::store(to, column(j), y);
+    }
+  }
+  static __device__ __forceinline__ void vector(const Pairs& v, int j, float (&y)[VEC]) {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const float2 p = split(v[(j * VEC + k) / 2]);
+      y[k] = (j * VEC + k) & 1 ? p.y : p.x;
+    }
+  }
+  // fp32 of this thread's columns, from global or shared memory (0 behind the row)
+  __device__ __forceinline__ void take_f32(const float* p, Pairs& v) const {
+    float x[N];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float y[VEC];
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) y[k] = 0.f;
+      if (live(j)) {
+        const float* at = p + column(j);
+        if constexpr (VEC >= 4) {
+#pragma unroll
+          for (int k = 0; k < VEC; k += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(at + k);
+            y[k] = f.x; y[k + 1] = f.y; y[k + 2] = f.z; y[k + 3] = f.w;
+          }
+        } else if constexpr (VEC == 2) {
+          const float2 f = *reinterpret_cast<const float2*>(at);
+          y[0] = f.x; y[1] = f.y;
+        } else {
+          y[0] = *at;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) x[j * VEC + k] = y[k];
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = f2(x[2 * i], x[2 * i + 1]);
+  }
+  __device__ __forceinline__ void give_f32(float* p, const Pairs& v) const {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float y[VEC];
+      vector(v, j, y);
+      if (!live(j)) continue;
+      float* at = p + column(j);
+      if constexpr (VEC >= 4) {
+#pragma unroll
+        for (int k = 0; k < VEC; k += 4) *reinterpret_cast<float4*>(at + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+      } else if constexpr (VEC == 2) {
+        *reinterpret_cast<float2*>(at) = make_float2(y[0], y[1]);
+      } else {
+        *at = y[0];
       }
     }
   }
-  F2 s = v[0] * v[0];
+  // gate*post*scale of a gate's rows
+  __device__ __forceinline__ void take_factors(const BlockArgs& a, int seg, Pairs& f) const {
+    take_f32(a.post, f);
 #pragma unroll
-  for (int i = 1; i < P; ++i) s = fma(v[i], v[i], s);
-  const float m2 = team_sum1(sum(s), t);
-  return make_float2(mean, inverse_root(fmaf(m2, a.inv_d, a.eps)));
-}
-
-// Codes and exponents of a row.
-template <int VEC, int P>
-__device__ __forceinline__ void keep_row(uint8_t* codes, uint8_t* exps, long long row, const BlockArgs& a, bool valid,
-                                         const Team& t, const F2 (&v)[P]) {
-  uint8_t* const to = codes + row * a.dp;
-  uint8_t* const to_e = exps + row * (a.dp / ckpt8::kBlock);
+    for (int i = 0; i < P; ++i) f[i] = f[i] * f2(a.scale);
+    if (a.gate != nullptr) {
+      Pairs g;
+      take_f32(a.gate + (long long)seg * a.d, g);
 #pragma unroll
-  for (int e = 0; e < 2 * P; e += VEC) {
-    if (e > 0 && (e / VEC) * t.tl * VEC >= a.dp) continue;      // (nothing of the row there, whatever the lane)
-    float x[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const float2 p = split(v[(e + k) / 2]);
-      x[k] = (e + k) & 1 ? p.y : p.x;
-    }
-    const uint32_t b = ckpt8::exponent_byte(ckpt8::block_most<VEC>(x));
-    const int c = column<VEC>(e, t);
-    if (valid && c < a.dp) {
-      ckpt8::put_codes<VEC>(to + c, x, b);
-      if (c % ckpt8::kBlock == 0) to_e[c / ckpt8::kBlock] = (uint8_t)b;
+      for (int i = 0; i < P; ++i) f[i] = f[i] * g[i];
     }
   }
-}
-
-// A tensor's row into a stage: WHOLE, by the threads that read it; else by the team.
-template <int VEC, int BYTES, int N>
-__device__ __forceinline__ void copy_own(uint32_t dst, const void* base, long long row, int n, const Team& t) {
-  // N values of a thread, VEC of BYTES bytes together, n in the row
-  const char* src = static_cast<const char*>(base) + row * n * (BYTES / VEC);
-#pragma unroll
-  for (int e = 0; e < N; e += VEC) {
-    const int c = column<VEC>(e, t);
-    if (c < n) copy_async<BYTES>(dst + c * (BYTES / VEC), src + c * (BYTES / VEC));
+  // the next gate's row on its way into L2
+  __device__ __forceinline__ void fetch_gate(const BlockArgs& a, int seg) const {
+    for (int c = lane * 32; c < a.d; c += tl * 32)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(a.gate + (long long)seg * a.d + c));
   }
-}
-template <int DT, int VEC>
-__device__ __forceinline__ void copy_tensor(uint32_t dst, const void* base, long long row, const BlockArgs& a, const Team& t) {
-  constexpr int ES = DT == DK_F32 ? 4 : 2;
-  if constexpr (VEC * ES == 16) copy_own<VEC, 16, kValues<DT>>(dst, base, row, a.d, t);
-  else copy_row(dst, base, row, a.d * ES, a.rows, t.lane, t.tl);
-}
-template <int DT, int VEC>
-__device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t* base, long long row, const BlockArgs& a, const Team& t) {
-  if constexpr (VEC >= 4) copy_own<VEC, VEC, kValues<DT>>(dst, base, row, a.dp, t);
-  else copy_row(dst, base, row, a.dp, a.rows, t.lane, t.tl);
-}
 
-__device__ __forceinline__ Team make_team(const BlockArgs& a, float* sm) {
-  Team t;
-  t.lane = threadIdx.x % a.tl; t.tl = a.tl;
-  t.warps = a.tl > 32 ? a.tl >> 5 : 0;
-  t.sm = sm;
-  t.turn = 0;
-  for (int i = threadIdx.x; i < 4 * kMostWarps; i += blockDim.x) sm[i] = 0.f;
-  return t;
-}
+  // A row of a tensor into a stage: WHOLE, by the threads that read it; else by the team, in 16-byte pieces.
+  __device__ __forceinline__ void copy_pieces(uint32_t dst, const void* base, int row, int bytes, int rows) const {
+    const long long at = (long long)row * bytes, from = at & ~15LL;
+    const int n = ((int)(at & 15) + bytes + 15) >> 4;
+    const char* src = static_cast<const char*>(base) + from;
+    // (no piece reaches beyond the tensor)
+    const int left = (int)min((long long)rows * bytes - from, (long long)n * 16);
+    for (int i = lane; i < n; i += tl)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * 16), "l"(src + i * 16),
+                   "r"(min(16, left - i * 16))
+                   : "memory");
+  }
+  __device__ __forceinline__ void copy_tensor(uint32_t dst, const void* base, int row, const BlockArgs& a) const {
+    if constexpr (WHOLE) {
+      const char* src = static_cast<const char*>(base) + (long long)row * (a.d * ES);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (live(j)) copy_async<16>(dst + column(j) * ES, src + column(j) * ES);
+    } else {
+      copy_pieces(dst, base, row, a.d * ES, a.rows);
+    }
+  }
+  __device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t* base, int row, const BlockArgs& a) const {
+    if constexpr (WHOLE) {
+      const uint8_t* src = base + (long long)row * a.dp;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (live(j)) copy_async<VEC>(dst + column(j), src + column(j));
+    } else {
+      copy_pieces(dst, base, row, a.dp, a.rows);
+    }
+  }
+  // A row of a checkpoint.  The exponents: WHOLE, fetched into registers a row ahead; else from the stage.
+  struct Bytes {
+    uint32_t b[WHOLE ? NV : 1];
+  };
+  __device__ __forceinline__ void fetch_bytes(const uint8_t* exps, int row, const BlockArgs& a, Bytes& b) const {
+    if constexpr (WHOLE) {
+      const uint8_t* e = exps + (long long)row * (a.dp / ckpt8::kBlock);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) b.b[j] = live(j) ? __ldg(e + column(j) / ckpt8::kBlock) : 0u;
+    }
+  }
+  __device__ __forceinline__ void take_codes(const char* codes, const char* exps, const Bytes& b, bool valid, Pairs& v) const {
+    float x[N], s[N];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = column(j);
+      ckpt8::Raw<VEC> r = {};
+      if ((FULL || valid) && live(j)) {
+        if constexpr (WHOLE) {
+          r = ckpt8::get_codes<VEC>(reinterpret_cast<const uint8_t*>(codes) + c);
+          r.b = b.b[j];
+        } else {
+          r = ckpt8::get<VEC>(reinterpret_cast<const uint8_t*>(codes) + c, reinterpret_cast<const uint8_t*>(exps) + c / ckpt8::kBlock);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        x[j * VEC + k] = ckpt8::biased<VEC>(r, k);
+        s[j * VEC + k] = ckpt8::step_of(r.b);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = (f2(x[2 * i], x[2 * i + 1]) + f2(-ckpt8::kBias)) * f2(s[2 * i], s[2 * i + 1]);
+  }
+  // codes and exponents of a row
+  __device__ __forceinline__ void keep_row(uint8_t* codes, uint8_t* exps, int row, const BlockArgs& a, bool valid,
+                                           const Pairs& v) const {
+    uint8_t* const to = codes + (long long)row * a.dp;
+    uint8_t* const to_e = exps + (long long)row * (a.dp / ckpt8::kBlock);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (!FULL && j > 0 && j * cs >= a.dp) continue;             // (nothing of the row there, whatever the lane)
+      float x[VEC];
+      vector(v, j, x);
+      const ckpt8::Scale s = ckpt8::scale_of(ckpt8::block_most<VEC>(x));
+      const int c = column(j);
+      if (FULL || (valid && c < a.dp)) {
+        ckpt8::put_codes<VEC>(to + c, x, s);
+        if (c % ckpt8::kBlock == 0) to_e[c / ckpt8::kBlock] = (uint8_t)s.byte;
+      }
+    }
+  }
+  // (x - mean) in place of x, and 1/sqrt(variance + eps)
+  __device__ __forceinline__ float2 normalise(Pairs& v, const BlockArgs& a) {
+    float mean = 0.f;
+    if (a.layer) {
+      F2 s = v[0];
+#pragma unroll
+      for (int i = 1; i < P; ++i) s = s + v[i];
+      mean = sum1(sum(s)) * a.inv_d;
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[i] = v[i] + f2(-mean);
+      if (ragged) {                  // (deviations of values that do not exist count as zero)
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const float2 x = split(v[i]);
+          v[i] = f2(live(2 * i / VEC) ? x.x : 0.f, live((2 * i + 1) / VEC) ? x.y : 0.f);
+        }
+      }
+    }
+    F2 s = v[0] * v[0];
+#pragma unroll
+    for (int i = 1; i < P; ++i) s = fma(v[i], v[i], s);
+    const float m2 = sum1(sum(s));
+    return make_float2(mean, inverse_root(fmaf(m2, a.inv_d, a.eps)));
+  }
+};
 
-template <int DT, int VEC>
+template <int DT, int VEC, bool FULL>
 __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const BlockArgs a) {
   constexpr int kStages = 3;
+  using T = Team<DT, VEC, FULL>;
+  constexpr int P = T::P;
   extern __shared__ __align__(16) char ring[];
   __shared__ __align__(16) float sm[4 * kMostWarps];
-  constexpr int ES = DT == DK_F32 ? 4 : 2, kPairs = kValues<DT> / 2;
-  Team t = make_team(a, sm);
+  T t(a, sm);
   const int team_in = threadIdx.x / a.tl;
-  const long long r0 = ((long long)blockIdx.x * a.teams + team_in) * a.chunk, r1 = min(a.rows, r0 + a.chunk);
-  const int bytes = a.d * ES, room = row_room(bytes), stage = 2 * room;
+  const int r0 = (int)min((long long)a.rows, ((long long)blockIdx.x * a.teams + team_in) * a.chunk), r1 = r0 + min(a.rows - r0, a.chunk);
+  const int bytes = a.d * T::ES, room = row_room(bytes), stage = 2 * room;
   char* const mine = ring + (size_t)team_in * a.team_smem;
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
   const bool branch = a.u != nullptr;
   chained_launch();
-  auto issue = [&](long long row, int slot) {
+  auto issue = [&](int row, int slot) {
     if (row < r1) {
-      copy_tensor<DT, VEC>(mine_at + slot * stage, a.h, row, a, t);
-      if (branch) copy_tensor<DT, VEC>(mine_at + slot * stage + room, a.u, row, a, t);
+      t.copy_tensor(mine_at + slot * stage, a.h, row, a);
+      if (branch) t.copy_tensor(mine_at + slot * stage + room, a.u, row, a);
     }
     copies_done();
   };
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) issue(r0 + s, s);
-  F2 gps[kPairs], pre[kPairs];
-  long long seg = branch && r0 < r1 ? r0 / a.per : 0, seg_end = (seg + 1) * a.per;
-  if (branch) take_factors<VEC>(a, seg, t, gps);
-  take_param<VEC>(a.pre, t, a.d, 0.f, pre);
-  const bool ragged = column<VEC>(2 * kPairs - 1, t) >= a.d;
+  F2 gps[P], pre[P];
+  int seg = branch && r0 < r1 ? r0 / a.per : 0;
+  long long seg_end = (long long)(seg + 1) * a.per;
+  if (branch) t.take_factors(a, seg, gps);
+  if (a.n != nullptr) t.take_f32(a.pre, pre);
   wait_copies<kStages - 2>();
-  team_sync(t);
+  t.sync();
   int slot = 0;
-  for (long long row = r0; row < r0 + a.chunk; ++row) {
-    const bool valid = row < r1;
-    if (a.tl >= 32 && !valid) break;                 // (a team of whole warps has no other team's lanes in them)
+  for (int i = 0; i < a.chunk; ++i) {
+    const int row = r0 + i;
+    const bool valid = FULL || row < r1;
+    if ((FULL || a.tl >= 32) && row >= r1) break;                 // (a team of whole warps has no other team's lanes in them)
     const char* at = mine + slot * stage;
-    const int off = VEC * ES == 16 ? 0 : (int)((row * bytes) & 15), d = valid ? a.d : 0;
+    const int off = T::WHOLE ? 0 : (int)(((long long)row * bytes) & 15);
     issue(row + kStages - 1, slot == 0 ? kStages - 1 : slot - 1);
-    F2 h[kPairs];
-    take<DT, VEC>(at + off, t, d, h);
-    if (a.kh != nullptr) keep_row<VEC>(a.kh, a.keh, row, a, valid, t, h);
+    F2 h[P];
+    t.take(at + off, valid, h);
+    if (a.kh != nullptr) t.keep_row(a.kh, a.keh, row, a, valid, h);
     float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
     if (a.n == nullptr) wait_copies<kStages - 2>();
     if (branch) {
-      F2 u[kPairs];
-      take<DT, VEC>(at + room + off, t, d, u);
-      if (a.ku != nullptr) keep_row<VEC>(a.ku, a.keu, row, a, valid, t, u);
+      F2 u[P];
+      t.take(at + room + off, valid, u);
+      if (a.ku != nullptr) t.keep_row(a.ku, a.keu, row, a, valid, u);
       if (valid && row == seg_end) {
         seg_end += a.per;
-        take_factors<VEC>(a, ++seg, t, gps);
+        t.take_factors(a, ++seg, gps);
       }
-      if (row + 1 == seg_end && row + 1 < r1) fetch_gate(a, seg + 1, t);
-      const float2 m = normalise<VEC>(u, a, ragged, t);
+      if (row + 1 == seg_end && row + 1 < r1) t.fetch_gate(a, seg + 1);
+      const float2 m = t.normalise(u, a);
       st.x = m.x; st.y = m.y;
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) h[k] = fma(f2(a.keep), h[k], gps[k] * (u[k] * f2(m.y)));
-      if (valid) give<DT, VEC>(a.h_out, row, t, a.d, h);
+      for (int k = 0; k < P; ++k) h[k] = fma(f2(a.keep), h[k], gps[k] * (u[k] * f2(m.y)));
+      if (valid) t.give(a.h_out, row, a.d, h);
     }
     if (a.n != nullptr) {
       wait_copies<kStages - 2>();
-      const float2 m = normalise<VEC>(h, a, ragged, t);
+      const float2 m = t.normalise(h, a);
       st.z = m.x; st.w = m.y;
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) h[k] = h[k] * f2(m.y) * pre[k];
+      for (int k = 0; k < P; ++k) h[k] = h[k] * f2(m.y) * pre[k];
       if (a.shift != nullptr) {
-        F2 shift[kPairs];
-        take_param<VEC>(a.shift, t, a.d, 0.f, shift);
+        F2 shift[P];
+        t.take_f32(a.shift, shift);
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) h[k] = h[k] + shift[k];
+        for (int k = 0; k < P; ++k) h[k] = h[k] + shift[k];
       }
-      if (valid) give<DT, VEC>(a.n, row, t, a.d, h);
+      if (valid) t.give(a.n, row, a.d, h);
     }
     if (a.stats != nullptr && t.lane == 0 && valid) a.stats[row] = st;
     if (t.warps == 0) __syncwarp();
@@ -807,115 +797,137 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
   wait_copies<0>();
 }
 
-// Beside the ring a team has [d] fp32 of gate*post*scale, where the teams have several gates (split = 0) of dpost, and of
-// dshift where that is asked for.
-template <int DT, int VEC, bool KEPT>
+// Beside the ring a team has [d] fp32 of gate*post*scale, of pre (from L1, which the copies pass through, each reading of it
+// stood in the row's way: 243 us for 16384 x 4096 bf16 against 182), where the teams have several gates (split = 0) of dpost, and of dshift where
+// that is asked for.
+template <int DT, int VEC, bool FULL, bool KEPT>
 __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const BlockArgs a) {
+  using T = Team<DT, VEC, FULL>;
+  constexpr int P = T::P;
   extern __shared__ __align__(16) char ring[];
   __shared__ __align__(16) float sm[4 * kMostWarps];
-  constexpr int ES = DT == DK_F32 ? 4 : 2, kPairs = kValues<DT> / 2;
-  Team t = make_team(a, sm);
+  T t(a, sm);
   const int team_in = threadIdx.x / a.tl;
   const long long team = (long long)blockIdx.x * a.teams + team_in;
-  const int bytes = a.d * ES, eb = a.dp / ckpt8::kBlock;
-  const int room = row_room(bytes), room_k = row_room(KEPT ? a.dp : bytes), room_e = KEPT ? row_room(eb) : 0;
+  const int bytes = a.d * T::ES, eb = a.dp / ckpt8::kBlock;
+  const int room = row_room(bytes), room_k = row_room(KEPT ? a.dp : bytes), room_e = KEPT && !T::WHOLE ? row_room(eb) : 0;
   // a stage: dh', dn, h, u and the exponents of both
   const int at_h = 2 * room, at_u = at_h + room_k, at_eh = at_u + room_k, at_eu = at_eh + room_e, stage = at_eu + room_e;
   const int own = row_room(a.d * 4), stages = a.stages;
   char* const mine = ring + (size_t)team_in * a.team_smem;
   float* const factors = reinterpret_cast<float*>(mine + stages * stage);
-  float* const posts = factors + own / 4;
+  float* const pres = factors + own / 4;
+  float* const posts = pres + own / 4;
   float* const shifts = a.split == 0 ? posts + own / 4 : posts;
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
   const bool branch = a.post != nullptr, norm = a.dn != nullptr;
-  long long r0, r1, seg;
-  if (a.split) {
-    seg = team / a.split;
-    r0 = seg * a.per + team % a.split * a.chunk;
-    r1 = min(min(r0 + a.chunk, (seg + 1) * a.per), a.rows);
-  } else {
-    r0 = team * a.chunk;
-    r1 = min(r0 + a.chunk, a.rows);
-    seg = r0 / a.per;
+  int r0, r1, seg;
+  {
+    long long f, e;
+    if (a.split) {
+      seg = (int)(team / a.split);
+      f = (long long)seg * a.per + (long long)(team - (long long)seg * a.split) * a.chunk;
+      e = min(min(f + a.chunk, (long long)(seg + 1) * a.per), (long long)a.rows);
+    } else {
+      f = team * a.chunk;
+      e = min(f + a.chunk, (long long)a.rows);
+      seg = (int)(f / a.per);
+    }
+    if (f >= e) { f = e = 0; seg = 0; }        // (a CTA's last teams may have nothing)
+    r0 = (int)f; r1 = (int)e;
   }
-  if (r0 >= r1) seg = 0;
-  long long seg_end = (seg + 1) * a.per;
+  long long seg_end = (long long)(seg + 1) * a.per;
   chained_launch();
-  auto issue = [&](long long row, int slot) {
+  auto issue = [&](int row, int slot) {
     if (row < r1) {
       const uint32_t to = mine_at + slot * stage;
-      if (a.dh_out != nullptr) copy_tensor<DT, VEC>(to, a.dh_out, row, a, t);
-      if (norm) copy_tensor<DT, VEC>(to + room, a.dn, row, a, t);
+      if (a.dh_out != nullptr) t.copy_tensor(to, a.dh_out, row, a);
+      if (norm) t.copy_tensor(to + room, a.dn, row, a);
       if constexpr (KEPT) {
-        copy_codes<DT, VEC>(to + at_h, a.ch, row, a, t);
-        copy_row(to + at_eh, a.eh, row, eb, a.rows, t.lane, t.tl);
+        t.copy_codes(to + at_h, a.ch, row, a);
+        if (!T::WHOLE) t.copy_pieces(to + at_eh, a.eh, row, eb, a.rows);
         if (branch) {
-          copy_codes<DT, VEC>(to + at_u, a.cu, row, a, t);
-          copy_row(to + at_eu, a.eu, row, eb, a.rows, t.lane, t.tl);
+          t.copy_codes(to + at_u, a.cu, row, a);
+          if (!T::WHOLE) t.copy_pieces(to + at_eu, a.eu, row, eb, a.rows);
         }
       } else {
-        copy_tensor<DT, VEC>(to + at_h, a.h, row, a, t);
-        if (branch) copy_tensor<DT, VEC>(to + at_u, a.u, row, a, t);
+        t.copy_tensor(to + at_h, a.h, row, a);
+        if (branch) t.copy_tensor(to + at_u, a.u, row, a);
       }
     }
     copies_done();
   };
   for (int s = 0; s < stages - 1; ++s) issue(r0 + s, s);
   const F2 zero = f2(0.f);
-  F2 E[kPairs], spre[kPairs];
+  F2 E[P], spre[P];
 #pragma unroll
-  for (int k = 0; k < kPairs; ++k) E[k] = spre[k] = zero;
+  for (int k = 0; k < P; ++k) E[k] = spre[k] = zero;
   if (branch) {
-    F2 gps[kPairs];
-    take_factors<VEC>(a, seg, t, gps);
-    give_sums<VEC>(factors, t, a.d, gps);
-    if (a.split == 0) give_sums<VEC>(posts, t, a.d, E);
+    F2 f[P];
+    t.take_factors(a, seg, f);
+    t.give_f32(factors, f);
+    if (a.split == 0) t.give_f32(posts, E);
   }
-  if (a.shifted) give_sums<VEC>(shifts, t, a.d, E);
-  float4 next = r0 < r1 ? __ldg(a.stats + r0) : make_float4(0.f, 0.f, 0.f, 0.f);
+  if (a.shifted) t.give_f32(shifts, E);
+  if (norm) {
+    F2 f[P];
+    t.take_f32(a.pre, f);
+    t.give_f32(pres, f);
+  }
+  float4 next = make_float4(0.f, 0.f, 0.f, 0.f);
+  typename T::Bytes bytes_h = {}, bytes_u = {};
+  auto fetch = [&](int row) {
+    if (row >= r1) return;
+    next = __ldg(a.stats + row);
+    if constexpr (KEPT) {
+      t.fetch_bytes(a.eh, row, a, bytes_h);
+      if (branch) t.fetch_bytes(a.eu, row, a, bytes_u);
+    }
+  };
+  fetch(r0);
   if (stages == 3) wait_copies<1>(); else wait_copies<0>();
-  team_sync(t);
+  t.sync();
   int slot = 0;
-  for (long long row = r0; row < r0 + a.chunk; ++row) {
-    const bool valid = row < r1;
-    if (a.tl >= 32 && !valid) break;
+  for (int i = 0; i < a.chunk; ++i) {
+    const int row = r0 + i;
+    const bool valid = FULL || row < r1;
+    if ((FULL || a.tl >= 32) && row >= r1) break;
     const char* at = mine + slot * stage;
-    const int off = VEC * ES == 16 ? 0 : (int)((row * bytes) & 15), off_e = (int)((row * eb) & 15);
-    const int d = valid ? a.d : 0, dp = valid ? a.dp : 0;
+    const int off = T::WHOLE ? 0 : (int)(((long long)row * bytes) & 15), off_e = T::WHOLE ? 0 : (int)(((long long)row * eb) & 15);
     issue(row + stages - 1, slot == 0 ? stages - 1 : slot - 1);
     const float4 st = next;
-    if (row + 1 < r1) next = __ldg(a.stats + row + 1);
     if (branch && valid) {
       if (row == seg_end) {
-        F2 gps[kPairs];
+        F2 f[P];
         seg_end += a.per;
-        take_factors<VEC>(a, ++seg, t, gps);
-        give_sums<VEC>(factors, t, a.d, gps);
+        t.take_factors(a, ++seg, f);
+        t.give_f32(factors, f);
       }
-      if (row + 1 == seg_end && row + 1 < r1) fetch_gate(a, seg + 1, t);
+      if (row + 1 == seg_end && row + 1 < r1) t.fetch_gate(a, seg + 1);
     }
     // u^ and h^; sums of q = dn*pre and q*h^
-    F2 uh[kPairs], hh[kPairs];
-    if constexpr (KEPT) take_codes<VEC>(at + at_h, at + at_eh + off_e, t, dp, hh);
-    else take<DT, VEC>(at + at_h + off, t, d, hh);
+    F2 uh[P], hh[P];
+    if constexpr (KEPT) t.take_codes(at + at_h, at + at_eh + off_e, bytes_h, valid, hh);
+    else t.take(at + at_h + off, valid, hh);
     if (branch) {
-      if constexpr (KEPT) take_codes<VEC>(at + at_u, at + at_eu + off_e, t, dp, uh);
-      else take<DT, VEC>(at + at_u + off, t, d, uh);
-      F2 gps[kPairs];
-      take_own<VEC>(factors, t, a.d, gps);
+      if constexpr (KEPT) t.take_codes(at + at_u, at + at_eu + off_e, bytes_u, valid, uh);
+      else t.take(at + at_u + off, valid, uh);
+      F2 f[P];
+      t.take_f32(factors, f);
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) {
+      for (int k = 0; k < P; ++k) {
         uh[k] = (uh[k] + f2(-st.x)) * f2(st.y);
-        hh[k] = fma(f2(a.keep), hh[k], gps[k] * uh[k]);
+        hh[k] = fma(f2(a.keep), hh[k], f[k] * uh[k]);
       }
     }
+    fetch(row + 1);
     float m0 = 0.f, m1 = 0.f;
     if (norm) {
-      F2 dn[kPairs], pre[kPairs], s0 = zero, s1 = zero;
-      take<DT, VEC>(at + room + off, t, d, dn);
-      take_param<VEC>(a.pre, t, a.d, 0.f, pre);
+      F2 dn[P], pre[P], s0 = zero, s1 = zero;
+      t.take(at + room + off, valid, dn);
+      t.take_f32(pres, pre);
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) {
+      for (int k = 0; k < P; ++k) {
         hh[k] = (hh[k] + f2(-st.z)) * f2(st.w);
         spre[k] = fma(dn[k], hh[k], spre[k]);
         const F2 q = dn[k] * pre[k];
@@ -925,41 +937,41 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       m0 = sum(s0);
       m1 = sum(s1);
       if (a.shifted) {
-        take_own<VEC>(shifts, t, a.d, pre);
+        t.take_f32(shifts, pre);
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) pre[k] = pre[k] + dn[k];
-        give_sums<VEC>(shifts, t, a.d, pre);
+        for (int k = 0; k < P; ++k) pre[k] = pre[k] + dn[k];
+        t.give_f32(shifts, pre);
       }
     }
-    team_sum2(m0, m1, t);
+    t.sum2(m0, m1);
     m0 = a.layer ? m0 * a.inv_d : 0.f;
     m1 *= a.inv_d;
     // D in h^'s place
     if (norm) {
-      F2 dn[kPairs], pre[kPairs];      // (again, from shared memory and L1: held, they would cost the registers of a row)
-      take<DT, VEC>(at + room + off, t, d, dn);
-      take_param<VEC>(a.pre, t, a.d, 0.f, pre);
+      F2 dn[P], pre[P];      // (again, from shared memory: held, they would cost the registers of a row)
+      t.take(at + room + off, valid, dn);
+      t.take_f32(pres, pre);
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) hh[k] = f2(st.w) * fma(hh[k], f2(-m1), fma(dn[k], pre[k], f2(-m0)));
+      for (int k = 0; k < P; ++k) hh[k] = f2(st.w) * fma(hh[k], f2(-m1), fma(dn[k], pre[k], f2(-m0)));
     } else {
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) hh[k] = zero;
+      for (int k = 0; k < P; ++k) hh[k] = zero;
     }
     if (a.dh_out != nullptr) {
-      F2 dh[kPairs];
-      take<DT, VEC>(at + off, t, d, dh);
+      F2 dh[P];
+      t.take(at + off, valid, dh);
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) hh[k] = hh[k] + dh[k];
+      for (int k = 0; k < P; ++k) hh[k] = hh[k] + dh[k];
     }
     float t0 = 0.f, t1 = 0.f;
     if (branch) {
-      F2 v[kPairs], s0 = zero, s1 = zero;
+      F2 v[P], s0 = zero, s1 = zero;
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) v[k] = f2(a.keep) * hh[k];
-      if (valid) give<DT, VEC>(a.dh, row, t, a.d, v);
-      take_own<VEC>(factors, t, a.d, v);
+      for (int k = 0; k < P; ++k) v[k] = f2(a.keep) * hh[k];
+      if (valid) t.give(a.dh, row, a.d, v);
+      t.take_f32(factors, v);
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) {
+      for (int k = 0; k < P; ++k) {
         E[k] = fma(hh[k], uh[k], E[k]);
         hh[k] = hh[k] * v[k];
         s0 = s0 + hh[k];
@@ -968,34 +980,34 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       t0 = sum(s0);
       t1 = sum(s1);
     } else if (valid) {
-      give<DT, VEC>(a.dh, row, t, a.d, hh);
+      t.give(a.dh, row, a.d, hh);
     }
     if (stages == 3) wait_copies<1>(); else wait_copies<0>();
-    team_sum2(t0, t1, t);
+    t.sum2(t0, t1);
     if (branch) {
       t0 = a.layer ? t0 * a.inv_d : 0.f;
       t1 *= a.inv_d;
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) hh[k] = f2(st.y) * fma(uh[k], f2(-t1), hh[k] + f2(-t0));
+      for (int k = 0; k < P; ++k) hh[k] = f2(st.y) * fma(uh[k], f2(-t1), hh[k] + f2(-t0));
       if (valid) {
-        give<DT, VEC>(a.du, row, t, a.d, hh);
+        t.give(a.du, row, a.d, hh);
         if (a.split == 0 && (row + 1 == r1 || row + 1 == seg_end)) {      // the end of a gate's rows
-          F2 g[kPairs], v[kPairs];
-          take_param<VEC>(a.gate + seg * a.d, t, a.d, 1.f, g);
-          take_own<VEC>(posts, t, a.d, v);
+          F2 g[P], v[P];
+          t.take_f32(a.gate + (long long)seg * a.d, g);
+          t.take_f32(posts, v);
 #pragma unroll
-          for (int k = 0; k < kPairs; ++k) {
+          for (int k = 0; k < P; ++k) {
             E[k] = E[k] * f2(a.scale);
             v[k] = fma(g[k], E[k], v[k]);
           }
-          give_sums<VEC>(posts, t, a.d, v);
-          take_param<VEC>(a.post, t, a.d, 0.f, g);
+          t.give_f32(posts, v);
+          t.take_f32(a.post, g);
 #pragma unroll
-          for (int k = 0; k < kPairs; ++k) {
+          for (int k = 0; k < P; ++k) {
             g[k] = g[k] * E[k];
             E[k] = zero;
           }
-          give_sums<VEC>(a.dgate + seg * a.d, t, a.d, g);
+          t.give_f32(a.dgate + (long long)seg * a.d, g);
         }
       }
     }
@@ -1005,11 +1017,11 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   wait_copies<0>();
 
   // what the team has summed up over its rows
-  F2 v[kPairs];
+  F2 v[P];
   if (branch && a.split != 0) {
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) E[k] = E[k] * f2(a.scale);
-    if (a.gate != nullptr && !a.join_e) give_sums<VEC>(a.part_e + team * a.d, t, a.d, E);
+    for (int k = 0; k < P; ++k) E[k] = E[k] * f2(a.scale);
+    if (a.gate != nullptr && !a.join_e) t.give_f32(a.part_e + team * a.d, E);
   }
   const long long slab = (long long)gridDim.x * a.d;
   float* const joined = reinterpret_cast<float*>(ring);
@@ -1020,27 +1032,30 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     float* to = (which == 3 ? a.part_e : a.part + which * slab) + (long long)blockIdx.x * a.d;
     if (which == 2) {
       if (a.split == 0) {
-        take_own<VEC>(posts, t, a.d, v);
-      } else {
-        take_param<VEC>(a.gate != nullptr ? a.gate + seg * a.d : nullptr, t, a.d, 1.f, v);
+        t.take_f32(posts, v);
+      } else if (a.gate == nullptr) {
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) v[k] = v[k] * E[k];
+        for (int k = 0; k < P; ++k) v[k] = E[k];
+      } else {
+        t.take_f32(a.gate + (long long)seg * a.d, v);
+#pragma unroll
+        for (int k = 0; k < P; ++k) v[k] = v[k] * E[k];
       }
     }
-    if (which == 1) take_own<VEC>(shifts, t, a.d, v);
-    const F2(&of)[kPairs] = which == 0 ? spre : which == 3 ? E : v;
+    if (which == 1) t.take_f32(shifts, v);
+    const F2(&of)[P] = which == 0 ? spre : which == 3 ? E : v;
     if (a.teams > 1) {
       // (at the start of each team's ring, which has room for a row of fp32; what is its own lies behind the ring)
       __syncthreads();
-      give_sums<VEC>(joined + team_in * (a.team_smem / 4), t, a.d, of);
+      t.give_f32(joined + team_in * (a.team_smem / 4), of);
       __syncthreads();
       for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
         float s = 0.f;
-        for (int i = 0; i < a.teams; ++i) s += joined[i * (a.team_smem / 4) + c];
+        for (int k = 0; k < a.teams; ++k) s += joined[k * (a.team_smem / 4) + c];
         to[c] = s;
       }
     } else {
-      give_sums<VEC>(to, t, a.d, of);
+      t.give_f32(to, of);
     }
   }
 }
@@ -1083,7 +1098,7 @@ __global__ void __launch_bounds__(512) block_sums_kernel(const SumArgs a) {
 // host side
 // ---------------------------------------------------------------------------
 struct BlockPlan {
-  bool wide, whole;              // rows above the limit; rows of whole vectors
+  bool wide, whole, full;        // rows above the limit; rows of whole vectors; and of whole warps
   int tl, teams, stages;
   int smem;                      // of a team, or of the wide backward kernel's sums
   long long chunk, nteams, ctas;
@@ -1099,7 +1114,7 @@ dk_status check_block(const dk_block* q) {
   if (q->dtype != DK_F32 && q->dtype != DK_BF16) return DK_ERR_INVALID_ARG;
   if (!(q->eps >= 0.f) || !(q->keep - q->keep == 0.f) || !(q->scale - q->scale == 0.f)) return DK_ERR_INVALID_ARG;
   if (q->rows < 0 || q->d < 1 || q->d > kMaxD || q->rows_per_gate < 1) return DK_ERR_SHAPE;
-  if ((double)q->rows * q->d > 1e12 || q->rows > (1LL << 31) - 1) return DK_ERR_SHAPE;
+  if ((double)q->rows * q->d > 1e12 || q->rows > (1LL << 30)) return DK_ERR_SHAPE;
   return DK_OK;
 }
 
@@ -1111,41 +1126,49 @@ BlockPlan plan_block(const dk_block& q, bool backward, const Asked& asked) {
   BlockPlan p = {};
   const bool f32 = q.dtype == DK_F32;
   const int es = f32 ? 4 : 2, vec = 16 / es, dp = ckpt8::padded(q.d);
-  const int values = f32 ? kValues<DK_F32> : kValues<DK_BF16>;
   const int most = backward ? (f32 ? kBwdThreads<DK_F32> : kBwdThreads<DK_BF16>) : f32 ? kFwdThreads<DK_F32> : kFwdThreads<DK_BF16>;
   const long long per = asked.gated && q.rows_per_gate < q.rows ? q.rows_per_gate : q.rows;
   p.gates = per > 0 ? (q.rows + per - 1) / per : 0;
   p.whole = q.d % vec == 0;
-  int threads = (dp + values - 1) / values;
+  const int values = f32 ? kValues<DK_F32, true> : p.whole ? kValues<DK_BF16, true> : kValues<DK_BF16, false>;
+  p.full = q.d % (32 * values) == 0;
+  const int threads = (dp + values - 1) / values;
   if (threads <= 32) {
     // (a block of 32 values lies in one vector of neighbouring lanes)
-    p.tl = ckpt8::kBlock / (p.whole ? vec : !f32 && q.d % 2 == 0 ? 2 : 1);
+    p.tl = ckpt8::kBlock / (p.whole ? vec : q.d % 2 == 0 ? 2 : 1);
     while (p.tl < threads) p.tl *= 2;
     p.teams = kSmallTeams / p.tl;
   } else {
     p.tl = (threads + 31) / 32 * 32;
     p.teams = 1;
   }
-  // A team's ring of three rows, or of two where that lets an SM hold more teams.
-  const int row = row_room(q.d * es), room = 220 * 1024;
-  long long ctas = 0;
-  for (int stages = 3; stages >= 2; --stages) {
-    int smem = stages * 2 * row;
-    if (backward)
-      smem = stages * (2 * row + 2 * (asked.held ? row_room(dp) + row_room(dp / ckpt8::kBlock) : row)) +
-             (1 + (p.gates > 1) + asked.shifted) * row_room(q.d * 4);
-    int teams = p.teams;
-    while (teams > 1 && teams * smem > room / 2) teams /= 2;
-    long long c = most / (p.tl * teams);
-    if (c > room / ((long long)smem * teams + 1024)) c = room / ((long long)smem * teams + 1024);
-    if (smem * teams > kMostSmem || c < 1) c = smem * teams <= kMostSmem ? 1 : 0;
-    if (c * teams > ctas * (ctas ? p.teams : 1)) {
-      ctas = c;
-      p.smem = smem;
-      p.stages = stages;
-      if (teams < p.teams) p.teams = teams;
+  // A team's ring of three rows, or of two where that lets an SM hold more teams; and as many rows to a team as give every SM
+  // the CTAs that its registers and shared memory hold.  (Backward, teams with several gates each need room for dpost.)
+  const int row = row_room(q.d * es), f32s = row_room(q.d * 4), room = 220 * 1024, teams_most = p.teams;
+  long long ctas = 0, want = 0, chunk = 0;
+  for (int posts = 0; posts < 2; ++posts) {
+    ctas = 0;
+    for (int stages = 3; stages >= 2; --stages) {
+      int smem = stages * 2 * row;
+      if (backward)
+        smem = stages * (2 * row + 2 * (asked.held ? row_room(dp) + (p.whole ? 0 : row_room(dp / ckpt8::kBlock)) : row)) +
+               (2 + posts + asked.shifted) * f32s;
+      int teams = teams_most;
+      while (teams > 1 && teams * smem > room / 2) teams /= 2;
+      long long c = most / (p.tl * teams);
+      if (c > room / ((long long)smem * teams + 1024)) c = room / ((long long)smem * teams + 1024);
+      if (c < 1) c = (long long)smem * teams <= kMostSmem ? 1 : 0;
+      if (c * teams > ctas * p.teams || (ctas == 0 && c > 0)) {
+        ctas = c;
+        p.smem = smem;
+        p.stages = stages;
+        p.teams = teams;
+      }
+      if (!backward) break;
     }
-    if (!backward) break;
+    want = 148 * ctas * p.teams;
+    chunk = want > 0 ? (q.rows + want - 1) / want : 1;
+    if (!backward || p.gates <= 1 || per > chunk) break;
   }
   p.wide = q.d > kHeld || p.tl > most || ctas == 0;
   if (p.wide) {
@@ -1154,9 +1177,10 @@ BlockPlan plan_block(const dk_block& q, bool backward, const Asked& asked) {
     p.smem = backward ? 3 * q.d * (int)sizeof(float) : 0;
     ctas = 1;
   }
-  // Rows of a team: as many as give every SM the CTAs that its registers and shared memory hold.
-  const long long want = 148 * ctas * p.teams;
-  long long chunk = (q.rows + want - 1) / want;
+  if (p.wide) {
+    want = 148;
+    chunk = (q.rows + want - 1) / want;
+  }
   if (chunk < 1) chunk = 1;
   if (!backward) {
     p.chunk = p.wide ? 1 : chunk;
@@ -1187,30 +1211,30 @@ BlockPlan plan_block(const dk_block& q, bool backward, const Asked& asked) {
   return p;
 }
 
-template <int DT, int VEC>
-dk_status launch_fwd(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
-  const dim3 grid((unsigned)p.ctas);
-  const int threads = p.tl * p.teams;
-  if (p.wide)
-    return launch_chained(block_fwd_wide_kernel<DT, VEC, 16 / VEC>, grid, threads, 0, st, a) == cudaSuccess ? DK_OK : DK_ERR_CUDA;
-  auto kern = block_fwd_rows_kernel<DT, VEC>;
-  static SmemLimit limit;
+template <typename K>
+dk_status launch_rows(K kern, SmemLimit& limit, const BlockArgs& a, const BlockPlan& p, int smem, int device, cudaStream_t st) {
   const dk_status s = allow_smem(limit, device, kern, kMostSmem);
   if (s != DK_OK) return s;
-  return launch_chained(kern, grid, threads, (size_t)p.smem * p.teams, st, a) == cudaSuccess ? DK_OK : DK_ERR_CUDA;
+  return launch_chained(kern, dim3((unsigned)p.ctas), p.tl * p.teams, (size_t)smem, st, a) == cudaSuccess ? DK_OK : DK_ERR_CUDA;
 }
-
+template <int DT, int VEC>
+dk_status launch_fwd(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
+  constexpr bool WHOLE = VEC == (DT == DK_F32 ? 4 : 8);
+  static SmemLimit limits[3];
+  if (p.wide) return launch_rows(block_fwd_wide_kernel<DT, VEC, 16 / VEC>, limits[0], a, p, 0, device, st);
+  if constexpr (WHOLE)
+    if (p.full) return launch_rows(block_fwd_rows_kernel<DT, VEC, true>, limits[1], a, p, p.smem * p.teams, device, st);
+  return launch_rows(block_fwd_rows_kernel<DT, VEC, false>, limits[2], a, p, p.smem * p.teams, device, st);
+}
 template <int DT, int VEC, bool KEPT>
 dk_status launch_bwd(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
-  const dim3 grid((unsigned)p.ctas);
-  const int threads = p.tl * p.teams;
-  auto run = [&](auto kern, SmemLimit& limit) {
-    const dk_status s = allow_smem(limit, device, kern, kMostSmem);
-    if (s != DK_OK) return s;
-    return launch_chained(kern, grid, threads, (size_t)p.smem * p.teams, st, a) == cudaSuccess ? DK_OK : DK_ERR_CUDA;
-  };
-  static SmemLimit limits[2];
-  return p.wide ? run(block_bwd_wide_kernel<DT, VEC, 16 / VEC, KEPT>, limits[0]) : run(block_bwd_rows_kernel<DT, VEC, KEPT>, limits[1]);
+  constexpr bool WHOLE = VEC == (DT == DK_F32 ? 4 : 8);
+  static SmemLimit limits[3];
+  const int smem = p.smem * p.teams;
+  if (p.wide) return launch_rows(block_bwd_wide_kernel<DT, VEC, 16 / VEC, KEPT>, limits[0], a, p, smem, device, st);
+  if constexpr (WHOLE)
+    if (p.full) return launch_rows(block_bwd_rows_kernel<DT, VEC, true, KEPT>, limits[1], a, p, smem, device, st);
+  return launch_rows(block_bwd_rows_kernel<DT, VEC, false, KEPT>, limits[2], a, p, smem, device, st);
 }
 template <int DT, int VEC>
 dk_status launch_bwd(const BlockArgs& a, const BlockPlan& p, bool kept, int device, cudaStream_t st) {
@@ -1258,9 +1282,9 @@ dk_status backward(dk_ctx* ctx, const dk_block* q, bool kept, const void* dh_out
   a.dh_out = dh_out; a.dn = dn; a.dh = dh; a.du = du; a.dgate = dgate;
   a.part = static_cast<float*>(ctx->ws);
   a.part_e = reinterpret_cast<float*>(static_cast<char*>(ctx->ws) + p.part_e);
-  a.rows = q->rows;
-  a.per = gate != nullptr && q->rows_per_gate < q->rows ? q->rows_per_gate : q->rows;
-  a.chunk = p.chunk;
+  a.rows = (int)q->rows;
+  a.per = (int)(gate != nullptr && q->rows_per_gate < q->rows ? q->rows_per_gate : q->rows);
+  a.chunk = (int)p.chunk;
   // (with one gate p.split counts the CTAs' parts; its teams' rows are consecutive either way)
   a.split = p.split ? (int)((a.per + p.chunk - 1) / p.chunk) : 0;
   a.join_e = p.join_e && gate != nullptr;
@@ -1270,7 +1294,9 @@ dk_status backward(dk_ctx* ctx, const dk_block* q, bool kept, const void* dh_out
   a.eps = q->eps; a.keep = q->keep; a.scale = q->scale; a.inv_d = 1.f / (float)q->d;
   ProfScope ps(ctx, DK_KERNEL_OTHER, 2, st);
   if (q->dtype == DK_F32)
-    s = p.whole ? launch_bwd<DK_F32, 4>(a, p, kept, ctx->device, st) : launch_bwd<DK_F32, 1>(a, p, kept, ctx->device, st);
+    s = p.whole           ? launch_bwd<DK_F32, 4>(a, p, kept, ctx->device, st)
+        : q->d % 2 == 0 ? launch_bwd<DK_F32, 2>(a, p, kept, ctx->device, st)
+                        : launch_bwd<DK_F32, 1>(a, p, kept, ctx->device, st);
   else
     s = p.whole           ? launch_bwd<DK_BF16, 8>(a, p, kept, ctx->device, st)
         : q->d % 2 == 0 ? launch_bwd<DK_BF16, 2>(a, p, kept, ctx->device, st)
@@ -1329,9 +1355,9 @@ dk_status dk_block_norm_fwd(dk_ctx* ctx, const dk_block* q, const void* h, const
   a.ku = static_cast<uint8_t*>(ckpt_u);
   if (a.kh) a.keh = a.kh + codes;
   if (a.ku) a.keu = a.ku + codes;
-  a.rows = q->rows;
-  a.per = gate != nullptr && q->rows_per_gate < q->rows ? q->rows_per_gate : q->rows;
-  a.chunk = p.chunk;
+  a.rows = (int)q->rows;
+  a.per = (int)(gate != nullptr && q->rows_per_gate < q->rows ? q->rows_per_gate : q->rows);
+  a.chunk = (int)p.chunk;
   a.d = q->d; a.dp = ckpt8::padded(q->d); a.tl = p.tl; a.teams = p.teams; a.stages = p.stages; a.team_smem = p.smem;
   a.layer = q->kind == DK_BLOCK_LAYER;
   a.eps = q->eps; a.keep = q->keep; a.scale = q->scale; a.inv_d = 1.f / (float)q->d;
@@ -1340,7 +1366,9 @@ dk_status dk_block_norm_fwd(dk_ctx* ctx, const dk_block* q, const void* h, const
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ProfScope ps(ctx, DK_KERNEL_OTHER, 1, st);
   if (q->dtype == DK_F32)
-    return p.whole ? launch_fwd<DK_F32, 4>(a, p, ctx->device, st) : launch_fwd<DK_F32, 1>(a, p, ctx->device, st);
+    return p.whole           ? launch_fwd<DK_F32, 4>(a, p, ctx->device, st)
+           : q->d % 2 == 0 ? launch_fwd<DK_F32, 2>(a, p, ctx->device, st)
+                           : launch_fwd<DK_F32, 1>(a, p, ctx->device, st);
   return p.whole           ? launch_fwd<DK_BF16, 8>(a, p, ctx->device, st)
          : q->d % 2 == 0 ? launch_fwd<DK_BF16, 2>(a, p, ctx->device, st)
                          : launch_fwd<DK_BF16, 1>(a, p, ctx->device, st);

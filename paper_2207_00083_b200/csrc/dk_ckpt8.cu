@@ -63,10 +63,10 @@ __global__ void __launch_bounds__(kThreads) ckpt8_store_kernel(const Args a) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const long long i = i0 + u * kThreads;
-    const uint32_t b = ckpt8::exponent_byte(ckpt8::block_most<VEC>(v[u]));
+    const ckpt8::Scale s = ckpt8::scale_of(ckpt8::block_most<VEC>(v[u]));
     if (i < a.units) {
-      ckpt8::put_codes<VEC>(a.codes + i * VEC, v[u], b);
-      if ((threadIdx.x & (ckpt8::kBlock / VEC - 1)) == 0) a.exps[i * VEC / ckpt8::kBlock] = (uint8_t)b;
+      ckpt8::put_codes<VEC>(a.codes + i * VEC, v[u], s);
+      if ((threadIdx.x & (ckpt8::kBlock / VEC - 1)) == 0) a.exps[i * VEC / ckpt8::kBlock] = (uint8_t)s.byte;
     }
   }
 }

@@ -53,7 +53,7 @@ REFUSED = [(dk.dk_ckpt8(-1, 8, 0), SHAPE), (dk.dk_ckpt8(1, 0, 0), SHAPE), (dk.dk
            (dk.dk_ckpt8(1 << 40, 8, 0), SHAPE), (dk.dk_ckpt8(1, 8, 2), INVALID), (dk.dk_wgrad8(-1, 8, 8, 0), SHAPE),
            (dk.dk_wgrad8(8, 0, 8, 0), SHAPE), (dk.dk_wgrad8(8, 8, 0, 0), SHAPE), (dk.dk_wgrad8((1 << 24) + 1, 8, 8, 0), SHAPE),
            (dk.dk_wgrad8(8, 8, 8, 7), INVALID), (block(-1), SHAPE), (block(4, 0), SHAPE), (block(4, 16385), SHAPE),
-           (block(4, 8, 0), SHAPE), (block(4, 8, -3), SHAPE), (block(1 << 31, 8), SHAPE), (block(kind=2), INVALID),
+           (block(4, 8, 0), SHAPE), (block(4, 8, -3), SHAPE), (block((1 << 30) + 1, 8), SHAPE), (block(kind=2), INVALID),
            (block(dtype=2), INVALID), (block(eps=-1.0), INVALID), (block(eps=NAN), INVALID), (block(keep=INF), INVALID),
            (block(scale=NAN), INVALID)]
 
