@@ -22,6 +22,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "dk_step.h"
 #include "dk_tc_pair.cuh"
 
@@ -51,6 +53,22 @@ struct Params {
   int bf16;                    // operand type: 1 bf16, 0 fp16
   int M, N;
   int* status;
+  // The last wave (epilogues with kTail; one matrix, ksplit = 1): tiles from tail_from on are cut into tail_slices slices
+  // of tail_kb stages, whose sums the last of a tile's slices to be done joins.
+  int tail_from, tail_slices, tail_kb;
+  float* tail_part;            // [slice of a tile][16 warps][32 lanes][128]
+  unsigned int* tail_count;    // [tile][16], zero between launches
+};
+
+// What an epilogue asks of the pair kernel: kTail (see above), kBulk (it stores by TMA, through the map that B's second plane
+// would have had; its stores are waited for at the end).
+template <class E, class = void>
+struct Asks {
+  static constexpr bool tail = false, bulk = false;
+};
+template <class E>
+struct Asks<E, std::void_t<decltype(E::kTail)>> {
+  static constexpr bool tail = E::kTail, bulk = E::kBulk;
 };
 
 // a stored matrix: `rows` rows of `cols` contiguous elements, `pitch` elements apart (a multiple of 8), one or two
@@ -61,9 +79,16 @@ struct Operand {
   long long rows, cols, pitch, batch_stride;     // in elements
 };
 
+template <bool TAIL = false>
 __device__ __forceinline__ void item_tile(const Params& p, int w, int& batch, int& ks, int& mt, int& nt) {
-  ks = w % p.ksplit;
-  int t = w / p.ksplit;
+  int t;
+  if (TAIL && w >= p.tail_from) {
+    ks = (w - p.tail_from) % p.tail_slices;
+    t = p.tail_from + (w - p.tail_from) / p.tail_slices;
+  } else {
+    ks = w % p.ksplit;
+    t = w / p.ksplit;
+  }
   batch = t / p.tiles;
   t -= batch * p.tiles;
   if (p.sym) {
@@ -78,6 +103,47 @@ __device__ __forceinline__ void item_tile(const Params& p, int w, int& batch, in
     nt = t / gm;
     mt = m0 + t - nt * gm;
   }
+}
+
+// the stages of an item, and which slice of its contraction it is
+template <bool TAIL>
+__device__ __forceinline__ int item_stages(const Params& p, int w, int& kb_lo, int& kb_hi) {
+  const bool tail = TAIL && w >= p.tail_from;
+  const int ks = tail ? (w - p.tail_from) % p.tail_slices : w % p.ksplit, per = tail ? p.tail_kb : p.kb_per_split;
+  kb_lo = ks * per;
+  kb_hi = min(p.KB, kb_lo + per);
+  return ks;
+}
+
+// A slice of the last wave: leaves the warp's sums, and, where it is the last of its tile's slices, joins them in the slices'
+// order.  True: `acc` is the whole sum.  (Done warp by warp: no barrier between the warps of a tile is needed.)
+template <int NH>
+__device__ __forceinline__ bool join_tail(const Params& p, int w, uint32_t rank, int epi_warp, float (&acc)[NH]) {
+  const int lane = threadIdx.x & 31, item = w - p.tail_from, ks = item % p.tail_slices, tile = item / p.tail_slices;
+  const int mine = (int)rank * kEpi + epi_warp;
+  auto at = [&](int slice) {      // [4 columns][lane]
+    return reinterpret_cast<float4*>(p.tail_part) + (((size_t)tile * p.tail_slices + slice) * (2 * kEpi) + mine) * (32 * NH / 4) + lane;
+  };
+#pragma unroll
+  for (int j = 0; j < NH; j += 4) __stcg(at(ks) + j / 4 * 32, make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]));
+  __threadfence();
+  __syncwarp();
+  unsigned int done = 0;
+  if (lane == 0) done = atomicAdd(p.tail_count + tile * 2 * kEpi + mine, 1u) + 1u;
+  done = __shfl_sync(0xffffffffu, done, 0);
+  if (done != (unsigned)p.tail_slices) return false;
+  __threadfence();
+  if (lane == 0) p.tail_count[tile * 2 * kEpi + mine] = 0u;
+#pragma unroll
+  for (int j = 0; j < NH; ++j) acc[j] = 0.f;
+  for (int s = 0; s < p.tail_slices; ++s) {
+#pragma unroll
+    for (int j = 0; j < NH; j += 4) {
+      const float4 v = __ldcg(at(s) + j / 4 * 32);
+      acc[j] += v.x; acc[j + 1] += v.y; acc[j + 2] += v.z; acc[j + 3] += v.w;
+    }
+  }
+  return true;
 }
 
 __device__ __forceinline__ void mma_f16_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
@@ -165,6 +231,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsG, 1)
 gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constant__ CUtensorMap map_a_lo,
               const __grid_constant__ CUtensorMap map_b_hi, const __grid_constant__ CUtensorMap map_b_lo, const Params p,
               const Epi epi) {
+  constexpr bool TAIL = Asks<Epi>::tail;
   constexpr int A_BYTES = ROWS * 128, B_BYTES = BN / 2 * 128;
   constexpr int PL = kPlanesA<NPROD>;
   constexpr int STAGE = stage_bytes<NPROD, BN>();
@@ -218,10 +285,10 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
         uint32_t phase = 0;
         bool alive = true;
         for (int w = pair; alive && w < p.nitems; w += npairs) {
-          int batch, ks, mt, nt;
-          item_tile(p, w, batch, ks, mt, nt);
+          int batch, ks, mt, nt, kb_lo, kb_hi;
+          item_tile<TAIL>(p, w, batch, ks, mt, nt);
+          item_stages<TAIL>(p, w, kb_lo, kb_hi);
           const int m0 = mt * TILE_M + (int)rank * ROWS, n0 = nt * BN + (int)rank * (BN / 2);
-          const int kb_lo = ks * p.kb_per_split, kb_hi = min(p.KB, kb_lo + p.kb_per_split);
           for (int kb = kb_lo; kb < kb_hi; ++kb) {
             if (!tc::mbar_wait(empty_bar + stage, phase ^ 1u, abort_flag, p.spin_cap)) { alive = false; break; }
             if (rank == 0) tc::mbar_expect_tx(full_bar + stage, (uint32_t)(2 * STAGE));
@@ -249,8 +316,8 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
         uint32_t phase = 0, acc_it = 0;
         bool alive = true;
         for (int w = pair; alive && w < p.nitems; w += npairs) {
-          const int ks = w % p.ksplit;
-          const int kb_lo = ks * p.kb_per_split, kb_hi = min(p.KB, kb_lo + p.kb_per_split);
+          int kb_lo, kb_hi;
+          item_stages<TAIL>(p, w, kb_lo, kb_hi);
           for (int kb = kb_lo; alive && kb < kb_hi; kb += p.chunk, ++acc_it) {
             const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
             if (!tc::mbar_wait(tempty_bar + buf, aphase ^ 1u, abort_flag, p.spin_cap)) { alive = false; break; }
@@ -289,9 +356,9 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
     bool alive = true;
     float acc[NH];
     for (int w = pair; alive && w < p.nitems; w += npairs) {
-      int batch, ks, mt, nt;
-      item_tile(p, w, batch, ks, mt, nt);
-      const int kb_lo = ks * p.kb_per_split, kb_hi = min(p.KB, kb_lo + p.kb_per_split);
+      int batch, ks, mt, nt, kb_lo, kb_hi;
+      item_tile<TAIL>(p, w, batch, ks, mt, nt);
+      item_stages<TAIL>(p, w, kb_lo, kb_hi);
       for (int kb = kb_lo; kb < kb_hi; kb += p.chunk, ++acc_it) {
         const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
         if (!tc::mbar_wait(tfull_bar + buf, aphase, abort_flag, p.spin_cap)) { alive = false; break; }
@@ -321,9 +388,14 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
         if (lane == 0) tc::mbar_arrive_cluster(tc::mapa_shared(smem_u32(tempty_bar + buf), 0u));
       }
       if (!alive) break;
-      epi(p, acc, batch, ks, mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, nt * BN + half * NH,
-          rows_mem + (warp - 4) * 4096);
+      if constexpr (TAIL) {
+        if (w >= p.tail_from && !join_tail<NH>(p, w, rank, warp - 4, acc)) continue;
+      }
+      const int row = mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, col0 = nt * BN + half * NH;
+      if constexpr (Asks<Epi>::bulk) epi(p, acc, row, col0, rows_mem + (warp - 4) * 4096, &map_b_lo);
+      else epi(p, acc, batch, ks, row, col0, rows_mem + (warp - 4) * 4096);
     }
+    if constexpr (Asks<Epi>::bulk) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
 
   // ---------------- teardown ----------------
@@ -725,6 +797,32 @@ __device__ __forceinline__ void store_terms(const float (&v)[NH], char* sm, __ha
   }
 }
 
+// fp32 rows of a warp stored by TMA: 32 columns at a time through the warp's 4 KiB of shared memory (128-byte rows, their
+// 16-byte pieces exchanged as the 128-byte swizzle has them, so the writes meet no bank twice).  The map clips what lies
+// outside the matrix.  A tile of 256 x 256 costs the epilogue a third of the instructions of warp_rows_f32.
+template <int NH>
+__device__ __forceinline__ void warp_rows_bulk(const float (&v)[NH], char* sm, const CUtensorMap* map, int row0, int col0, int cols) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int c = 0; c < NH; c += 32) {
+    if (c >= cols) break;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      *reinterpret_cast<float4*>(sm + lane * 128 + ((q ^ (lane & 7)) << 4)) =
+          make_float4(v[c + 4 * q], v[c + 4 * q + 1], v[c + 4 * q + 2], v[c + 4 * q + 3]);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"((col0 + c) * 4),
+                   "r"(row0), "r"(smem_u32(sm))
+                   : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+}
+
 // fp32 partial sums of a contraction slice: part[ks][batch][M][pitch]
 struct EpiPartial {
   static constexpr bool kAhead = false;
@@ -877,12 +975,18 @@ dk_status launch_small(dk_ctx* ctx, const Operand& A, const Operand& B, Params p
 
 // p: MT, NT, nbatch, sym, tiles, KB, ksplit, kb_per_split, M, N, chunk are set by the caller
 template <int NPROD, bool AMN, bool BMN, int BN, class Epi>
-dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, const Epi& epi, cudaStream_t st) {
+dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, const Epi& epi, cudaStream_t st,
+                 const CUtensorMap* out = nullptr) {
+  static_assert(!Asks<Epi>::bulk || NPROD < 3, "the second plane of B has the map");
   static SmemLimit limit;
   CUtensorMap ma, mal, mb, mbl;
   if (!make_map(ctx, &ma, A.hi, A, p.nbatch, AMN, ROWS) || !make_map(ctx, &mb, B.hi, B, p.nbatch, BMN, BN / 2))
     return DK_ERR_CUDA;
   mal = ma; mbl = mb;
+  if (Asks<Epi>::bulk) {
+    if (out == nullptr) return DK_ERR_INVALID_ARG;
+    mbl = *out;
+  }
   if ((NPROD >= 2 && !make_map(ctx, &mal, A.lo, A, p.nbatch, AMN, ROWS)) ||
       (NPROD == 3 && !make_map(ctx, &mbl, B.lo, B, p.nbatch, BMN, BN / 2)))
     return DK_ERR_CUDA;
@@ -904,6 +1008,22 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
   ctx->opt.v[DK_OPT_TEST_WITHHOLD] = -1;
   p.status = device_status_word(ctx);
   int pairs = ctx->sm_count / 2;
+  if constexpr (Asks<Epi>::tail) {
+    // What the last wave leaves idle, against what joining a tile's slices takes (some 12000 cycles: 128 KiB a CTA written
+    // and read again through L2).  16384 rows, 4096 x 4096: 256 tiles on 74 pairs, 3.46 waves.
+    p.tail_from = p.tiles;
+    p.tail_slices = 1;
+    const int rest = p.tiles % pairs;
+    int slices = rest > 0 ? pairs / rest : 1;
+    const int kb = (p.KB + slices - 1) / slices;
+    slices = (p.KB + kb - 1) / kb;
+    if (slices > 1 && (p.KB - kb) * 512 * NPROD > 12000 && rest * 2 * kEpi <= kStepCounters && p.tail_part != nullptr) {
+      p.tail_from = p.tiles - rest;
+      p.tail_slices = slices;
+      p.tail_kb = kb;
+      p.nitems = p.tail_from + rest * slices;
+    }
+  }
   if (pairs > p.nitems) pairs = p.nitems;
   return launch_chained(kern, dim3(2 * (unsigned)pairs), kThreadsG, (size_t)smem, st, ma, mal, mb, mbl, p, epi) == cudaSuccess
              ? DK_OK
