@@ -5,8 +5,9 @@
 // number as it stands.  bf16: dy and x enter unrounded, one product.  fp32: dy as two fp16 terms under a power of two of
 // each output (its column of dy, its row of dW), x as one fp16 plane under a power of two of the whole checkpoint (q*2^k
 // is an fp16 number for 33 powers of two, subnormals included), two products.
-//   wgrad8_columns_kernel: sums (for db) and largest magnitudes of dy's columns, the checkpoint's largest exponent
-//   wgrad8_prep_kernel: the operands, and db
+//   wgrad8_columns_kernel: sums (db) and largest magnitudes of dy's columns; bf16: the operand from the checkpoint; fp32: its
+//     largest exponent
+//   wgrad8_prep_kernel: fp32: the operands
 //   the product (dk_gemm16.cuh), both operands read across their rows in place
 #include <math.h>
 
@@ -25,7 +26,7 @@ using g16::scale_exp;
 
 constexpr int kThreads = 256;
 constexpr int kMaxParts = 64;            // parts of the rows in which columns are summed
-constexpr int kMaxBlocks = 1024;         // of wgrad8_columns_kernel that look at the exponents
+constexpr int kMaxBlocks = 148;          // of wgrad8_columns_kernel that look at the exponents
 
 struct Wg8 {
   const void* dy;
@@ -37,12 +38,22 @@ struct Wg8 {
   float* sums;               // [parts][out]
   unsigned int* most;        // [parts][out]; then [out] of all
   unsigned int* most_all;
-  unsigned int* block_exp;   // [columns blocks]: largest exponent; block_exp[kMaxBlocks]: of all
+  unsigned int* block_exp;   // [blocks]: largest exponent; block_exp[kMaxBlocks]: of all
   float* db;
   long long rows;
-  int d, dp, out, op, parts, blocks, copy_dy;
+  unsigned int* count;       // [strips], zero between launches
+  int d, dp, out, op, strips, parts, blocks, copy_dy, with_sums;
   float scale, keep;
 };
+
+// db of a column from its parts' sums
+__device__ __forceinline__ void join_db(const Wg8& a, int c) {
+  float t = 0.f;
+#pragma unroll 8
+  for (int p = 0; p < a.parts; ++p) t += __ldcg(a.sums + (long long)p * a.out + c);
+  t *= a.scale;
+  a.db[c] = a.keep != 0.f ? fmaf(a.keep, a.db[c], t) : t;
+}
 
 // the checkpoint's power of two: its largest step becomes 2^8, so the largest value is below 2^15
 __device__ __forceinline__ int x_exp(unsigned int largest) {
@@ -50,160 +61,12 @@ __device__ __forceinline__ int x_exp(unsigned int largest) {
   return largest == 0u ? 0 : min(s, 126);
 }
 
-// grid (strips of 32 vectors, parts of the rows)
-template <int DT, int VEC>
-__global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
-  chained_launch();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c = (blockIdx.x * 32 + lane) * VEC;
-  const long long per = (a.rows + a.parts - 1) / a.parts;
-  const long long r0 = blockIdx.y * per, r1 = min(a.rows, r0 + per);
-  float s[VEC];
-  unsigned int m[VEC];
-#pragma unroll
-  for (int k = 0; k < VEC; ++k) { s[k] = 0.f; m[k] = 0u; }
-  if (c < a.out) {
-    constexpr int U = 4;
-    for (long long r = r0 + warp; r < r1; r += 8 * U) {
-      typename Vec<DT, VEC>::Raw raw[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + 8 * u < r1) raw[u] = Vec<DT, VEC>::get(a.dy, (r + 8 * u) * a.out + c);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + 8 * u < r1) {
-          float v[VEC];
-          Vec<DT, VEC>::unpack(raw[u], v);
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) {
-            s[k] += v[k];
-            if (DT == DK_F32) m[k] = max(m[k], magnitude(__float_as_uint(v[k])));
-          }
-        }
-    }
-  }
-  __shared__ float ss[8][32 * VEC + 1];
-  __shared__ unsigned int sm[DT == DK_F32 ? 8 : 1][32 * VEC + 1];
-#pragma unroll
-  for (int k = 0; k < VEC; ++k) {
-    ss[warp][lane * VEC + k] = s[k];
-    if (DT == DK_F32) sm[warp][lane * VEC + k] = m[k];
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 32 * VEC; i += kThreads) {
-    const int col = blockIdx.x * 32 * VEC + i;
-    if (col >= a.out) continue;
-    float t = 0.f;
-    unsigned int u = 0;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      t += ss[w][i];
-      if (DT == DK_F32) u = max(u, sm[w][i]);
-    }
-    a.sums[(long long)blockIdx.y * a.out + col] = t;
-    if (DT == DK_F32) a.most[(long long)blockIdx.y * a.out + col] = u;
-  }
-  if constexpr (DT == DK_F32) {
-    // this block's share of the exponents
-    const int block = blockIdx.y * gridDim.x + blockIdx.x, blocks = a.blocks;
-    if (block >= blocks) return;
-    const long long n = a.rows * (a.dp / ckpt8::kBlock);
-    unsigned int e = 0;
-    for (long long i = (long long)block * kThreads + threadIdx.x; i < n; i += (long long)blocks * kThreads) {
-      const unsigned int b = a.exps[i];
-      e = max(e, b == 255u ? 0u : b);
-    }
-    e = __reduce_max_sync(0xffffffffu, e);
-    __shared__ unsigned int se[8];
-    if (lane == 0) se[warp] = e;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-#pragma unroll
-      for (int w = 1; w < 8; ++w) e = max(e, se[w]);
-      a.block_exp[block] = e;
-    }
-  }
-}
-
-// The operands.  The first CTAs take dy's columns (grid_dy of them: strips of 256 columns by row parts), the others the
-// checkpoint, eight values a thread.
+// The checkpoint's values as operands, eight a thread.
 template <int DT>
-__global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int strips, int row_parts, int grid_dy,
-                                                               int with_db) {
-  chained_launch();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if ((int)blockIdx.x < grid_dy) {
-    const int strip = blockIdx.x % strips, part = blockIdx.x / strips;
-    const int c = strip * 256 + lane * 8;
-    if (c >= a.op) return;
-    float f[8];
-    if constexpr (DT == DK_F32) {
-      unsigned int m[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) m[k] = 0u;
-      for (int p = 0; p < a.parts; ++p) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (c + k < a.out) m[k] = max(m[k], __ldg(a.most + (long long)p * a.out + c + k));
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        f[k] = pow2(scale_exp(m[k]));
-        if (part == 0 && warp == 0 && c + k < a.out) a.most_all[c + k] = m[k];
-      }
-    }
-    if (with_db && part == 0 && warp == 1) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (c + k < a.out) {
-          float t = 0.f;
-          for (int p = 0; p < a.parts; ++p) t += __ldg(a.sums + (long long)p * a.out + c + k);
-          t *= a.scale;
-          a.db[c + k] = a.keep != 0.f ? fmaf(a.keep, a.db[c + k], t) : t;
-        }
-    }
-    if (DT == DK_BF16 && !a.copy_dy) return;
-    for (long long r = (long long)part * 8 + warp; r < a.rows; r += (long long)row_parts * 8) {
-      if constexpr (DT == DK_F32) {
-        const float* s = static_cast<const float*>(a.dy) + r * a.out + c;
-        float v[8];
-        if (a.out % 4 == 0 && c + 8 <= a.out) {
-          const float4 x = __ldg(reinterpret_cast<const float4*>(s)), y = __ldg(reinterpret_cast<const float4*>(s) + 1);
-          v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = c + k < a.out ? __ldg(s + k) : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= f[k];
-        g16::store_planes<8>(static_cast<__half*>(a.hi) + r * a.op + c, static_cast<__half*>(a.lo) + r * a.op + c, v, 8);
-      } else {
-        const uint16_t* s = static_cast<const uint16_t*>(a.dy) + r * a.out + c;
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          w[k] = (c + 2 * k < a.out ? (uint32_t)s[2 * k] : 0u) | (c + 2 * k + 1 < a.out ? (uint32_t)s[2 * k + 1] << 16 : 0u);
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.hi) + r * a.op + c) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-    return;
-  }
-  int s = 0;
-  if constexpr (DT == DK_F32) {
-    __shared__ unsigned int se[8];
-    unsigned int e = 0;
-    for (int i = threadIdx.x; i < a.blocks; i += kThreads) e = max(e, __ldg(a.block_exp + i));
-    e = __reduce_max_sync(0xffffffffu, e);
-    if (lane == 0) se[warp] = e;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 8; ++w) e = max(e, se[w]);
-    if ((int)blockIdx.x == grid_dy && threadIdx.x == 0) a.block_exp[kMaxBlocks] = e;
-    s = x_exp(e);
-  }
+__device__ __forceinline__ void expand(const Wg8& a, int s, long long i0, long long step) {
   constexpr int U = 4;
-  const long long units = a.rows * (a.dp / 8), step = (long long)(gridDim.x - grid_dy) * kThreads;
-  for (long long i = (long long)(blockIdx.x - grid_dy) * kThreads + threadIdx.x; i < units; i += U * step) {
+  const long long units = a.rows * (a.dp / 8);
+  for (long long i = i0; i < units; i += U * step) {
     ckpt8::Raw<8> r[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -226,6 +89,181 @@ __global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int 
       *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.x16) + (i + u * step) * 8) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
+}
+
+// Columns of dy: their sums and (fp32) largest magnitudes, over parts of the rows; a CTA has a strip of 32 vectors of 16
+// bytes.  bf16: rows of no whole vectors are copied to a pitch of such; the last CTA of a strip to be done joins db; and
+// the CTAs behind those of dy expand the checkpoint, so nothing else comes before the product.  fp32: they look for the
+// checkpoint's largest exponent.
+template <int DT, int VEC>
+__global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
+  chained_launch();
+  constexpr int FULL = DT == DK_F32 ? 4 : 8, NV = FULL / VEC, U = NV >= 4 ? 2 : 8 / NV;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, columns = a.with_sums ? a.strips * a.parts : 0;
+  if ((int)blockIdx.x >= columns) {
+    const long long i0 = (long long)(blockIdx.x - columns) * kThreads + threadIdx.x, step = (long long)(gridDim.x - columns) * kThreads;
+    if constexpr (DT == DK_BF16) {
+      expand<DT>(a, 0, i0, step);
+    } else {
+      // (four bytes at a time; those of the end, and 255, by themselves)
+      const long long n = a.rows * (a.dp / ckpt8::kBlock);
+      unsigned int e = 0;
+      for (long long i = i0; i < n / 4; i += step) {
+        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(a.exps) + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const unsigned int b = w >> 8 * k & 255u;
+          e = max(e, b == 255u ? 0u : b);
+        }
+      }
+      for (long long i = n / 4 * 4 + i0; i < n; i += step) e = max(e, a.exps[i] == 255u ? 0u : (unsigned)a.exps[i]);
+      e = __reduce_max_sync(0xffffffffu, e);
+      __shared__ unsigned int se[8];
+      if (lane == 0) se[warp] = e;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+#pragma unroll
+        for (int w = 1; w < 8; ++w) e = max(e, se[w]);
+        a.block_exp[blockIdx.x - columns] = e;
+      }
+    }
+    return;
+  }
+  const int strip = blockIdx.x % a.strips, part = blockIdx.x / a.strips, c0 = strip * 32 * FULL + lane * VEC;
+  const long long per = (a.rows + a.parts - 1) / a.parts;
+  const long long r0 = part * per, r1 = min(a.rows, r0 + per);
+  float s[NV][VEC];
+  unsigned int m[NV][VEC];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) { s[j][k] = 0.f; m[j][k] = 0u; }
+  for (long long r = r0 + warp; r < r1; r += 8 * U) {
+    typename Vec<DT, VEC>::Raw raw[U][NV];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (r + 8 * u < r1 && c0 + j * 32 * VEC < a.out) raw[u][j] = Vec<DT, VEC>::get(a.dy, (r + 8 * u) * a.out + c0 + j * 32 * VEC);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = c0 + j * 32 * VEC;
+        if (r + 8 * u >= r1 || c >= a.op) continue;
+        if (c < a.out) {
+          float v[VEC];
+          Vec<DT, VEC>::unpack(raw[u][j], v);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            s[j][k] += v[k];
+            if (DT == DK_F32) m[j][k] = max(m[j][k], magnitude(__float_as_uint(v[k])));
+          }
+        } else {
+          raw[u][j] = typename Vec<DT, VEC>::Raw{};
+        }
+        if (DT == DK_BF16 && a.copy_dy) Vec<DT, VEC>::put(a.hi, (r + 8 * u) * a.op + c, raw[u][j]);
+      }
+  }
+  __shared__ float ss[8][32 * FULL + 1];
+  __shared__ unsigned int sm[DT == DK_F32 ? 8 : 1][32 * FULL + 1];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      ss[warp][j * 32 * VEC + lane * VEC + k] = s[j][k];
+      if (DT == DK_F32) sm[warp][j * 32 * VEC + lane * VEC + k] = m[j][k];
+    }
+  __syncthreads();
+  const int i = threadIdx.x, col = strip * 32 * FULL + i;
+  if (i < 32 * FULL && col < a.out) {
+    float t = 0.f;
+    unsigned int u = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      t += ss[w][i];
+      if (DT == DK_F32) u = max(u, sm[w][i]);
+    }
+    __stcg(a.sums + (long long)part * a.out + col, t);
+    if (DT == DK_F32) a.most[(long long)part * a.out + col] = u;
+  }
+  if constexpr (DT == DK_BF16) {
+    if (a.db == nullptr) return;
+    __shared__ unsigned int last;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(a.count + strip, 1u) + 1u == (unsigned)a.parts;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    if (threadIdx.x == 0) a.count[strip] = 0u;
+    if (i < 32 * FULL && col < a.out) join_db(a, col);
+  }
+}
+
+// fp32: the operands.  The first CTAs take dy's columns (grid_dy of them: strips of 256 columns by row parts), the others the
+// checkpoint.
+__global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int strips, int row_parts, int grid_dy) {
+  chained_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if ((int)blockIdx.x < grid_dy) {
+    const int strip = blockIdx.x % strips, part = blockIdx.x / strips;
+    const int c = strip * 256 + lane * 8;
+    if (c >= a.op) return;
+    unsigned int m[8];
+    float f[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = 0u;
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < a.out) m[k] = max(m[k], __ldg(a.most + (long long)p * a.out + c + k));
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      f[k] = pow2(scale_exp(m[k]));
+      if (part == 0 && warp == 0 && c + k < a.out) a.most_all[c + k] = m[k];
+      if (part == 0 && warp == 1 && a.db != nullptr && c + k < a.out) join_db(a, c + k);
+    }
+    constexpr int U = 4;
+    const bool whole = a.out % 4 == 0 && c + 8 <= a.out;
+    const long long step = (long long)row_parts * 8;
+    for (long long r = (long long)part * 8 + warp; r < a.rows; r += U * step) {
+      float v[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (r + u * step >= a.rows) continue;
+        const float* s = static_cast<const float*>(a.dy) + (r + u * step) * a.out + c;
+        if (whole) {
+          const float4 x = __ldg(reinterpret_cast<const float4*>(s)), y = __ldg(reinterpret_cast<const float4*>(s) + 1);
+          v[u][0] = x.x; v[u][1] = x.y; v[u][2] = x.z; v[u][3] = x.w; v[u][4] = y.x; v[u][5] = y.y; v[u][6] = y.z; v[u][7] = y.w;
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[u][k] = c + k < a.out ? __ldg(s + k) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (r + u * step >= a.rows) continue;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[u][k] *= f[k];
+        const long long at = (r + u * step) * a.op + c;
+        g16::store_planes<8>(static_cast<__half*>(a.hi) + at, static_cast<__half*>(a.lo) + at, v[u], 8);
+      }
+    }
+    return;
+  }
+  __shared__ unsigned int se[8];
+  unsigned int e = 0;
+  for (int i = threadIdx.x; i < a.blocks; i += kThreads) e = max(e, __ldg(a.block_exp + i));
+  e = __reduce_max_sync(0xffffffffu, e);
+  if (lane == 0) se[warp] = e;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) e = max(e, se[w]);
+  if ((int)blockIdx.x == grid_dy && threadIdx.x == 0) a.block_exp[kMaxBlocks] = e;
+  expand<DK_F32>(a, x_exp(e), (long long)(blockIdx.x - grid_dy) * kThreads + threadIdx.x, (long long)(gridDim.x - grid_dy) * kThreads);
 }
 
 // dW = keep*dW + scale*product, the operands' powers of two undone
@@ -269,7 +307,7 @@ struct EpiW {
 
 // the same without a dW to add to, rows of whole 16 bytes: stored by TMA
 struct EpiWBulk {
-  static constexpr bool kAhead = false, kTail = true, kBulk = true;
+  static constexpr bool kTail = true, kBulk = true;
   EpiW w;
   template <int NH>
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int row, int col0, char* sm,
@@ -334,9 +372,8 @@ Plan plan_of(const dk_wgrad8& q) {
   p.dp = ckpt8::padded(q.d);
   p.op = (q.out + 7) / 8 * 8;
   p.copy_dy = p.f32 || q.out % 8 != 0;
-  int vec = p.f32 ? 4 : 8;
-  while (q.out % vec) vec /= 2;
-  p.strips = (q.out + 32 * vec - 1) / (32 * vec);
+  const int wide = 32 * (p.f32 ? 4 : 8);
+  p.strips = (p.op + wide - 1) / wide;
   // parts of the rows: two CTAs for every SM, 32 rows each at least
   long long parts = 2 * 148 / p.strips;
   if (parts > kMaxParts) parts = kMaxParts;
@@ -383,22 +420,28 @@ dk_status run(dk_ctx* ctx, const dk_wgrad8& q, const Plan& pl, Wg8& a, float* dW
   char* ws = static_cast<char*>(ctx->ws);
   int vec = F32 ? 4 : 8;
   while (q.out % vec) vec /= 2;
-  if (F32 || a.db != nullptr) {
-    const dim3 grid((unsigned)pl.strips, (unsigned)pl.parts);
-    a.blocks = (int)(grid.x * grid.y < kMaxBlocks ? grid.x * grid.y : kMaxBlocks);
-    DK_CUDA_CHECK(columns<DT>(a, grid, vec, st));
-    count_launches(ctx, DK_KERNEL_OTHER, 1);
+  long long grid_x = (q.rows * (pl.dp / 8) + kThreads - 1) / kThreads;      // of what expands the checkpoint
+  if (grid_x > 8LL * sms) grid_x = 8LL * sms;
+  a.with_sums = F32 || a.db != nullptr || pl.copy_dy;
+  a.strips = pl.strips;
+  a.count = step_counters(ctx);
+  if (pl.strips > kStepCounters) return DK_ERR_SHAPE;
+  long long more = grid_x;
+  if (F32) {
+    more = (q.rows * (pl.dp / ckpt8::kBlock) / 4 + kThreads - 1) / kThreads;
+    if (more < 1) more = 1;
+    if (more > kMaxBlocks) more = kMaxBlocks;
   }
-  {
+  a.blocks = (int)more;
+  DK_CUDA_CHECK(columns<DT>(a, dim3((unsigned)((a.with_sums ? pl.strips * pl.parts : 0) + more)), vec, st));
+  if (F32) {
     const int strips = (pl.op + 255) / 256;
     long long row_parts = (q.rows + 31) / 32;
     if (row_parts > 8LL * sms / strips) row_parts = 8LL * sms / strips;
-    if (row_parts < 1 || !pl.copy_dy) row_parts = 1;
-    const int grid_dy = pl.copy_dy || a.db != nullptr ? (int)(strips * row_parts) : 0;
-    long long grid_x = (q.rows * (pl.dp / 8) + kThreads - 1) / kThreads;
-    if (grid_x > 8LL * sms) grid_x = 8LL * sms;
-    DK_CUDA_CHECK(launch_chained(wgrad8_prep_kernel<DT>, dim3((unsigned)(grid_dy + grid_x)), kThreads, 0, st, a, strips,
-                                 (int)row_parts, grid_dy, a.db != nullptr ? 1 : 0));
+    if (row_parts < 1) row_parts = 1;
+    const int grid_dy = (int)(strips * row_parts);
+    DK_CUDA_CHECK(launch_chained(wgrad8_prep_kernel, dim3((unsigned)(grid_dy + grid_x)), kThreads, 0, st, a, strips, (int)row_parts,
+                                 grid_dy));
   }
   const size_t plane = (size_t)q.rows * pl.op;
   const Operand dy{pl.copy_dy ? (const void*)a.hi : a.dy, static_cast<const uint16_t*>(a.hi) + plane, q.rows, q.out, pl.op, 0};
@@ -492,7 +535,7 @@ dk_status dk_linear_bwd_wgrad_ckpt8(dk_ctx* ctx, const dk_wgrad8* q, const void*
   a.parts = pl.parts;
   a.copy_dy = pl.copy_dy;
   a.scale = scale; a.keep = keep;
-  ProfScope ps(ctx, DK_KERNEL_OTHER, 2, st);
+  ProfScope ps(ctx, DK_KERNEL_OTHER, pl.f32 ? 3 : 2, st);
   return pl.f32 ? run<true>(ctx, *q, pl, a, dW, st) : run<false>(ctx, *q, pl, a, dW, st);
 }
 

@@ -160,7 +160,8 @@ def wgrad_bound(dy, x, dtype):
 
 
 WGRADS = [(1, 1, 1), (1, 16, 8), (3, 33, 5), (64, 512, 1000), (65, 60, 129), (128, 256, 256), (2047, 1001, 1502), (500, 64, 7),
-          (4096, 512, 384), (256, 5000, 700), (33000, 40, 24), (1000, 96, 2050), (129, 2048, 4096)]
+          (4096, 512, 384), (256, 5000, 700), (33000, 40, 24), (1000, 96, 2050), (129, 2048, 4096),
+          (4000, 2560, 2560), (3900, 2562, 2500), (70, 33, 4001), (2100, 64, 66000)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
