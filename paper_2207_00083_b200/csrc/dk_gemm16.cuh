@@ -71,6 +71,10 @@ struct Asks<E, std::void_t<decltype(E::kTail)>> {
   static constexpr bool tail = E::kTail, bulk = E::kBulk;
 };
 
+// shared memory of an epilogue warp
+template <class E>
+constexpr int kRowsMem = Asks<E>::bulk ? 8192 : 4096;
+
 // a stored matrix: `rows` rows of `cols` contiguous elements, `pitch` elements apart (a multiple of 8), one or two
 // planes
 struct Operand {
@@ -241,7 +245,7 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                          ~static_cast<uintptr_t>(1023));
   char* rows_mem = reinterpret_cast<char*>(smem + (size_t)p.nstages * STAGE);
-  unsigned char* ctrl = reinterpret_cast<unsigned char*>(rows_mem + kEpi * 4096);
+  unsigned char* ctrl = reinterpret_cast<unsigned char*>(rows_mem + kEpi * kRowsMem<Epi>);
   uint64_t* full_bar = reinterpret_cast<uint64_t*>(ctrl);      // used in the leader only
   uint64_t* empty_bar = full_bar + tc::kMaxStages;
   uint64_t* tfull_bar = empty_bar + tc::kMaxStages;
@@ -359,6 +363,8 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
       int batch, ks, mt, nt, kb_lo, kb_hi;
       item_tile<TAIL>(p, w, batch, ks, mt, nt);
       item_stages<TAIL>(p, w, kb_lo, kb_hi);
+      [[maybe_unused]] float2 ahead;      // (what `before` reads is on its way while the products run)
+      if constexpr (Asks<Epi>::bulk) ahead = epi.before(p, mt * TILE_M + (int)rank * ROWS + quad * 32 + lane);
       for (int kb = kb_lo; kb < kb_hi; kb += p.chunk, ++acc_it) {
         const uint32_t buf = acc_it & 1u, aphase = (acc_it >> 1) & 1u;
         if (!tc::mbar_wait(tfull_bar + buf, aphase, abort_flag, p.spin_cap)) { alive = false; break; }
@@ -391,9 +397,12 @@ gemm16_kernel(const __grid_constant__ CUtensorMap map_a_hi, const __grid_constan
       if constexpr (TAIL) {
         if (w >= p.tail_from && !join_tail<NH>(p, w, rank, warp - 4, acc)) continue;
       }
-      const int row = mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, col0 = nt * BN + half * NH;
-      if constexpr (Asks<Epi>::bulk) epi(p, acc, row, col0, rows_mem + (warp - 4) * 4096, &map_b_lo);
-      else epi(p, acc, batch, ks, row, col0, rows_mem + (warp - 4) * 4096);
+      if constexpr (Asks<Epi>::bulk)
+        epi(p, acc, mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, nt * BN + half * NH, ahead,
+            rows_mem + (warp - 4) * kRowsMem<Epi>, &map_b_lo);
+      else
+        epi(p, acc, batch, ks, mt * TILE_M + (int)rank * ROWS + quad * 32 + lane, nt * BN + half * NH,
+            rows_mem + (warp - 4) * 4096);
     }
     if constexpr (Asks<Epi>::bulk) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
@@ -797,26 +806,28 @@ __device__ __forceinline__ void store_terms(const float (&v)[NH], char* sm, __ha
   }
 }
 
-// fp32 rows of a warp stored by TMA: 32 columns at a time through the warp's 4 KiB of shared memory (128-byte rows, their
-// 16-byte pieces exchanged as the 128-byte swizzle has them, so the writes meet no bank twice).  The map clips what lies
-// outside the matrix.  A tile of 256 x 256 costs the epilogue a third of the instructions of warp_rows_f32.
+// fp32 rows of a warp stored by TMA: 32 columns at a time through the two halves of the warp's 8 KiB of shared memory
+// (128-byte rows, their 16-byte pieces exchanged as the 128-byte swizzle has them, so the writes meet no bank twice).  The
+// map clips what lies outside the matrix.  A tile of 256 x 256 takes half the instructions of warp_rows_f32 (256 rows, 25088
+// x 4096 fp32: 1568 tiles of four stages, the product takes 172 us with warp_rows_f32, 121 with one half, 110 with two).
 template <int NH>
 __device__ __forceinline__ void warp_rows_bulk(const float (&v)[NH], char* sm, const CUtensorMap* map, int row0, int col0, int cols) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int c = 0; c < NH; c += 32) {
     if (c >= cols) break;
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    char* const to = sm + (c / 32 & 1) * 4096;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
     __syncwarp();
 #pragma unroll
     for (int q = 0; q < 8; ++q)
-      *reinterpret_cast<float4*>(sm + lane * 128 + ((q ^ (lane & 7)) << 4)) =
+      *reinterpret_cast<float4*>(to + lane * 128 + ((q ^ (lane & 7)) << 4)) =
           make_float4(v[c + 4 * q], v[c + 4 * q + 1], v[c + 4 * q + 2], v[c + 4 * q + 3]);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) {
       asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"((col0 + c) * 4),
-                   "r"(row0), "r"(smem_u32(sm))
+                   "r"(row0), "r"(smem_u32(to))
                    : "memory");
       asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
@@ -992,7 +1003,7 @@ dk_status launch(dk_ctx* ctx, const Operand& A, const Operand& B, Params p, cons
     return DK_ERR_CUDA;
   constexpr int STAGE = stage_bytes<NPROD, BN>();
   constexpr int CTRL = (2 * tc::kMaxStages + 4) * 8 + 16;
-  constexpr int ROWS_MEM = kEpi * 4096;
+  constexpr int ROWS_MEM = kEpi * kRowsMem<Epi>;
   p.nstages = (227 * 1024 - 1024 - CTRL - ROWS_MEM) / STAGE;
   if (p.nstages > tc::kMaxStages) p.nstages = tc::kMaxStages;
   const int smem = p.nstages * STAGE + ROWS_MEM + CTRL + 1024;

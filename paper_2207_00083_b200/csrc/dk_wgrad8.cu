@@ -92,9 +92,9 @@ __device__ __forceinline__ void expand(const Wg8& a, int s, long long i0, long l
 }
 
 // Columns of dy: their sums and (fp32) largest magnitudes, over parts of the rows; a CTA has a strip of 32 vectors of 16
-// bytes.  bf16: rows of no whole vectors are copied to a pitch of such; the last CTA of a strip to be done joins db; and
-// the CTAs behind those of dy expand the checkpoint, so nothing else comes before the product.  fp32: they look for the
-// checkpoint's largest exponent.
+// bytes.  bf16: rows of no whole vectors are copied to a pitch of such; and the
+// CTAs behind those of dy expand the checkpoint, so nothing else comes before the product.  fp32: they look for the
+// checkpoint's largest exponent.  The last CTA of a strip to be done joins its parts.
 template <int DT, int VEC>
 __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
   chained_launch();
@@ -185,19 +185,24 @@ __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
       if (DT == DK_F32) u = max(u, sm[w][i]);
     }
     __stcg(a.sums + (long long)part * a.out + col, t);
-    if (DT == DK_F32) a.most[(long long)part * a.out + col] = u;
+    if (DT == DK_F32) __stcg(a.most + (long long)part * a.out + col, u);
   }
-  if constexpr (DT == DK_BF16) {
-    if (a.db == nullptr) return;
-    __shared__ unsigned int last;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(a.count + strip, 1u) + 1u == (unsigned)a.parts;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    if (threadIdx.x == 0) a.count[strip] = 0u;
-    if (i < 32 * FULL && col < a.out) join_db(a, col);
+  if (DT == DK_BF16 && a.db == nullptr) return;
+  __shared__ unsigned int last;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(a.count + strip, 1u) + 1u == (unsigned)a.parts;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  if (threadIdx.x == 0) a.count[strip] = 0u;
+  if (i >= 32 * FULL || col >= a.out) return;
+  if (a.db != nullptr) join_db(a, col);
+  if constexpr (DT == DK_F32) {
+    unsigned int u = 0;
+#pragma unroll 8
+    for (int p = 0; p < a.parts; ++p) u = max(u, __ldcg(a.most + (long long)p * a.out + col));
+    a.most_all[col] = u;
   }
 }
 
@@ -210,22 +215,9 @@ __global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int 
     const int strip = blockIdx.x % strips, part = blockIdx.x / strips;
     const int c = strip * 256 + lane * 8;
     if (c >= a.op) return;
-    unsigned int m[8];
     float f[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m[k] = 0u;
-#pragma unroll 4
-    for (int p = 0; p < a.parts; ++p) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (c + k < a.out) m[k] = max(m[k], __ldg(a.most + (long long)p * a.out + c + k));
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      f[k] = pow2(scale_exp(m[k]));
-      if (part == 0 && warp == 0 && c + k < a.out) a.most_all[c + k] = m[k];
-      if (part == 0 && warp == 1 && a.db != nullptr && c + k < a.out) join_db(a, c + k);
-    }
+    for (int k = 0; k < 8; ++k) f[k] = c + k < a.out ? pow2(scale_exp(__ldg(a.most_all + c + k))) : 0.f;
     constexpr int U = 4;
     const bool whole = a.out % 4 == 0 && c + 8 <= a.out;
     const long long step = (long long)row_parts * 8;
@@ -309,15 +301,18 @@ struct EpiW {
 struct EpiWBulk {
   static constexpr bool kTail = true, kBulk = true;
   EpiW w;
+  __device__ __forceinline__ float2 before(const Params& p, int row) const {
+    float f1;
+    const float f0 = w.undo(min(row, p.M - 1), f1);
+    return make_float2(f0 * w.scale, f1);
+  }
   template <int NH>
-  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int row, int col0, char* sm,
+  __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int row, int col0, float2 f, char* sm,
                                              const CUtensorMap* map) const {
     const int row0 = row - (int)(threadIdx.x & 31);
     if (row0 >= p.M || col0 >= p.N) return;
-    float f1;
-    const float f0 = w.undo(min(row, p.M - 1), f1) * w.scale;
 #pragma unroll
-    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1;
+    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f.x * f.y;
     g16::warp_rows_bulk<NH>(acc, sm, map, row0, col0, p.N - col0);
   }
 };
