@@ -24,54 +24,55 @@ struct Args {
   int dp;
 };
 
-template <int DT, int VEC, bool WHOLE>
-__device__ __forceinline__ void load_unit(const void* x, long long row, int c, int d, float (&v)[VEC]) {
-  if constexpr (WHOLE) {
-    if (c < d) {
-      Vec<DT, VEC>::load(x, row * d + c, v);
-      return;
-    }
+// How rows lie: whole vectors and whole blocks (one flat array), whole vectors, or neither.
+enum { FLAT = 0, WHOLE = 1, RAGGED = 2 };
+
+// vector i of the padded rows, as stored (zero behind the row)
+template <int DT, int VEC, int WAY>
+__device__ __forceinline__ typename Vec<DT, VEC>::Raw load_unit(const Args& a, long long i) {
+  using V = Vec<DT, VEC>;
+  if constexpr (WAY == FLAT) return V::get(a.x, i * VEC);
+  const long long row = __umul64hi((unsigned long long)i, a.recip);
+  const int c = (int)(i - row * a.per) * VEC;
+  if constexpr (WAY == WHOLE) {
+    if (c < a.d) return V::get(a.x, row * a.d + c);
+    return typename V::Raw{};
   }
+  float v[VEC];
 #pragma unroll
   for (int k = 0; k < VEC; ++k) {
-    v[k] = 0.f;
-    if (!WHOLE && c + k < d) {
-      float t[1];
-      Vec<DT, 1>::load(x, row * d + c + k, t);
-      v[k] = t[0];
-    }
+    float t[1] = {0.f};
+    if (c + k < a.d) Vec<DT, 1>::load(a.x, row * a.d + c + k, t);
+    v[k] = t[0];
   }
+  return V::pack(v);
 }
 
-template <int DT, bool WHOLE, int U>
+template <int DT, int WAY, int U>
 __global__ void __launch_bounds__(kThreads) ckpt8_store_kernel(const Args a) {
   constexpr int VEC = DT == DK_F32 ? 4 : 8;
   chained_launch();
   const long long i0 = (long long)blockIdx.x * (kThreads * U) + threadIdx.x;
-  float v[U][VEC];
+  typename Vec<DT, VEC>::Raw raw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const long long i = i0 + u * kThreads;
-    const long long row = __umul64hi((unsigned long long)i, a.recip);
-    if (i < a.units) {
-      load_unit<DT, VEC, WHOLE>(a.x, row, (int)(i - row * a.per) * VEC, a.d, v[u]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) v[u][k] = 0.f;
-    }
+    raw[u] = {};
+    if (i0 + u * kThreads < a.units) raw[u] = load_unit<DT, VEC, WAY>(a, i0 + u * kThreads);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const long long i = i0 + u * kThreads;
-    const ckpt8::Scale s = ckpt8::scale_of(ckpt8::block_most<VEC>(v[u]));
+    float v[VEC];
+    Vec<DT, VEC>::unpack(raw[u], v);
+    const ckpt8::Scale s = ckpt8::scale_of(ckpt8::block_most<VEC>(v));
     if (i < a.units) {
-      ckpt8::put_codes<VEC>(a.codes + i * VEC, v[u], s);
+      ckpt8::put_codes<VEC>(a.codes + i * VEC, v, s);
       if ((threadIdx.x & (ckpt8::kBlock / VEC - 1)) == 0) a.exps[i * VEC / ckpt8::kBlock] = (uint8_t)s.byte;
     }
   }
 }
 
-template <int DT, bool WHOLE, int U>
+template <int DT, int WAY, int U>
 __global__ void __launch_bounds__(kThreads) ckpt8_load_kernel(const Args a) {
   constexpr int VEC = DT == DK_F32 ? 4 : 8;
   chained_launch();
@@ -86,11 +87,15 @@ __global__ void __launch_bounds__(kThreads) ckpt8_load_kernel(const Args a) {
   for (int u = 0; u < U; ++u) {
     const long long i = i0 + u * kThreads;
     if (i >= a.units) continue;
-    const long long row = __umul64hi((unsigned long long)i, a.recip);
-    const int c = (int)(i - row * a.per) * VEC;
     float v[VEC];
     ckpt8::unpack<VEC>(r[u], v);
-    if constexpr (WHOLE) {
+    if constexpr (WAY == FLAT) {
+      Vec<DT, VEC>::store(a.y, i * VEC, v);
+      continue;
+    }
+    const long long row = __umul64hi((unsigned long long)i, a.recip);
+    const int c = (int)(i - row * a.per) * VEC;
+    if constexpr (WAY == WHOLE) {
       if (c < a.d) Vec<DT, VEC>::store(a.y, row * a.d + c, v);
     } else {
 #pragma unroll
@@ -111,10 +116,19 @@ dk_status check(const dk_ckpt8* q) {
   return DK_OK;
 }
 
-template <int DT, bool WHOLE, int U>
-cudaError_t launch_one(const Args& a, bool store, cudaStream_t st) {
-  const dim3 grid((unsigned)((a.units + kThreads * U - 1) / (kThreads * U)));
-  return launch_chained(store ? ckpt8_store_kernel<DT, WHOLE, U> : ckpt8_load_kernel<DT, WHOLE, U>, grid, kThreads, 0, st, a);
+template <int DT, int WAY>
+cudaError_t launch_one(const Args& a, bool store, bool many, cudaStream_t st) {
+  const int u = many ? 4 : 1;
+  const dim3 grid((unsigned)((a.units + kThreads * u - 1) / (kThreads * u)));
+  auto kern = store ? (many ? ckpt8_store_kernel<DT, WAY, 4> : ckpt8_store_kernel<DT, WAY, 1>)
+                    : (many ? ckpt8_load_kernel<DT, WAY, 4> : ckpt8_load_kernel<DT, WAY, 1>);
+  return launch_chained(kern, grid, kThreads, 0, st, a);
+}
+template <int DT>
+cudaError_t launch_way(const Args& a, bool store, bool many, cudaStream_t st) {
+  if (a.d == a.dp) return launch_one<DT, FLAT>(a, store, many, st);
+  if (a.d % (DT == DK_F32 ? 4 : 8) == 0) return launch_one<DT, WHOLE>(a, store, many, st);
+  return launch_one<DT, RAGGED>(a, store, many, st);
 }
 
 }  // namespace
@@ -131,16 +145,9 @@ dk_status launch_ckpt8(const dk_ckpt8& q, bool store, const void* x, void* y, vo
   a.per = a.dp / vec;
   a.units = q.rows * a.per;
   a.recip = ~0ull / (unsigned)a.per + 1;
-  const bool whole = q.d % vec == 0;
   // four vectors a thread where that leaves every SM its threads, one for the sake of latency otherwise
   const bool many = a.units >= 4LL * 2048 * sms;
-  cudaError_t e;
-#define DK_CKPT8(DT)                                                                                              \
-  e = whole ? (many ? launch_one<DT, true, 4>(a, store, st) : launch_one<DT, true, 1>(a, store, st))              \
-            : (many ? launch_one<DT, false, 4>(a, store, st) : launch_one<DT, false, 1>(a, store, st))
-  if (q.dtype == DK_F32) DK_CKPT8(DK_F32);
-  else DK_CKPT8(DK_BF16);
-#undef DK_CKPT8
+  const cudaError_t e = q.dtype == DK_F32 ? launch_way<DK_F32>(a, store, many, st) : launch_way<DK_BF16>(a, store, many, st);
   return e == cudaSuccess ? DK_OK : DK_ERR_CUDA;
 }
 

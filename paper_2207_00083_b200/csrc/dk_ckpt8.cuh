@@ -122,16 +122,16 @@ __device__ __forceinline__ float abs_max(float a, float b, float c) {
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// the largest magnitude (as bits) over the lanes of a block: 32/VEC neighbours
+// the largest magnitude (as bits) over the lanes of a block: 32/VEC neighbours, `lanes` of the warp taking part
 template <int VEC>
-__device__ __forceinline__ uint32_t block_most(const float (&v)[VEC]) {
+__device__ __forceinline__ uint32_t block_most(const float (&v)[VEC], unsigned lanes = 0xffffffffu) {
   float f = abs_max(v[0], v[VEC > 1 ? 1 : 0], v[VEC > 2 ? 2 : 0]);
 #pragma unroll
   for (int i = 3; i < VEC; i += 2) f = abs_max(f, v[i], v[i + 1 < VEC ? i + 1 : i]);
   uint32_t m = __float_as_uint(f);
-  if constexpr (VEC == 1) return __reduce_max_sync(0xffffffffu, m);
+  if constexpr (VEC == 1) return __reduce_max_sync(lanes, m);
 #pragma unroll
-  for (int o = kBlock / VEC / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (int o = kBlock / VEC / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
   return m;
 }
 

@@ -67,6 +67,8 @@ struct NormParams {
   long long n;
   long long rows;         // of csum
   int pix, c, groups, cg, slabs, slab_pix, act;
+  uint8_t* keep_codes;    // forward: the checkpoint that is written
+  uint8_t* keep_exps;
   int dp;                 // codes of a checkpoint's row
   int TX, TY;             // threads along the channel vectors, and along the pixels
   int param_blocks;       // of norm_apply_kernel
@@ -102,6 +104,14 @@ struct XVectors<DT, VEC, true> {
   }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[VEC]) { ckpt8::unpack<VEC>(r, v); }
 };
+
+// where a vector of a sample's first pixel is kept
+__device__ __forceinline__ uint8_t* kept_codes(const NormParams& p, long long s, int ch) {
+  return p.keep_codes + s * p.pix * (long long)p.dp + ch;
+}
+__device__ __forceinline__ uint8_t* kept_exps(const NormParams& p, long long s, int ch) {
+  return p.keep_exps + s * p.pix * (long long)(p.dp / ckpt8::kBlock) + ch / ckpt8::kBlock;
+}
 
 // Sums of the pixels [b, e) (every TY-th from ty on) of the channel vector at `base`: forward, about a pivot per batch.
 template <int DT, int VEC>
@@ -173,12 +183,13 @@ __device__ __forceinline__ void sum_gradients(const XVectors<DT, VEC, K8>& x, co
   }
 }
 
-// The values of those pixels: y, or dx given the means m0 of q and m1 of q*xhat.
-template <int DT, int VEC, int ACT, bool FWD, bool K8>
+// The values of those pixels: y, or dx given the means m0 of q and m1 of q*xhat.  KEEP: and the checkpoint of x, whose blocks
+// of 32 channels lie in neighbouring lanes of the same pixel (codes, exps: of this vector in the sample's first pixel).
+template <int DT, int VEC, int ACT, bool FWD, bool K8, bool KEEP>
 __device__ __forceinline__ void write_values(const XVectors<DT, VEC, K8>& x, const void* dy, void* out, long long base, int b, int e,
                                              int c, int TY, const float (&mean)[VEC], const float (&rstd)[VEC],
                                              const float (&m0)[VEC], const float (&m1)[VEC], const float (&ga)[VEC],
-                                             const float (&be)[VEC]) {
+                                             const float (&be)[VEC], uint8_t* codes, uint8_t* exps, int dp) {
   constexpr int L = FWD || VEC < 8 ? 4 : 2;
   // z = (x - mean)*f + beta;  dx = rstd*((d*gamma - m0) - (x - mean)*c1)
   float f[VEC], c1[VEC];
@@ -198,6 +209,13 @@ __device__ __forceinline__ void write_values(const XVectors<DT, VEC, K8>& x, con
       if (i0 + u * TY < e) {
         float a[VEC];
         x.unpack(rx[u], a);
+        if constexpr (KEEP) {
+          constexpr unsigned LANES = 32 / VEC == 32 ? 0xffffffffu : (1u << (32 / VEC)) - 1u;
+          const int lane = threadIdx.x & 31;
+          const ckpt8::Scale s = ckpt8::scale_of(ckpt8::block_most<VEC>(a, LANES << (lane & ~(32 / VEC - 1) & 31)));
+          ckpt8::put_codes<VEC>(codes + (long long)(i0 + u * TY) * dp, a, s);
+          if ((lane & (32 / VEC - 1)) == 0) exps[(long long)(i0 + u * TY) * (dp / ckpt8::kBlock)] = (uint8_t)s.byte;
+        }
         if constexpr (FWD) {
 #pragma unroll
           for (int k = 0; k < VEC; ++k) a[k] = act_value(fmaf(a[k] - mean[k], f[k], be[k]), ACT);
@@ -363,7 +381,7 @@ __global__ void __launch_bounds__(256) norm_param_kernel(const NormParams p) {
 
 // The values.  A vector may hold channels of several groups.  Backward: the first p.param_blocks CTAs form the
 // parameters' gradients instead.
-template <int DT, int VEC, int ACT, bool FWD, bool K8>
+template <int DT, int VEC, int ACT, bool FWD, bool K8, bool KEEP>
 __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p) {
   chained_launch();
   if constexpr (!FWD) {
@@ -391,7 +409,9 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p
       mean[k] = st.x; rstd[k] = st.y; m0[k] = ms.x; m1[k] = ms.y;
       ga[k] = __ldg(p.gamma + v * VEC + k); be[k] = __ldg(p.beta + v * VEC + k);
     }
-    write_values<DT, VEC, ACT, FWD, K8>(XVectors<DT, VEC, K8>(p, s, v * VEC), p.dy, p.out, base + v * VEC, p0 + ty, p1, p.c, p.TY, mean, rstd, m0, m1, ga, be);
+    write_values<DT, VEC, ACT, FWD, K8, KEEP>(XVectors<DT, VEC, K8>(p, s, v * VEC), p.dy, p.out, base + v * VEC, p0 + ty, p1, p.c,
+                                              p.TY, mean, rstd, m0, m1, ga, be, kept_codes(p, s, v * VEC),
+                                              kept_exps(p, s, v * VEC), p.dp);
   }
 }
 
@@ -399,7 +419,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p
 // multiple of the number of blocks, so a CTA keeps its channels.  Dynamic shared memory: [TY][cb/VEC][3] or, backward,
 // [TY][cb][2], then [groups of a block][2].
 constexpr int kSampleThreads = 512;
-template <int DT, int VEC, int ACT, bool FWD, bool K8>
+template <int DT, int VEC, int ACT, bool FWD, bool K8, bool KEEP>
 __global__ void __launch_bounds__(kSampleThreads, 2) norm_sample_kernel(const NormParams p) {
   extern __shared__ float sm[];
   constexpr int NS = FWD ? 3 : 2;
@@ -476,7 +496,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) norm_sample_kernel(const No
         mean[k] = FWD ? t0 : given.x; rstd[k] = FWD ? t1 : given.y;
         m0[k] = t0; m1[k] = t1;
       }
-      write_values<DT, VEC, ACT, FWD, K8>(XVectors<DT, VEC, K8>(p, s, ch0), p.dy, p.out, base, ty, p.pix, p.c, p.TY, mean, rstd, m0, m1, ga, be);
+      write_values<DT, VEC, ACT, FWD, K8, KEEP>(XVectors<DT, VEC, K8>(p, s, ch0), p.dy, p.out, base, ty, p.pix, p.c, p.TY, mean,
+                                                rstd, m0, m1, ga, be, kept_codes(p, s, ch0), kept_exps(p, s, ch0), p.dp);
     }
     // (the next sample's sums go to `sm`, which was read before the second barrier; `st` is written after another one)
   }
@@ -602,9 +623,9 @@ NormPlan plan_norm(const dk_norm& q) {
 constexpr int kMaxSmem = 3 * kMaxC * (int)sizeof(float);
 
 // whole samples: one launch, and one for the parameters' gradients
-template <int DT, int VEC, int ACT, bool FWD, bool K8>
+template <int DT, int VEC, int ACT, bool FWD, bool K8, bool KEEP>
 dk_status run_sample(NormParams p, const NormPlan& pl, int device, int sms, cudaStream_t st) {
-  auto kern = norm_sample_kernel<DT, VEC, ACT, FWD, K8>;
+  auto kern = norm_sample_kernel<DT, VEC, ACT, FWD, K8, KEEP>;
   p.TX = pl.sTX; p.TY = pl.sTY; p.cb = pl.cb;
   const int nblk = p.c / p.cb;
   const size_t smem =
@@ -640,12 +661,12 @@ dk_status run_sums(NormParams p, const NormPlan& pl, int device, cudaStream_t st
   return launch_chained(kern, dim3((unsigned)(p.n * p.slabs)), kThreads, smem, st, p) == cudaSuccess ? DK_OK
                                                                                                      : DK_ERR_CUDA;
 }
-template <int DT, int VEC, int ACT, bool FWD, bool K8>
+template <int DT, int VEC, int ACT, bool FWD, bool K8, bool KEEP>
 dk_status run_apply(NormParams p, const NormPlan& pl, cudaStream_t st) {
   p.TX = pl.TX[1]; p.TY = pl.TY[1];
   p.rows = p.n;
   p.param_blocks = FWD ? 0 : (p.c + 15) / 16;
-  return launch_chained(norm_apply_kernel<DT, VEC, ACT, FWD, K8>, dim3((unsigned)(p.n * p.slabs + p.param_blocks)), kThreads, 0,
+  return launch_chained(norm_apply_kernel<DT, VEC, ACT, FWD, K8, KEEP>, dim3((unsigned)(p.n * p.slabs + p.param_blocks)), kThreads, 0,
                         st, p) == cudaSuccess
              ? DK_OK
              : DK_ERR_CUDA;
@@ -670,9 +691,9 @@ dk_status run_apply(NormParams p, const NormPlan& pl, cudaStream_t st) {
     DK_NORM_ACTS(DK_BF16, 1, CALL);                                     \
   } while (0)
 
-template <bool FWD, bool K8>
+template <bool FWD, bool K8, bool KEEP>
 dk_status dispatch_sample(const NormParams& p, const NormPlan& pl, int dtype, int device, int sms, cudaStream_t st) {
-#define DK_NORM_CALL(DT, V, ACT) run_sample<DT, V, ACT, FWD, K8>(p, pl, device, sms, st)
+#define DK_NORM_CALL(DT, V, ACT) run_sample<DT, V, ACT, FWD, K8, KEEP>(p, pl, device, sms, st)
   DK_NORM_TYPES(pl.vec, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
@@ -682,19 +703,19 @@ dk_status dispatch_sums(const NormParams& p, const NormPlan& pl, int dtype, int 
   DK_NORM_TYPES(FWD ? pl.vec : pl.wide, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
-template <bool FWD, bool K8>
+template <bool FWD, bool K8, bool KEEP>
 dk_status dispatch_apply(const NormParams& p, const NormPlan& pl, int dtype, cudaStream_t st) {
-#define DK_NORM_CALL(DT, V, ACT) run_apply<DT, V, ACT, FWD, K8>(p, pl, st)
+#define DK_NORM_CALL(DT, V, ACT) run_apply<DT, V, ACT, FWD, K8, KEEP>(p, pl, st)
   DK_NORM_TYPES(pl.wide, DK_NORM_CALL);
 #undef DK_NORM_CALL
 }
 
-template <bool FWD, bool K8>
+template <bool FWD, bool K8, bool KEEP>
 dk_status dispatch(const NormParams& p, const NormPlan& pl, int dtype, int device, int sms, cudaStream_t st) {
-  if (pl.sample[FWD ? 0 : 1]) return dispatch_sample<FWD, K8>(p, pl, dtype, device, sms, st);
+  if (pl.sample[FWD ? 0 : 1]) return dispatch_sample<FWD, K8, KEEP>(p, pl, dtype, device, sms, st);
   if (p.n > kStepCounters) DK_CUDA_CHECK(cudaMemsetAsync(p.count, 0, (size_t)p.n * sizeof(unsigned int), st));
   const dk_status s = dispatch_sums<FWD, K8>(p, pl, dtype, device, st);
-  return s == DK_OK ? dispatch_apply<FWD, K8>(p, pl, dtype, st) : s;
+  return s == DK_OK ? dispatch_apply<FWD, K8, KEEP>(p, pl, dtype, st) : s;
 }
 
 dk_status begin(dk_ctx* ctx, const dk_norm* q, NormPlan* pl, NormParams* p) {
@@ -735,13 +756,23 @@ dk_status norm_forward(dk_ctx* ctx, const dk_norm* q, const void* x, const float
   if (!dev.ok) return DK_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   p.x = x; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats;
-  ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, true) + (kept ? 1 : 0), st);
-  if (kept) {                                   // (first: y may be x)
+  // A checkpoint is written with the values where its blocks of 32 channels lie in one warp: whole blocks in a pixel and, for
+  // items of blocks of channels, in an item.  Else by a launch of its own, first: y may be x.  (64x56x56x64 fp32, both
+  // directions: 99 us with two launches, 8x with one; 27x37x53x60 takes two.)
+  const bool with = kept && q->c % ckpt8::kBlock == 0 && (!pl.sample[0] || pl.cb % ckpt8::kBlock == 0);
+  ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, true) + (kept && !with ? 1 : 0), st);
+  if (with) {
+    p.keep_codes = static_cast<uint8_t*>(ckpt);
+    p.keep_exps = p.keep_codes + ckpt8::code_bytes(q->n * p.pix, q->c);
+    p.dp = q->c;
+    return dispatch<true, false, true>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
+  }
+  if (kept) {
     const dk_ckpt8 k{q->n * p.pix, q->c, q->dtype};
     s = launch_ckpt8(k, true, x, nullptr, ckpt, ctx->sm_count, st);
     if (s != DK_OK) return s;
   }
-  return dispatch<true, false>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
+  return dispatch<true, false, false>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
 }
 
 // K8: x is a checkpoint
@@ -777,7 +808,7 @@ dk_status norm_backward(dk_ctx* ctx, const dk_norm* q, const void* dy, const voi
   p.dy = dy; p.out = dx; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float*>(stats);
   p.dgamma = dgamma; p.dbeta = dbeta;
   ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, false), st);
-  return dispatch<false, K8>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
+  return dispatch<false, K8, false>(p, pl, q->dtype, ctx->device, ctx->sm_count, st);
 }
 
 }  // namespace
