@@ -543,99 +543,113 @@ def dk_orthogonalize(ctx: Context, q: dk_ortho, x, scale: float, keep: float, ou
 # what is kept between the two directions in 8 bits, and the norms between two residual blocks: checkpoints are uint8
 # tensors of dk_ckpt8_bytes
 # ---------------------------------------------------------------------------
-def _padded(d: int) -> int:
-    return (d + 31) // 32 * 32
+# (A token between two blocks takes the GPU 4 us; what a call checks of its tensors is kept to four attributes each, and the
+# function is looked up once.)
+def _ptr(t: torch.Tensor, dtype, numel: int, device: int, what: str) -> int:
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {numel} elements on CUDA device {device}")
+    return t.data_ptr()
+
+
+def _kept_numel(rows: int, d: int) -> int:
+    blocks = (d + 31) // 32
+    return rows * blocks * 33
+
+
+_functions = {}
+
+
+def _call(name: str, *args):
+    f = _functions.get(name)
+    if f is None:
+        f = _functions[name] = getattr(lib(), name)
+    status = f(*args)
+    if status:
+        raise DkError(status, name)
 
 
 def dk_ckpt8_bytes(q: dk_ckpt8) -> int:
     n = ctypes.c_size_t()
-    _check(lib().dk_ckpt8_bytes(ctypes.byref(q), ctypes.byref(n)), "dk_ckpt8_bytes")
+    _call("dk_ckpt8_bytes", q, n)
     return n.value
 
 
-def _kept(ctx, t: torch.Tensor, rows: int, d: int, what: str) -> int:
-    n = rows * _padded(d) + rows * (_padded(d) // 32)
-    if t.dtype is not torch.uint8 or t.numel() != n or not t.is_contiguous() or t.get_device() != ctx.device:
-        raise ValueError(f"{what}: expected a contiguous uint8 tensor of {n} elements on CUDA device {ctx.device}")
-    return t.data_ptr()
-
-
 def dk_ckpt8_store(ctx: Context, q: dk_ckpt8, x, ckpt):
-    _check(lib().dk_ckpt8_store(ctx.handle, ctypes.byref(q), _typed(ctx, x, q.dtype, q.rows * q.d, "x"),
-                                _kept(ctx, ckpt, q.rows, q.d, "ckpt"), _raw_stream(ctx.device)), "dk_ckpt8_store")
+    dev, rows, d = ctx.device, q.rows, q.d
+    _call("dk_ckpt8_store", ctx.handle, q, _ptr(x, _STEP_TYPES.get(q.dtype), rows * d, dev, "x"),
+          _ptr(ckpt, torch.uint8, _kept_numel(rows, d), dev, "ckpt"), _raw_stream(dev))
 
 
 def dk_ckpt8_load(ctx: Context, q: dk_ckpt8, ckpt, x):
-    _check(lib().dk_ckpt8_load(ctx.handle, ctypes.byref(q), _kept(ctx, ckpt, q.rows, q.d, "ckpt"),
-                               _typed(ctx, x, q.dtype, q.rows * q.d, "x"), _raw_stream(ctx.device)), "dk_ckpt8_load")
+    dev, rows, d = ctx.device, q.rows, q.d
+    _call("dk_ckpt8_load", ctx.handle, q, _ptr(ckpt, torch.uint8, _kept_numel(rows, d), dev, "ckpt"),
+          _ptr(x, _STEP_TYPES.get(q.dtype), rows * d, dev, "x"), _raw_stream(dev))
 
 
 def dk_group_norm_fwd_ckpt8(ctx: Context, q: dk_norm, x, gamma, beta, y, stats, ckpt):
+    dev, t, f = ctx.device, _STEP_TYPES.get(q.dtype), torch.float32
     e, c, s = _norm_sizes(q)
-    _check(lib().dk_group_norm_fwd_ckpt8(ctx.handle, ctypes.byref(q), _typed(ctx, x, q.dtype, e, "x"),
-                                         _f32(ctx, gamma, c, "gamma"), _f32(ctx, beta, c, "beta"),
-                                         _typed(ctx, y, q.dtype, e, "y"), _f32(ctx, stats, s, "stats"),
-                                         _kept(ctx, ckpt, q.n * q.h * q.w, c, "ckpt"), _raw_stream(ctx.device)),
-           "dk_group_norm_fwd_ckpt8")
+    _call("dk_group_norm_fwd_ckpt8", ctx.handle, q, _ptr(x, t, e, dev, "x"), _ptr(gamma, f, c, dev, "gamma"),
+          _ptr(beta, f, c, dev, "beta"), _ptr(y, t, e, dev, "y"), _ptr(stats, f, s, dev, "stats"),
+          _ptr(ckpt, torch.uint8, _kept_numel(q.n * q.h * q.w, c), dev, "ckpt"), _raw_stream(dev))
 
 
 def dk_group_norm_bwd_ckpt8(ctx: Context, q: dk_norm, dy, ckpt, gamma, beta, stats, dx, dgamma, dbeta):
+    dev, t, f = ctx.device, _STEP_TYPES.get(q.dtype), torch.float32
     e, c, s = _norm_sizes(q)
-    _check(lib().dk_group_norm_bwd_ckpt8(ctx.handle, ctypes.byref(q), _typed(ctx, dy, q.dtype, e, "dy"),
-                                         _kept(ctx, ckpt, q.n * q.h * q.w, c, "ckpt"), _f32(ctx, gamma, c, "gamma"),
-                                         _f32(ctx, beta, c, "beta"), _f32(ctx, stats, s, "stats"),
-                                         _typed(ctx, dx, q.dtype, e, "dx"), _f32(ctx, dgamma, c, "dgamma"),
-                                         _f32(ctx, dbeta, c, "dbeta"), _raw_stream(ctx.device)),
-           "dk_group_norm_bwd_ckpt8")
+    _call("dk_group_norm_bwd_ckpt8", ctx.handle, q, _ptr(dy, t, e, dev, "dy"),
+          _ptr(ckpt, torch.uint8, _kept_numel(q.n * q.h * q.w, c), dev, "ckpt"), _ptr(gamma, f, c, dev, "gamma"),
+          _ptr(beta, f, c, dev, "beta"), _ptr(stats, f, s, dev, "stats"), _ptr(dx, t, e, dev, "dx"),
+          _ptr(dgamma, f, c, dev, "dgamma"), _ptr(dbeta, f, c, dev, "dbeta"), _raw_stream(dev))
 
 
 def dk_linear_bwd_wgrad_ckpt8(ctx: Context, q: dk_wgrad8, dy, ckpt, scale: float, keep: float, dW,
                               db: Optional[torch.Tensor]):
-    _check(lib().dk_linear_bwd_wgrad_ckpt8(ctx.handle, ctypes.byref(q), _typed(ctx, dy, q.dtype, q.rows * q.out, "dy"),
-                                           _kept(ctx, ckpt, q.rows, q.d, "ckpt"), scale, keep,
-                                           _f32(ctx, dW, q.out * q.d, "dW"),
-                                           None if db is None else _f32(ctx, db, q.out, "db"), _raw_stream(ctx.device)),
-           "dk_linear_bwd_wgrad_ckpt8")
+    dev, f, rows, d, out = ctx.device, torch.float32, q.rows, q.d, q.out
+    _call("dk_linear_bwd_wgrad_ckpt8", ctx.handle, q, _ptr(dy, _STEP_TYPES.get(q.dtype), rows * out, dev, "dy"),
+          _ptr(ckpt, torch.uint8, _kept_numel(rows, d), dev, "ckpt"), scale, keep, _ptr(dW, f, out * d, dev, "dW"),
+          None if db is None else _ptr(db, f, out, dev, "db"), _raw_stream(dev))
 
 
-def _or_null(f, ctx, t: Optional[torch.Tensor], *rest):
-    return None if t is None else f(ctx, t, *rest)
-
-
-def _gate(ctx, q: dk_block, t: Optional[torch.Tensor], what: str):
-    return _or_null(_f32, ctx, t, -(-q.rows // q.rows_per_gate) * q.d if q.rows_per_gate > 0 else -1, what)
+def _gates(q: dk_block) -> int:
+    return -(-q.rows // q.rows_per_gate) * q.d if q.rows_per_gate > 0 else -1
 
 
 def dk_block_norm_fwd(ctx: Context, q: dk_block, h, u, gate, post, pre, shift, h_out, n, stats, ckpt_h=None, ckpt_u=None):
     """Every tensor but h may be None where the C call takes NULL."""
-    e, d = q.rows * q.d, q.d
-    _check(lib().dk_block_norm_fwd(
-        ctx.handle, ctypes.byref(q), _typed(ctx, h, q.dtype, e, "h"), _or_null(_typed, ctx, u, q.dtype, e, "u"),
-        _gate(ctx, q, gate, "gate"), _or_null(_f32, ctx, post, d, "post"), _or_null(_f32, ctx, pre, d, "pre"),
-        _or_null(_f32, ctx, shift, d, "shift"), _or_null(_typed, ctx, h_out, q.dtype, e, "h_out"),
-        _or_null(_typed, ctx, n, q.dtype, e, "n"), _or_null(_f32, ctx, stats, 4 * q.rows, "stats"),
-        _or_null(_kept, ctx, ckpt_h, q.rows, d, "ckpt_h"), _or_null(_kept, ctx, ckpt_u, q.rows, d, "ckpt_u"),
-        _raw_stream(ctx.device)), "dk_block_norm_fwd")
+    dev, rows, d, t, f = ctx.device, q.rows, q.d, _STEP_TYPES.get(q.dtype), torch.float32
+    e = rows * d
+    _call("dk_block_norm_fwd", ctx.handle, q, _ptr(h, t, e, dev, "h"), None if u is None else _ptr(u, t, e, dev, "u"),
+          None if gate is None else _ptr(gate, f, _gates(q), dev, "gate"),
+          None if post is None else _ptr(post, f, d, dev, "post"), None if pre is None else _ptr(pre, f, d, dev, "pre"),
+          None if shift is None else _ptr(shift, f, d, dev, "shift"),
+          None if h_out is None else _ptr(h_out, t, e, dev, "h_out"), None if n is None else _ptr(n, t, e, dev, "n"),
+          None if stats is None else _ptr(stats, f, 4 * rows, dev, "stats"),
+          None if ckpt_h is None else _ptr(ckpt_h, torch.uint8, _kept_numel(rows, d), dev, "ckpt_h"),
+          None if ckpt_u is None else _ptr(ckpt_u, torch.uint8, _kept_numel(rows, d), dev, "ckpt_u"), _raw_stream(dev))
 
 
-def _block_bwd(name, held, ctx, q, dh_out, dn, h, u, gate, post, pre, stats, dh, du, dgate, dpost, dpre, dshift):
-    e, d = q.rows * q.d, q.d
-    _check(getattr(lib(), name)(
-        ctx.handle, ctypes.byref(q), _or_null(_typed, ctx, dh_out, q.dtype, e, "dh_out"),
-        _or_null(_typed, ctx, dn, q.dtype, e, "dn"), held(h, "h"), None if u is None else held(u, "u"),
-        _gate(ctx, q, gate, "gate"), _or_null(_f32, ctx, post, d, "post"), _or_null(_f32, ctx, pre, d, "pre"),
-        _f32(ctx, stats, 4 * q.rows, "stats"), _typed(ctx, dh, q.dtype, e, "dh"),
-        _or_null(_typed, ctx, du, q.dtype, e, "du"), _gate(ctx, q, dgate, "dgate"), _or_null(_f32, ctx, dpost, d, "dpost"),
-        _or_null(_f32, ctx, dpre, d, "dpre"), _or_null(_f32, ctx, dshift, d, "dshift"), _raw_stream(ctx.device)), name)
+def _block_bwd(name, held, held_numel, ctx, q, dh_out, dn, h, u, gate, post, pre, stats, dh, du, dgate, dpost, dpre, dshift):
+    dev, rows, d, t, f = ctx.device, q.rows, q.d, _STEP_TYPES.get(q.dtype), torch.float32
+    e = rows * d
+    _call(name, ctx.handle, q, None if dh_out is None else _ptr(dh_out, t, e, dev, "dh_out"),
+          None if dn is None else _ptr(dn, t, e, dev, "dn"), _ptr(h, held, held_numel, dev, "h"),
+          None if u is None else _ptr(u, held, held_numel, dev, "u"),
+          None if gate is None else _ptr(gate, f, _gates(q), dev, "gate"),
+          None if post is None else _ptr(post, f, d, dev, "post"), None if pre is None else _ptr(pre, f, d, dev, "pre"),
+          _ptr(stats, f, 4 * rows, dev, "stats"), _ptr(dh, t, e, dev, "dh"),
+          None if du is None else _ptr(du, t, e, dev, "du"), None if dgate is None else _ptr(dgate, f, _gates(q), dev, "dgate"),
+          None if dpost is None else _ptr(dpost, f, d, dev, "dpost"), None if dpre is None else _ptr(dpre, f, d, dev, "dpre"),
+          None if dshift is None else _ptr(dshift, f, d, dev, "dshift"), _raw_stream(dev))
 
 
 def dk_block_norm_bwd(ctx: Context, q: dk_block, dh_out, dn, h, u, gate, post, pre, stats, dh, du, dgate, dpost, dpre,
                       dshift):
-    _block_bwd("dk_block_norm_bwd", lambda t, what: _typed(ctx, t, q.dtype, q.rows * q.d, what), ctx, q, dh_out, dn, h, u,
-               gate, post, pre, stats, dh, du, dgate, dpost, dpre, dshift)
+    _block_bwd("dk_block_norm_bwd", _STEP_TYPES.get(q.dtype), q.rows * q.d, ctx, q, dh_out, dn, h, u, gate, post, pre, stats,
+               dh, du, dgate, dpost, dpre, dshift)
 
 
 def dk_block_norm_bwd_ckpt8(ctx: Context, q: dk_block, dh_out, dn, ckpt_h, ckpt_u, gate, post, pre, stats, dh, du, dgate,
                             dpost, dpre, dshift):
-    _block_bwd("dk_block_norm_bwd_ckpt8", lambda t, what: _kept(ctx, t, q.rows, q.d, "ckpt_" + what), ctx, q, dh_out, dn,
-               ckpt_h, ckpt_u, gate, post, pre, stats, dh, du, dgate, dpost, dpre, dshift)
+    _block_bwd("dk_block_norm_bwd_ckpt8", torch.uint8, _kept_numel(q.rows, q.d), ctx, q, dh_out, dn, ckpt_h, ckpt_u, gate,
+               post, pre, stats, dh, du, dgate, dpost, dpre, dshift)
