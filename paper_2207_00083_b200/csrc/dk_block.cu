@@ -49,6 +49,9 @@ struct BlockArgs {
   int join_e;              // E is joined over a CTA's teams
   int d, dp, tl, teams;    // tl: threads of a team; teams: of a CTA
   int stages, team_smem;   // rows of a team's ring, bytes of its shared memory
+  unsigned spin_cap;       // polls of a wait
+  int withhold;            // test hook: the first team arms its n-th row but copies nothing from there on (-1 = off)
+  int* status;
   int shifted;             // dshift is asked for
   int layer;
   float eps, keep, scale, inv_d;
@@ -397,12 +400,12 @@ __global__ void __launch_bounds__(1024) block_bwd_wide_kernel(const BlockArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// The same with rows on their way into shared memory while others are worked on: a team has a ring of kStages rows of each
-// tensor, filled by asynchronous copies two rows ahead.  Rows of whole 16-byte vectors: a thread copies the vectors that it
-// reads itself.  Others: copied in 16-byte pieces from the boundary before them on (the last piece no further than the
-// tensor's end), and read by single values, so that every length streams alike.  The copies of the next row are waited for
-// before a barrier of this row's sums, which hands them to the whole team; the copies issued at a row's start go where the
-// row before lay, whose last reading is before that row's last barrier.
+// The same with rows on their way into shared memory while others are worked on: a team has a ring of two or three rows of
+// each tensor, filled by asynchronous copies.  A team of whole warps has one lane issue bulk copies of whole rows, from the
+// 16-byte boundary before a row to the one behind it (no further than the tensor's end: the last row's odd bytes are copied
+// by hand), so every length streams alike and the other threads spend nothing on it; they wait on the stage's barrier.
+// Teams of fewer lanes copy with cp.async, the vectors that they read themselves or 16-byte pieces.  The copies issued at a
+// row's start go where the row before lay, whose last reading is before that row's last barrier.
 //
 // What bounds it besides HBM is instructions: bf16 rows from checkpoints leave some 55 per value at the rate of HBM.  So a
 // thread has sixteen values, over which a row's sums, its copies and its scalars are shared out (eight: 86 and 91 per
@@ -410,6 +413,22 @@ __global__ void __launch_bounds__(1024) block_bwd_wide_kernel(const BlockArgs a)
 // instruction.
 // ---------------------------------------------------------------------------
 constexpr int kMostWarps = 24;               // of a team
+constexpr int kMostStages = 3, kBulkTeams = kSmallTeams / 32, kMostSources = 6;
+
+// What a stage is made of: tensors (rows of `bytes` bytes) and where their rows go.  In shared memory: a lane each.
+struct Source {
+  const void* base;
+  int bytes, at;
+};
+struct Sources {
+  Source of[kMostSources];
+  int n;
+  __device__ __forceinline__ void add(const void* base, int bytes, int at) {
+    if (base != nullptr) of[n++] = Source{base, bytes, at};
+  }
+};
+
+__device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
@@ -442,8 +461,12 @@ struct Team {
   bool ragged;                 // not all of them
   float* sm;                   // [2][2*kMostWarps], zero behind the team's warps
   int turn;
+  // bulk copies (whole warps)
+  bool bulk;
+  uint64_t* full;              // barriers of the ring's stages
+  volatile int* abort_flag;
 
-  __device__ __forceinline__ Team(const BlockArgs& a, float* shared) {
+  __device__ __forceinline__ Team(const BlockArgs& a, float* shared, uint64_t* bars, volatile int* flag, int sources) {
     lane = threadIdx.x % a.tl; tl = a.tl;
     warps = a.tl > 32 ? a.tl >> 5 : 0;
     c0 = lane * VEC; cs = tl * VEC;
@@ -453,6 +476,68 @@ struct Team {
     sm = shared;
     turn = 0;
     for (int i = threadIdx.x; i < 4 * kMostWarps; i += blockDim.x) sm[i] = 0.f;
+    bulk = FULL || tl >= 32;
+    full = bars + (bulk ? threadIdx.x / tl * kMostStages : 0);
+    abort_flag = flag;
+    if (threadIdx.x == 0) *flag = 0;
+    if (bulk && lane == 0) {
+      for (int i = 0; i < kMostStages; ++i)
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_at(full + i)), "r"(sources) : "memory");
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+  }
+  // Waits for a stage's copies.  A wait that runs out raises the CTA's flag, after which none waits; what is then computed is
+  // not the result, and the status says so.
+  __device__ __forceinline__ void wait_row(int slot, uint32_t phase, const BlockArgs& a) const {
+    if (!bulk) return;
+    const uint32_t bar = shared_at(full + slot);
+    for (unsigned i = 0; i < a.spin_cap; ++i) {
+      uint32_t ok;
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(ok)
+          : "r"(bar), "r"(phase)
+          : "memory");
+      if (ok || *abort_flag) return;
+    }
+    *abort_flag = 1;
+  }
+  // One lane: its tensor's row into a stage at `to`.
+  __device__ __forceinline__ void bulk_row(uint32_t to, const Source& src, int row, int rows, int slot) const {
+    const long long at = (long long)row * src.bytes, from = at & ~15LL, left = (long long)rows * src.bytes - from;
+    const int end = (int)(at & 15) + src.bytes, size = (int)min((long long)(end + 15 & ~15), left & ~15LL);
+    const uint32_t dst = to + src.at, bar = shared_at(full + slot);
+    const char* p = static_cast<const char*>(src.base) + from;
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(size) : "memory");
+    if (size > 0)
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(p),
+                   "r"(size), "r"(bar)
+                   : "memory");
+    for (int i = size; i < end; ++i)      // (handed to the team by a barrier before the row is read)
+      asm volatile("st.shared.u8 [%0], %1;" ::"r"(dst + i), "r"((uint32_t) * reinterpret_cast<const uint8_t*>(p + i)) : "memory");
+  }
+  // The team's first lanes, one for each tensor.
+  __device__ __forceinline__ void issue_bulk(uint32_t to, const Sources& from, int row, int r0, int r1, int slot,
+                                             const BlockArgs& a) const {
+    if (lane < from.n && row < r1 && issues(row - r0, slot, a)) bulk_row(to, from.of[lane], row, a.rows, slot);
+  }
+  // Whether a team's i-th row is copied: not once a wait has run out; nor, under the test hook, from the n-th on, which is
+  // armed for bytes that nothing brings.
+  __device__ __forceinline__ bool issues(int i, int slot, const BlockArgs& a) const {
+    if (*abort_flag) return false;
+    if (a.withhold < 0 || blockIdx.x > 0 || i < a.withhold) return true;
+    if (i == a.withhold)
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], 16;" ::"r"(shared_at(full + slot)) : "memory");
+    return false;
+  }
+  // at the kernel's end: after a wait that ran out, time for copies in flight to land
+  __device__ __forceinline__ void leave(const BlockArgs& a) const {
+    if (!bulk || !*abort_flag) return;
+    if (lane == 0 && a.status != nullptr) atomicExch(a.status, (int)DK_ERR_TIMEOUT);
+    for (int i = 0; i < 64; ++i) __nanosleep(16384);
   }
   __device__ __forceinline__ int column(int j) const { return c0 + j * cs; }
   __device__ __forceinline__ bool live(int j) const { return FULL || lives[j]; }
@@ -719,20 +804,33 @@ struct Team {
 
 template <int DT, int VEC, bool FULL>
 __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const BlockArgs a) {
-  constexpr int kStages = 3;
+  constexpr int kStages = kMostStages;
   using T = Team<DT, VEC, FULL>;
   constexpr int P = T::P;
   extern __shared__ __align__(16) char ring[];
   __shared__ __align__(16) float sm[4 * kMostWarps];
-  T t(a, sm);
+  __shared__ __align__(8) uint64_t bars[kMostStages * kBulkTeams];
+  __shared__ int flag;
+  __shared__ Sources sources;
+  const bool branch = a.u != nullptr;
+  T t(a, sm, bars, &flag, branch ? 2 : 1);
   const int team_in = threadIdx.x / a.tl;
   const int r0 = (int)min((long long)a.rows, ((long long)blockIdx.x * a.teams + team_in) * a.chunk), r1 = r0 + min(a.rows - r0, a.chunk);
   const int bytes = a.d * T::ES, room = row_room(bytes), stage = 2 * room;
   char* const mine = ring + (size_t)team_in * a.team_smem;
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
-  const bool branch = a.u != nullptr;
+  if (threadIdx.x == 0) {
+    sources.n = 0;
+    sources.add(a.h, bytes, 0);
+    sources.add(a.u, bytes, room);
+  }
+  __syncthreads();
   chained_launch();
   auto issue = [&](int row, int slot) {
+    if (t.bulk) {
+      t.issue_bulk(mine_at + slot * stage, sources, row, r0, r1, slot, a);
+      return;
+    }
     if (row < r1) {
       t.copy_tensor(mine_at + slot * stage, a.h, row, a);
       if (branch) t.copy_tensor(mine_at + slot * stage + room, a.u, row, a);
@@ -746,9 +844,10 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
   long long seg_end = (long long)(seg + 1) * a.per;
   if (branch) t.take_factors(a, seg, gps);
   if (a.n != nullptr) t.take_f32(a.pre, pre);
-  wait_copies<kStages - 2>();
+  if (!t.bulk) wait_copies<kStages - 2>();
   t.sync();
   int slot = 0;
+  uint32_t phase = 0;
   for (int i = 0; i < a.chunk; ++i) {
     const int row = r0 + i;
     const bool valid = FULL || row < r1;
@@ -756,11 +855,12 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
     const char* at = mine + slot * stage;
     const int off = T::WHOLE ? 0 : (int)(((long long)row * bytes) & 15);
     issue(row + kStages - 1, slot == 0 ? kStages - 1 : slot - 1);
+    t.wait_row(slot, phase, a);
     F2 h[P];
     t.take(at + off, valid, h);
     if (a.kh != nullptr) t.keep_row(a.kh, a.keh, row, a, valid, h);
     float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (a.n == nullptr) wait_copies<kStages - 2>();
+    if (!t.bulk && a.n == nullptr) wait_copies<kStages - 2>();
     if (branch) {
       F2 u[P];
       t.take(at + room + off, valid, u);
@@ -777,7 +877,7 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
       if (valid) t.give(a.h_out, row, a.d, h);
     }
     if (a.n != nullptr) {
-      wait_copies<kStages - 2>();
+      if (!t.bulk) wait_copies<kStages - 2>();
       const float2 m = t.normalise(h, a);
       st.z = m.x; st.w = m.y;
 #pragma unroll
@@ -792,9 +892,10 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
     }
     if (a.stats != nullptr && t.lane == 0 && valid) a.stats[row] = st;
     if (t.warps == 0) __syncwarp();
-    slot = slot + 1 == kStages ? 0 : slot + 1;
+    if (++slot == kStages) { slot = 0; phase ^= 1u; }
   }
   wait_copies<0>();
+  t.leave(a);
 }
 
 // Beside the ring a team has [d] fp32 of gate*post*scale, of pre (from L1, which the copies pass through, each reading of it
@@ -806,7 +907,11 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   constexpr int P = T::P;
   extern __shared__ __align__(16) char ring[];
   __shared__ __align__(16) float sm[4 * kMostWarps];
-  T t(a, sm);
+  __shared__ __align__(8) uint64_t bars[kMostStages * kBulkTeams];
+  __shared__ int flag;
+  __shared__ Sources sources;
+  const bool branch = a.post != nullptr, norm = a.dn != nullptr;
+  T t(a, sm, bars, &flag, (a.dh_out != nullptr) + norm + (KEPT && !T::WHOLE ? 2 : 1) * (1 + branch));
   const int team_in = threadIdx.x / a.tl;
   const long long team = (long long)blockIdx.x * a.teams + team_in;
   const int bytes = a.d * T::ES, eb = a.dp / ckpt8::kBlock;
@@ -820,7 +925,18 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   float* const posts = pres + own / 4;
   float* const shifts = a.split == 0 ? posts + own / 4 : posts;
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
-  const bool branch = a.post != nullptr, norm = a.dn != nullptr;
+  if (threadIdx.x == 0) {
+    sources.n = 0;
+    sources.add(a.dh_out, bytes, 0);
+    sources.add(a.dn, bytes, room);
+    sources.add(KEPT ? (const void*)a.ch : a.h, KEPT ? a.dp : bytes, at_h);
+    sources.add(KEPT ? (const void*)a.cu : a.u, KEPT ? a.dp : bytes, at_u);
+    if (KEPT && !T::WHOLE) {
+      sources.add(a.eh, eb, at_eh);
+      sources.add(branch ? a.eu : nullptr, eb, at_eu);
+    }
+  }
+  __syncthreads();
   int r0, r1, seg;
   {
     long long f, e;
@@ -839,8 +955,12 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   long long seg_end = (long long)(seg + 1) * a.per;
   chained_launch();
   auto issue = [&](int row, int slot) {
+    const uint32_t to = mine_at + slot * stage;
+    if (t.bulk) {
+      t.issue_bulk(to, sources, row, r0, r1, slot, a);
+      return;
+    }
     if (row < r1) {
-      const uint32_t to = mine_at + slot * stage;
       if (a.dh_out != nullptr) t.copy_tensor(to, a.dh_out, row, a);
       if (norm) t.copy_tensor(to + room, a.dn, row, a);
       if constexpr (KEPT) {
@@ -885,9 +1005,12 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     }
   };
   fetch(r0);
-  if (stages == 3) wait_copies<1>(); else wait_copies<0>();
+  if (!t.bulk) {
+    if (stages == 3) wait_copies<1>(); else wait_copies<0>();
+  }
   t.sync();
   int slot = 0;
+  uint32_t phase = 0;
   for (int i = 0; i < a.chunk; ++i) {
     const int row = r0 + i;
     const bool valid = FULL || row < r1;
@@ -895,6 +1018,7 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     const char* at = mine + slot * stage;
     const int off = T::WHOLE ? 0 : (int)(((long long)row * bytes) & 15), off_e = T::WHOLE ? 0 : (int)(((long long)row * eb) & 15);
     issue(row + stages - 1, slot == 0 ? stages - 1 : slot - 1);
+    t.wait_row(slot, phase, a);
     const float4 st = next;
     if (branch && valid) {
       if (row == seg_end) {
@@ -982,7 +1106,9 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     } else if (valid) {
       t.give(a.dh, row, a.d, hh);
     }
-    if (stages == 3) wait_copies<1>(); else wait_copies<0>();
+    if (!t.bulk) {
+      if (stages == 3) wait_copies<1>(); else wait_copies<0>();
+    }
     t.sum2(t0, t1);
     if (branch) {
       t0 = a.layer ? t0 * a.inv_d : 0.f;
@@ -1012,9 +1138,10 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       }
     }
     if (t.warps == 0) __syncwarp();
-    slot = slot + 1 == stages ? 0 : slot + 1;
+    if (++slot == stages) { slot = 0; phase ^= 1u; }
   }
   wait_copies<0>();
+  t.leave(a);
 
   // what the team has summed up over its rows
   F2 v[P];
@@ -1241,6 +1368,17 @@ dk_status launch_bwd(const BlockArgs& a, const BlockPlan& p, bool kept, int devi
   return kept ? launch_bwd<DT, VEC, true>(a, p, device, st) : launch_bwd<DT, VEC, false>(a, p, device, st);
 }
 
+// how long the kernels of bulk copies wait
+void take_waits(dk_ctx* ctx, const BlockPlan& p, BlockArgs& a) {
+  a.spin_cap = (unsigned)ctx->opt.v[DK_OPT_SPIN_LIMIT];
+  a.status = device_status_word(ctx);
+  a.withhold = -1;
+  if (!p.wide && p.tl >= 32) {
+    a.withhold = ctx->opt.v[DK_OPT_TEST_WITHHOLD];
+    ctx->opt.v[DK_OPT_TEST_WITHHOLD] = -1;
+  }
+}
+
 dk_status backward(dk_ctx* ctx, const dk_block* q, bool kept, const void* dh_out, const void* dn, const void* h,
                    const void* u, const float* gate, const float* post, const float* pre, const float* stats, void* dh,
                    void* du, float* dgate, float* dpost, float* dpre, float* dshift, void* stream) {
@@ -1289,6 +1427,7 @@ dk_status backward(dk_ctx* ctx, const dk_block* q, bool kept, const void* dh_out
   a.split = p.split ? (int)((a.per + p.chunk - 1) / p.chunk) : 0;
   a.join_e = p.join_e && gate != nullptr;
   a.shifted = dshift != nullptr;
+  take_waits(ctx, p, a);
   a.d = q->d; a.dp = ckpt8::padded(q->d); a.tl = p.tl; a.teams = p.teams; a.stages = p.stages; a.team_smem = p.smem;
   a.layer = q->kind == DK_BLOCK_LAYER;
   a.eps = q->eps; a.keep = q->keep; a.scale = q->scale; a.inv_d = 1.f / (float)q->d;
@@ -1364,6 +1503,7 @@ dk_status dk_block_norm_fwd(dk_ctx* ctx, const dk_block* q, const void* h, const
   OnDevice dev(ctx->device);
   if (!dev.ok) return DK_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  take_waits(ctx, p, a);
   ProfScope ps(ctx, DK_KERNEL_OTHER, 1, st);
   if (q->dtype == DK_F32)
     return p.whole           ? launch_fwd<DK_F32, 4>(a, p, ctx->device, st)

@@ -253,6 +253,30 @@ def test_rows_of_one_value_and_infinities(ctx, kind):
     assert bool(torch.isfinite(got["dh"][ok]).all()) and bool(torch.isfinite(got["du"][ok]).all())
 
 
+@pytest.mark.parametrize("d,dtype", [(4096, "bf16"), (1001, "f32"), (512, "bf16"), (300, "f32")])
+@pytest.mark.parametrize("row", [0, 1, 2])
+def test_copies_that_do_not_come(ctx, d, dtype, row):
+    """A host-set option makes the first team arm a row without copying it (a team of 512 values has five of these rows, the
+    others more): every wait ends within a short poll limit, the
+    status says so, and the next call is as it should be."""
+    c = Case(12000, d, "rms", "channel", 1, dtype)
+    ctx.ensure_workspace(c.q)
+    c.forward(ctx)
+    for held in (None, False, True):
+        dk.dk_set_option(ctx, dk.DK_OPT_SPIN_LIMIT, 1 << 12)
+        dk.dk_set_option(ctx, dk.DK_OPT_TEST_WITHHOLD, row)
+        if held is None:
+            c.forward(ctx, checkpoints=False, stats=False)
+        else:
+            c.backward(ctx, held)
+        assert dk.dk_get_option(ctx, dk.DK_OPT_TEST_WITHHOLD) == -1
+        assert dk.dk_device_status(ctx) == dk.DK_ERR_TIMEOUT
+        assert dk.dk_device_status(ctx) == 0
+        dk.dk_set_option(ctx, dk.DK_OPT_SPIN_LIMIT, 1 << 22)
+        c.check_forward(ctx)
+        c.check_backward(ctx, bool(held))
+
+
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 def test_against_differences(ctx, kind):
     """Slopes of <h_out, a> + <n, b> along a random direction of every input, from the forward call itself: its rounding
