@@ -1,12 +1,13 @@
 """A small network trained with masked convolutions, every step of it through the library.
 
-    python examples/masked_training.py [--steps N]
+    python examples/masked_training.py [--steps N] [--keep8]
 
 Per step: conv1 (masked) -> group norm + SiLU -> conv2 (masked) -> group norm + SiLU -> a linear layer over many
 classes with softmax cross entropy; backwards through the same layers with the masked weight gradient on the stored
 encodings and dgrad; the convolutions' weights move along the orthogonalised gradient, everything else along the
 gradient.  The images are synthetic: one random prototype per class under noise of twice its size, so that the loss falls
-over the whole run (6.5 to 0.24 in 30 steps).
+over the whole run (6.5 to 0.24 in 30 steps).  With --keep8 the norms' inputs are kept from the forward to the backward pass
+in 8 bits instead of 32.
 """
 from __future__ import annotations
 
@@ -30,13 +31,13 @@ EPS, QUINTIC = 1e-5, (3.4445, -4.7750, 2.0315)
 
 
 class Network:
-    def __init__(self, seed: int = 0):
+    def __init__(self, seed: int = 0, keep8: bool = False):
         g = torch.Generator(device="cuda").manual_seed(seed)
 
         def normal(*shape):
             return torch.randn(shape, generator=g, device="cuda")
 
-        self.ctx, self.n = dk.Context(0), K * G
+        self.ctx, self.n, self.keep8 = dk.Context(0), K * G, keep8
         self.rng, self.gen = np.random.default_rng(seed), g
         self.convs = [dk.dk_problem(dk.DK_CONV2D, dk.DK_NHWC, CHANNELS[i], CHANNELS[i + 1], SIZE, SIZE, 3, 3, 1, 1, K, G,
                                     dk.DK_PREC_DEFAULT, 1e-4) for i in range(2)]
@@ -63,7 +64,13 @@ class Network:
             v = dk.new_verdict()
             dk.dk_masked_linear(ctx, p, W, a, r, C, None, z, encoded, v)
             y, stats = empty(p.cout), torch.empty((self.n, GROUPS, 2), device="cuda")
-            dk.dk_group_norm_fwd(ctx, q, z, gamma, beta, y, stats)
+            if self.keep8:
+                k8 = dk.dk_ckpt8(self.n * SIZE * SIZE, p.cout, dk.DK_F32)
+                held = torch.empty(dk.dk_ckpt8_bytes(k8), dtype=torch.uint8, device="cuda")
+                dk.dk_group_norm_fwd_ckpt8(ctx, q, z, gamma, beta, y, stats, held)
+                z = held
+            else:
+                dk.dk_group_norm_fwd(ctx, q, z, gamma, beta, y, stats)
             kept.append((C, encoded, z, stats))
             verdicts.append(v)
             a = y
@@ -74,10 +81,10 @@ class Network:
         grads = {"V": dV}
         for i in (1, 0):
             C, encoded, z, stats = kept[i]
-            p, dz = self.convs[i], torch.empty_like(z)
+            p, dz = self.convs[i], empty(self.convs[i].cout)
             grads[f"gamma{i}"], grads[f"beta{i}"] = torch.empty_like(self.gamma[i]), torch.empty_like(self.beta[i])
-            dk.dk_group_norm_bwd(ctx, self.norms[i], dh, z, self.gamma[i], self.beta[i], stats, dz, grads[f"gamma{i}"],
-                                 grads[f"beta{i}"])
+            back = dk.dk_group_norm_bwd_ckpt8 if self.keep8 else dk.dk_group_norm_bwd
+            back(ctx, self.norms[i], dh, z, self.gamma[i], self.beta[i], stats, dz, grads[f"gamma{i}"], grads[f"beta{i}"])
             grads[f"W{i}"] = torch.empty_like(self.W[i])
             dk.dk_linear_bwd_wgrad(ctx, p, dz, encoded, K + 2, C, synth.draw_gamma(self.rng, K, G), 1.0, grads[f"W{i}"])
             if i:
@@ -106,8 +113,8 @@ def images(n: int, seed: int = 1):
         yield prototypes[target] + 2.0 * torch.randn((n, SIZE, SIZE, CHANNELS[0]), generator=g, device="cuda"), target
 
 
-def main(steps: int = 30):
-    net = Network()
+def main(steps: int = 30, keep8: bool = False):
+    net = Network(keep8=keep8)
     losses = []
     for i, (x, target) in zip(range(steps), images(net.n)):
         losses.append(net.step(x, target))
@@ -120,4 +127,6 @@ def main(steps: int = 30):
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=30)
-    main(ap.parse_args().steps)
+    ap.add_argument("--keep8", action="store_true")
+    args = ap.parse_args()
+    main(args.steps, args.keep8)
