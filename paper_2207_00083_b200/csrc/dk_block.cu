@@ -21,9 +21,8 @@ namespace {
 constexpr int kMaxD = 16384;
 constexpr int kHeld = 8192;            // longest rows that are held in registers
 // Values of a thread, and threads of a CTA at most (they share out the registers).
-// (bf16 rows of whole vectors 16: see below; of single values 8, sixteen of which spill)
-template <int DT, bool WHOLE>
-constexpr int kValues = DT == DK_BF16 && WHOLE ? 16 : 8;
+template <int DT>
+constexpr int kValues = DT == DK_BF16 ? 16 : 8;
 template <int DT>
 constexpr int kFwdThreads = DT == DK_F32 ? 768 : 512;
 template <int DT>
@@ -439,7 +438,10 @@ __device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_gr
 template <int LEFT>
 __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-__host__ __device__ inline int row_room(int bytes) { return (bytes + 15 + 15) / 16 * 16; }
+__host__ __device__ inline int row_room(int bytes) { return (bytes + 15) / 16 * 16; }
+// A row of a tensor in a stage; RAGGED: its vectors are read as two of a row that starts anywhere, and rows on their way out
+// have 16 bytes before them.
+__host__ __device__ inline int stage_room(int bytes, bool ragged) { return row_room(bytes) + (ragged ? 48 : 0); }
 
 // 1/sqrt(x): the instruction's 22 bits and one step of Newton's method
 __device__ __forceinline__ float inverse_root(float x) {
@@ -448,16 +450,24 @@ __device__ __forceinline__ float inverse_root(float x) {
 }
 
 // A team and a thread's place in it.  Its N values: NV vectors of VEC, tl*VEC apart; as P pairs in that order.
-// FULL: every thread of every team has all of its values (whole warps; rows are multiples of 32*N values).
-template <int DT, int VEC, bool FULL>
+// How rows lie.  FULL: rows of multiples of 32*N values; every thread of every team has all of its values, and teams are
+// whole warps.  WHOLE: rows of whole 16-byte vectors.  Others start anywhere (`off` bytes behind a 16-byte boundary, the same
+// for the whole row).  RAGGED, bf16: a vector is read as two of the stage's and shifted, and written to shared memory first,
+// from where the team stores the row in whole aligned vectors (and its two ends by single values).  PAIRS and SINGLES, fp32:
+// two values to an access where rows have an even number, else one.  Both sides: 16384 x 1001 bf16 takes 66 us forward and
+// 113 backward as RAGGED, 130 and 143 as SINGLES; 4095 x 2050 fp32 62 and 82, but 47 and 61 as PAIRS (a shift serves four
+// values there, not eight).
+enum { FULL = 0, WHOLE = 1, RAGGED = 2, PAIRS = 3, SINGLES = 4 };
+template <int DT, int WAY>
 struct Team {
-  static constexpr int ES = DT == DK_F32 ? 4 : 2;
-  static constexpr bool WHOLE = VEC * ES == 16;      // rows of whole 16-byte vectors
-  static constexpr int N = kValues<DT, WHOLE>, NV = N / VEC, P = N / 2;
+  static constexpr int ES = DT == DK_F32 ? 4 : 2, VEC = WAY == PAIRS ? 2 : WAY == SINGLES ? 1 : 16 / ES;
+  static constexpr int N = kValues<DT>, NV = N / VEC, P = N / 2;
+  static constexpr bool NARROW = WAY >= PAIRS;
   using Pairs = F2[P];
   int lane, tl, warps;         // warps: of a team that is the CTA, else 0
   int c0, cs;                  // first column, and from one vector to the next
-  bool lives[NV];              // vectors that exist
+  int d;
+  bool lives[NV];              // vectors of which a value exists
   bool ragged;                 // not all of them
   float* sm;                   // [2][2*kMostWarps], zero behind the team's warps
   int turn;
@@ -469,14 +479,14 @@ struct Team {
   __device__ __forceinline__ Team(const BlockArgs& a, float* shared, uint64_t* bars, volatile int* flag, int sources) {
     lane = threadIdx.x % a.tl; tl = a.tl;
     warps = a.tl > 32 ? a.tl >> 5 : 0;
-    c0 = lane * VEC; cs = tl * VEC;
+    c0 = lane * VEC; cs = tl * VEC; d = a.d;
 #pragma unroll
     for (int j = 0; j < NV; ++j) lives[j] = column(j) < a.d;
-    ragged = !live(NV - 1);
+    ragged = WAY == RAGGED ? column(NV - 1) + VEC > a.d : !live(NV - 1);
     sm = shared;
     turn = 0;
     for (int i = threadIdx.x; i < 4 * kMostWarps; i += blockDim.x) sm[i] = 0.f;
-    bulk = FULL || tl >= 32;
+    bulk = WAY == FULL || tl >= 32;
     full = bars + (bulk ? threadIdx.x / tl * kMostStages : 0);
     abort_flag = flag;
     if (threadIdx.x == 0) *flag = 0;
@@ -540,13 +550,18 @@ struct Team {
     for (int i = 0; i < 64; ++i) __nanosleep(16384);
   }
   __device__ __forceinline__ int column(int j) const { return c0 + j * cs; }
-  __device__ __forceinline__ bool live(int j) const { return FULL || lives[j]; }
+  __device__ __forceinline__ bool live(int j) const { return WAY == FULL || lives[j]; }
+  __device__ __forceinline__ bool live(int j, int k) const { return WAY == RAGGED ? column(j) + k < d : live(j); }
   __device__ __forceinline__ void sync() const {
     if (warps) __syncthreads(); else __syncwarp();
   }
+  // (behind a sum, which is a barrier only for teams of several warps)
+  __device__ __forceinline__ void after_sum() const {
+    if (!warps) __syncwarp();
+  }
 
   __device__ __forceinline__ float sum1(float x) {
-    if (!FULL && tl < 32) {
+    if (WAY != FULL && tl < 32) {
       for (int o = tl >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
       return x;
     }
@@ -565,7 +580,7 @@ struct Team {
     return sum(y);
   }
   __device__ __forceinline__ void sum2(float& a, float& b) {
-    if (!FULL && tl < 32) {
+    if (WAY != FULL && tl < 32) {
       for (int o = tl >> 1; o > 0; o >>= 1) {
         a += __shfl_xor_sync(0xffffffffu, a, o);
         b += __shfl_xor_sync(0xffffffffu, b, o);
@@ -597,28 +612,81 @@ struct Team {
     b = r.y;
   }
 
-  // values of a row (in shared memory; zero where there are none)
-  __device__ __forceinline__ void take(const char* row, bool valid, Pairs& v) const {
+  // the low words of eight, shifted down by `off` bytes (even; fp32: a multiple of four)
+  static __device__ __forceinline__ uint4 shifted(const uint4& x, const uint4& y, int off) {
+    uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    if (off & 8) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (off & 4) {
+#pragma unroll
+      for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (DT == DK_BF16 && (off & 2)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  // values of a row in a stage, `off` bytes behind `row` (zero where there are none)
+  __device__ __forceinline__ void take(const char* row, int off, bool valid, Pairs& v) const {
     float x[N];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      typename Vec<DT, VEC>::Raw r = {};
+      if ((WAY == FULL || valid) && live(j)) {
+        if constexpr (WAY == RAGGED) {
+          const uint4* at = reinterpret_cast<const uint4*>(row + column(j) * ES);
+          r = shifted(at[0], at[1], off);
+        } else {
+          r = Vec<DT, VEC>::get(row + off, column(j));
+        }
+      }
       float y[VEC];
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) y[k] = 0.f;
-      if ((FULL || valid) && live(j)) Vec<DT, VEC>::load(row, column(j), y);
+      Vec<DT, VEC>::unpack(r, y);
 #pragma unroll
       for (int k = 0; k < VEC; ++k) x[j * VEC + k] = y[k];
+    }
+    if (WAY == RAGGED && ragged) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = live(i / VEC, i % VEC) ? x[i] : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) v[i] = f2(x[2 * i], x[2 * i + 1]);
   }
-  __device__ __forceinline__ void give(void* base, int row, int d, const Pairs& v) const {
-    char* const to = static_cast<char*>(base) + (long long)row * (d * ES);
+  // A result's row: RAGGED, to `out` first, from where the team stores it (`flush`, behind a barrier); else at once.
+  __device__ __forceinline__ void give(void* base, int row, const Pairs& v, char* out) const {
+    char* const to = WAY == RAGGED ? out : static_cast<char*>(base) + (long long)row * (d * ES);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float y[VEC];
       vector(v, j, y);
       if (live(j)) Vec<DT, VEC>::store(to, column(j), y);
+    }
+  }
+  // (`out` has 16 bytes of room before the row)
+  __device__ __forceinline__ void flush(void* base, int row, const char* out) const {
+    if constexpr (WAY == RAGGED) {
+      const long long at = (long long)row * (d * ES);
+      const int off = (int)(at & 15), bytes = d * ES, n = (off + bytes + 15) >> 4;
+      char* const to = static_cast<char*>(base) + (at - off);
+      for (int q = lane; q < n; q += tl) {
+        const uint4* from = reinterpret_cast<const uint4*>(out) + q;
+        const uint4 w = off == 0 ? from[0] : shifted(from[-1], from[0], 16 - off);
+        const int lo = q == 0 ? off : 0, hi = min(16, off + bytes - q * 16);
+        if (lo == 0 && hi == 16) {
+          *reinterpret_cast<uint4*>(to + q * 16) = w;
+        } else {
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int i = 0; i < 16 / ES; ++i) {
+            if (i * ES < lo || i * ES >= hi) continue;
+            if constexpr (DT == DK_F32) *reinterpret_cast<uint32_t*>(to + q * 16 + i * 4) = u[i];
+            else *reinterpret_cast<uint16_t*>(to + q * 16 + i * 2) = (uint16_t)(i & 1 ? u[i / 2] >> 16 : u[i / 2]);
+          }
+        }
+      }
     }
   }
   static __device__ __forceinline__ void vector(const Pairs& v, int j, float (&y)[VEC]) {
@@ -628,27 +696,35 @@ struct Team {
       y[k] = (j * VEC + k) & 1 ? p.y : p.x;
     }
   }
-  // fp32 of this thread's columns, from global or shared memory (0 behind the row)
-  __device__ __forceinline__ void take_f32(const float* p, Pairs& v) const {
+  // fp32 of this thread's columns (0 behind the row): a parameter's, or what give_f32 has put there
+  __device__ __forceinline__ void take_f32(const float* p, Pairs& v) const { load_f32<WAY == RAGGED>(p, v); }
+  __device__ __forceinline__ void give_f32(float* p, const Pairs& v) const { store_f32<WAY == RAGGED>(p, v); }
+  // the same in the team's own shared memory, whole vectors
+  __device__ __forceinline__ void take_own(const float* p, Pairs& v) const { load_f32<false>(p, v); }
+  __device__ __forceinline__ void give_own(float* p, const Pairs& v) const { store_f32<false>(p, v); }
+  template <bool SINGLE>
+  __device__ __forceinline__ void load_f32(const float* p, Pairs& v) const {
     float x[N];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      const float* const at = p + column(j);
       float y[VEC];
 #pragma unroll
       for (int k = 0; k < VEC; ++k) y[k] = 0.f;
-      if (live(j)) {
-        const float* at = p + column(j);
-        if constexpr (VEC >= 4) {
+      if constexpr (SINGLE || VEC == 1) {
 #pragma unroll
-          for (int k = 0; k < VEC; k += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(at + k);
-            y[k] = f.x; y[k + 1] = f.y; y[k + 2] = f.z; y[k + 3] = f.w;
-          }
-        } else if constexpr (VEC == 2) {
-          const float2 f = *reinterpret_cast<const float2*>(at);
-          y[0] = f.x; y[1] = f.y;
-        } else {
-          y[0] = *at;
+        for (int k = 0; k < VEC; ++k)
+          if (live(j, k)) y[k] = at[k];
+      } else if constexpr (VEC == 2) {
+        float2 f = make_float2(0.f, 0.f);
+        if (live(j)) f = *reinterpret_cast<const float2*>(at);
+        y[0] = f.x; y[1] = f.y;
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; k += 4) {
+          float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (live(j)) f = *reinterpret_cast<const float4*>(at + k);
+          y[k] = f.x; y[k + 1] = f.y; y[k + 2] = f.z; y[k + 3] = f.w;
         }
       }
 #pragma unroll
@@ -657,20 +733,23 @@ struct Team {
 #pragma unroll
     for (int i = 0; i < P; ++i) v[i] = f2(x[2 * i], x[2 * i + 1]);
   }
-  __device__ __forceinline__ void give_f32(float* p, const Pairs& v) const {
+  template <bool SINGLE>
+  __device__ __forceinline__ void store_f32(float* p, const Pairs& v) const {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float y[VEC];
       vector(v, j, y);
-      if (!live(j)) continue;
-      float* at = p + column(j);
-      if constexpr (VEC >= 4) {
+      float* const at = p + column(j);
+      if constexpr (SINGLE || VEC == 1) {
 #pragma unroll
-        for (int k = 0; k < VEC; k += 4) *reinterpret_cast<float4*>(at + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+        for (int k = 0; k < VEC; ++k)
+          if (live(j, k)) at[k] = y[k];
       } else if constexpr (VEC == 2) {
-        *reinterpret_cast<float2*>(at) = make_float2(y[0], y[1]);
+        if (live(j)) *reinterpret_cast<float2*>(at) = make_float2(y[0], y[1]);
       } else {
-        *at = y[0];
+#pragma unroll
+        for (int k = 0; k < VEC; k += 4)
+          if (live(j)) *reinterpret_cast<float4*>(at + k) = make_float4(y[k], y[k + 1], y[k + 2], y[k + 3]);
       }
     }
   }
@@ -692,44 +771,43 @@ struct Team {
       asm volatile("prefetch.global.L2 [%0];" ::"l"(a.gate + (long long)seg * a.d + c));
   }
 
-  // A row of a tensor into a stage: WHOLE, by the threads that read it; else by the team, in 16-byte pieces.
+  // Teams of less than a warp: a row of a tensor into a stage by the threads that read it; or in 16-byte pieces, none of which
+  // reaches beyond the tensor.
   __device__ __forceinline__ void copy_pieces(uint32_t dst, const void* base, int row, int bytes, int rows) const {
     const long long at = (long long)row * bytes, from = at & ~15LL;
-    const int n = ((int)(at & 15) + bytes + 15) >> 4;
+    const int n = ((int)(at & 15) + bytes + 15) >> 4, left = (int)min((long long)rows * bytes - from, (long long)n * 16);
     const char* src = static_cast<const char*>(base) + from;
-    // (no piece reaches beyond the tensor)
-    const int left = (int)min((long long)rows * bytes - from, (long long)n * 16);
     for (int i = lane; i < n; i += tl)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * 16), "l"(src + i * 16),
                    "r"(min(16, left - i * 16))
                    : "memory");
   }
   __device__ __forceinline__ void copy_tensor(uint32_t dst, const void* base, int row, const BlockArgs& a) const {
-    if constexpr (WHOLE) {
-      const char* src = static_cast<const char*>(base) + (long long)row * (a.d * ES);
+    if constexpr (WAY >= RAGGED) {
+      copy_pieces(dst, base, row, d * ES, a.rows);
+    } else {
+      const char* src = static_cast<const char*>(base) + (long long)row * (d * ES);
 #pragma unroll
       for (int j = 0; j < NV; ++j)
         if (live(j)) copy_async<16>(dst + column(j) * ES, src + column(j) * ES);
-    } else {
-      copy_pieces(dst, base, row, a.d * ES, a.rows);
     }
   }
   __device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t* base, int row, const BlockArgs& a) const {
-    if constexpr (WHOLE) {
+    if constexpr (NARROW) {
+      copy_pieces(dst, base, row, a.dp, a.rows);
+    } else {
       const uint8_t* src = base + (long long)row * a.dp;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
         if (live(j)) copy_async<VEC>(dst + column(j), src + column(j));
-    } else {
-      copy_pieces(dst, base, row, a.dp, a.rows);
     }
   }
-  // A row of a checkpoint.  The exponents: WHOLE, fetched into registers a row ahead; else from the stage.
+  // A row of a checkpoint: codes from the stage; the exponents of a thread's vectors fetched a row ahead, NARROW from the stage.
   struct Bytes {
-    uint32_t b[WHOLE ? NV : 1];
+    uint32_t b[NARROW ? 1 : NV];
   };
   __device__ __forceinline__ void fetch_bytes(const uint8_t* exps, int row, const BlockArgs& a, Bytes& b) const {
-    if constexpr (WHOLE) {
+    if constexpr (!NARROW) {
       const uint8_t* e = exps + (long long)row * (a.dp / ckpt8::kBlock);
 #pragma unroll
       for (int j = 0; j < NV; ++j) b.b[j] = live(j) ? __ldg(e + column(j) / ckpt8::kBlock) : 0u;
@@ -739,15 +817,10 @@ struct Team {
     float x[N], s[N];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = column(j);
       ckpt8::Raw<VEC> r = {};
-      if ((FULL || valid) && live(j)) {
-        if constexpr (WHOLE) {
-          r = ckpt8::get_codes<VEC>(reinterpret_cast<const uint8_t*>(codes) + c);
-          r.b = b.b[j];
-        } else {
-          r = ckpt8::get<VEC>(reinterpret_cast<const uint8_t*>(codes) + c, reinterpret_cast<const uint8_t*>(exps) + c / ckpt8::kBlock);
-        }
+      if ((WAY == FULL || valid) && live(j)) {
+        r = ckpt8::get_codes<VEC>(reinterpret_cast<const uint8_t*>(codes) + column(j));
+        r.b = NARROW ? reinterpret_cast<const uint8_t*>(exps)[column(j) / ckpt8::kBlock] : b.b[NARROW ? 0 : j];
       }
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
@@ -765,12 +838,12 @@ struct Team {
     uint8_t* const to_e = exps + (long long)row * (a.dp / ckpt8::kBlock);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if (!FULL && j > 0 && j * cs >= a.dp) continue;             // (nothing of the row there, whatever the lane)
+      if (WAY != FULL && j > 0 && j * cs >= a.dp) continue;             // (nothing of the row there, whatever the lane)
       float x[VEC];
       vector(v, j, x);
       const ckpt8::Scale s = ckpt8::scale_of(ckpt8::block_most<VEC>(x));
       const int c = column(j);
-      if (FULL || (valid && c < a.dp)) {
+      if (WAY == FULL || (valid && c < a.dp)) {
         ckpt8::put_codes<VEC>(to + c, x, s);
         if (c % ckpt8::kBlock == 0) to_e[c / ckpt8::kBlock] = (uint8_t)s.byte;
       }
@@ -790,7 +863,7 @@ struct Team {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
           const float2 x = split(v[i]);
-          v[i] = f2(live(2 * i / VEC) ? x.x : 0.f, live((2 * i + 1) / VEC) ? x.y : 0.f);
+          v[i] = f2(live(2 * i / VEC, 2 * i % VEC) ? x.x : 0.f, live((2 * i + 1) / VEC, (2 * i + 1) % VEC) ? x.y : 0.f);
         }
       }
     }
@@ -802,10 +875,10 @@ struct Team {
   }
 };
 
-template <int DT, int VEC, bool FULL>
+template <int DT, int WAY>
 __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const BlockArgs a) {
   constexpr int kStages = kMostStages;
-  using T = Team<DT, VEC, FULL>;
+  using T = Team<DT, WAY>;
   constexpr int P = T::P;
   extern __shared__ __align__(16) char ring[];
   __shared__ __align__(16) float sm[4 * kMostWarps];
@@ -816,9 +889,12 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
   T t(a, sm, bars, &flag, branch ? 2 : 1);
   const int team_in = threadIdx.x / a.tl;
   const int r0 = (int)min((long long)a.rows, ((long long)blockIdx.x * a.teams + team_in) * a.chunk), r1 = r0 + min(a.rows - r0, a.chunk);
-  const int bytes = a.d * T::ES, room = row_room(bytes), stage = 2 * room;
+  const int bytes = a.d * T::ES, room = stage_room(bytes, WAY >= RAGGED), stage = 2 * room;
   char* const mine = ring + (size_t)team_in * a.team_smem;
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+  // (behind the ring, RAGGED: rows on their way out, and shift)
+  char* const out = mine + kStages * stage + 16;
+  float* const shifts = reinterpret_cast<float*>(mine + kStages * stage + (WAY == RAGGED ? 2 * room : 0));
   if (threadIdx.x == 0) {
     sources.n = 0;
     sources.add(a.h, bytes, 0);
@@ -844,26 +920,31 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
   long long seg_end = (long long)(seg + 1) * a.per;
   if (branch) t.take_factors(a, seg, gps);
   if (a.n != nullptr) t.take_f32(a.pre, pre);
+  if (a.shift != nullptr) {
+    F2 v[P];
+    t.take_f32(a.shift, v);
+    t.give_own(shifts, v);
+  }
   if (!t.bulk) wait_copies<kStages - 2>();
   t.sync();
-  int slot = 0;
+  int slot = 0, before = -1;      // RAGGED: the row whose n is still on its way out
   uint32_t phase = 0;
   for (int i = 0; i < a.chunk; ++i) {
     const int row = r0 + i;
-    const bool valid = FULL || row < r1;
-    if ((FULL || a.tl >= 32) && row >= r1) break;                 // (a team of whole warps has no other team's lanes in them)
+    const bool valid = WAY == FULL || row < r1;
+    if ((WAY == FULL || a.tl >= 32) && row >= r1) break;                 // (a team of whole warps has no other team's lanes in them)
     const char* at = mine + slot * stage;
-    const int off = T::WHOLE ? 0 : (int)(((long long)row * bytes) & 15);
+    const int off = WAY >= RAGGED ? (int)(((long long)row * bytes) & 15) : 0;
     issue(row + kStages - 1, slot == 0 ? kStages - 1 : slot - 1);
     t.wait_row(slot, phase, a);
     F2 h[P];
-    t.take(at + off, valid, h);
+    t.take(at, off, valid, h);
     if (a.kh != nullptr) t.keep_row(a.kh, a.keh, row, a, valid, h);
     float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
     if (!t.bulk && a.n == nullptr) wait_copies<kStages - 2>();
     if (branch) {
       F2 u[P];
-      t.take(at + room + off, valid, u);
+      t.take(at + room, off, valid, u);
       if (a.ku != nullptr) t.keep_row(a.ku, a.keu, row, a, valid, u);
       if (valid && row == seg_end) {
         seg_end += a.per;
@@ -871,39 +952,61 @@ __global__ void __launch_bounds__(kFwdThreads<DT>) block_fwd_rows_kernel(const B
       }
       if (row + 1 == seg_end && row + 1 < r1) t.fetch_gate(a, seg + 1);
       const float2 m = t.normalise(u, a);
+      if (WAY == RAGGED) {
+        t.after_sum();
+        if (before >= 0) t.flush(a.n, before, out + room);
+      }
       st.x = m.x; st.y = m.y;
 #pragma unroll
       for (int k = 0; k < P; ++k) h[k] = fma(f2(a.keep), h[k], gps[k] * (u[k] * f2(m.y)));
-      if (valid) t.give(a.h_out, row, a.d, h);
+      if (valid) t.give(a.h_out, row, h, out);
     }
     if (a.n != nullptr) {
       if (!t.bulk) wait_copies<kStages - 2>();
       const float2 m = t.normalise(h, a);
+      if (WAY == RAGGED) {
+        t.after_sum();
+        if (branch && valid) t.flush(a.h_out, row, out);
+      }
       st.z = m.x; st.w = m.y;
 #pragma unroll
       for (int k = 0; k < P; ++k) h[k] = h[k] * f2(m.y) * pre[k];
       if (a.shift != nullptr) {
         F2 shift[P];
-        t.take_f32(a.shift, shift);
+        t.take_own(shifts, shift);
 #pragma unroll
         for (int k = 0; k < P; ++k) h[k] = h[k] + shift[k];
       }
-      if (valid) t.give(a.n, row, a.d, h);
+      if (valid) t.give(a.n, row, h, out + room);
+    }
+    if (WAY == RAGGED) {
+      // (n waits for the next row's first sum; with one norm alone there is no sum between its rows' ways out)
+      before = a.n != nullptr && valid ? row : -1;
+      if (a.n == nullptr || !branch) {
+        t.sync();
+        if (valid) t.flush(a.n != nullptr ? a.n : a.h_out, row, a.n != nullptr ? out + room : out);
+        before = -1;
+        t.sync();
+      }
     }
     if (a.stats != nullptr && t.lane == 0 && valid) a.stats[row] = st;
     if (t.warps == 0) __syncwarp();
     if (++slot == kStages) { slot = 0; phase ^= 1u; }
   }
   wait_copies<0>();
+  if (WAY == RAGGED) {
+    t.sync();
+    if (before >= 0) t.flush(a.n, before, out + room);
+  }
   t.leave(a);
 }
 
 // Beside the ring a team has [d] fp32 of gate*post*scale, of pre (from L1, which the copies pass through, each reading of it
 // stood in the row's way: 243 us for 16384 x 4096 bf16 against 182), where the teams have several gates (split = 0) of dpost, and of dshift where
 // that is asked for.
-template <int DT, int VEC, bool FULL, bool KEPT>
+template <int DT, int WAY, bool KEPT>
 __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const BlockArgs a) {
-  using T = Team<DT, VEC, FULL>;
+  using T = Team<DT, WAY>;
   constexpr int P = T::P;
   extern __shared__ __align__(16) char ring[];
   __shared__ __align__(16) float sm[4 * kMostWarps];
@@ -911,16 +1014,18 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   __shared__ int flag;
   __shared__ Sources sources;
   const bool branch = a.post != nullptr, norm = a.dn != nullptr;
-  T t(a, sm, bars, &flag, (a.dh_out != nullptr) + norm + (KEPT && !T::WHOLE ? 2 : 1) * (1 + branch));
+  T t(a, sm, bars, &flag, (a.dh_out != nullptr) + norm + (KEPT && T::NARROW ? 2 : 1) * (1 + branch));
   const int team_in = threadIdx.x / a.tl;
   const long long team = (long long)blockIdx.x * a.teams + team_in;
   const int bytes = a.d * T::ES, eb = a.dp / ckpt8::kBlock;
-  const int room = row_room(bytes), room_k = row_room(KEPT ? a.dp : bytes), room_e = KEPT && !T::WHOLE ? row_room(eb) : 0;
-  // a stage: dh', dn, h, u and the exponents of both
+  const int room = stage_room(bytes, WAY >= RAGGED), room_k = KEPT ? row_room(a.dp) : room;
+  const int room_e = KEPT && T::NARROW ? stage_room(eb, true) : 0;
+  // a stage: dh', dn, h, u and, NARROW, the exponents of both
   const int at_h = 2 * room, at_u = at_h + room_k, at_eh = at_u + room_k, at_eu = at_eh + room_e, stage = at_eu + room_e;
-  const int own = row_room(a.d * 4), stages = a.stages;
+  const int own = row_room(a.dp * 4), stages = a.stages;
   char* const mine = ring + (size_t)team_in * a.team_smem;
-  float* const factors = reinterpret_cast<float*>(mine + stages * stage);
+  char* const out = mine + stages * stage + 16;      // (RAGGED: rows on their way out)
+  float* const factors = reinterpret_cast<float*>(mine + stages * stage + (WAY == RAGGED ? 2 * room : 0));
   float* const pres = factors + own / 4;
   float* const posts = pres + own / 4;
   float* const shifts = a.split == 0 ? posts + own / 4 : posts;
@@ -931,7 +1036,7 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     sources.add(a.dn, bytes, room);
     sources.add(KEPT ? (const void*)a.ch : a.h, KEPT ? a.dp : bytes, at_h);
     sources.add(KEPT ? (const void*)a.cu : a.u, KEPT ? a.dp : bytes, at_u);
-    if (KEPT && !T::WHOLE) {
+    if (KEPT && T::NARROW) {
       sources.add(a.eh, eb, at_eh);
       sources.add(branch ? a.eu : nullptr, eb, at_eu);
     }
@@ -965,10 +1070,10 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       if (norm) t.copy_tensor(to + room, a.dn, row, a);
       if constexpr (KEPT) {
         t.copy_codes(to + at_h, a.ch, row, a);
-        if (!T::WHOLE) t.copy_pieces(to + at_eh, a.eh, row, eb, a.rows);
+        if (T::NARROW) t.copy_pieces(to + at_eh, a.eh, row, eb, a.rows);
         if (branch) {
           t.copy_codes(to + at_u, a.cu, row, a);
-          if (!T::WHOLE) t.copy_pieces(to + at_eu, a.eu, row, eb, a.rows);
+          if (T::NARROW) t.copy_pieces(to + at_eu, a.eu, row, eb, a.rows);
         }
       } else {
         t.copy_tensor(to + at_h, a.h, row, a);
@@ -985,14 +1090,14 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   if (branch) {
     F2 f[P];
     t.take_factors(a, seg, f);
-    t.give_f32(factors, f);
-    if (a.split == 0) t.give_f32(posts, E);
+    t.give_own(factors, f);
+    if (a.split == 0) t.give_own(posts, E);
   }
-  if (a.shifted) t.give_f32(shifts, E);
+  if (a.shifted) t.give_own(shifts, E);
   if (norm) {
     F2 f[P];
     t.take_f32(a.pre, f);
-    t.give_f32(pres, f);
+    t.give_own(pres, f);
   }
   float4 next = make_float4(0.f, 0.f, 0.f, 0.f);
   typename T::Bytes bytes_h = {}, bytes_u = {};
@@ -1013,10 +1118,11 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   uint32_t phase = 0;
   for (int i = 0; i < a.chunk; ++i) {
     const int row = r0 + i;
-    const bool valid = FULL || row < r1;
-    if ((FULL || a.tl >= 32) && row >= r1) break;
+    const bool valid = WAY == FULL || row < r1;
+    if ((WAY == FULL || a.tl >= 32) && row >= r1) break;
     const char* at = mine + slot * stage;
-    const int off = T::WHOLE ? 0 : (int)(((long long)row * bytes) & 15), off_e = T::WHOLE ? 0 : (int)(((long long)row * eb) & 15);
+    const int off = WAY >= RAGGED ? (int)(((long long)row * bytes) & 15) : 0;
+    const int off_e = T::NARROW ? (int)(((long long)row * eb) & 15) : 0;
     issue(row + stages - 1, slot == 0 ? stages - 1 : slot - 1);
     t.wait_row(slot, phase, a);
     const float4 st = next;
@@ -1025,19 +1131,19 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
         F2 f[P];
         seg_end += a.per;
         t.take_factors(a, ++seg, f);
-        t.give_f32(factors, f);
+        t.give_own(factors, f);
       }
       if (row + 1 == seg_end && row + 1 < r1) t.fetch_gate(a, seg + 1);
     }
     // u^ and h^; sums of q = dn*pre and q*h^
     F2 uh[P], hh[P];
     if constexpr (KEPT) t.take_codes(at + at_h, at + at_eh + off_e, bytes_h, valid, hh);
-    else t.take(at + at_h + off, valid, hh);
+    else t.take(at + at_h, off, valid, hh);
     if (branch) {
       if constexpr (KEPT) t.take_codes(at + at_u, at + at_eu + off_e, bytes_u, valid, uh);
-      else t.take(at + at_u + off, valid, uh);
+      else t.take(at + at_u, off, valid, uh);
       F2 f[P];
-      t.take_f32(factors, f);
+      t.take_own(factors, f);
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         uh[k] = (uh[k] + f2(-st.x)) * f2(st.y);
@@ -1048,8 +1154,8 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     float m0 = 0.f, m1 = 0.f;
     if (norm) {
       F2 dn[P], pre[P], s0 = zero, s1 = zero;
-      t.take(at + room + off, valid, dn);
-      t.take_f32(pres, pre);
+      t.take(at + room, off, valid, dn);
+      t.take_own(pres, pre);
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         hh[k] = (hh[k] + f2(-st.z)) * f2(st.w);
@@ -1061,10 +1167,10 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       m0 = sum(s0);
       m1 = sum(s1);
       if (a.shifted) {
-        t.take_f32(shifts, pre);
+        t.take_own(shifts, pre);
 #pragma unroll
         for (int k = 0; k < P; ++k) pre[k] = pre[k] + dn[k];
-        t.give_f32(shifts, pre);
+        t.give_own(shifts, pre);
       }
     }
     t.sum2(m0, m1);
@@ -1073,8 +1179,8 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     // D in h^'s place
     if (norm) {
       F2 dn[P], pre[P];      // (again, from shared memory: held, they would cost the registers of a row)
-      t.take(at + room + off, valid, dn);
-      t.take_f32(pres, pre);
+      t.take(at + room, off, valid, dn);
+      t.take_own(pres, pre);
 #pragma unroll
       for (int k = 0; k < P; ++k) hh[k] = f2(st.w) * fma(hh[k], f2(-m1), fma(dn[k], pre[k], f2(-m0)));
     } else {
@@ -1083,7 +1189,7 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     }
     if (a.dh_out != nullptr) {
       F2 dh[P];
-      t.take(at + off, valid, dh);
+      t.take(at, off, valid, dh);
 #pragma unroll
       for (int k = 0; k < P; ++k) hh[k] = hh[k] + dh[k];
     }
@@ -1092,8 +1198,8 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       F2 v[P], s0 = zero, s1 = zero;
 #pragma unroll
       for (int k = 0; k < P; ++k) v[k] = f2(a.keep) * hh[k];
-      if (valid) t.give(a.dh, row, a.d, v);
-      t.take_f32(factors, v);
+      if (valid) t.give(a.dh, row, v, out);
+      t.take_own(factors, v);
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         E[k] = fma(hh[k], uh[k], E[k]);
@@ -1104,10 +1210,14 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       t0 = sum(s0);
       t1 = sum(s1);
     } else if (valid) {
-      t.give(a.dh, row, a.d, hh);
+      t.give(a.dh, row, hh, out);
     }
     if (!t.bulk) {
       if (stages == 3) wait_copies<1>(); else wait_copies<0>();
+    }
+    if (WAY == RAGGED) {
+      t.sync();
+      if (valid) t.flush(a.dh, row, out);
     }
     t.sum2(t0, t1);
     if (branch) {
@@ -1116,17 +1226,17 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
 #pragma unroll
       for (int k = 0; k < P; ++k) hh[k] = f2(st.y) * fma(uh[k], f2(-t1), hh[k] + f2(-t0));
       if (valid) {
-        t.give(a.du, row, a.d, hh);
+        t.give(a.du, row, hh, out + room);
         if (a.split == 0 && (row + 1 == r1 || row + 1 == seg_end)) {      // the end of a gate's rows
           F2 g[P], v[P];
           t.take_f32(a.gate + (long long)seg * a.d, g);
-          t.take_f32(posts, v);
+          t.take_own(posts, v);
 #pragma unroll
           for (int k = 0; k < P; ++k) {
             E[k] = E[k] * f2(a.scale);
             v[k] = fma(g[k], E[k], v[k]);
           }
-          t.give_f32(posts, v);
+          t.give_own(posts, v);
           t.take_f32(a.post, g);
 #pragma unroll
           for (int k = 0; k < P; ++k) {
@@ -1136,6 +1246,12 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
           t.give_f32(a.dgate + (long long)seg * a.d, g);
         }
       }
+    }
+    // (at once: held back until the next row's sum, as the forward pass does with n, the way out costs registers: 148 us for
+    // 16384 x 1001 against 114)
+    if (WAY == RAGGED && branch) {
+      t.sync();
+      if (valid) t.flush(a.du, row, out + room);
     }
     if (t.warps == 0) __syncwarp();
     if (++slot == stages) { slot = 0; phase ^= 1u; }
@@ -1159,7 +1275,7 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
     float* to = (which == 3 ? a.part_e : a.part + which * slab) + (long long)blockIdx.x * a.d;
     if (which == 2) {
       if (a.split == 0) {
-        t.take_f32(posts, v);
+        t.take_own(posts, v);
       } else if (a.gate == nullptr) {
 #pragma unroll
         for (int k = 0; k < P; ++k) v[k] = E[k];
@@ -1169,12 +1285,12 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
         for (int k = 0; k < P; ++k) v[k] = v[k] * E[k];
       }
     }
-    if (which == 1) t.take_f32(shifts, v);
+    if (which == 1) t.take_own(shifts, v);
     const F2(&of)[P] = which == 0 ? spre : which == 3 ? E : v;
     if (a.teams > 1) {
       // (at the start of each team's ring, which has room for a row of fp32; what is its own lies behind the ring)
       __syncthreads();
-      t.give_f32(joined + team_in * (a.team_smem / 4), of);
+      t.give_own(joined + team_in * (a.team_smem / 4), of);
       __syncthreads();
       for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
         float s = 0.f;
@@ -1257,12 +1373,12 @@ BlockPlan plan_block(const dk_block& q, bool backward, const Asked& asked) {
   const long long per = asked.gated && q.rows_per_gate < q.rows ? q.rows_per_gate : q.rows;
   p.gates = per > 0 ? (q.rows + per - 1) / per : 0;
   p.whole = q.d % vec == 0;
-  const int values = f32 ? kValues<DK_F32, true> : p.whole ? kValues<DK_BF16, true> : kValues<DK_BF16, false>;
+  const int values = f32 ? kValues<DK_F32> : kValues<DK_BF16>;
   p.full = q.d % (32 * values) == 0;
   const int threads = (dp + values - 1) / values;
   if (threads <= 32) {
     // (a block of 32 values lies in one vector of neighbouring lanes)
-    p.tl = ckpt8::kBlock / (p.whole ? vec : q.d % 2 == 0 ? 2 : 1);
+    p.tl = ckpt8::kBlock / (p.whole || !f32 ? vec : q.d % 2 == 0 ? 2 : 1);
     while (p.tl < threads) p.tl *= 2;
     p.teams = kSmallTeams / p.tl;
   } else {
@@ -1271,15 +1387,15 @@ BlockPlan plan_block(const dk_block& q, bool backward, const Asked& asked) {
   }
   // A team's ring of three rows, or of two where that lets an SM hold more teams; and as many rows to a team as give every SM
   // the CTAs that its registers and shared memory hold.  (Backward, teams with several gates each need room for dpost.)
-  const int row = row_room(q.d * es), f32s = row_room(q.d * 4), room = 220 * 1024, teams_most = p.teams;
+  const int row = stage_room(q.d * es, !p.whole), f32s = row_room(dp * 4), out = p.whole || f32 ? 0 : 2 * row, room = 220 * 1024;
+  const int exps = f32 && !p.whole ? stage_room(dp / ckpt8::kBlock, true) : 0;
+  const int teams_most = p.teams;
   long long ctas = 0, want = 0, chunk = 0;
   for (int posts = 0; posts < 2; ++posts) {
     ctas = 0;
     for (int stages = 3; stages >= 2; --stages) {
-      int smem = stages * 2 * row;
-      if (backward)
-        smem = stages * (2 * row + 2 * (asked.held ? row_room(dp) + (p.whole ? 0 : row_room(dp / ckpt8::kBlock)) : row)) +
-               (2 + posts + asked.shifted) * f32s;
+      int smem = stages * 2 * row + out + f32s;
+      if (backward) smem = stages * (2 * row + 2 * (asked.held ? row_room(dp) + exps : row)) + out + (2 + posts + asked.shifted) * f32s;
       int teams = teams_most;
       while (teams > 1 && teams * smem > room / 2) teams /= 2;
       long long c = most / (p.tl * teams);
@@ -1344,28 +1460,57 @@ dk_status launch_rows(K kern, SmemLimit& limit, const BlockArgs& a, const BlockP
   if (s != DK_OK) return s;
   return launch_chained(kern, dim3((unsigned)p.ctas), p.tl * p.teams, (size_t)smem, st, a) == cudaSuccess ? DK_OK : DK_ERR_CUDA;
 }
+// (rows above the limit: vectors as wide as all rows' alignment allows)
 template <int DT, int VEC>
-dk_status launch_fwd(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
-  constexpr bool WHOLE = VEC == (DT == DK_F32 ? 4 : 8);
-  static SmemLimit limits[3];
-  if (p.wide) return launch_rows(block_fwd_wide_kernel<DT, VEC, 16 / VEC>, limits[0], a, p, 0, device, st);
-  if constexpr (WHOLE)
-    if (p.full) return launch_rows(block_fwd_rows_kernel<DT, VEC, true>, limits[1], a, p, p.smem * p.teams, device, st);
-  return launch_rows(block_fwd_rows_kernel<DT, VEC, false>, limits[2], a, p, p.smem * p.teams, device, st);
+dk_status launch_fwd_wide(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
+  static SmemLimit limit;
+  return launch_rows(block_fwd_wide_kernel<DT, VEC, 16 / VEC>, limit, a, p, 0, device, st);
 }
-template <int DT, int VEC, bool KEPT>
-dk_status launch_bwd(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
-  constexpr bool WHOLE = VEC == (DT == DK_F32 ? 4 : 8);
-  static SmemLimit limits[3];
+template <int DT, int VEC>
+dk_status launch_bwd_wide(const BlockArgs& a, const BlockPlan& p, bool kept, int device, cudaStream_t st) {
+  static SmemLimit limits[2];
+  return kept ? launch_rows(block_bwd_wide_kernel<DT, VEC, 16 / VEC, true>, limits[0], a, p, p.smem, device, st)
+              : launch_rows(block_bwd_wide_kernel<DT, VEC, 16 / VEC, false>, limits[1], a, p, p.smem, device, st);
+}
+template <int DT, int WAY>
+dk_status launch_fwd_rows(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
+  static SmemLimit limit;
+  return launch_rows(block_fwd_rows_kernel<DT, WAY>, limit, a, p, p.smem * p.teams, device, st);
+}
+template <int DT, int WAY>
+dk_status launch_bwd_rows(const BlockArgs& a, const BlockPlan& p, bool kept, int device, cudaStream_t st) {
+  static SmemLimit limits[2];
   const int smem = p.smem * p.teams;
-  if (p.wide) return launch_rows(block_bwd_wide_kernel<DT, VEC, 16 / VEC, KEPT>, limits[0], a, p, smem, device, st);
-  if constexpr (WHOLE)
-    if (p.full) return launch_rows(block_bwd_rows_kernel<DT, VEC, true, KEPT>, limits[1], a, p, smem, device, st);
-  return launch_rows(block_bwd_rows_kernel<DT, VEC, false, KEPT>, limits[2], a, p, smem, device, st);
+  return kept ? launch_rows(block_bwd_rows_kernel<DT, WAY, true>, limits[0], a, p, smem, device, st)
+              : launch_rows(block_bwd_rows_kernel<DT, WAY, false>, limits[1], a, p, smem, device, st);
 }
-template <int DT, int VEC>
+template <int DT>
+dk_status launch_fwd(const BlockArgs& a, const BlockPlan& p, int device, cudaStream_t st) {
+  if (p.wide) {
+    if constexpr (DT == DK_BF16)
+      if (p.whole) return launch_fwd_wide<DT, 8>(a, p, device, st);
+    if constexpr (DT == DK_F32)
+      if (p.whole) return launch_fwd_wide<DT, 4>(a, p, device, st);
+    return a.d % 2 == 0 ? launch_fwd_wide<DT, 2>(a, p, device, st) : launch_fwd_wide<DT, 1>(a, p, device, st);
+  }
+  if (p.full) return launch_fwd_rows<DT, FULL>(a, p, device, st);
+  if (p.whole) return launch_fwd_rows<DT, WHOLE>(a, p, device, st);
+  if constexpr (DT == DK_BF16) return launch_fwd_rows<DT, RAGGED>(a, p, device, st);
+  else return a.d % 2 == 0 ? launch_fwd_rows<DT, PAIRS>(a, p, device, st) : launch_fwd_rows<DT, SINGLES>(a, p, device, st);
+}
+template <int DT>
 dk_status launch_bwd(const BlockArgs& a, const BlockPlan& p, bool kept, int device, cudaStream_t st) {
-  return kept ? launch_bwd<DT, VEC, true>(a, p, device, st) : launch_bwd<DT, VEC, false>(a, p, device, st);
+  if (p.wide) {
+    if constexpr (DT == DK_BF16)
+      if (p.whole) return launch_bwd_wide<DT, 8>(a, p, kept, device, st);
+    if constexpr (DT == DK_F32)
+      if (p.whole) return launch_bwd_wide<DT, 4>(a, p, kept, device, st);
+    return a.d % 2 == 0 ? launch_bwd_wide<DT, 2>(a, p, kept, device, st) : launch_bwd_wide<DT, 1>(a, p, kept, device, st);
+  }
+  if (p.full) return launch_bwd_rows<DT, FULL>(a, p, kept, device, st);
+  if (p.whole) return launch_bwd_rows<DT, WHOLE>(a, p, kept, device, st);
+  if constexpr (DT == DK_BF16) return launch_bwd_rows<DT, RAGGED>(a, p, kept, device, st);
+  else return a.d % 2 == 0 ? launch_bwd_rows<DT, PAIRS>(a, p, kept, device, st) : launch_bwd_rows<DT, SINGLES>(a, p, kept, device, st);
 }
 
 // how long the kernels of bulk copies wait
@@ -1432,14 +1577,7 @@ dk_status backward(dk_ctx* ctx, const dk_block* q, bool kept, const void* dh_out
   a.layer = q->kind == DK_BLOCK_LAYER;
   a.eps = q->eps; a.keep = q->keep; a.scale = q->scale; a.inv_d = 1.f / (float)q->d;
   ProfScope ps(ctx, DK_KERNEL_OTHER, 2, st);
-  if (q->dtype == DK_F32)
-    s = p.whole           ? launch_bwd<DK_F32, 4>(a, p, kept, ctx->device, st)
-        : q->d % 2 == 0 ? launch_bwd<DK_F32, 2>(a, p, kept, ctx->device, st)
-                        : launch_bwd<DK_F32, 1>(a, p, kept, ctx->device, st);
-  else
-    s = p.whole           ? launch_bwd<DK_BF16, 8>(a, p, kept, ctx->device, st)
-        : q->d % 2 == 0 ? launch_bwd<DK_BF16, 2>(a, p, kept, ctx->device, st)
-                        : launch_bwd<DK_BF16, 1>(a, p, kept, ctx->device, st);
+  s = q->dtype == DK_F32 ? launch_bwd<DK_F32>(a, p, kept, ctx->device, st) : launch_bwd<DK_BF16>(a, p, kept, ctx->device, st);
   if (s != DK_OK) return s;
   const bool gates = gate != nullptr && p.split != 0;
   const SumArgs v{a.part, a.part_e, post, dpre, dshift, dpost, dgate, p.ctas, p.gates, q->d, p.split};
@@ -1505,13 +1643,7 @@ dk_status dk_block_norm_fwd(dk_ctx* ctx, const dk_block* q, const void* h, const
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   take_waits(ctx, p, a);
   ProfScope ps(ctx, DK_KERNEL_OTHER, 1, st);
-  if (q->dtype == DK_F32)
-    return p.whole           ? launch_fwd<DK_F32, 4>(a, p, ctx->device, st)
-           : q->d % 2 == 0 ? launch_fwd<DK_F32, 2>(a, p, ctx->device, st)
-                           : launch_fwd<DK_F32, 1>(a, p, ctx->device, st);
-  return p.whole           ? launch_fwd<DK_BF16, 8>(a, p, ctx->device, st)
-         : q->d % 2 == 0 ? launch_fwd<DK_BF16, 2>(a, p, ctx->device, st)
-                         : launch_fwd<DK_BF16, 1>(a, p, ctx->device, st);
+  return q->dtype == DK_F32 ? launch_fwd<DK_F32>(a, p, ctx->device, st) : launch_fwd<DK_BF16>(a, p, ctx->device, st);
 }
 
 dk_status dk_block_norm_bwd(dk_ctx* ctx, const dk_block* q, const void* dh_out, const void* dn, const void* h, const void* u,
