@@ -213,35 +213,60 @@ __global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if ((int)blockIdx.x < grid_dy) {
     const int strip = blockIdx.x % strips, part = blockIdx.x / strips;
-    const int c = strip * 256 + lane * 8;
-    if (c >= a.op) return;
-    float f[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = c + k < a.out ? pow2(scale_exp(__ldg(a.most_all + c + k))) : 0.f;
-    constexpr int U = 4;
-    const bool whole = a.out % 4 == 0 && c + 8 <= a.out;
     const long long step = (long long)row_parts * 8;
-    for (long long r = (long long)part * 8 + warp; r < a.rows; r += U * step) {
-      float v[U][8];
+    const float* dy = static_cast<const float*>(a.dy);
+    __half* const hi = static_cast<__half*>(a.hi);
+    __half* const lo = static_cast<__half*>(a.lo);
+    float f[8];
+    if (a.out % 4 == 0) {
+      const int c = strip * 256 + lane * 8;
+      if (c >= a.op) return;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (r + u * step >= a.rows) continue;
-        const float* s = static_cast<const float*>(a.dy) + (r + u * step) * a.out + c;
-        if (whole) {
-          const float4 x = __ldg(reinterpret_cast<const float4*>(s)), y = __ldg(reinterpret_cast<const float4*>(s) + 1);
-          v[u][0] = x.x; v[u][1] = x.y; v[u][2] = x.z; v[u][3] = x.w; v[u][4] = y.x; v[u][5] = y.y; v[u][6] = y.z; v[u][7] = y.w;
-        } else {
+      for (int k = 0; k < 8; ++k) f[k] = c + k < a.out ? pow2(scale_exp(__ldg(a.most_all + c + k))) : 0.f;
+      constexpr int U = 4;
+      for (long long r = (long long)part * 8 + warp; r < a.rows; r += U * step) {
+        float4 x[U], y[U];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[u][k] = c + k < a.out ? __ldg(s + k) : 0.f;
+        for (int u = 0; u < U; ++u) {
+          x[u] = y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (r + u * step >= a.rows) continue;
+          const float* s = dy + (r + u * step) * a.out + c;
+          x[u] = __ldg(reinterpret_cast<const float4*>(s));
+          if (c + 4 < a.out) y[u] = __ldg(reinterpret_cast<const float4*>(s) + 1);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (r + u * step >= a.rows) continue;
+          const float v[8] = {x[u].x * f[0], x[u].y * f[1], x[u].z * f[2], x[u].w * f[3],
+                              y[u].x * f[4], y[u].y * f[5], y[u].z * f[6], y[u].w * f[7]};
+          const long long at = (r + u * step) * a.op + c;
+          g16::store_planes<8>(hi + at, lo + at, v, 8);
         }
       }
+    } else {
+      // (rows of no whole vectors: neighbouring lanes take neighbouring columns)
+      const int c = strip * 256 + lane;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (r + u * step >= a.rows) continue;
+      for (int k = 0; k < 8; ++k) f[k] = c + 32 * k < a.out ? pow2(scale_exp(__ldg(a.most_all + c + 32 * k))) : 0.f;
+      constexpr int U = 2;
+      for (long long r = (long long)part * 8 + warp; r < a.rows; r += U * step) {
+        float v[U][8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[u][k] *= f[k];
-        const long long at = (r + u * step) * a.op + c;
-        g16::store_planes<8>(static_cast<__half*>(a.hi) + at, static_cast<__half*>(a.lo) + at, v[u], 8);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            v[u][k] = r + u * step < a.rows && c + 32 * k < a.out ? __ldg(dy + (r + u * step) * a.out + c + 32 * k) : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (r + u * step >= a.rows || c + 32 * k >= a.op) continue;
+            const float w = v[u][k] * f[k];
+            const __half h = __float2half_rn(w);
+            const long long at = (r + u * step) * a.op + c + 32 * k;
+            hi[at] = h;
+            lo[at] = __float2half_rn(w - __half2float(h));
+          }
       }
     }
     return;
