@@ -248,8 +248,9 @@ DK_API dk_status dk_destroy(dk_ctx* ctx);
  *                     it and stops, so every consumer's wait runs out; nothing is
  *                     read or written out of bounds.  (dk_orthogonalize's form
  *                     for short sides of at most 128: a CTA does not count at its
- *                     n-th meeting with the others.)  The option switches itself
- *                     off after one launch. */
+ *                     n-th meeting with the others; the block norms: a team
+ *                     of threads does not copy its n-th row.)  The option switches
+ *                     itself off after one launch. */
 enum {
   DK_OPT_TC_CHUNK = 0, DK_OPT_WG_CHUNK = 1, DK_OPT_TC_BK = 2, DK_OPT_TC_PAIR = 3, DK_OPT_WG_PACK = 4,
   DK_OPT_WG_PAIR = 5, DK_OPT_TC_STEM = 6, DK_OPT_FIELD_PATH = 7, DK_OPT_SPIN_LIMIT = 8,
@@ -561,7 +562,8 @@ DK_API dk_status dk_group_norm_bwd_ckpt8(dk_ctx* ctx, const dk_norm* q, const vo
  *   dW[o][c] = keep*dW[o][c] + scale*sum_r dy[r][o]*x[r][c]
  *   db[o]    = keep*db[o]    + scale*sum_r dy[r][o]
  * dy: [rows][out]; dW, db: fp32, db nullable.  keep = 0: neither is read.  The
- * checkpoint's values enter the tensor cores as they are.  DK_BF16: so does dy.
+ * checkpoint's values enter the tensor cores as they are.  DK_BF16: so does dy (a
+ * sum beyond fp32's range is infinite whatever `scale` is).
  * DK_F32: dy as two fp16 terms under a power of two of each output (22 bits down
  * to 2^-17 of the output's largest magnitude, an absolute error of 2^-39 of it
  * below), and the checkpoint's values under one power of two of all of it, exact

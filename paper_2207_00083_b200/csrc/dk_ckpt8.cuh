@@ -2,8 +2,8 @@
 // for each 32 consecutive values of a row,
 //   value = q*2^(b - 127),  |q| <= 127,
 // the rows of q padded with zeros to whole blocks, then the bytes b.  The power of two is the least under which no value
-// of the block rounds beyond 127, so a value is off by at most half a step, at
-// most 1/127 of the block's largest magnitude.  Powers of two, not max/127: x/2^k and q*2^k are exact, so what a value becomes
+// of the block rounds beyond 127, so a value is off by at most half a step, at most 1/127 of the block's largest magnitude.
+// Powers of two, not max/127: x/2^k and q*2^k are exact, so what a value becomes
 // does not depend on how the division is done, and q*2^k is a bf16 number, which the tensor cores take without another
 // rounding.  The largest b is 248: the few values beyond 127.5*2^121, which would round to 2^128, become 127*2^121 (a mask
 // of the type's largest magnitude among them).  b = 255: the block held an infinity or a NaN, and all its values are NaN.
@@ -129,10 +129,13 @@ __device__ __forceinline__ uint32_t block_most(const float (&v)[VEC], unsigned l
 #pragma unroll
   for (int i = 3; i < VEC; i += 2) f = abs_max(f, v[i], v[i + 1 < VEC ? i + 1 : i]);
   uint32_t m = __float_as_uint(f);
-  if constexpr (VEC == 1) return __reduce_max_sync(lanes, m);
+  if constexpr (VEC == 1) {
+    return __reduce_max_sync(lanes, m);
+  } else {
 #pragma unroll
-  for (int o = kBlock / VEC / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
-  return m;
+    for (int o = kBlock / VEC / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
+    return m;
+  }
 }
 
 }  // namespace ckpt8

@@ -758,7 +758,7 @@ dk_status norm_forward(dk_ctx* ctx, const dk_norm* q, const void* x, const float
   p.x = x; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats;
   // A checkpoint is written with the values where its blocks of 32 channels lie in one warp: whole blocks in a pixel and, for
   // items of blocks of channels, in an item.  Else by a launch of its own, first: y may be x.  (64x56x56x64 fp32, both
-  // directions: 99 us with two launches, 8x with one; 27x37x53x60 takes two.)
+  // directions: 99 us with two launches, 92 with one; 27x37x53x60 takes two.)
   const bool with = kept && q->c % ckpt8::kBlock == 0 && (!pl.sample[0] || pl.cb % ckpt8::kBlock == 0);
   ProfScope ps(ctx, DK_KERNEL_OTHER, launches(pl, true) + (kept && !with ? 1 : 0), st);
   if (with) {

@@ -1,4 +1,5 @@
-// Shared by the operators around the masked products (dk_norm.cu, dk_xent.cu, dk_ortho.cu).
+// Shared by the operators around the masked products (dk_norm.cu, dk_xent.cu, dk_ortho.cu,
+// dk_ckpt8.cu, dk_wgrad8.cu, dk_block.cu).
 #pragma once
 
 #include <cuda_runtime.h>

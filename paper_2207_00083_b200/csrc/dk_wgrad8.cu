@@ -9,6 +9,9 @@
 //     largest exponent
 //   wgrad8_prep_kernel: fp32: the operands
 //   the product (dk_gemm16.cuh), both operands read across their rows in place
+// Large products are bound by the tensor cores (16384 rows, 4096 x 4096 bf16: 445 us, of which 31 in the first launch; 1.24
+// PFLOP/s), products of few rows by the writing of dW (256 rows, 25088 x 4096 fp32: 126 us for 411 MB, floor 64), small ones
+// by the chain of launches (64 rows, 512 x 1000 fp32: 14 us).
 #include <math.h>
 
 #include "dk_ckpt8.cuh"
@@ -288,15 +291,17 @@ struct EpiW {
   static constexpr bool kAhead = false, kTail = true, kBulk = false;
   float* dW;
   long long pitch;
-  float scale, keep;
+  float scale;                       // of magnitude 1/2 to 1, its power of two in `exp`
+  int exp;
+  float keep;
   const unsigned int* most;          // fp32: of the outputs; null: nothing to undo
   const unsigned int* x_largest;
-  // (two factors, the smaller one first: together they may leave fp32's range where the result does not)
+  // All powers of two as two factors, both at least one or both at most one: nothing on the way leaves fp32's range unless
+  // the result does.
   __device__ __forceinline__ float undo(int row, float& second) const {
-    if (most == nullptr) return second = 1.f;
-    const float fx = pow2(-x_exp(*x_largest)), fo = pow2(-scale_exp(most[row]));
-    second = fmaxf(fx, fo);
-    return fminf(fx, fo);
+    const int e = most == nullptr ? exp : exp - x_exp(*x_largest) - scale_exp(most[row]), first = min(max(e, -126), 126);
+    second = pow2(min(max(e - first, -126), 126));
+    return pow2(first);
   }
   template <int NH>
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
@@ -305,7 +310,7 @@ struct EpiW {
     float f1;
     const float f0 = undo(min(row, p.M - 1), f1);
 #pragma unroll
-    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1 * scale;
+    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * scale * f0 * f1;
     const int rows = p.M - row0, cols = p.N - col0;
     float* dst = dW + (long long)row0 * pitch + col0;
     g16::warp_rows_f32<NH>(acc, sm, [&](int r, int c, float4 u) {
@@ -329,7 +334,7 @@ struct EpiWBulk {
   __device__ __forceinline__ float2 before(const Params& p, int row) const {
     float f1;
     const float f0 = w.undo(min(row, p.M - 1), f1);
-    return make_float2(f0 * w.scale, f1);
+    return make_float2(f0, f1);
   }
   template <int NH>
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int row, int col0, float2 f, char* sm,
@@ -337,7 +342,7 @@ struct EpiWBulk {
     const int row0 = row - (int)(threadIdx.x & 31);
     if (row0 >= p.M || col0 >= p.N) return;
 #pragma unroll
-    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f.x * f.y;
+    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * w.scale * f.x * f.y;
     g16::warp_rows_bulk<NH>(acc, sm, map, row0, col0, p.N - col0);
   }
 };
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(kThreads) wgrad8_slices_kernel(const float* __
     }
     float f1;
     const float f0 = e.undo(row, f1);
-    v = v * f0 * f1 * e.scale;
+    v = v * e.scale * f0 * f1;
     e.dW[i] = e.keep != 0.f ? fmaf(e.keep, e.dW[i], v) : v;
   }
 }
@@ -478,7 +483,9 @@ dk_status run(dk_ctx* ctx, const dk_wgrad8& q, const Plan& pl, Wg8& a, float* dW
   p.chunk = F32 ? 4 : 16;
   p.comp = (F32 ? 2.4f : 1.2f) / 16777216.f;
   p.comp_small = 1.2f / 16777216.f;
-  const EpiW e{dW, q.d, a.scale, a.keep, F32 ? a.most_all : nullptr, F32 ? a.block_exp + kMaxBlocks : nullptr};
+  int exp;
+  const float part_of_scale = frexpf(a.scale, &exp);
+  const EpiW e{dW, q.d, part_of_scale, exp, a.keep, F32 ? a.most_all : nullptr, F32 ? a.block_exp + kMaxBlocks : nullptr};
   if (!t.cs && t.ksplit > 1) {
     float* part = reinterpret_cast<float*>(ws + pl.off_part);
     const int pitch = (q.d + 3) / 4 * 4;

@@ -209,6 +209,28 @@ def test_wgrad_ranges(ctx, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("of_dy,of_x,scale", [(-100, 100, 1e-6), (60, 60, 1e-37), (-60, -55, 1e30), (-110, 115, 1.0), (90, -95, 1e-30)])
+@pytest.mark.parametrize("rows,d,out", [(300, 160, 60), (256, 2560, 4096), (256, 2562, 4096), (2000, 2560, 2560)])
+def test_wgrad_far_from_one(ctx, rows, d, out, of_dy, of_x, scale, dtype):
+    """Operands' powers of two and `scale` that lie far apart: where the result is a number, so is what leads to it."""
+    code, dt = TYPES[dtype]
+    dy, x = draw(rows, out, dt, spread=0.5) * 2.0 ** of_dy, draw(rows, d, dt, seed=3, spread=0.5) * 2.0 ** of_x
+    ckpt = stored(ctx, x)
+    q = dk.dk_wgrad8(rows, d, out, code)
+    ctx.ensure_workspace(q)
+    dW = torch.empty((out, d), device="cuda")
+    dk.dk_linear_bwd_wgrad_ckpt8(ctx, q, dy, ckpt, scale, 0.0, dW, None)
+    xv, dyv = kept.decode(ckpt, rows, d), dy.double()
+    want, tol = dyv.t() @ xv * scale, wgrad_bound(dyv, xv, dtype) * scale + 2.0 ** -126
+    good = (dW.double() - want).abs() <= tol
+    if dtype == "bf16":
+        # (bf16 operands enter as they are: where the magnitudes of the products add up to more than fp32's largest number, a
+        # part of their sum may be more too, before `scale` makes a number of it)
+        good = good | (dyv.abs().t() @ xv.abs() >= 2.0 ** 128)
+    assert bool(good.all()), float(((dW.double() - want).abs() / tol).max())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_wgrad_of_infinities(ctx, dtype):
     """An infinity or a NaN in dy spoils its output's row of dW (and db) alone, one in x its block's columns."""
     code, dt = TYPES[dtype]
