@@ -296,12 +296,12 @@ struct EpiW {
   float keep;
   const unsigned int* most;          // fp32: of the outputs; null: nothing to undo
   const unsigned int* x_largest;
-  // All powers of two as two factors, both at least one or both at most one: nothing on the way leaves fp32's range unless
-  // the result does.
+  // Scale and all powers of two as two factors, of which the second is one unless their power of two lies beyond fp32's
+  // range, and then on the first one's side: nothing on the way leaves the range unless the result does.
   __device__ __forceinline__ float undo(int row, float& second) const {
-    const int e = most == nullptr ? exp : exp - x_exp(*x_largest) - scale_exp(most[row]), first = min(max(e, -126), 126);
+    const int e = most == nullptr ? exp : exp - x_exp(*x_largest) - scale_exp(most[row]), first = min(max(e, -125), 126);
     second = pow2(min(max(e - first, -126), 126));
-    return pow2(first);
+    return scale * pow2(first);
   }
   template <int NH>
   __device__ __forceinline__ void operator()(const Params& p, float (&acc)[NH], int, int, int row, int col0, char* sm) const {
@@ -310,7 +310,7 @@ struct EpiW {
     float f1;
     const float f0 = undo(min(row, p.M - 1), f1);
 #pragma unroll
-    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * scale * f0 * f1;
+    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f0 * f1;
     const int rows = p.M - row0, cols = p.N - col0;
     float* dst = dW + (long long)row0 * pitch + col0;
     g16::warp_rows_f32<NH>(acc, sm, [&](int r, int c, float4 u) {
@@ -342,7 +342,7 @@ struct EpiWBulk {
     const int row0 = row - (int)(threadIdx.x & 31);
     if (row0 >= p.M || col0 >= p.N) return;
 #pragma unroll
-    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * w.scale * f.x * f.y;
+    for (int j = 0; j < NH; ++j) acc[j] = acc[j] * f.x * f.y;
     g16::warp_rows_bulk<NH>(acc, sm, map, row0, col0, p.N - col0);
   }
 };
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kThreads) wgrad8_slices_kernel(const float* __
     }
     float f1;
     const float f0 = e.undo(row, f1);
-    v = v * e.scale * f0 * f1;
+    v = v * f0 * f1;
     e.dW[i] = e.keep != 0.f ? fmaf(e.keep, e.dW[i], v) : v;
   }
 }
