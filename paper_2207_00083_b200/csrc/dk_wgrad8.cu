@@ -28,7 +28,7 @@ using g16::pow2;
 using g16::scale_exp;
 
 constexpr int kThreads = 256;
-constexpr int kMaxParts = 64;            // parts of the rows in which columns are summed
+constexpr int kMaxParts = 148;           // parts of the rows in which columns are summed
 constexpr int kMaxBlocks = 148;          // of wgrad8_columns_kernel that look at the exponents
 
 struct Wg8 {
@@ -38,8 +38,8 @@ struct Wg8 {
   void* x16;                 // [rows][dp]
   void* hi;                  // [rows][op] (dy's terms, or a copy with whole pitch)
   void* lo;
-  float* sums;               // [parts][out]
-  unsigned int* most;        // [parts][out]; then [out] of all
+  float* sums;               // [parts][op]
+  unsigned int* most;        // [parts][op]
   unsigned int* most_all;
   unsigned int* block_exp;   // [blocks]: largest exponent; block_exp[kMaxBlocks]: of all
   float* db;
@@ -48,15 +48,6 @@ struct Wg8 {
   int d, dp, out, op, strips, parts, blocks, copy_dy, with_sums;
   float scale, keep;
 };
-
-// db of a column from its parts' sums
-__device__ __forceinline__ void join_db(const Wg8& a, int c) {
-  float t = 0.f;
-#pragma unroll 8
-  for (int p = 0; p < a.parts; ++p) t += __ldcg(a.sums + (long long)p * a.out + c);
-  t *= a.scale;
-  a.db[c] = a.keep != 0.f ? fmaf(a.keep, a.db[c], t) : t;
-}
 
 // the checkpoint's power of two: its largest step becomes 2^8, so the largest value is below 2^15
 __device__ __forceinline__ int x_exp(unsigned int largest) {
@@ -101,7 +92,7 @@ __device__ __forceinline__ void expand(const Wg8& a, int s, long long i0, long l
 template <int DT, int VEC>
 __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
   chained_launch();
-  constexpr int FULL = DT == DK_F32 ? 4 : 8, NV = FULL / VEC, U = NV >= 4 ? 2 : 8 / NV;
+  constexpr int FULL = DT == DK_F32 ? 4 : 8, NV = FULL / VEC, U = NV >= 4 ? 4 : 8 / NV;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, columns = a.with_sums ? a.strips * a.parts : 0;
   if ((int)blockIdx.x >= columns) {
     const long long i0 = (long long)(blockIdx.x - columns) * kThreads + threadIdx.x, step = (long long)(gridDim.x - columns) * kThreads;
@@ -179,7 +170,7 @@ __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
     }
   __syncthreads();
   const int i = threadIdx.x, col = strip * 32 * FULL + i;
-  if (i < 32 * FULL && col < a.out) {
+  if (i < 32 * FULL && col < a.op) {       // (zeros behind the row)
     float t = 0.f;
     unsigned int u = 0;
 #pragma unroll
@@ -187,8 +178,8 @@ __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
       t += ss[w][i];
       if (DT == DK_F32) u = max(u, sm[w][i]);
     }
-    __stcg(a.sums + (long long)part * a.out + col, t);
-    if (DT == DK_F32) __stcg(a.most + (long long)part * a.out + col, u);
+    __stcg(a.sums + (long long)part * a.op + col, t);
+    if (DT == DK_F32) __stcg(a.most + (long long)part * a.op + col, u);
   }
   if (DT == DK_BF16 && a.db == nullptr) return;
   __shared__ unsigned int last;
@@ -199,14 +190,40 @@ __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
   if (!last) return;
   __threadfence();
   if (threadIdx.x == 0) a.count[strip] = 0u;
-  if (i >= 32 * FULL || col >= a.out) return;
-  if (a.db != nullptr) join_db(a, col);
-  if constexpr (DT == DK_F32) {
-    unsigned int u = 0;
+  // The last CTA: four columns a thread, the parts shared out to G groups of threads, whose sums are added in order.
+  constexpr int G = kThreads / (8 * FULL);
+  const int q = threadIdx.x % (8 * FULL), g = threadIdx.x / (8 * FULL), c = strip * 32 * FULL + 4 * q;
+  if (c < a.op) {
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll 8
-    for (int p = 0; p < a.parts; ++p) u = max(u, __ldcg(a.most + (long long)p * a.out + col));
-    a.most_all[col] = u;
+    for (int p = g; p < a.parts; p += G) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(a.sums + (long long)p * a.op + c));
+      t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+      if constexpr (DT == DK_F32) {
+        const uint4 w = __ldcg(reinterpret_cast<const uint4*>(a.most + (long long)p * a.op + c));
+        u.x = max(u.x, w.x); u.y = max(u.y, w.y); u.z = max(u.z, w.z); u.w = max(u.w, w.w);
+      }
+    }
+    ss[g][4 * q] = t.x; ss[g][4 * q + 1] = t.y; ss[g][4 * q + 2] = t.z; ss[g][4 * q + 3] = t.w;
+    if constexpr (DT == DK_F32) {
+      sm[g][4 * q] = u.x; sm[g][4 * q + 1] = u.y; sm[g][4 * q + 2] = u.z; sm[g][4 * q + 3] = u.w;
+    }
   }
+  __syncthreads();
+  if (i >= 32 * FULL || col >= a.out) return;
+  float t = 0.f;
+  unsigned int u = 0;
+#pragma unroll
+  for (int k = 0; k < G; ++k) {
+    t += ss[k][i];
+    if (DT == DK_F32) u = max(u, sm[k][i]);
+  }
+  if (a.db != nullptr) {
+    t *= a.scale;
+    a.db[col] = a.keep != 0.f ? fmaf(a.keep, a.db[col], t) : t;
+  }
+  if (DT == DK_F32) a.most_all[col] = u;
 }
 
 // fp32: the operands.  The first CTAs take dy's columns (grid_dy of them: strips of 256 columns by row parts), the others the
@@ -347,21 +364,36 @@ struct EpiWBulk {
   }
 };
 
-// joins the slices of a contraction that was cut
+// Joins the slices of a contraction that was cut: a value a thread; or, of many slices, eight threads a value (S = 8: a small
+// dW has few threads, which would wait for one batch of slices after the other).
+template <int S>
 __global__ void __launch_bounds__(kThreads) wgrad8_slices_kernel(const float* __restrict__ part, int ks, int out, int d,
                                                                  int pitch, const EpiW e) {
   chained_launch();
   const long long n = (long long)out * d, slice = (long long)out * pitch;
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kThreads) {
-    const int row = (int)(i / d), c = (int)(i - (long long)row * d);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ float sm[8][32];
+  for (long long i0 = (long long)blockIdx.x * (kThreads / S); i0 < n; i0 += (long long)gridDim.x * (kThreads / S)) {
+    const long long i = i0 + (S == 1 ? (int)threadIdx.x : lane);
+    const int first = S == 1 ? 0 : warp, row = (int)(min(i, n - 1) / d), c = (int)(min(i, n - 1) - (long long)row * d);
     float v = 0.f;
-    for (int k = 0; k < ks; k += 8) {            // eight loads in flight
+    for (int k = first; k < ks; k += 8 * S) {            // eight loads in flight
       float t[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = __ldg(part + min(k + j, ks - 1) * slice + (long long)row * pitch + c);
+      for (int j = 0; j < 8; ++j) t[j] = __ldg(part + min(k + j * S, ks - 1) * slice + (long long)row * pitch + c);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v += k + j < ks ? t[j] : 0.f;
+      for (int j = 0; j < 8; ++j) v += k + j * S < ks ? t[j] : 0.f;
     }
+    if constexpr (S > 1) {
+      __syncthreads();
+      sm[warp][lane] = v;
+      __syncthreads();
+      if (warp > 0) continue;
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) v += sm[w][lane];
+    }
+    if (i >= n) continue;
     float f1;
     const float f0 = e.undo(row, f1);
     v = v * f0 * f1;
@@ -412,8 +444,8 @@ Plan plan_of(const dk_wgrad8& q) {
   };
   p.off_x = room((size_t)q.rows * p.dp * 2);
   p.off_dy = room(p.copy_dy ? (size_t)q.rows * p.op * (p.f32 ? 4 : 2) : 0);
-  p.off_sums = room((size_t)p.parts * q.out * sizeof(float));
-  p.off_most = room(p.f32 ? (size_t)p.parts * q.out * sizeof(unsigned int) : 0);
+  p.off_sums = room((size_t)p.parts * p.op * sizeof(float));
+  p.off_most = room(p.f32 ? (size_t)p.parts * p.op * sizeof(unsigned int) : 0);
   p.off_all = room(p.f32 ? (size_t)q.out * sizeof(unsigned int) : 0);
   p.off_exp = room(p.f32 ? (kMaxBlocks + 1) * sizeof(unsigned int) : 0);
   p.off_part = room(kPartBytes);
@@ -492,9 +524,12 @@ dk_status run(dk_ctx* ctx, const dk_wgrad8& q, const Plan& pl, Wg8& a, float* dW
     const dk_status s = g16::launch<NP, true, true, 256>(ctx, dy, x, p, g16::EpiPartial{part, pitch}, st);
     if (s != DK_OK) return s;
     count_launches(ctx, DK_KERNEL_OTHER, 1);
+    const bool many = t.ksplit >= 16;
     long long grid = ((long long)q.out * q.d + kThreads - 1) / kThreads;
+    if (many) grid = ((long long)q.out * q.d + 31) / 32;
     if (grid > 8LL * sms) grid = 8LL * sms;
-    DK_CUDA_CHECK(launch_chained(wgrad8_slices_kernel, dim3((unsigned)grid), kThreads, 0, st, part, t.ksplit, q.out, q.d, pitch, e));
+    DK_CUDA_CHECK(launch_chained(many ? wgrad8_slices_kernel<8> : wgrad8_slices_kernel<1>, dim3((unsigned)grid), kThreads, 0, st,
+                                 part, t.ksplit, q.out, q.d, pitch, e));
     return DK_OK;
   }
   p.tail_part = reinterpret_cast<float*>(ws + pl.off_part);
