@@ -612,23 +612,6 @@ struct Team {
     b = r.y;
   }
 
-  // the low words of eight, shifted down by `off` bytes (even; fp32: a multiple of four)
-  static __device__ __forceinline__ uint4 shifted(const uint4& x, const uint4& y, int off) {
-    uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-    if (off & 8) {
-#pragma unroll
-      for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-    }
-    if (off & 4) {
-#pragma unroll
-      for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-    }
-    if (DT == DK_BF16 && (off & 2)) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
   // values of a row in a stage, `off` bytes behind `row` (zero where there are none)
   __device__ __forceinline__ void take(const char* row, int off, bool valid, Pairs& v) const {
     float x[N];
@@ -638,7 +621,7 @@ struct Team {
       if ((WAY == FULL || valid) && live(j)) {
         if constexpr (WAY == RAGGED) {
           const uint4* at = reinterpret_cast<const uint4*>(row + column(j) * ES);
-          r = shifted(at[0], at[1], off);
+          r = shifted<DT>(at[0], at[1], off);
         } else {
           r = Vec<DT, VEC>::get(row + off, column(j));
         }
@@ -673,7 +656,7 @@ struct Team {
       char* const to = static_cast<char*>(base) + (at - off);
       for (int q = lane; q < n; q += tl) {
         const uint4* from = reinterpret_cast<const uint4*>(out) + q;
-        const uint4 w = off == 0 ? from[0] : shifted(from[-1], from[0], 16 - off);
+        const uint4 w = off == 0 ? from[0] : shifted<DT>(from[-1], from[0], 16 - off);
         const int lo = q == 0 ? off : 0, hi = min(16, off + bytes - q * 16);
         if (lo == 0 && hi == 16) {
           *reinterpret_cast<uint4*>(to + q * 16) = w;

@@ -2,7 +2,10 @@
 //
 // Bound by HBM.  A thread takes one vector of 16 bytes of the tensor (4 fp32 or 8 bf16 values) at a time, of which U are in
 // flight; the 8 or 4 neighbouring lanes of a block of 32 values exchange their largest magnitude.  Rows whose length is no
-// multiple of the vector are read by single elements.  64*224*224 x 64 bf16, stored and brought back: 184 us for 1.25 GB, 6.8
+// multiple of the vector start anywhere, and are read by single elements (as two aligned vectors, shifted: 40000 x 1693 bf16
+// 64 us, by elements 59; 28286 x 1693 fp32 66 and 45).  bf16 rows are written in aligned vectors, their codes being shifted
+// instead (40000 x 1693: 55 us, by elements 189), fp32 rows by elements (28286 x 1693: 57 us, in vectors 51; but 3000000 x
+// 33, where every eighth vector has a row's end in it: 130 and 239).  64*224*224 x 64 bf16, stored and brought back: 184 us for 1.25 GB, 6.8
 // TB/s, what a copy does; 196 x 512 fp32: 8.6 us for the two launches.
 #include "dk_ckpt8.cuh"
 #include "dk_internal.h"
@@ -19,14 +22,16 @@ struct Args {
   void* y;                   // load: the tensor
   uint8_t* codes;
   uint8_t* exps;
-  long long units;           // vectors of all padded rows
-  unsigned long long recip;  // 2^64/per rounded up: i/per is its high product with i (exact for i < 2^50)
+  long long units;           // vectors of all padded rows; load, SHIFTED: of the tensor
+  long long elements;
+  unsigned long long recip;  // 2^64/per rounded up: i/per is its high product with i (exact for i*per < 2^64)
   int d, per;                // per: vectors of a padded row
   int dp;
 };
 
-// How rows lie: whole vectors and whole blocks (one flat array), whole vectors, or neither.
-enum { FLAT = 0, WHOLE = 1, RAGGED = 2 };
+// How rows lie: whole vectors and whole blocks (one flat array), whole vectors, or neither.  SHIFTED: neither, and bf16 to be
+// written.
+enum { FLAT = 0, WHOLE = 1, RAGGED = 2, SHIFTED = 3 };
 
 // vector i of the padded rows, as stored (zero behind the row)
 template <int DT, int VEC, int WAY>
@@ -79,33 +84,78 @@ __global__ void __launch_bounds__(kThreads) ckpt8_load_kernel(const Args a) {
   constexpr int VEC = DT == DK_F32 ? 4 : 8;
   chained_launch();
   const long long i0 = (long long)blockIdx.x * (kThreads * U) + threadIdx.x;
-  ckpt8::Raw<VEC> r[U];
+  if constexpr (WAY != SHIFTED) {
+    ckpt8::Raw<VEC> r[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const long long i = i0 + u * kThreads;
-    if (i < a.units) r[u] = ckpt8::get<VEC>(a.codes + i * VEC, a.exps + i * VEC / ckpt8::kBlock);
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const long long i = i0 + u * kThreads;
-    if (i >= a.units) continue;
-    float v[VEC];
-    ckpt8::unpack<VEC>(r[u], v);
-    if constexpr (WAY == FLAT) {
-      Vec<DT, VEC>::store(a.y, i * VEC, v);
-      continue;
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * kThreads;
+      if (i < a.units) r[u] = ckpt8::get<VEC>(a.codes + i * VEC, a.exps + i * VEC / ckpt8::kBlock);
     }
-    const long long row = __umul64hi((unsigned long long)i, a.recip);
-    const int c = (int)(i - row * a.per) * VEC;
-    if constexpr (WAY == WHOLE) {
-      if (c < a.d) Vec<DT, VEC>::store(a.y, row * a.d + c, v);
-    } else {
 #pragma unroll
-      for (int k = 0; k < VEC; ++k)
-        if (c + k < a.d) {
-          const float t[1] = {v[k]};
-          Vec<DT, 1>::store(a.y, row * a.d + c + k, t);
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * kThreads;
+      if (i >= a.units) continue;
+      float v[VEC];
+      ckpt8::unpack<VEC>(r[u], v);
+      if constexpr (WAY == FLAT) {
+        Vec<DT, VEC>::store(a.y, i * VEC, v);
+        continue;
+      }
+      const long long row = __umul64hi((unsigned long long)i, a.recip);
+      const int c = (int)(i - row * a.per) * VEC;
+      if constexpr (WAY == WHOLE) {
+        if (c < a.d) Vec<DT, VEC>::store(a.y, row * a.d + c, v);
+      } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+          if (c + k < a.d) {
+            const float t[1] = {v[k]};
+            Vec<DT, 1>::store(a.y, row * a.d + c + k, t);
+          }
+      }
+    }
+  } else {
+    // A vector of the tensor: codes from c on, of one row; at a row's end and the tensor's, by single elements.
+    constexpr int W = VEC / 4 + 1;
+    uint32_t w[U][W], b0[U], b1[U];
+    long long row[U];
+    int c[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * kThreads;
+      row[u] = a.d == 1 ? i * VEC : __umul64hi((unsigned long long)i * VEC, a.recip);
+      c[u] = (int)(i * VEC - row[u] * a.d);
+      if (i >= a.units || c[u] + VEC > a.d) continue;
+      const uint32_t* from = reinterpret_cast<const uint32_t*>(a.codes + row[u] * a.dp + (c[u] & ~3));
+      const uint8_t* exps = a.exps + row[u] * (a.dp / ckpt8::kBlock);
+#pragma unroll
+      for (int k = 0; k < W; ++k) w[u][k] = k < W - 1 || (c[u] & 3) ? __ldg(from + k) : 0u;
+      b0[u] = __ldg(exps + c[u] / ckpt8::kBlock);
+      b1[u] = __ldg(exps + (c[u] + VEC - 1) / ckpt8::kBlock);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long i = i0 + u * kThreads;
+      if (i >= a.units) continue;
+      float v[VEC];
+      if (c[u] + VEC <= a.d) {
+        ckpt8::Raw<VEC> r;
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k) r.w[k] = __funnelshift_r(w[u][k], w[u][k + 1], 8 * (c[u] & 3));
+        const int left = ckpt8::kBlock - c[u] % ckpt8::kBlock;      // values of the first block
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+          v[k] = (ckpt8::biased<VEC>(r, k) - ckpt8::kBias) * ckpt8::step_of(k < left ? b0[u] : b1[u]);
+        Vec<DT, VEC>::store(a.y, i * VEC, v);
+      } else {
+        long long at = row[u];
+        for (int k = 0, col = c[u]; k < VEC && i * VEC + k < a.elements; ++k, ++col) {
+          if (col == a.d) { ++at; col = 0; }
+          float t[1];
+          ckpt8::unpack<1>(ckpt8::get<1>(a.codes + at * a.dp + col, a.exps + at * (a.dp / ckpt8::kBlock) + col / ckpt8::kBlock), t);
+          Vec<DT, 1>::store(a.y, i * VEC + k, t);
         }
+      }
     }
   }
 }
@@ -120,10 +170,11 @@ dk_status check(const dk_ckpt8* q) {
 
 template <int DT, int WAY>
 cudaError_t launch_one(const Args& a, bool store, bool many, cudaStream_t st) {
+  constexpr int LOAD = DT == DK_BF16 && WAY == RAGGED ? SHIFTED : WAY;
   const int u = many ? 4 : 1;
   const dim3 grid((unsigned)((a.units + kThreads * u - 1) / (kThreads * u)));
   auto kern = store ? (many ? ckpt8_store_kernel<DT, WAY, 4> : ckpt8_store_kernel<DT, WAY, 1>)
-                    : (many ? ckpt8_load_kernel<DT, WAY, 4> : ckpt8_load_kernel<DT, WAY, 1>);
+                    : (many ? ckpt8_load_kernel<DT, LOAD, 4> : ckpt8_load_kernel<DT, LOAD, 1>);
   return launch_chained(kern, grid, kThreads, 0, st, a);
 }
 template <int DT>
@@ -146,7 +197,13 @@ dk_status launch_ckpt8(const dk_ckpt8& q, bool store, const void* x, void* y, vo
   a.dp = ckpt8::padded(q.d);
   a.per = a.dp / vec;
   a.units = q.rows * a.per;
-  a.recip = ~0ull / (unsigned)a.per + 1;
+  a.elements = q.rows * q.d;
+  int by = a.per;
+  if (!store && q.dtype == DK_BF16 && q.d % vec != 0) {           // (SHIFTED)
+    a.units = (a.elements + vec - 1) / vec;
+    by = q.d;
+  }
+  a.recip = ~0ull / (unsigned)by + 1;          // (0 for 1)
   // four vectors a thread where that leaves every SM its threads, one for the sake of latency otherwise
   const bool many = a.units >= 4LL * 2048 * sms;
   const cudaError_t e = q.dtype == DK_F32 ? launch_way<DK_F32>(a, store, many, st) : launch_way<DK_BF16>(a, store, many, st);

@@ -249,6 +249,31 @@ __device__ __forceinline__ bool last_to_arrive(const NormParams& p, long long s)
   return last != 0u;
 }
 
+// Sums over the slabs b = r, r + R, ... of NC columns (every kThreads-th from i on) of [slabs][C2], in the slabs' order; U
+// slabs' loads are in flight (one CTA reads them all, so it waits for L2 rather than for its bandwidth).
+template <int U, int NC>
+__device__ __forceinline__ void join_slabs(const float* part, int slabs, int C2, int r, int R, int i, float* to) {
+  float t[NC];
+#pragma unroll
+  for (int k = 0; k < NC; ++k) t[k] = 0.f;
+  for (int b = r; b < slabs; b += U * R) {
+    float v[U][NC];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+        if (b + u * R < slabs && i + k * kThreads < C2) v[u][k] = __ldcg(part + (long long)(b + u * R) * C2 + i + k * kThreads);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+        if (b + u * R < slabs && i + k * kThreads < C2) t[k] += v[u][k];
+  }
+#pragma unroll
+  for (int k = 0; k < NC; ++k)
+    if (i + k * kThreads < C2) to[i + k * kThreads] = t[k];
+}
+
 // Sums of one slab.  Dynamic shared memory: forward [TY][c/VEC][3], backward [TY][c][2] floats.
 template <int DT, int VEC, int ACT, bool FWD, bool K8>
 __global__ void __launch_bounds__(kThreads) norm_sums_kernel(const NormParams p) {
@@ -318,14 +343,12 @@ __global__ void __launch_bounds__(kThreads) norm_sums_kernel(const NormParams p)
     if (!last_to_arrive(p, s)) return;
     // the sample's sums per channel: the slabs are dealt to R rows of threads, whose sums are joined in order
     const int C2 = 2 * p.c, R = C2 < kThreads ? kThreads / C2 : 1;
-    for (int i0 = 0; i0 < C2; i0 += kThreads) {
-      const int r = C2 < kThreads ? (int)threadIdx.x / C2 : 0, i = i0 + (C2 < kThreads ? (int)threadIdx.x % C2 : (int)threadIdx.x);
-      if (r < R && i < C2) {
-        float t = 0.f;
-#pragma unroll 8
-        for (int b = r; b < p.slabs; b += R) t += __ldcg(p.part + (s * p.slabs + b) * C2 + i);
-        sm[r * C2 + i] = t;
-      }
+    const float* part = p.part + s * p.slabs * C2;
+    if (C2 < kThreads) {
+      const int r = (int)threadIdx.x / C2;
+      if (r < R) join_slabs<8, 1>(part, p.slabs, C2, r, R, (int)threadIdx.x % C2, sm + r * C2);
+    } else {
+      for (int i0 = 0; i0 < C2; i0 += 2 * kThreads) join_slabs<8, 2>(part, p.slabs, C2, 0, 1, i0 + (int)threadIdx.x, sm);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < C2; i += kThreads) {

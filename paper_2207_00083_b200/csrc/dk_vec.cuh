@@ -65,6 +65,26 @@ struct Vec {
   static __device__ __forceinline__ void store(void* base, long long e, const float (&v)[VEC]) { put(base, e, pack(v)); }
 };
 
+// The low words of eight, shifted down by `off` bytes, 0 to 14 (even; fp32: a multiple of four): a vector that starts `off`
+// bytes behind an aligned one.
+template <int DT>
+__device__ __forceinline__ uint4 shifted(const uint4& x, const uint4& y, int off) {
+  uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  if (off & 8) {
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  }
+  if (off & 4) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  }
+  if (DT == DK_BF16 && (off & 2)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // (count, mean, sum of squared deviations) of the union of two sets
 struct Moments {
   float n, mean, m2;
