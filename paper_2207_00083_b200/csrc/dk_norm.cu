@@ -85,8 +85,7 @@ struct XVectors<DT, VEC, false> {
   const void* x;
   long long base;
   int c;
-  __device__ __forceinline__ XVectors(const NormParams& p, long long s, int ch)
-      : x(p.x), base(s * p.pix * (long long)p.c + ch), c(p.c) {}
+  __device__ __forceinline__ XVectors(const NormParams& p, long long, int, long long at) : x(p.x), base(at), c(p.c) {}
   __device__ __forceinline__ Raw get(int i) const { return Vec<DT, VEC>::get(x, base + (long long)i * c); }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[VEC]) { Vec<DT, VEC>::unpack(r, v); }
 };
@@ -96,7 +95,7 @@ struct XVectors<DT, VEC, true> {
   const uint8_t* codes;
   const uint8_t* exps;
   int dp;
-  __device__ __forceinline__ XVectors(const NormParams& p, long long s, int ch)
+  __device__ __forceinline__ XVectors(const NormParams& p, long long s, int ch, long long)
       : codes(p.codes + s * p.pix * (long long)p.dp + ch),
         exps(p.exps + s * p.pix * (long long)(p.dp / ckpt8::kBlock) + ch / ckpt8::kBlock), dp(p.dp) {}
   __device__ __forceinline__ Raw get(int i) const {
@@ -301,7 +300,7 @@ __global__ void __launch_bounds__(kThreads) norm_sums_kernel(const NormParams p)
           ga[k] = __ldg(p.gamma + v * VEC + k); be[k] = __ldg(p.beta + v * VEC + k);
           sb[k] = sg[k] = 0.f;
         }
-        sum_gradients<DT, VEC, ACT, K8>(XVectors<DT, VEC, K8>(p, s, v * VEC), p.dy, base + v * VEC, p0 + ty, p1, p.c, p.TY, mean, rstd, ga, be, sb, sg);
+        sum_gradients<DT, VEC, ACT, K8>(XVectors<DT, VEC, K8>(p, s, v * VEC, base + v * VEC), p.dy, base + v * VEC, p0 + ty, p1, p.c, p.TY, mean, rstd, ga, be, sb, sg);
         float* e = sm + 2 * ((size_t)ty * p.c + v * VEC);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { e[2 * k] = sb[k]; e[2 * k + 1] = sg[k]; }
@@ -432,7 +431,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const NormParams p
       mean[k] = st.x; rstd[k] = st.y; m0[k] = ms.x; m1[k] = ms.y;
       ga[k] = __ldg(p.gamma + v * VEC + k); be[k] = __ldg(p.beta + v * VEC + k);
     }
-    write_values<DT, VEC, ACT, FWD, K8, KEEP>(XVectors<DT, VEC, K8>(p, s, v * VEC), p.dy, p.out, base + v * VEC, p0 + ty, p1, p.c,
+    write_values<DT, VEC, ACT, FWD, K8, KEEP>(XVectors<DT, VEC, K8>(p, s, v * VEC, base + v * VEC), p.dy, p.out, base + v * VEC, p0 + ty, p1, p.c,
                                               p.TY, mean, rstd, m0, m1, ga, be, kept_codes(p, s, v * VEC),
                                               kept_exps(p, s, v * VEC), p.dp);
   }
@@ -477,7 +476,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) norm_sample_kernel(const No
         float mean[VEC], rstd[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { mean[k] = given.x; rstd[k] = given.y; }
-        sum_gradients<DT, VEC, ACT, K8>(XVectors<DT, VEC, K8>(p, s, ch0), p.dy, base, ty, p.pix, p.c, p.TY, mean, rstd, ga, be, sb, sg);
+        sum_gradients<DT, VEC, ACT, K8>(XVectors<DT, VEC, K8>(p, s, ch0, base), p.dy, base, ty, p.pix, p.c, p.TY, mean, rstd, ga, be, sb, sg);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
           cb[k] += sb[k]; cg[k] += sg[k];
@@ -519,7 +518,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) norm_sample_kernel(const No
         mean[k] = FWD ? t0 : given.x; rstd[k] = FWD ? t1 : given.y;
         m0[k] = t0; m1[k] = t1;
       }
-      write_values<DT, VEC, ACT, FWD, K8, KEEP>(XVectors<DT, VEC, K8>(p, s, ch0), p.dy, p.out, base, ty, p.pix, p.c, p.TY, mean,
+      write_values<DT, VEC, ACT, FWD, K8, KEEP>(XVectors<DT, VEC, K8>(p, s, ch0, base), p.dy, p.out, base, ty, p.pix, p.c, p.TY, mean,
                                                 rstd, m0, m1, ga, be, kept_codes(p, s, ch0), kept_exps(p, s, ch0), p.dp);
     }
     // (the next sample's sums go to `sm`, which was read before the second barrier; `st` is written after another one)
