@@ -12,7 +12,6 @@ import torch
 import kept
 from paper_2207_00083_b200 import binding as dk
 from test_gpu_ckpt8 import draw, stored, wgrad_bound
-from test_gpu_step_launches import check as count_launches
 
 pytestmark = pytest.mark.gpu
 TYPES = {dk.DK_F32: torch.float32, dk.DK_BF16: torch.bfloat16}
@@ -240,6 +239,25 @@ def test_guard_behind_the_workspace(q):
     ctx.close()
 
 
+def count_launches(ctx, call):
+    """dk_profile_read counts every kernel that a call launches: as many as the call leaves in a captured graph."""
+    call()
+    torch.cuda.synchronize()
+    dk.dk_profile_reset(ctx)
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    cuda, of, n = ctypes.CDLL("libcuda.so.1"), ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t()
+    assert cuda.cuGraphGetNodes(of, None, ctypes.byref(n)) == 0 and n.value > 0
+    nodes, kind = (ctypes.c_void_p * n.value)(), ctypes.c_int()
+    assert cuda.cuGraphGetNodes(of, nodes, ctypes.byref(n)) == 0
+    kernels = 0
+    for node in nodes:
+        assert cuda.cuGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0
+        kernels += kind.value == 0                              # CU_GRAPH_NODE_TYPE_KERNEL
+    assert kernels and dk.dk_profile_read(ctx)["other"][2] == kernels
+
+
 # small tiles, pair tiles with and without a cut last wave, slices joined by a kernel of their own
 WGRADS = [(64, 512, 1000), (4000, 2560, 2560), (300, 2600, 4100), (33000, 40, 24), (2000, 1000, 3001)]
 
@@ -259,20 +277,20 @@ def test_launches_of_the_others_are_counted(ctx):
     ctx.ensure_workspace(q)
     h, u, gate, vec = draw(100, 60, torch.float32), draw(100, 60, torch.float32), torch.ones((15, 60), device="cuda"), torch.ones(60, device="cuda")
     kh, ku, st = stored(ctx, h), stored(ctx, u), torch.empty((100, 4), device="cuda")
-    a, b = torch.empty_like(h), torch.empty_like(h)
+    a, b, dgate, dpost, dpre = (torch.empty_like(t) for t in (h, h, gate, vec, vec))
     count_launches(ctx, lambda: dk.dk_ckpt8_store(ctx, k, h, kh))
     count_launches(ctx, lambda: dk.dk_ckpt8_load(ctx, k, kh, a))
     count_launches(ctx, lambda: dk.dk_block_norm_fwd(ctx, q, h, u, gate, vec, vec, None, a, b, st, kh, ku))
-    count_launches(ctx, lambda: dk.dk_block_norm_bwd_ckpt8(ctx, q, h, u, kh, ku, gate, vec, vec, st, a, b, gate.clone(), vec.clone(),
-                                                           vec.clone(), None))
+    count_launches(ctx, lambda: dk.dk_block_norm_bwd_ckpt8(ctx, q, h, u, kh, ku, gate, vec, vec, st, a, b, dgate, dpost, dpre,
+                                                           None))
     for c, groups in ((64, 8), (60, 5)):                        # (the checkpoint with the values, and by itself)
         for n, hw in ((3, 5), (4, 200)):
             x, g = draw(n * hw * hw, c, torch.float32), torch.ones(c, device="cuda")
             qn, ck = dk.dk_norm(n, hw, hw, c, groups, 2, dk.DK_F32, 1e-5), stored(ctx, x)
             ctx.ensure_workspace(qn)
-            y, s = torch.empty_like(x), torch.empty((n, groups, 2), device="cuda")
+            y, s, dg, db = torch.empty_like(x), torch.empty((n, groups, 2), device="cuda"), torch.empty_like(g), torch.empty_like(g)
             count_launches(ctx, lambda: dk.dk_group_norm_fwd_ckpt8(ctx, qn, x, g, g, y, s, ck))
-            count_launches(ctx, lambda: dk.dk_group_norm_bwd_ckpt8(ctx, qn, x, ck, g, g, s, y, g.clone(), g.clone()))
+            count_launches(ctx, lambda: dk.dk_group_norm_bwd_ckpt8(ctx, qn, x, ck, g, g, s, y, dg, db))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
