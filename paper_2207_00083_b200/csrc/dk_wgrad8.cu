@@ -9,9 +9,9 @@
 //     largest exponent
 //   wgrad8_prep_kernel: fp32: the operands
 //   the product (dk_gemm16.cuh), both operands read across their rows in place
-// Large products are bound by the tensor cores (16384 rows, 4096 x 4096 bf16: 445 us, of which 31 in the first launch; 1.24
-// PFLOP/s), products of few rows by the writing of dW (256 rows, 25088 x 4096 fp32: 126 us for 411 MB, floor 64), small ones
-// by the chain of launches (64 rows, 512 x 1000 fp32: 14 us).
+// Large products are bound by the tensor cores (16384 rows, 4096 x 4096 bf16: 434 us, 1.27 PFLOP/s, and 456
+// with db, for which dy is read once more), products of few rows by the writing of dW (256 rows, 25088 x 4096 fp32: 126 us for 411 MB, floor 64), small ones
+// by the chain of launches (64 rows, 512 x 1000 fp32: 13 us).
 #include <math.h>
 
 #include "dk_ckpt8.cuh"
