@@ -460,7 +460,7 @@ def exact(case, seed):
 
     for a in range(0, t, 4096):
         at = slice(a, min(a + 4096, t))
-        row = torch.arange(at.start, at.stop, device="cuda") // (per if gates else t)
+        row = torch.arange(at.start, at.stop, device="cuda") // per
         gate = s["gate"].to(f64)[row] if gates else torch.ones((at.stop - at.start, 1), dtype=f64, device="cuda")
         h, u = s["h"][at].to(f64), s["u"][at].to(f64)
         mu, ru = moments(u)
