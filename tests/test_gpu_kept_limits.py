@@ -1,0 +1,45 @@
+"""Checkpoints and the weight gradient from one where they can go wrong at the edges: tiles that end anywhere, columns of very
+many rows, infinities, the ends of the 8-bit form's range."""
+import pytest
+import torch
+
+import kept
+from paper_2207_00083_b200 import binding as dk
+from test_gpu_ckpt8 import draw, stored, wgrad_bound
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": (dk.DK_F32, torch.float32), "bf16": (dk.DK_BF16, torch.bfloat16)}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = dk.Context(0)
+    yield c
+    assert dk.dk_device_status(c) == 0
+    c.close()
+
+
+# Tiles of 256 x 256 stored by TMA, more of them than CTA pairs (so a warp has several), of few stages each (so stores queue
+# up), with 1 to 32 or 65 to 96 columns left of a warp's 128 at the right edge: one or three pieces of 32, by the side of
+# tiles that have none left, two or four.
+EDGES = [(256, 4128, 4096), (64, 4176, 5000), (256, 1056, 8192), (256, 4192, 11008), (2048, 96, 66000), (64, 2084, 9000),
+         (100, 1124, 8192), (1000, 8352, 2304)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d,out", EDGES)
+def test_wgrad_tiles_at_the_edge(ctx, rows, d, out, dtype):
+    """Every value, and the same bits in every one of many calls without a pause between them: no tile takes the place of
+    another on its way out."""
+    code, dt = TYPES[dtype]
+    x, dy = stored(ctx, draw(rows, d, dt, spread=0.5)), draw(rows, out, dt, seed=5, spread=0.5)
+    q = dk.dk_wgrad8(rows, d, out, code)
+    ctx.ensure_workspace(q)
+    results = [torch.full((out, d), float("nan"), device="cuda") for _ in range(6)]
+    for dW in results:
+        dk.dk_linear_bwd_wgrad_ckpt8(ctx, q, dy, x, 1.0, 0.0, dW, None)
+    xv, dyv = kept.decode(x, rows, d), dy.double()
+    err = (results[0].double() - dyv.t() @ xv).abs_()
+    assert bool((err <= wgrad_bound(dyv, xv, dtype)).all())
+    for dW in results[1:]:
+        assert torch.equal(dW, results[0])
