@@ -28,7 +28,8 @@ using g16::pow2;
 using g16::scale_exp;
 
 constexpr int kThreads = 256;
-constexpr int kMaxParts = 148;           // parts of the rows in which columns are summed
+constexpr int kMaxParts = 148;           // parts of the rows in which columns are summed, but of
+constexpr long long kPartRows = 1 << 15; // rows at most each
 constexpr int kMaxBlocks = 148;          // of wgrad8_columns_kernel that look at the exponents
 
 struct Wg8 {
@@ -88,9 +89,10 @@ __device__ __forceinline__ void expand(const Wg8& a, int s, long long i0, long l
 // Columns of dy: their sums and (fp32) largest magnitudes, over parts of the rows; a CTA has a strip of 32 vectors of 16
 // bytes.  bf16: rows of no whole vectors are copied to a pitch of such; and the
 // CTAs behind those of dy expand the checkpoint, so nothing else comes before the product.  fp32: they look for the
-// checkpoint's largest exponent.  The last CTA of a strip to be done joins its parts.
+// checkpoint's largest exponent.  The last CTA of a strip to be done joins its parts.  (bf16: three CTAs an SM, for the sake of
+// what expands the checkpoint: 1000 rows, 8192 by 1024 without db 29 us, with two 30.)
 template <int DT, int VEC>
-__global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
+__global__ void __launch_bounds__(kThreads, DT == DK_BF16 ? 3 : 2) wgrad8_columns_kernel(const Wg8 a) {
   chained_launch();
   constexpr int FULL = DT == DK_F32 ? 4 : 8, NV = FULL / VEC, U = NV >= 4 ? 4 : 8 / NV;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, columns = a.with_sums ? a.strips * a.parts : 0;
@@ -126,13 +128,32 @@ __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
   const int strip = blockIdx.x % a.strips, part = blockIdx.x / a.strips, c0 = strip * 32 * FULL + lane * VEC;
   const long long per = (a.rows + a.parts - 1) / a.parts;
   const long long r0 = part * per, r1 = min(a.rows, r0 + per);
+  // A thread's sums: of kFold rows at a time, then, in shared memory, of those.  (A wide dy has few parts, one from 37889 bf16
+  // or 18945 fp32 outputs on: all of a thread's rows one after the other would lose what is small beside the sum so far.)
+  constexpr int kFold = 64;
+  __shared__ float ss[8][32 * FULL + 1];
+  __shared__ unsigned int sm[DT == DK_F32 ? 8 : 1][32 * FULL + 1];
+  float* const mine = ss[warp] + lane * VEC;
   float s[NV][VEC];
   unsigned int m[NV][VEC];
+  int ahead = 0;                     // rows in s
+  bool folded = false;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int k = 0; k < VEC; ++k) { s[j][k] = 0.f; m[j][k] = 0u; }
   for (long long r = r0 + warp; r < r1; r += 8 * U) {
+    if ((ahead += U) > kFold) {
+      ahead = U;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          mine[j * 32 * VEC + k] = folded ? mine[j * 32 * VEC + k] + s[j][k] : s[j][k];
+          s[j][k] = 0.f;
+        }
+      folded = true;
+    }
     typename Vec<DT, VEC>::Raw raw[U][NV];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -159,13 +180,11 @@ __global__ void __launch_bounds__(kThreads) wgrad8_columns_kernel(const Wg8 a) {
         if (DT == DK_BF16 && a.copy_dy) Vec<DT, VEC>::put(a.hi, (r + 8 * u) * a.op + c, raw[u][j]);
       }
   }
-  __shared__ float ss[8][32 * FULL + 1];
-  __shared__ unsigned int sm[DT == DK_F32 ? 8 : 1][32 * FULL + 1];
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-      ss[warp][j * 32 * VEC + lane * VEC + k] = s[j][k];
+      mine[j * 32 * VEC + k] = folded ? mine[j * 32 * VEC + k] + s[j][k] : s[j][k];
       if (DT == DK_F32) sm[warp][j * 32 * VEC + lane * VEC + k] = m[j][k];
     }
   __syncthreads();
@@ -431,10 +450,12 @@ Plan plan_of(const dk_wgrad8& q) {
   p.copy_dy = p.f32 || q.out % 8 != 0;
   const int wide = 32 * (p.f32 ? 4 : 8);
   p.strips = (p.op + wide - 1) / wide;
-  // parts of the rows: two CTAs for every SM, 32 rows each at least
+  // parts of the rows: two CTAs for every SM, 32 rows each at least; and kPartRows at most, so that no sum is of more than 64
+  // of a thread's rows, 64 of those, 8 warps, and an eighth (bf16: a fourth) of the parts, 512 at most
   long long parts = 2 * 148 / p.strips;
   if (parts > kMaxParts) parts = kMaxParts;
   if (parts > (q.rows + 31) / 32) parts = (q.rows + 31) / 32;
+  if (parts < (q.rows + kPartRows - 1) / kPartRows) parts = (q.rows + kPartRows - 1) / kPartRows;
   p.parts = parts < 1 ? 1 : (int)parts;
   size_t off = 0;
   auto room = [&off](size_t bytes) {

@@ -43,3 +43,22 @@ def test_wgrad_tiles_at_the_edge(ctx, rows, d, out, dtype):
     assert bool((err <= wgrad_bound(dyv, xv, dtype)).all())
     for dW in results[1:]:
         assert torch.equal(dW, results[0])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,out,parts", [(20000, 38400, 1), (5000000, 16, 153)])
+def test_columns_of_many_rows(ctx, rows, out, parts, dtype):
+    """db of a wide layer, whose columns are summed in one part of the rows, and of more rows than the usual parts take: a large
+    value before many small ones.  A thread has every eighth of a part's rows and sums 64 at a time, then those sums; then
+    come eight warps, the parts by eight groups of threads at most and those: so many roundings of 2^-24, and scale's."""
+    code, dt = TYPES[dtype]
+    d = 32
+    x, dy = stored(ctx, draw(rows, d, dt, spread=0.5)), torch.ones((rows, out), dtype=dt, device="cuda")
+    dy[0], dy[5, ::2] = 2.0 ** 25, -(2.0 ** 25)
+    q = dk.dk_wgrad8(rows, d, out, code)
+    ctx.ensure_workspace(q)
+    dW, db = torch.empty((out, d), device="cuda"), torch.full((out,), float("nan"), device="cuda")
+    dk.dk_linear_bwd_wgrad_ckpt8(ctx, q, dy, x, 0.75, 0.0, dW, db)
+    depth = 64 + -(-rows // parts) / 8 / 64 + 8 + parts / 4 + 8
+    want, size = (f(dy).sum(dim=0, dtype=torch.float64) * 0.75 for f in (lambda t: t, torch.abs))
+    assert bool(((db.double() - want).abs() <= size * (depth + 2) * 2.0 ** -24).all())
