@@ -677,8 +677,13 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 t = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
 }
+// what the first of two terms leaves of a value; INF: nothing of an infinity, whose products then have the first term's
+template <bool INF>
+__device__ __forceinline__ float left_over(float v, float first) {
+  return INF && fabsf(first) == __int_as_float(0x7f800000) ? 0.f : v - first;
+}
 // two fp16 terms of v[j]
-template <int NV>
+template <int NV, bool INF = false>
 __device__ __forceinline__ void store_planes(__half* hi, __half* lo, const float (&v)[NV], int count) {
   // (pitches are multiples of 8 and padding columns may be written: they are zero, as the operands' are)
 #pragma unroll
@@ -690,7 +695,7 @@ __device__ __forceinline__ void store_planes(__half* hi, __half* lo, const float
         const float a = v[j + 2 * q], b = v[j + 2 * q + 1];
         const __half2 t = __floats2half2_rn(a, b);
         h[q] = *reinterpret_cast<const uint32_t*>(&t);
-        l[q] = pack_f16(a - __low2float(t), b - __high2float(t));
+        l[q] = pack_f16(left_over<INF>(a, __low2float(t)), left_over<INF>(b, __high2float(t)));
       }
       *reinterpret_cast<uint4*>(hi + j) = make_uint4(h[0], h[1], h[2], h[3]);
       *reinterpret_cast<uint4*>(lo + j) = make_uint4(l[0], l[1], l[2], l[3]);

@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, DT == DK_BF16 ? 3 : 2) wgrad8_column
   if (DT == DK_F32) a.most_all[col] = u;
 }
 
-// fp32: the operands.  The first CTAs take dy's columns (grid_dy of them: strips of 256 columns by row parts), the others the
+// fp32: the operands (an infinity in dy is one term, so dW has infinities where the formula has).  The first CTAs take dy's columns (grid_dy of them: strips of 256 columns by row parts), the others the
 // checkpoint.
 __global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int strips, int row_parts, int grid_dy) {
   chained_launch();
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int 
           const float v[8] = {x[u].x * f[0], x[u].y * f[1], x[u].z * f[2], x[u].w * f[3],
                               y[u].x * f[4], y[u].y * f[5], y[u].z * f[6], y[u].w * f[7]};
           const long long at = (r + u * step) * a.op + c;
-          g16::store_planes<8>(hi + at, lo + at, v, 8);
+          g16::store_planes<8, true>(hi + at, lo + at, v, 8);
         }
       }
     } else {
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kThreads) wgrad8_prep_kernel(const Wg8 a, int 
             const __half h = __float2half_rn(w);
             const long long at = (r + u * step) * a.op + c + 32 * k;
             hi[at] = h;
-            lo[at] = __float2half_rn(w - __half2float(h));
+            lo[at] = __float2half_rn(g16::left_over<true>(w, __half2float(h)));
           }
       }
     }

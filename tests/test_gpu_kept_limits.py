@@ -62,3 +62,24 @@ def test_columns_of_many_rows(ctx, rows, out, parts, dtype):
     depth = 64 + -(-rows // parts) / 8 / 64 + 8 + parts / 4 + 8
     want, size = (f(dy).sum(dim=0, dtype=torch.float64) * 0.75 for f in (lambda t: t, torch.abs))
     assert bool(((db.double() - want).abs() <= size * (depth + 2) * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d,out", [(100, 96, 40), (100, 96, 41), (256, 1056, 8192), (33000, 40, 24)])
+def test_wgrad_infinities_as_in_the_formula(ctx, rows, d, out, dtype):
+    """An infinity in dy times x: infinities of the products' signs, NaN where x is zero or two of them meet; so in db."""
+    code, dt = TYPES[dtype]
+    dy, x = draw(rows, out, dt, spread=0.5), draw(rows, d, dt, seed=2, spread=0.5)
+    inf = float("inf")
+    dy[7, 3], dy[9, 11], dy[20, 5], dy[60, 5], dy[2, 6], dy[3, 6], x[7, 8] = inf, -inf, inf, inf, inf, -inf, 0.0
+    ckpt = stored(ctx, x)
+    q = dk.dk_wgrad8(rows, d, out, code)
+    ctx.ensure_workspace(q)
+    dW, db = torch.empty((out, d), device="cuda"), torch.empty(out, device="cuda")
+    for scale in (1.0, -0.5):
+        dk.dk_linear_bwd_wgrad_ckpt8(ctx, q, dy, ckpt, scale, 0.0, dW, db)
+        want, want_b = scale * (dy.double().t() @ kept.decode(ckpt, rows, d)), scale * dy.double().sum(dim=0)
+        for got, w in ((dW, want), (db, want_b)):
+            bad = ~torch.isfinite(w)
+            assert torch.equal(~torch.isfinite(got), bad)
+            assert torch.equal(got[bad].double().nan_to_num(nan=7.0), w[bad].nan_to_num(nan=7.0))
