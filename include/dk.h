@@ -528,14 +528,16 @@ DK_API dk_status dk_orthogonalize(dk_ctx* ctx, const dk_ortho* q, const void* x,
  *   value = q*2^(b - 127)
  * with the least b from 1 to 248 under which no value of the block rounds beyond
  * 127; q is the nearest whole number, halves to even.  So a value is off by at most
- * half of 2^(b - 127), at most 1/127 of the block's largest magnitude (magnitudes
- * beyond 127.5*2^121, 3.39e38, become 127*2^121).  A block
- * with an infinity or a NaN (b = 255) comes back as NaN, all of it; what lies
- * below 2^-127 comes back as 0.
+ * half of 2^(b - 127), which is at most 1/127 of the block's largest magnitude where
+ * that is at least 63.75*2^-126 (7.5e-37), and 2^-127 where it is less: there digits
+ * are lost, and what is not above 2^-127 comes back as 0.  Magnitudes from 127.5*2^121
+ * (3.39e38) on become 127*2^121, off by less than one 2^(b - 127), less than
+ * 1/127 of themselves.  A block with an infinity or a NaN (b = 255) comes back as NaN,
+ * all of it.
  * Layout: q [rows][32*ceil(d/32)] (signed bytes, zeros behind d), then
  * b [rows][ceil(d/32)].  The calls that write a checkpoint write all of it. */
 typedef struct {
-  int64_t rows;       /* 0: nothing to do                                         */
+  int64_t rows;       /* 0: nothing to do; rows times padded d at most 10^12      */
   int32_t d;          /* values of a row, 1 .. 2^20                               */
   int32_t dtype;      /* of the tensor that is stored or loaded                   */
 } dk_ckpt8;
@@ -568,11 +570,12 @@ DK_API dk_status dk_group_norm_bwd_ckpt8(dk_ctx* ctx, const dk_norm* q, const vo
  * to 2^-17 of the output's largest magnitude, an absolute error of 2^-39 of it
  * below), and the checkpoint's values under one power of two of all of it, exact
  * for blocks whose b lies within 32 of the largest, with an absolute error below
- * 2^-39 of the tensor's largest value for those further down.  Needs the
- * workspace. */
+ * 2^-39 of the tensor's largest value for those further down.  db is a sum in fp32
+ * of dy as it is, of either type, infinite where it leaves fp32's range before
+ * `scale`.  Infinities and NaN in dy are those of the formula.  Needs the workspace. */
 typedef struct {
-  int64_t rows;       /* 0: dW and db become keep times themselves                */
-  int32_t d, out;     /* features of x and of dy                                  */
+  int64_t rows;       /* 0: dW and db become keep times themselves; at most 2^24  */
+  int32_t d, out;     /* features of x and of dy, 1 .. 2^20 each                  */
   int32_t dtype;      /* of dy                                                    */
 } dk_wgrad8;
 
@@ -590,8 +593,8 @@ DK_API dk_status dk_linear_bwd_wgrad_ckpt8(dk_ctx* ctx, const dk_wgrad8* q, cons
  * formed from it before that. */
 enum { DK_BLOCK_RMS = 0, DK_BLOCK_LAYER = 1 };
 typedef struct {
-  int64_t rows;          /* tokens, pixels, at most 2^30 (0: nothing to do; gradients of parameters
-                            are zero)                                                */
+  int64_t rows;          /* tokens, pixels, at most 2^30, rows*d at most 10^12 (0: nothing to do, gate
+                            has no rows; gradients of the other parameters are zero) */
   int32_t d;             /* features, 1 .. 16384                                     */
   int64_t rows_per_gate; /* consecutive rows that share a row of gate (>= 1)         */
   int32_t kind;          /* DK_BLOCK_RMS | DK_BLOCK_LAYER                            */

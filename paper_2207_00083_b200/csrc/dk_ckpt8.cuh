@@ -2,11 +2,12 @@
 // for each 32 consecutive values of a row,
 //   value = q*2^(b - 127),  |q| <= 127,
 // the rows of q padded with zeros to whole blocks, then the bytes b.  The power of two is the least under which no value
-// of the block rounds beyond 127, so a value is off by at most half a step, at most 1/127 of the block's largest magnitude.
+// of the block rounds beyond 127, so a value is off by at most half a step, at most 1/127 of the block's largest magnitude (but
+// of blocks below 63.75*2^-126, whose step is the least there is, 2^-126).
 // Powers of two, not max/127: x/2^k and q*2^k are exact, so what a value becomes
 // does not depend on how the division is done, and q*2^k is a bf16 number, which the tensor cores take without another
-// rounding.  The largest b is 248: the few values beyond 127.5*2^121, which would round to 2^128, become 127*2^121 (a mask
-// of the type's largest magnitude among them).  b = 255: the block held an infinity or a NaN, and all its values are NaN.
+// rounding.  The largest b is 248: the few values from 127.5*2^121 on, which would round to 2^128, become 127*2^121, off by up to
+// a whole step (a mask of the type's largest magnitude among them).  b = 255: the block held an infinity or a NaN, and all its values are NaN.
 #pragma once
 
 #include <stdint.h>

@@ -83,3 +83,33 @@ def test_wgrad_infinities_as_in_the_formula(ctx, rows, d, out, dtype):
             bad = ~torch.isfinite(w)
             assert torch.equal(~torch.isfinite(got), bad)
             assert torch.equal(got[bad].double().nan_to_num(nan=7.0), w[bad].nan_to_num(nan=7.0))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_how_far_a_kept_value_is_off(ctx, dtype):
+    """Over all of fp32's range: half of the block's step; that is 1/127 of its largest magnitude from 63.75*2^-126 on; and one
+    step, 1/127 of themselves, for magnitudes beyond 127.5*2^121.  (fp32 subtraction of neighbours is exact; so is 64 bits'.)"""
+    code, dt = TYPES[dtype]
+    top = torch.arange(-149, 128, device="cuda").repeat_interleave(8)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.rand((len(top), 64), generator=g, device="cuda", dtype=torch.float64) * 2 - 1
+    x[:, ::32] = 1 + torch.rand((len(top), 2), generator=g, device="cuda", dtype=torch.float64)
+    x[::8, 0], x[1::8, 0], x[2::8, 0] = 2.0 - 2.0 ** -8, 127.5 / 64, 127.0 / 64
+    x = (x * kept.power(top)[:, None]).to(dt)
+    x = torch.where(torch.isfinite(x), x, torch.full_like(x, torch.finfo(dt).max))
+    rows, d = x.shape
+    ckpt = stored(ctx, x)
+    y = torch.empty_like(x)
+    dk.dk_ckpt8_load(ctx, dk.dk_ckpt8(rows, d, code), ckpt, y)
+    step = kept.power(kept.parts(ckpt, rows, d)[1].to(torch.int64) - 127).repeat_interleave(32, dim=1)
+    v, off = x.double(), (y.double() - x.double()).abs()
+    largest = v.abs().reshape(rows, -1, 32).amax(dim=2).repeat_interleave(32, dim=1)
+    far = v.abs() > 127.5 * 2.0 ** 121
+    assert bool(far.any()) == (dtype == "f32")             # (the largest bf16 number is 127.5*2^121)
+    assert bool((largest < 63.75 * 2.0 ** -126).any())
+    assert bool((off[~far] <= step[~far] / 2).all())
+    assert bool((off[far] < step[far]).all()) and bool((off[far] < v[far].abs() / 127).all())
+    ordinary = (largest >= 63.75 * 2.0 ** -126) & ~far
+    assert bool((off[ordinary] <= largest[ordinary] / 127).all())
+    small = largest < 63.75 * 2.0 ** -126
+    assert bool((off[small] <= 2.0 ** -127).all()) and not bool(y[v.abs() <= 2.0 ** -127].any())
