@@ -621,7 +621,9 @@ DK_API dk_status dk_block_norm_fwd(dk_ctx* ctx, const dk_block* q, const void* h
  *   du = rstd_u*(s - mean(s) - uhat*mean(s*uhat)),  s = scale*gate*post*D
  *   dpre = sum dn*hhat,  dshift = sum dn,  dpost = sum scale*D*gate*uhat,
  *   dgate = sum over the gate's rows of scale*D*post*uhat
- * (root mean square: without mean(q) and mean(s)).  Nullable: dh_out (zero) or dn
+ * (root mean square: without mean(q) and mean(s)).  A row whose mean*rstd leaves
+ * fp32's range while rstd is finite is one value, and its uhat or hhat are zero.
+ * Nullable: dh_out (zero) or dn
  * with pre and dpre; u with post, du and dpost; gate with dgate; dshift.  dh may be
  * dh_out.  Parameters' gradients are fp32 and overwritten.  Needs the workspace. */
 DK_API dk_status dk_block_norm_bwd(dk_ctx* ctx, const dk_block* q, const void* dh_out, const void* dn, const void* h,

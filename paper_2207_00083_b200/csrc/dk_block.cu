@@ -218,6 +218,14 @@ __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(const BlockArgs a)
   if (a.stats != nullptr && lane == 0) a.stats[row] = st;
 }
 
+// rstd as what brings deviations to normalised values.  mean*rstd beyond fp32's range is the mark of a row of one value (where
+// values differ it is below 2^24*sqrt(d)), whose normalised values are zero.  They are made so, because the kernels with values
+// in registers have zeros where a row has none, and (0 - mean)*rstd there is to be a number.
+__device__ __forceinline__ float normaliser(float mean, float rstd) {
+  const float inf = __int_as_float(0x7f800000);
+  return fabsf(mean * rstd) == inf && rstd < inf ? 0.f : rstd;
+}
+
 // One vector of h or u of the backward pass.
 template <int DT, int VEC, bool KEPT>
 __device__ __forceinline__ void load_kept(const void* x, const uint8_t* codes, const uint8_t* exps, long long row, int c,
@@ -245,14 +253,16 @@ __device__ __forceinline__ void load_cell(Cell<VEC>& e, const BlockArgs& a, long
     float post[VEC], g[VEC];
     load_param<VEC>(a.post, c, post);
     load_gate<VEC>(gate, c, g);
+    const float ru = normaliser(st.x, st.y);
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-      e.uh[k] = (e.uh[k] - st.x) * st.y;
+      e.uh[k] = (e.uh[k] - st.x) * ru;
       e.hh[k] = fmaf(a.keep, e.hh[k], a.scale * (g[k] * (e.uh[k] * post[k])));
     }
   }
+  const float rh = normaliser(st.z, st.w);
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) e.hh[k] = (e.hh[k] - st.z) * st.w;
+  for (int k = 0; k < VEC; ++k) e.hh[k] = (e.hh[k] - st.z) * rh;
 }
 
 // Wide rows, a CTA each: read again in each phase, sums over rows in shared memory ([3][d]: E, dpre, dshift).
@@ -1085,7 +1095,10 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
   float4 next = make_float4(0.f, 0.f, 0.f, 0.f);
   typename T::Bytes bytes_h = {}, bytes_u = {};
   auto fetch = [&](int row) {
-    if (row >= r1) return;
+    if (row >= r1) {
+      next = make_float4(0.f, 0.f, 0.f, 0.f);      // (of a row that a team does not have)
+      return;
+    }
     next = __ldg(a.stats + row);
     if constexpr (KEPT) {
       t.fetch_bytes(a.eh, row, a, bytes_h);
@@ -1127,9 +1140,10 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       else t.take(at + at_u, off, valid, uh);
       F2 f[P];
       t.take_own(factors, f);
+      const float ru = normaliser(st.x, st.y);
 #pragma unroll
       for (int k = 0; k < P; ++k) {
-        uh[k] = (uh[k] + f2(-st.x)) * f2(st.y);
+        uh[k] = (uh[k] + f2(-st.x)) * f2(ru);
         hh[k] = fma(f2(a.keep), hh[k], f[k] * uh[k]);
       }
     }
@@ -1139,9 +1153,10 @@ __global__ void __launch_bounds__(kBwdThreads<DT>) block_bwd_rows_kernel(const B
       F2 dn[P], pre[P], s0 = zero, s1 = zero;
       t.take(at + room, off, valid, dn);
       t.take_own(pres, pre);
+      const float rh = normaliser(st.z, st.w);
 #pragma unroll
       for (int k = 0; k < P; ++k) {
-        hh[k] = (hh[k] + f2(-st.z)) * f2(st.w);
+        hh[k] = (hh[k] + f2(-st.z)) * f2(rh);
         spre[k] = fma(dn[k], hh[k], spre[k]);
         const F2 q = dn[k] * pre[k];
         s0 = s0 + q;
