@@ -6,10 +6,14 @@
 //   E = scale*D*u^:  dgate = sum E*post over the gate's rows,  dpost = sum E*gate,  dpre = sum dn*h^,  dshift = sum dn
 // (root mean square: the means that are subtracted are zero, and rstd = 1/sqrt(mean(x^2) + eps)).
 //
-// A row is a team's: 4 to 32 lanes, or a CTA; a thread has sixteen of its values in registers, so a row is read once.  A team
+// A row is a team's: 4 to 32 lanes, or a CTA; a thread has sixteen (fp32: eight) of its values in registers, so a row is read
+// once.  A team
 // takes consecutive rows; backward it keeps the sums over rows of its columns in registers, and the rows of one gate are
 // never split unevenly, so a gate's sums are either one team's, written at once, or of a fixed number of teams, joined in
-// order by block_sums_kernel.  Rows above 8192 values have kernels of their own.
+// order by block_sums_kernel.  Rows that a CTA's registers or shared memory do not hold have kernels of their own, which read a
+// row three times backward: from 8193 bf16 and 6145 fp32 values forward, from 4609 fp32 backward, and bf16 backward from 8193, or
+// where several gates a team, shift's gradient and rows of no whole vectors ask for more shared memory, from 6377 on at the
+// earliest.
 #include "dk_ckpt8.cuh"
 #include "dk_internal.h"
 #include "dk_step.h"
@@ -19,7 +23,7 @@ namespace dk {
 namespace {
 
 constexpr int kMaxD = 16384;
-constexpr int kHeld = 8192;            // longest rows that are held in registers
+constexpr int kHeld = 8192;            // longest rows that are held in registers (bf16; fp32: 8 values a thread)
 // Values of a thread, and threads of a CTA at most (they share out the registers).
 template <int DT>
 constexpr int kValues = DT == DK_BF16 ? 16 : 8;

@@ -113,3 +113,25 @@ def test_how_far_a_kept_value_is_off(ctx, dtype):
     assert bool((off[ordinary] <= largest[ordinary] / 127).all())
     small = largest < 63.75 * 2.0 ** -126
     assert bool((off[small] <= 2.0 ** -127).all()) and not bool(y[v.abs() <= 2.0 ** -127].any())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d,out", [(64, 512, 256), (1024, 512, 384), (16384, 1024, 1024), (2047, 1001, 1502), (33000, 40, 24),
+                                        (256, 5000, 4096), (4000, 2560, 2560)])
+def test_wgrad_sums_of_one_sign(ctx, rows, d, out, dtype):
+    """Where the tensor pipe's truncation is a bias.  A promotion every 16 stages of 64 rows (fp32: 4 stages, each of two products)
+    is one rounding of 2^-24; each of the 4 instructions of a stage and product before it loses two units of 2^-23 at most of a
+    sum that grows to S; the compensation gives back 1.2 (fp32 2.4) times 2^-24 of it for each stage of a chunk; joins of slices,
+    undone powers of two and `scale` are 8 roundings more.  fp32: 2^-22 of dy's terms."""
+    code, dt = TYPES[dtype]
+    x, dy = stored(ctx, draw(rows, d, dt, spread=0.3).abs()), draw(rows, out, dt, seed=5, spread=0.3).abs()
+    q = dk.dk_wgrad8(rows, d, out, code)
+    ctx.ensure_workspace(q)
+    dW = torch.full((out, d), float("nan"), device="cuda")
+    dk.dk_linear_bwd_wgrad_ckpt8(ctx, q, dy, x, 1.0, 0.0, dW, None)
+    want = dy.double().t() @ kept.decode(x, rows, d)
+    stages, chunk, products = -(-rows // 64), 16 if dtype == "bf16" else 4, 1 if dtype == "bf16" else 2
+    units = 2 * 4 * products * min(chunk, stages) + 1.2 * products * min(chunk, stages) / 2 + (stages / chunk + 8) / 2
+    if dtype == "f32":
+        units += 2
+    assert bool(((dW.double() - want).abs() <= want * units * 2.0 ** -23).all())
