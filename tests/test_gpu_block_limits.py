@@ -34,3 +34,74 @@ def test_rows_of_one_large_value(ctx, rows, d, branch, dtype):
     for held in (False, True):
         for k, t in c.check_backward(ctx, held).items():
             assert t is None or bool(torch.isfinite(t).all()), (k, held)
+
+
+@pytest.mark.parametrize("rows,d,per,held", [(2200000, 1000, 2200000, True), (2200000, 1001, 7, False), (530000, 4096, 1024, True),
+                                             (140000, 16000, 140000, False)])
+def test_rows_past_32_bits_of_offset(ctx, rows, d, per, held):
+    """More than 2^31 values: the last rows come out as in a call of their own (a row's results are its own).  Sums over rows: of
+    ones, with parameters of ones, so that dshift counts the rows exactly; they are below 2^24."""
+    dt, tail = torch.bfloat16, 4 * 7 * 1024
+    q, few = (dk.dk_block(n, d, p, dk.DK_BLOCK_LAYER, dk.DK_BF16, 1e-5, KEEP, SCALE) for n, p in ((rows, per), (tail, min(per, tail))))
+    for p in (q, few):
+        ctx.ensure_workspace(p)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    some = [torch.randn((tail, d), generator=g, device="cuda").to(dt) for _ in range(3)]
+    first = rows - tail
+    first -= first % per if per <= tail else 0                     # (the rows of a gate together)
+    h, u, dh_out = (torch.zeros((rows, d), dtype=dt, device="cuda") for _ in range(3))
+    for big, small in zip((h, u, dh_out), some):
+        big[first:first + tail] = small
+    dn, vec = torch.ones((rows, d), dtype=dt, device="cuda"), torch.ones(d, device="cuda")
+
+    def both(q, rows, h, u, dh_out, dn):
+        gate = torch.ones((-(-rows // q.rows_per_gate), d), device="cuda")
+        new = lambda: torch.empty((rows, d), dtype=dt, device="cuda")      # noqa: E731
+        h_out, n, dh, du, stats = new(), new(), new(), new(), torch.empty((rows, 4), device="cuda")
+        size = dk.dk_ckpt8_bytes(dk.dk_ckpt8(rows, d, dk.DK_BF16))
+        kh, ku = (torch.empty(size, dtype=torch.uint8, device="cuda") if held else None for _ in range(2))
+        dgate, dpost, dpre, dshift = torch.empty_like(gate), torch.empty_like(vec), torch.empty_like(vec), torch.empty_like(vec)
+        dk.dk_block_norm_fwd(ctx, q, h, u, gate, vec, vec, vec, h_out, n, stats, kh, ku)
+        back, a, b = (dk.dk_block_norm_bwd_ckpt8, kh, ku) if held else (dk.dk_block_norm_bwd, h, u)
+        back(ctx, q, dh_out, dn, a, b, gate, vec, vec, stats, dh, du, dgate, dpost, dpre, dshift)
+        assert bool((dshift == rows).all())
+        return h_out, n, stats, dh, du
+
+    want = both(few, tail, *some, dn[:tail])
+    got = both(q, rows, h, u, dh_out, dn)
+    for a, b in zip(got, want):
+        assert torch.equal(a[first:first + tail], b)
+
+
+def shifted(t):
+    """The same tensor 16 bytes behind a 512-byte boundary."""
+    if t is None:
+        return None
+    skip = 16 // t.element_size()
+    return torch.empty(t.numel() + skip, dtype=t.dtype, device="cuda")[skip:].view(t.shape).copy_(t)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d,gate,per", [(300, 96, "rows", 7), (300, 1030, "channel", 1), (77, 4096, "rows", 1), (301, 1001, "none", 1),
+                                             (40, 9000, "rows", 3), (5, 33, "rows", 2)])
+def test_tensors_on_any_16_bytes(ctx, rows, d, gate, per, dtype):
+    """The same bits wherever the tensors begin."""
+    c = Case(rows, d, "layer", gate, per, dtype, shift=True)
+    ctx.ensure_workspace(c.q)
+    c.forward(ctx)
+    want = [c.h_out, c.n, c.stats, c.kh, c.ku]
+    back = [c.backward(ctx, held) for held in (False, True)]
+    for k in ("h", "u", "gate", "post", "pre", "shift", "dh_out", "dn"):
+        setattr(c, k, shifted(getattr(c, k)))
+    got = [shifted(t) for t in want]
+    for t in got:
+        t.zero_()
+    dk.dk_block_norm_fwd(ctx, c.q, c.h, c.u, c.gate, c.post, c.pre, c.shift, *got)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for held, w in zip((False, True), back):
+        out = {k: shifted(t) for k, t in w.items()}
+        call, h, u = (dk.dk_block_norm_bwd_ckpt8, got[3], got[4]) if held else (dk.dk_block_norm_bwd, c.h, c.u)
+        call(ctx, c.q, c.dh_out, c.dn, h, u, c.gate, c.post, c.pre, got[2], *[None if t is None else t.zero_() for t in out.values()])
+        for k in w:
+            assert w[k] is None or torch.equal(out[k], w[k]), k

@@ -135,3 +135,56 @@ def test_wgrad_sums_of_one_sign(ctx, rows, d, out, dtype):
     if dtype == "f32":
         units += 2
     assert bool(((dW.double() - want).abs() <= want * units * 2.0 ** -23).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_wgrad_rows_past_32_bits_of_offset(ctx, dtype):
+    """More than 2^31 values of dy and codes of x: sums of small whole numbers, exact but for the compensation (2^-19 of a chunk's
+    sum); the rows are zeros but for the first and the last."""
+    code, dt = TYPES[dtype]
+    rows, d, out, some = 4300000, 500, 504, 1000
+    g = torch.Generator(device="cuda").manual_seed(2)
+    ends = [torch.randint(-9, 10, (2 * some, n), generator=g, device="cuda").to(dt) for n in (d, out)]
+    x, dy = torch.zeros((rows, d), dtype=dt, device="cuda"), torch.zeros((rows, out), dtype=dt, device="cuda")
+    for big, small in zip((x, dy), ends):
+        big[:some], big[-some:] = small[:some], small[some:]
+    ckpt = stored(ctx, x)
+    del x
+    q = dk.dk_wgrad8(rows, d, out, code)
+    ctx.ensure_workspace(q)
+    dW, db = torch.empty((out, d), device="cuda"), torch.empty(out, device="cuda")
+    dk.dk_linear_bwd_wgrad_ckpt8(ctx, q, dy, ckpt, 1.0, 0.0, dW, db)
+    xv, dyv = ends[0].double(), ends[1].double()
+    size = dyv.abs().t() @ xv.abs()
+    assert bool(((dW.double() - dyv.t() @ xv).abs() <= size * 2.0 ** -18).all())
+    assert torch.equal(db.double(), dyv.sum(dim=0))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d,out", [(64, 512, 1000), (300, 333, 77), (256, 1056, 8192), (33000, 40, 24), (2000, 1000, 3001)])
+def test_wgrad_tensors_on_any_16_bytes(ctx, rows, d, out, dtype):
+    code, dt = TYPES[dtype]
+
+    def shifted(t):
+        skip = 16 // t.element_size()
+        return torch.empty(t.numel() + skip, dtype=t.dtype, device="cuda")[skip:].view(t.shape).copy_(t)
+
+    x, dy = draw(rows, d, dt, spread=0.5), draw(rows, out, dt, seed=5, spread=0.5)
+    ckpt, q, k = stored(ctx, x), dk.dk_wgrad8(rows, d, out, code), dk.dk_ckpt8(rows, d, code)
+    ctx.ensure_workspace(q)
+    kept_there = shifted(ckpt).zero_()
+    dk.dk_ckpt8_store(ctx, k, shifted(x), kept_there)
+    assert torch.equal(kept_there, ckpt)
+    back = [torch.empty_like(x), shifted(x).zero_()]
+    for c, t in zip((ckpt, kept_there), back):
+        dk.dk_ckpt8_load(ctx, k, c, t)
+    assert torch.equal(*back)
+    res = []
+    for c, y in ((ckpt, dy), (kept_there, shifted(dy))):
+        dW, db = torch.ones((out, d), device="cuda"), torch.ones(out, device="cuda")
+        if res:
+            dW, db = shifted(dW), shifted(db)
+        for keep in (0.0, 0.5):
+            dk.dk_linear_bwd_wgrad_ckpt8(ctx, q, y, c, 1.0, keep, dW, db)
+        res.append((dW, db))
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
