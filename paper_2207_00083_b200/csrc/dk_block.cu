@@ -7,10 +7,9 @@
 // (root mean square: the means that are subtracted are zero, and rstd = 1/sqrt(mean(x^2) + eps)).
 //
 // A row is a team's: 4 to 32 lanes, or a CTA; a thread has sixteen (fp32: eight) of its values in registers, so a row is read
-// once.  A team
-// takes consecutive rows; backward it keeps the sums over rows of its columns in registers, and the rows of one gate are
-// never split unevenly, so a gate's sums are either one team's, written at once, or of a fixed number of teams, joined in
-// order by block_sums_kernel.  Rows that a CTA's registers or shared memory do not hold have kernels of their own, which read a
+// once.  A team takes consecutive rows; backward it keeps the sums over rows of its columns in registers, and the rows of one
+// gate are never split unevenly, so a gate's sums are either one team's, written at once, or of a fixed number of teams,
+// joined in order by block_sums_kernel.  Rows that a CTA's registers or shared memory do not hold have kernels of their own, which read a
 // row three times backward: from 8193 bf16 and 6145 fp32 values forward, from 4609 fp32 backward, and bf16 backward from 8193, or
 // where several gates a team, shift's gradient and rows of no whole vectors ask for more shared memory, from 6377 on at the
 // earliest.
@@ -420,8 +419,9 @@ __global__ void __launch_bounds__(1024) block_bwd_wide_kernel(const BlockArgs a)
 // Teams of fewer lanes copy with cp.async, the vectors that they read themselves or 16-byte pieces.  The copies issued at a
 // row's start go where the row before lay, whose last reading is before that row's last barrier.
 //
-// What bounds it besides HBM is instructions: bf16 rows from checkpoints leave some 55 per value at the rate of HBM.  So a
-// thread has sixteen values, over which a row's sums, its copies and its scalars are shared out (eight: 86 and 91 per
+// What bounds it besides HBM is instructions: bf16 rows from checkpoints leave some 55 per value at the rate of HBM and four a
+// cycle; there are 37 forward and 54 backward, of which 15 warps an SM issue 2.0 and 2.3 a cycle (16384 x 4096: 134 and 181
+// us).  So a thread has sixteen values, over which a row's sums, its copies and its scalars are shared out (eight: 86 and 91 per
 // value forward and backward, 261 and 272 us for 16384 x 4096; 512 threads a row), and works on pairs, two to an
 // instruction.
 // ---------------------------------------------------------------------------
@@ -469,7 +469,7 @@ __device__ __forceinline__ float inverse_root(float x) {
 // for the whole row).  RAGGED, bf16: a vector is read as two of the stage's and shifted, and written to shared memory first,
 // from where the team stores the row in whole aligned vectors (and its two ends by single values).  PAIRS and SINGLES, fp32:
 // two values to an access where rows have an even number, else one.  Both sides: 16384 x 1001 bf16 takes 66 us forward and
-// 113 backward as RAGGED, 130 and 143 as SINGLES; 4095 x 2050 fp32 62 and 82, but 47 and 61 as PAIRS (a shift serves four
+// 115 backward as RAGGED, 130 and 143 as SINGLES; 4095 x 2050 fp32 62 and 82, but 47 and 60 as PAIRS (a shift serves four
 // values there, not eight).
 enum { FULL = 0, WHOLE = 1, RAGGED = 2, PAIRS = 3, SINGLES = 4 };
 template <int DT, int WAY>
