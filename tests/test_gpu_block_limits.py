@@ -105,3 +105,25 @@ def test_tensors_on_any_16_bytes(ctx, rows, d, gate, per, dtype):
         call(ctx, c.q, c.dh_out, c.dn, h, u, c.gate, c.post, c.pre, got[2], *[None if t is None else t.zero_() for t in out.values()])
         for k in w:
             assert w[k] is None or torch.equal(out[k], w[k]), k
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("branch", [True, False])
+@pytest.mark.parametrize("rows,d", [(700, 35), (300, 38), (500, 1001), (400, 2050), (300, 4096), (40, 5120), (40, 7001), (20, 9000), (7, 16384)])
+def test_in_place_whatever_the_rows(ctx, rows, d, branch, dtype):
+    """h_out over h and dh over dh_out: the bits of a call with tensors of their own."""
+    c = Case(rows, d, "layer", "rows", 3, dtype, branch=branch)
+    ctx.ensure_workspace(c.q)
+    c.forward(ctx)
+    h, n = c.h.clone(), torch.empty_like(c.n)
+    if branch:
+        dk.dk_block_norm_fwd(ctx, c.q, h, c.u, c.gate, c.post, c.pre, c.shift, h, n, None)
+        assert torch.equal(h, c.h_out) and torch.equal(n, c.n)
+    for held in (False, True):
+        want = c.backward(ctx, held)
+        got = {k: None if t is None else torch.empty_like(t) for k, t in want.items()}
+        got["dh"] = c.dh_out.clone()
+        call, h, u = (dk.dk_block_norm_bwd_ckpt8, c.kh, c.ku) if held else (dk.dk_block_norm_bwd, c.h, c.u)
+        call(ctx, c.q, got["dh"], c.dn, h, u, c.gate, c.post, c.pre, c.stats, *got.values())
+        for k in want:
+            assert want[k] is None or torch.equal(got[k], want[k]), k
